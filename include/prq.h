@@ -421,6 +421,138 @@ int prq_search_alpha(const uint16_t* W_bf16, int32_t N, int32_t K,
                      int32_t scale_mode, int32_t flags,
                      double* nrmse, int32_t* best, hipStream_t stream);
 
+/* ------------------------------------------------------------------------
+ * The attention block around the linears: per-head norm, rotation and cache
+ * append of the projections' outputs; attention over the paged cache; low-rank
+ * adapters beside a projection.  Inference only.  Asynchronous like the other
+ * device calls; tables on the device (offsets, page tables, lengths, slots,
+ * positions, ranks) are checked by the kernels themselves: an entry that names
+ * something outside the buffers is passed over as each call says, never read or
+ * written through.
+ *
+ * The paged cache: K and V, each [num_pages][Hk][page_size][D] bf16, pages
+ * page_stride elements apart (>= Hk * page_size * D, a multiple of 8; one
+ * allocation may hold both, or several layers).  page_size is a power of two in
+ * [16, 4096].  Token t of a request lies on page page_table[request][t /
+ * page_size] at offset t % page_size; a slot is page * page_size + offset.
+ * D is 64, 128 or 256; Hq is a multiple of Hk, at most 1024.
+ */
+
+/* Element types of the calls that take more than one. */
+enum {
+  PRQ_F32 = 0,
+  PRQ_BF16 = 1
+};
+
+/*
+ * prq_qk_norm_rope -- queries, keys and values from the projections to the
+ * attention in one pass.  Row i, in float32 throughout, each stored value
+ * rounded once to bf16:
+ *   every query head, and every key head: x / sqrt(mean(x^2) + eps) * weight
+ *     over its D elements (weight NULL: x as it is), then the first rotary_dim
+ *     dims rotated: with (c_j, s_j) = table[positions[i]][j],
+ *       (a, b) -> (a c_j - b s_j, b c_j + a s_j)
+ *     for (a, b) = dims (j, j + rotary_dim / 2), or (2j, 2j + 1) where
+ *     interleaved; the dims from rotary_dim on pass;
+ *   q_out[i] = the query heads; K and V at slots[i] = the key heads and the value
+ *     heads (values neither normed nor rotated).
+ *
+ *   q, k, v    [M] rows, ld_q / ld_k / ld_v elements apart, of Hq, Hk and Hk
+ *              heads of D, in_type PRQ_F32 (a GEMM's Y) or PRQ_BF16; 16-byte
+ *              aligned rows
+ *   q_weight, k_weight  [D] of weight_type, or NULL
+ *   positions  [M] int32; a position outside [0, table_rows) turns the rotated
+ *              dims of its row to NaN.  Not read where rotary_dim is 0
+ *   table      [table_rows][rotary_dim / 2][2] float32 cosine, sine
+ *   rotary_dim multiple of 8, 0 .. D
+ *   q_out      [M][Hq][D] bf16
+ *   slots      [M] int64; a row whose slot is outside [0, num_pages * page_size)
+ *              (-1: a padding row) is not written to the cache.  Two rows of one
+ *              call on the same slot leave either's values
+ * PRQ_EINVAL, PRQ_EALIGN (also rotary_dim), PRQ_EUNSUPPORTED (D, page_size, Hq or
+ * M beyond the limits), PRQ_EDEVICE.  M == 0 is a no-op.
+ */
+int prq_qk_norm_rope(const void* q, int64_t ld_q, const void* k, int64_t ld_k, const void* v, int64_t ld_v,
+                     int32_t in_type, int32_t M, int32_t Hq, int32_t Hk, int32_t D, const void* q_weight,
+                     const void* k_weight, int32_t weight_type, float eps, const int32_t* positions,
+                     const float* table, int32_t table_rows, int32_t rotary_dim, int32_t interleaved, void* q_out,
+                     void* K_cache, void* V_cache, int64_t page_stride, int32_t num_pages, int32_t page_size,
+                     const int64_t* slots, hipStream_t stream);
+
+/*
+ * prq_tree_attention -- attention of B requests' rows over their pages.  Request
+ * b has rows q_offsets[b] .. q_offsets[b + 1] - 1 (n of them: one token, a tree
+ * of drafted tokens, a chunk of a prompt), whose keys and values are in the cache
+ * already, as its tokens cached_lens[b] .. + n - 1.  Row i of it sees its cached
+ * tokens before them, and of its n own tokens j:
+ *   tree_mask given:  those with tree_mask[row][j] != 0 (row counted over all
+ *                     requests; columns from mask_wide on are unseen);
+ *   tree_mask NULL:   j <= i.
+ * For query head h and kv head h / (Hq / Hk):
+ *   s_j = scale * q . k_j,  out = sum_j softmax(s)_j v_j over the seen j,
+ *   lse = log sum_j exp(s_j)
+ * out = 0 and lse = -inf for a row that sees nothing.  What a row does not see
+ * does not reach it, whatever it holds (NaN included).
+ *
+ *   q          [M] rows of Hq heads of D bf16, ld_q elements apart (multiple of 8)
+ *   page_table [B] rows of pages_wide int32, ld_pages apart; tokens beyond
+ *              pages_wide * page_size, and tokens on a page outside the pool, are
+ *              not seen
+ *   cached_lens [B], q_offsets [B + 1] int32; rows of no request are not computed
+ *   max_kv_len the most tokens (cached and own) a request is expected to have: it
+ *              sizes the split over workgroups.  A longer request is computed too,
+ *              more slowly
+ *   tree_mask  [M] rows of mask_wide bytes, ld_mask apart, or NULL
+ *   out        [M][Hq][D] bf16
+ *   lse        [M][Hq] float32, or NULL
+ *   workspace  prq_tree_attention_workspace_bytes(...) bytes, 16-byte aligned;
+ *              need not be cleared, and holds nothing between calls
+ * Scores, statistics and sums are float32; probabilities are rounded to bf16 as
+ * they enter the second product.  Bitwise reproducible.  PRQ_EINVAL, PRQ_EALIGN,
+ * PRQ_EUNSUPPORTED (D, page_size; B > 4096; M * Hq > 2^25; pages_wide * page_size >
+ * 2^30), PRQ_EWORKSPACE, PRQ_EDEVICE.  M == 0 or B == 0 is a no-op.
+ */
+size_t prq_tree_attention_workspace_bytes(int32_t M, int32_t B, int32_t Hq, int32_t Hk, int32_t D,
+                                          int32_t max_kv_len);
+int prq_tree_attention(const void* q, int64_t ld_q, int32_t M, int32_t Hq, int32_t Hk, int32_t D,
+                       const void* K_cache, const void* V_cache, int64_t page_stride, int32_t num_pages,
+                       int32_t page_size, const int32_t* page_table, int64_t ld_pages, int32_t pages_wide,
+                       const int32_t* cached_lens, const int32_t* q_offsets, int32_t B, int32_t max_kv_len,
+                       float scale, const uint8_t* tree_mask, int64_t ld_mask, int32_t mask_wide, void* out,
+                       float* lse, void* workspace, size_t workspace_bytes, hipStream_t stream);
+
+/*
+ * prq_lora -- low-rank adapters of many requests beside a shared projection:
+ *   out[i] = Y[i] + scales[a] * B_a (A_a x[i])
+ * for the rows i of segment s = [segment_offsets[s], segment_offsets[s + 1]) and
+ * a = segment_adapter[s]; out[i] = Y[i] where a is outside [0, adapters) (-1:
+ * none).  Rows of no segment are left alone.
+ *
+ *   x_bf16     [M] rows of K bf16, ld_x apart (multiple of 8; the projection's own
+ *              input, unquantized); K % 8 == 0
+ *   A          [rank_rows][K] bf16: adapter a's [rank, K] from row rank_offsets[a]
+ *   B          bf16: adapter a's [N, rank] from element N * rank_offsets[a]
+ *   rank_offsets [adapters + 1] int32, multiples of 8 (pad a rank with zero rows
+ *              of A and columns of B); an adapter whose offsets are not, or reach
+ *              beyond rank_rows, or hold more than max_rank, counts as none
+ *   max_rank   multiple of 8, at most 256
+ *   scales     [adapters] float32
+ *   Y, out     [M] rows of N float32, ld_y / ld_out apart (multiples of 4); out
+ *              may be Y (with ld_out == ld_y), and must not overlap it otherwise.
+ *              N % 16 == 0
+ *   workspace  prq_lora_workspace_bytes(...) bytes, 16-byte aligned; need not be
+ *              cleared, and holds nothing between calls
+ * A_a x stays float32.  Bitwise reproducible.  PRQ_EINVAL, PRQ_EALIGN,
+ * PRQ_EUNSUPPORTED (max_rank, segments > 4096, M > 2^19), PRQ_EWORKSPACE,
+ * PRQ_EDEVICE.  M == 0 or segments == 0 is a no-op.
+ */
+size_t prq_lora_workspace_bytes(int32_t M, int32_t segments, int32_t N, int32_t K, int32_t max_rank);
+int prq_lora(const void* x_bf16, int64_t ld_x, int32_t M, int32_t K, const void* A, const void* B,
+             const int32_t* rank_offsets, const float* scales, int32_t adapters, int32_t rank_rows,
+             int32_t max_rank, const int32_t* segment_offsets, const int32_t* segment_adapter, int32_t segments,
+             int32_t N, const float* Y, int64_t ld_y, float* out, int64_t ld_out, void* workspace,
+             size_t workspace_bytes, hipStream_t stream);
+
 #ifdef __cplusplus
 }
 #endif

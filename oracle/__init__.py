@@ -15,9 +15,11 @@ precision, written from the paper's definitions:
   Sec. "Activation tail construction"), the augmented GEMM of Eq. 3, its
   grouped (MoE expert) form, the unquantized identity of Eq. 1 and the
   normalized reconstruction error used for alpha selection and the ablation.
+* ``oracle.attention`` -- the attention block around the linears (not in the paper):
+  per-head norm and rotation, attention over a paged cache, low-rank adapters.
 
 It shares no code, header, table or helper with the HIP path.  Inputs come from
 the seeded generators in ``paper_2609_22106_amd.inputs`` (random draws only, no
 arithmetic of the method).
 """
-from . import mxfp4, prquant  # noqa: F401
+from . import attention, mxfp4, prquant  # noqa: F401

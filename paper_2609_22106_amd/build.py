@@ -36,8 +36,9 @@ HOST_FLAGS = ["-O2", "-std=c++17", "-fPIC", "-ffp-contract=off", "-Wall",
 
 DEVICE_SOURCES = ["act_quant.hip", "swiglu_quant.hip", "prepare_device.hip", "pack.hip", "gemm_tile.hip", "gemm_stream.hip", "gemm_decode.hip",
                   "gemm_streamk.hip",
+                  "norm_rope.hip", "tree_attention.hip", "lora.hip",
                   "evaluate.hip", "noalloc.hip"]
-HOST_SOURCES = ["prepare.cpp", "abi.cpp"]
+HOST_SOURCES = ["prepare.cpp", "abi.cpp", "abi_attention.cpp"]
 PROBE_SOURCES = ["probe.hip"]
 
 

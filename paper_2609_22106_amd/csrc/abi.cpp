@@ -70,6 +70,13 @@ int check_gemm_common(const uint8_t* Aq, const uint8_t* Asc, int32_t M, const ui
 
 }  // namespace
 
+int prq::current_device_cus(int* num_cus) {
+  DeviceInfo dev;
+  const int st = current_device(&dev);
+  *num_cus = dev.num_cus;
+  return st;
+}
+
 extern "C" {
 
 const char* prq_strerror(int status) {

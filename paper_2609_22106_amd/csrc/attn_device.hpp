@@ -1,0 +1,87 @@
+// Device-side bf16 helpers of the attention block's kernels (norm_rope.hip,
+// tree_attention.hip, lora.hip) for gfx950.
+#pragma once
+
+#include <hip/hip_runtime.h>
+
+#include <cstdint>
+
+namespace prq {
+namespace dev {
+
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef uint32_t u32x4v __attribute__((ext_vector_type(4)));
+
+// bf16 pair (low half first) of two floats, round to nearest even.
+__device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
+  const f32x2 v = {lo, hi};
+  return __builtin_bit_cast(uint32_t, __builtin_convertvector(v, bf16x2));
+}
+
+__device__ __forceinline__ float bf16_lo(uint32_t w) { return __uint_as_float(w << 16); }
+__device__ __forceinline__ float bf16_hi(uint32_t w) { return __uint_as_float(w & 0xFFFF0000u); }
+__device__ __forceinline__ float bf16_float(uint16_t b) { return __uint_as_float(static_cast<uint32_t>(b) << 16); }
+
+// D (16 x 16, float32) += A (16 x 32) B (32 x 16), bf16.  Lane l: A row l % 16 and
+// B column l % 16, both at k = 8 (l / 16) .. + 7; D column l % 16, rows
+// 4 (l / 16) .. + 3.
+__device__ __forceinline__ f32x4 mfma_bf16(u32x4v a, u32x4v b, f32x4 c) {
+  return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c,
+                                                 0, 0, 0);
+}
+
+// Segment tables on the device: segment s holds rows [offsets[s], offsets[s + 1]),
+// cut into tiles of `rows` times `per_row` units each.  find_tile: the segment that
+// holds tile `t` (counted over all segments) and the tile's number in it; -1 past
+// the last.  Offsets outside [0, M] or descending are clamped to empty segments, so
+// no table makes a kernel leave its buffers.  Every lane of the wave calls it.
+struct TileAt {
+  int segment, tile, first, rows;
+};
+
+__device__ __forceinline__ TileAt find_tile(const int32_t* __restrict__ offsets, int segments, int M, int t,
+                                            int per_row, int per_tile) {
+  const int lane = static_cast<int>(threadIdx.x) & 63;
+  int before = 0;
+  for (int base = 0; base < segments; base += 64) {
+    const int s = base + lane;
+    int lo = 0, n = 0, tiles = 0;
+    if (s < segments) {
+      lo = min(max(offsets[s], 0), M);
+      n = max(min(max(offsets[s + 1], 0), M) - lo, 0);
+      tiles = (n * per_row + per_tile - 1) / per_tile;
+    }
+    int sum = tiles;
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+      const int x = __shfl_up(sum, d);
+      if (lane >= d) sum += x;
+    }
+    const uint64_t past = __ballot(before + sum > t);
+    if (past) {
+      const int at = __builtin_ctzll(past);
+      TileAt r;
+      r.segment = base + at;
+      r.tile = t - before - (__builtin_amdgcn_readlane(sum, at) - __builtin_amdgcn_readlane(tiles, at));
+      r.first = __builtin_amdgcn_readlane(lo, at);
+      r.rows = __builtin_amdgcn_readlane(n, at);
+      return r;
+    }
+    before += __builtin_amdgcn_readlane(sum, 63);
+  }
+  return {-1, 0, 0, 0};
+}
+
+}  // namespace dev
+
+// The most tiles that find_tile counts for `rows` rows in `segments` segments.
+inline int64_t most_tiles(int64_t rows, int64_t segments, int64_t per_row, int64_t per_tile) {
+  const int64_t used = segments < rows ? segments : rows;
+  return (rows * per_row + (per_tile - 1) * used) / per_tile;
+}
+
+}  // namespace prq

@@ -195,4 +195,50 @@ hipError_t launch_gemm_decode(const uint8_t* Aq, const uint8_t* Asc, int M,
                               const uint8_t* Wps, int N, int K_aug, float* Y,
                               const DecodeConfig& cfg, hipStream_t stream, bool packed_a = false);
 
+// abi.cpp: the current device's compute units (cached per device); a status as the
+// ABI returns it, PRQ_EUNSUPPORTED where the device is not gfx950.
+int current_device_cus(int* num_cus);
+
+// The attention block.  Its cache: K and V [num_pages][Hk][page size][D] bf16, pages
+// page_stride elements apart, the page size 2^page_shift.
+struct PagedCache {
+  uint16_t *K = nullptr, *V = nullptr;
+  int64_t page_stride = 0;
+  int num_pages = 0, page_shift = 0;
+};
+
+// norm_rope.hip.
+hipError_t launch_qk_norm_rope(const void* q, int64_t ld_q, const void* k, int64_t ld_k, const void* v, int64_t ld_v,
+                               bool in_bf16, int M, int Hq, int Hk, int D, const void* wq, const void* wk,
+                               bool w_bf16, float eps, const int32_t* positions, const float* table, int table_rows,
+                               int rot, bool interleaved, uint16_t* q_out, const PagedCache& cache,
+                               const int64_t* slots, int num_cus, hipStream_t stream);
+
+// tree_attention.hip.  Query columns a workgroup (16, 32 or 64), their tiles over all
+// requests and key ranges a tile, and the blocks of the launch.
+struct TreePlan {
+  int tile_cols = 16, splits = 1, split_len = 0;
+  int64_t tiles = 0, blocks = 0;
+};
+TreePlan plan_tree_attention(int M, int B, int Hq, int Hk, int D, int max_kv_len, int num_cus);
+size_t tree_workspace_bytes(const TreePlan& c, int M, int Hq, int D);
+hipError_t launch_tree_attention(const TreePlan& c, const uint16_t* q, int64_t ld_q, int M, int Hq, int Hk, int D,
+                                 const PagedCache& cache, const int32_t* pages, int64_t ld_pages, int max_keys,
+                                 const int32_t* cached, const int32_t* offsets, int B, float scale,
+                                 const uint8_t* mask, int64_t ld_mask, int mask_wide, uint16_t* out, float* lse,
+                                 void* workspace, hipStream_t stream);
+
+// lora.hip.  16-row tiles and ranges of K of the first product; 16 * row_tiles-row
+// tiles and columns a workgroup of the second.
+struct LoraPlan {
+  int64_t tiles = 0, up_tiles = 0;
+  int splits = 1, k_per = 0, row_tiles = 1, n_per = 0;
+};
+LoraPlan plan_lora(int M, int segments, int N, int K, int max_rank, int num_cus);
+size_t lora_workspace_bytes(const LoraPlan& c, int M, int max_rank);
+hipError_t launch_lora(const LoraPlan& c, const uint16_t* x, int64_t ld_x, int M, int K, const uint16_t* A,
+                       const uint16_t* B, const int32_t* rank_offsets, const float* scales, int adapters,
+                       int rank_rows, int max_rank, const int32_t* offsets, const int32_t* of, int segments, int N, const float* Y,
+                       int64_t ld_y, float* out, int64_t ld_out, void* workspace, hipStream_t stream);
+
 }  // namespace prq

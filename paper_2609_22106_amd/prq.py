@@ -83,6 +83,20 @@ _ggemm = _decl("prq_grouped_gemm", ctypes.c_int,
 _ggemm_ex = _decl("prq_grouped_gemm_ex", ctypes.c_int,
                   [_p, _p, _p, _i32, _i32, _p, _p, _i32, _i32, _p, _p, _sz, _i32, _p])
 
+PRQ_F32, PRQ_BF16 = 0, 1
+_f32 = ctypes.c_float
+_qk_norm_rope = _decl("prq_qk_norm_rope", ctypes.c_int,
+                      [_p, _i64, _p, _i64, _p, _i64, _i32, _i32, _i32, _i32, _i32, _p, _p, _i32, _f32, _p, _p, _i32,
+                       _i32, _i32, _p, _p, _p, _i64, _i32, _i32, _p, _p])
+_tree_ws = _decl("prq_tree_attention_workspace_bytes", _sz, [_i32, _i32, _i32, _i32, _i32, _i32])
+_tree = _decl("prq_tree_attention", ctypes.c_int,
+              [_p, _i64, _i32, _i32, _i32, _i32, _p, _p, _i64, _i32, _i32, _p, _i64, _i32, _p, _p, _i32, _i32, _f32,
+               _p, _i64, _i32, _p, _p, _p, _sz, _p])
+_lora_ws = _decl("prq_lora_workspace_bytes", _sz, [_i32, _i32, _i32, _i32, _i32])
+_lora = _decl("prq_lora", ctypes.c_int,
+              [_p, _i64, _i32, _i32, _p, _p, _p, _p, _i32, _i32, _i32, _p, _p, _i32, _i32, _p, _i64, _p, _i64, _p,
+               _sz, _p])
+
 
 class PRQError(RuntimeError):
     def __init__(self, status, where):
@@ -607,3 +621,270 @@ def prq_grouped_gemm(Aq, Asc, group_offsets, W, Y=None, workspace=None, variant=
                    W.Wps.data_ptr(), N, K_aug, Y.data_ptr(), ws, ws_bytes, variant, _stream_of_call(stream))
     _check(st, "prq_grouped_gemm")
     return Y
+
+
+# --------------------------------------------------------- attention block ---
+_BF16, _I64, _BOOL = torch.bfloat16, torch.int64, torch.bool
+
+
+class PagedKV:
+    """A paged key/value cache: K and V [pages, kv heads, page size, D] bf16, each page
+    contiguous (views into a larger pool may leave room between pages)."""
+
+    __slots__ = ("K", "V", "pages", "heads", "page_size", "D", "stride")
+
+    def __init__(self, K, V):
+        self.K, self.V = K, V
+        if not (type(K) is type(V) is torch.Tensor and K.dtype is V.dtype is _BF16 and K.dim() == 4
+                and K.shape == V.shape and K.is_cuda and V.is_cuda):
+            raise ValueError("K and V must be bfloat16 GPU tensors [pages, kv heads, page size, D] of one shape")
+        self.pages, self.heads, self.page_size, self.D = K.shape
+        strides = K.stride()
+        if strides[1:] != (self.page_size * self.D, self.D, 1) or V.stride() != strides:
+            raise ValueError(f"each page of K and V must be contiguous, at one stride (strides {strides}, "
+                             f"{V.stride()})")
+        self.stride = max(strides[0], self.heads * self.page_size * self.D) if self.pages == 1 else strides[0]
+
+
+def prq_paged_kv(pages, heads, page_size, D, device="cuda"):
+    """A cache of `pages` empty pages (zeros)."""
+    return PagedKV(*(_alloc(torch.zeros, (pages, heads, page_size, D), _BF16, device, None) for _ in range(2)))
+
+
+def prq_rope_table(positions, rotary_dim, theta=10000.0, scaling="none", factor=1.0, original_positions=None,
+                   beta_fast=32.0, beta_slow=1.0, device="cuda"):
+    """Cosine and sine of every position and rotated pair, float32 [positions, rotary_dim / 2, 2],
+    from angles in float64: position * f_i, f_i = theta^(-2i / rotary_dim), i < rotary_dim / 2.
+
+    scaling, for contexts `factor` >= 1 times the one that a model was trained on:
+      "linear": f_i / factor;
+      "ntk":    theta * factor^(rotary_dim / (rotary_dim - 2)) in theta's place (the slowest pair
+                then turns as with "linear", the fastest as without);
+      "yarn":   f_i (g_i / factor + 1 - g_i), g_i a ramp over i from 0 to 1 between the pairs that
+                turn beta_fast and beta_slow times in original_positions (their indices rounded
+                outwards), and cosine and sine times 0.1 ln(factor) + 1."""
+    r = int(rotary_dim)
+    if r <= 0 or r % 8 or positions < 0:
+        raise ValueError(f"rotary_dim {rotary_dim} must be a positive multiple of 8, positions {positions} >= 0")
+    if scaling not in ("none", "linear", "ntk", "yarn"):
+        raise ValueError(f"unknown scaling {scaling!r}")
+    if not theta > 1 or not factor >= 1:
+        raise ValueError(f"theta {theta} must be above 1 and factor {factor} at least 1")
+    i = np.arange(r // 2, dtype=np.float64)
+    base = theta * factor ** (r / (r - 2)) if scaling == "ntk" else theta
+    f = base ** (-2.0 * i / r)
+    gain = 1.0
+    if scaling == "linear":
+        f = f / factor
+    elif scaling == "yarn":
+        if not original_positions or original_positions < 1 or not beta_fast > beta_slow > 0:
+            raise ValueError("yarn needs original_positions and beta_fast > beta_slow > 0")
+        # index whose pair turns `turns` times over the original context
+        index = [r * np.log(original_positions / (turns * 2 * np.pi)) / (2 * np.log(theta))
+                 for turns in (beta_fast, beta_slow)]
+        lo, hi = max(np.floor(index[0]), 0.0), min(np.ceil(index[1]), r - 1.0)
+        ramp = np.clip((i - lo) / max(hi - lo, 1e-3), 0.0, 1.0)
+        f = f * (ramp / factor + (1.0 - ramp))
+        gain = 0.1 * np.log(factor) + 1.0
+    angle = np.arange(int(positions), dtype=np.float64)[:, None] * f
+    table = np.stack([np.cos(angle), np.sin(angle)], axis=-1) * gain
+    return torch.from_numpy(table.astype(np.float32)).to(device)
+
+
+def _rows(t, name, dtypes, wide):
+    """A 2-D GPU tensor of rows of `wide` contiguous elements -> its row stride."""
+    if not (type(t) is torch.Tensor and t.dim() == 2 and t.dtype in dtypes and t.is_cuda and t.shape[1] == wide
+            and (t.stride(1) == 1 or wide == 1)):
+        raise ValueError(f"{name} must be a 2-D GPU tensor of {' or '.join(map(str, dtypes))} with rows of {wide} "
+                         f"contiguous elements" + (f" (is {t.dtype} {tuple(t.shape)}, strides {t.stride()})"
+                                                   if isinstance(t, torch.Tensor) else ""))
+    return t.stride(0) if t.shape[0] > 1 else wide
+
+
+def _vector(t, name, dtype, n):
+    if not _is(t, dtype, (n,)):
+        _need(t, name, dtype, (n,))
+        _on_gpu(**{name: t})
+
+
+def prq_qk_norm_rope(q, k, v, positions, table, cache, slots, q_weight=None, k_weight=None, eps=1e-6,
+                     interleaved=False, out=None, stream=None):
+    """Queries, keys and values [M, heads * D] (float32 or bf16) -> queries [M, Hq, D] bf16, normed
+    per head (where a weight is given) and rotated by `positions` int32 [M]; keys, the same, and
+    values go to `slots` int64 [M] of the cache (-1: nowhere).  table: prq_rope_table's, or None
+    for no rotation."""
+    D, Hk = cache.D, cache.heads
+    kinds = (_F32, _BF16)
+    if not isinstance(q, torch.Tensor) or q.dim() != 2 or q.shape[1] % D or q.shape[1] == 0:
+        raise ValueError(f"q must be [M, heads * {D}]")
+    M, wide = q.shape
+    ld_q = _rows(q, "q", kinds, wide)
+    ld_k, ld_v = _rows(k, "k", kinds, Hk * D), _rows(v, "v", kinds, Hk * D)
+    if not (q.dtype is k.dtype is v.dtype) or k.shape[0] != M or v.shape[0] != M:
+        raise ValueError("q, k and v must have one type and number of rows")
+    Hq = wide // D
+    if table is None:
+        rot = rows = 0
+    else:
+        if not (type(table) is torch.Tensor and table.dim() == 3 and table.dtype is _F32 and table.shape[2] == 2
+                and table.is_cuda and table.is_contiguous()):
+            raise ValueError("table must be a contiguous float32 GPU tensor [positions, rotary_dim / 2, 2]")
+        rows, rot = table.shape[0], 2 * table.shape[1]
+        _vector(positions, "positions", _I32, M)
+    _vector(slots, "slots", _I64, M)
+    kind = _F32
+    for name, w in (("q_weight", q_weight), ("k_weight", k_weight)):
+        if w is not None:
+            if not (_is(w, _F32, (D,)) or _is(w, _BF16, (D,))):
+                _need(w, name, kinds, (D,))
+                _on_gpu(**{name: w})
+            kind = w.dtype
+    if q_weight is not None and k_weight is not None and q_weight.dtype is not k_weight.dtype:
+        raise ValueError("q_weight and k_weight must have one type")
+    if out is None:
+        out = _alloc(torch.empty, (M, Hq, D), _BF16, q.device, stream)
+    elif not _is(out, _BF16, (M, Hq, D)):
+        _need(out, "out", _BF16, (M, Hq, D))
+        _on_gpu(out=out)
+    st = _qk_norm_rope(q.data_ptr(), ld_q, k.data_ptr(), ld_k, v.data_ptr(), ld_v, int(q.dtype is _BF16), M, Hq, Hk, D,
+                       _ptr(q_weight), _ptr(k_weight), int(kind is _BF16), eps, _ptr(positions) if rot else None,
+                       _ptr(table) if rot else None, rows, rot, int(interleaved), out.data_ptr(), cache.K.data_ptr(),
+                       cache.V.data_ptr(), cache.stride, cache.pages, cache.page_size, slots.data_ptr(),
+                       _stream_of_call(stream))
+    _check(st, "prq_qk_norm_rope")
+    return out
+
+
+def prq_tree_attention_workspace_bytes(M, B, Hq, Hk, D, max_kv_len):
+    return int(_tree_ws(M, B, Hq, Hk, D, max_kv_len))
+
+
+def prq_tree_attention(q, cache, page_table, cached_lens, q_offsets, scale, tree_mask=None, max_kv_len=None,
+                       out=None, lse=None, workspace=None, stream=None):
+    """q [M, Hq, D] bf16 (rows of B requests, q_offsets int32 [B + 1]) over the cache -> (out [M, Hq, D]
+    bf16, lse [M, Hq] float32).  Request b's own tokens follow its cached_lens[b] (int32 [B]) cached
+    ones on its pages (page_table int32 [B, pages]); tree_mask bool [M, w] says which of its own tokens
+    a row sees (None: itself and those before it).  max_kv_len: the most tokens a request has (default:
+    what the page table holds).  workspace: uint8, prq_tree_attention_workspace_bytes (else allocated)."""
+    if not (type(q) is torch.Tensor and q.dim() == 3 and q.dtype is _BF16 and q.is_cuda and q.shape[2] == cache.D
+            and q.stride(2) == 1 and (q.shape[1] <= 1 or q.stride(1) == cache.D)):
+        raise ValueError(f"q must be a bfloat16 GPU tensor [M, heads, {cache.D}] with contiguous rows")
+    M, Hq, D = q.shape
+    ld_q = q.stride(0) if M > 1 else Hq * D
+    if not (type(page_table) is torch.Tensor and page_table.dim() == 2 and page_table.dtype is _I32
+            and page_table.is_cuda and (page_table.shape[1] <= 1 or page_table.stride(1) == 1)):
+        raise ValueError("page_table must be an int32 GPU tensor [requests, pages] with contiguous rows")
+    B, wide = page_table.shape
+    ld_pages = page_table.stride(0) if B > 1 else wide
+    _vector(cached_lens, "cached_lens", _I32, B)
+    _vector(q_offsets, "q_offsets", _I32, B + 1)
+    mask, ld_mask, mask_wide = None, 0, 0
+    if tree_mask is not None:
+        if not (type(tree_mask) is torch.Tensor and tree_mask.dim() == 2 and tree_mask.dtype in (_BOOL, _U8)
+                and tree_mask.is_cuda and tree_mask.shape[0] == M
+                and (tree_mask.shape[1] <= 1 or tree_mask.stride(1) == 1)):
+            raise ValueError(f"tree_mask must be a bool GPU tensor [{M}, tokens] with contiguous rows")
+        mask_wide = tree_mask.shape[1]
+        ld_mask = tree_mask.stride(0) if M > 1 else mask_wide
+        mask = tree_mask.data_ptr()
+        if not mask_wide:                # no column: nothing seen, which a null pointer does not say
+            mask = q_offsets.data_ptr()
+    if max_kv_len is None:
+        max_kv_len = wide * cache.page_size
+    if out is None:
+        out = _alloc(torch.empty, (M, Hq, D), _BF16, q.device, stream)
+    elif not _is(out, _BF16, (M, Hq, D)):
+        _need(out, "out", _BF16, (M, Hq, D))
+        _on_gpu(out=out)
+    if lse is None:
+        lse = _alloc(torch.empty, (M, Hq), _F32, q.device, stream)
+    elif not _is(lse, _F32, (M, Hq)):
+        _need(lse, "lse", _F32, (M, Hq))
+        _on_gpu(lse=lse)
+    if workspace is None:
+        need = int(_tree_ws(M, B, Hq, cache.heads, D, max_kv_len))
+        if need:
+            workspace = _alloc(torch.empty, need, _U8, q.device, stream, kept=False)
+    ws, ws_bytes = _workspace_arg(workspace)
+    st = _tree(q.data_ptr(), ld_q, M, Hq, cache.heads, D, cache.K.data_ptr(), cache.V.data_ptr(), cache.stride,
+               cache.pages, cache.page_size, page_table.data_ptr(), ld_pages, wide, cached_lens.data_ptr(),
+               q_offsets.data_ptr(), B, max_kv_len, scale, mask, ld_mask, mask_wide, out.data_ptr(), lse.data_ptr(),
+               ws, ws_bytes, _stream_of_call(stream))
+    _check(st, "prq_tree_attention")
+    return out, lse
+
+
+class LoraAdapters:
+    """Device buffers of a set of adapters: A [sum of ranks, K] bf16, B bf16 flat (adapter a's [N, rank]
+    from element N * rank_offsets[a]), rank_offsets int32 [adapters + 1] in multiples of 8, scales float32
+    [adapters], and the largest rank."""
+
+    __slots__ = ("A", "B", "rank_offsets", "scales", "max_rank")
+
+    def __init__(self, A, B, rank_offsets, scales, max_rank):
+        self.A, self.B, self.rank_offsets, self.scales, self.max_rank = A, B, rank_offsets, scales, max_rank
+
+
+def prq_lora_adapters(pairs, scales, device="cuda"):
+    """LoraAdapters of [(A [r, K], B [N, r]), ...] and one scale each; ranks padded with zeros to multiples
+    of 8, values rounded to bf16."""
+    if not pairs or len(pairs) != len(scales):
+        raise ValueError("as many scales as adapters are needed, and one adapter at least")
+    K, N = pairs[0][0].shape[1], pairs[0][1].shape[0]
+    ranks, As, Bs = [], [], []
+    for A, B in pairs:
+        r = A.shape[0]
+        if A.shape != (r, K) or B.shape != (N, r):
+            raise ValueError(f"adapter shapes {tuple(A.shape)}, {tuple(B.shape)} do not fit [r, {K}], [{N}, r]")
+        pad = -r % 8
+        A, B = A.to(device, _BF16), B.to(device, _BF16)
+        As.append(torch.nn.functional.pad(A, (0, 0, 0, pad)))
+        Bs.append(torch.nn.functional.pad(B, (0, pad)).reshape(-1))
+        ranks.append(r + pad)
+    return LoraAdapters(torch.cat(As).contiguous(), torch.cat(Bs).contiguous(),
+                        torch.tensor(np.concatenate([[0], np.cumsum(ranks)]), dtype=_I32, device=device),
+                        torch.tensor([float(s) for s in scales], dtype=_F32, device=device), max(ranks))
+
+
+def prq_lora_workspace_bytes(M, segments, N, K, max_rank):
+    return int(_lora_ws(M, segments, N, K, max_rank))
+
+
+def prq_lora(x, adapters, segment_offsets, segment_adapter, Y, out=None, workspace=None, stream=None):
+    """out [M, N] float32 = Y + scale * B_a (A_a x) with each segment's adapter (segment_offsets int32
+    [S + 1] over x's rows [M, K] bf16, segment_adapter int32 [S], -1: none).  out=None adds into Y.
+    workspace: uint8, prq_lora_workspace_bytes (else allocated)."""
+    if not isinstance(x, torch.Tensor) or x.dim() != 2 or not isinstance(Y, torch.Tensor) or Y.dim() != 2:
+        raise ValueError("x and Y must be 2-D tensors")
+    (M, K), N = x.shape, Y.shape[1]
+    ld_x, ld_y = _rows(x, "x", (_BF16,), K), _rows(Y, "Y", (_F32,), N)
+    if out is None:
+        out = Y
+    ld_out = _rows(out, "out", (_F32,), N)
+    if Y.shape[0] != M or out.shape[0] != M:
+        raise ValueError(f"x has {M} rows, Y {Y.shape[0]}, out {out.shape[0]}")
+    a = adapters
+    n = a.scales.shape[0]
+    if not (type(a.A) is torch.Tensor and a.A.dim() == 2 and _is(a.A, _BF16, (a.A.shape[0], K))
+            and _holds(a.B, _BF16, N * a.A.shape[0]) and _is(a.rank_offsets, _I32, (n + 1,)) and _is(a.scales, _F32, (n,))):
+        _need(a.A, "adapters.A", _BF16, (a.A.shape[0], K))
+        _need(a.B, "adapters.B", _BF16, min_numel=N * a.A.shape[0])
+        _need(a.rank_offsets, "adapters.rank_offsets", _I32, (n + 1,))
+        _need(a.scales, "adapters.scales", _F32, (n,))
+        _on_gpu(A=a.A, B=a.B, rank_offsets=a.rank_offsets, scales=a.scales)
+    if not (type(segment_adapter) is torch.Tensor and segment_adapter.dim() == 1):
+        raise ValueError("segment_adapter must be an int32 GPU tensor [segments]")
+    segments = segment_adapter.shape[0]
+    _vector(segment_adapter, "segment_adapter", _I32, segments)
+    _vector(segment_offsets, "segment_offsets", _I32, segments + 1)
+    if workspace is None:
+        need = int(_lora_ws(M, segments, N, K, a.max_rank))
+        if need:
+            workspace = _alloc(torch.empty, need, _U8, x.device, stream, kept=False)
+    ws, ws_bytes = _workspace_arg(workspace)
+    st = _lora(x.data_ptr(), ld_x, M, K, a.A.data_ptr(), a.B.data_ptr(), a.rank_offsets.data_ptr(),
+               a.scales.data_ptr(), n, a.A.shape[0], a.max_rank, segment_offsets.data_ptr(),
+               segment_adapter.data_ptr(), segments, N, Y.data_ptr(), ld_y, out.data_ptr(), ld_out, ws, ws_bytes,
+               _stream_of_call(stream))
+    _check(st, "prq_lora")
+    return out

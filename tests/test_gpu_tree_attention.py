@@ -1,0 +1,302 @@
+"""prq_tree_attention against the float64 oracle: head sizes and groups, page sizes, requests of no,
+one and many rows and of no and many cached tokens, trees, chains, masks that leave rows empty, splits
+of the keys, garbage where nothing may be read.
+
+Bar, per element of out (P = sum_j p_j |v_j| and S = scale * max_j sum_d |q_d k_d| from the oracle):
+  2^-8 |out|            the output's rounding to bf16
+  2^-8 P                each probability's rounding to bf16
+  2^-18 (S + 16) P      float32 scores (D products of relative error 2^-24 each, at most 256 of
+                        them), the exponential's argument and the sums, all relative to P
+lse: 2^-18 (S + 16) + 2^-22 |lse|."""
+import numpy as np
+import pytest
+
+torch = pytest.importorskip("torch")
+
+from oracle import attention as at            # noqa: E402
+from tests.gpu_util import say                # noqa: E402
+
+pytestmark = pytest.mark.gpu
+BF16 = torch.bfloat16
+
+
+def _prq():
+    from paper_2609_22106_amd import prq
+    return prq
+
+
+def _tree(rng, n):
+    see = np.zeros((n, n), bool)
+    for i in range(n):
+        parent = int(rng.integers(-1, i)) if i else -1
+        if parent >= 0:
+            see[i] = see[parent]
+        see[i, i] = True
+    return see
+
+
+class Case:
+    """Requests [(cached, rows), ...] with their tokens on shuffled pages; everything that no row may
+    see -- the rest of the last pages, unused pages, unused page-table entries -- is garbage."""
+
+    def __init__(self, requests, Hq, Hk, D, page, seed=0, mask="tree", wide=None, garbage=float("nan"), size=1.5):
+        rng = np.random.default_rng(seed)
+        self.requests, self.Hq, self.Hk, self.D, self.page = requests, Hq, Hk, D, page
+        n = [r for _, r in requests]
+        M = sum(n)
+        used = [-(-(c + r) // page) for c, r in requests]
+        pages = sum(used) + 3
+        order = rng.permutation(pages)
+        width = max(used + [1]) + 1
+        table = np.full((len(requests), width), 1 << 30, np.int32)      # past the pool
+        K = torch.full((pages, Hk, page, D), garbage, dtype=BF16, device="cuda")
+        V = torch.full((pages, Hk, page, D), garbage, dtype=BF16, device="cuda")
+        self.keys, self.values, at_page = [], [], 0
+        g = torch.Generator(device="cuda").manual_seed(seed)
+        for b, (c, r) in enumerate(requests):
+            ids = order[at_page:at_page + used[b]]
+            at_page += used[b]
+            table[b, :used[b]] = ids
+            L = c + r
+            k = torch.randn(L, Hk, D, generator=g, device="cuda").to(BF16)
+            v = (torch.randn(L, Hk, D, generator=g, device="cuda") + 0.3).to(BF16)
+            slot = torch.arange(L, device="cuda")
+            at_ = torch.from_numpy(ids.astype(np.int64)).cuda()
+            if L:
+                K[at_[slot // page], :, slot % page] = k
+                V[at_[slot // page], :, slot % page] = v
+            self.keys.append(k)
+            self.values.append(v)
+        self.q = (size * torch.randn(M, Hq, D, generator=g, device="cuda")).to(BF16)
+        self.cache = _prq().PagedKV(K, V)
+        self.table = torch.from_numpy(table).cuda()
+        self.cached = torch.tensor([c for c, _ in requests], dtype=torch.int32, device="cuda")
+        self.offsets = torch.tensor(np.concatenate([[0], np.cumsum(n)]), dtype=torch.int32, device="cuda")
+        self.scale = 1.0 / D ** 0.5
+        self.mask = None
+        if mask is not None:
+            w = max(n + [0]) if wide is None else wide
+            m = np.ones((M, w), bool)                                   # columns past a request's rows: set
+            row = 0
+            for r in n:
+                one = {"tree": lambda: _tree(rng, r), "self": lambda: np.eye(r, dtype=bool),
+                       "none": lambda: np.zeros((r, r), bool),
+                       "any": lambda: rng.random((r, r)) < 0.4}[mask]()
+                m[row:row + r, :min(r, w)] = one[:, :w]
+                row += r
+            self.mask = torch.from_numpy(m).cuda()
+
+    def run(self, **kw):
+        kw.setdefault("max_kv_len", max([c + r for c, r in self.requests] + [0]))
+        M = self.q.shape[0]
+        kw.setdefault("out", torch.full((M, self.Hq, self.D), float("nan"), dtype=BF16, device="cuda"))
+        kw.setdefault("lse", torch.full((M, self.Hq), float("nan"), device="cuda"))
+        return _prq().prq_tree_attention(self.q, self.cache, self.table, self.cached, self.offsets, self.scale,
+                                         tree_mask=self.mask, **kw)
+
+    def check(self, out, lse, keys=None, values=None):
+        out, lse = out.double().cpu().numpy(), lse.double().cpu().numpy()
+        q = self.q.double().cpu().numpy()
+        mask = None if self.mask is None else self.mask.cpu().numpy()
+        row = 0
+        for b, (c, r) in enumerate(self.requests):
+            k = (self.keys[b] if keys is None else keys[b]).double().cpu().numpy()
+            v = (self.values[b] if values is None else values[b]).double().cpu().numpy()
+            rows = slice(row, row + r)
+            want, wl, spread, size = at.tree_attention(q[rows], k, v, c, self.scale,
+                                                       None if mask is None else mask[rows, :r])
+            S = (self.scale * size + 16)[..., None]
+            tol = 2.0 ** -8 * np.abs(want) + (2.0 ** -8 + 2.0 ** -18 * S) * spread
+            err = np.abs(out[rows] - want)
+            assert np.all(err <= tol), (b, float(np.max(err - tol)))
+            empty = np.isneginf(wl)
+            assert np.array_equal(np.isneginf(lse[rows]), empty)
+            err = np.abs(lse[rows][~empty] - wl[~empty])
+            assert np.all(err <= 2.0 ** -18 * S[..., 0][~empty] + 2.0 ** -22 * np.abs(wl[~empty])), float(err.max())
+            row += r
+
+
+CASES = [
+    # requests, Hq, Hk, D, page
+    ([(0, 1)], 1, 1, 64, 16), ([(1, 1)], 4, 1, 128, 16), ([(0, 0), (5, 1), (0, 0), (31, 1)], 8, 2, 64, 16),
+    ([(33, 1)] * 5, 32, 8, 128, 64), ([(127, 1), (128, 1), (129, 1), (0, 1)], 8, 8, 128, 128),
+    ([(700, 3), (15, 13), (16, 1), (0, 7)], 6, 2, 64, 32), ([(100, 16), (90, 5)], 12, 3, 128, 16),
+    ([(1000, 64), (37, 33)], 8, 2, 128, 16), ([(1023, 65)], 4, 4, 64, 64), ([(250, 9), (3, 2)], 16, 1, 128, 16),
+    ([(77, 5), (500, 20)], 4, 2, 256, 16), ([(40, 70)], 5, 1, 256, 32), ([(2000, 1), (3, 1)], 40, 2, 64, 256),
+    ([(64, 3)], 64, 1, 128, 16), ([(5000, 2)], 2, 1, 128, 4096), ([(300, 17)] * 3, 21, 7, 64, 16)]
+
+
+@pytest.mark.parametrize("requests,Hq,Hk,D,page", CASES)
+@pytest.mark.parametrize("mask", ["tree", "any", None])
+def test_matches_oracle(requests, Hq, Hk, D, page, mask):
+    say("tree attention", requests, Hq, Hk, D, page, mask)
+    c = Case(requests, Hq, Hk, D, page, seed=len(requests) + D, mask=mask)
+    c.check(*c.run())
+
+
+def test_many_requests_of_one_token():
+    rng = np.random.default_rng(5)
+    c = Case([(int(rng.integers(0, 200)), 1) for _ in range(150)], 8, 2, 64, 16, mask=None)
+    c.check(*c.run())
+
+
+def test_masks_that_leave_rows_empty():
+    """No own token seen: the cached ones alone, or nothing at all (0 and -inf)."""
+    for mask, wide in (("none", None), ("none", 0), ("self", 2)):
+        say("empty rows", mask, wide)
+        c = Case([(0, 5), (40, 3), (0, 1)], 4, 2, 128, 16, mask=mask, wide=wide)
+        out, lse = c.run()
+        c.check(out, lse)
+        if mask == "none":
+            assert not out[:5].any() and not out[8:].any() and bool(torch.isneginf(lse[:5]).all())
+
+
+def test_a_long_chunk_of_a_prompt():
+    c = Case([(50, 300), (0, 129)], 4, 2, 64, 16, mask=None)
+    c.check(*c.run())
+
+
+@pytest.mark.parametrize("max_kv", [0, 1, 64, 300, 10 ** 6])
+def test_max_kv_len_is_only_a_plan(max_kv):
+    c = Case([(300, 4), (2, 1)], 8, 2, 64, 16)
+    c.check(*c.run(max_kv_len=max_kv))
+
+
+def test_unseen_infinities_and_nan_do_not_reach_a_row():
+    """Own token 3 holds NaN and infinities that rows 3.. do or do not see: a row that sees them has
+    them where they are, every other row is as without them."""
+    for D, Hq, Hk in ((64, 4, 2), (128, 32, 8), (256, 2, 2)):
+        c = Case([(45, 8), (10, 4)], Hq, Hk, D, 16, mask="tree", seed=D)
+        c.mask[:8, 3] = False
+        c.mask[5, 3] = True
+        page, at_ = c.table[0, 48 // 16].item(), 48 % 16
+        c.check(*c.run())
+        clean = c.run()
+        V = c.cache.V
+        V[page, :, at_, 7], V[page, :, at_, 8] = float("nan"), float("inf")
+        out, lse = c.run()
+        keep = torch.ones(12, Hq, D, dtype=torch.bool, device="cuda")
+        keep[5, :, 7:9] = False
+        assert bool(torch.isnan(out[5, :, 7]).all()) and bool((out[5, :, 8] == float("inf")).all())
+        assert bool((out[keep].float() - clean[0][keep].float()).abs().max() < 2.0 ** -5)
+        assert torch.equal(lse, clean[1])
+        c.cache.K[page, :, at_] = float("nan")
+        out, lse = c.run()
+        assert bool(torch.isnan(out[5]).all()) and bool(torch.isnan(lse[5]).all())
+        rows = [r for r in range(12) if r != 5]
+        assert bool(torch.isfinite(out[rows]).all()) and torch.equal(lse[rows], clean[1][rows])
+
+
+def test_large_scores_and_scores_of_minus_infinity():
+    """Scores that pass the maximum by far, rising and falling along the keys; a seen key of -inf."""
+    for falling in (False, True):
+        c = Case([(600, 2)], 2, 1, 64, 16, mask=None, size=1.0)
+        k = c.keys[0]
+        ramp = torch.linspace(40 * falling, 40 * (not falling), 602, device="cuda")
+        k[:, :, 0] = ramp[:, None].to(BF16)
+        slot = torch.arange(602, device="cuda")
+        c.cache.K[c.table[0].long()[slot // 16], :, slot % 16] = k
+        c.q[:, :, 0] = 20
+        c.check(*c.run())
+    c = Case([(5, 1)], 1, 1, 64, 16, mask=None)
+    c.cache.K[c.table[0, 0].item(), :, 2, 0] = float("-inf")
+    c.q[:, :, 0] = 1.0
+    out, lse = c.run()
+    keep = [0, 1, 3, 4, 5]
+    c.requests = [(4, 1)]
+    c.check(out, lse, keys=[c.keys[0][keep]], values=[c.values[0][keep]])
+
+
+def test_pages_outside_the_pool_are_not_seen():
+    c = Case([(100, 1)], 4, 2, 64, 16, mask=None)
+    for bad in (-1, c.cache.pages, -(1 << 31)):
+        t = c.table.clone()
+        t[0, 2] = bad
+        keep = [i for i in range(101) if not 32 <= i < 48]
+        M = c.q.shape[0]
+        out, lse = _prq().prq_tree_attention(c.q, c.cache, t, c.cached, c.offsets, c.scale, max_kv_len=101)
+        one = Case.__new__(Case)
+        one.__dict__.update(c.__dict__, requests=[(len(keep) - 1, 1)])
+        assert M == 1
+        one.check(out, lse, keys=[c.keys[0][keep]], values=[c.values[0][keep]])
+
+
+def test_lengths_past_the_page_table_are_cut():
+    c = Case([(60, 1)], 2, 1, 64, 16, mask=None)
+    c.cached[0] = 1 << 30
+    out, lse = _prq().prq_tree_attention(c.q, c.cache, c.table[:, :2], c.cached, c.offsets, c.scale)
+    c.requests = [(32, 1)]
+    c.check(out, lse, keys=[c.keys[0][:32]], values=[c.values[0][:32]])
+    c.cached[0] = -5                                    # taken as 0: the row's own token alone, at slot 0
+    out, lse = _prq().prq_tree_attention(c.q, c.cache, c.table[:, :2], c.cached, c.offsets, c.scale)
+    c.requests = [(0, 1)]
+    c.check(out, lse, keys=[c.keys[0][:1]], values=[c.values[0][:1]])
+
+
+def test_offsets_outside_the_rows_are_clamped():
+    c = Case([(20, 3), (9, 2)], 2, 1, 64, 16, mask=None)
+    want = c.run()
+    c.offsets = torch.tensor([0, 3, 99], dtype=torch.int32, device="cuda")
+    got = c.run()
+    assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+
+
+def test_strided_queries_masks_tables_and_pools():
+    c = Case([(300, 7), (90, 12)], 8, 2, 128, 16, mask="tree")
+    want = c.run()
+    M = c.q.shape[0]
+    wide = torch.randn(M, 13 * 128, device="cuda").to(BF16)
+    wide[:, 128:9 * 128] = c.q.view(M, -1)
+    c.q = wide[:, 128:9 * 128].unflatten(1, (8, 128))
+    m = torch.ones(M, 40, dtype=torch.bool, device="cuda")
+    m[:, 3:15] = c.mask
+    c.mask = m[:, 3:15]
+    t = torch.full((2, 99), -7, dtype=torch.int32, device="cuda")
+    t[:, 5:5 + c.table.shape[1]] = c.table
+    c.table = t[:, 5:5 + c.table.shape[1]]
+    pool = torch.stack([c.cache.K, c.cache.V], 1)
+    c.cache = _prq().PagedKV(pool[:, 0], pool[:, 1])
+    got = c.run()
+    assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+
+
+def test_pool_past_32_bits():
+    Hk, page, D = 8, 16, 128
+    c = Case([(70, 2), (33, 1)], 16, Hk, D, page, mask=None)
+    want = c.run()
+    pages = (1 << 31) // (Hk * page * D) + 700
+    K = torch.empty(pages, Hk, page, D, dtype=BF16, device="cuda")
+    V = torch.empty(pages, Hk, page, D, dtype=BF16, device="cuda")
+    n = c.cache.pages
+    K[-n:], V[-n:] = c.cache.K, c.cache.V
+    c.table = torch.where(c.table < n, c.table + (pages - n), c.table)
+    c.cache = _prq().PagedKV(K, V)
+    got = c.run()
+    assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+
+
+def test_calls_repeat_bit_for_bit_and_need_no_clean_workspace():
+    prq = _prq()
+    c = Case([(3000, 2), (100, 1)], 32, 8, 128, 64)
+    need = prq.prq_tree_attention_workspace_bytes(3, 2, 32, 8, 128, 3002)
+    assert need > 0
+    a = c.run(workspace=torch.zeros(need, dtype=torch.uint8, device="cuda"))
+    b = c.run(workspace=torch.full((need,), 255, dtype=torch.uint8, device="cuda"))
+    assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1])
+    with pytest.raises(prq.PRQError) as e:
+        c.run(workspace=torch.zeros(need - 1, dtype=torch.uint8, device="cuda"))
+    assert e.value.status == prq.PRQ_EWORKSPACE
+
+
+def test_no_rows_and_no_requests():
+    prq = _prq()
+    c = Case([(3, 1)], 2, 1, 64, 16, mask=None)
+    out, lse = prq.prq_tree_attention(c.q[:0], c.cache, c.table, c.cached, c.offsets * 0, c.scale)
+    assert out.shape == (0, 2, 64) and lse.shape == (0, 2)
+    with pytest.raises(ValueError):
+        prq.prq_tree_attention(c.q, c.cache, c.table, c.cached, c.offsets[:1], c.scale)
+    with pytest.raises(ValueError):
+        prq.prq_tree_attention(c.q, c.cache, c.table.long(), c.cached, c.offsets, c.scale)
+    with pytest.raises(ValueError):
+        prq.prq_tree_attention(c.q, c.cache, c.table, c.cached, c.offsets, c.scale,
+                               tree_mask=torch.ones(2, 1, dtype=torch.bool, device="cuda"))           # rows
