@@ -35,45 +35,55 @@ __device__ __forceinline__ f32x4 mfma_bf16(u32x4v a, u32x4v b, f32x4 c) {
 }
 
 // Segment tables on the device: segment s holds rows [offsets[s], offsets[s + 1]),
-// cut into tiles of `rows` times `per_row` units each.  find_tile: the segment that
-// holds tile `t` (counted over all segments) and the tile's number in it; -1 past
-// the last.  Offsets outside [0, M] or descending are clamped to empty segments, so
-// no table makes a kernel leave its buffers.  Every lane of the wave calls it.
+// per_row units each, cut into tiles of per_tile units.  find_tile: the segment that
+// holds tile `t` (counted over all segments), the tile's number in it, and the
+// segment's entry of `with` (loaded beside the offsets: one round trip to memory);
+// segment -1 past the last.  Offsets outside [0, M] or descending are clamped to empty
+// segments, so no table makes a kernel leave its buffers.  Every lane of the wave calls
+// it.
 struct TileAt {
-  int segment, tile, first, rows;
+  int segment, tile, first, rows, with;
 };
 
-__device__ __forceinline__ TileAt find_tile(const int32_t* __restrict__ offsets, int segments, int M, int t,
-                                            int per_row, int per_tile) {
+__device__ __forceinline__ TileAt find_tile(const int32_t* __restrict__ offsets, const int32_t* __restrict__ with,
+                                            int segments, int M, int t, int per_row, int per_tile) {
   const int lane = static_cast<int>(threadIdx.x) & 63;
-  int before = 0;
-  for (int base = 0; base < segments; base += 64) {
+  int before = 0, base = 0, at = -1;
+  int lo = 0, n = 0, tiles = 0, entry = 0, sum = 0;
+  for (; base < segments; base += 64) {
     const int s = base + lane;
-    int lo = 0, n = 0, tiles = 0;
+    lo = n = tiles = entry = 0;
     if (s < segments) {
-      lo = min(max(offsets[s], 0), M);
-      n = max(min(max(offsets[s + 1], 0), M) - lo, 0);
+      lo = offsets[s];
+      n = offsets[s + 1];
+      entry = with[s];
+      lo = min(max(lo, 0), M);
+      n = max(min(max(n, 0), M) - lo, 0);
       tiles = (n * per_row + per_tile - 1) / per_tile;
     }
-    int sum = tiles;
+    sum = tiles;
+    if (segments > 1) {
 #pragma unroll
-    for (int d = 1; d < 64; d <<= 1) {
-      const int x = __shfl_up(sum, d);
-      if (lane >= d) sum += x;
+      for (int d = 1; d < 64; d <<= 1) {
+        const int x = __shfl_up(sum, d);
+        if (lane >= d) sum += x;
+      }
     }
     const uint64_t past = __ballot(before + sum > t);
     if (past) {
-      const int at = __builtin_ctzll(past);
-      TileAt r;
-      r.segment = base + at;
-      r.tile = t - before - (__builtin_amdgcn_readlane(sum, at) - __builtin_amdgcn_readlane(tiles, at));
-      r.first = __builtin_amdgcn_readlane(lo, at);
-      r.rows = __builtin_amdgcn_readlane(n, at);
-      return r;
+      at = __builtin_ctzll(past);
+      break;
     }
     before += __builtin_amdgcn_readlane(sum, 63);
   }
-  return {-1, 0, 0, 0};
+  TileAt r;
+  r.segment = at < 0 ? -1 : base + at;
+  at = max(at, 0);
+  r.tile = t - before - (__builtin_amdgcn_readlane(sum, at) - __builtin_amdgcn_readlane(tiles, at));
+  r.first = __builtin_amdgcn_readlane(lo, at);
+  r.rows = __builtin_amdgcn_readlane(n, at);
+  r.with = __builtin_amdgcn_readlane(entry, at);
+  return r;
 }
 
 }  // namespace dev

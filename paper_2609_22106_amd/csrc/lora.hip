@@ -64,7 +64,7 @@ __global__ __launch_bounds__(kThreads) void lora_down_kernel(const LoraArgs p) {
   __shared__ f32x4 sh[kWaves][kRankTiles][64];
   const int lane = static_cast<int>(threadIdx.x) & 63, r = lane & 15, g = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x) >> 6);
-  const dev::TileAt at = dev::find_tile(p.offsets, p.segments, p.M, static_cast<int>(blockIdx.y), 1, 16);
+  const dev::TileAt at = dev::find_tile(p.offsets, p.of, p.segments, p.M, static_cast<int>(blockIdx.y), 1, 16);
   if (at.segment < 0) return;
   const Adapter ad = adapter_of(p, at.segment);
   if (ad.rank <= 0) return;
@@ -127,7 +127,7 @@ __global__ __launch_bounds__(kThreads) void lora_up_kernel(const LoraArgs p, int
   const int lane = static_cast<int>(threadIdx.x) & 63, r = lane & 15, g = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x) >> 6);
   const dev::TileAt at =
-      dev::find_tile(p.offsets, p.segments, p.M, static_cast<int>(blockIdx.y), 1, 16 * kRowTiles);
+      dev::find_tile(p.offsets, p.of, p.segments, p.M, static_cast<int>(blockIdx.y), 1, 16 * kRowTiles);
   if (at.segment < 0) return;
   const Adapter ad = adapter_of(p, at.segment);
   const int rows = min(at.rows - 16 * kRowTiles * at.tile, 16 * kRowTiles);

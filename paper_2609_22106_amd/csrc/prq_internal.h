@@ -215,9 +215,9 @@ hipError_t launch_qk_norm_rope(const void* q, int64_t ld_q, const void* k, int64
                                const int64_t* slots, int num_cus, hipStream_t stream);
 
 // tree_attention.hip.  Query columns a workgroup (16, 32 or 64), their tiles over all
-// requests and key ranges a tile, and the blocks of the launch.
+// requests, parts of a request's keys, and the blocks of the launch.
 struct TreePlan {
-  int tile_cols = 16, splits = 1, split_len = 0;
+  int tile_cols = 16, splits = 1;
   int64_t tiles = 0, blocks = 0;
 };
 TreePlan plan_tree_attention(int M, int B, int Hq, int Hk, int D, int max_kv_len, int num_cus);

@@ -13,9 +13,12 @@
 // rounded to bf16 they are its operand of the second product, O^T = V^T P^T, as they
 // stand.  That product's A operand needs 8 keys of one column of V: a lane group loads
 // whole rows of its 8 keys, 16 lanes a row, and pairs up halves of registers
-// (32 v_perm per 32 x 128 tile); nothing goes through LDS until the waves' results
-// are joined.  The 16 queries of a product's column side are the G query heads of
-// the kv head for 16 / G tokens, 1, 2 or 4 such tiles a wave.
+// (32 v_perm per 32 x 128 tile).  The 16 queries of a product's column side are the G
+// query heads of the kv head for 16 / G tokens.  Up to 16 columns a request, the waves
+// take keys of their own, straight from memory into registers, and join their results
+// through LDS; more columns are dealt to the waves, one or two tiles each, and K and V go
+// through LDS once for all of them (trees of up to 64 nodes over 8 x 32 k tokens: four tiles
+// a wave straight from memory 714 us, through LDS 303).
 //
 // The maximum is kept per lane group and only joined across the groups when a score
 // passes it by 8 (powers of two): until then the stale maximum serves, P up to 2^8.
@@ -23,12 +26,13 @@
 // error 2^-9 each, as large as the rounding of the output; the sum that divides takes
 // the unrounded P).
 //
-// Few rows leave most CUs idle, so the keys are split over workgroups and the partial
-// (m, l, O) joined by a second kernel in a fixed order.
+// Few rows leave most CUs idle, so each request's keys are split into equal parts over
+// workgroups and the partial (m, l, O) joined by a second kernel in a fixed order.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
 #include <cmath>
+#include <type_traits>
 
 #include "attn_device.hpp"
 #include "prq_internal.h"
@@ -40,7 +44,7 @@ using dev::f32x4;
 using dev::u32x4v;
 
 constexpr int kWaves = 4, kThreads = 64 * kWaves;
-constexpr int kStep = 32 * kWaves;       // keys a workgroup takes at a time
+constexpr int kStep = 32 * kWaves;       // keys a narrow workgroup takes at a time
 constexpr int kMaxSplits = 64;
 constexpr float kSlack = 8.0f;           // log2 a score may pass the maximum by before it is renewed
 constexpr float kNone = -INFINITY;
@@ -58,24 +62,54 @@ struct TreeArgs {
   const uint8_t* mask;
   int64_t ld_mask;
   int mask_wide;
-  float scale;                           // times log2 e
+  float scale, slack;                    // scale times log2 e, positive; kSlack / scale
+  uint32_t flip;                         // sign bits to turn in q (a negative scale)
   uint16_t* out;
   float *lse, *part_o;
   float2* part_ml;
-  int M, B, Hq, Hk, G, tiles, splits, split_len;
+  int M, B, Hq, Hk, G, tiles, splits;
 };
 
 __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
 
-// exp2(a - b), 0 where a is -inf (b may be, too).
-__device__ __forceinline__ float exp2_from(float a, float b) { return a == kNone ? 0.f : exp2_fast(a - b); }
+// exp2(scale (a - b)), 0 where a is -inf (b may be, too).
+__device__ __forceinline__ float exp2_from(float a, float b, float scale) {
+  return a == kNone ? 0.f : exp2_fast((a - b) * scale);
+}
 
+// The largest; a NaN stays one (its column is NaN whatever the maximum), which takes an
+// instruction less than dropping it.
+__device__ __forceinline__ float max_of(float a, float b) { return __builtin_elementwise_maximum(a, b); }
+__device__ __forceinline__ float max_of(float a, float b, float c) { return max_of(max_of(a, b), c); }
+
+__device__ __forceinline__ bool word_finite(uint32_t w) {
+  return (w & 0x7F80u) != 0x7F80u && (w & 0x7F800000u) != 0x7F800000u;
+}
+
+// K and V of 32 keys, as a lane (g = l / 16, r = l % 16) holds them.
 template <int D>
-struct Tile {                            // K and V of 32 keys, as a lane holds them
+struct Tile {
   static constexpr int kChunks = D / 32, kWords = D / 32;
-  u32x4v k[2][kChunks];                  // keys l % 16 of two 16-key blocks, dims 32 c + 8 g ..
-  uint32_t v[8][kWords];                 // keys 4 g .. + 3 of both blocks, dims (D / 16) (l % 16) ..
+  u32x4v k[2][kChunks];                  // key r of two 16-key blocks, dims 32 c + 8 g ..
+  uint32_t v[8][kWords];                 // keys 4 g .. + 3 of both blocks, dims (D / 16) r ..
 };
+
+// A lane's part of one row of V.
+template <int D>
+__device__ __forceinline__ void load_v(const uint16_t* at, uint32_t (&v)[D / 32]) {
+  if constexpr (D == 64) {
+    const dev::u32x2 w = *reinterpret_cast<const dev::u32x2*>(at);
+    v[0] = w.x;
+    v[1] = w.y;
+  } else {
+#pragma unroll
+    for (int c = 0; c < D / 128; ++c) {
+      const u32x4v w = *reinterpret_cast<const u32x4v*>(at + 8 * c);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) v[4 * c + e] = w[e];
+    }
+  }
+}
 
 template <int D>
 __device__ __forceinline__ void load_tile(const TreeArgs& p, const int64_t (&base)[2], Tile<D>* t) {
@@ -90,122 +124,73 @@ __device__ __forceinline__ void load_tile(const TreeArgs& p, const int64_t (&bas
   for (int b = 0; b < 2; ++b) {
     const uint16_t* vp = p.V + base[b] + 4 * g * D + r * (D / 16);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      if constexpr (D == 64) {
-        const dev::u32x2 w = *reinterpret_cast<const dev::u32x2*>(vp + i * D);
-        t->v[4 * b + i][0] = w.x;
-        t->v[4 * b + i][1] = w.y;
-      } else {
-#pragma unroll
-        for (int c = 0; c < D / 128; ++c) {
-          const u32x4v w = *reinterpret_cast<const u32x4v*>(vp + i * D + 8 * c);
-#pragma unroll
-          for (int e = 0; e < 4; ++e) t->v[4 * b + i][4 * c + e] = w[e];
-        }
-      }
-    }
+    for (int i = 0; i < 4; ++i) load_v<D>(vp + i * D, t->v[4 * b + i]);
   }
 }
 
-__device__ __forceinline__ bool word_finite(uint32_t w) {
-  return (w & 0x7F80u) != 0x7F80u && (w & 0x7F800000u) != 0x7F800000u;
-}
+// What a workgroup works on: a tile of one request's query columns (column c is token
+// c / G, head h G + c % G), and a range of its keys.
+struct Part {
+  dev::TileAt at;
+  int h, split, c0, cols, cached, lo, hi;
+};
 
-template <int D, int T>
-__global__ __launch_bounds__(kThreads, T == 1 && D <= 128 ? 2 : 1) void tree_attention_kernel(const TreeArgs p) {
-  constexpr int kCols = 16 * T, kChunks = D / 32, kV = D / 16, kPitch = D + 4;
-  __shared__ __align__(16) float sh_o[kWaves][kCols][kPitch];
-  __shared__ float sh_m[kWaves][kCols], sh_l[kWaves][kCols];
-
-  const int lane = static_cast<int>(threadIdx.x) & 63, r = lane & 15, g = lane >> 4;
-  const int wave = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x) >> 6);
-  const int h = static_cast<int>(blockIdx.x) % p.Hk;
+// false: nothing to do (where the keys are split, the join is told so).
+__device__ __forceinline__ bool find_part(const TreeArgs& p, int per_tile, Part* w) {
+  w->h = static_cast<int>(blockIdx.x) % p.Hk;
   const int rest = static_cast<int>(blockIdx.x) / p.Hk;
-  const int split = rest / p.tiles;
-  const dev::TileAt at = dev::find_tile(p.offsets, p.B, p.M, rest % p.tiles, p.G, kCols);
-  if (at.segment < 0) return;
-  const int c0 = at.tile * kCols;
-  const int cols = min(at.rows * p.G - c0, kCols);
-  const int cached = min(max(p.cached[at.segment], 0), p.max_keys);
-  const int keys = min(at.rows, p.max_keys - cached) + cached;
-  const int lo = split * p.split_len;
-  const int hi = split == p.splits - 1 ? keys : min(keys, lo + p.split_len);
-  if (p.splits > 1 && hi <= lo) {        // nothing here for this request: say so to the join
-    if (static_cast<int>(threadIdx.x) < cols) {
-      const int c = c0 + static_cast<int>(threadIdx.x);
-      const int64_t row = at.first + c / p.G;
-      p.part_ml[(split * static_cast<int64_t>(p.M) + row) * p.Hq + h * p.G + c % p.G] = {kNone, 0.f};
-    }
-    return;
+  w->split = rest / p.tiles;
+  w->at = dev::find_tile(p.offsets, p.cached, p.B, p.M, rest % p.tiles, p.G, per_tile);
+  if (w->at.segment < 0) return false;
+  w->c0 = w->at.tile * per_tile;
+  w->cols = min(w->at.rows * p.G - w->c0, per_tile);
+  w->cached = min(max(w->at.with, 0), p.max_keys);
+  const int keys = min(w->at.rows, p.max_keys - w->cached) + w->cached;
+  // equal parts of this request's own keys, whole steps
+  const int part = ((keys + p.splits - 1) / p.splits + kStep - 1) / kStep * kStep;
+  w->lo = min(w->split * part, keys);
+  w->hi = min(w->lo + part, keys);
+  if (p.splits == 1 || w->hi > w->lo) return true;
+  for (int x = static_cast<int>(threadIdx.x); x < w->cols; x += kThreads) {
+    const int c = w->c0 + x;
+    const int64_t row = w->at.first + c / p.G;
+    p.part_ml[(w->split * static_cast<int64_t>(p.M) + row) * p.Hq + w->h * p.G + c % p.G] = {kNone, 0.f};
   }
+  return false;
+}
 
-  // Queries: column r of tile t is token c / G, head h G + c % G.
+// A wave's T tiles of 16 query columns: operands, running maximum (of q . k, the same
+// in the four lanes of a column), sum (a lane's own keys) and output.
+template <int D, int T>
+struct Wave {
+  static constexpr int kChunks = D / 32, kV = D / 16;
   u32x4v q[T][kChunks];
   int token[T];
-#pragma unroll
-  for (int t = 0; t < T; ++t) {
-    const int c = c0 + 16 * t + r;
-    token[t] = min(c / p.G, at.rows - 1);
-    const uint16_t* qp = p.q + (at.first + token[t]) * p.ld_q + (h * p.G + c % p.G) * D + 8 * g;
-#pragma unroll
-    for (int k = 0; k < kChunks; ++k) q[t][k] = *reinterpret_cast<const u32x4v*>(qp + 32 * k);
-  }
-
   f32x4 o[T][kV];
   float m[T], l[T];
+
+  __device__ __forceinline__ void start(const TreeArgs& p, const Part& w, int c0) {
+    const int lane = static_cast<int>(threadIdx.x) & 63, r = lane & 15, g = lane >> 4;
 #pragma unroll
-  for (int t = 0; t < T; ++t) {
-    m[t] = kNone;
-    l[t] = 0.f;
+    for (int t = 0; t < T; ++t) {
+      const int c = c0 + 16 * t + r;     // past the last column: the last token, not stored
+      token[t] = min(c / p.G, w.at.rows - 1);
+      const uint16_t* qp = p.q + (w.at.first + token[t]) * p.ld_q + (w.h * p.G + c % p.G) * D + 8 * g;
 #pragma unroll
-    for (int v = 0; v < kV; ++v) o[t][v] = {0.f, 0.f, 0.f, 0.f};
+      for (int k = 0; k < kChunks; ++k) q[t][k] = *reinterpret_cast<const u32x4v*>(qp + 32 * k) ^ p.flip;
+      m[t] = kNone;
+      l[t] = 0.f;
+#pragma unroll
+      for (int v = 0; v < kV; ++v) o[t][v] = {0.f, 0.f, 0.f, 0.f};
+    }
   }
 
-  const int in_page = (1 << p.page_shift) - 1;
-  const int32_t* table = p.pages + at.segment * p.ld_pages;
-  const int first = lo + 32 * wave;
-  const int steps = hi > first ? (hi - first + kStep - 1) / kStep : 0;
-  int entries = -1;                      // lane 2 s + b: page of block b of step s (of 32 steps)
-  auto load_entries = [&](int step) {
-    const int key = first + kStep * (step + (lane >> 1)) + 16 * (lane & 1);
-    entries = key < hi ? table[key >> p.page_shift] : -1;
-    if (entries >= p.num_pages) entries = -1;
-  };
-  // Element offsets of a step's two blocks; a block past the keys, or on a page
-  // outside the pool, reads the pool's first page, and its keys are not seen.
-  int64_t base[2];
-  bool held[2];
-  auto find = [&](int step) {
-#pragma unroll
-    for (int b = 0; b < 2; ++b) {
-      const int page = __builtin_amdgcn_readlane(entries, 2 * (step & 31) + b);
-      const int key = first + kStep * step + 16 * b;
-      held[b] = page >= 0;
-      base[b] = held[b] ? page * p.page_stride +
-                              ((static_cast<int64_t>(h) << p.page_shift) + (key & in_page)) * D
-                        : 0;
-    }
-  };
-
-  Tile<D> now, next;
-  bool held_now[2] = {false, false};
-  int64_t base_now[2] = {0, 0};
-  if (steps > 0) {
-    load_entries(0);
-    find(0);
-    load_tile<D>(p, base, &now);
-  }
-  for (int step = 0; step < steps; ++step) {
-    held_now[0] = held[0];
-    held_now[1] = held[1];
-    base_now[0] = base[0];
-    base_now[1] = base[1];
-    if (step + 1 < steps) {
-      if (((step + 1) & 31) == 0) load_entries(step + 1);
-      find(step + 1);
-      load_tile<D>(p, base, &next);
-    }
-    const int k0 = first + kStep * step;
+  // Keys k0 .. k0 + 31; held: whether their two blocks are on pages of the pool, at
+  // element offsets base.  kPlain: every row sees all of them.
+  template <bool kPlain>
+  __device__ __forceinline__ void step(const TreeArgs& p, const Part& w, Tile<D>& tile, int k0, bool held0, bool held1,
+                                       int64_t base0, int64_t base1) {
+    const int lane = static_cast<int>(threadIdx.x) & 63, r = lane & 15, g = lane >> 4;
     float s[T][8];
 #pragma unroll
     for (int t = 0; t < T; ++t) {
@@ -213,24 +198,23 @@ __global__ __launch_bounds__(kThreads, T == 1 && D <= 128 ? 2 : 1) void tree_att
       for (int b = 0; b < 2; ++b) {
         f32x4 x = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int c = 0; c < kChunks; ++c) x = dev::mfma_bf16(now.k[b][c], q[t][c], x);
+        for (int c = 0; c < kChunks; ++c) x = dev::mfma_bf16(tile.k[b][c], q[t][c], x);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) s[t][4 * b + i] = x[i] * p.scale;
+        for (int i = 0; i < 4; ++i) s[t][4 * b + i] = x[i];
       }
     }
-    const bool plain = k0 + 32 <= cached && held_now[0] && held_now[1];
     uint32_t seen[T];
-    bool odd_v = false;                  // some drafted key's V holds an infinity or a NaN
-    if (!plain) {
+    bool odd_v = false;                  // some key's V holds an infinity or a NaN
+    if constexpr (!kPlain) {
 #pragma unroll
       for (int t = 0; t < T; ++t) {
-        const uint8_t* see = p.mask ? p.mask + (at.first + token[t]) * p.ld_mask : nullptr;
+        const uint8_t* see = p.mask ? p.mask + (w.at.first + token[t]) * p.ld_mask : nullptr;
         seen[t] = 0;
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
           const int key = k0 + 16 * (e >> 2) + 4 * g + (e & 3);
-          const int j = key - cached;
-          bool ok = key < hi && held_now[e >> 2];
+          const int j = key - w.cached;
+          bool ok = key < w.hi && (e < 4 ? held0 : held1);
           if (ok && j >= 0) ok = see ? j < p.mask_wide && see[j] != 0 : j <= token[t];
           if (ok)
             seen[t] |= 1u << e;
@@ -244,12 +228,12 @@ __global__ __launch_bounds__(kThreads, T == 1 && D <= 128 ? 2 : 1) void tree_att
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
         const int key = k0 + 16 * (e >> 2) + 4 * g + (e & 3);
-        const bool ok = key < hi && held_now[e >> 2];
+        const bool ok = key < w.hi && (e < 4 ? held0 : held1);
 #pragma unroll
-        for (int w = 0; w < Tile<D>::kWords; ++w) {
-          if (!ok) now.v[e][w] = 0;
-          if (!word_finite(now.v[e][w])) {
-            now.v[e][w] = 0;
+        for (int x = 0; x < Tile<D>::kWords; ++x) {
+          if (!ok) tile.v[e][x] = 0;
+          if (!word_finite(tile.v[e][x])) {
+            tile.v[e][x] = 0;
             odd_v = true;
           }
         }
@@ -257,22 +241,21 @@ __global__ __launch_bounds__(kThreads, T == 1 && D <= 128 ? 2 : 1) void tree_att
       odd_v = __any(odd_v);
     }
 
-    // A lane group whose scores pass the running maximum renews it.
+    // A lane whose scores pass the running maximum by more than the slack renews it.
     bool past = false;
     float top[T];
 #pragma unroll
     for (int t = 0; t < T; ++t) {
-      top[t] = fmaxf(fmaxf(fmaxf(s[t][0], s[t][1]), fmaxf(s[t][2], s[t][3])),
-                     fmaxf(fmaxf(s[t][4], s[t][5]), fmaxf(s[t][6], s[t][7])));
-      past |= top[t] > m[t] + kSlack;
+      top[t] = max_of(max_of(max_of(s[t][0], s[t][1], s[t][2]), s[t][3], s[t][4]), s[t][5], max_of(s[t][6], s[t][7]));
+      past |= top[t] > m[t] + p.slack;
     }
     if (__any(past)) {
 #pragma unroll
       for (int t = 0; t < T; ++t) {
-        float x = fmaxf(m[t], top[t]);
-        x = fmaxf(x, __shfl_xor(x, 16));
-        x = fmaxf(x, __shfl_xor(x, 32));
-        const float a = exp2_from(m[t], x);
+        float x = max_of(m[t], top[t]);
+        x = max_of(x, __shfl_xor(x, 16));
+        x = max_of(x, __shfl_xor(x, 32));
+        const float a = exp2_from(m[t], x, p.scale);
         m[t] = x;
         l[t] *= a;
 #pragma unroll
@@ -282,32 +265,32 @@ __global__ __launch_bounds__(kThreads, T == 1 && D <= 128 ? 2 : 1) void tree_att
     u32x4v pw[T];
 #pragma unroll
     for (int t = 0; t < T; ++t) {
-      const float from = m[t] == kNone ? 0.f : m[t];
+      const float from = m[t] == kNone ? 0.f : m[t] * p.scale;
 #pragma unroll
-      for (int e = 0; e < 8; ++e) s[t][e] = exp2_fast(s[t][e] - from);
+      for (int e = 0; e < 8; ++e) s[t][e] = exp2_fast(__builtin_fmaf(s[t][e], p.scale, -from));
       l[t] += ((s[t][0] + s[t][1]) + (s[t][2] + s[t][3])) + ((s[t][4] + s[t][5]) + (s[t][6] + s[t][7]));
 #pragma unroll
       for (int e = 0; e < 4; ++e) pw[t][e] = dev::pack_bf16(s[t][2 * e], s[t][2 * e + 1]);
     }
     // V^T: register pairs of neighbouring keys -> the low and the high halves' columns.
 #pragma unroll
-    for (int w = 0; w < Tile<D>::kWords; ++w) {
+    for (int x = 0; x < Tile<D>::kWords; ++x) {
       u32x4v even, odd;
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        even[e] = __builtin_amdgcn_perm(now.v[2 * e + 1][w], now.v[2 * e][w], 0x05040100u);
-        odd[e] = __builtin_amdgcn_perm(now.v[2 * e + 1][w], now.v[2 * e][w], 0x07060302u);
+        even[e] = __builtin_amdgcn_perm(tile.v[2 * e + 1][x], tile.v[2 * e][x], 0x05040100u);
+        odd[e] = __builtin_amdgcn_perm(tile.v[2 * e + 1][x], tile.v[2 * e][x], 0x07060302u);
       }
 #pragma unroll
       for (int t = 0; t < T; ++t) {
-        o[t][2 * w] = dev::mfma_bf16(even, pw[t], o[t][2 * w]);
-        o[t][2 * w + 1] = dev::mfma_bf16(odd, pw[t], o[t][2 * w + 1]);
+        o[t][2 * x] = dev::mfma_bf16(even, pw[t], o[t][2 * x]);
+        o[t][2 * x + 1] = dev::mfma_bf16(odd, pw[t], o[t][2 * x + 1]);
       }
     }
-    if (!plain && odd_v) {               // rare: the words taken out above, row by row
+    if (!kPlain && odd_v) {              // rare: the words taken out above, row by row
       for (int kk = 0; kk < 32; ++kk) {
-        if (k0 + kk >= hi || !(kk < 16 ? held_now[0] : held_now[1])) continue;
-        const uint16_t* vp = p.V + (kk < 16 ? base_now[0] : base_now[1]) + (kk & 15) * D;
+        if (k0 + kk >= w.hi || !(kk < 16 ? held0 : held1)) continue;
+        const uint16_t* vp = p.V + (kk < 16 ? base0 : base1) + (kk & 15) * D;
         const int from = 16 * ((kk & 15) >> 2) + r, e = 4 * (kk >> 4) + (kk & 3);
 #pragma unroll
         for (int t = 0; t < T; ++t) {
@@ -327,58 +310,266 @@ __global__ __launch_bounds__(kThreads, T == 1 && D <= 128 ? 2 : 1) void tree_att
         }
       }
     }
-    if (step + 1 < steps) now = next;
   }
+};
+
+// Element offset of the 16-key block with key `key` on page `page` of the pool.  A block
+// past the keys, or on a page outside the pool (-1), reads the pool's first page, and its
+// keys are not seen.
+template <int D>
+__device__ __forceinline__ int64_t block_base(const TreeArgs& p, int h, int page, int key) {
+  return max(page, 0) * p.page_stride +
+         ((static_cast<int64_t>(h) << p.page_shift) + (key & ((1 << p.page_shift) - 1))) * D;
+}
+
+// The page of the block at `key`, -1 where there is none.
+__device__ __forceinline__ int page_entry(const TreeArgs& p, const Part& w, int key) {
+  const int page = key < w.hi ? p.pages[w.at.segment * p.ld_pages + (key >> p.page_shift)] : -1;
+  return page < p.num_pages ? page : -1;
+}
+
+// Up to 16 query columns: the waves take every fourth 32 keys each, straight into
+// registers, the next ones under way, and join through LDS at the end.
+template <int D>
+__global__ __launch_bounds__(kThreads, D <= 128 ? 2 : 1) void tree_attention_kernel(const TreeArgs p) {
+  constexpr int kV = D / 16, kPitch = D + 4;
+  __shared__ __align__(16) float sh_o[kWaves][16][kPitch];
+  __shared__ float sh_m[kWaves][16], sh_l[kWaves][16];
+  Part w;
+  if (!find_part(p, 16, &w)) return;
+  const int lane = static_cast<int>(threadIdx.x) & 63, r = lane & 15, g = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x) >> 6);
+  const int first = w.lo + 32 * wave;
+  const int steps = w.hi > first ? (w.hi - first + kStep - 1) / kStep : 0;
+  // lane 2 s + b: page of block b of step s (of 32 steps)
+  int entries = page_entry(p, w, first + kStep * (lane >> 1) + 16 * (lane & 1));
+  int64_t base[2];
+  bool held[2];
+  auto find = [&](int step) {
+#pragma unroll
+    for (int b = 0; b < 2; ++b) {
+      const int page = __builtin_amdgcn_readlane(entries, 2 * (step & 31) + b);
+      held[b] = page >= 0;
+      base[b] = block_base<D>(p, w.h, page, first + kStep * step + 16 * b);
+    }
+  };
+  Wave<D, 1> q;
+  q.start(p, w, w.c0);
+  Tile<D> now, next;
+  if (steps > 0) {
+    find(0);
+    load_tile<D>(p, base, &now);
+  }
+  auto one = [&](int step, auto plain) {
+    const bool held0 = held[0], held1 = held[1];
+    const int64_t base0 = base[0], base1 = base[1];
+    if (step + 1 < steps) {
+      if (((step + 1) & 31) == 0)
+        entries = page_entry(p, w, first + kStep * (step + 1 + (lane >> 1)) + 16 * (lane & 1));
+      find(step + 1);
+      load_tile<D>(p, base, &next);
+    }
+    q.template step<decltype(plain)::value>(p, w, now, first + kStep * step, held0, held1, base0, base1);
+    if (step + 1 < steps) now = next;
+  };
+  // every row sees the whole step: of cached tokens alone, on pages of the pool
+  int step = 0;
+  for (; step < steps && first + kStep * step + 32 <= min(w.cached, w.hi) && held[0] && held[1]; ++step)
+    one(step, std::true_type{});
+  for (; step < steps; ++step) one(step, std::false_type{});
 
   // Join the waves.
-#pragma unroll
-  for (int t = 0; t < T; ++t) {
-    l[t] += __shfl_xor(l[t], 16);
-    l[t] += __shfl_xor(l[t], 32);
-    if (g == 0) {
-      sh_m[wave][16 * t + r] = m[t];
-      sh_l[wave][16 * t + r] = l[t];
-    }
+  float l = q.l[0];
+  l += __shfl_xor(l, 16);
+  l += __shfl_xor(l, 32);
+  if (g == 0) {
+    sh_m[wave][r] = q.m[0];
+    sh_l[wave][r] = l;
   }
   __syncthreads();
+  const float a = exp2_from(q.m[0], fmaxf(fmaxf(sh_m[0][r], sh_m[1][r]), fmaxf(sh_m[2][r], sh_m[3][r])), p.scale);
 #pragma unroll
-  for (int t = 0; t < T; ++t) {
-    const int c = 16 * t + r;
-    const float top = fmaxf(fmaxf(sh_m[0][c], sh_m[1][c]), fmaxf(sh_m[2][c], sh_m[3][c]));
-    const float a = exp2_from(m[t], top);
+  for (int i = 0; i < 4; ++i)
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
-#pragma unroll
-      for (int v = 0; v < kV; v += 4)
-        *reinterpret_cast<f32x4*>(&sh_o[wave][c][kV * (4 * g + i) + v]) =
-            f32x4{o[t][v][i], o[t][v + 1][i], o[t][v + 2][i], o[t][v + 3][i]} * a;
-  }
+    for (int v = 0; v < kV; v += 4)
+      *reinterpret_cast<f32x4*>(&sh_o[wave][r][kV * (4 * g + i) + v]) =
+          f32x4{q.o[0][v][i], q.o[0][v + 1][i], q.o[0][v + 2][i], q.o[0][v + 3][i]} * a;
   __syncthreads();
   constexpr int kPer = D / 8;            // threads a column
-  for (int x = static_cast<int>(threadIdx.x); x < cols * kPer; x += kThreads) {
+  for (int x = static_cast<int>(threadIdx.x); x < w.cols * kPer; x += kThreads) {
     const int c = x / kPer, d = 8 * (x % kPer);
     const float top = fmaxf(fmaxf(sh_m[0][c], sh_m[1][c]), fmaxf(sh_m[2][c], sh_m[3][c]));
     float sum = 0.f;
-    f32x4 a = {0.f, 0.f, 0.f, 0.f}, b = a;
+    f32x4 lo = {0.f, 0.f, 0.f, 0.f}, hi = lo;
 #pragma unroll
-    for (int w = 0; w < kWaves; ++w) {
-      sum += sh_l[w][c] * exp2_from(sh_m[w][c], top);
-      a += *reinterpret_cast<const f32x4*>(&sh_o[w][c][d]);
-      b += *reinterpret_cast<const f32x4*>(&sh_o[w][c][d + 4]);
+    for (int y = 0; y < kWaves; ++y) {
+      sum += sh_l[y][c] * exp2_from(sh_m[y][c], top, p.scale);
+      lo += *reinterpret_cast<const f32x4*>(&sh_o[y][c][d]);
+      hi += *reinterpret_cast<const f32x4*>(&sh_o[y][c][d + 4]);
     }
-    const int64_t row = at.first + (c0 + c) / p.G;
-    const int64_t head = row * p.Hq + h * p.G + (c0 + c) % p.G;
+    const int64_t head = (w.at.first + (w.c0 + c) / p.G) * static_cast<int64_t>(p.Hq) + w.h * p.G + (w.c0 + c) % p.G;
     if (p.splits == 1) {
       const float inv = sum == 0.f ? 0.f : 1.0f / sum;
-      const u32x4v w = {dev::pack_bf16(a[0] * inv, a[1] * inv), dev::pack_bf16(a[2] * inv, a[3] * inv),
-                        dev::pack_bf16(b[0] * inv, b[1] * inv), dev::pack_bf16(b[2] * inv, b[3] * inv)};
-      *reinterpret_cast<u32x4v*>(p.out + head * D + d) = w;
-      if (p.lse && d == 0) p.lse[head] = sum == 0.f ? kNone : (top + log2f(sum)) * 0.69314718055994531f;
+      const u32x4v y = {dev::pack_bf16(lo[0] * inv, lo[1] * inv), dev::pack_bf16(lo[2] * inv, lo[3] * inv),
+                        dev::pack_bf16(hi[0] * inv, hi[1] * inv), dev::pack_bf16(hi[2] * inv, hi[3] * inv)};
+      *reinterpret_cast<u32x4v*>(p.out + head * D + d) = y;
+      if (p.lse && d == 0) p.lse[head] = sum == 0.f ? kNone : (top * p.scale + log2f(sum)) * 0.69314718055994531f;
     } else {
-      const int64_t part = split * static_cast<int64_t>(p.M) * p.Hq + head;
-      *reinterpret_cast<f32x4*>(p.part_o + part * D + d) = a;
-      *reinterpret_cast<f32x4*>(p.part_o + part * D + d + 4) = b;
-      if (d == 0) p.part_ml[part] = {top, sum};
+      const int64_t part = w.split * static_cast<int64_t>(p.M) * p.Hq + head;
+      *reinterpret_cast<f32x4*>(p.part_o + part * D + d) = lo;
+      *reinterpret_cast<f32x4*>(p.part_o + part * D + d + 4) = hi;
+      if (d == 0) p.part_ml[part] = {top * p.scale, sum};
+    }
+  }
+}
+
+// More columns: each wave its own T tiles of them, all waves the same keys, K and V staged
+// in LDS (two stages of kKeys keys; a row's 16-byte units permuted by its number, so
+// that neither the K reads, a column of rows, nor the V reads, a whole row, conflict).
+template <int D, int T>
+__global__ __launch_bounds__(kThreads, D <= 128 ? 2 : 1) void tree_attention_wide_kernel(const TreeArgs p) {
+  constexpr int kV = D / 16, kKeys = D <= 128 ? 64 : 32;
+  constexpr int kUnits = D / 8, kRows = kThreads / kUnits, kPasses = kKeys / kRows;
+  __shared__ __align__(16) uint16_t sh[2][2][kKeys * D];     // stage, K or V
+  Part w;
+  if (!find_part(p, 16 * T * kWaves, &w)) return;
+  const int lane = static_cast<int>(threadIdx.x) & 63, r = lane & 15, g = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x) >> 6);
+  // Unit u of row k lies at unit u ^ turn(k).
+  auto turn = [](int k) { return D == 64 ? (k >> 1) & 7 : k & 15; };
+
+  int entries = page_entry(p, w, w.lo + 16 * lane);          // lane b: page of block b (of 64)
+  Wave<D, T> q;
+  q.start(p, w, w.c0 + 16 * T * wave);
+  const bool works = 16 * T * wave < w.cols;                 // else the wave only helps to load
+
+  const int unit = static_cast<int>(threadIdx.x) % kUnits, row = static_cast<int>(threadIdx.x) / kUnits;
+  u32x4v k_in[kPasses], v_in[kPasses];
+  auto load = [&](int stage) {           // stage's rows row, row + kRows, ... of K and V
+#pragma unroll
+    for (int x = 0; x < kPasses; ++x) {
+      const int k = kRows * x + row;     // its block is the same for the wave
+      const int block = __builtin_amdgcn_readfirstlane(k >> 4);
+      const int page = __builtin_amdgcn_readlane(entries, (stage * (kKeys / 16) + block) & 63);
+      const int64_t at = block_base<D>(p, w.h, page, w.lo + kKeys * stage + 16 * block) + (k & 15) * D + 8 * unit;
+      k_in[x] = *reinterpret_cast<const u32x4v*>(p.K + at);
+      v_in[x] = *reinterpret_cast<const u32x4v*>(p.V + at);
+    }
+  };
+  auto store = [&](int stage) {
+#pragma unroll
+    for (int x = 0; x < kPasses; ++x) {
+      const int k = kRows * x + row;
+      const int at = k * D + 8 * (unit ^ turn(k));
+      *reinterpret_cast<u32x4v*>(&sh[stage & 1][0][at]) = k_in[x];
+      *reinterpret_cast<u32x4v*>(&sh[stage & 1][1][at]) = v_in[x];
+    }
+  };
+  const int stages = (w.hi - w.lo + kKeys - 1) / kKeys;
+  // Stages that every row sees whole: of cached tokens alone, on pages of the pool (as far
+  // as the entries at hand say).
+  int plain = max(min(w.cached, w.hi) - w.lo, 0) / kKeys;
+  auto check = [&](int stage) {
+    if (__any(w.lo + kKeys * stage + 16 * lane < w.hi && entries < 0)) plain = min(plain, stage);
+  };
+  check(0);
+  if (stages > 0) {
+    load(0);
+    store(0);
+  }
+  // A lane's places in a stage (elements): rows r of a 16-key block of K, 4 g + i of V; the
+  // blocks are 16 rows apart, and turn(k) has k's low bits alone.
+  int k_at[Tile<D>::kChunks], v_at[4];
+#pragma unroll
+  for (int c = 0; c < Tile<D>::kChunks; ++c) k_at[c] = r * D + 8 * ((4 * c + g) ^ turn(r));
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int k = 4 * g + i;
+    v_at[i] = k * D + (D == 64 ? 8 * ((r >> 1) ^ turn(k)) + 4 * (r & 1) : 8 * ((D / 128 * r) ^ turn(k)));
+  }
+  auto one = [&](int stage, auto all) {
+    __syncthreads();
+    const int entries_now = entries;
+    if (stage + 1 < stages) {
+      if (((stage + 1) * (kKeys / 16) & 63) == 0) {
+        entries = page_entry(p, w, w.lo + kKeys * (stage + 1) + 16 * lane);
+        check(stage + 1);
+      }
+      load(stage + 1);
+    }
+    if (works) {
+#pragma unroll 1
+      for (int half = 0; half < kKeys / 32; ++half) {
+        const int k0 = w.lo + kKeys * stage + 32 * half;
+        if (!decltype(all)::value && k0 >= w.hi) break;
+        const uint16_t* const ks = sh[stage & 1][0] + 32 * half * D;
+        const uint16_t* const vs = sh[stage & 1][1] + 32 * half * D;
+        Tile<D> tile;
+#pragma unroll
+        for (int b = 0; b < 2; ++b) {
+#pragma unroll
+          for (int c = 0; c < Tile<D>::kChunks; ++c)
+            tile.k[b][c] = *reinterpret_cast<const u32x4v*>(ks + k_at[c] + 16 * b * D);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            if constexpr (D <= 128) {
+              load_v<D>(vs + v_at[i] + 16 * b * D, tile.v[4 * b + i]);
+            } else {                     // the row's second unit lies at the first one's neighbour
+#pragma unroll
+              for (int c = 0; c < 2; ++c) {
+                const u32x4v x = *reinterpret_cast<const u32x4v*>(vs + (v_at[i] ^ (8 * c)) + 16 * b * D);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) tile.v[4 * b + i][4 * c + e] = x[e];
+              }
+            }
+          }
+        }
+        int page0 = 0, page1 = 0;
+        if constexpr (!decltype(all)::value) {
+          const int block = (stage * (kKeys / 16) + 2 * half) & 63;
+          page0 = __builtin_amdgcn_readlane(entries_now, block);
+          page1 = __builtin_amdgcn_readlane(entries_now, block + 1);
+        }
+        q.template step<decltype(all)::value>(p, w, tile, k0, page0 >= 0, page1 >= 0,
+                                              block_base<D>(p, w.h, page0, k0),
+                                              block_base<D>(p, w.h, page1, k0 + 16));
+      }
+    }
+    if (stage + 1 < stages) store(stage + 1);
+  };
+  int stage = 0;
+  for (; stage < plain; ++stage) one(stage, std::true_type{});
+  for (; stage < stages; ++stage) one(stage, std::false_type{});
+
+#pragma unroll
+  for (int t = 0; t < T; ++t) {
+    float sum = q.l[t];
+    sum += __shfl_xor(sum, 16);
+    sum += __shfl_xor(sum, 32);
+    const int c = 16 * (T * wave + t) + r;
+    if (c >= w.cols) continue;
+    const int64_t head = (w.at.first + (w.c0 + c) / p.G) * static_cast<int64_t>(p.Hq) + w.h * p.G + (w.c0 + c) % p.G;
+    const float top = q.m[t] * p.scale;
+    if (p.splits == 1) {
+      const float inv = sum == 0.f ? 0.f : 1.0f / sum;
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int v = 0; v < kV; v += 4) {
+          const dev::u32x2 y = {dev::pack_bf16(q.o[t][v][i] * inv, q.o[t][v + 1][i] * inv),
+                                dev::pack_bf16(q.o[t][v + 2][i] * inv, q.o[t][v + 3][i] * inv)};
+          *reinterpret_cast<dev::u32x2*>(p.out + head * D + kV * (4 * g + i) + v) = y;
+        }
+      if (p.lse && g == 0) p.lse[head] = sum == 0.f ? kNone : (top + log2f(sum)) * 0.69314718055994531f;
+    } else {
+      const int64_t part = w.split * static_cast<int64_t>(p.M) * p.Hq + head;
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int v = 0; v < kV; v += 4)
+          *reinterpret_cast<f32x4*>(p.part_o + part * D + kV * (4 * g + i) + v) =
+              f32x4{q.o[t][v][i], q.o[t][v + 1][i], q.o[t][v + 2][i], q.o[t][v + 3][i]};
+      if (g == 0) p.part_ml[part] = {top, sum};
     }
   }
 }
@@ -389,25 +580,38 @@ __global__ __launch_bounds__(kThreads) void tree_join_kernel(const float* __rest
                                                              const float2* __restrict__ part_ml, int64_t heads,
                                                              int splits, uint16_t* __restrict__ out,
                                                              float* __restrict__ lse) {
-  constexpr int kPer = D / 4, kAtOnce = 64 / kPer;     // lanes a split, splits at a time
+  constexpr int kPer = D / 4, kAtOnce = 64 / kPer;     // lanes a split, splits a load
+  constexpr int kBatch = 8;                            // loads under way
   const int lane = static_cast<int>(threadIdx.x) & 63;
   const int64_t head = static_cast<int64_t>(blockIdx.x) * kWaves + (threadIdx.x >> 6);
   if (head >= heads) return;
   float2 ml = {kNone, 0.f};
   if (lane < splits) ml = part_ml[lane * heads + head];
+  f32x4 in[kBatch];
+  auto load = [&](int s0) {
+#pragma unroll
+    for (int x = 0; x < kBatch; ++x) {
+      const int s = min(s0 + x * kAtOnce + lane / kPer, splits - 1);
+      in[x] = *reinterpret_cast<const f32x4*>(part_o + (s * heads + head) * D + 4 * (lane % kPer));
+    }
+  };
+  load(0);
   float top = ml.x;
 #pragma unroll
   for (int d = 32; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor(top, d));
-  const float a = exp2_from(ml.x, top);
+  const float a = exp2_from(ml.x, top, 1.0f);
   float sum = a * ml.y;
 #pragma unroll
   for (int d = 32; d > 0; d >>= 1) sum += __shfl_xor(sum, d);
   f32x4 o = {0.f, 0.f, 0.f, 0.f};
-  for (int s0 = 0; s0 < splits; s0 += kAtOnce) {
-    const int s = s0 + lane / kPer;
-    const float w = __shfl(a, s & 63);
-    if (s < splits && w != 0.f)          // a split with nothing for this row wrote no O
-      o += w * *reinterpret_cast<const f32x4*>(part_o + (s * heads + head) * D + 4 * (lane % kPer));
+  for (int s0 = 0; s0 < splits; s0 += kBatch * kAtOnce) {
+    if (s0 > 0) load(s0);
+#pragma unroll
+    for (int x = 0; x < kBatch; ++x) {
+      const int s = s0 + x * kAtOnce + lane / kPer;
+      const float w = __shfl(a, s & 63);
+      if (s < splits && w != 0.f) o += w * in[x];      // a split with nothing for this row wrote no O
+    }
   }
 #pragma unroll
   for (int d = kPer; d < 64; d <<= 1)
@@ -425,10 +629,11 @@ template <int D>
 void launch(const TreeArgs& p, int tile_cols, int64_t blocks, hipStream_t stream) {
   const dim3 grid(static_cast<unsigned>(blocks));
   if (tile_cols == 16)
-    tree_attention_kernel<D, 1><<<grid, kThreads, 0, stream>>>(p);
+    tree_attention_kernel<D><<<grid, kThreads, 0, stream>>>(p);
+  else if (tile_cols == 64)
+    tree_attention_wide_kernel<D, 1><<<grid, kThreads, 0, stream>>>(p);
   else if constexpr (D <= 128)
-    tile_cols == 32 ? tree_attention_kernel<D, 2><<<grid, kThreads, 0, stream>>>(p)
-                    : tree_attention_kernel<D, 4><<<grid, kThreads, 0, stream>>>(p);
+    tree_attention_wide_kernel<D, 2><<<grid, kThreads, 0, stream>>>(p);
   if (p.splits > 1) {
     const int64_t heads = static_cast<int64_t>(p.M) * p.Hq;
     tree_join_kernel<D><<<dim3(static_cast<unsigned>((heads + kWaves - 1) / kWaves)), kThreads, 0, stream>>>(
@@ -443,14 +648,13 @@ TreePlan plan_tree_attention(int M, int B, int Hq, int Hk, int D, int max_kv_len
   const int64_t G = Hq / Hk;
   const int64_t used = std::max(1, std::min(M, B));
   const int64_t per = (M * G + used - 1) / used;        // query columns of a mean request
-  c.tile_cols = per <= 16 || D > 128 ? 16 : per <= 32 ? 32 : 64;
+  c.tile_cols = per <= 16 ? 16 : per <= 64 || D > 128 ? 64 : 128;
   c.tiles = most_tiles(M, B, G, c.tile_cols);
   const int64_t groups = c.tiles * Hk;
   const int64_t want = (4 * static_cast<int64_t>(num_cus) + groups - 1) / groups;
   const int64_t keys = std::max(max_kv_len, 1);
-  const int64_t splits = std::max<int64_t>(1, std::min({want, static_cast<int64_t>(kMaxSplits), (keys + kStep - 1) / kStep}));
-  c.split_len = static_cast<int>(((keys + splits - 1) / splits + kStep - 1) / kStep * kStep);
-  c.splits = static_cast<int>((keys + c.split_len - 1) / c.split_len);
+  const int64_t most = std::min<int64_t>(kMaxSplits, (keys + kStep - 1) / kStep);
+  c.splits = static_cast<int>(std::max<int64_t>(1, std::min(want, most)));
   c.blocks = groups * c.splits;
   return c;
 }
@@ -467,9 +671,12 @@ hipError_t launch_tree_attention(const TreePlan& c, const uint16_t* q, int64_t l
   const int64_t heads = static_cast<int64_t>(M) * Hq;
   float* const part_o = static_cast<float*>(workspace);
   float2* const part_ml = c.splits > 1 ? reinterpret_cast<float2*>(part_o + c.splits * heads * D) : nullptr;
+  // A negative scale turns the queries' signs; 0 is as good as the smallest used here
+  // (q . k times it vanishes beside 1) and keeps an unseen -inf from becoming 0 x inf.
+  const float size = std::max(std::fabs(scale) * 1.44269504088896341f, 0x1p-100f);
   const TreeArgs p{q, ld_q, cache.K, cache.V, cache.page_stride, cache.page_shift, cache.num_pages, pages, ld_pages,
-                   max_keys, cached, offsets, mask, ld_mask, mask_wide, scale * 1.44269504088896341f, out, lse,
-                   part_o, part_ml, M, B, Hq, Hk, Hq / Hk, static_cast<int>(c.tiles), c.splits, c.split_len};
+                   max_keys, cached, offsets, mask, ld_mask, mask_wide, size, kSlack / size,
+                   std::signbit(scale) ? 0x80008000u : 0u, out, lse, part_o, part_ml, M, B, Hq, Hk, Hq / Hk, static_cast<int>(c.tiles), c.splits};
   if (D == 64) launch<64>(p, c.tile_cols, c.blocks, stream);
   else if (D == 128) launch<128>(p, c.tile_cols, c.blocks, stream);
   else launch<256>(p, c.tile_cols, c.blocks, stream);
