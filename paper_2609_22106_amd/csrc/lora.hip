@@ -4,10 +4,16 @@
 // Y and out float32 [M, N] (out may be Y), x bf16 [M, K].
 //
 // Two products with the rank between them, in two kernels: `down` forms
-// t = A_a x over ranges of K (a workgroup per 16 rows of one segment and range, so
+// t = A_a x over ranges of K (a workgroup per 16 or 32 rows of one segment and range, so
 // that a few decoding rows still occupy the chip; partial sums in the workspace) and
 // `up` adds them in order, scales and multiplies by B_a.  The bytes of Y and out bound
 // long prompts; the adapters' own bytes and the two launches a decoding step.
+//
+// An operand's neighbouring lanes hold different rows, so operands loaded straight from
+// rows in memory use 16 of the 64 bytes a clock of a CU's first cache: rows are loaded
+// whole and pass through LDS instead (64 requests, ranks up to 64, K = 9728: `down` 13.3
+// -> 8.4 us), and `up` of many rows lays its columns out so that 16 lanes load and store 256
+// bytes of a row of Y (8192 rows x 9728 columns: 167 -> 126 us).
 //
 // t stays float32: `up` splits each value into three bf16 terms (8 + 8 + 8 bits, the
 // remainders exact), and three bf16 MFMAs add their products with B_a, so that the
@@ -26,6 +32,7 @@ using dev::f32x4;
 using dev::u32x4v;
 
 constexpr int kWaves = 4, kThreads = 64 * kWaves;
+constexpr int kMaxRanges = 8;            // of K
 
 struct LoraArgs {
   const uint16_t* x;
@@ -41,14 +48,14 @@ struct LoraArgs {
   int adapters, rank_rows, segments, M, N, K, max_rank, splits, k_per;
 };
 
-// The adapter of a segment: its first rank row and its rank, 0 where it has none (or
+// An adapter: its first rank row and its rank, 0 where it has none (or
 // where the tables name one that A and B do not hold).
 struct Adapter {
   int index, first, rank;
 };
 
-__device__ __forceinline__ Adapter adapter_of(const LoraArgs& p, int segment) {
-  Adapter a{p.of[segment], 0, 0};
+__device__ __forceinline__ Adapter adapter_of(const LoraArgs& p, int index) {
+  Adapter a{index, 0, 0};
   if (a.index < 0 || a.index >= p.adapters) return a;
   const int first = p.rank_offsets[a.index], end = p.rank_offsets[a.index + 1];
   if (first < 0 || end > p.rank_rows || end - first > p.max_rank || ((first | end) & 7)) return a;
@@ -57,55 +64,110 @@ __device__ __forceinline__ Adapter adapter_of(const LoraArgs& p, int segment) {
   return a;
 }
 
-// t of 16 rows over one range of K.  The waves take every fourth 32-element step, all
-// ranks each, and are joined through LDS.
-template <int kRankTiles>
-__global__ __launch_bounds__(kThreads) void lora_down_kernel(const LoraArgs p) {
-  __shared__ f32x4 sh[kWaves][kRankTiles][64];
+// t of 16 kRowTiles rows over one range of K, for up to 16 kTiles ranks from `rank0` on.
+// The waves take every kWaves-th step of 64 elements.  A row's 128 bytes of a step are
+// loaded by 8 neighbouring lanes -- an operand's own lanes, each on another row, would
+// take the first cache four times as long -- and reach their operand's place through a
+// part of LDS of the wave's own (unit u of row k at u ^ (k / 2 & 7): no conflicts).
+template <int kRowTiles, int kTiles>
+__device__ __forceinline__ void down_rows(const LoraArgs& p, const Adapter& ad, int64_t row0, int rows, int rank0,
+                                          u32x4v* sh) {
+  constexpr int kLoads = 2 * (kRowTiles + kTiles);           // of 8 rows, a step
+  constexpr int kAtOnce = kLoads <= 6 ? 4 : 2;               // steps under way
   const int lane = static_cast<int>(threadIdx.x) & 63, r = lane & 15, g = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x) >> 6);
-  const dev::TileAt at = dev::find_tile(p.offsets, p.of, p.segments, p.M, static_cast<int>(blockIdx.y), 1, 16);
+  const int k0 = static_cast<int>(blockIdx.x) * p.k_per, end = min(k0 + p.k_per, p.K);
+  const int lr = lane >> 3, unit = lane & 7;
+  // rows and ranks past the end read the last one and are not used
+  const uint16_t* src[kLoads];
+#pragma unroll
+  for (int i = 0; i < 2 * kRowTiles; ++i) src[i] = p.x + (row0 + min(8 * i + lr, rows - 1)) * p.ld_x;
+#pragma unroll
+  for (int i = 0; i < 2 * kTiles; ++i)
+    src[2 * kRowTiles + i] = p.A + static_cast<int64_t>(ad.first + min(rank0 + 8 * i + lr, ad.rank - 1)) * p.K;
+  u32x4v* const mine = sh + wave * kLoads * 64;
+  f32x4 acc[kRowTiles][kTiles];
+#pragma unroll
+  for (int a = 0; a < kRowTiles; ++a)
+#pragma unroll
+    for (int j = 0; j < kTiles; ++j) acc[a][j] = {0.f, 0.f, 0.f, 0.f};
+  const u32x4v none = {0, 0, 0, 0};
+  for (int k = k0 + 64 * wave; k < end; k += kAtOnce * 64 * kWaves) {
+    u32x4v in[kAtOnce][kLoads];
+#pragma unroll
+    for (int s = 0; s < kAtOnce; ++s) {
+      const int at = k + s * 64 * kWaves + 8 * unit;         // K % 8 == 0: a unit is whole or absent
+#pragma unroll
+      for (int i = 0; i < kLoads; ++i) in[s][i] = *reinterpret_cast<const u32x4v*>(src[i] + (at < end ? at : 0));
+    }
+#pragma unroll
+    for (int s = 0; s < kAtOnce; ++s) {
+      if (s && k + s * 64 * kWaves >= end) break;
+      const bool here = k + s * 64 * kWaves + 8 * unit < end;
+#pragma unroll
+      for (int i = 0; i < kLoads; ++i)
+        mine[(8 * i + lr) * 8 + (unit ^ ((8 * i + lr) >> 1 & 7))] = here ? in[s][i] : none;
+      __builtin_amdgcn_wave_barrier();
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        u32x4v x[kRowTiles];
+#pragma unroll
+        for (int a = 0; a < kRowTiles; ++a) x[a] = mine[(16 * a + r) * 8 + ((4 * h + g) ^ (r >> 1))];
+#pragma unroll
+        for (int j = 0; j < kTiles; ++j) {
+          const u32x4v w = mine[(16 * (kRowTiles + j) + r) * 8 + ((4 * h + g) ^ (r >> 1))];
+#pragma unroll
+          for (int a = 0; a < kRowTiles; ++a) acc[a][j] = dev::mfma_bf16(x[a], w, acc[a][j]);
+        }
+      }
+      __builtin_amdgcn_wave_barrier();
+    }
+  }
+  // Join the waves, 16 rows at a time: sum[w][j][16 g + c][i] is row 4 g + i, rank 16 j + c.
+  f32x4* const sum = reinterpret_cast<f32x4*>(sh);
+  float* const t = p.t + (static_cast<int64_t>(blockIdx.x) * p.M + row0) * p.max_rank + rank0;
+#pragma unroll
+  for (int a = 0; a < kRowTiles; ++a) {
+    __syncthreads();
+#pragma unroll
+    for (int j = 0; j < kTiles; ++j) sum[(wave * kTiles + j) * 64 + lane] = acc[a][j];
+    __syncthreads();
+#pragma unroll
+    for (int e = static_cast<int>(threadIdx.x); e < 256 * kTiles; e += kThreads) {
+      const int rank = e % (16 * kTiles), row = e / (16 * kTiles);
+      if (16 * a + row < rows && rank0 + rank < ad.rank) {
+        float x = 0.f;
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w)
+          x += sum[(w * kTiles + (rank >> 4)) * 64 + 16 * (row >> 2) + (rank & 15)][row & 3];
+        t[(16 * a + row) * p.max_rank + rank] = x;
+      }
+    }
+  }
+}
+
+template <int kRowTiles, int kMost>
+__global__ __launch_bounds__(kThreads) void lora_down_kernel(const LoraArgs p) {
+  __shared__ u32x4v sh[kWaves * 2 * (kRowTiles + kMost) * 64];
+  const dev::TileAt at = dev::find_tile(p.offsets, p.of, p.segments, p.M, static_cast<int>(blockIdx.y), 1,
+                                        16 * kRowTiles);
   if (at.segment < 0) return;
-  const Adapter ad = adapter_of(p, at.segment);
+  const Adapter ad = adapter_of(p, at.with);
   if (ad.rank <= 0) return;
-  const int rows = min(at.rows - 16 * at.tile, 16);
-  const int64_t row0 = at.first + 16 * at.tile;
-  const int k0 = static_cast<int>(blockIdx.x) * p.k_per, k1 = min(k0 + p.k_per, p.K);
-  // A operand: x's rows; B operand: the adapter's rank rows.  Rows and ranks past the
-  // end read the last one and are not stored.
-  const uint16_t* xp = p.x + (row0 + min(r, rows - 1)) * p.ld_x + 8 * g;
-  const uint16_t* ap[kRankTiles];
-#pragma unroll
-  for (int j = 0; j < kRankTiles; ++j)
-    ap[j] = p.A + static_cast<int64_t>(ad.first + min(16 * j + r, ad.rank - 1)) * p.K + 8 * g;
-  f32x4 acc[kRankTiles];
-#pragma unroll
-  for (int j = 0; j < kRankTiles; ++j) acc[j] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll 2
-  for (int k = k0 + 32 * wave; k < k1; k += 32 * kWaves) {
-    const u32x4v none = {0, 0, 0, 0};
-    const bool in = k + 8 * g < k1;      // K % 8 == 0: a group of 8 is whole or absent
-    const u32x4v xa = in ? *reinterpret_cast<const u32x4v*>(xp + k) : none;
-#pragma unroll
-    for (int j = 0; j < kRankTiles; ++j) {
-      const u32x4v b = in ? *reinterpret_cast<const u32x4v*>(ap[j] + k) : none;
-      acc[j] = dev::mfma_bf16(xa, b, acc[j]);
+  const int rows = min(at.rows - 16 * kRowTiles * at.tile, 16 * kRowTiles);
+  const int64_t row0 = at.first + 16 * kRowTiles * at.tile;
+  // this adapter's own rank, not the largest one, says what is read; 64 ranks at a time
+  int rank0 = 0;
+  if constexpr (kMost == 4)
+    for (; ad.rank - rank0 > 32; rank0 += 64) {
+      if (rank0) __syncthreads();
+      down_rows<kRowTiles, 4>(p, ad, row0, rows, rank0, sh);
     }
-  }
-#pragma unroll
-  for (int j = 0; j < kRankTiles; ++j) sh[wave][j][lane] = acc[j];
-  __syncthreads();
-  // sh[.][j][16 g + c][i] is row 4 g + i, rank 16 j + c
-  float* const t = p.t + (static_cast<int64_t>(blockIdx.x) * p.M + row0) * p.max_rank;
-  for (int e = static_cast<int>(threadIdx.x); e < 256 * kRankTiles; e += kThreads) {
-    const int rank = e % (16 * kRankTiles), row = e / (16 * kRankTiles);
-    if (row < rows && rank < ad.rank) {
-      float sum = 0.f;
-#pragma unroll
-      for (int w = 0; w < kWaves; ++w) sum += sh[w][rank >> 4][16 * (row >> 2) + (rank & 15)][row & 3];
-      t[row * p.max_rank + rank] = sum;
-    }
-  }
+  if (ad.rank <= rank0) return;
+  if (rank0) __syncthreads();
+  if constexpr (kMost >= 2)
+    if (ad.rank - rank0 > 16) return down_rows<kRowTiles, 2>(p, ad, row0, rows, rank0, sh);
+  down_rows<kRowTiles, 1>(p, ad, row0, rows, rank0, sh);
 }
 
 // x's three bf16 terms: x = a + b + c up to 2^-24 of x.  An infinity or a NaN is a's alone.
@@ -119,90 +181,234 @@ __device__ __forceinline__ void split3(float x, float (&part)[3]) {
   part[2] = finite ? rest - b : 0.f;
 }
 
-// Y's rows of kRowTiles * 16 rows of one segment, columns of one slice: A operand
-// B_a's rows (16 columns of Y), B operand t's rows, so that a lane holds 4
-// neighbouring columns of one row.
-template <int kSteps, int kRowTiles>
+// lo, hi: ranks 8 g .. + 7 of one 32-rank step, scaled -> the step's three B operands.
+__device__ __forceinline__ void split_operand(f32x4 lo, f32x4 hi, u32x4v (&out)[3]) {
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    float one[3], two[3];
+    split3(e < 2 ? lo[2 * e] : hi[2 * e - 4], one);
+    split3(e < 2 ? lo[2 * e + 1] : hi[2 * e - 3], two);
+#pragma unroll
+    for (int w = 0; w < 3; ++w) out[w][e] = dev::pack_bf16(one[w], two[w]);
+  }
+}
+
+// Quadruple `quad` of t's row `row` of the tile: the ranges of K added in order, scaled; 0
+// past the rank and the rows.
+__device__ __forceinline__ f32x4 join_ranges(const LoraArgs& p, const Adapter& ad, int64_t row0, int row, int rows,
+                                             int quad, float scale) {
+  f32x4 sum = {0.f, 0.f, 0.f, 0.f};
+  if (row < rows && 4 * quad < ad.rank) {
+    const float* tp = p.t + (row0 + row) * p.max_rank + 4 * quad;
+    const int64_t next_range = static_cast<int64_t>(p.M) * p.max_rank;
+    f32x4 in[kMaxRanges];
+#pragma unroll
+    for (int s = 0; s < kMaxRanges; ++s) in[s] = *reinterpret_cast<const f32x4*>(tp + min(s, p.splits - 1) * next_range);
+    sum = in[0];
+#pragma unroll
+    for (int s = 1; s < kMaxRanges; ++s)
+      if (s < p.splits) sum += in[s];
+  }
+  return sum * scale;
+}
+
+// Few rows: 16 rows of one segment, the columns of one slice.  A operand B_a's rows (16
+// columns of Y), straight from memory, B operand t's rows, so that a lane holds 4
+// neighbouring columns of one row.  A wave takes 32 columns at a time, the next ones' Y and
+// B_a under way.
+template <int kSteps>
 __global__ __launch_bounds__(kThreads) void lora_up_kernel(const LoraArgs p, int n_per) {
   const int lane = static_cast<int>(threadIdx.x) & 63, r = lane & 15, g = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x) >> 6);
-  const dev::TileAt at =
-      dev::find_tile(p.offsets, p.of, p.segments, p.M, static_cast<int>(blockIdx.y), 1, 16 * kRowTiles);
+  const dev::TileAt at = dev::find_tile(p.offsets, p.of, p.segments, p.M, static_cast<int>(blockIdx.y), 1, 16);
   if (at.segment < 0) return;
-  const Adapter ad = adapter_of(p, at.segment);
-  const int rows = min(at.rows - 16 * kRowTiles * at.tile, 16 * kRowTiles);
-  const int64_t row0 = at.first + 16 * kRowTiles * at.tile;
+  const int rows = min(at.rows - 16 * at.tile, 16);
+  const int64_t row0 = at.first + 16 * at.tile;
   const int n0 = static_cast<int>(blockIdx.x) * n_per, n1 = min(n0 + n_per, p.N);
+  struct In {
+    f32x4 y[2];
+    u32x4v b[2][kSteps];
+  } now, next;
+  const float* const yp = p.Y + (row0 + min(r, rows - 1)) * p.ld_y + 4 * g;
+  // N % 16 == 0: a tile's columns are all there, or none (then the last tile is read)
+  auto load_y = [&](int n, In* in) {
+#pragma unroll
+    for (int j = 0; j < 2; ++j) in->y[j] = *reinterpret_cast<const f32x4*>(yp + min(n + 16 * j, p.N - 16));
+  };
+  int n = n0 + 32 * wave;
+  if (n < n1) load_y(n, &now);
+  const Adapter ad = adapter_of(p, at.with);
   if (ad.rank <= 0 && p.out == p.Y) return;
-
-  u32x4v t[kRowTiles][kSteps][3];
-  const float scale = ad.rank > 0 ? p.scales[ad.index] : 0.f;
-#pragma unroll
-  for (int a = 0; a < kRowTiles; ++a) {
-    const int64_t row = row0 + min(16 * a + r, rows - 1);
-#pragma unroll
-    for (int k = 0; k < kSteps; ++k) {
-      f32x4 lo = {0.f, 0.f, 0.f, 0.f}, hi = lo;
-      if (32 * k + 8 * g < ad.rank) {    // ranks are multiples of 8
-        for (int s = 0; s < p.splits; ++s) {
-          const f32x4* tp = reinterpret_cast<const f32x4*>(p.t + (static_cast<int64_t>(s) * p.M + row) * p.max_rank +
-                                                           32 * k + 8 * g);
-          lo += tp[0];
-          hi += tp[1];
-        }
-        lo *= scale;
-        hi *= scale;
-      }
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        float one[3], two[3];
-        split3(e < 2 ? lo[2 * e] : hi[2 * e - 4], one);
-        split3(e < 2 ? lo[2 * e + 1] : hi[2 * e - 3], two);
-#pragma unroll
-        for (int w = 0; w < 3; ++w) t[a][k][w][e] = dev::pack_bf16(one[w], two[w]);
-      }
-    }
-  }
   const uint16_t* const B = p.B + static_cast<int64_t>(p.N) * ad.first;
-  for (int n = n0 + 16 * wave; n < n1; n += 16 * kWaves) {
-    // N % 16 == 0: the tile's columns are all there
-    f32x4 y[kRowTiles];
+  auto load_b = [&](int n, In* in) {
 #pragma unroll
-    for (int a = 0; a < kRowTiles; ++a) {
-      const int64_t row = row0 + min(16 * a + r, rows - 1);
-      y[a] = *reinterpret_cast<const f32x4*>(p.Y + row * p.ld_y + n + 4 * g);
+    for (int j = 0; j < 2; ++j)
+#pragma unroll
+      for (int k = 0; k < kSteps; ++k) {
+        in->b[j][k] = u32x4v{0, 0, 0, 0};
+        if (32 * k + 8 * g < ad.rank)    // ranks are multiples of 8
+          in->b[j][k] = *reinterpret_cast<const u32x4v*>(
+              B + static_cast<int64_t>(min(n + 16 * j, p.N - 16) + r) * ad.rank + 32 * k + 8 * g);
+      }
+  };
+  if (n < n1) load_b(n, &now);
+  constexpr int kQuads = 8 * kSteps, kPitch = 32 * kSteps + 4;
+  __shared__ __align__(16) float sh[16][kPitch];
+  const float scale = ad.rank > 0 ? p.scales[ad.index] : 0.f;
+#pragma unroll 1
+  for (int e = static_cast<int>(threadIdx.x); e < 16 * kQuads; e += kThreads)
+    *reinterpret_cast<f32x4*>(&sh[e / kQuads][4 * (e % kQuads)]) =
+        join_ranges(p, ad, row0, e / kQuads, rows, e % kQuads, scale);
+  __syncthreads();
+  u32x4v t[kSteps][3];
+#pragma unroll
+  for (int k = 0; k < kSteps; ++k) {
+    const f32x4* in = reinterpret_cast<const f32x4*>(&sh[r][32 * k + 8 * g]);
+    split_operand(in[0], in[1], t[k]);
+  }
+  for (; n < n1; n += 32 * kWaves) {
+    const int after = n + 32 * kWaves;
+    if (after < n1) {
+      load_y(after, &next);
+      load_b(after, &next);
     }
-    u32x4v b[kSteps];
 #pragma unroll
-    for (int k = 0; k < kSteps; ++k) {
-      b[k] = u32x4v{0, 0, 0, 0};
-      if (32 * k + 8 * g < ad.rank)
-        b[k] = *reinterpret_cast<const u32x4v*>(B + static_cast<int64_t>(n + r) * ad.rank + 32 * k + 8 * g);
-    }
-    f32x4 acc[kRowTiles];
-#pragma unroll
-    for (int a = 0; a < kRowTiles; ++a) {
-      acc[a] = {0.f, 0.f, 0.f, 0.f};
+    for (int j = 0; j < 2; ++j) {
+      f32x4 acc = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
       for (int w = 2; w >= 0; --w)       // the small terms first
 #pragma unroll
-        for (int k = 0; k < kSteps; ++k) acc[a] = dev::mfma_bf16(b[k], t[a][k][w], acc[a]);
+        for (int k = 0; k < kSteps; ++k) acc = dev::mfma_bf16(now.b[j][k], t[k][w], acc);
+      if (r < rows && n + 16 * j < n1)
+        *reinterpret_cast<f32x4*>(p.out + (row0 + r) * p.ld_out + n + 16 * j + 4 * g) = now.y[j] + acc;
     }
-#pragma unroll
-    for (int a = 0; a < kRowTiles; ++a)
-      if (16 * a + r < rows)
-        *reinterpret_cast<f32x4*>(p.out + (row0 + 16 * a + r) * p.ld_out + n + 4 * g) = y[a] + acc[a];
+    now = next;
   }
 }
 
-template <int kRankTiles>
-void launch_down(const LoraArgs& p, int64_t tiles, hipStream_t stream) {
-  lora_down_kernel<kRankTiles><<<dim3(p.splits, static_cast<unsigned>(tiles)), kThreads, 0, stream>>>(p);
+// Many rows: 64 rows of one segment, 16 a wave, the columns of one slice, 64 at a time.  A
+// operand t's rows, B operand B_a's rows, column c of the product's tile j being column
+// 4 c + j of the 64, so that a lane holds 4 neighbouring columns of 4 rows and 16 lanes load
+// and store 256 bytes of a row.  B_a's rows come whole and through LDS, once for the four
+// waves, at most 64 ranks at a time (kMany: more than 64; t's operands are then made again
+// for every 64).
+template <bool kMany>
+__global__ __launch_bounds__(kThreads) void lora_up_wide_kernel(const LoraArgs p, int n_per) {
+  constexpr int kRows = 16 * kWaves, kCols = 64;
+  constexpr int kPitch = (kMany ? 256 : 64) + 4;
+  __shared__ __align__(16) float sh_t[kRows][kPitch];
+  __shared__ u32x4v sh_b[kCols * 8];
+  const int lane = static_cast<int>(threadIdx.x) & 63, r = lane & 15, g = lane >> 4;
+  const int my_row = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x) >> 6) * 16;
+  const dev::TileAt at = dev::find_tile(p.offsets, p.of, p.segments, p.M, static_cast<int>(blockIdx.y), 1, kRows);
+  if (at.segment < 0) return;
+  const int rows = min(at.rows - kRows * at.tile, kRows);
+  const int64_t row0 = at.first + kRows * at.tile;
+  const int n0 = static_cast<int>(blockIdx.x) * n_per, n1 = min(n0 + n_per, p.N);
+  // N % 16 == 0: a lane's columns are all there, or none (then the last ones are read)
+  const float* yp[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) yp[i] = p.Y + (row0 + min(my_row + 4 * g + i, rows - 1)) * p.ld_y;
+  f32x4 y[4];
+  auto load_y = [&](int n) {
+    const int c = min(n + 4 * r, p.N - 4);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) y[i] = *reinterpret_cast<const f32x4*>(yp[i] + c);
+  };
+  load_y(n0);
+  const Adapter ad = adapter_of(p, at.with);
+  if (ad.rank <= 0 && p.out == p.Y) return;
+  // Ranks rank0 .. + 63 of B_a's rows n .. + 63: thread's rows bk and bk + 32, unit bu (of
+  // 16 bytes).  Row k's unit u lies in LDS at row k ^ (k / 4 & 1), unit u ^ (k / 8 & 7), so
+  // that the operand's rows 4 c + j do not conflict.
+  const int bk = static_cast<int>(threadIdx.x) >> 3, bu = static_cast<int>(threadIdx.x) & 7;
+  u32x4v b_in[2];
+  auto load_b = [&](int n, int rank0) {
+    const uint16_t* const B = p.B + static_cast<int64_t>(p.N) * ad.first + rank0 + 8 * bu;
+    if (rank0 + 8 * bu < ad.rank)
+#pragma unroll
+      for (int x = 0; x < 2; ++x)
+        b_in[x] = *reinterpret_cast<const u32x4v*>(B + static_cast<int64_t>(min(n + bk + 32 * x, p.N - 1)) * ad.rank);
+  };
+  if (ad.rank > 0) load_b(n0, 0);
+  const float scale = ad.rank > 0 ? p.scales[ad.index] : 0.f;
+  const int quads = (ad.rank + 63) / 64 * 16;
+#pragma unroll 1
+  for (int q0 = 0; q0 < quads; q0 += 16)
+#pragma unroll 1
+    for (int e = static_cast<int>(threadIdx.x); e < 16 * kRows; e += kThreads)
+      *reinterpret_cast<f32x4*>(&sh_t[e >> 4][4 * (q0 + (e & 15))]) =
+          join_ranges(p, ad, row0, e >> 4, rows, q0 + (e & 15), scale);
+  __syncthreads();
+  u32x4v t[2][3];
+  auto operands = [&](int rank0) {
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+      const f32x4* in = reinterpret_cast<const f32x4*>(&sh_t[my_row + r][rank0 + 32 * k + 8 * g]);
+      split_operand(in[0], in[1], t[k]);
+    }
+  };
+  if (ad.rank > 0) operands(0);
+  for (int n = n0; n < n1; n += kCols) {
+    f32x4 acc[4], y_now[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      acc[j] = {0.f, 0.f, 0.f, 0.f};
+      y_now[j] = y[j];
+    }
+    for (int rank0 = 0; rank0 < ad.rank; rank0 += 64) {
+#pragma unroll
+      for (int x = 0; x < 2; ++x) {
+        const int k = bk + 32 * x;
+        sh_b[(k ^ (k >> 2 & 1)) * 8 + (bu ^ (k >> 3 & 7))] = b_in[x];
+      }
+      __syncthreads();
+      if (kMany && rank0 + 64 < ad.rank) {
+        load_b(n, rank0 + 64);
+      } else if (n + kCols < n1) {
+        load_y(n + kCols);
+        load_b(n + kCols, 0);
+      }
+      if (kMany) operands(rank0);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const int k = 4 * r + j;
+        u32x4v b[2];
+#pragma unroll
+        for (int s = 0; s < 2; ++s) {
+          b[s] = sh_b[(k ^ (k >> 2 & 1)) * 8 + ((4 * s + g) ^ (k >> 3 & 7))];
+          if (rank0 + 32 * s + 8 * g >= ad.rank) b[s] = u32x4v{0, 0, 0, 0};
+        }
+#pragma unroll
+        for (int w = 2; w >= 0; --w)     // the small terms first
+#pragma unroll
+          for (int s = 0; s < 2; ++s) acc[j] = dev::mfma_bf16(t[s][w], b[s], acc[j]);
+      }
+      __syncthreads();
+    }
+    if (ad.rank <= 0 && n + kCols < n1) load_y(n + kCols);
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (my_row + 4 * g + i < rows && n + 4 * r < n1)
+        *reinterpret_cast<f32x4*>(p.out + (row0 + my_row + 4 * g + i) * p.ld_out + n + 4 * r) =
+            y_now[i] + f32x4{acc[0][i], acc[1][i], acc[2][i], acc[3][i]};
+  }
 }
 
-template <int kSteps, int kRowTiles>
+template <int kRowTiles, int kMost>
+void launch_down(const LoraArgs& p, int64_t tiles, hipStream_t stream) {
+  lora_down_kernel<kRowTiles, kMost><<<dim3(p.splits, static_cast<unsigned>(tiles)), kThreads, 0, stream>>>(p);
+}
+
+template <int kSteps>
 void launch_up(const LoraArgs& p, int64_t tiles, int n_per, hipStream_t stream) {
-  lora_up_kernel<kSteps, kRowTiles>
+  lora_up_kernel<kSteps>
+      <<<dim3((p.N + n_per - 1) / n_per, static_cast<unsigned>(tiles)), kThreads, 0, stream>>>(p, n_per);
+}
+
+template <bool kMany>
+void launch_up_wide(const LoraArgs& p, int64_t tiles, int n_per, hipStream_t stream) {
+  lora_up_wide_kernel<kMany>
       <<<dim3((p.N + n_per - 1) / n_per, static_cast<unsigned>(tiles)), kThreads, 0, stream>>>(p, n_per);
 }
 
@@ -210,18 +416,24 @@ void launch_up(const LoraArgs& p, int64_t tiles, int n_per, hipStream_t stream) 
 
 LoraPlan plan_lora(int M, int segments, int N, int K, int max_rank, int num_cus) {
   LoraPlan c;
-  c.tiles = most_tiles(M, segments, 1, 16);
-  const int steps = (K + 31) / 32;
-  const int64_t want = (2 * static_cast<int64_t>(num_cus) + c.tiles - 1) / c.tiles;
-  const int most = std::max(1, steps / 16);            // at least four steps a wave
-  int splits = static_cast<int>(std::max<int64_t>(1, std::min<int64_t>({want, most, 16})));
-  c.k_per = (steps + splits - 1) / splits * 32;
-  c.splits = (K + c.k_per - 1) / c.k_per;
+  // Rows share an adapter's loads where segments have them to share.
   const int64_t mean = M / std::max(1, std::min(M, segments));
-  c.row_tiles = mean >= 64 && max_rank <= 64 ? 4 : 1;
-  c.up_tiles = most_tiles(M, segments, 1, 16 * c.row_tiles);
-  const int64_t slices = std::max<int64_t>(1, (4 * static_cast<int64_t>(num_cus) + c.up_tiles - 1) / c.up_tiles);
-  c.n_per = static_cast<int>((N + slices - 1) / slices + 16 * kWaves - 1) / (16 * kWaves) * (16 * kWaves);
+  c.row_tiles = mean >= 32 ? 2 : 1;
+  c.row_waves = mean >= 32 ? kWaves : 1;
+  c.tiles = most_tiles(M, segments, 1, 16 * c.row_tiles);
+  c.up_tiles = most_tiles(M, segments, 1, 16 * c.row_waves);
+  // Ranges of K until there are four workgroups a CU, two steps a wave at least.
+  const int steps = (K + 63) / 64;
+  const int64_t want = (4 * static_cast<int64_t>(num_cus) + c.tiles - 1) / c.tiles;
+  const int64_t most = std::min(std::max(1, steps / (2 * kWaves)), kMaxRanges);
+  const int splits = static_cast<int>(std::max<int64_t>(1, std::min(want, most)));
+  c.k_per = (steps + splits - 1) / splits * 64;
+  c.splits = (K + c.k_per - 1) / c.k_per;
+  // Short slices: many workgroups a CU hide each other's start (8192 rows x 9728 columns,
+  // slices for 4 / 8 / 24 workgroups a CU: 161 / 155 / 145 us).
+  const int64_t slices = std::max<int64_t>(1, (24 * static_cast<int64_t>(num_cus) + c.up_tiles - 1) / c.up_tiles);
+  const int cols = c.row_waves == 1 ? 32 * kWaves : 64;
+  c.n_per = static_cast<int>((N + slices - 1) / slices + cols - 1) / cols * cols;
   return c;
 }
 
@@ -235,19 +447,23 @@ hipError_t launch_lora(const LoraPlan& c, const uint16_t* x, int64_t ld_x, int M
                        int64_t ld_y, float* out, int64_t ld_out, void* workspace, hipStream_t stream) {
   const LoraArgs p{x, ld_x, A, B, rank_offsets, scales, offsets, of, Y, out, ld_y, ld_out,
                    static_cast<float*>(workspace), adapters, rank_rows, segments, M, N, K, max_rank, c.splits, c.k_per};
-  if (max_rank <= 16) launch_down<1>(p, c.tiles, stream);
-  else if (max_rank <= 32) launch_down<2>(p, c.tiles, stream);
-  else if (max_rank <= 64) launch_down<4>(p, c.tiles, stream);
-  else if (max_rank <= 128) launch_down<8>(p, c.tiles, stream);
-  else launch_down<16>(p, c.tiles, stream);
-  if (c.row_tiles == 4) {
-    if (max_rank <= 32) launch_up<1, 4>(p, c.up_tiles, c.n_per, stream);
-    else launch_up<2, 4>(p, c.up_tiles, c.n_per, stream);
+  if (c.row_tiles == 2) {
+    if (max_rank <= 16) launch_down<2, 1>(p, c.tiles, stream);
+    else if (max_rank <= 32) launch_down<2, 2>(p, c.tiles, stream);
+    else launch_down<2, 4>(p, c.tiles, stream);
   } else {
-    if (max_rank <= 32) launch_up<1, 1>(p, c.up_tiles, c.n_per, stream);
-    else if (max_rank <= 64) launch_up<2, 1>(p, c.up_tiles, c.n_per, stream);
-    else if (max_rank <= 128) launch_up<4, 1>(p, c.up_tiles, c.n_per, stream);
-    else launch_up<8, 1>(p, c.up_tiles, c.n_per, stream);
+    if (max_rank <= 16) launch_down<1, 1>(p, c.tiles, stream);
+    else if (max_rank <= 32) launch_down<1, 2>(p, c.tiles, stream);
+    else launch_down<1, 4>(p, c.tiles, stream);
+  }
+  if (c.row_waves == kWaves) {
+    if (max_rank <= 64) launch_up_wide<false>(p, c.up_tiles, c.n_per, stream);
+    else launch_up_wide<true>(p, c.up_tiles, c.n_per, stream);
+  } else {
+    if (max_rank <= 32) launch_up<1>(p, c.up_tiles, c.n_per, stream);
+    else if (max_rank <= 64) launch_up<2>(p, c.up_tiles, c.n_per, stream);
+    else if (max_rank <= 128) launch_up<4>(p, c.up_tiles, c.n_per, stream);
+    else launch_up<8>(p, c.up_tiles, c.n_per, stream);
   }
   return hipGetLastError();
 }

@@ -228,11 +228,11 @@ hipError_t launch_tree_attention(const TreePlan& c, const uint16_t* q, int64_t l
                                  const uint8_t* mask, int64_t ld_mask, int mask_wide, uint16_t* out, float* lse,
                                  void* workspace, hipStream_t stream);
 
-// lora.hip.  16-row tiles and ranges of K of the first product; 16 * row_tiles-row
-// tiles and columns a workgroup of the second.
+// lora.hip.  Tiles of 16 * row_tiles rows and ranges of K a tile of the first product;
+// tiles of 16 * row_waves rows and columns a workgroup of the second.
 struct LoraPlan {
   int64_t tiles = 0, up_tiles = 0;
-  int splits = 1, k_per = 0, row_tiles = 1, n_per = 0;
+  int splits = 1, k_per = 0, row_tiles = 1, row_waves = 1, n_per = 0;
 };
 LoraPlan plan_lora(int M, int segments, int N, int K, int max_rank, int num_cus);
 size_t lora_workspace_bytes(const LoraPlan& c, int M, int max_rank);
