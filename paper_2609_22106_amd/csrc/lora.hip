@@ -31,7 +31,7 @@ namespace {
 using dev::f32x4;
 using dev::u32x4v;
 
-constexpr int kWaves = 4, kThreads = 64 * kWaves;
+constexpr int kWaves = 4, kThreads = 64 * kWaves, kSmallWaves = 8;
 constexpr int kMaxRanges = 8;            // of K
 
 struct LoraArgs {
@@ -64,19 +64,20 @@ __device__ __forceinline__ Adapter adapter_of(const LoraArgs& p, int index) {
   return a;
 }
 
-// t of 16 kRowTiles rows over one range of K, for up to 16 kTiles ranks from `rank0` on.
-// The waves take every kWaves-th step of 64 elements.  A row's 128 bytes of a step are
-// loaded by 8 neighbouring lanes -- an operand's own lanes, each on another row, would
-// take the first cache four times as long -- and reach their operand's place through a
-// part of LDS of the wave's own (unit u of row k at u ^ (k / 2 & 7): no conflicts).
-template <int kRowTiles, int kTiles>
+// t of 16 kRowTiles rows over K's elements [k0, end), for up to 16 kTiles ranks from `rank0`
+// on, by kN waves: emit(row, rank, value), by any thread.  The waves take every kN-th step
+// of 64 elements.  A row's 128 bytes of a step are loaded by 8 neighbouring lanes -- an
+// operand's own lanes, each on another row, would take the first cache four times as long
+// -- and reach their operand's place through a part of LDS of the wave's own (unit u of row k
+// at u ^ (k / 2 & 7): no conflicts).
+template <int kRowTiles, int kTiles, int kN, typename Emit>
 __device__ __forceinline__ void down_rows(const LoraArgs& p, const Adapter& ad, int64_t row0, int rows, int rank0,
-                                          u32x4v* sh) {
+                                          int k0, int end, u32x4v* sh, Emit emit) {
   constexpr int kLoads = 2 * (kRowTiles + kTiles);           // of 8 rows, a step
-  constexpr int kAtOnce = kLoads <= 6 ? 4 : 2;               // steps under way
+  // steps under way: the small kernel has the registers for all of K = 2560 at up to 32 ranks
+  constexpr int kAtOnce = kN == kSmallWaves ? (kLoads <= 6 ? 5 : 3) : kLoads <= 6 ? 4 : 2;
   const int lane = static_cast<int>(threadIdx.x) & 63, r = lane & 15, g = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x) >> 6);
-  const int k0 = static_cast<int>(blockIdx.x) * p.k_per, end = min(k0 + p.k_per, p.K);
   const int lr = lane >> 3, unit = lane & 7;
   // rows and ranks past the end read the last one and are not used
   const uint16_t* src[kLoads];
@@ -92,18 +93,19 @@ __device__ __forceinline__ void down_rows(const LoraArgs& p, const Adapter& ad, 
 #pragma unroll
     for (int j = 0; j < kTiles; ++j) acc[a][j] = {0.f, 0.f, 0.f, 0.f};
   const u32x4v none = {0, 0, 0, 0};
-  for (int k = k0 + 64 * wave; k < end; k += kAtOnce * 64 * kWaves) {
+  for (int k = k0 + 64 * wave; k < end; k += kAtOnce * 64 * kN) {
     u32x4v in[kAtOnce][kLoads];
 #pragma unroll
     for (int s = 0; s < kAtOnce; ++s) {
-      const int at = k + s * 64 * kWaves + 8 * unit;         // K % 8 == 0: a unit is whole or absent
+      const int at = k + s * 64 * kN + 8 * unit;             // K % 8 == 0: a unit is whole or absent
+      if (kN == kSmallWaves && s && k + s * 64 * kN >= end) break;
 #pragma unroll
       for (int i = 0; i < kLoads; ++i) in[s][i] = *reinterpret_cast<const u32x4v*>(src[i] + (at < end ? at : 0));
     }
 #pragma unroll
     for (int s = 0; s < kAtOnce; ++s) {
-      if (s && k + s * 64 * kWaves >= end) break;
-      const bool here = k + s * 64 * kWaves + 8 * unit < end;
+      if (s && k + s * 64 * kN >= end) break;
+      const bool here = k + s * 64 * kN + 8 * unit < end;
 #pragma unroll
       for (int i = 0; i < kLoads; ++i)
         mine[(8 * i + lr) * 8 + (unit ^ ((8 * i + lr) >> 1 & 7))] = here ? in[s][i] : none;
@@ -125,7 +127,6 @@ __device__ __forceinline__ void down_rows(const LoraArgs& p, const Adapter& ad, 
   }
   // Join the waves, 16 rows at a time: sum[w][j][16 g + c][i] is row 4 g + i, rank 16 j + c.
   f32x4* const sum = reinterpret_cast<f32x4*>(sh);
-  float* const t = p.t + (static_cast<int64_t>(blockIdx.x) * p.M + row0) * p.max_rank + rank0;
 #pragma unroll
   for (int a = 0; a < kRowTiles; ++a) {
     __syncthreads();
@@ -133,21 +134,39 @@ __device__ __forceinline__ void down_rows(const LoraArgs& p, const Adapter& ad, 
     for (int j = 0; j < kTiles; ++j) sum[(wave * kTiles + j) * 64 + lane] = acc[a][j];
     __syncthreads();
 #pragma unroll
-    for (int e = static_cast<int>(threadIdx.x); e < 256 * kTiles; e += kThreads) {
+    for (int e = static_cast<int>(threadIdx.x); e < 256 * kTiles; e += 64 * kN) {
       const int rank = e % (16 * kTiles), row = e / (16 * kTiles);
       if (16 * a + row < rows && rank0 + rank < ad.rank) {
         float x = 0.f;
 #pragma unroll
-        for (int w = 0; w < kWaves; ++w)
+        for (int w = 0; w < kN; ++w)
           x += sum[(w * kTiles + (rank >> 4)) * 64 + 16 * (row >> 2) + (rank & 15)][row & 3];
-        t[(16 * a + row) * p.max_rank + rank] = x;
+        emit(16 * a + row, rank0 + rank, x);
       }
     }
   }
 }
 
+// The same for all of an adapter's ranks, up to 16 kMost of them at a time: the adapter's
+// own rank, not the largest one, says what is read.
+template <int kRowTiles, int kMost, int kN, typename Emit>
+__device__ __forceinline__ void down_ranks(const LoraArgs& p, const Adapter& ad, int64_t row0, int rows, int k0,
+                                           int end, u32x4v* sh, Emit emit) {
+  int rank0 = 0;
+  if constexpr (kMost == 4)
+    for (; ad.rank - rank0 > 32; rank0 += 64) {
+      if (rank0) __syncthreads();
+      down_rows<kRowTiles, 4, kN>(p, ad, row0, rows, rank0, k0, end, sh, emit);
+    }
+  if (ad.rank <= rank0) return;
+  if (rank0) __syncthreads();
+  if constexpr (kMost >= 2)
+    if (ad.rank - rank0 > 16) return down_rows<kRowTiles, 2, kN>(p, ad, row0, rows, rank0, k0, end, sh, emit);
+  down_rows<kRowTiles, 1, kN>(p, ad, row0, rows, rank0, k0, end, sh, emit);
+}
+
 template <int kRowTiles, int kMost>
-__global__ __launch_bounds__(kThreads) void lora_down_kernel(const LoraArgs p) {
+__global__ __launch_bounds__(kThreads, kRowTiles == 1 ? 3 : 2) void lora_down_kernel(const LoraArgs p) {
   __shared__ u32x4v sh[kWaves * 2 * (kRowTiles + kMost) * 64];
   const dev::TileAt at = dev::find_tile(p.offsets, p.of, p.segments, p.M, static_cast<int>(blockIdx.y), 1,
                                         16 * kRowTiles);
@@ -156,18 +175,10 @@ __global__ __launch_bounds__(kThreads) void lora_down_kernel(const LoraArgs p) {
   if (ad.rank <= 0) return;
   const int rows = min(at.rows - 16 * kRowTiles * at.tile, 16 * kRowTiles);
   const int64_t row0 = at.first + 16 * kRowTiles * at.tile;
-  // this adapter's own rank, not the largest one, says what is read; 64 ranks at a time
-  int rank0 = 0;
-  if constexpr (kMost == 4)
-    for (; ad.rank - rank0 > 32; rank0 += 64) {
-      if (rank0) __syncthreads();
-      down_rows<kRowTiles, 4>(p, ad, row0, rows, rank0, sh);
-    }
-  if (ad.rank <= rank0) return;
-  if (rank0) __syncthreads();
-  if constexpr (kMost >= 2)
-    if (ad.rank - rank0 > 16) return down_rows<kRowTiles, 2>(p, ad, row0, rows, rank0, sh);
-  down_rows<kRowTiles, 1>(p, ad, row0, rows, rank0, sh);
+  const int k0 = static_cast<int>(blockIdx.x) * p.k_per;
+  float* const t = p.t + (static_cast<int64_t>(blockIdx.x) * p.M + row0) * p.max_rank;
+  down_ranks<kRowTiles, kMost, kWaves>(p, ad, row0, rows, k0, min(k0 + p.k_per, p.K), sh,
+                                       [&](int row, int rank, float x) { t[row * p.max_rank + rank] = x; });
 }
 
 // x's three bf16 terms: x = a + b + c up to 2^-24 of x.  An infinity or a NaN is a's alone.
@@ -193,54 +204,62 @@ __device__ __forceinline__ void split_operand(f32x4 lo, f32x4 hi, u32x4v (&out)[
   }
 }
 
-// Quadruple `quad` of t's row `row` of the tile: the ranges of K added in order, scaled; 0
-// past the rank and the rows.
-__device__ __forceinline__ f32x4 join_ranges(const LoraArgs& p, const Adapter& ad, int64_t row0, int row, int rows,
-                                             int quad, float scale) {
-  f32x4 sum = {0.f, 0.f, 0.f, 0.f};
-  if (row < rows && 4 * quad < ad.rank) {
+// 8 ranks of t, 0 where there are none, as operands.
+__device__ __forceinline__ void load_operand(const float* sh, bool here, u32x4v (&out)[3]) {
+  const f32x4 none = {0.f, 0.f, 0.f, 0.f};
+  const f32x4* in = reinterpret_cast<const f32x4*>(sh);
+  const f32x4 lo = in[0], hi = in[1];
+  split_operand(here ? lo : none, here ? hi : none, out);
+}
+
+// t of the tile's rows, the ranges of K added in order, scaled, into sh (rows `pitch`
+// apart); what lies past the rows and the rank is left as it is.
+template <int kAtOnce>
+__device__ __forceinline__ void join_ranges(const LoraArgs& p, const Adapter& ad, int64_t row0, int rows, float* sh,
+                                            int pitch) {
+  if (ad.rank <= 0) return;
+  const float scale = p.scales[ad.index];
+  const int quads = ad.rank >> 2, all = rows * quads;
+  const int64_t next_range = static_cast<int64_t>(p.M) * p.max_rank;
+#pragma unroll kAtOnce
+  for (int e = static_cast<int>(threadIdx.x); e < all; e += kThreads) {
+    const int row = e / quads, quad = e - row * quads;
     const float* tp = p.t + (row0 + row) * p.max_rank + 4 * quad;
-    const int64_t next_range = static_cast<int64_t>(p.M) * p.max_rank;
     f32x4 in[kMaxRanges];
 #pragma unroll
     for (int s = 0; s < kMaxRanges; ++s) in[s] = *reinterpret_cast<const f32x4*>(tp + min(s, p.splits - 1) * next_range);
-    sum = in[0];
+    f32x4 sum = in[0];
 #pragma unroll
     for (int s = 1; s < kMaxRanges; ++s)
       if (s < p.splits) sum += in[s];
+    *reinterpret_cast<f32x4*>(sh + row * pitch + 4 * quad) = sum * scale;
   }
-  return sum * scale;
 }
 
-// Few rows: 16 rows of one segment, the columns of one slice.  A operand B_a's rows (16
-// columns of Y), straight from memory, B operand t's rows, so that a lane holds 4
-// neighbouring columns of one row.  A wave takes 32 columns at a time, the next ones' Y and
-// B_a under way.
+// 16 rows of one segment, 32 columns of Y at a time: A operand B_a's rows (16 columns),
+// straight from memory, B operand t's rows, so that a lane holds 4 neighbouring columns of
+// one row.
 template <int kSteps>
-__global__ __launch_bounds__(kThreads) void lora_up_kernel(const LoraArgs p, int n_per) {
-  const int lane = static_cast<int>(threadIdx.x) & 63, r = lane & 15, g = lane >> 4;
-  const int wave = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x) >> 6);
-  const dev::TileAt at = dev::find_tile(p.offsets, p.of, p.segments, p.M, static_cast<int>(blockIdx.y), 1, 16);
-  if (at.segment < 0) return;
-  const int rows = min(at.rows - 16 * at.tile, 16);
-  const int64_t row0 = at.first + 16 * at.tile;
-  const int n0 = static_cast<int>(blockIdx.x) * n_per, n1 = min(n0 + n_per, p.N);
+struct Up {
+  const LoraArgs& p;
+  int64_t row0;
+  int rows;
   struct In {
     f32x4 y[2];
     u32x4v b[2][kSteps];
   } now, next;
-  const float* const yp = p.Y + (row0 + min(r, rows - 1)) * p.ld_y + 4 * g;
+  u32x4v t[kSteps][3];
+
   // N % 16 == 0: a tile's columns are all there, or none (then the last tile is read)
-  auto load_y = [&](int n, In* in) {
+  __device__ __forceinline__ void load_y(int n, In* in) const {
+    const int lane = static_cast<int>(threadIdx.x) & 63, r = lane & 15, g = lane >> 4;
+    const float* const yp = p.Y + (row0 + min(r, rows - 1)) * p.ld_y + 4 * g;
 #pragma unroll
     for (int j = 0; j < 2; ++j) in->y[j] = *reinterpret_cast<const f32x4*>(yp + min(n + 16 * j, p.N - 16));
-  };
-  int n = n0 + 32 * wave;
-  if (n < n1) load_y(n, &now);
-  const Adapter ad = adapter_of(p, at.with);
-  if (ad.rank <= 0 && p.out == p.Y) return;
-  const uint16_t* const B = p.B + static_cast<int64_t>(p.N) * ad.first;
-  auto load_b = [&](int n, In* in) {
+  }
+  __device__ __forceinline__ void load_b(const Adapter& ad, int n, In* in) const {
+    const int lane = static_cast<int>(threadIdx.x) & 63, r = lane & 15, g = lane >> 4;
+    const uint16_t* const B = p.B + static_cast<int64_t>(p.N) * ad.first;
 #pragma unroll
     for (int j = 0; j < 2; ++j)
 #pragma unroll
@@ -250,40 +269,78 @@ __global__ __launch_bounds__(kThreads) void lora_up_kernel(const LoraArgs p, int
           in->b[j][k] = *reinterpret_cast<const u32x4v*>(
               B + static_cast<int64_t>(min(n + 16 * j, p.N - 16) + r) * ad.rank + 32 * k + 8 * g);
       }
-  };
-  if (n < n1) load_b(n, &now);
-  constexpr int kQuads = 8 * kSteps, kPitch = 32 * kSteps + 4;
-  __shared__ __align__(16) float sh[16][kPitch];
-  const float scale = ad.rank > 0 ? p.scales[ad.index] : 0.f;
-#pragma unroll 1
-  for (int e = static_cast<int>(threadIdx.x); e < 16 * kQuads; e += kThreads)
-    *reinterpret_cast<f32x4*>(&sh[e / kQuads][4 * (e % kQuads)]) =
-        join_ranges(p, ad, row0, e / kQuads, rows, e % kQuads, scale);
+  }
+  // t's rows, pitch floats apart, scaled; rows past the last are not stored, whatever they hold.
+  __device__ __forceinline__ void operands(const Adapter& ad, const float* sh, int pitch) {
+    const int lane = static_cast<int>(threadIdx.x) & 63, r = lane & 15, g = lane >> 4;
+#pragma unroll
+    for (int k = 0; k < kSteps; ++k) load_operand(sh + r * pitch + 32 * k + 8 * g, 32 * k + 8 * g < ad.rank, t[k]);
+  }
+  // Columns n, n + stride, .. below n1, the next ones' Y and B_a under way; `now` holds n's.
+  __device__ __forceinline__ void columns(const Adapter& ad, int n, int n1, int stride) {
+    const int lane = static_cast<int>(threadIdx.x) & 63, r = lane & 15, g = lane >> 4;
+    for (; n < n1; n += stride) {
+      if (n + stride < n1) {
+        load_y(n + stride, &next);
+        load_b(ad, n + stride, &next);
+      }
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int w = 2; w >= 0; --w)     // the small terms first
+#pragma unroll
+          for (int k = 0; k < kSteps; ++k) acc = dev::mfma_bf16(now.b[j][k], t[k][w], acc);
+        if (r < rows && n + 16 * j < n1)
+          *reinterpret_cast<f32x4*>(p.out + (row0 + r) * p.ld_out + n + 16 * j + 4 * g) = now.y[j] + acc;
+      }
+      now = next;
+    }
+  }
+};
+
+// Few rows, `up`: 16 rows of one segment, the columns of one slice.
+template <int kSteps>
+__global__ __launch_bounds__(kThreads) void lora_up_kernel(const LoraArgs p, int n_per) {
+  const int wave = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x) >> 6);
+  const dev::TileAt at = dev::find_tile(p.offsets, p.of, p.segments, p.M, static_cast<int>(blockIdx.y), 1, 16);
+  if (at.segment < 0) return;
+  Up<kSteps> up{p, at.first + 16 * at.tile, min(at.rows - 16 * at.tile, 16)};
+  const int n0 = static_cast<int>(blockIdx.x) * n_per, n1 = min(n0 + n_per, p.N), n = n0 + 32 * wave;
+  if (n < n1) up.load_y(n, &up.now);
+  const Adapter ad = adapter_of(p, at.with);
+  if (ad.rank <= 0 && p.out == p.Y) return;
+  if (n < n1) up.load_b(ad, n, &up.now);
+  constexpr int kPitch = 32 * kSteps + 4;
+  __shared__ __align__(16) float sh[16 * kPitch];
+  join_ranges<1>(p, ad, up.row0, up.rows, sh, kPitch);
   __syncthreads();
-  u32x4v t[kSteps][3];
-#pragma unroll
-  for (int k = 0; k < kSteps; ++k) {
-    const f32x4* in = reinterpret_cast<const f32x4*>(&sh[r][32 * k + 8 * g]);
-    split_operand(in[0], in[1], t[k]);
-  }
-  for (; n < n1; n += 32 * kWaves) {
-    const int after = n + 32 * kWaves;
-    if (after < n1) {
-      load_y(after, &next);
-      load_b(after, &next);
-    }
-#pragma unroll
-    for (int j = 0; j < 2; ++j) {
-      f32x4 acc = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-      for (int w = 2; w >= 0; --w)       // the small terms first
-#pragma unroll
-        for (int k = 0; k < kSteps; ++k) acc = dev::mfma_bf16(now.b[j][k], t[k][w], acc);
-      if (r < rows && n + 16 * j < n1)
-        *reinterpret_cast<f32x4*>(p.out + (row0 + r) * p.ld_out + n + 16 * j + 4 * g) = now.y[j] + acc;
-    }
-    now = next;
-  }
+  up.operands(ad, sh, kPitch);
+  up.columns(ad, n, n1, 32 * kWaves);
+}
+
+// Both products in one launch: a workgroup of 16 rows and a slice of columns forms all of
+// the rows' t for itself.
+template <int kMost>
+__global__ __launch_bounds__(64 * kSmallWaves) void lora_small_kernel(const LoraArgs p, int n_per) {
+  constexpr int kSteps = kMost <= 2 ? 1 : 2, kPitch = 32 * kSteps + 4;
+  __shared__ u32x4v sh[kSmallWaves * 2 * (1 + kMost) * 64];
+  __shared__ __align__(16) float sh_t[16 * kPitch];
+  const int wave = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x) >> 6);
+  const dev::TileAt at = dev::find_tile(p.offsets, p.of, p.segments, p.M, static_cast<int>(blockIdx.y), 1, 16);
+  if (at.segment < 0) return;
+  Up<kSteps> up{p, at.first + 16 * at.tile, min(at.rows - 16 * at.tile, 16)};
+  const int n0 = static_cast<int>(blockIdx.x) * n_per, n1 = min(n0 + n_per, p.N), n = n0 + 32 * wave;
+  if (n < n1) up.load_y(n, &up.now);
+  const Adapter ad = adapter_of(p, at.with);
+  if (ad.rank <= 0 && p.out == p.Y) return;
+  if (n < n1) up.load_b(ad, n, &up.now);
+  const float scale = ad.rank > 0 ? p.scales[ad.index] : 0.f;
+  down_ranks<1, kMost, kSmallWaves>(p, ad, up.row0, up.rows, 0, p.K, sh,
+                                    [&](int row, int rank, float x) { sh_t[row * kPitch + rank] = x * scale; });
+  __syncthreads();
+  up.operands(ad, sh_t, kPitch);
+  up.columns(ad, n, n1, 32 * kSmallWaves);
 }
 
 // Many rows: 64 rows of one segment, 16 a wave, the columns of one slice, 64 at a time.  A
@@ -331,22 +388,13 @@ __global__ __launch_bounds__(kThreads) void lora_up_wide_kernel(const LoraArgs p
         b_in[x] = *reinterpret_cast<const u32x4v*>(B + static_cast<int64_t>(min(n + bk + 32 * x, p.N - 1)) * ad.rank);
   };
   if (ad.rank > 0) load_b(n0, 0);
-  const float scale = ad.rank > 0 ? p.scales[ad.index] : 0.f;
-  const int quads = (ad.rank + 63) / 64 * 16;
-#pragma unroll 1
-  for (int q0 = 0; q0 < quads; q0 += 16)
-#pragma unroll 1
-    for (int e = static_cast<int>(threadIdx.x); e < 16 * kRows; e += kThreads)
-      *reinterpret_cast<f32x4*>(&sh_t[e >> 4][4 * (q0 + (e & 15))]) =
-          join_ranges(p, ad, row0, e >> 4, rows, q0 + (e & 15), scale);
+  join_ranges<2>(p, ad, row0, rows, &sh_t[0][0], kPitch);
   __syncthreads();
   u32x4v t[2][3];
   auto operands = [&](int rank0) {
 #pragma unroll
-    for (int k = 0; k < 2; ++k) {
-      const f32x4* in = reinterpret_cast<const f32x4*>(&sh_t[my_row + r][rank0 + 32 * k + 8 * g]);
-      split_operand(in[0], in[1], t[k]);
-    }
+    for (int k = 0; k < 2; ++k)
+      load_operand(&sh_t[my_row + r][rank0 + 32 * k + 8 * g], rank0 + 32 * k + 8 * g < ad.rank, t[k]);
   };
   if (ad.rank > 0) operands(0);
   for (int n = n0; n < n1; n += kCols) {
@@ -416,6 +464,19 @@ void launch_up_wide(const LoraArgs& p, int64_t tiles, int n_per, hipStream_t str
 
 LoraPlan plan_lora(int M, int segments, int N, int K, int max_rank, int num_cus) {
   LoraPlan c;
+  c.tiles = most_tiles(M, segments, 1, 16);
+  // One launch while what every slice forms again, all of its rows' t, costs less than a
+  // launch: us, one / two launches, rank 16, K = 2560, N = 4096: 1 row 6.2 / 6.9, 64 requests
+  // of a row 8.0 / 11.4, 3000 rows 25.7 / 32.3; N = 9728: 2000 rows 45 / 51, 3000 rows 79 / 60;
+  // K = 9728, 1 row: 11.6 / 7.8; rank 64, K = 4096, 8 requests: 14 / 9.2.
+  if (max_rank <= 64 && K <= 4096 && max_rank * K <= 32 * 4096 && c.tiles <= num_cus &&
+      (N <= 4096 || 2 * c.tiles <= num_cus)) {
+    c.small = true;
+    const int cols = 32 * kSmallWaves;
+    const int64_t slices = std::max<int64_t>(1, num_cus / c.tiles);
+    c.n_per = static_cast<int>(((N + slices - 1) / slices + cols - 1) / cols * cols);
+    return c;
+  }
   // Rows share an adapter's loads where segments have them to share.
   const int64_t mean = M / std::max(1, std::min(M, segments));
   c.row_tiles = mean >= 32 ? 2 : 1;
@@ -438,7 +499,7 @@ LoraPlan plan_lora(int M, int segments, int N, int K, int max_rank, int num_cus)
 }
 
 size_t lora_workspace_bytes(const LoraPlan& c, int M, int max_rank) {
-  return static_cast<size_t>(c.splits) * M * max_rank * 4;
+  return c.small ? 0 : static_cast<size_t>(c.splits) * M * max_rank * 4;
 }
 
 hipError_t launch_lora(const LoraPlan& c, const uint16_t* x, int64_t ld_x, int M, int K, const uint16_t* A,
@@ -447,6 +508,13 @@ hipError_t launch_lora(const LoraPlan& c, const uint16_t* x, int64_t ld_x, int M
                        int64_t ld_y, float* out, int64_t ld_out, void* workspace, hipStream_t stream) {
   const LoraArgs p{x, ld_x, A, B, rank_offsets, scales, offsets, of, Y, out, ld_y, ld_out,
                    static_cast<float*>(workspace), adapters, rank_rows, segments, M, N, K, max_rank, c.splits, c.k_per};
+  if (c.small) {
+    const dim3 grid((N + c.n_per - 1) / c.n_per, static_cast<unsigned>(c.tiles));
+    if (max_rank <= 16) lora_small_kernel<1><<<grid, 64 * kSmallWaves, 0, stream>>>(p, c.n_per);
+    else if (max_rank <= 32) lora_small_kernel<2><<<grid, 64 * kSmallWaves, 0, stream>>>(p, c.n_per);
+    else lora_small_kernel<4><<<grid, 64 * kSmallWaves, 0, stream>>>(p, c.n_per);
+    return hipGetLastError();
+  }
   if (c.row_tiles == 2) {
     if (max_rank <= 16) launch_down<2, 1>(p, c.tiles, stream);
     else if (max_rank <= 32) launch_down<2, 2>(p, c.tiles, stream);

@@ -229,8 +229,10 @@ hipError_t launch_tree_attention(const TreePlan& c, const uint16_t* q, int64_t l
                                  void* workspace, hipStream_t stream);
 
 // lora.hip.  Tiles of 16 * row_tiles rows and ranges of K a tile of the first product;
-// tiles of 16 * row_waves rows and columns a workgroup of the second.
+// tiles of 16 * row_waves rows and columns a workgroup of the second; small: one launch of
+// both, `tiles` of 16 rows by slices of n_per columns.
 struct LoraPlan {
+  bool small = false;
   int64_t tiles = 0, up_tiles = 0;
   int splits = 1, k_per = 0, row_tiles = 1, row_waves = 1, n_per = 0;
 };

@@ -635,15 +635,18 @@ class PagedKV:
 
     def __init__(self, K, V):
         self.K, self.V = K, V
-        if not (type(K) is type(V) is torch.Tensor and K.dtype is V.dtype is _BF16 and K.dim() == 4
-                and K.shape == V.shape and K.is_cuda and V.is_cuda):
+        if not (type(K) is type(V) is torch.Tensor and K.dtype is V.dtype is _BF16 and K.dim() == 4 and K.is_cuda
+                and V.is_cuda and K.shape == V.shape):
             raise ValueError("K and V must be bfloat16 GPU tensors [pages, kv heads, page size, D] of one shape")
         self.pages, self.heads, self.page_size, self.D = K.shape
-        strides = K.stride()
-        if strides[1:] != (self.page_size * self.D, self.D, 1) or V.stride() != strides:
-            raise ValueError(f"each page of K and V must be contiguous, at one stride (strides {strides}, "
-                             f"{V.stride()})")
-        self.stride = max(strides[0], self.heads * self.page_size * self.D) if self.pages == 1 else strides[0]
+        page = self.heads * self.page_size * self.D
+        self.stride = page
+        if not (K.is_contiguous() and V.is_contiguous()):
+            strides = K.stride()
+            if strides[1:] != (self.page_size * self.D, self.D, 1) or V.stride() != strides:
+                raise ValueError(f"each page of K and V must be contiguous, at one stride (strides {strides}, "
+                                 f"{V.stride()})")
+            self.stride = max(strides[0], page) if self.pages == 1 else strides[0]
 
 
 def prq_paged_kv(pages, heads, page_size, D, device="cuda"):
@@ -691,20 +694,34 @@ def prq_rope_table(positions, rotary_dim, theta=10000.0, scaling="none", factor=
     return torch.from_numpy(table.astype(np.float32)).to(device)
 
 
-def _rows(t, name, dtypes, wide):
-    """A 2-D GPU tensor of rows of `wide` contiguous elements -> its row stride."""
-    if not (type(t) is torch.Tensor and t.dim() == 2 and t.dtype in dtypes and t.is_cuda and t.shape[1] == wide
-            and (t.stride(1) == 1 or wide == 1)):
-        raise ValueError(f"{name} must be a 2-D GPU tensor of {' or '.join(map(str, dtypes))} with rows of {wide} "
-                         f"contiguous elements" + (f" (is {t.dtype} {tuple(t.shape)}, strides {t.stride()})"
-                                                   if isinstance(t, torch.Tensor) else ""))
-    return t.stride(0) if t.shape[0] > 1 else wide
+def _rows(t, name, dtypes, M, wide):
+    """A GPU tensor [M, wide] whose rows are contiguous -> its row stride."""
+    if type(t) is torch.Tensor and t.dtype in dtypes and t.is_cuda and t.shape == (M, wide):
+        if t.is_contiguous():
+            return wide
+        if t.stride(1) == 1 or wide == 1:
+            return t.stride(0) if M > 1 else wide
+    raise ValueError(f"{name} must be a GPU tensor of {' or '.join(map(str, dtypes))}, {M} rows of {wide} "
+                     f"contiguous elements"
+                     + (f" (is {t.dtype} {tuple(t.shape)}, strides {t.stride()}, on {t.device})"
+                        if isinstance(t, torch.Tensor) else ""))
 
 
 def _vector(t, name, dtype, n):
     if not _is(t, dtype, (n,)):
         _need(t, name, dtype, (n,))
         _on_gpu(**{name: t})
+
+
+def _output(t, name, shape, dtype, like, stream):
+    """An output of a call: `t`, checked, or a new one beside the tensor `like`."""
+    if t is None:
+        return like.new_empty(shape, dtype=dtype) if stream is None else _alloc(torch.empty, shape, dtype, like.device,
+                                                                                stream)
+    if not _is(t, dtype, shape):
+        _need(t, name, dtype, shape)
+        _on_gpu(**{name: t})
+    return t
 
 
 def prq_qk_norm_rope(q, k, v, positions, table, cache, slots, q_weight=None, k_weight=None, eps=1e-6,
@@ -714,43 +731,38 @@ def prq_qk_norm_rope(q, k, v, positions, table, cache, slots, q_weight=None, k_w
     values go to `slots` int64 [M] of the cache (-1: nowhere).  table: prq_rope_table's, or None
     for no rotation."""
     D, Hk = cache.D, cache.heads
-    kinds = (_F32, _BF16)
     if not isinstance(q, torch.Tensor) or q.dim() != 2 or q.shape[1] % D or q.shape[1] == 0:
         raise ValueError(f"q must be [M, heads * {D}]")
     M, wide = q.shape
-    ld_q = _rows(q, "q", kinds, wide)
-    ld_k, ld_v = _rows(k, "k", kinds, Hk * D), _rows(v, "v", kinds, Hk * D)
-    if not (q.dtype is k.dtype is v.dtype) or k.shape[0] != M or v.shape[0] != M:
-        raise ValueError("q, k and v must have one type and number of rows")
-    Hq = wide // D
-    if table is None:
-        rot = rows = 0
-    else:
-        if not (type(table) is torch.Tensor and table.dim() == 3 and table.dtype is _F32 and table.shape[2] == 2
-                and table.is_cuda and table.is_contiguous()):
+    Hq, kind = wide // D, (q.dtype,)
+    ld_q = _rows(q, "q", (_F32, _BF16), M, wide)
+    ld_k, ld_v = _rows(k, "k", kind, M, Hk * D), _rows(v, "v", kind, M, Hk * D)
+    rot = rows = 0
+    table_at = positions_at = None
+    if table is not None:
+        if not (type(table) is torch.Tensor and table.dtype is _F32 and table.is_cuda and table.is_contiguous()
+                and table.dim() == 3 and table.shape[2] == 2):
             raise ValueError("table must be a contiguous float32 GPU tensor [positions, rotary_dim / 2, 2]")
-        rows, rot = table.shape[0], 2 * table.shape[1]
-        _vector(positions, "positions", _I32, M)
+        rows, half, _ = table.shape
+        rot = 2 * half
+        if rot:
+            _vector(positions, "positions", _I32, M)
+            table_at, positions_at = table.data_ptr(), positions.data_ptr()
     _vector(slots, "slots", _I64, M)
-    kind = _F32
+    w_kind = _F32
     for name, w in (("q_weight", q_weight), ("k_weight", k_weight)):
         if w is not None:
-            if not (_is(w, _F32, (D,)) or _is(w, _BF16, (D,))):
-                _need(w, name, kinds, (D,))
+            if not (_is(w, _BF16, (D,)) or _is(w, _F32, (D,))):
+                _need(w, name, (_F32, _BF16), (D,))
                 _on_gpu(**{name: w})
-            kind = w.dtype
-    if q_weight is not None and k_weight is not None and q_weight.dtype is not k_weight.dtype:
+            w_kind = w.dtype
+    if q_weight is not None and q_weight.dtype is not w_kind:
         raise ValueError("q_weight and k_weight must have one type")
-    if out is None:
-        out = _alloc(torch.empty, (M, Hq, D), _BF16, q.device, stream)
-    elif not _is(out, _BF16, (M, Hq, D)):
-        _need(out, "out", _BF16, (M, Hq, D))
-        _on_gpu(out=out)
+    out = _output(out, "out", (M, Hq, D), _BF16, q, stream)
     st = _qk_norm_rope(q.data_ptr(), ld_q, k.data_ptr(), ld_k, v.data_ptr(), ld_v, int(q.dtype is _BF16), M, Hq, Hk, D,
-                       _ptr(q_weight), _ptr(k_weight), int(kind is _BF16), eps, _ptr(positions) if rot else None,
-                       _ptr(table) if rot else None, rows, rot, int(interleaved), out.data_ptr(), cache.K.data_ptr(),
-                       cache.V.data_ptr(), cache.stride, cache.pages, cache.page_size, slots.data_ptr(),
-                       _stream_of_call(stream))
+                       _ptr(q_weight), _ptr(k_weight), int(w_kind is _BF16), eps, positions_at, table_at, rows, rot,
+                       int(interleaved), out.data_ptr(), cache.K.data_ptr(), cache.V.data_ptr(), cache.stride,
+                       cache.pages, cache.page_size, slots.data_ptr(), _stream_of_call(stream))
     _check(st, "prq_qk_norm_rope")
     return out
 
@@ -766,41 +778,27 @@ def prq_tree_attention(q, cache, page_table, cached_lens, q_offsets, scale, tree
     ones on its pages (page_table int32 [B, pages]); tree_mask bool [M, w] says which of its own tokens
     a row sees (None: itself and those before it).  max_kv_len: the most tokens a request has (default:
     what the page table holds).  workspace: uint8, prq_tree_attention_workspace_bytes (else allocated)."""
-    if not (type(q) is torch.Tensor and q.dim() == 3 and q.dtype is _BF16 and q.is_cuda and q.shape[2] == cache.D
-            and q.stride(2) == 1 and (q.shape[1] <= 1 or q.stride(1) == cache.D)):
+    if not (type(q) is torch.Tensor and q.dtype is _BF16 and q.is_cuda and q.dim() == 3 and q.shape[2] == cache.D
+            and (q.is_contiguous() or (q.stride(2) == 1 and (q.shape[1] <= 1 or q.stride(1) == cache.D)))):
         raise ValueError(f"q must be a bfloat16 GPU tensor [M, heads, {cache.D}] with contiguous rows")
     M, Hq, D = q.shape
     ld_q = q.stride(0) if M > 1 else Hq * D
-    if not (type(page_table) is torch.Tensor and page_table.dim() == 2 and page_table.dtype is _I32
-            and page_table.is_cuda and (page_table.shape[1] <= 1 or page_table.stride(1) == 1)):
-        raise ValueError("page_table must be an int32 GPU tensor [requests, pages] with contiguous rows")
+    if not (type(page_table) is torch.Tensor and page_table.dim() == 2):
+        raise ValueError("page_table must be a GPU tensor [requests, pages]")
     B, wide = page_table.shape
-    ld_pages = page_table.stride(0) if B > 1 else wide
+    ld_pages = _rows(page_table, "page_table", (_I32,), B, wide)
     _vector(cached_lens, "cached_lens", _I32, B)
     _vector(q_offsets, "q_offsets", _I32, B + 1)
     mask, ld_mask, mask_wide = None, 0, 0
     if tree_mask is not None:
-        if not (type(tree_mask) is torch.Tensor and tree_mask.dim() == 2 and tree_mask.dtype in (_BOOL, _U8)
-                and tree_mask.is_cuda and tree_mask.shape[0] == M
-                and (tree_mask.shape[1] <= 1 or tree_mask.stride(1) == 1)):
-            raise ValueError(f"tree_mask must be a bool GPU tensor [{M}, tokens] with contiguous rows")
-        mask_wide = tree_mask.shape[1]
-        ld_mask = tree_mask.stride(0) if M > 1 else mask_wide
-        mask = tree_mask.data_ptr()
-        if not mask_wide:                # no column: nothing seen, which a null pointer does not say
-            mask = q_offsets.data_ptr()
+        mask_wide = tree_mask.shape[1] if tree_mask.dim() == 2 else -1
+        ld_mask = _rows(tree_mask, "tree_mask", (_BOOL, _U8), M, mask_wide)
+        # without a column nothing is seen, which a null pointer would not say
+        mask = tree_mask.data_ptr() if mask_wide else q_offsets.data_ptr()
     if max_kv_len is None:
         max_kv_len = wide * cache.page_size
-    if out is None:
-        out = _alloc(torch.empty, (M, Hq, D), _BF16, q.device, stream)
-    elif not _is(out, _BF16, (M, Hq, D)):
-        _need(out, "out", _BF16, (M, Hq, D))
-        _on_gpu(out=out)
-    if lse is None:
-        lse = _alloc(torch.empty, (M, Hq), _F32, q.device, stream)
-    elif not _is(lse, _F32, (M, Hq)):
-        _need(lse, "lse", _F32, (M, Hq))
-        _on_gpu(lse=lse)
+    out = _output(out, "out", (M, Hq, D), _BF16, q, stream)
+    lse = _output(lse, "lse", (M, Hq), _F32, q, stream)
     if workspace is None:
         need = int(_tree_ws(M, B, Hq, cache.heads, D, max_kv_len))
         if need:
@@ -819,10 +817,11 @@ class LoraAdapters:
     from element N * rank_offsets[a]), rank_offsets int32 [adapters + 1] in multiples of 8, scales float32
     [adapters], and the largest rank."""
 
-    __slots__ = ("A", "B", "rank_offsets", "scales", "max_rank")
+    __slots__ = ("A", "B", "rank_offsets", "scales", "max_rank", "rank_rows", "count")
 
     def __init__(self, A, B, rank_offsets, scales, max_rank):
         self.A, self.B, self.rank_offsets, self.scales, self.max_rank = A, B, rank_offsets, scales, max_rank
+        self.rank_rows, self.count = A.shape[0], scales.shape[0]
 
 
 def prq_lora_adapters(pairs, scales, device="cuda"):
@@ -857,18 +856,16 @@ def prq_lora(x, adapters, segment_offsets, segment_adapter, Y, out=None, workspa
     if not isinstance(x, torch.Tensor) or x.dim() != 2 or not isinstance(Y, torch.Tensor) or Y.dim() != 2:
         raise ValueError("x and Y must be 2-D tensors")
     (M, K), N = x.shape, Y.shape[1]
-    ld_x, ld_y = _rows(x, "x", (_BF16,), K), _rows(Y, "Y", (_F32,), N)
+    ld_x, ld_y = _rows(x, "x", (_BF16,), M, K), _rows(Y, "Y", (_F32,), M, N)
     if out is None:
         out = Y
-    ld_out = _rows(out, "out", (_F32,), N)
-    if Y.shape[0] != M or out.shape[0] != M:
-        raise ValueError(f"x has {M} rows, Y {Y.shape[0]}, out {out.shape[0]}")
+    ld_out = _rows(out, "out", (_F32,), M, N)
     a = adapters
-    n = a.scales.shape[0]
-    if not (type(a.A) is torch.Tensor and a.A.dim() == 2 and _is(a.A, _BF16, (a.A.shape[0], K))
-            and _holds(a.B, _BF16, N * a.A.shape[0]) and _is(a.rank_offsets, _I32, (n + 1,)) and _is(a.scales, _F32, (n,))):
-        _need(a.A, "adapters.A", _BF16, (a.A.shape[0], K))
-        _need(a.B, "adapters.B", _BF16, min_numel=N * a.A.shape[0])
+    n, R = a.count, a.rank_rows
+    if not (_is(a.A, _BF16, (R, K)) and _holds(a.B, _BF16, N * R) and _is(a.rank_offsets, _I32, (n + 1,))
+            and _is(a.scales, _F32, (n,))):
+        _need(a.A, "adapters.A", _BF16, (R, K))
+        _need(a.B, "adapters.B", _BF16, min_numel=N * R)
         _need(a.rank_offsets, "adapters.rank_offsets", _I32, (n + 1,))
         _need(a.scales, "adapters.scales", _F32, (n,))
         _on_gpu(A=a.A, B=a.B, rank_offsets=a.rank_offsets, scales=a.scales)
@@ -883,7 +880,7 @@ def prq_lora(x, adapters, segment_offsets, segment_adapter, Y, out=None, workspa
             workspace = _alloc(torch.empty, need, _U8, x.device, stream, kept=False)
     ws, ws_bytes = _workspace_arg(workspace)
     st = _lora(x.data_ptr(), ld_x, M, K, a.A.data_ptr(), a.B.data_ptr(), a.rank_offsets.data_ptr(),
-               a.scales.data_ptr(), n, a.A.shape[0], a.max_rank, segment_offsets.data_ptr(),
+               a.scales.data_ptr(), n, R, a.max_rank, segment_offsets.data_ptr(),
                segment_adapter.data_ptr(), segments, N, Y.data_ptr(), ld_y, out.data_ptr(), ld_out, ws, ws_bytes,
                _stream_of_call(stream))
     _check(st, "prq_lora")

@@ -159,7 +159,7 @@ def test_workspace_sizes_of_refused_sizes_are_zero():
     assert prq.prq_lora_workspace_bytes(0, 2, 64, 256, 16) == 0
     # a few rows over many keys, or a long K, are split: there is something to join
     assert prq.prq_tree_attention_workspace_bytes(1, 1, 32, 8, 128, 4096) > 0
-    assert prq.prq_lora_workspace_bytes(1, 1, 64, 256, 16) > 0
+    assert prq.prq_lora_workspace_bytes(64, 64, 2560, 9728, 64) > 0
 
 
 # ------------------------------------------------------------ binding refusals ---
