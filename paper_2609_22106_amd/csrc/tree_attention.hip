@@ -86,12 +86,23 @@ __device__ __forceinline__ bool word_finite(uint32_t w) {
   return (w & 0x7F80u) != 0x7F80u && (w & 0x7F800000u) != 0x7F800000u;
 }
 
-// K and V of 32 keys, as a lane (g = l / 16, r = l % 16) holds them.
+// K and V of two 16-key blocks, as a lane (g = l / 16, r = l % 16) holds them.
 template <int D>
 struct Tile {
   static constexpr int kChunks = D / 32, kWords = D / 32;
-  u32x4v k[2][kChunks];                  // key r of two 16-key blocks, dims 32 c + 8 g ..
-  uint32_t v[8][kWords];                 // keys 4 g .. + 3 of both blocks, dims (D / 16) r ..
+  u32x4v keys[2][kChunks];               // key r of each block, dims 32 c + 8 g ..
+  uint32_t values[8][kWords];            // keys 4 g .. + 3 of each block, dims (D / 16) r ..
+
+  __device__ __forceinline__ void k(int b, u32x4v (&out)[kChunks]) const {
+#pragma unroll
+    for (int c = 0; c < kChunks; ++c) out[c] = keys[b][c];
+  }
+  __device__ __forceinline__ void v(int, uint32_t (&out)[8][kWords]) const {
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+#pragma unroll
+      for (int x = 0; x < kWords; ++x) out[e][x] = values[e][x];
+  }
 };
 
 // A lane's part of one row of V.
@@ -118,13 +129,13 @@ __device__ __forceinline__ void load_tile(const TreeArgs& p, const int64_t (&bas
   for (int b = 0; b < 2; ++b) {
     const uint16_t* kp = p.K + base[b] + r * D + 8 * g;
 #pragma unroll
-    for (int c = 0; c < Tile<D>::kChunks; ++c) t->k[b][c] = *reinterpret_cast<const u32x4v*>(kp + 32 * c);
+    for (int c = 0; c < Tile<D>::kChunks; ++c) t->keys[b][c] = *reinterpret_cast<const u32x4v*>(kp + 32 * c);
   }
 #pragma unroll
   for (int b = 0; b < 2; ++b) {
     const uint16_t* vp = p.V + base[b] + 4 * g * D + r * (D / 16);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) load_v<D>(vp + i * D, t->v[4 * b + i]);
+    for (int i = 0; i < 4; ++i) load_v<D>(vp + i * D, t->values[4 * b + i]);
   }
 }
 
@@ -159,6 +170,15 @@ __device__ __forceinline__ bool find_part(const TreeArgs& p, int per_tile, Part*
   return false;
 }
 
+// Element offset of the 16-key block with key `key` on page `page` of the pool.  A block
+// past the keys, or on a page outside the pool (-1), reads the pool's first page, and its
+// keys are not seen.
+template <int D>
+__device__ __forceinline__ int64_t block_base(const TreeArgs& p, int h, int page, int key) {
+  return max(page, 0) * p.page_stride +
+         ((static_cast<int64_t>(h) << p.page_shift) + (key & ((1 << p.page_shift) - 1))) * D;
+}
+
 // A wave's T tiles of 16 query columns: operands, running maximum (of q . k, the same
 // in the four lanes of a column), sum (a lane's own keys) and output.
 template <int D, int T>
@@ -185,60 +205,46 @@ struct Wave {
     }
   }
 
-  // Keys k0 .. k0 + 31; held: whether their two blocks are on pages of the pool, at
-  // element offsets base.  kPlain: every row sees all of them.
-  template <bool kPlain>
-  __device__ __forceinline__ void step(const TreeArgs& p, const Part& w, Tile<D>& tile, int k0, bool held0, bool held1,
-                                       int64_t base0, int64_t base1) {
+  // The 16 kBlocks keys from k0 on; block b of them on page page[b] of the pool (-1: none).
+  // kPlain: every row sees all of them.
+  // `src`: where the operands are, k(b, ..) block b's keys, v(b, ..) those of blocks b and
+  // b + 1.
+  template <bool kPlain, int kBlocks, typename Source>
+  __device__ __forceinline__ void step(const TreeArgs& p, const Part& w, const Source& src, int k0,
+                                       const int (&page)[kBlocks]) {
+    constexpr int kOwn = 4 * kBlocks;    // keys of a lane: e is 16 (e / 4) + 4 g + e % 4
     const int lane = static_cast<int>(threadIdx.x) & 63, r = lane & 15, g = lane >> 4;
-    float s[T][8];
+    float s[T][kOwn];
 #pragma unroll
-    for (int t = 0; t < T; ++t) {
+    for (int b = 0; b < kBlocks; ++b) {
+      u32x4v k[kChunks];
+      src.k(b, k);
 #pragma unroll
-      for (int b = 0; b < 2; ++b) {
+      for (int t = 0; t < T; ++t) {
         f32x4 x = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int c = 0; c < kChunks; ++c) x = dev::mfma_bf16(tile.k[b][c], q[t][c], x);
+        for (int c = 0; c < kChunks; ++c) x = dev::mfma_bf16(k[c], q[t][c], x);
 #pragma unroll
         for (int i = 0; i < 4; ++i) s[t][4 * b + i] = x[i];
       }
     }
     uint32_t seen[T];
-    bool odd_v = false;                  // some key's V holds an infinity or a NaN
     if constexpr (!kPlain) {
 #pragma unroll
       for (int t = 0; t < T; ++t) {
         const uint8_t* see = p.mask ? p.mask + (w.at.first + token[t]) * p.ld_mask : nullptr;
         seen[t] = 0;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          const int key = k0 + 16 * (e >> 2) + 4 * g + (e & 3);
-          const int j = key - w.cached;
-          bool ok = key < w.hi && (e < 4 ? held0 : held1);
-          if (ok && j >= 0) ok = see ? j < p.mask_wide && see[j] != 0 : j <= token[t];
-          if (ok)
-            seen[t] |= 1u << e;
-          else
-            s[t][e] = kNone;
+        for (int e = 0; e < kOwn; ++e) {
+          const int j = k0 + 16 * (e >> 2) + 4 * g + (e & 3) - w.cached;
+          const int own = see && j >= 0 && j < p.mask_wide ? see[j] : 0;
+          const bool ok = j < w.hi - w.cached && page[e >> 2] >= 0 && (j < 0 || (see ? own != 0 : j <= token[t]));
+          seen[t] |= static_cast<uint32_t>(ok) << e;
         }
-      }
-      // What no row may see must not reach the product either (0 x NaN): V past the
-      // keys becomes 0, and infinities and NaN are taken out and added below for the
-      // rows that do see them.
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        const int key = k0 + 16 * (e >> 2) + 4 * g + (e & 3);
-        const bool ok = key < w.hi && (e < 4 ? held0 : held1);
-#pragma unroll
-        for (int x = 0; x < Tile<D>::kWords; ++x) {
-          if (!ok) tile.v[e][x] = 0;
-          if (!word_finite(tile.v[e][x])) {
-            tile.v[e][x] = 0;
-            odd_v = true;
-          }
-        }
+        for (int e = 0; e < kOwn; ++e)
+          if (!(seen[t] >> e & 1)) s[t][e] = kNone;
       }
-      odd_v = __any(odd_v);
     }
 
     // A lane whose scores pass the running maximum by more than the slack renews it.
@@ -246,7 +252,9 @@ struct Wave {
     float top[T];
 #pragma unroll
     for (int t = 0; t < T; ++t) {
-      top[t] = max_of(max_of(max_of(s[t][0], s[t][1], s[t][2]), s[t][3], s[t][4]), s[t][5], max_of(s[t][6], s[t][7]));
+      top[t] = max_of(s[t][0], s[t][1]);
+#pragma unroll
+      for (int e = 2; e < kOwn; e += 2) top[t] = max_of(top[t], s[t][e], s[t][e + 1]);
       past |= top[t] > m[t] + p.slack;
     }
     if (__any(past)) {
@@ -262,65 +270,88 @@ struct Wave {
         for (int v = 0; v < kV; ++v) o[t][v] *= a;
       }
     }
-    u32x4v pw[T];
+    u32x4v pw[T][kBlocks / 2];
 #pragma unroll
     for (int t = 0; t < T; ++t) {
       const float from = m[t] == kNone ? 0.f : m[t] * p.scale;
 #pragma unroll
-      for (int e = 0; e < 8; ++e) s[t][e] = exp2_fast(__builtin_fmaf(s[t][e], p.scale, -from));
-      l[t] += ((s[t][0] + s[t][1]) + (s[t][2] + s[t][3])) + ((s[t][4] + s[t][5]) + (s[t][6] + s[t][7]));
+      for (int b = 0; b < kBlocks; b += 2) {
+        float* x = s[t] + 4 * b;
 #pragma unroll
-      for (int e = 0; e < 4; ++e) pw[t][e] = dev::pack_bf16(s[t][2 * e], s[t][2 * e + 1]);
-    }
-    // V^T: register pairs of neighbouring keys -> the low and the high halves' columns.
+        for (int e = 0; e < 8; ++e) x[e] = exp2_fast(__builtin_fmaf(x[e], p.scale, -from));
+        l[t] += ((x[0] + x[1]) + (x[2] + x[3])) + ((x[4] + x[5]) + (x[6] + x[7]));
 #pragma unroll
-    for (int x = 0; x < Tile<D>::kWords; ++x) {
-      u32x4v even, odd;
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        even[e] = __builtin_amdgcn_perm(tile.v[2 * e + 1][x], tile.v[2 * e][x], 0x05040100u);
-        odd[e] = __builtin_amdgcn_perm(tile.v[2 * e + 1][x], tile.v[2 * e][x], 0x07060302u);
-      }
-#pragma unroll
-      for (int t = 0; t < T; ++t) {
-        o[t][2 * x] = dev::mfma_bf16(even, pw[t], o[t][2 * x]);
-        o[t][2 * x + 1] = dev::mfma_bf16(odd, pw[t], o[t][2 * x + 1]);
+        for (int e = 0; e < 4; ++e) pw[t][b / 2][e] = dev::pack_bf16(x[2 * e], x[2 * e + 1]);
       }
     }
-    if (!kPlain && odd_v) {              // rare: the words taken out above, row by row
-      for (int kk = 0; kk < 32; ++kk) {
-        if (k0 + kk >= w.hi || !(kk < 16 ? held0 : held1)) continue;
-        const uint16_t* vp = p.V + (kk < 16 ? base0 : base1) + (kk & 15) * D;
-        const int from = 16 * ((kk & 15) >> 2) + r, e = 4 * (kk >> 4) + (kk & 3);
+    bool odd_v = false;                  // some key's V holds an infinity or a NaN
+#pragma unroll
+    for (int b = 0; b < kBlocks / 2; ++b) {
+      if (b) __builtin_amdgcn_sched_barrier(0);              // one pair's V in registers at a time
+      uint32_t y[8][D / 32];
+      src.v(2 * b, y);
+      // What no row may see must not reach the product either (0 x NaN): V past the
+      // keys becomes 0, and infinities and NaN are taken out and added below for the
+      // rows that do see them.
+      if constexpr (!kPlain) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          const bool ok = k0 + 32 * b + 16 * (e >> 2) + 4 * g + (e & 3) < w.hi && page[2 * b + (e >> 2)] >= 0;
+#pragma unroll
+          for (int x = 0; x < D / 32; ++x) {
+            if (!ok) y[e][x] = 0;
+            if (!word_finite(y[e][x])) {
+              y[e][x] = 0;
+              odd_v = true;
+            }
+          }
+        }
+      }
+      // V^T: register pairs of neighbouring keys -> the low and the high halves' columns.
+#pragma unroll
+      for (int x = 0; x < D / 32; ++x) {
+        u32x4v even, odd;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          even[e] = __builtin_amdgcn_perm(y[2 * e + 1][x], y[2 * e][x], 0x05040100u);
+          odd[e] = __builtin_amdgcn_perm(y[2 * e + 1][x], y[2 * e][x], 0x07060302u);
+        }
 #pragma unroll
         for (int t = 0; t < T; ++t) {
-          float mine = 0.f;
+          o[t][2 * x] = dev::mfma_bf16(even, pw[t][b], o[t][2 * x]);
+          o[t][2 * x + 1] = dev::mfma_bf16(odd, pw[t][b], o[t][2 * x + 1]);
+        }
+      }
+    }
+    if (!kPlain && __any(odd_v)) {            // rare: the words taken out above, row by row
 #pragma unroll
-          for (int x = 0; x < 8; ++x) mine = x == e ? s[t][x] : mine;
-          const float pk = __shfl(mine, from);
-          const bool sees = (__shfl(static_cast<int>(seen[t]), from) >> e) & 1;
+      for (int b = 0; b < kBlocks; ++b) {
+        const int64_t base = block_base<D>(p, w.h, page[b], k0 + 16 * b);
+        for (int kk = 0; kk < 16; ++kk) {
+          if (k0 + 16 * b + kk >= w.hi || page[b] < 0) break;
+          const uint16_t* vp = p.V + base + kk * D;
+          const int from = 16 * (kk >> 2) + r;
 #pragma unroll
-          for (int v = 0; v < kV; ++v)
+          for (int t = 0; t < T; ++t) {
+            float mine = 0.f;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              const int d = kV * (4 * g + i) + v;
-              const uint32_t word = vp[d & ~1] | static_cast<uint32_t>(vp[d | 1]) << 16;
-              if (sees && !word_finite(word)) o[t][v][i] += pk * dev::bf16_float(vp[d]);
-            }
+            for (int x = 0; x < 4; ++x) mine = x == (kk & 3) ? s[t][4 * b + x] : mine;
+            const float pk = __shfl(mine, from);
+            const bool sees = (__shfl(static_cast<int>(seen[t]), from) >> (4 * b + (kk & 3))) & 1;
+#pragma unroll
+            for (int v = 0; v < kV; ++v)
+#pragma unroll
+              for (int i = 0; i < 4; ++i) {
+                const int d = kV * (4 * g + i) + v;
+                const uint32_t word = vp[d & ~1] | static_cast<uint32_t>(vp[d | 1]) << 16;
+                if (sees && !word_finite(word)) o[t][v][i] += pk * dev::bf16_float(vp[d]);
+              }
+          }
         }
       }
     }
   }
 };
-
-// Element offset of the 16-key block with key `key` on page `page` of the pool.  A block
-// past the keys, or on a page outside the pool (-1), reads the pool's first page, and its
-// keys are not seen.
-template <int D>
-__device__ __forceinline__ int64_t block_base(const TreeArgs& p, int h, int page, int key) {
-  return max(page, 0) * p.page_stride +
-         ((static_cast<int64_t>(h) << p.page_shift) + (key & ((1 << p.page_shift) - 1))) * D;
-}
 
 // The page of the block at `key`, -1 where there is none.
 __device__ __forceinline__ int page_entry(const TreeArgs& p, const Part& w, int key) {
@@ -343,38 +374,33 @@ __global__ __launch_bounds__(kThreads, D <= 128 ? 2 : 1) void tree_attention_ker
   const int steps = w.hi > first ? (w.hi - first + kStep - 1) / kStep : 0;
   // lane 2 s + b: page of block b of step s (of 32 steps)
   int entries = page_entry(p, w, first + kStep * (lane >> 1) + 16 * (lane & 1));
-  int64_t base[2];
-  bool held[2];
-  auto find = [&](int step) {
+  int page[2];
+  auto load = [&](int step, Tile<D>* tile) {
+    int64_t base[2];
 #pragma unroll
     for (int b = 0; b < 2; ++b) {
-      const int page = __builtin_amdgcn_readlane(entries, 2 * (step & 31) + b);
-      held[b] = page >= 0;
-      base[b] = block_base<D>(p, w.h, page, first + kStep * step + 16 * b);
+      page[b] = __builtin_amdgcn_readlane(entries, 2 * (step & 31) + b);
+      base[b] = block_base<D>(p, w.h, page[b], first + kStep * step + 16 * b);
     }
+    load_tile<D>(p, base, tile);
   };
   Wave<D, 1> q;
   q.start(p, w, w.c0);
   Tile<D> now, next;
-  if (steps > 0) {
-    find(0);
-    load_tile<D>(p, base, &now);
-  }
+  if (steps > 0) load(0, &now);
   auto one = [&](int step, auto plain) {
-    const bool held0 = held[0], held1 = held[1];
-    const int64_t base0 = base[0], base1 = base[1];
+    const int page_now[2] = {page[0], page[1]};
     if (step + 1 < steps) {
       if (((step + 1) & 31) == 0)
         entries = page_entry(p, w, first + kStep * (step + 1 + (lane >> 1)) + 16 * (lane & 1));
-      find(step + 1);
-      load_tile<D>(p, base, &next);
+      load(step + 1, &next);
     }
-    q.template step<decltype(plain)::value>(p, w, now, first + kStep * step, held0, held1, base0, base1);
+    q.template step<decltype(plain)::value, 2>(p, w, now, first + kStep * step, page_now);
     if (step + 1 < steps) now = next;
   };
   // every row sees the whole step: of cached tokens alone, on pages of the pool
   int step = 0;
-  for (; step < steps && first + kStep * step + 32 <= min(w.cached, w.hi) && held[0] && held[1]; ++step)
+  for (; step < steps && first + kStep * step + 32 <= min(w.cached, w.hi) && (page[0] | page[1]) >= 0; ++step)
     one(step, std::true_type{});
   for (; step < steps; ++step) one(step, std::false_type{});
 
@@ -423,18 +449,59 @@ __global__ __launch_bounds__(kThreads, D <= 128 ? 2 : 1) void tree_attention_ker
   }
 }
 
+// Copies 16 bytes a lane straight to LDS, lane l's at lds + 16 l (LDS address, the same for
+// the wave).
+__device__ __forceinline__ void lds_copy16(const uint16_t* src, uint32_t lds) {
+  asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off"
+               :
+               : "v"(src), "s"(lds)
+               : "memory", "m0");
+}
+
+// K and V of a stage in LDS, and a lane's places in it (elements): rows r of a 16-key block
+// of K, 4 g + i of V.
+template <int D>
+struct Staged {
+  const uint16_t *ks, *vs;
+  const int (&k_at)[D / 32];
+  const int (&v_at)[4];
+
+  __device__ __forceinline__ void k(int b, u32x4v (&out)[D / 32]) const {
+#pragma unroll
+    for (int c = 0; c < D / 32; ++c) out[c] = *reinterpret_cast<const u32x4v*>(ks + k_at[c] + 16 * b * D);
+  }
+  __device__ __forceinline__ void v(int b, uint32_t (&out)[8][D / 32]) const {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const uint16_t* const at = vs + 16 * (b + (e >> 2)) * D;
+      if constexpr (D <= 128) {
+        load_v<D>(at + v_at[e & 3], out[e]);
+      } else {                           // the row's second unit lies at the first one's neighbour
+#pragma unroll
+        for (int c = 0; c < 2; ++c) {
+          const u32x4v x = *reinterpret_cast<const u32x4v*>(at + (v_at[e & 3] ^ (8 * c)));
+#pragma unroll
+          for (int i = 0; i < 4; ++i) out[e][4 * c + i] = x[i];
+        }
+      }
+    }
+  }
+};
+
 // More columns: each wave its own T tiles of them, all waves the same keys, K and V staged
 // in LDS (two stages of kKeys keys; a row's 16-byte units permuted by its number, so
 // that neither the K reads, a column of rows, nor the V reads, a whole row, conflict).
 template <int D, int T>
 __global__ __launch_bounds__(kThreads, D <= 128 ? 2 : 1) void tree_attention_wide_kernel(const TreeArgs p) {
   constexpr int kV = D / 16, kKeys = D <= 128 ? 64 : 32;
-  constexpr int kUnits = D / 8, kRows = kThreads / kUnits, kPasses = kKeys / kRows;
+  constexpr int kUnits = D / 8, kRows = 64 / kUnits, kCopies = kKeys / kRows / kWaves;
   __shared__ __align__(16) uint16_t sh[2][2][kKeys * D];     // stage, K or V
   Part w;
   if (!find_part(p, 16 * T * kWaves, &w)) return;
   const int lane = static_cast<int>(threadIdx.x) & 63, r = lane & 15, g = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x) >> 6);
+  const uint32_t sh_at = static_cast<uint32_t>(
+      reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) void*)(&sh[0][0][0])));
   // Unit u of row k lies at unit u ^ turn(k).
   auto turn = [](int k) { return D == 64 ? (k >> 1) & 7 : k & 15; };
 
@@ -443,26 +510,18 @@ __global__ __launch_bounds__(kThreads, D <= 128 ? 2 : 1) void tree_attention_wid
   q.start(p, w, w.c0 + 16 * T * wave);
   const bool works = 16 * T * wave < w.cols;                 // else the wave only helps to load
 
-  const int unit = static_cast<int>(threadIdx.x) % kUnits, row = static_cast<int>(threadIdx.x) / kUnits;
-  u32x4v k_in[kPasses], v_in[kPasses];
-  auto load = [&](int stage) {           // stage's rows row, row + kRows, ... of K and V
+  // A stage's rows are copied kRows to a wave copy (a kilobyte), lane i to unit i of it.
+  auto load = [&](int stage) {
+    const uint32_t to = sh_at + (stage & 1) * 2 * kKeys * D * 2;
 #pragma unroll
-    for (int x = 0; x < kPasses; ++x) {
-      const int k = kRows * x + row;     // its block is the same for the wave
-      const int block = __builtin_amdgcn_readfirstlane(k >> 4);
-      const int page = __builtin_amdgcn_readlane(entries, (stage * (kKeys / 16) + block) & 63);
-      const int64_t at = block_base<D>(p, w.h, page, w.lo + kKeys * stage + 16 * block) + (k & 15) * D + 8 * unit;
-      k_in[x] = *reinterpret_cast<const u32x4v*>(p.K + at);
-      v_in[x] = *reinterpret_cast<const u32x4v*>(p.V + at);
-    }
-  };
-  auto store = [&](int stage) {
-#pragma unroll
-    for (int x = 0; x < kPasses; ++x) {
-      const int k = kRows * x + row;
-      const int at = k * D + 8 * (unit ^ turn(k));
-      *reinterpret_cast<u32x4v*>(&sh[stage & 1][0][at]) = k_in[x];
-      *reinterpret_cast<u32x4v*>(&sh[stage & 1][1][at]) = v_in[x];
+    for (int x = 0; x < kCopies; ++x) {
+      const int c = wave + kWaves * x;                       // rows kRows c .. of the stage
+      const int k = kRows * c + lane / kUnits;
+      const int page = __builtin_amdgcn_readlane(entries, (stage * (kKeys / 16) + kRows * c / 16) & 63);
+      const int64_t at = block_base<D>(p, w.h, page, w.lo + kKeys * stage + (kRows * c / 16) * 16) + (k & 15) * D +
+                         8 * (lane % kUnits ^ turn(k));
+      lds_copy16(p.K + at, to + c * 1024);
+      lds_copy16(p.V + at, to + kKeys * D * 2 + c * 1024);
     }
   };
   const int stages = (w.hi - w.lo + kKeys - 1) / kKeys;
@@ -473,21 +532,18 @@ __global__ __launch_bounds__(kThreads, D <= 128 ? 2 : 1) void tree_attention_wid
     if (__any(w.lo + kKeys * stage + 16 * lane < w.hi && entries < 0)) plain = min(plain, stage);
   };
   check(0);
-  if (stages > 0) {
-    load(0);
-    store(0);
-  }
-  // A lane's places in a stage (elements): rows r of a 16-key block of K, 4 g + i of V; the
-  // blocks are 16 rows apart, and turn(k) has k's low bits alone.
-  int k_at[Tile<D>::kChunks], v_at[4];
+  if (stages > 0) load(0);
+  // the blocks are 16 rows apart, and turn(k) has k's low bits alone
+  int k_at[D / 32], v_at[4];
 #pragma unroll
-  for (int c = 0; c < Tile<D>::kChunks; ++c) k_at[c] = r * D + 8 * ((4 * c + g) ^ turn(r));
+  for (int c = 0; c < D / 32; ++c) k_at[c] = r * D + 8 * ((4 * c + g) ^ turn(r));
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     const int k = 4 * g + i;
     v_at[i] = k * D + (D == 64 ? 8 * ((r >> 1) ^ turn(k)) + 4 * (r & 1) : 8 * ((D / 128 * r) ^ turn(k)));
   }
   auto one = [&](int stage, auto all) {
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");         // this wave's copies of the stage
     __syncthreads();
     const int entries_now = entries;
     if (stage + 1 < stages) {
@@ -498,44 +554,14 @@ __global__ __launch_bounds__(kThreads, D <= 128 ? 2 : 1) void tree_attention_wid
       load(stage + 1);
     }
     if (works) {
-#pragma unroll 1
-      for (int half = 0; half < kKeys / 32; ++half) {
-        const int k0 = w.lo + kKeys * stage + 32 * half;
-        if (!decltype(all)::value && k0 >= w.hi) break;
-        const uint16_t* const ks = sh[stage & 1][0] + 32 * half * D;
-        const uint16_t* const vs = sh[stage & 1][1] + 32 * half * D;
-        Tile<D> tile;
+      constexpr int kBlocks = kKeys / 16;
+      const Staged<D> src{sh[stage & 1][0], sh[stage & 1][1], k_at, v_at};
+      int page[kBlocks];
 #pragma unroll
-        for (int b = 0; b < 2; ++b) {
-#pragma unroll
-          for (int c = 0; c < Tile<D>::kChunks; ++c)
-            tile.k[b][c] = *reinterpret_cast<const u32x4v*>(ks + k_at[c] + 16 * b * D);
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            if constexpr (D <= 128) {
-              load_v<D>(vs + v_at[i] + 16 * b * D, tile.v[4 * b + i]);
-            } else {                     // the row's second unit lies at the first one's neighbour
-#pragma unroll
-              for (int c = 0; c < 2; ++c) {
-                const u32x4v x = *reinterpret_cast<const u32x4v*>(vs + (v_at[i] ^ (8 * c)) + 16 * b * D);
-#pragma unroll
-                for (int e = 0; e < 4; ++e) tile.v[4 * b + i][4 * c + e] = x[e];
-              }
-            }
-          }
-        }
-        int page0 = 0, page1 = 0;
-        if constexpr (!decltype(all)::value) {
-          const int block = (stage * (kKeys / 16) + 2 * half) & 63;
-          page0 = __builtin_amdgcn_readlane(entries_now, block);
-          page1 = __builtin_amdgcn_readlane(entries_now, block + 1);
-        }
-        q.template step<decltype(all)::value>(p, w, tile, k0, page0 >= 0, page1 >= 0,
-                                              block_base<D>(p, w.h, page0, k0),
-                                              block_base<D>(p, w.h, page1, k0 + 16));
-      }
+      for (int b = 0; b < kBlocks; ++b)
+        page[b] = decltype(all)::value ? 0 : __builtin_amdgcn_readlane(entries_now, (stage * kBlocks + b) & 63);
+      q.template step<decltype(all)::value, kBlocks>(p, w, src, w.lo + kKeys * stage, page);
     }
-    if (stage + 1 < stages) store(stage + 1);
   };
   int stage = 0;
   for (; stage < plain; ++stage) one(stage, std::true_type{});

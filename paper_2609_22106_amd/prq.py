@@ -625,6 +625,7 @@ def prq_grouped_gemm(Aq, Asc, group_offsets, W, Y=None, workspace=None, variant=
 
 # --------------------------------------------------------- attention block ---
 _BF16, _I64, _BOOL = torch.bfloat16, torch.int64, torch.bool
+_ROPE_IN = (_F32, _BF16)
 
 
 class PagedKV:
@@ -713,6 +714,16 @@ def _vector(t, name, dtype, n):
         _on_gpu(**{name: t})
 
 
+def _head_weight(w, name, D):
+    """(address, type) of a norm's weight [D]."""
+    if _is(w, _BF16, (D,)):
+        return w.data_ptr(), PRQ_BF16
+    if not _is(w, _F32, (D,)):
+        _need(w, name, (_F32, _BF16), (D,))
+        _on_gpu(**{name: w})
+    return w.data_ptr(), PRQ_F32
+
+
 def _output(t, name, shape, dtype, like, stream):
     """An output of a call: `t`, checked, or a new one beside the tensor `like`."""
     if t is None:
@@ -731,12 +742,14 @@ def prq_qk_norm_rope(q, k, v, positions, table, cache, slots, q_weight=None, k_w
     values go to `slots` int64 [M] of the cache (-1: nowhere).  table: prq_rope_table's, or None
     for no rotation."""
     D, Hk = cache.D, cache.heads
-    if not isinstance(q, torch.Tensor) or q.dim() != 2 or q.shape[1] % D or q.shape[1] == 0:
+    if not isinstance(q, torch.Tensor) or q.dim() != 2:
         raise ValueError(f"q must be [M, heads * {D}]")
     M, wide = q.shape
-    Hq, kind = wide // D, (q.dtype,)
-    ld_q = _rows(q, "q", (_F32, _BF16), M, wide)
-    ld_k, ld_v = _rows(k, "k", kind, M, Hk * D), _rows(v, "v", kind, M, Hk * D)
+    if wide % D or not wide:
+        raise ValueError(f"q must be [M, heads * {D}]")
+    Hq, kind, wide_k = wide // D, (q.dtype,), Hk * D
+    ld_q = _rows(q, "q", _ROPE_IN, M, wide)
+    ld_k, ld_v = _rows(k, "k", kind, M, wide_k), _rows(v, "v", kind, M, wide_k)
     rot = rows = 0
     table_at = positions_at = None
     if table is not None:
@@ -749,18 +762,18 @@ def prq_qk_norm_rope(q, k, v, positions, table, cache, slots, q_weight=None, k_w
             _vector(positions, "positions", _I32, M)
             table_at, positions_at = table.data_ptr(), positions.data_ptr()
     _vector(slots, "slots", _I64, M)
-    w_kind = _F32
-    for name, w in (("q_weight", q_weight), ("k_weight", k_weight)):
-        if w is not None:
-            if not (_is(w, _BF16, (D,)) or _is(w, _F32, (D,))):
-                _need(w, name, (_F32, _BF16), (D,))
-                _on_gpu(**{name: w})
-            w_kind = w.dtype
-    if q_weight is not None and q_weight.dtype is not w_kind:
-        raise ValueError("q_weight and k_weight must have one type")
+    wq = wk = None
+    w_kind = 0
+    if k_weight is not None:
+        wk, w_kind = _head_weight(k_weight, "k_weight", D)
+    if q_weight is not None:
+        wq, kind = _head_weight(q_weight, "q_weight", D)
+        if wk is not None and kind != w_kind:
+            raise ValueError("q_weight and k_weight must have one type")
+        w_kind = kind
     out = _output(out, "out", (M, Hq, D), _BF16, q, stream)
     st = _qk_norm_rope(q.data_ptr(), ld_q, k.data_ptr(), ld_k, v.data_ptr(), ld_v, int(q.dtype is _BF16), M, Hq, Hk, D,
-                       _ptr(q_weight), _ptr(k_weight), int(w_kind is _BF16), eps, positions_at, table_at, rows, rot,
+                       wq, wk, w_kind, eps, positions_at, table_at, rows, rot,
                        int(interleaved), out.data_ptr(), cache.K.data_ptr(), cache.V.data_ptr(), cache.stride,
                        cache.pages, cache.page_size, slots.data_ptr(), _stream_of_call(stream))
     _check(st, "prq_qk_norm_rope")
