@@ -505,8 +505,11 @@ int prq_qk_norm_rope(const void* q, int64_t ld_q, const void* k, int64_t ld_k, c
  *   tree_mask  [M] rows of mask_wide bytes, ld_mask apart, or NULL
  *   out        [M][Hq][D] bf16
  *   lse        [M][Hq] float32, or NULL
- *   workspace  prq_tree_attention_workspace_bytes(...) bytes, 16-byte aligned;
- *              need not be cleared, and holds nothing between calls
+ *   workspace  prq_tree_attention_workspace_bytes(...) bytes, 16-byte aligned.
+ *              Starts with a 16 KiB state head, as prq_gemm's does: zero before
+ *              the first use, left zero by every call; the rest need not be
+ *              cleared and holds nothing between calls.  Calls that may overlap
+ *              need workspaces of their own
  * Scores, statistics and sums are float32; probabilities are rounded to bf16 as
  * they enter the second product.  Bitwise reproducible.  PRQ_EINVAL, PRQ_EALIGN,
  * PRQ_EUNSUPPORTED (D, page_size; B > 4096; M * Hq > 2^25; pages_wide * page_size >

@@ -104,7 +104,7 @@ int prq_qk_norm_rope(const void* q, int64_t ld_q, const void* k, int64_t ld_k, c
 size_t prq_tree_attention_workspace_bytes(int32_t M, int32_t B, int32_t Hq, int32_t Hk, int32_t D,
                                           int32_t max_kv_len) {
   if (check_tree_sizes(M, B, Hq, Hk, D, max_kv_len) != PRQ_OK || M == 0 || B == 0) return 0;
-  return prq::tree_workspace_bytes(prq::plan_tree_attention(M, B, Hq, Hk, D, max_kv_len, device_cus()), M, Hq, D);
+  return prq::tree_workspace_bytes(prq::plan_tree_attention(M, B, Hq, Hk, D, max_kv_len, device_cus()), M, D);
 }
 
 int prq_tree_attention(const void* q, int64_t ld_q, int32_t M, int32_t Hq, int32_t Hk, int32_t D,
@@ -131,7 +131,7 @@ int prq_tree_attention(const void* q, int64_t ld_q, int32_t M, int32_t Hq, int32
   if (st != PRQ_OK) return st;
   const prq::TreePlan plan = prq::plan_tree_attention(M, B, Hq, Hk, D, max_kv_len, cus);
   if (plan.blocks > kMaxBlocks) return PRQ_EUNSUPPORTED;
-  const size_t need = prq::tree_workspace_bytes(plan, M, Hq, D);
+  const size_t need = prq::tree_workspace_bytes(plan, M, D);
   if (need && (!workspace || workspace_bytes < need)) return PRQ_EWORKSPACE;
   if (need && !aligned(workspace, 16)) return PRQ_EALIGN;
   return launch_status(prq::launch_tree_attention(

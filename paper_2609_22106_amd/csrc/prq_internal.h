@@ -214,14 +214,16 @@ hipError_t launch_qk_norm_rope(const void* q, int64_t ld_q, const void* k, int64
                                int rot, bool interleaved, uint16_t* q_out, const PagedCache& cache,
                                const int64_t* slots, int num_cus, hipStream_t stream);
 
-// tree_attention.hip.  Query columns a workgroup (16, 32 or 64), their tiles over all
-// requests, parts of a request's keys, and the blocks of the launch.
+// tree_attention.hip.  Query columns a workgroup (16, 64 or 128); slots a kv head, each a
+// tile of one request's columns and a part of its keys; whether keys are split, and if so
+// whether the tiles fill the chip as it is; the blocks of the launch.
 struct TreePlan {
-  int tile_cols = 16, splits = 1;
-  int64_t tiles = 0, blocks = 0;
+  int tile_cols = 16, step = 128;    // parts are multiples of `step` keys
+  bool split = false, spread = false;
+  int64_t slots = 0, blocks = 0;
 };
 TreePlan plan_tree_attention(int M, int B, int Hq, int Hk, int D, int max_kv_len, int num_cus);
-size_t tree_workspace_bytes(const TreePlan& c, int M, int Hq, int D);
+size_t tree_workspace_bytes(const TreePlan& c, int M, int D);
 hipError_t launch_tree_attention(const TreePlan& c, const uint16_t* q, int64_t ld_q, int M, int Hq, int Hk, int D,
                                  const PagedCache& cache, const int32_t* pages, int64_t ld_pages, int max_keys,
                                  const int32_t* cached, const int32_t* offsets, int B, float scale,

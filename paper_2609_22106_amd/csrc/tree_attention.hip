@@ -26,8 +26,11 @@
 // error 2^-9 each, as large as the rounding of the output; the sum that divides takes
 // the unrounded P).
 //
-// Few rows leave most CUs idle, so each request's keys are split into equal parts over
-// workgroups and the partial (m, l, O) joined by a second kernel in a fixed order.
+// Few rows leave most CUs idle, so a request's keys are split over workgroups: as many
+// parts as the chip holds at once, dealt to the requests by their lengths, and the partial
+// (m, l, O) joined in a fixed order: by the last part of a tile to arrive where there are few
+// columns, by a second kernel where they are many (13-node trees 50 us the first way, 24.5
+// the second: one workgroup is then slow to read all parts of a tile).
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -43,8 +46,9 @@ namespace {
 using dev::f32x4;
 using dev::u32x4v;
 
-constexpr int kWaves = 4, kThreads = 64 * kWaves;
-constexpr int kStep = 32 * kWaves;       // keys a narrow workgroup takes at a time
+constexpr int kWaves = 4, kThreads = 64 * kWaves;                // of the wide kernel
+template <int D>
+constexpr int kNarrowWaves = D <= 128 ? 8 : 4;                       // of the narrow one (by its registers)
 constexpr int kMaxSplits = 64;
 constexpr float kSlack = 8.0f;           // log2 a score may pass the maximum by before it is renewed
 constexpr float kNone = -INFINITY;
@@ -67,7 +71,10 @@ struct TreeArgs {
   uint16_t* out;
   float *lse, *part_o;
   float2* part_ml;
-  int M, B, Hq, Hk, G, tiles, splits;
+  uint32_t* arrived;                     // narrow: parts done, of every tile that has several (0 between calls)
+  int4* joins;                           // wide, of every row: its request's first row, first slot, tiles, parts
+  int M, B, Hq, Hk, G, slots, step;      // a part of the keys is a multiple of `step`
+  bool split, spread;                    // keys may be split; there are enough tiles as it is
 };
 
 __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
@@ -140,34 +147,137 @@ __device__ __forceinline__ void load_tile(const TreeArgs& p, const int64_t (&bas
 }
 
 // What a workgroup works on: a tile of one request's query columns (column c is token
-// c / G, head h G + c % G), and a range of its keys.
+// c / G, head h G + c % G), and a part of its keys.
 struct Part {
-  dev::TileAt at;
-  int h, split, c0, cols, cached, lo, hi;
+  int segment, first, rows;              // the request, its first row and their number
+  int h, c0, cols, cached, lo, hi;       // kv head, first column and their number, keys
+  int splits, first_slot, tiles;         // parts of this request's keys; the tile's slots are
+};                                       // first_slot + tiles s
+
+// Every lane's sum over itself and the lanes before it.
+__device__ __forceinline__ int prefix_sum(int x) {
+  x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xF, 0xF, false);    // row_shr 1, 2, 4, 8
+  x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xF, 0xF, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xF, 0xF, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xF, 0xF, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xA, 0xF, false);    // row_bcast 15, 31
+  x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xC, 0xF, false);
+  return x;
+}
+
+// One request as a lane holds it; offsets and lengths that no table should hold are
+// clamped, so that nothing outside the buffers is reached.
+struct Request {
+  int first = 0, rows = 0, cached = 0, tiles = 0, keys = 0, units = 0;
 };
 
-// false: nothing to do (where the keys are split, the join is told so).
-__device__ __forceinline__ bool find_part(const TreeArgs& p, int per_tile, Part* w) {
-  w->h = static_cast<int>(blockIdx.x) % p.Hk;
-  const int rest = static_cast<int>(blockIdx.x) / p.Hk;
-  w->split = rest / p.tiles;
-  w->at = dev::find_tile(p.offsets, p.cached, p.B, p.M, rest % p.tiles, p.G, per_tile);
-  if (w->at.segment < 0) return false;
-  w->c0 = w->at.tile * per_tile;
-  w->cols = min(w->at.rows * p.G - w->c0, per_tile);
-  w->cached = min(max(w->at.with, 0), p.max_keys);
-  const int keys = min(w->at.rows, p.max_keys - w->cached) + w->cached;
-  // equal parts of this request's own keys, whole steps
-  const int part = ((keys + p.splits - 1) / p.splits + kStep - 1) / kStep * kStep;
-  w->lo = min(w->split * part, keys);
-  w->hi = min(w->lo + part, keys);
-  if (p.splits == 1 || w->hi > w->lo) return true;
-  for (int x = static_cast<int>(threadIdx.x); x < w->cols; x += kThreads) {
-    const int c = w->c0 + x;
-    const int64_t row = w->at.first + c / p.G;
-    p.part_ml[(w->split * static_cast<int64_t>(p.M) + row) * p.Hq + w->h * p.G + c % p.G] = {kNone, 0.f};
+__device__ __forceinline__ Request load_request(const TreeArgs& p, int s, int per_tile) {
+  Request r;
+  if (s < p.B) {
+    r.first = p.offsets[s];
+    r.rows = p.offsets[s + 1];
+    r.cached = p.cached[s];
+    r.first = min(max(r.first, 0), p.M);
+    r.rows = max(min(max(r.rows, 0), p.M) - r.first, 0);
+    r.cached = min(max(r.cached, 0), p.max_keys);
+    r.tiles = (r.rows * p.G + per_tile - 1) / per_tile;
+    r.keys = min(r.rows, p.max_keys - r.cached) + r.cached;
+    r.units = (r.keys + p.step - 1) / p.step;
   }
-  return false;
+  return r;
+}
+
+// Parts of `units` of at most about 1 / per units each: a plan, any number is right.
+__device__ __forceinline__ int parts_of(int units, float per) {
+  return min(max(static_cast<int>(ceilf(static_cast<float>(units) * per)), 1), kMaxSplits);
+}
+
+// Slot x of the launch (the same for the kv heads).  A request's keys are cut into equal
+// parts, and the most units (of p.step keys) that a part may have is the least for which
+// the slots suffice: every workgroup then has as much to do, and all of them are on the
+// chip at once.  false: nothing to do.
+__device__ __forceinline__ bool find_part(const TreeArgs& p, int per_tile, Part* w) {
+  const int lane = static_cast<int>(threadIdx.x) & 63;
+  w->h = static_cast<int>(blockIdx.x) % p.Hk;
+  const int x = static_cast<int>(blockIdx.x) / p.Hk;
+  Request r = load_request(p, lane, per_tile);
+  float per = 0.f;                       // parts a unit
+  if (p.split && !p.spread && p.B == 1) {
+    per = static_cast<float>(p.slots / max(r.tiles, 1)) / static_cast<float>(max(r.units, 1));
+    per = __shfl(per, 0) * 0.999f;       // rounded up by parts_of, and never past the slots
+  } else if (p.split) {
+    int tiles = 0, longest = 1;
+    float total = 0.f;
+    for (int base = 0; base < p.B; base += 64) {
+      const Request y = base ? load_request(p, base + lane, per_tile) : r;
+      tiles += __builtin_amdgcn_readlane(prefix_sum(y.tiles), 63);
+      float units = static_cast<float>(y.tiles) * static_cast<float>(y.units);
+      int top = y.units;
+#pragma unroll
+      for (int d = 32; d > 0; d >>= 1) {
+        units += __shfl_xor(units, d);
+        top = max(top, __shfl_xor(top, d));
+      }
+      total += __shfl(units, 0);
+      longest = max(longest, __shfl(top, 0));
+    }
+    // total / most + tiles parts at most: `high` suffices, nothing below `low` does.  Where
+    // there are tiles enough to fill the chip only what is half as long again as the mean
+    // is cut.
+    float low = max(total / p.slots, 1.f);
+    float high = p.slots > tiles ? max(min(total / (p.slots - tiles), static_cast<float>(longest)), low)
+                                 : static_cast<float>(longest);
+    if (p.spread)
+      high = 1.5f * max(total, 1.f) / max(tiles, 1);
+    else if (p.B <= 64)
+      for (int i = 0; i < 4; ++i) {
+        const float mid = 0.5f * (low + high);
+        const bool fits =
+            __builtin_amdgcn_readlane(prefix_sum(r.tiles * parts_of(r.units, 1.f / mid)), 63) <= p.slots;
+        low = fits ? low : mid;
+        high = fits ? mid : high;
+      }
+    per = p.slots > tiles ? 1.f / (1.0001f * high) : 0.f;
+  }
+  int before = 0, base = 0, at = -1, splits = 1, sum = 0;
+  for (; base < p.B; base += 64) {
+    if (base) r = load_request(p, base + lane, per_tile);
+    splits = p.split ? parts_of(r.units, per) : 1;
+    sum = prefix_sum(r.tiles * splits);
+    if (p.B <= 64 && __builtin_amdgcn_readlane(sum, 63) > p.slots) {   // (not by the bounds above)
+      splits = 1;
+      sum = prefix_sum(r.tiles);
+    }
+    const uint64_t past = __ballot(before + sum > x);
+    if (past) {
+      at = __builtin_ctzll(past);
+      break;
+    }
+    before += __builtin_amdgcn_readlane(sum, 63);
+  }
+  if (at < 0) return false;
+  const int tiles = __builtin_amdgcn_readlane(r.tiles, at);
+  const int keys = __builtin_amdgcn_readlane(r.keys, at);
+  w->segment = base + at;
+  w->first = __builtin_amdgcn_readlane(r.first, at);
+  w->rows = __builtin_amdgcn_readlane(r.rows, at);
+  w->cached = __builtin_amdgcn_readlane(r.cached, at);
+  w->splits = __builtin_amdgcn_readlane(splits, at);
+  const int slot = before + __builtin_amdgcn_readlane(sum, at) - tiles * w->splits;    // the request's first
+  const int split = (x - slot) / tiles, tile = (x - slot) - split * tiles;
+  w->tiles = tiles;
+  w->first_slot = slot + tile;
+  w->c0 = tile * per_tile;
+  w->cols = min(w->rows * p.G - w->c0, per_tile);
+  const int part = ((keys + w->splits - 1) / w->splits + p.step - 1) / p.step * p.step;
+  w->lo = min(split * part, keys);
+  w->hi = min(w->lo + part, keys);
+  return true;
+}
+
+// Output (row, query head) of a column.
+__device__ __forceinline__ int64_t head_of(const TreeArgs& p, const Part& w, int c) {
+  return (w.first + (w.c0 + c) / p.G) * static_cast<int64_t>(p.Hq) + w.h * p.G + (w.c0 + c) % p.G;
 }
 
 // Element offset of the 16-key block with key `key` on page `page` of the pool.  A block
@@ -189,13 +299,14 @@ struct Wave {
   f32x4 o[T][kV];
   float m[T], l[T];
 
+  // Tile t holds columns c0 + 16 t .. + 15.
   __device__ __forceinline__ void start(const TreeArgs& p, const Part& w, int c0) {
     const int lane = static_cast<int>(threadIdx.x) & 63, r = lane & 15, g = lane >> 4;
 #pragma unroll
     for (int t = 0; t < T; ++t) {
       const int c = c0 + 16 * t + r;     // past the last column: the last token, not stored
-      token[t] = min(c / p.G, w.at.rows - 1);
-      const uint16_t* qp = p.q + (w.at.first + token[t]) * p.ld_q + (w.h * p.G + c % p.G) * D + 8 * g;
+      token[t] = min(c / p.G, w.rows - 1);
+      const uint16_t* qp = p.q + (w.first + token[t]) * p.ld_q + (w.h * p.G + c % p.G) * D + 8 * g;
 #pragma unroll
       for (int k = 0; k < kChunks; ++k) q[t][k] = *reinterpret_cast<const u32x4v*>(qp + 32 * k) ^ p.flip;
       m[t] = kNone;
@@ -232,7 +343,7 @@ struct Wave {
     if constexpr (!kPlain) {
 #pragma unroll
       for (int t = 0; t < T; ++t) {
-        const uint8_t* see = p.mask ? p.mask + (w.at.first + token[t]) * p.ld_mask : nullptr;
+        const uint8_t* see = p.mask ? p.mask + (w.first + token[t]) * p.ld_mask : nullptr;
         seen[t] = 0;
 #pragma unroll
         for (int e = 0; e < kOwn; ++e) {
@@ -355,32 +466,151 @@ struct Wave {
 
 // The page of the block at `key`, -1 where there is none.
 __device__ __forceinline__ int page_entry(const TreeArgs& p, const Part& w, int key) {
-  const int page = key < w.hi ? p.pages[w.at.segment * p.ld_pages + (key >> p.page_shift)] : -1;
+  const int page = key < w.hi ? p.pages[w.segment * p.ld_pages + (key >> p.page_shift)] : -1;
   return page < p.num_pages ? page : -1;
 }
 
-// Up to 16 query columns: the waves take every fourth 32 keys each, straight into
+// Values that another workgroup reads in this launch, perhaps on another XCD with an L2 of its
+// own: device-scope accesses, 8 bytes each.
+__device__ __forceinline__ void put(void* at, float a, float b) {
+  const uint64_t x = static_cast<uint64_t>(__float_as_uint(b)) << 32 | __float_as_uint(a);
+  __hip_atomic_store(static_cast<uint64_t*>(at), x, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+__device__ __forceinline__ void put(float* at, f32x4 v) {
+  put(at, v[0], v[1]);
+  put(at + 2, v[2], v[3]);
+}
+__device__ __forceinline__ float2 get(const void* at) {
+  const uint64_t x =
+      __hip_atomic_load(static_cast<const uint64_t*>(at), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  return {__uint_as_float(static_cast<uint32_t>(x)), __uint_as_float(static_cast<uint32_t>(x >> 32))};
+}
+
+// The end of a narrow workgroup with one of several parts of a tile: the last of them to
+// arrive joins the parts' (m, l, O), in an order that does not depend on who that is.  sh:
+// LDS of kJoinFloats, no longer used for anything else.
+template <int D>
+constexpr int kJoinCols = D <= 128 ? 4 : 1;                  // columns at a time
+constexpr int kJoinWeights = 16 * (2 * kMaxSplits + 1);
+template <int D>
+constexpr int kJoinFloats = kJoinWeights + 2 * kJoinCols<D> * 64 * kNarrowWaves<D>;
+
+template <int D>
+__device__ __forceinline__ void join_parts(const TreeArgs& p, const Part& w, float* sh) {
+  constexpr int kThreads = 64 * kNarrowWaves<D>, kCols = kJoinCols<D>;
+  __shared__ int sh_last;
+  const int tid = static_cast<int>(threadIdx.x);
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");           // what this wave has put is there
+  __syncthreads();
+  uint32_t* const arrived = p.arrived + w.first_slot * p.Hk + w.h;
+  if (tid == 0)
+    sh_last = __hip_atomic_fetch_add(arrived, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) ==
+              static_cast<uint32_t>(w.splits - 1);
+  __syncthreads();
+  if (!sh_last) return;
+  if (tid == 0) __hip_atomic_store(arrived, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  auto part = [&](int s) { return (static_cast<int64_t>(w.first_slot + w.tiles * s) * p.Hk + w.h) * 16; };
+  // A thread's two elements of every kGroups-th part, kCols columns at a time; the
+  // first ones under way before their weights are known.
+  constexpr int kPairs = D / 2, kGroups = kThreads / kPairs, kEach = kMaxSplits / kGroups;
+  const int pair = tid % kPairs, group = tid / kPairs;
+  float2 in[kCols][kEach];
+  auto load = [&](int c0) {
+#pragma unroll
+    for (int c = 0; c < kCols; ++c)
+#pragma unroll
+      for (int y = 0; y < kEach; ++y)
+        if (c0 + c < w.cols && group + kGroups * y < w.splits)
+          in[c][y] = get(p.part_o + (part(group + kGroups * y) + c0 + c) * D + 2 * pair);
+  };
+  load(0);
+  // Each part's maximum, then its weight, in each column; its sum; 1 / the column's sum.
+  float* const weight = sh;                                  // [column][part]
+  float* const l = weight + 16 * kMaxSplits;                 // [column][part]
+  float* const inv = l + 16 * kMaxSplits;
+  float* const red = sh + kJoinWeights;                      // [group][column][D]
+  for (int e = tid; e < w.cols * w.splits; e += kThreads) {
+    const int c = e / w.splits, s = e - c * w.splits;
+    const float2 ml = get(p.part_ml + part(s) + c);
+    weight[c * kMaxSplits + s] = ml.x;
+    l[c * kMaxSplits + s] = ml.y;
+  }
+  __syncthreads();
+  for (int c = tid >> 6; c < w.cols; c += kNarrowWaves<D>) {    // a wave a column
+    const int s = tid & 63;
+    const float m = s < w.splits ? weight[c * kMaxSplits + s] : kNone;
+    float top = m;
+#pragma unroll
+    for (int d = 32; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor(top, d));
+    const float a = exp2_from(m, top, 1.0f);
+    float sum = s < w.splits ? a * l[c * kMaxSplits + s] : 0.f;
+#pragma unroll
+    for (int d = 32; d > 0; d >>= 1) sum += __shfl_xor(sum, d);
+    weight[c * kMaxSplits + s] = a;
+    if (s == 0) {
+      inv[c] = sum == 0.f ? 0.f : 1.0f / sum;
+      if (p.lse) p.lse[head_of(p, w, c)] = sum == 0.f ? kNone : (top + log2f(sum)) * 0.69314718055994531f;
+    }
+  }
+  __syncthreads();
+  for (int c0 = 0; c0 < w.cols; c0 += kCols) {
+    if (c0) load(c0);
+#pragma unroll
+    for (int c = 0; c < kCols; ++c) {
+      float2 o = {0.f, 0.f};
+#pragma unroll
+      for (int y = 0; y < kEach; ++y)
+        if (c0 + c < w.cols && group + kGroups * y < w.splits) {
+          const float a = weight[(c0 + c) * kMaxSplits + group + kGroups * y];
+          if (a != 0.f) {                                    // a part that a row saw nothing of adds nothing
+            o.x += a * in[c][y].x;
+            o.y += a * in[c][y].y;
+          }
+        }
+      *reinterpret_cast<float2*>(red + (group * kCols + c) * D + 2 * pair) = o;
+    }
+    __syncthreads();
+    for (int x = tid; x < kCols * kPairs; x += kThreads) {
+      const int c = x / kPairs, d = 2 * (x % kPairs);
+      if (c0 + c < w.cols) {
+        float2 o = {0.f, 0.f};
+#pragma unroll
+        for (int g = 0; g < kGroups; ++g) {
+          const float2 y = *reinterpret_cast<const float2*>(red + (g * kCols + c) * D + d);
+          o.x += y.x;
+          o.y += y.y;
+        }
+        *reinterpret_cast<uint32_t*>(p.out + head_of(p, w, c0 + c) * D + d) =
+            dev::pack_bf16(o.x * inv[c0 + c], o.y * inv[c0 + c]);
+      }
+    }
+    __syncthreads();
+  }
+}
+
+// Up to 16 query columns: the waves take every kN-th 32 keys each, straight into
 // registers, the next ones under way, and join through LDS at the end.
 template <int D>
-__global__ __launch_bounds__(kThreads, D <= 128 ? 2 : 1) void tree_attention_kernel(const TreeArgs p) {
-  constexpr int kV = D / 16, kPitch = D + 4;
-  __shared__ __align__(16) float sh_o[kWaves][16][kPitch];
-  __shared__ float sh_m[kWaves][16], sh_l[kWaves][16];
+__global__ __launch_bounds__(64 * kNarrowWaves<D>, D <= 128 ? 2 : 1) void tree_attention_kernel(const TreeArgs p) {
+  constexpr int kV = D / 16, kPitch = D + 4, kN = kNarrowWaves<D>, kThreads = 64 * kN, kStride = 32 * kN;
+  __shared__ __align__(16) float sh_o[kN][16][kPitch];
+  static_assert(kN * 16 * kPitch >= kJoinFloats<D>, "the join's LDS");
+  __shared__ float sh_m[kN][16], sh_l[kN][16];
   Part w;
   if (!find_part(p, 16, &w)) return;
   const int lane = static_cast<int>(threadIdx.x) & 63, r = lane & 15, g = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x) >> 6);
   const int first = w.lo + 32 * wave;
-  const int steps = w.hi > first ? (w.hi - first + kStep - 1) / kStep : 0;
+  const int steps = w.hi > first ? (w.hi - first + kStride - 1) / kStride : 0;
   // lane 2 s + b: page of block b of step s (of 32 steps)
-  int entries = page_entry(p, w, first + kStep * (lane >> 1) + 16 * (lane & 1));
+  int entries = page_entry(p, w, first + kStride * (lane >> 1) + 16 * (lane & 1));
   int page[2];
   auto load = [&](int step, Tile<D>* tile) {
     int64_t base[2];
 #pragma unroll
     for (int b = 0; b < 2; ++b) {
       page[b] = __builtin_amdgcn_readlane(entries, 2 * (step & 31) + b);
-      base[b] = block_base<D>(p, w.h, page[b], first + kStep * step + 16 * b);
+      base[b] = block_base<D>(p, w.h, page[b], first + kStride * step + 16 * b);
     }
     load_tile<D>(p, base, tile);
   };
@@ -392,15 +622,15 @@ __global__ __launch_bounds__(kThreads, D <= 128 ? 2 : 1) void tree_attention_ker
     const int page_now[2] = {page[0], page[1]};
     if (step + 1 < steps) {
       if (((step + 1) & 31) == 0)
-        entries = page_entry(p, w, first + kStep * (step + 1 + (lane >> 1)) + 16 * (lane & 1));
+        entries = page_entry(p, w, first + kStride * (step + 1 + (lane >> 1)) + 16 * (lane & 1));
       load(step + 1, &next);
     }
-    q.template step<decltype(plain)::value, 2>(p, w, now, first + kStep * step, page_now);
+    q.template step<decltype(plain)::value, 2>(p, w, now, first + kStride * step, page_now);
     if (step + 1 < steps) now = next;
   };
   // every row sees the whole step: of cached tokens alone, on pages of the pool
   int step = 0;
-  for (; step < steps && first + kStep * step + 32 <= min(w.cached, w.hi) && (page[0] | page[1]) >= 0; ++step)
+  for (; step < steps && first + kStride * step + 32 <= min(w.cached, w.hi) && (page[0] | page[1]) >= 0; ++step)
     one(step, std::true_type{});
   for (; step < steps; ++step) one(step, std::false_type{});
 
@@ -413,7 +643,13 @@ __global__ __launch_bounds__(kThreads, D <= 128 ? 2 : 1) void tree_attention_ker
     sh_l[wave][r] = l;
   }
   __syncthreads();
-  const float a = exp2_from(q.m[0], fmaxf(fmaxf(sh_m[0][r], sh_m[1][r]), fmaxf(sh_m[2][r], sh_m[3][r])), p.scale);
+  auto top_of = [&](int c) {
+    float top = sh_m[0][c];
+#pragma unroll
+    for (int y = 1; y < kN; ++y) top = max_of(top, sh_m[y][c]);
+    return top;
+  };
+  const float a = exp2_from(q.m[0], top_of(r), p.scale);
 #pragma unroll
   for (int i = 0; i < 4; ++i)
 #pragma unroll
@@ -424,29 +660,30 @@ __global__ __launch_bounds__(kThreads, D <= 128 ? 2 : 1) void tree_attention_ker
   constexpr int kPer = D / 8;            // threads a column
   for (int x = static_cast<int>(threadIdx.x); x < w.cols * kPer; x += kThreads) {
     const int c = x / kPer, d = 8 * (x % kPer);
-    const float top = fmaxf(fmaxf(sh_m[0][c], sh_m[1][c]), fmaxf(sh_m[2][c], sh_m[3][c]));
+    const float top = top_of(c);
     float sum = 0.f;
     f32x4 lo = {0.f, 0.f, 0.f, 0.f}, hi = lo;
 #pragma unroll
-    for (int y = 0; y < kWaves; ++y) {
+    for (int y = 0; y < kN; ++y) {
       sum += sh_l[y][c] * exp2_from(sh_m[y][c], top, p.scale);
       lo += *reinterpret_cast<const f32x4*>(&sh_o[y][c][d]);
       hi += *reinterpret_cast<const f32x4*>(&sh_o[y][c][d + 4]);
     }
-    const int64_t head = (w.at.first + (w.c0 + c) / p.G) * static_cast<int64_t>(p.Hq) + w.h * p.G + (w.c0 + c) % p.G;
-    if (p.splits == 1) {
+    const int64_t head = head_of(p, w, c);
+    if (w.splits == 1) {
       const float inv = sum == 0.f ? 0.f : 1.0f / sum;
       const u32x4v y = {dev::pack_bf16(lo[0] * inv, lo[1] * inv), dev::pack_bf16(lo[2] * inv, lo[3] * inv),
                         dev::pack_bf16(hi[0] * inv, hi[1] * inv), dev::pack_bf16(hi[2] * inv, hi[3] * inv)};
       *reinterpret_cast<u32x4v*>(p.out + head * D + d) = y;
       if (p.lse && d == 0) p.lse[head] = sum == 0.f ? kNone : (top * p.scale + log2f(sum)) * 0.69314718055994531f;
     } else {
-      const int64_t part = w.split * static_cast<int64_t>(p.M) * p.Hq + head;
-      *reinterpret_cast<f32x4*>(p.part_o + part * D + d) = lo;
-      *reinterpret_cast<f32x4*>(p.part_o + part * D + d + 4) = hi;
-      if (d == 0) p.part_ml[part] = {top * p.scale, sum};
+      const int64_t part = static_cast<int64_t>(blockIdx.x) * 16 + c;
+      put(p.part_o + part * D + d, lo);
+      put(p.part_o + part * D + d + 4, hi);
+      if (d == 0) put(p.part_ml + part, top * p.scale, sum);
     }
   }
+  if (w.splits > 1) join_parts<D>(p, w, &sh_o[0][0][0]);
 }
 
 // Copies 16 bytes a lane straight to LDS, lane l's at lds + 16 l (LDS address, the same for
@@ -495,13 +732,17 @@ template <int D, int T>
 __global__ __launch_bounds__(kThreads, D <= 128 ? 2 : 1) void tree_attention_wide_kernel(const TreeArgs p) {
   constexpr int kV = D / 16, kKeys = D <= 128 ? 64 : 32;
   constexpr int kUnits = D / 8, kRows = 64 / kUnits, kCopies = kKeys / kRows / kWaves;
-  __shared__ __align__(16) uint16_t sh[2][2][kKeys * D];     // stage, K or V
+  constexpr int kStage = 2 * kKeys * D;                      // K, then V
+  __shared__ __align__(16) uint16_t sh[2 * kStage];
   Part w;
   if (!find_part(p, 16 * T * kWaves, &w)) return;
+  if (p.split && w.h == 0 && static_cast<int>(blockIdx.x) / p.Hk == w.first_slot)      // for the join
+    for (int row = w.c0 / p.G + static_cast<int>(threadIdx.x); row * p.G < w.c0 + w.cols; row += kThreads)
+      p.joins[w.first + row] = {w.first, w.first_slot - w.c0 / (16 * T * kWaves), w.tiles, w.splits};
   const int lane = static_cast<int>(threadIdx.x) & 63, r = lane & 15, g = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x) >> 6);
   const uint32_t sh_at = static_cast<uint32_t>(
-      reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) void*)(&sh[0][0][0])));
+      reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) void*)(sh)));
   // Unit u of row k lies at unit u ^ turn(k).
   auto turn = [](int k) { return D == 64 ? (k >> 1) & 7 : k & 15; };
 
@@ -512,7 +753,7 @@ __global__ __launch_bounds__(kThreads, D <= 128 ? 2 : 1) void tree_attention_wid
 
   // A stage's rows are copied kRows to a wave copy (a kilobyte), lane i to unit i of it.
   auto load = [&](int stage) {
-    const uint32_t to = sh_at + (stage & 1) * 2 * kKeys * D * 2;
+    const uint32_t to = sh_at + (stage & 1) * kStage * 2;
 #pragma unroll
     for (int x = 0; x < kCopies; ++x) {
       const int c = wave + kWaves * x;                       // rows kRows c .. of the stage
@@ -555,7 +796,8 @@ __global__ __launch_bounds__(kThreads, D <= 128 ? 2 : 1) void tree_attention_wid
     }
     if (works) {
       constexpr int kBlocks = kKeys / 16;
-      const Staged<D> src{sh[stage & 1][0], sh[stage & 1][1], k_at, v_at};
+      const uint16_t* const ks = sh + (stage & 1) * kStage;
+      const Staged<D> src{ks, ks + kKeys * D, k_at, v_at};
       int page[kBlocks];
 #pragma unroll
       for (int b = 0; b < kBlocks; ++b)
@@ -574,9 +816,9 @@ __global__ __launch_bounds__(kThreads, D <= 128 ? 2 : 1) void tree_attention_wid
     sum += __shfl_xor(sum, 32);
     const int c = 16 * (T * wave + t) + r;
     if (c >= w.cols) continue;
-    const int64_t head = (w.at.first + (w.c0 + c) / p.G) * static_cast<int64_t>(p.Hq) + w.h * p.G + (w.c0 + c) % p.G;
+    const int64_t head = head_of(p, w, c);
     const float top = q.m[t] * p.scale;
-    if (p.splits == 1) {
+    if (w.splits == 1) {
       const float inv = sum == 0.f ? 0.f : 1.0f / sum;
 #pragma unroll
       for (int i = 0; i < 4; ++i)
@@ -588,7 +830,7 @@ __global__ __launch_bounds__(kThreads, D <= 128 ? 2 : 1) void tree_attention_wid
         }
       if (p.lse && g == 0) p.lse[head] = sum == 0.f ? kNone : (top + log2f(sum)) * 0.69314718055994531f;
     } else {
-      const int64_t part = w.split * static_cast<int64_t>(p.M) * p.Hq + head;
+      const int64_t part = static_cast<int64_t>(blockIdx.x) * (16 * T * kWaves) + c;
 #pragma unroll
       for (int i = 0; i < 4; ++i)
 #pragma unroll
@@ -600,26 +842,39 @@ __global__ __launch_bounds__(kThreads, D <= 128 ? 2 : 1) void tree_attention_wid
   }
 }
 
-// The splits' (m, l, O) of one row and head, a wave each.
+// After the wide kernel: the parts' (m, l, O) of one row and head, a wave each; nothing
+// where a workgroup had all of the row's keys.  (What `joins` holds for a row of no request
+// may be anything: it is clamped to the workspace.)
 template <int D>
 __global__ __launch_bounds__(kThreads) void tree_join_kernel(const float* __restrict__ part_o,
-                                                             const float2* __restrict__ part_ml, int64_t heads,
-                                                             int splits, uint16_t* __restrict__ out,
-                                                             float* __restrict__ lse) {
-  constexpr int kPer = D / 4, kAtOnce = 64 / kPer;     // lanes a split, splits a load
+                                                             const float2* __restrict__ part_ml,
+                                                             const int4* __restrict__ joins, int64_t heads, int Hq,
+                                                             int Hk, int tile_cols, int slots,
+                                                             uint16_t* __restrict__ out, float* __restrict__ lse) {
+  constexpr int kPer = D / 4, kAtOnce = 64 / kPer;     // lanes a part, parts a load
   constexpr int kBatch = 8;                            // loads under way
   const int lane = static_cast<int>(threadIdx.x) & 63;
   const int64_t head = static_cast<int64_t>(blockIdx.x) * kWaves + (threadIdx.x >> 6);
   if (head >= heads) return;
+  const int64_t row = head / Hq;
+  const int4 j = joins[row];
+  const int splits = min(j.w, kMaxSplits);
+  if (splits <= 1) return;
+  const int G = Hq / Hk, q = static_cast<int>(head - row * Hq);
+  const uint32_t c = static_cast<uint32_t>((row - j.x) * G + q % G);
+  const int col = static_cast<int>(c % tile_cols), tile = static_cast<int>(c / tile_cols);
+  auto at = [&](int s) {
+    const int64_t slot = j.y + static_cast<int64_t>(s) * j.z + tile;
+    return (min(max(slot, int64_t{0}), static_cast<int64_t>(slots - 1)) * Hk + q / G) * tile_cols + col;
+  };
   float2 ml = {kNone, 0.f};
-  if (lane < splits) ml = part_ml[lane * heads + head];
+  if (lane < splits) ml = part_ml[at(lane)];
   f32x4 in[kBatch];
   auto load = [&](int s0) {
 #pragma unroll
-    for (int x = 0; x < kBatch; ++x) {
-      const int s = min(s0 + x * kAtOnce + lane / kPer, splits - 1);
-      in[x] = *reinterpret_cast<const f32x4*>(part_o + (s * heads + head) * D + 4 * (lane % kPer));
-    }
+    for (int x = 0; x < kBatch; ++x)
+      in[x] = *reinterpret_cast<const f32x4*>(part_o + at(min(s0 + x * kAtOnce + lane / kPer, splits - 1)) * D +
+                                              4 * (lane % kPer));
   };
   load(0);
   float top = ml.x;
@@ -636,7 +891,7 @@ __global__ __launch_bounds__(kThreads) void tree_join_kernel(const float* __rest
     for (int x = 0; x < kBatch; ++x) {
       const int s = s0 + x * kAtOnce + lane / kPer;
       const float w = __shfl(a, s & 63);
-      if (s < splits && w != 0.f) o += w * in[x];      // a split with nothing for this row wrote no O
+      if (s < splits && w != 0.f) o += w * in[x];      // a part that a row saw nothing of adds nothing
     }
   }
 #pragma unroll
@@ -655,15 +910,15 @@ template <int D>
 void launch(const TreeArgs& p, int tile_cols, int64_t blocks, hipStream_t stream) {
   const dim3 grid(static_cast<unsigned>(blocks));
   if (tile_cols == 16)
-    tree_attention_kernel<D><<<grid, kThreads, 0, stream>>>(p);
+    tree_attention_kernel<D><<<grid, 64 * kNarrowWaves<D>, 0, stream>>>(p);
   else if (tile_cols == 64)
     tree_attention_wide_kernel<D, 1><<<grid, kThreads, 0, stream>>>(p);
   else if constexpr (D <= 128)
     tree_attention_wide_kernel<D, 2><<<grid, kThreads, 0, stream>>>(p);
-  if (p.splits > 1) {
+  if (p.split && tile_cols > 16) {
     const int64_t heads = static_cast<int64_t>(p.M) * p.Hq;
     tree_join_kernel<D><<<dim3(static_cast<unsigned>((heads + kWaves - 1) / kWaves)), kThreads, 0, stream>>>(
-        p.part_o, p.part_ml, heads, p.splits, p.out, p.lse);
+        p.part_o, p.part_ml, p.joins, heads, p.Hq, p.Hk, tile_cols, p.slots, p.out, p.lse);
   }
 }
 
@@ -675,18 +930,27 @@ TreePlan plan_tree_attention(int M, int B, int Hq, int Hk, int D, int max_kv_len
   const int64_t used = std::max(1, std::min(M, B));
   const int64_t per = (M * G + used - 1) / used;        // query columns of a mean request
   c.tile_cols = per <= 16 ? 16 : per <= 64 || D > 128 ? 64 : 128;
-  c.tiles = most_tiles(M, B, G, c.tile_cols);
-  const int64_t groups = c.tiles * Hk;
-  const int64_t want = (4 * static_cast<int64_t>(num_cus) + groups - 1) / groups;
-  const int64_t keys = std::max(max_kv_len, 1);
-  const int64_t most = std::min<int64_t>(kMaxSplits, (keys + kStep - 1) / kStep);
-  c.splits = static_cast<int>(std::max<int64_t>(1, std::min(want, most)));
-  c.blocks = groups * c.splits;
+  c.step = c.tile_cols == 16 ? 32 * (D <= 128 ? kNarrowWaves<128> : kNarrowWaves<256>) : 128;
+  const int64_t tiles = most_tiles(M, B, G, c.tile_cols);
+  // Slots a kv head: as many as the chip holds workgroups at once (by their registers and
+  // LDS), but no more than there are parts; where the tiles alone are that many, some for
+  // requests that are longer than the others.
+  const int per_cu = c.tile_cols == 16 || D > 128 ? 1 : D == 128 || c.tile_cols == 128 ? 2 : 4;
+  const int64_t at_once = std::max<int64_t>(static_cast<int64_t>(per_cu) * num_cus / Hk, 1);
+  const int64_t parts = tiles * std::min<int64_t>(kMaxSplits, std::max((max_kv_len + c.step - 1) / c.step, 1));
+  c.spread = tiles >= at_once;
+  c.slots = c.spread ? tiles + (2 * tiles + 2) / 3 : std::max(tiles, std::min(at_once, parts));
+  c.split = c.slots > tiles && tiles < 4 * at_once &&
+            c.slots * Hk * static_cast<int64_t>(sizeof(uint32_t)) <= static_cast<int64_t>(kWorkspaceStateBytes);
+  if (!c.split) c.slots = tiles;
+  c.blocks = c.slots * Hk;
   return c;
 }
 
-size_t tree_workspace_bytes(const TreePlan& c, int M, int Hq, int D) {
-  return c.splits > 1 ? static_cast<size_t>(c.splits) * M * Hq * (D + 2) * 4 : 0;
+size_t tree_workspace_bytes(const TreePlan& c, int M, int D) {
+  if (!c.split) return 0;
+  return kWorkspaceStateBytes + static_cast<size_t>(c.blocks) * c.tile_cols * (D + 2) * 4 +
+         static_cast<size_t>(M) * sizeof(int4);
 }
 
 hipError_t launch_tree_attention(const TreePlan& c, const uint16_t* q, int64_t ld_q, int M, int Hq, int Hk, int D,
@@ -694,15 +958,17 @@ hipError_t launch_tree_attention(const TreePlan& c, const uint16_t* q, int64_t l
                                  const int32_t* cached, const int32_t* offsets, int B, float scale,
                                  const uint8_t* mask, int64_t ld_mask, int mask_wide, uint16_t* out, float* lse,
                                  void* workspace, hipStream_t stream) {
-  const int64_t heads = static_cast<int64_t>(M) * Hq;
-  float* const part_o = static_cast<float*>(workspace);
-  float2* const part_ml = c.splits > 1 ? reinterpret_cast<float2*>(part_o + c.splits * heads * D) : nullptr;
+  const int64_t cols = c.blocks * c.tile_cols;
+  uint32_t* const arrived = static_cast<uint32_t*>(workspace);         // the state head
+  float* const part_o = c.split ? reinterpret_cast<float*>(static_cast<char*>(workspace) + kWorkspaceStateBytes) : nullptr;
+  float2* const part_ml = c.split ? reinterpret_cast<float2*>(part_o + cols * D) : nullptr;
+  int4* const joins = c.split ? reinterpret_cast<int4*>(part_ml + cols) : nullptr;
   // A negative scale turns the queries' signs; 0 is as good as the smallest used here
   // (q . k times it vanishes beside 1) and keeps an unseen -inf from becoming 0 x inf.
   const float size = std::max(std::fabs(scale) * 1.44269504088896341f, 0x1p-100f);
   const TreeArgs p{q, ld_q, cache.K, cache.V, cache.page_stride, cache.page_shift, cache.num_pages, pages, ld_pages,
                    max_keys, cached, offsets, mask, ld_mask, mask_wide, size, kSlack / size,
-                   std::signbit(scale) ? 0x80008000u : 0u, out, lse, part_o, part_ml, M, B, Hq, Hk, Hq / Hk, static_cast<int>(c.tiles), c.splits};
+                   std::signbit(scale) ? 0x80008000u : 0u, out, lse, part_o, part_ml, arrived, joins, M, B, Hq, Hk, Hq / Hk, static_cast<int>(c.slots), c.step, c.split, c.spread};
   if (D == 64) launch<64>(p, c.tile_cols, c.blocks, stream);
   else if (D == 128) launch<128>(p, c.tile_cols, c.blocks, stream);
   else launch<256>(p, c.tile_cols, c.blocks, stream);

@@ -790,7 +790,8 @@ def prq_tree_attention(q, cache, page_table, cached_lens, q_offsets, scale, tree
     bf16, lse [M, Hq] float32).  Request b's own tokens follow its cached_lens[b] (int32 [B]) cached
     ones on its pages (page_table int32 [B, pages]); tree_mask bool [M, w] says which of its own tokens
     a row sees (None: itself and those before it).  max_kv_len: the most tokens a request has (default:
-    what the page table holds).  workspace: uint8, prq_tree_attention_workspace_bytes (else allocated)."""
+    what the page table holds).  workspace: uint8, prq_tree_attention_workspace_bytes, zeroed before its
+    first use and left ready by every call (else allocated, zeroed by another launch)."""
     if not (type(q) is torch.Tensor and q.dtype is _BF16 and q.is_cuda and q.dim() == 3 and q.shape[2] == cache.D
             and (q.is_contiguous() or (q.stride(2) == 1 and (q.shape[1] <= 1 or q.stride(1) == cache.D)))):
         raise ValueError(f"q must be a bfloat16 GPU tensor [M, heads, {cache.D}] with contiguous rows")
@@ -815,7 +816,7 @@ def prq_tree_attention(q, cache, page_table, cached_lens, q_offsets, scale, tree
     if workspace is None:
         need = int(_tree_ws(M, B, Hq, cache.heads, D, max_kv_len))
         if need:
-            workspace = _alloc(torch.empty, need, _U8, q.device, stream, kept=False)
+            workspace = _alloc(torch.zeros, need, _U8, q.device, stream, kept=False)
     ws, ws_bytes = _workspace_arg(workspace)
     st = _tree(q.data_ptr(), ld_q, M, Hq, cache.heads, D, cache.K.data_ptr(), cache.V.data_ptr(), cache.stride,
                cache.pages, cache.page_size, page_table.data_ptr(), ld_pages, wide, cached_lens.data_ptr(),

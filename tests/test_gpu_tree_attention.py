@@ -275,17 +275,37 @@ def test_pool_past_32_bits():
     assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
 
 
-def test_calls_repeat_bit_for_bit_and_need_no_clean_workspace():
+def test_calls_repeat_bit_for_bit_and_leave_the_state_head_zero():
+    """Whatever the scratch behind the head held, and for calls of other sizes in between."""
     prq = _prq()
     c = Case([(3000, 2), (100, 1)], 32, 8, 128, 64)
+    other = Case([(1500, 40)], 8, 2, 64, 16)
     need = prq.prq_tree_attention_workspace_bytes(3, 2, 32, 8, 128, 3002)
-    assert need > 0
-    a = c.run(workspace=torch.zeros(need, dtype=torch.uint8, device="cuda"))
-    b = c.run(workspace=torch.full((need,), 255, dtype=torch.uint8, device="cuda"))
-    assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1])
+    assert need > 16384
+    ws = torch.zeros(64 << 20, dtype=torch.uint8, device="cuda")
+    a = c.run(workspace=ws)
+    for fill in (255, 1):
+        ws[16384:] = fill
+        b = c.run(workspace=ws)
+        assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1])
+        other.check(*other.run(workspace=ws))
+        assert not ws[:16384].any()
+    d = c.run()
+    assert torch.equal(a[0], d[0]) and torch.equal(a[1], d[1])
     with pytest.raises(prq.PRQError) as e:
         c.run(workspace=torch.zeros(need - 1, dtype=torch.uint8, device="cuda"))
     assert e.value.status == prq.PRQ_EWORKSPACE
+
+
+def test_uneven_requests_share_the_chip():
+    """One long request among short ones, more requests than a wave has lanes, and both."""
+    rng = np.random.default_rng(3)
+    for requests in ([(9000, 1)] + [(int(rng.integers(0, 60)), 1) for _ in range(20)],
+                     [(int(rng.integers(0, 400)), int(rng.integers(0, 3))) for _ in range(70)] + [(4000, 2)],
+                     [(5000, 9), (0, 0), (17, 30), (2500, 3)]):
+        say("uneven", requests[:3])
+        c = Case(requests, 4, 1, 64, 16)
+        c.check(*c.run())
 
 
 def test_no_rows_and_no_requests():
