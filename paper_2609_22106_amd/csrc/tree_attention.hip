@@ -7,18 +7,25 @@
 //   s_j = scale q . k_j,  p = softmax of the visible s,  o = sum_j p_j v_j,
 // o = 0 and lse = -inf for a row that sees nothing.
 //
-// One pass over K and V with the running maximum and sum: a wave takes 32 keys at a
-// time and holds everything in registers.  Scores are computed transposed, keys x
-// queries (A = K rows, B = Q rows), so that a lane ends with 8 keys of one query:
-// rounded to bf16 they are its operand of the second product, O^T = V^T P^T, as they
-// stand.  That product's A operand needs 8 keys of one column of V: a lane group loads
-// whole rows of its 8 keys, 16 lanes a row, and pairs up halves of registers
-// (32 v_perm per 32 x 128 tile).  The 16 queries of a product's column side are the G
-// query heads of the kv head for 16 / G tokens.  Up to 16 columns a request, the waves
-// take keys of their own, straight from memory into registers, and join their results
-// through LDS; more columns are dealt to the waves, one or two tiles each, and K and V go
-// through LDS once for all of them (trees of up to 64 nodes over 8 x 32 k tokens: four tiles
-// a wave straight from memory 714 us, through LDS 303).
+// One pass over K and V with the running maximum and sum.  Scores are computed transposed,
+// keys x queries (A = K rows, B = Q rows), so that a lane ends with 8 of 32 keys of one
+// query: rounded to bf16 they are its operand of the second product, O^T = V^T P^T, as they
+// stand.  The 16 queries of a product's column side are the G query heads of the kv head for
+// 16 / G tokens.
+//
+// Up to 16 columns a request (narrow): K and V are read once for few products, so memory
+// bounds it.  The waves of a workgroup take 32 keys each at a time, straight into registers,
+// the next ones under way, and join through LDS.  V's operand needs 8 keys of one column: a
+// lane group loads whole rows of its 8 keys, 16 lanes a row, and pairs up halves of registers
+// (32 v_perm per 32 x 128 tile).  32 sequences of 1 .. 8192 tokens, 8 kv heads of 128:
+// 46 us, 206 MB of K and V at 4.5 TB/s; one token over 4097: 13.9 us, the latency of the
+// loads, the arrival and the join one after another.
+//
+// More columns (wide): they are dealt to the waves, one or two tiles of 16 each, and 64 keys
+// at a time go through LDS once for all of them, copied there without a register; V is read
+// back transposed.  64-node trees over 8 x 32 k tokens: straight from memory 714 us, through
+// LDS with v_perm 272, transposed reads 255 .. 262: 610 TFLOP/s, matrix units a third of the
+// time, the exponentials and the rest of the vector work more than that.
 //
 // The maximum is kept per lane group and only joined across the groups when a score
 // passes it by 8 (powers of two): until then the stale maximum serves, P up to 2^8.
@@ -89,9 +96,7 @@ __device__ __forceinline__ float exp2_from(float a, float b, float scale) {
 __device__ __forceinline__ float max_of(float a, float b) { return __builtin_elementwise_maximum(a, b); }
 __device__ __forceinline__ float max_of(float a, float b, float c) { return max_of(max_of(a, b), c); }
 
-__device__ __forceinline__ bool word_finite(uint32_t w) {
-  return (w & 0x7F80u) != 0x7F80u && (w & 0x7F800000u) != 0x7F800000u;
-}
+__device__ __forceinline__ bool finite_bf16(uint32_t b) { return (b & 0x7F80u) != 0x7F80u; }
 
 // K and V of two 16-key blocks, as a lane (g = l / 16, r = l % 16) holds them.
 template <int D>
@@ -104,12 +109,17 @@ struct Tile {
 #pragma unroll
     for (int c = 0; c < kChunks; ++c) out[c] = keys[b][c];
   }
-  __device__ __forceinline__ void v(int, uint32_t (&out)[8][kWords]) const {
+  // V^T's operand of the product's dims dim(x, 0 .. 15): register pairs of neighbouring keys
+  // -> the low or the high halves.
+  __device__ __forceinline__ u32x4v v(int, int x) const {
+    u32x4v out;
 #pragma unroll
-    for (int e = 0; e < 8; ++e)
-#pragma unroll
-      for (int x = 0; x < kWords; ++x) out[e][x] = values[e][x];
+    for (int e = 0; e < 4; ++e)
+      out[e] = __builtin_amdgcn_perm(values[2 * e + 1][x >> 1], values[2 * e][x >> 1],
+                                     x & 1 ? 0x07060302u : 0x05040100u);
+    return out;
   }
+  static __device__ __forceinline__ int dim(int x, int m) { return D / 16 * m + x; }
 };
 
 // A lane's part of one row of V.
@@ -272,6 +282,8 @@ __device__ __forceinline__ bool find_part(const TreeArgs& p, int per_tile, Part*
   const int part = ((keys + w->splits - 1) / w->splits + p.step - 1) / p.step * p.step;
   w->lo = min(split * part, keys);
   w->hi = min(w->lo + part, keys);
+  if (!p.mask)                           // a chain: nothing past the tile's last token is seen
+    w->hi = max(min(w->hi, w->cached + (w->c0 + w->cols - 1) / p.G + 1), w->lo);
   return true;
 }
 
@@ -318,26 +330,34 @@ struct Wave {
 
   // The 16 kBlocks keys from k0 on; block b of them on page page[b] of the pool (-1: none).
   // kPlain: every row sees all of them.
-  // `src`: where the operands are, k(b, ..) block b's keys, v(b, ..) those of blocks b and
-  // b + 1.
+  // `src`: where the operands are, k(b, ..) block b's keys, v(b, x) V^T's for the keys of
+  // blocks b and b + 1 and the dims dim(x, 0 .. 15).
   template <bool kPlain, int kBlocks, typename Source>
   __device__ __forceinline__ void step(const TreeArgs& p, const Part& w, const Source& src, int k0,
                                        const int (&page)[kBlocks]) {
     constexpr int kOwn = 4 * kBlocks;    // keys of a lane: e is 16 (e / 4) + 4 g + e % 4
     const int lane = static_cast<int>(threadIdx.x) & 63, r = lane & 15, g = lane >> 4;
     float s[T][kOwn];
+    // two blocks at a time: a product does not wait for the one before it
 #pragma unroll
-    for (int b = 0; b < kBlocks; ++b) {
-      u32x4v k[kChunks];
-      src.k(b, k);
+    for (int b = 0; b < kBlocks; b += 2) {
+      u32x4v k[2][kChunks];
+      f32x4 x[T][2];
 #pragma unroll
-      for (int t = 0; t < T; ++t) {
-        f32x4 x = {0.f, 0.f, 0.f, 0.f};
+      for (int y = 0; y < 2; ++y) src.k(b + y, k[y]);
 #pragma unroll
-        for (int c = 0; c < kChunks; ++c) x = dev::mfma_bf16(k[c], q[t][c], x);
+      for (int c = 0; c < kChunks; ++c)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) s[t][4 * b + i] = x[i];
-      }
+        for (int y = 0; y < 2; ++y)
+#pragma unroll
+          for (int t = 0; t < T; ++t)
+            x[t][y] = dev::mfma_bf16(k[y][c], q[t][c], c ? x[t][y] : f32x4{0.f, 0.f, 0.f, 0.f});
+#pragma unroll
+      for (int t = 0; t < T; ++t)
+#pragma unroll
+        for (int y = 0; y < 2; ++y)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) s[t][4 * (b + y) + i] = x[t][y][i];
     }
     uint32_t seen[T];
     if constexpr (!kPlain) {
@@ -399,39 +419,23 @@ struct Wave {
 #pragma unroll
     for (int b = 0; b < kBlocks / 2; ++b) {
       if (b) __builtin_amdgcn_sched_barrier(0);              // one pair's V in registers at a time
-      uint32_t y[8][D / 32];
-      src.v(2 * b, y);
-      // What no row may see must not reach the product either (0 x NaN): V past the
-      // keys becomes 0, and infinities and NaN are taken out and added below for the
-      // rows that do see them.
-      if constexpr (!kPlain) {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          const bool ok = k0 + 32 * b + 16 * (e >> 2) + 4 * g + (e & 3) < w.hi && page[2 * b + (e >> 2)] >= 0;
+      for (int x = 0; x < kV; ++x) {
+        u32x4v a = src.v(2 * b, x);
+        // What no row may see must not reach the product either (0 x NaN): V past the
+        // keys becomes 0, and infinities and NaN are taken out and added below for the
+        // rows that do see them.
+        if constexpr (!kPlain) {
 #pragma unroll
-          for (int x = 0; x < D / 32; ++x) {
-            if (!ok) y[e][x] = 0;
-            if (!word_finite(y[e][x])) {
-              y[e][x] = 0;
-              odd_v = true;
-            }
+          for (int e = 0; e < 8; ++e) {
+            const bool ok = k0 + 32 * b + 16 * (e >> 2) + 4 * g + (e & 3) < w.hi && page[2 * b + (e >> 2)] >= 0;
+            const bool odd = ok && !finite_bf16(a[e >> 1] >> (16 * (e & 1)));
+            if (!ok || odd) a[e >> 1] &= e & 1 ? 0xFFFFu : 0xFFFF0000u;
+            odd_v |= odd;
           }
         }
-      }
-      // V^T: register pairs of neighbouring keys -> the low and the high halves' columns.
 #pragma unroll
-      for (int x = 0; x < D / 32; ++x) {
-        u32x4v even, odd;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          even[e] = __builtin_amdgcn_perm(y[2 * e + 1][x], y[2 * e][x], 0x05040100u);
-          odd[e] = __builtin_amdgcn_perm(y[2 * e + 1][x], y[2 * e][x], 0x07060302u);
-        }
-#pragma unroll
-        for (int t = 0; t < T; ++t) {
-          o[t][2 * x] = dev::mfma_bf16(even, pw[t][b], o[t][2 * x]);
-          o[t][2 * x + 1] = dev::mfma_bf16(odd, pw[t][b], o[t][2 * x + 1]);
-        }
+        for (int t = 0; t < T; ++t) o[t][x] = dev::mfma_bf16(a, pw[t][b], o[t][x]);
       }
     }
     if (!kPlain && __any(odd_v)) {            // rare: the words taken out above, row by row
@@ -453,9 +457,8 @@ struct Wave {
             for (int v = 0; v < kV; ++v)
 #pragma unroll
               for (int i = 0; i < 4; ++i) {
-                const int d = kV * (4 * g + i) + v;
-                const uint32_t word = vp[d & ~1] | static_cast<uint32_t>(vp[d | 1]) << 16;
-                if (sees && !word_finite(word)) o[t][v][i] += pk * dev::bf16_float(vp[d]);
+                const uint16_t x = vp[Source::dim(v, 4 * g + i)];
+                if (sees && !finite_bf16(x)) o[t][v][i] += pk * dev::bf16_float(x);
               }
           }
         }
@@ -695,39 +698,43 @@ __device__ __forceinline__ void lds_copy16(const uint16_t* src, uint32_t lds) {
                : "memory", "m0");
 }
 
-// K and V of a stage in LDS, and a lane's places in it (elements): rows r of a 16-key block
-// of K, 4 g + i of V.
+// K and V of a stage in LDS.  Unit u (16 bytes) of row k lies at unit u ^ turn(k), so that
+// neither a K read (a unit of 16 rows) nor a V read (32 bytes of 8 rows at a time) conflicts.
 template <int D>
 struct Staged {
-  const uint16_t *ks, *vs;
-  const int (&k_at)[D / 32];
-  const int (&v_at)[4];
+  static __device__ __forceinline__ int turn_k(int k) { return D == 64 ? (k >> 1) & 7 : k & 15; }
+  static __device__ __forceinline__ int turn_v(int k) { return D == 64 ? k & 6 : 2 * (k & 7); }
+
+  const uint16_t* ks;
+  uint32_t vs;                           // LDS address
+  const int (&k_at)[D / 32];             // a lane's places (elements): row r of a 16-key block
+  uint32_t v_at;                         // (bytes): dims 4 (r % 4) .. of row 4 g + r / 4
 
   __device__ __forceinline__ void k(int b, u32x4v (&out)[D / 32]) const {
 #pragma unroll
     for (int c = 0; c < D / 32; ++c) out[c] = *reinterpret_cast<const u32x4v*>(ks + k_at[c] + 16 * b * D);
   }
-  __device__ __forceinline__ void v(int b, uint32_t (&out)[8][D / 32]) const {
+  // Transposed as they are read: of 16 lanes, four to a row's 16 dims, lane i gets dim i of
+  // the four rows.
+  __device__ __forceinline__ u32x4v v(int b, int x) const {
+    typedef short s16x4 __attribute__((ext_vector_type(4)));
+    u32x4v out;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      const uint16_t* const at = vs + 16 * (b + (e >> 2)) * D;
-      if constexpr (D <= 128) {
-        load_v<D>(at + v_at[e & 3], out[e]);
-      } else {                           // the row's second unit lies at the first one's neighbour
-#pragma unroll
-        for (int c = 0; c < 2; ++c) {
-          const u32x4v x = *reinterpret_cast<const u32x4v*>(at + (v_at[e & 3] ^ (8 * c)));
-#pragma unroll
-          for (int i = 0; i < 4; ++i) out[e][4 * c + i] = x[i];
-        }
-      }
+    for (int h = 0; h < 2; ++h) {
+      const uint32_t at = (vs + (v_at ^ 32 * x)) + 32 * (b + h) * D;
+      const dev::u32x2 y = __builtin_bit_cast(
+          dev::u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                              (__attribute__((address_space(3))) s16x4*)(static_cast<uintptr_t>(at))));
+      out[2 * h] = y.x;
+      out[2 * h + 1] = y.y;
     }
+    return out;
   }
+  static __device__ __forceinline__ int dim(int x, int m) { return 16 * x + m; }
 };
 
-// More columns: each wave its own T tiles of them, all waves the same keys, K and V staged
-// in LDS (two stages of kKeys keys; a row's 16-byte units permuted by its number, so
-// that neither the K reads, a column of rows, nor the V reads, a whole row, conflict).
+// More columns: each wave its own T tiles of them, all waves the same keys, K and V copied
+// to LDS in two stages of kKeys keys.
 template <int D, int T>
 __global__ __launch_bounds__(kThreads, D <= 128 ? 2 : 1) void tree_attention_wide_kernel(const TreeArgs p) {
   constexpr int kV = D / 16, kKeys = D <= 128 ? 64 : 32;
@@ -743,9 +750,6 @@ __global__ __launch_bounds__(kThreads, D <= 128 ? 2 : 1) void tree_attention_wid
   const int wave = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x) >> 6);
   const uint32_t sh_at = static_cast<uint32_t>(
       reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) void*)(sh)));
-  // Unit u of row k lies at unit u ^ turn(k).
-  auto turn = [](int k) { return D == 64 ? (k >> 1) & 7 : k & 15; };
-
   int entries = page_entry(p, w, w.lo + 16 * lane);          // lane b: page of block b (of 64)
   Wave<D, T> q;
   q.start(p, w, w.c0 + 16 * T * wave);
@@ -759,10 +763,9 @@ __global__ __launch_bounds__(kThreads, D <= 128 ? 2 : 1) void tree_attention_wid
       const int c = wave + kWaves * x;                       // rows kRows c .. of the stage
       const int k = kRows * c + lane / kUnits;
       const int page = __builtin_amdgcn_readlane(entries, (stage * (kKeys / 16) + kRows * c / 16) & 63);
-      const int64_t at = block_base<D>(p, w.h, page, w.lo + kKeys * stage + (kRows * c / 16) * 16) + (k & 15) * D +
-                         8 * (lane % kUnits ^ turn(k));
-      lds_copy16(p.K + at, to + c * 1024);
-      lds_copy16(p.V + at, to + kKeys * D * 2 + c * 1024);
+      const int64_t at = block_base<D>(p, w.h, page, w.lo + kKeys * stage + (kRows * c / 16) * 16) + (k & 15) * D;
+      lds_copy16(p.K + at + 8 * (lane % kUnits ^ Staged<D>::turn_k(k)), to + c * 1024);
+      lds_copy16(p.V + at + 8 * (lane % kUnits ^ Staged<D>::turn_v(k)), to + kKeys * D * 2 + c * 1024);
     }
   };
   const int stages = (w.hi - w.lo + kKeys - 1) / kKeys;
@@ -774,15 +777,12 @@ __global__ __launch_bounds__(kThreads, D <= 128 ? 2 : 1) void tree_attention_wid
   };
   check(0);
   if (stages > 0) load(0);
-  // the blocks are 16 rows apart, and turn(k) has k's low bits alone
-  int k_at[D / 32], v_at[4];
+  // the blocks are 16 rows apart, and the turns have a row's low bits alone
+  int k_at[D / 32];
 #pragma unroll
-  for (int c = 0; c < D / 32; ++c) k_at[c] = r * D + 8 * ((4 * c + g) ^ turn(r));
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const int k = 4 * g + i;
-    v_at[i] = k * D + (D == 64 ? 8 * ((r >> 1) ^ turn(k)) + 4 * (r & 1) : 8 * ((D / 128 * r) ^ turn(k)));
-  }
+  for (int c = 0; c < D / 32; ++c) k_at[c] = r * D + 8 * ((4 * c + g) ^ Staged<D>::turn_k(r));
+  const int vr = 4 * g + (r >> 2);
+  const uint32_t v_at = vr * D * 2 + 16 * Staged<D>::turn_v(vr) + 8 * (r & 3);
   auto one = [&](int stage, auto all) {
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");         // this wave's copies of the stage
     __syncthreads();
@@ -796,8 +796,7 @@ __global__ __launch_bounds__(kThreads, D <= 128 ? 2 : 1) void tree_attention_wid
     }
     if (works) {
       constexpr int kBlocks = kKeys / 16;
-      const uint16_t* const ks = sh + (stage & 1) * kStage;
-      const Staged<D> src{ks, ks + kKeys * D, k_at, v_at};
+      const Staged<D> src{sh + (stage & 1) * kStage, sh_at + ((stage & 1) * kStage + kKeys * D) * 2, k_at, v_at};
       int page[kBlocks];
 #pragma unroll
       for (int b = 0; b < kBlocks; ++b)
@@ -821,22 +820,16 @@ __global__ __launch_bounds__(kThreads, D <= 128 ? 2 : 1) void tree_attention_wid
     if (w.splits == 1) {
       const float inv = sum == 0.f ? 0.f : 1.0f / sum;
 #pragma unroll
-      for (int i = 0; i < 4; ++i)
-#pragma unroll
-        for (int v = 0; v < kV; v += 4) {
-          const dev::u32x2 y = {dev::pack_bf16(q.o[t][v][i] * inv, q.o[t][v + 1][i] * inv),
-                                dev::pack_bf16(q.o[t][v + 2][i] * inv, q.o[t][v + 3][i] * inv)};
-          *reinterpret_cast<dev::u32x2*>(p.out + head * D + kV * (4 * g + i) + v) = y;
-        }
+      for (int x = 0; x < kV; ++x) {
+        const dev::u32x2 y = {dev::pack_bf16(q.o[t][x][0] * inv, q.o[t][x][1] * inv),
+                              dev::pack_bf16(q.o[t][x][2] * inv, q.o[t][x][3] * inv)};
+        *reinterpret_cast<dev::u32x2*>(p.out + head * D + 16 * x + 4 * g) = y;
+      }
       if (p.lse && g == 0) p.lse[head] = sum == 0.f ? kNone : (top + log2f(sum)) * 0.69314718055994531f;
     } else {
       const int64_t part = static_cast<int64_t>(blockIdx.x) * (16 * T * kWaves) + c;
 #pragma unroll
-      for (int i = 0; i < 4; ++i)
-#pragma unroll
-        for (int v = 0; v < kV; v += 4)
-          *reinterpret_cast<f32x4*>(p.part_o + part * D + kV * (4 * g + i) + v) =
-              f32x4{q.o[t][v][i], q.o[t][v + 1][i], q.o[t][v + 2][i], q.o[t][v + 3][i]};
+      for (int x = 0; x < kV; ++x) *reinterpret_cast<f32x4*>(p.part_o + part * D + 16 * x + 4 * g) = q.o[t][x];
       if (g == 0) p.part_ml[part] = {top, sum};
     }
   }
