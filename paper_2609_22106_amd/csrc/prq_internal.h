@@ -214,7 +214,7 @@ hipError_t launch_qk_norm_rope(const void* q, int64_t ld_q, const void* k, int64
                                int rot, bool interleaved, uint16_t* q_out, const PagedCache& cache,
                                const int64_t* slots, int num_cus, hipStream_t stream);
 
-// tree_attention.hip.  Query columns a workgroup (16, 64 or 128); slots a kv head, each a
+// tree_attention.hip.  Query columns a workgroup (16, 64, 128 or 256); slots a kv head, each a
 // tile of one request's columns and a part of its keys; whether keys are split, and if so
 // whether the tiles fill the chip as it is; the blocks of the launch.
 struct TreePlan {

@@ -17,15 +17,18 @@
 // bounds it.  The waves of a workgroup take 32 keys each at a time, straight into registers,
 // the next ones under way, and join through LDS.  V's operand needs 8 keys of one column: a
 // lane group loads whole rows of its 8 keys, 16 lanes a row, and pairs up halves of registers
-// (32 v_perm per 32 x 128 tile).  32 sequences of 1 .. 8192 tokens, 8 kv heads of 128:
-// 46 us, 206 MB of K and V at 4.5 TB/s; one token over 4097: 13.9 us, the latency of the
+// (32 v_perm per 32 x 128 tile).  32 sequences of up to 2176 tokens, 8 kv heads of 128:
+// 46 us, 206 MB of K and V at 4.5 TB/s; one token over 4097: 14 us, the latency of the
 // loads, the arrival and the join one after another.
 //
-// More columns (wide): they are dealt to the waves, one or two tiles of 16 each, and 64 keys
+// More columns (wide): they are dealt to the waves, one or two tiles of 16 each, and 32 keys
 // at a time go through LDS once for all of them, copied there without a register; V is read
-// back transposed.  64-node trees over 8 x 32 k tokens: straight from memory 714 us, through
-// LDS with v_perm 272, transposed reads 255 .. 262: 610 TFLOP/s, matrix units a third of the
-// time, the exponentials and the rest of the vector work more than that.
+// back transposed.  Trees of up to 64 nodes over 8 x 32 k tokens (377 rows, 204 k keys): straight
+// from memory 714 us, through LDS with v_perm 272, transposed reads 258; a stage's scores
+// beside the exponentials of the one before and LDS read ahead, 8 waves for more than 128
+// columns, those dealt evenly to the SIMDs, a barrier every two stages, 234: 670 TFLOP/s, the
+// matrix units 40% of the time.  What is left: the parts, unequal by 17%, and a SIMD's two
+// waves, in step more often than in turn.
 //
 // The maximum is kept per lane group and only joined across the groups when a score
 // passes it by 8 (powers of two): until then the stale maximum serves, P up to 2^8.
@@ -53,7 +56,6 @@ namespace {
 using dev::f32x4;
 using dev::u32x4v;
 
-constexpr int kWaves = 4, kThreads = 64 * kWaves;                // of the wide kernel
 template <int D>
 constexpr int kNarrowWaves = D <= 128 ? 8 : 4;                       // of the narrow one (by its registers)
 constexpr int kMaxSplits = 64;
@@ -111,7 +113,7 @@ struct Tile {
   }
   // V^T's operand of the product's dims dim(x, 0 .. 15): register pairs of neighbouring keys
   // -> the low or the high halves.
-  __device__ __forceinline__ u32x4v v(int, int x) const {
+  __device__ __forceinline__ u32x4v v(int x) const {
     u32x4v out;
 #pragma unroll
     for (int e = 0; e < 4; ++e)
@@ -328,64 +330,74 @@ struct Wave {
     }
   }
 
-  // The 16 kBlocks keys from k0 on; block b of them on page page[b] of the pool (-1: none).
+  // A step: 32 keys from k0 on, blocks 0 and 1 of them on pages page[] of the pool (-1: none).
   // kPlain: every row sees all of them.
-  // `src`: where the operands are, k(b, ..) block b's keys, v(b, x) V^T's for the keys of
-  // blocks b and b + 1 and the dims dim(x, 0 .. 15).
-  template <bool kPlain, int kBlocks, typename Source>
-  __device__ __forceinline__ void step(const TreeArgs& p, const Part& w, const Source& src, int k0,
-                                       const int (&page)[kBlocks]) {
-    constexpr int kOwn = 4 * kBlocks;    // keys of a lane: e is 16 (e / 4) + 4 g + e % 4
-    const int lane = static_cast<int>(threadIdx.x) & 63, r = lane & 15, g = lane >> 4;
-    float s[T][kOwn];
-    // two blocks at a time: a product does not wait for the one before it
+  // `src`: where the operands are, k(b, ..) block b's keys, v(x) V^T's for both blocks and the
+  // dims dim(x, 0 .. 15).  A lane's keys: e is 16 (e / 4) + 4 g + e % 4.
+  struct Scores {
+    float s[T][8];
+    uint32_t seen[T];                    // (not plain) bit e
+  };
+
+  template <bool kPlain>
+  __device__ __forceinline__ void scores(const TreeArgs& p, const Part& w, const u32x4v (&k)[2][kChunks], int k0,
+                                         const int (&page)[2], Scores* out) const {
+    const int lane = static_cast<int>(threadIdx.x) & 63, g = lane >> 4;
+    f32x4 x[T][2];
+    // blocks and tiles in turn: a product does not wait for the one before it
 #pragma unroll
-    for (int b = 0; b < kBlocks; b += 2) {
-      u32x4v k[2][kChunks];
-      f32x4 x[T][2];
+    for (int c = 0; c < kChunks; ++c)
 #pragma unroll
-      for (int y = 0; y < 2; ++y) src.k(b + y, k[y]);
+      for (int y = 0; y < 2; ++y)
 #pragma unroll
-      for (int c = 0; c < kChunks; ++c)
+        for (int t = 0; t < T; ++t)
+          x[t][y] = dev::mfma_bf16(k[y][c], q[t][c], c ? x[t][y] : f32x4{0.f, 0.f, 0.f, 0.f});
 #pragma unroll
-        for (int y = 0; y < 2; ++y)
+    for (int t = 0; t < T; ++t)
 #pragma unroll
-          for (int t = 0; t < T; ++t)
-            x[t][y] = dev::mfma_bf16(k[y][c], q[t][c], c ? x[t][y] : f32x4{0.f, 0.f, 0.f, 0.f});
-#pragma unroll
-      for (int t = 0; t < T; ++t)
-#pragma unroll
-        for (int y = 0; y < 2; ++y)
-#pragma unroll
-          for (int i = 0; i < 4; ++i) s[t][4 * (b + y) + i] = x[t][y][i];
-    }
-    uint32_t seen[T];
+      for (int e = 0; e < 8; ++e) out->s[t][e] = x[t][e >> 2][e & 3];
     if constexpr (!kPlain) {
 #pragma unroll
       for (int t = 0; t < T; ++t) {
-        const uint8_t* see = p.mask ? p.mask + (w.first + token[t]) * p.ld_mask : nullptr;
-        seen[t] = 0;
+        // own token of the lane's first key, and which of the request's the row sees: the mask's
+        // bytes are all loaded, from its last column on past it, so that none waits for another
+        const int j0 = k0 + 4 * g - w.cached, have = w.hi - w.cached;
+        uint32_t seen = 0;
+        if (p.mask_wide > 0) {
+          const uint8_t* see = p.mask + (w.first + token[t]) * p.ld_mask;
+          uint8_t own[8];
 #pragma unroll
-        for (int e = 0; e < kOwn; ++e) {
-          const int j = k0 + 16 * (e >> 2) + 4 * g + (e & 3) - w.cached;
-          const int own = see && j >= 0 && j < p.mask_wide ? see[j] : 0;
-          const bool ok = j < w.hi - w.cached && page[e >> 2] >= 0 && (j < 0 || (see ? own != 0 : j <= token[t]));
-          seen[t] |= static_cast<uint32_t>(ok) << e;
+          for (int e = 0; e < 8; ++e) own[e] = see[min(max(j0 + 16 * (e >> 2) + (e & 3), 0), p.mask_wide - 1)];
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            const int j = j0 + 16 * (e >> 2) + (e & 3);
+            seen |= static_cast<uint32_t>(j < 0 || (j < p.mask_wide && own[e] != 0)) << e;
+          }
+        } else {
+          const int last = p.mask ? -1 : token[t];           // a mask without a column: no own tokens
+#pragma unroll
+          for (int e = 0; e < 8; ++e) seen |= static_cast<uint32_t>(j0 + 16 * (e >> 2) + (e & 3) <= last) << e;
         }
 #pragma unroll
-        for (int e = 0; e < kOwn; ++e)
-          if (!(seen[t] >> e & 1)) s[t][e] = kNone;
+        for (int e = 0; e < 8; ++e)
+          if (j0 + 16 * (e >> 2) + (e & 3) >= have || page[e >> 2] < 0) seen &= ~(1u << e);
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+          if (!(seen >> e & 1)) out->s[t][e] = kNone;
+        out->seen[t] = seen;
       }
     }
+  }
 
-    // A lane whose scores pass the running maximum by more than the slack renews it.
+  // A lane whose scores pass the running maximum by more than the slack renews it.
+  __device__ __forceinline__ void renew(const TreeArgs& p, const Scores& in) {
     bool past = false;
     float top[T];
 #pragma unroll
     for (int t = 0; t < T; ++t) {
-      top[t] = max_of(s[t][0], s[t][1]);
+      top[t] = max_of(in.s[t][0], in.s[t][1]);
 #pragma unroll
-      for (int e = 2; e < kOwn; e += 2) top[t] = max_of(top[t], s[t][e], s[t][e + 1]);
+      for (int e = 2; e < 8; e += 2) top[t] = max_of(top[t], in.s[t][e], in.s[t][e + 1]);
       past |= top[t] > m[t] + p.slack;
     }
     if (__any(past)) {
@@ -401,46 +413,48 @@ struct Wave {
         for (int v = 0; v < kV; ++v) o[t][v] *= a;
       }
     }
-    u32x4v pw[T][kBlocks / 2];
+  }
+
+  // Probabilities (left in `in`, too) and their sum.
+  __device__ __forceinline__ void weights(const TreeArgs& p, Scores* in, u32x4v (&pw)[T]) {
 #pragma unroll
     for (int t = 0; t < T; ++t) {
       const float from = m[t] == kNone ? 0.f : m[t] * p.scale;
+      float* x = in->s[t];
 #pragma unroll
-      for (int b = 0; b < kBlocks; b += 2) {
-        float* x = s[t] + 4 * b;
+      for (int e = 0; e < 8; ++e) x[e] = exp2_fast(__builtin_fmaf(x[e], p.scale, -from));
+      l[t] += ((x[0] + x[1]) + (x[2] + x[3])) + ((x[4] + x[5]) + (x[6] + x[7]));
 #pragma unroll
-        for (int e = 0; e < 8; ++e) x[e] = exp2_fast(__builtin_fmaf(x[e], p.scale, -from));
-        l[t] += ((x[0] + x[1]) + (x[2] + x[3])) + ((x[4] + x[5]) + (x[6] + x[7]));
-#pragma unroll
-        for (int e = 0; e < 4; ++e) pw[t][b / 2][e] = dev::pack_bf16(x[2 * e], x[2 * e + 1]);
-      }
+      for (int e = 0; e < 4; ++e) pw[t][e] = dev::pack_bf16(x[2 * e], x[2 * e + 1]);
     }
+  }
+
+  template <bool kPlain, typename Source>
+  __device__ __forceinline__ void absorb(const TreeArgs& p, const Part& w, const Source& src, int k0,
+                                         const int (&page)[2], const Scores* in, const u32x4v (&pw)[T]) {
+    const int lane = static_cast<int>(threadIdx.x) & 63, r = lane & 15, g = lane >> 4;
     bool odd_v = false;                  // some key's V holds an infinity or a NaN
 #pragma unroll
-    for (int b = 0; b < kBlocks / 2; ++b) {
-      if (b) __builtin_amdgcn_sched_barrier(0);              // one pair's V in registers at a time
+    for (int x = 0; x < kV; ++x) {
+      u32x4v a = src.v(x);
+      // What no row may see must not reach the product either (0 x NaN): V past the
+      // keys becomes 0, and infinities and NaN are taken out and added below for the
+      // rows that do see them.
+      if constexpr (!kPlain) {
 #pragma unroll
-      for (int x = 0; x < kV; ++x) {
-        u32x4v a = src.v(2 * b, x);
-        // What no row may see must not reach the product either (0 x NaN): V past the
-        // keys becomes 0, and infinities and NaN are taken out and added below for the
-        // rows that do see them.
-        if constexpr (!kPlain) {
-#pragma unroll
-          for (int e = 0; e < 8; ++e) {
-            const bool ok = k0 + 32 * b + 16 * (e >> 2) + 4 * g + (e & 3) < w.hi && page[2 * b + (e >> 2)] >= 0;
-            const bool odd = ok && !finite_bf16(a[e >> 1] >> (16 * (e & 1)));
-            if (!ok || odd) a[e >> 1] &= e & 1 ? 0xFFFFu : 0xFFFF0000u;
-            odd_v |= odd;
-          }
+        for (int e = 0; e < 8; ++e) {
+          const bool ok = k0 + 16 * (e >> 2) + 4 * g + (e & 3) < w.hi && page[e >> 2] >= 0;
+          const bool odd = ok && !finite_bf16(a[e >> 1] >> (16 * (e & 1)));
+          if (!ok || odd) a[e >> 1] &= e & 1 ? 0xFFFFu : 0xFFFF0000u;
+          odd_v |= odd;
         }
-#pragma unroll
-        for (int t = 0; t < T; ++t) o[t][x] = dev::mfma_bf16(a, pw[t][b], o[t][x]);
       }
+#pragma unroll
+      for (int t = 0; t < T; ++t) o[t][x] = dev::mfma_bf16(a, pw[t], o[t][x]);
     }
     if (!kPlain && __any(odd_v)) {            // rare: the words taken out above, row by row
 #pragma unroll
-      for (int b = 0; b < kBlocks; ++b) {
+      for (int b = 0; b < 2; ++b) {
         const int64_t base = block_base<D>(p, w.h, page[b], k0 + 16 * b);
         for (int kk = 0; kk < 16; ++kk) {
           if (k0 + 16 * b + kk >= w.hi || page[b] < 0) break;
@@ -450,9 +464,9 @@ struct Wave {
           for (int t = 0; t < T; ++t) {
             float mine = 0.f;
 #pragma unroll
-            for (int x = 0; x < 4; ++x) mine = x == (kk & 3) ? s[t][4 * b + x] : mine;
+            for (int x = 0; x < 4; ++x) mine = x == (kk & 3) ? in->s[t][4 * b + x] : mine;
             const float pk = __shfl(mine, from);
-            const bool sees = (__shfl(static_cast<int>(seen[t]), from) >> (4 * b + (kk & 3))) & 1;
+            const bool sees = (__shfl(static_cast<int>(in->seen[t]), from) >> (4 * b + (kk & 3))) & 1;
 #pragma unroll
             for (int v = 0; v < kV; ++v)
 #pragma unroll
@@ -464,6 +478,19 @@ struct Wave {
         }
       }
     }
+  }
+
+  template <bool kPlain, typename Source>
+  __device__ __forceinline__ void step(const TreeArgs& p, const Part& w, const Source& src, int k0,
+                                       const int (&page)[2]) {
+    Scores s;
+    u32x4v k[2][kChunks], pw[T];
+#pragma unroll
+    for (int b = 0; b < 2; ++b) src.k(b, k[b]);
+    scores<kPlain>(p, w, k, k0, page, &s);
+    renew(p, s);
+    weights(p, &s, pw);
+    absorb<kPlain>(p, w, src, k0, page, &s, pw);
   }
 };
 
@@ -628,7 +655,7 @@ __global__ __launch_bounds__(64 * kNarrowWaves<D>, D <= 128 ? 2 : 1) void tree_a
         entries = page_entry(p, w, first + kStride * (step + 1 + (lane >> 1)) + 16 * (lane & 1));
       load(step + 1, &next);
     }
-    q.template step<decltype(plain)::value, 2>(p, w, now, first + kStride * step, page_now);
+    q.template step<decltype(plain)::value>(p, w, now, first + kStride * step, page_now);
     if (step + 1 < steps) now = next;
   };
   // every row sees the whole step: of cached tokens alone, on pages of the pool
@@ -689,14 +716,18 @@ __global__ __launch_bounds__(64 * kNarrowWaves<D>, D <= 128 ? 2 : 1) void tree_a
   if (w.splits > 1) join_parts<D>(p, w, &sh_o[0][0][0]);
 }
 
-// Copies 16 bytes a lane straight to LDS, lane l's at lds + 16 l (LDS address, the same for
-// the wave).
-__device__ __forceinline__ void lds_copy16(const uint16_t* src, uint32_t lds) {
-  asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off"
+// Copies 16 bytes a lane straight to LDS: from src (the same for the wave) + the lane's
+// offset, lane l's to lds + 16 l (LDS address, the same for the wave).
+__device__ __forceinline__ void lds_copy16(const void* src, uint32_t bytes, uint32_t lds) {
+  asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1"
                :
-               : "v"(src), "s"(lds)
+               : "v"(bytes), "s"(src), "s"(lds)
                : "memory", "m0");
 }
+
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+template <typename T>
+using InLds = const __attribute__((address_space(3))) T*;
 
 // K and V of a stage in LDS.  Unit u (16 bytes) of row k lies at unit u ^ turn(k), so that
 // neither a K read (a unit of 16 rows) nor a V read (32 bytes of 8 rows at a time) conflicts.
@@ -704,27 +735,30 @@ template <int D>
 struct Staged {
   static __device__ __forceinline__ int turn_k(int k) { return D == 64 ? (k >> 1) & 7 : k & 15; }
   static __device__ __forceinline__ int turn_v(int k) { return D == 64 ? k & 6 : 2 * (k & 7); }
+  // A lane's own places in a stage (bytes): unit g of row r; dims 4 (r % 4) .. of row 4 g + r / 4.
+  static __device__ __forceinline__ uint32_t k_lane(int r, int g) { return 2 * r * D + 16 * (g ^ turn_k(r)); }
+  static __device__ __forceinline__ uint32_t v_lane(int r, int g) {
+    const int k = 4 * g + (r >> 2);
+    return 2 * k * D + 16 * turn_v(k) + 8 * (r & 3);
+  }
 
-  const uint16_t* ks;
-  uint32_t vs;                           // LDS address
-  const int (&k_at)[D / 32];             // a lane's places (elements): row r of a 16-key block
-  uint32_t v_at;                         // (bytes): dims 4 (r % 4) .. of row 4 g + r / 4
+  uint32_t k_at, v_at;                   // LDS addresses: those in the stage
 
+  // (the blocks are 16 rows apart, and the turns have a row's low bits alone)
   __device__ __forceinline__ void k(int b, u32x4v (&out)[D / 32]) const {
 #pragma unroll
-    for (int c = 0; c < D / 32; ++c) out[c] = *reinterpret_cast<const u32x4v*>(ks + k_at[c] + 16 * b * D);
+    for (int c = 0; c < D / 32; ++c)
+      out[c] = *reinterpret_cast<InLds<u32x4v>>(static_cast<uintptr_t>((k_at ^ 64 * c) + 32 * b * D));
   }
   // Transposed as they are read: of 16 lanes, four to a row's 16 dims, lane i gets dim i of
   // the four rows.
-  __device__ __forceinline__ u32x4v v(int b, int x) const {
-    typedef short s16x4 __attribute__((ext_vector_type(4)));
+  __device__ __forceinline__ u32x4v v(int x) const {
     u32x4v out;
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
-      const uint32_t at = (vs + (v_at ^ 32 * x)) + 32 * (b + h) * D;
+      const auto at = static_cast<uintptr_t>((v_at ^ 32 * x) + 32 * h * D);
       const dev::u32x2 y = __builtin_bit_cast(
-          dev::u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-                              (__attribute__((address_space(3))) s16x4*)(static_cast<uintptr_t>(at))));
+          dev::u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)(at)));
       out[2 * h] = y.x;
       out[2 * h + 1] = y.y;
     }
@@ -733,113 +767,223 @@ struct Staged {
   static __device__ __forceinline__ int dim(int x, int m) { return 16 * x + m; }
 };
 
-// More columns: each wave its own T tiles of them, all waves the same keys, K and V copied
-// to LDS in two stages of kKeys keys.
-template <int D, int T>
-__global__ __launch_bounds__(kThreads, D <= 128 ? 2 : 1) void tree_attention_wide_kernel(const TreeArgs p) {
-  constexpr int kV = D / 16, kKeys = D <= 128 ? 64 : 32;
-  constexpr int kUnits = D / 8, kRows = 64 / kUnits, kCopies = kKeys / kRows / kWaves;
-  constexpr int kStage = 2 * kKeys * D;                      // K, then V
-  __shared__ __align__(16) uint16_t sh[2 * kStage];
+// V^T's operands of a stage, read from LDS.
+template <int D>
+struct Taken {
+  u32x4v values[D / 16];
+  __device__ __forceinline__ void take(const Staged<D>& src, int from, int to) {
+#pragma unroll
+    for (int x = 0; x < D / 16; ++x)
+      if (x >= from && x < to) values[x] = src.v(x);
+  }
+  __device__ __forceinline__ u32x4v v(int x) const { return values[x]; }
+  static __device__ __forceinline__ int dim(int x, int m) { return Staged<D>::dim(x, m); }
+};
+
+// More columns: each of kN waves its own 1 .. T tiles of them, all waves the same keys, K and
+// V copied to LDS 32 keys (a stage) at a time, kAhead stages ahead.  Within a wave a stage's
+// scores are formed beside the exponentials of the one before it, and its keys are read from
+// LDS beside the second product of the one before that, so that neither unit waits for the
+// other or for LDS.  A wave in the first of these phases goes first: the second one, products
+// alone, leaves room for it (236 -> 228 us).
+template <int D, int T, int kN>
+__global__ __launch_bounds__(64 * kN, D <= 128 ? 2 : 1) void tree_attention_wide_kernel(const TreeArgs p) {
+  constexpr int kV = D / 16, kKeys = 32, kThreads = 64 * kN;
+  constexpr int kAhead = kN == 8 ? 6 : 2;                    // even
+  // Stages in LDS: under way, and the two whose keys are read; for V also the two behind them.
+  constexpr int kKeyBuffers = kAhead + 2, kValueBuffers = kAhead + 4;
+  constexpr int kUnits = D / 8, kRows = 64 / kUnits;         // 16 bytes of a row; rows a copy
+  constexpr int kEach = kKeys / kRows, kCopies = 2 * kEach / kN;         // copies of K; a wave's
+  constexpr int kStage = kKeys * D;                          // of K or of V
+  __shared__ __align__(1024) uint16_t sh[(kKeyBuffers + kValueBuffers) * kStage];
   Part w;
-  if (!find_part(p, 16 * T * kWaves, &w)) return;
+  if (!find_part(p, 16 * T * kN, &w)) return;
   if (p.split && w.h == 0 && static_cast<int>(blockIdx.x) / p.Hk == w.first_slot)      // for the join
     for (int row = w.c0 / p.G + static_cast<int>(threadIdx.x); row * p.G < w.c0 + w.cols; row += kThreads)
-      p.joins[w.first + row] = {w.first, w.first_slot - w.c0 / (16 * T * kWaves), w.tiles, w.splits};
+      p.joins[w.first + row] = {w.first, w.first_slot - w.c0 / (16 * T * kN), w.tiles, w.splits};
   const int lane = static_cast<int>(threadIdx.x) & 63, r = lane & 15, g = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x) >> 6);
   const uint32_t sh_at = static_cast<uint32_t>(
       reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) void*)(sh)));
-  int entries = page_entry(p, w, w.lo + 16 * lane);          // lane b: page of block b (of 64)
-  Wave<D, T> q;
-  q.start(p, w, w.c0 + 16 * T * wave);
-  const bool works = 16 * T * wave < w.cols;                 // else the wave only helps to load
-
-  // A stage's rows are copied kRows to a wave copy (a kilobyte), lane i to unit i of it.
-  auto load = [&](int stage) {
-    const uint32_t to = sh_at + (stage & 1) * kStage * 2;
-#pragma unroll
-    for (int x = 0; x < kCopies; ++x) {
-      const int c = wave + kWaves * x;                       // rows kRows c .. of the stage
-      const int k = kRows * c + lane / kUnits;
-      const int page = __builtin_amdgcn_readlane(entries, (stage * (kKeys / 16) + kRows * c / 16) & 63);
-      const int64_t at = block_base<D>(p, w.h, page, w.lo + kKeys * stage + (kRows * c / 16) * 16) + (k & 15) * D;
-      lds_copy16(p.K + at + 8 * (lane % kUnits ^ Staged<D>::turn_k(k)), to + c * 1024);
-      lds_copy16(p.V + at + 8 * (lane % kUnits ^ Staged<D>::turn_v(k)), to + kKeys * D * 2 + c * 1024);
-    }
-  };
+  // The columns in tiles of 16, as many to each SIMD (a wave or two of the workgroup): a
+  // SIMD's second wave has one the less, or as many.
+  const int tiles = (w.cols + 15) / 16, simd = wave % 4;
+  const int simd_tiles = tiles / 4 + (simd < tiles % 4), second = kN == 8 ? simd_tiles / 2 : 0;
+  const int mine = wave < 4 ? simd_tiles - second : second;
+  const int tile0 = simd * (tiles / 4) + min(simd, tiles % 4) + (wave < 4 ? 0 : simd_tiles - second);
   const int stages = (w.hi - w.lo + kKeys - 1) / kKeys;
   // Stages that every row sees whole: of cached tokens alone, on pages of the pool (as far
   // as the entries at hand say).
   int plain = max(min(w.cached, w.hi) - w.lo, 0) / kKeys;
-  auto check = [&](int stage) {
-    if (__any(w.lo + kKeys * stage + 16 * lane < w.hi && entries < 0)) plain = min(plain, stage);
+  // A stage's place in LDS (bytes) follows the one before it, around a ring.
+  auto keys_after = [&](uint32_t at) { return at == (kKeyBuffers - 1) * 2 * kStage ? 0 : at + 2 * kStage; };
+  auto values_after = [&](uint32_t at) {
+    return at == (kKeyBuffers + kValueBuffers - 1) * 2 * kStage ? kKeyBuffers * 2 * kStage : at + 2 * kStage;
   };
-  check(0);
-  if (stages > 0) load(0);
-  // the blocks are 16 rows apart, and the turns have a row's low bits alone
-  int k_at[D / 32];
+
+  // A stage's rows are copied kRows to a wave copy (a kilobyte), lane i to unit i of it.
+  // (Stages past the last are copied from the pool's first page, so that as many are always
+  // under way.)
+  int64_t entry = 0;                     // lane b: byte offset of block b (of 64)
+  uint32_t load_k = 0, load_v = kKeyBuffers * 2 * kStage;    // of the next stage to load
+  auto look_up = [&](int stage) {        // before the load of a stage that starts 64 blocks
+    if (stage % 32) return;
+    const int key = w.lo + kKeys * stage + 16 * lane, page = page_entry(p, w, key);
+    entry = 2 * block_base<D>(p, w.h, page, key);
+    if (__any(key < w.hi && page < 0)) plain = min(plain, stage);
+  };
+  uint32_t of[kCopies];                  // a lane's place in its block
 #pragma unroll
-  for (int c = 0; c < D / 32; ++c) k_at[c] = r * D + 8 * ((4 * c + g) ^ Staged<D>::turn_k(r));
-  const int vr = 4 * g + (r >> 2);
-  const uint32_t v_at = vr * D * 2 + 16 * Staged<D>::turn_v(vr) + 8 * (r & 3);
-  auto one = [&](int stage, auto all) {
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");         // this wave's copies of the stage
-    __syncthreads();
-    const int entries_now = entries;
-    if (stage + 1 < stages) {
-      if (((stage + 1) * (kKeys / 16) & 63) == 0) {
-        entries = page_entry(p, w, w.lo + kKeys * (stage + 1) + 16 * lane);
-        check(stage + 1);
+  for (int x = 0; x < kCopies; ++x) {
+    const int c = wave + kN * x, k = kRows * (c % kEach) % 16 + lane / kUnits, unit = lane % kUnits;
+    of[x] = 2 * k * D + 16 * (unit ^ (c < kEach ? Staged<D>::turn_k(k) : Staged<D>::turn_v(k)));
+  }
+  auto load = [&](int stage) {
+#pragma unroll
+    for (int x = 0; x < kCopies; ++x) {
+      const int c = wave + kN * x, rows = c % kEach;         // rows kRows rows .. of the stage
+      const int b = (2 * stage + kRows * rows / 16) & 63;
+      const uint64_t at = static_cast<uint64_t>(static_cast<uint32_t>(
+                              __builtin_amdgcn_readlane(static_cast<int>(entry >> 32), b))) << 32 |
+                          static_cast<uint32_t>(__builtin_amdgcn_readlane(static_cast<int>(entry), b));
+      lds_copy16(reinterpret_cast<const char*>(c < kEach ? p.K : p.V) + at, of[x],
+                 sh_at + (c < kEach ? load_k : load_v) + rows * 1024);
+    }
+    load_k = keys_after(load_k);
+    load_v = values_after(load_v);
+  };
+  // A stage's copies are there (a wave's end in order, and the later stages' are under way):
+  // the next load takes buffers whose last readers are behind this barrier.
+  auto arrive = [&] {
+    asm volatile("s_waitcnt vmcnt(%0)" ::"n"((kAhead - 2) * kCopies) : "memory");
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+  };
+  auto enter = [&](int stage) {
+    look_up(stage + kAhead);
+    arrive();
+    load(stage + kAhead);
+  };
+  if (stages > 0) {
+    look_up(0);
+    for (int stage = 0; stage < kAhead; ++stage) load(stage);
+  }
+  uint32_t read_k = 0, read_v = kKeyBuffers * 2 * kStage;    // of the next stage to read
+  const uint32_t k_lane = sh_at + Staged<D>::k_lane(r, g), v_lane = sh_at + Staged<D>::v_lane(r, g);
+  auto work = [&](auto count) {
+    constexpr int kT = decltype(count)::value;
+    Wave<D, kT> q;
+    q.start(p, w, w.c0 + 16 * tile0);
+    using Scores = typename Wave<D, kT>::Scores;
+    constexpr int kNoPage[2] = {0, 0};
+    Scores now, after;
+    u32x4v k[2][D / 32], pw[kT];
+    auto read_keys = [&] {
+      const Staged<D> src{read_k + k_lane, 0};
+      src.k(0, k[0]);
+      src.k(1, k[1]);
+      read_k = keys_after(read_k);
+    };
+    if (plain > 0) {
+      enter(0);
+      read_keys();
+      q.template scores<true>(p, w, k, 0, kNoPage, &now);
+      q.renew(p, now);
+      enter(1);
+      read_keys();
+      for (int stage = 0; stage + 1 < plain; ++stage) {
+        if (!(stage & 1)) look_up(stage + 2 + kAhead);
+        Taken<D> values;
+        const Staged<D> src{0, read_v + v_lane};
+        read_v = values_after(read_v);
+        values.take(src, 0, kV / 2);
+        __builtin_amdgcn_sched_barrier(0);
+        __builtin_amdgcn_s_setprio(1);
+        q.template scores<true>(p, w, k, 0, kNoPage, &after);
+        q.weights(p, &now, pw);
+#pragma unroll
+        for (int t = 0; t < kT; ++t) asm volatile("" : "+v"(pw[t]));     // here, not after the barrier
+        __builtin_amdgcn_sched_barrier(0);
+        __builtin_amdgcn_s_setprio(0);
+        values.take(src, kV / 2, kV);
+        if (!(stage & 1)) {              // two stages, if only to wait: they may not be plain, or none
+          arrive();
+          load(stage + 2 + kAhead);
+          load(stage + 3 + kAhead);
+        }
+        read_keys();
+        __builtin_amdgcn_sched_barrier(0);
+        q.template absorb<true>(p, w, values, 0, kNoPage, &now, pw);
+        now = after;
+        q.renew(p, now);
       }
-      load(stage + 1);
+      q.weights(p, &now, pw);
+      q.template absorb<true>(p, w, Staged<D>{0, read_v + v_lane}, 0, kNoPage, &now, pw);
     }
-    if (works) {
-      constexpr int kBlocks = kKeys / 16;
-      const Staged<D> src{sh + (stage & 1) * kStage, sh_at + ((stage & 1) * kStage + kKeys * D) * 2, k_at, v_at};
-      int page[kBlocks];
-#pragma unroll
-      for (int b = 0; b < kBlocks; ++b)
-        page[b] = decltype(all)::value ? 0 : __builtin_amdgcn_readlane(entries_now, (stage * kBlocks + b) & 63);
-      q.template step<decltype(all)::value, kBlocks>(p, w, src, w.lo + kKeys * stage, page);
+    // plain > 0: stage `plain` has been entered, and one more if it is even
+    read_k = plain % kKeyBuffers * 2 * kStage;
+    read_v = (kKeyBuffers + plain % kValueBuffers) * 2 * kStage;
+    for (int stage = plain; stage < stages; ++stage) {
+      if (stage > plain + 1 - (plain & 1) || plain == 0) enter(stage);
+      const int k0 = w.lo + kKeys * stage;
+      const int page[2] = {page_entry(p, w, k0), page_entry(p, w, k0 + 16)};
+      q.template step<false>(p, w, Staged<D>{read_k + k_lane, read_v + v_lane}, k0, page);
+      read_k = keys_after(read_k);
+      read_v = values_after(read_v);
     }
-  };
-  int stage = 0;
-  for (; stage < plain; ++stage) one(stage, std::true_type{});
-  for (; stage < stages; ++stage) one(stage, std::false_type{});
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");           // no copy outlives the workgroup
 
 #pragma unroll
-  for (int t = 0; t < T; ++t) {
-    float sum = q.l[t];
-    sum += __shfl_xor(sum, 16);
-    sum += __shfl_xor(sum, 32);
-    const int c = 16 * (T * wave + t) + r;
-    if (c >= w.cols) continue;
-    const int64_t head = head_of(p, w, c);
-    const float top = q.m[t] * p.scale;
-    if (w.splits == 1) {
-      const float inv = sum == 0.f ? 0.f : 1.0f / sum;
+    for (int t = 0; t < kT; ++t) {
+      float sum = q.l[t];
+      sum += __shfl_xor(sum, 16);
+      sum += __shfl_xor(sum, 32);
+      const int c = 16 * (tile0 + t) + r;
+      if (c >= w.cols) continue;
+      const int64_t head = head_of(p, w, c);
+      const float top = q.m[t] * p.scale;
+      if (w.splits == 1) {
+        const float inv = sum == 0.f ? 0.f : 1.0f / sum;
 #pragma unroll
-      for (int x = 0; x < kV; ++x) {
-        const dev::u32x2 y = {dev::pack_bf16(q.o[t][x][0] * inv, q.o[t][x][1] * inv),
-                              dev::pack_bf16(q.o[t][x][2] * inv, q.o[t][x][3] * inv)};
-        *reinterpret_cast<dev::u32x2*>(p.out + head * D + 16 * x + 4 * g) = y;
+        for (int x = 0; x < kV; ++x) {
+          const dev::u32x2 y = {dev::pack_bf16(q.o[t][x][0] * inv, q.o[t][x][1] * inv),
+                                dev::pack_bf16(q.o[t][x][2] * inv, q.o[t][x][3] * inv)};
+          *reinterpret_cast<dev::u32x2*>(p.out + head * D + 16 * x + 4 * g) = y;
+        }
+        if (p.lse && g == 0) p.lse[head] = sum == 0.f ? kNone : (top + log2f(sum)) * 0.69314718055994531f;
+      } else {
+        const int64_t part = static_cast<int64_t>(blockIdx.x) * (16 * T * kN) + c;
+#pragma unroll
+        for (int x = 0; x < kV; ++x) *reinterpret_cast<f32x4*>(p.part_o + part * D + 16 * x + 4 * g) = q.o[t][x];
+        if (g == 0) p.part_ml[part] = {top, sum};
       }
-      if (p.lse && g == 0) p.lse[head] = sum == 0.f ? kNone : (top + log2f(sum)) * 0.69314718055994531f;
-    } else {
-      const int64_t part = static_cast<int64_t>(blockIdx.x) * (16 * T * kWaves) + c;
-#pragma unroll
-      for (int x = 0; x < kV; ++x) *reinterpret_cast<f32x4*>(p.part_o + part * D + 16 * x + 4 * g) = q.o[t][x];
-      if (g == 0) p.part_ml[part] = {top, sum};
+    }
+  };
+  if constexpr (T == 2) {
+    if (mine == 2) return work(std::integral_constant<int, 2>{});
+  }
+  if (mine == 1) return work(std::integral_constant<int, 1>{});
+  // a wave without columns only helps to load
+  if (plain > 0) {
+    enter(0);
+    enter(1);
+    for (int stage = 0; stage + 1 < plain; stage += 2) {
+      look_up(stage + 2 + kAhead);
+      arrive();
+      load(stage + 2 + kAhead);
+      load(stage + 3 + kAhead);
     }
   }
+  for (int stage = plain > 0 ? plain + 2 - (plain & 1) : 0; stage < stages; ++stage) enter(stage);
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
 }
 
 // After the wide kernel: the parts' (m, l, O) of one row and head, a wave each; nothing
 // where a workgroup had all of the row's keys.  (What `joins` holds for a row of no request
 // may be anything: it is clamped to the workspace.)
+constexpr int kJoinWaves = 4;
 template <int D>
-__global__ __launch_bounds__(kThreads) void tree_join_kernel(const float* __restrict__ part_o,
+__global__ __launch_bounds__(64 * kJoinWaves) void tree_join_kernel(const float* __restrict__ part_o,
                                                              const float2* __restrict__ part_ml,
                                                              const int4* __restrict__ joins, int64_t heads, int Hq,
                                                              int Hk, int tile_cols, int slots,
@@ -847,7 +991,7 @@ __global__ __launch_bounds__(kThreads) void tree_join_kernel(const float* __rest
   constexpr int kPer = D / 4, kAtOnce = 64 / kPer;     // lanes a part, parts a load
   constexpr int kBatch = 8;                            // loads under way
   const int lane = static_cast<int>(threadIdx.x) & 63;
-  const int64_t head = static_cast<int64_t>(blockIdx.x) * kWaves + (threadIdx.x >> 6);
+  const int64_t head = static_cast<int64_t>(blockIdx.x) * kJoinWaves + (threadIdx.x >> 6);
   if (head >= heads) return;
   const int64_t row = head / Hq;
   const int4 j = joins[row];
@@ -905,13 +1049,18 @@ void launch(const TreeArgs& p, int tile_cols, int64_t blocks, hipStream_t stream
   if (tile_cols == 16)
     tree_attention_kernel<D><<<grid, 64 * kNarrowWaves<D>, 0, stream>>>(p);
   else if (tile_cols == 64)
-    tree_attention_wide_kernel<D, 1><<<grid, kThreads, 0, stream>>>(p);
-  else if constexpr (D <= 128)
-    tree_attention_wide_kernel<D, 2><<<grid, kThreads, 0, stream>>>(p);
+    tree_attention_wide_kernel<D, 1, 4><<<grid, 256, 0, stream>>>(p);
+  else if constexpr (D <= 128) {
+    if (tile_cols == 128)
+      tree_attention_wide_kernel<D, 2, 4><<<grid, 256, 0, stream>>>(p);
+    else
+      tree_attention_wide_kernel<D, 2, 8><<<grid, 512, 0, stream>>>(p);
+  }
   if (p.split && tile_cols > 16) {
     const int64_t heads = static_cast<int64_t>(p.M) * p.Hq;
-    tree_join_kernel<D><<<dim3(static_cast<unsigned>((heads + kWaves - 1) / kWaves)), kThreads, 0, stream>>>(
-        p.part_o, p.part_ml, p.joins, heads, p.Hq, p.Hk, tile_cols, p.slots, p.out, p.lse);
+    tree_join_kernel<D><<<dim3(static_cast<unsigned>((heads + kJoinWaves - 1) / kJoinWaves)), 64 * kJoinWaves, 0,
+                          stream>>>(p.part_o, p.part_ml, p.joins, heads, p.Hq, p.Hk, tile_cols, p.slots, p.out,
+                                    p.lse);
   }
 }
 
@@ -922,13 +1071,14 @@ TreePlan plan_tree_attention(int M, int B, int Hq, int Hk, int D, int max_kv_len
   const int64_t G = Hq / Hk;
   const int64_t used = std::max(1, std::min(M, B));
   const int64_t per = (M * G + used - 1) / used;        // query columns of a mean request
-  c.tile_cols = per <= 16 ? 16 : per <= 64 || D > 128 ? 64 : 128;
+  // (188 columns a request over 32 k tokens, heads of 128: 256 / 128 columns a workgroup 247 / 258 us)
+  c.tile_cols = per <= 16 ? 16 : per <= 64 || D > 128 ? 64 : per <= 128 ? 128 : 256;
   c.step = c.tile_cols == 16 ? 32 * (D <= 128 ? kNarrowWaves<128> : kNarrowWaves<256>) : 128;
   const int64_t tiles = most_tiles(M, B, G, c.tile_cols);
   // Slots a kv head: as many as the chip holds workgroups at once (by their registers and
   // LDS), but no more than there are parts; where the tiles alone are that many, some for
   // requests that are longer than the others.
-  const int per_cu = c.tile_cols == 16 || D > 128 ? 1 : D == 128 || c.tile_cols == 128 ? 2 : 4;
+  const int per_cu = c.tile_cols == 16 || c.tile_cols == 256 || D > 128 ? 1 : c.tile_cols == 128 || D == 128 ? 2 : 4;
   const int64_t at_once = std::max<int64_t>(static_cast<int64_t>(per_cu) * num_cus / Hk, 1);
   const int64_t parts = tiles * std::min<int64_t>(kMaxSplits, std::max((max_kv_len + c.step - 1) / c.step, 1));
   c.spread = tiles >= at_once;
@@ -960,7 +1110,7 @@ hipError_t launch_tree_attention(const TreePlan& c, const uint16_t* q, int64_t l
   // (q . k times it vanishes beside 1) and keeps an unseen -inf from becoming 0 x inf.
   const float size = std::max(std::fabs(scale) * 1.44269504088896341f, 0x1p-100f);
   const TreeArgs p{q, ld_q, cache.K, cache.V, cache.page_stride, cache.page_shift, cache.num_pages, pages, ld_pages,
-                   max_keys, cached, offsets, mask, ld_mask, mask_wide, size, kSlack / size,
+                   max_keys, cached, offsets, mask, ld_mask, mask ? mask_wide : 0, size, kSlack / size,
                    std::signbit(scale) ? 0x80008000u : 0u, out, lse, part_o, part_ml, arrived, joins, M, B, Hq, Hk, Hq / Hk, static_cast<int>(c.slots), c.step, c.split, c.spread};
   if (D == 64) launch<64>(p, c.tile_cols, c.blocks, stream);
   else if (D == 128) launch<128>(p, c.tile_cols, c.blocks, stream);
