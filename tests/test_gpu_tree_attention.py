@@ -320,3 +320,50 @@ def test_no_rows_and_no_requests():
     with pytest.raises(ValueError):
         prq.prq_tree_attention(c.q, c.cache, c.table, c.cached, c.offsets, c.scale,
                                tree_mask=torch.ones(2, 1, dtype=torch.bool, device="cuda"))           # rows
+
+
+@pytest.mark.parametrize("rows,D,page", [(1, 128, 16), (5, 64, 64), (13, 128, 16), (13, 64, 32), (13, 256, 16),
+                                         (20, 128, 64), (20, 64, 16), (40, 128, 16), (40, 64, 64), (64, 128, 128)])
+def test_long_parts(rows, D, page):
+    """Many kv heads leave few workgroups to a head, so that each goes through more than a thousand
+    keys, of which one page is missing; against float64 products on the device (same bars)."""
+    Hk, G = 32, 4
+    g = torch.Generator(device="cuda").manual_seed(rows + D)
+    cached = [2500 + 37 * i for i in range(7)] + [31]
+    n = [rows - (i % 3 if rows > 3 else 0) for i in range(8)]
+    used = [-(-(c + r) // page) for c, r in zip(cached, n)]
+    order = torch.randperm(sum(used), generator=g, device="cuda").int()
+    table = torch.full((8, max(used)), -1, dtype=torch.int32, device="cuda")
+    for b in range(8):
+        table[b, :used[b]] = order[sum(used[:b]):sum(used[:b + 1])]
+    table[3, 1600 // page] = -1
+    K, V = ((torch.randn(sum(used), Hk, page, D, generator=g, device="cuda") + 0.2 * i).to(BF16) for i in range(2))
+    q = (1.5 * torch.randn(sum(n), Hk * G, D, generator=g, device="cuda")).to(BF16)
+    mask = torch.rand(sum(n), rows, generator=g, device="cuda") < 0.5
+    offsets = torch.tensor(np.concatenate([[0], np.cumsum(n)]), dtype=torch.int32, device="cuda")
+    say("long parts", rows, D, page)
+    out, lse = _prq().prq_tree_attention(q, _prq().PagedKV(K, V), table,
+                                         torch.tensor(cached, dtype=torch.int32, device="cuda"), offsets, D ** -0.5,
+                                         mask)
+    at_ = 0
+    for b in range(8):
+        L, r = cached[b] + n[b], slice(at_, at_ + n[b])
+        at_ += n[b]
+        ids = table[b, :used[b]].long()
+        there = (ids >= 0).repeat_interleave(page)[:L]
+        k, v = (t[ids.clamp(min=0)].transpose(1, 2).reshape(-1, Hk, D)[:L].transpose(0, 1).double() for t in (K, V))
+        qb = q[r].reshape(n[b], Hk, G, D).permute(1, 2, 0, 3).reshape(Hk, G * n[b], D).double()
+        see = there.repeat(n[b], 1)
+        see[:, cached[b]:] &= mask[r, :n[b]]
+        s = (qb @ k.transpose(1, 2).contiguous()) * D ** -0.5
+        s = s.masked_fill(~see.repeat(G, 1), float("-inf"))
+        want_l = torch.logsumexp(s, -1)
+        p = torch.exp(s - want_l[..., None])
+        want, spread = p @ v, p @ v.abs()
+        size = (qb.abs() @ k.abs().transpose(1, 2).contiguous()).amax(-1)
+        S = (D ** -0.5 * size + 16)[..., None]
+        rows_of = lambda t: t.reshape(n[b], Hk, G, -1).permute(1, 2, 0, 3).reshape(Hk, G * n[b], -1).double()  # noqa
+        err = (rows_of(out[r]) - want).abs()
+        assert bool((err <= 2.0 ** -8 * want.abs() + (2.0 ** -8 + 2.0 ** -18 * S) * spread).all()), (b, float(err.max()))
+        err = (rows_of(lse[r])[..., 0] - want_l).abs()
+        assert bool((err <= 2.0 ** -18 * S[..., 0] + 2.0 ** -22 * want_l.abs()).all()), (b, float(err.max()))
