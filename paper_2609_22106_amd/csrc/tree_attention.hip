@@ -26,8 +26,8 @@
 // back transposed.  Trees of up to 64 nodes over 8 x 32 k tokens (377 rows, 204 k keys): straight
 // from memory 714 us, through LDS with v_perm 272, transposed reads 258; a stage's scores
 // beside the exponentials of the one before and LDS read ahead, 8 waves for more than 128
-// columns, those dealt evenly to the SIMDs, a barrier every two stages, 234: 670 TFLOP/s, the
-// matrix units 40% of the time.  What is left: the parts, unequal by 17%, and a SIMD's two
+// columns, those dealt evenly to the SIMDs, a barrier every two stages, 227: 700 TFLOP/s, the
+// matrix units 40% of the time, 9 us of it the join's.  What is left: the parts, unequal by 17%, and a SIMD's two
 // waves, in step more often than in turn.
 //
 // The maximum is kept per lane group and only joined across the groups when a score
@@ -39,8 +39,8 @@
 // Few rows leave most CUs idle, so a request's keys are split over workgroups: as many
 // parts as the chip holds at once, dealt to the requests by their lengths, and the partial
 // (m, l, O) joined in a fixed order: by the last part of a tile to arrive where there are few
-// columns, by a second kernel where they are many (13-node trees 50 us the first way, 24.5
-// the second: one workgroup is then slow to read all parts of a tile).
+// columns, by a second kernel where they are many (trees of up to 13 nodes over 6 x 8 k tokens 50 us
+// the first way, 24.5 the second, 22.7 by now: one workgroup is then slow to read all parts of a tile).
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -995,7 +995,7 @@ __global__ __launch_bounds__(64 * kJoinWaves) void tree_join_kernel(const float*
   if (head >= heads) return;
   const int64_t row = head / Hq;
   const int4 j = joins[row];
-  const int splits = min(j.w, kMaxSplits);
+  const int splits = __builtin_amdgcn_readfirstlane(min(j.w, kMaxSplits));
   if (splits <= 1) return;
   const int G = Hq / Hk, q = static_cast<int>(head - row * Hq);
   const uint32_t c = static_cast<uint32_t>((row - j.x) * G + q % G);
@@ -1010,8 +1010,9 @@ __global__ __launch_bounds__(64 * kJoinWaves) void tree_join_kernel(const float*
   auto load = [&](int s0) {
 #pragma unroll
     for (int x = 0; x < kBatch; ++x)
-      in[x] = *reinterpret_cast<const f32x4*>(part_o + at(min(s0 + x * kAtOnce + lane / kPer, splits - 1)) * D +
-                                              4 * (lane % kPer));
+      if (s0 + x * kAtOnce < splits)
+        in[x] = *reinterpret_cast<const f32x4*>(
+            part_o + at(min(s0 + x * kAtOnce + lane / kPer, splits - 1)) * D + 4 * (lane % kPer));
   };
   load(0);
   float top = ml.x;
@@ -1026,6 +1027,7 @@ __global__ __launch_bounds__(64 * kJoinWaves) void tree_join_kernel(const float*
     if (s0 > 0) load(s0);
 #pragma unroll
     for (int x = 0; x < kBatch; ++x) {
+      if (s0 + x * kAtOnce >= splits) break;
       const int s = s0 + x * kAtOnce + lane / kPer;
       const float w = __shfl(a, s & 63);
       if (s < splits && w != 0.f) o += w * in[x];      // a part that a row saw nothing of adds nothing
@@ -1078,7 +1080,9 @@ TreePlan plan_tree_attention(int M, int B, int Hq, int Hk, int D, int max_kv_len
   // Slots a kv head: as many as the chip holds workgroups at once (by their registers and
   // LDS), but no more than there are parts; where the tiles alone are that many, some for
   // requests that are longer than the others.
-  const int per_cu = c.tile_cols == 16 || c.tile_cols == 256 || D > 128 ? 1 : c.tile_cols == 128 || D == 128 ? 2 : 4;
+  // (heads of 64, 64 columns, of which four would fit: 1 / 2 / 3 / 4 a CU 29.2 / 24.1 / 25.7 / 25.8 us,
+  // trees of up to 13 nodes over 6 x 8 k tokens)
+  const int per_cu = c.tile_cols == 16 || c.tile_cols == 256 || D > 128 ? 1 : 2;
   const int64_t at_once = std::max<int64_t>(static_cast<int64_t>(per_cu) * num_cus / Hk, 1);
   const int64_t parts = tiles * std::min<int64_t>(kMaxSplits, std::max((max_kv_len + c.step - 1) / c.step, 1));
   c.spread = tiles >= at_once;
@@ -1103,7 +1107,8 @@ hipError_t launch_tree_attention(const TreePlan& c, const uint16_t* q, int64_t l
                                  void* workspace, hipStream_t stream) {
   const int64_t cols = c.blocks * c.tile_cols;
   uint32_t* const arrived = static_cast<uint32_t*>(workspace);         // the state head
-  float* const part_o = c.split ? reinterpret_cast<float*>(static_cast<char*>(workspace) + kWorkspaceStateBytes) : nullptr;
+  char* const parts = static_cast<char*>(workspace) + kWorkspaceStateBytes;
+  float* const part_o = c.split ? reinterpret_cast<float*>(parts) : nullptr;
   float2* const part_ml = c.split ? reinterpret_cast<float2*>(part_o + cols * D) : nullptr;
   int4* const joins = c.split ? reinterpret_cast<int4*>(part_ml + cols) : nullptr;
   // A negative scale turns the queries' signs; 0 is as good as the smallest used here
@@ -1111,7 +1116,8 @@ hipError_t launch_tree_attention(const TreePlan& c, const uint16_t* q, int64_t l
   const float size = std::max(std::fabs(scale) * 1.44269504088896341f, 0x1p-100f);
   const TreeArgs p{q, ld_q, cache.K, cache.V, cache.page_stride, cache.page_shift, cache.num_pages, pages, ld_pages,
                    max_keys, cached, offsets, mask, ld_mask, mask ? mask_wide : 0, size, kSlack / size,
-                   std::signbit(scale) ? 0x80008000u : 0u, out, lse, part_o, part_ml, arrived, joins, M, B, Hq, Hk, Hq / Hk, static_cast<int>(c.slots), c.step, c.split, c.spread};
+                   std::signbit(scale) ? 0x80008000u : 0u, out, lse, part_o, part_ml, arrived, joins, M, B, Hq, Hk,
+                   Hq / Hk, static_cast<int>(c.slots), c.step, c.split, c.spread};
   if (D == 64) launch<64>(p, c.tile_cols, c.blocks, stream);
   else if (D == 128) launch<128>(p, c.tile_cols, c.blocks, stream);
   else launch<256>(p, c.tile_cols, c.blocks, stream);
