@@ -27,8 +27,8 @@
 // from memory 714 us, through LDS with v_perm 272, transposed reads 258; a stage's scores
 // beside the exponentials of the one before and LDS read ahead, 8 waves for more than 128
 // columns, those dealt evenly to the SIMDs, a barrier every two stages, 227: 700 TFLOP/s, the
-// matrix units 40% of the time, 9 us of it the join's.  What is left: the parts, unequal by 17%, and a SIMD's two
-// waves, in step more often than in turn.
+// matrix units 40% of the time, 9 us of it the join's.  What is left: the parts, unequal by 17%,
+// and a SIMD's two waves, in step more often than in turn.
 //
 // The maximum is kept per lane group and only joined across the groups when a score
 // passes it by 8 (powers of two): until then the stale maximum serves, P up to 2^8.
@@ -39,8 +39,9 @@
 // Few rows leave most CUs idle, so a request's keys are split over workgroups: as many
 // parts as the chip holds at once, dealt to the requests by their lengths, and the partial
 // (m, l, O) joined in a fixed order: by the last part of a tile to arrive where there are few
-// columns, by a second kernel where they are many (trees of up to 13 nodes over 6 x 8 k tokens 50 us
-// the first way, 24.5 the second, 22.7 by now: one workgroup is then slow to read all parts of a tile).
+// columns, by a second kernel where they are many (trees of up to 13 nodes over 6 x 8 k tokens
+// 50 us the first way, 24.5 the second, 22.7 by now: one workgroup is then slow to read all parts
+// of a tile).
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
