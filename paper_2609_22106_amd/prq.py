@@ -889,10 +889,13 @@ def prq_lora(x, adapters, segment_offsets, segment_adapter, Y, out=None, workspa
     _vector(segment_adapter, "segment_adapter", _I32, segments)
     _vector(segment_offsets, "segment_offsets", _I32, segments + 1)
     if workspace is None:
-        need = int(_lora_ws(M, segments, N, K, a.max_rank))
-        if need:
-            workspace = _alloc(torch.empty, need, _U8, x.device, stream, kept=False)
-    ws, ws_bytes = _workspace_arg(workspace)
+        ws, ws_bytes = None, _lora_ws(M, segments, N, K, a.max_rank)
+        if ws_bytes:
+            workspace = (x.new_empty(ws_bytes, dtype=_U8) if stream is None
+                         else _alloc(torch.empty, ws_bytes, _U8, x.device, stream, kept=False))
+            ws = workspace.data_ptr()
+    else:
+        ws, ws_bytes = _workspace_arg(workspace)
     st = _lora(x.data_ptr(), ld_x, M, K, a.A.data_ptr(), a.B.data_ptr(), a.rank_offsets.data_ptr(),
                a.scales.data_ptr(), n, R, a.max_rank, segment_offsets.data_ptr(),
                segment_adapter.data_ptr(), segments, N, Y.data_ptr(), ld_y, out.data_ptr(), ld_out, ws, ws_bytes,
