@@ -142,7 +142,7 @@ int prq_tree_attention(const void* q, int64_t ld_q, int32_t M, int32_t Hq, int32
 
 size_t prq_lora_workspace_bytes(int32_t M, int32_t segments, int32_t N, int32_t K, int32_t max_rank) {
   if (check_lora_sizes(M, segments, N, K, max_rank) != PRQ_OK || M == 0 || segments == 0) return 0;
-  return prq::lora_workspace_bytes(prq::plan_lora(M, segments, N, K, max_rank, device_cus()), M, max_rank);
+  return prq::lora_workspace_bytes(prq::plan_lora(M, segments, M, N, K, max_rank, device_cus()), M, max_rank);
 }
 
 int prq_lora(const void* x_bf16, int64_t ld_x, int32_t M, int32_t K, const void* A, const void* B,
@@ -165,7 +165,7 @@ int prq_lora(const void* x_bf16, int64_t ld_x, int32_t M, int32_t K, const void*
   int cus = 0;
   st = prq::current_device_cus(&cus);
   if (st != PRQ_OK) return st;
-  const prq::LoraPlan plan = prq::plan_lora(M, segments, N, K, max_rank, cus);
+  const prq::LoraPlan plan = prq::plan_lora(M, segments, adapters, N, K, max_rank, cus);
   const size_t need = prq::lora_workspace_bytes(plan, M, max_rank);
   if (need && (!workspace || workspace_bytes < need)) return PRQ_EWORKSPACE;
   if (need && !aligned(workspace, 16)) return PRQ_EALIGN;

@@ -34,6 +34,17 @@ __device__ __forceinline__ f32x4 mfma_bf16(u32x4v a, u32x4v b, f32x4 c) {
                                                  0, 0, 0);
 }
 
+// Every lane's sum over itself and the lanes before it.
+__device__ __forceinline__ int prefix_sum(int x) {
+  x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xF, 0xF, false);    // row_shr 1, 2, 4, 8
+  x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xF, 0xF, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xF, 0xF, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xF, 0xF, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xA, 0xF, false);    // row_bcast 15, 31
+  x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xC, 0xF, false);
+  return x;
+}
+
 // Segment tables on the device: segment s holds rows [offsets[s], offsets[s + 1]),
 // per_row units each, cut into tiles of per_tile units.  find_tile: the segment that
 // holds tile `t` (counted over all segments), the tile's number in it, and the
@@ -61,14 +72,7 @@ __device__ __forceinline__ TileAt find_tile(const int32_t* __restrict__ offsets,
       n = max(min(max(n, 0), M) - lo, 0);
       tiles = (n * per_row + per_tile - 1) / per_tile;
     }
-    sum = tiles;
-    if (segments > 1) {
-#pragma unroll
-      for (int d = 1; d < 64; d <<= 1) {
-        const int x = __shfl_up(sum, d);
-        if (lane >= d) sum += x;
-      }
-    }
+    sum = prefix_sum(tiles);
     const uint64_t past = __ballot(before + sum > t);
     if (past) {
       at = __builtin_ctzll(past);

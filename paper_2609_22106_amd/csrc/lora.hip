@@ -4,10 +4,10 @@
 // Y and out float32 [M, N] (out may be Y), x bf16 [M, K].
 //
 // Two products with the rank between them, in two kernels: `down` forms
-// t = A_a x over ranges of K (a workgroup per 16 or 32 rows of one segment and range, so
-// that a few decoding rows still occupy the chip; partial sums in the workspace) and
-// `up` adds them in order, scales and multiplies by B_a.  The bytes of Y and out bound
-// long prompts; the adapters' own bytes and the two launches a decoding step.
+// t = A_a x over ranges of K (a workgroup per 16 or 32 rows of one segment, or of one
+// adapter, and range, so that a few decoding rows still occupy the chip; partial sums in the
+// workspace) and `up` adds them in order, scales and multiplies by B_a.  The bytes of Y and
+// out bound long prompts; the adapters' own bytes and the two launches a decoding step.
 //
 // An operand's neighbouring lanes hold different rows, so operands loaded straight from
 // rows in memory use 16 of the 64 bytes a clock of a CU's first cache: rows are loaded
@@ -64,14 +64,70 @@ __device__ __forceinline__ Adapter adapter_of(const LoraArgs& p, int index) {
   return a;
 }
 
+// 16 rows that have an adapter (or none) in common.
+struct Tile {
+  int with, rows, mine;                  // its index; the rows; row lane % 16 of them (the last one past the end)
+};
+
+// Tile y of the launch: 16 neighbouring rows of one segment, or (kGrouped, M <= 64) of all rows
+// with one adapter, wherever they are: lane i asks for row i, and the adapters are taken in the
+// order of their first rows.  owner: 64 words of LDS of the wave's own.  false: there is none.
+template <bool kGrouped>
+__device__ __forceinline__ bool find_rows(const LoraArgs& p, int* owner, Tile* out) {
+  const int lane = static_cast<int>(threadIdx.x) & 63;
+  int t = static_cast<int>(blockIdx.y);
+  if constexpr (!kGrouped) {
+    const dev::TileAt at = dev::find_tile(p.offsets, p.of, p.segments, p.M, t, 1, 16);
+    if (at.segment < 0) return false;
+    const int rows = min(at.rows - 16 * at.tile, 16);
+    *out = {at.with, rows, at.first + 16 * at.tile + min(lane & 15, rows - 1)};
+    return true;
+  }
+  constexpr int kNobody = -2;
+  owner[lane] = kNobody;
+  __builtin_amdgcn_wave_barrier();
+  for (int base = 0; base < p.segments; base += 64) {
+    const int s = base + lane;
+    if (s < p.segments) {
+      const int with = p.of[s], first = min(max(p.offsets[s], 0), p.M), end = min(max(p.offsets[s + 1], 0), p.M);
+      for (int row = first; row < end; ++row) owner[row] = with >= 0 && with < p.adapters ? with : -1;
+    }
+  }
+  __builtin_amdgcn_wave_barrier();
+  const int own = lane < p.M ? owner[lane] : kNobody;
+  // The rows with the lane's adapter, bit by bit of its index; the first of them counts their tiles.
+  uint64_t same = __ballot(own != kNobody);
+  for (int b = 0; p.adapters >> b; ++b) {
+    const bool bit = (own + 1) >> b & 1;
+    const uint64_t set = __ballot(bit);
+    same &= bit ? set : ~set;
+  }
+  const bool leads = own != kNobody && __builtin_ctzll(same) == lane;
+  const int tiles = leads ? (__builtin_popcountll(same) + 15) / 16 : 0, sum = dev::prefix_sum(tiles);
+  const uint64_t past = __ballot(sum > t);
+  if (!past) return false;
+  const int at = __builtin_ctzll(past);
+  t -= __builtin_amdgcn_readlane(sum - tiles, at);
+  const uint64_t rows = static_cast<uint64_t>(static_cast<uint32_t>(
+                            __builtin_amdgcn_readlane(static_cast<int>(same >> 32), at))) << 32 |
+                        static_cast<uint32_t>(__builtin_amdgcn_readlane(static_cast<int>(same), at));
+  const int with = __builtin_amdgcn_readlane(own, at);
+  const int n = min(__builtin_popcountll(rows) - 16 * t, 16);
+  const int rank = __builtin_popcountll(rows & ((uint64_t{1} << lane) - 1)) - 16 * t;
+  const bool in = (rows >> lane & 1) && rank >= 0 && rank < 16;
+  const int sent = __builtin_amdgcn_ds_permute(4 * (in ? rank : 63), lane);     // lane 63's is not used
+  *out = {with, n, __shfl(sent, min(lane & 15, n - 1))};
+  return true;
+}
+
 // t of 16 kRowTiles rows over K's elements [k0, end), for up to 16 kTiles ranks from `rank0`
 // on, by kN waves: emit(row, rank, value), by any thread.  The waves take every kN-th step
 // of 64 elements.  A row's 128 bytes of a step are loaded by 8 neighbouring lanes -- an
 // operand's own lanes, each on another row, would take the first cache four times as long
 // -- and reach their operand's place through a part of LDS of the wave's own (unit u of row k
 // at u ^ (k / 2 & 7): no conflicts).
-template <int kRowTiles, int kTiles, int kN, typename Emit>
-__device__ __forceinline__ void down_rows(const LoraArgs& p, const Adapter& ad, int64_t row0, int rows, int rank0,
+template <int kRowTiles, int kTiles, int kN, typename RowAt, typename Emit>
+__device__ __forceinline__ void down_rows(const LoraArgs& p, const Adapter& ad, RowAt row_at, int rows, int rank0,
                                           int k0, int end, u32x4v* sh, Emit emit) {
   constexpr int kLoads = 2 * (kRowTiles + kTiles);           // of 8 rows, a step
   // steps under way: the small kernel has the registers for all of K = 2560 at up to 32 ranks
@@ -82,7 +138,7 @@ __device__ __forceinline__ void down_rows(const LoraArgs& p, const Adapter& ad, 
   // rows and ranks past the end read the last one and are not used
   const uint16_t* src[kLoads];
 #pragma unroll
-  for (int i = 0; i < 2 * kRowTiles; ++i) src[i] = p.x + (row0 + min(8 * i + lr, rows - 1)) * p.ld_x;
+  for (int i = 0; i < 2 * kRowTiles; ++i) src[i] = p.x + row_at(min(8 * i + lr, rows - 1)) * p.ld_x;
 #pragma unroll
   for (int i = 0; i < 2 * kTiles; ++i)
     src[2 * kRowTiles + i] = p.A + static_cast<int64_t>(ad.first + min(rank0 + 8 * i + lr, ad.rank - 1)) * p.K;
@@ -149,36 +205,48 @@ __device__ __forceinline__ void down_rows(const LoraArgs& p, const Adapter& ad, 
 
 // The same for all of an adapter's ranks, up to 16 kMost of them at a time: the adapter's
 // own rank, not the largest one, says what is read.
-template <int kRowTiles, int kMost, int kN, typename Emit>
-__device__ __forceinline__ void down_ranks(const LoraArgs& p, const Adapter& ad, int64_t row0, int rows, int k0,
+template <int kRowTiles, int kMost, int kN, typename RowAt, typename Emit>
+__device__ __forceinline__ void down_ranks(const LoraArgs& p, const Adapter& ad, RowAt row_at, int rows, int k0,
                                            int end, u32x4v* sh, Emit emit) {
   int rank0 = 0;
   if constexpr (kMost == 4)
     for (; ad.rank - rank0 > 32; rank0 += 64) {
       if (rank0) __syncthreads();
-      down_rows<kRowTiles, 4, kN>(p, ad, row0, rows, rank0, k0, end, sh, emit);
+      down_rows<kRowTiles, 4, kN>(p, ad, row_at, rows, rank0, k0, end, sh, emit);
     }
   if (ad.rank <= rank0) return;
   if (rank0) __syncthreads();
   if constexpr (kMost >= 2)
-    if (ad.rank - rank0 > 16) return down_rows<kRowTiles, 2, kN>(p, ad, row0, rows, rank0, k0, end, sh, emit);
-  down_rows<kRowTiles, 1, kN>(p, ad, row0, rows, rank0, k0, end, sh, emit);
+    if (ad.rank - rank0 > 16) return down_rows<kRowTiles, 2, kN>(p, ad, row_at, rows, rank0, k0, end, sh, emit);
+  down_rows<kRowTiles, 1, kN>(p, ad, row_at, rows, rank0, k0, end, sh, emit);
 }
 
-template <int kRowTiles, int kMost>
+template <int kRowTiles, int kMost, bool kGrouped>
 __global__ __launch_bounds__(kThreads, kRowTiles == 1 ? 3 : 2) void lora_down_kernel(const LoraArgs p) {
   __shared__ u32x4v sh[kWaves * 2 * (kRowTiles + kMost) * 64];
-  const dev::TileAt at = dev::find_tile(p.offsets, p.of, p.segments, p.M, static_cast<int>(blockIdx.y), 1,
-                                        16 * kRowTiles);
-  if (at.segment < 0) return;
-  const Adapter ad = adapter_of(p, at.with);
-  if (ad.rank <= 0) return;
-  const int rows = min(at.rows - 16 * kRowTiles * at.tile, 16 * kRowTiles);
-  const int64_t row0 = at.first + 16 * kRowTiles * at.tile;
-  const int k0 = static_cast<int>(blockIdx.x) * p.k_per;
-  float* const t = p.t + (static_cast<int64_t>(blockIdx.x) * p.M + row0) * p.max_rank;
-  down_ranks<kRowTiles, kMost, kWaves>(p, ad, row0, rows, k0, min(k0 + p.k_per, p.K), sh,
-                                       [&](int row, int rank, float x) { t[row * p.max_rank + rank] = x; });
+  const int k0 = static_cast<int>(blockIdx.x) * p.k_per, end = min(k0 + p.k_per, p.K);
+  float* const t = p.t + static_cast<int64_t>(blockIdx.x) * p.M * p.max_rank;
+  if constexpr (kGrouped) {
+    __shared__ int owner[kWaves][64], row[16];
+    Tile at;
+    if (!find_rows<true>(p, owner[threadIdx.x >> 6], &at)) return;
+    const Adapter ad = adapter_of(p, at.with);
+    if (ad.rank <= 0) return;
+    if (threadIdx.x < 16) row[threadIdx.x] = at.mine;        // (down_rows has barriers before it is read)
+    down_ranks<1, kMost, kWaves>(
+        p, ad, [&](int k) { return static_cast<int64_t>(__shfl(at.mine, k)); }, at.rows, k0, end, sh,
+        [&](int k, int rank, float x) { t[static_cast<int64_t>(row[k]) * p.max_rank + rank] = x; });
+  } else {
+    const dev::TileAt at = dev::find_tile(p.offsets, p.of, p.segments, p.M, static_cast<int>(blockIdx.y), 1,
+                                          16 * kRowTiles);
+    if (at.segment < 0) return;
+    const Adapter ad = adapter_of(p, at.with);
+    if (ad.rank <= 0) return;
+    const int64_t row0 = at.first + 16 * kRowTiles * at.tile;
+    down_ranks<kRowTiles, kMost, kWaves>(
+        p, ad, [&](int k) { return row0 + k; }, min(at.rows - 16 * kRowTiles * at.tile, 16 * kRowTiles), k0, end, sh,
+        [&](int k, int rank, float x) { t[(row0 + k) * p.max_rank + rank] = x; });
+  }
 }
 
 // x's three bf16 terms: x = a + b + c up to 2^-24 of x.  An infinity or a NaN is a's alone.
@@ -214,8 +282,8 @@ __device__ __forceinline__ void load_operand(const float* sh, bool here, u32x4v 
 
 // t of the tile's rows, the ranges of K added in order, scaled, into sh (rows `pitch`
 // apart); what lies past the rows and the rank is left as it is.
-template <int kAtOnce>
-__device__ __forceinline__ void join_ranges(const LoraArgs& p, const Adapter& ad, int64_t row0, int rows, float* sh,
+template <int kAtOnce, typename RowAt>
+__device__ __forceinline__ void join_ranges(const LoraArgs& p, const Adapter& ad, RowAt row_at, int rows, float* sh,
                                             int pitch) {
   if (ad.rank <= 0) return;
   const float scale = p.scales[ad.index];
@@ -224,7 +292,7 @@ __device__ __forceinline__ void join_ranges(const LoraArgs& p, const Adapter& ad
 #pragma unroll kAtOnce
   for (int e = static_cast<int>(threadIdx.x); e < all; e += kThreads) {
     const int row = e / quads, quad = e - row * quads;
-    const float* tp = p.t + (row0 + row) * p.max_rank + 4 * quad;
+    const float* tp = p.t + row_at(row) * p.max_rank + 4 * quad;
     f32x4 in[kMaxRanges];
 #pragma unroll
     for (int s = 0; s < kMaxRanges; ++s) in[s] = *reinterpret_cast<const f32x4*>(tp + min(s, p.splits - 1) * next_range);
@@ -236,13 +304,13 @@ __device__ __forceinline__ void join_ranges(const LoraArgs& p, const Adapter& ad
   }
 }
 
-// 16 rows of one segment, 32 columns of Y at a time: A operand B_a's rows (16 columns),
+// A tile's 16 rows, 32 columns of Y at a time: A operand B_a's rows (16 columns),
 // straight from memory, B operand t's rows, so that a lane holds 4 neighbouring columns of
 // one row.
 template <int kSteps>
 struct Up {
   const LoraArgs& p;
-  int64_t row0;
+  int64_t row;                           // row lane % 16
   int rows;
   struct In {
     f32x4 y[2];
@@ -252,8 +320,8 @@ struct Up {
 
   // N % 16 == 0: a tile's columns are all there, or none (then the last tile is read)
   __device__ __forceinline__ void load_y(int n, In* in) const {
-    const int lane = static_cast<int>(threadIdx.x) & 63, r = lane & 15, g = lane >> 4;
-    const float* const yp = p.Y + (row0 + min(r, rows - 1)) * p.ld_y + 4 * g;
+    const int lane = static_cast<int>(threadIdx.x) & 63, g = lane >> 4;
+    const float* const yp = p.Y + row * p.ld_y + 4 * g;
 #pragma unroll
     for (int j = 0; j < 2; ++j) in->y[j] = *reinterpret_cast<const f32x4*>(yp + min(n + 16 * j, p.N - 16));
   }
@@ -292,20 +360,21 @@ struct Up {
 #pragma unroll
           for (int k = 0; k < kSteps; ++k) acc = dev::mfma_bf16(now.b[j][k], t[k][w], acc);
         if (r < rows && n + 16 * j < n1)
-          *reinterpret_cast<f32x4*>(p.out + (row0 + r) * p.ld_out + n + 16 * j + 4 * g) = now.y[j] + acc;
+          *reinterpret_cast<f32x4*>(p.out + row * p.ld_out + n + 16 * j + 4 * g) = now.y[j] + acc;
       }
       now = next;
     }
   }
 };
 
-// Few rows, `up`: 16 rows of one segment, the columns of one slice.
-template <int kSteps>
+// Few rows, `up`: a tile of 16 rows, the columns of one slice.
+template <int kSteps, bool kGrouped>
 __global__ __launch_bounds__(kThreads) void lora_up_kernel(const LoraArgs p, int n_per) {
+  __shared__ int owner[kWaves][kGrouped ? 64 : 1], row[16];
   const int wave = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x) >> 6);
-  const dev::TileAt at = dev::find_tile(p.offsets, p.of, p.segments, p.M, static_cast<int>(blockIdx.y), 1, 16);
-  if (at.segment < 0) return;
-  Up<kSteps> up{p, at.first + 16 * at.tile, min(at.rows - 16 * at.tile, 16)};
+  Tile at;
+  if (!find_rows<kGrouped>(p, owner[wave], &at)) return;
+  Up<kSteps> up{p, at.mine, at.rows};
   const int n0 = static_cast<int>(blockIdx.x) * n_per, n1 = min(n0 + n_per, p.N), n = n0 + 32 * wave;
   if (n < n1) up.load_y(n, &up.now);
   const Adapter ad = adapter_of(p, at.with);
@@ -313,31 +382,40 @@ __global__ __launch_bounds__(kThreads) void lora_up_kernel(const LoraArgs p, int
   if (n < n1) up.load_b(ad, n, &up.now);
   constexpr int kPitch = 32 * kSteps + 4;
   __shared__ __align__(16) float sh[16 * kPitch];
-  join_ranges<1>(p, ad, up.row0, up.rows, sh, kPitch);
+  if constexpr (kGrouped) {
+    if (threadIdx.x < 16) row[threadIdx.x] = at.mine;
+    __syncthreads();
+    join_ranges<1>(p, ad, [&](int k) { return static_cast<int64_t>(row[k]); }, at.rows, sh, kPitch);
+  } else {
+    const int64_t row0 = __builtin_amdgcn_readfirstlane(at.mine);
+    join_ranges<1>(p, ad, [&](int k) { return row0 + k; }, at.rows, sh, kPitch);
+  }
   __syncthreads();
   up.operands(ad, sh, kPitch);
   up.columns(ad, n, n1, 32 * kWaves);
 }
 
-// Both products in one launch: a workgroup of 16 rows and a slice of columns forms all of
+// Both products in one launch: a workgroup of a tile and a slice of columns forms all of
 // the rows' t for itself.
-template <int kMost>
+template <int kMost, bool kGrouped>
 __global__ __launch_bounds__(64 * kSmallWaves) void lora_small_kernel(const LoraArgs p, int n_per) {
   constexpr int kSteps = kMost <= 2 ? 1 : 2, kPitch = 32 * kSteps + 4;
   __shared__ u32x4v sh[kSmallWaves * 2 * (1 + kMost) * 64];
   __shared__ __align__(16) float sh_t[16 * kPitch];
+  __shared__ int owner[kSmallWaves][kGrouped ? 64 : 1];
   const int wave = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x) >> 6);
-  const dev::TileAt at = dev::find_tile(p.offsets, p.of, p.segments, p.M, static_cast<int>(blockIdx.y), 1, 16);
-  if (at.segment < 0) return;
-  Up<kSteps> up{p, at.first + 16 * at.tile, min(at.rows - 16 * at.tile, 16)};
+  Tile at;
+  if (!find_rows<kGrouped>(p, owner[wave], &at)) return;
+  Up<kSteps> up{p, at.mine, at.rows};
   const int n0 = static_cast<int>(blockIdx.x) * n_per, n1 = min(n0 + n_per, p.N), n = n0 + 32 * wave;
   if (n < n1) up.load_y(n, &up.now);
   const Adapter ad = adapter_of(p, at.with);
   if (ad.rank <= 0 && p.out == p.Y) return;
   if (n < n1) up.load_b(ad, n, &up.now);
   const float scale = ad.rank > 0 ? p.scales[ad.index] : 0.f;
-  down_ranks<1, kMost, kSmallWaves>(p, ad, up.row0, up.rows, 0, p.K, sh,
-                                    [&](int row, int rank, float x) { sh_t[row * kPitch + rank] = x * scale; });
+  down_ranks<1, kMost, kSmallWaves>(
+      p, ad, [&](int k) { return static_cast<int64_t>(__shfl(at.mine, k)); }, at.rows, 0, p.K, sh,
+      [&](int k, int rank, float x) { sh_t[k * kPitch + rank] = x * scale; });
   __syncthreads();
   up.operands(ad, sh_t, kPitch);
   up.columns(ad, n, n1, 32 * kSmallWaves);
@@ -388,7 +466,7 @@ __global__ __launch_bounds__(kThreads) void lora_up_wide_kernel(const LoraArgs p
         b_in[x] = *reinterpret_cast<const u32x4v*>(B + static_cast<int64_t>(min(n + bk + 32 * x, p.N - 1)) * ad.rank);
   };
   if (ad.rank > 0) load_b(n0, 0);
-  join_ranges<2>(p, ad, row0, rows, &sh_t[0][0], kPitch);
+  join_ranges<2>(p, ad, [&](int k) { return row0 + k; }, rows, &sh_t[0][0], kPitch);
   __syncthreads();
   u32x4v t[2][3];
   auto operands = [&](int rank0) {
@@ -444,14 +522,24 @@ __global__ __launch_bounds__(kThreads) void lora_up_wide_kernel(const LoraArgs p
 }
 
 template <int kRowTiles, int kMost>
-void launch_down(const LoraArgs& p, int64_t tiles, hipStream_t stream) {
-  lora_down_kernel<kRowTiles, kMost><<<dim3(p.splits, static_cast<unsigned>(tiles)), kThreads, 0, stream>>>(p);
+void launch_down(const LoraArgs& p, int64_t tiles, bool grouped, hipStream_t stream) {
+  const dim3 grid(p.splits, static_cast<unsigned>(tiles));
+  if (kRowTiles == 1 && grouped) lora_down_kernel<1, kMost, true><<<grid, kThreads, 0, stream>>>(p);
+  else lora_down_kernel<kRowTiles, kMost, false><<<grid, kThreads, 0, stream>>>(p);
 }
 
 template <int kSteps>
-void launch_up(const LoraArgs& p, int64_t tiles, int n_per, hipStream_t stream) {
-  lora_up_kernel<kSteps>
-      <<<dim3((p.N + n_per - 1) / n_per, static_cast<unsigned>(tiles)), kThreads, 0, stream>>>(p, n_per);
+void launch_up(const LoraArgs& p, int64_t tiles, int n_per, bool grouped, hipStream_t stream) {
+  const dim3 grid((p.N + n_per - 1) / n_per, static_cast<unsigned>(tiles));
+  if (grouped) lora_up_kernel<kSteps, true><<<grid, kThreads, 0, stream>>>(p, n_per);
+  else lora_up_kernel<kSteps, false><<<grid, kThreads, 0, stream>>>(p, n_per);
+}
+
+template <int kMost>
+void launch_small(const LoraArgs& p, int64_t tiles, int n_per, bool grouped, hipStream_t stream) {
+  const dim3 grid((p.N + n_per - 1) / n_per, static_cast<unsigned>(tiles));
+  if (grouped) lora_small_kernel<kMost, true><<<grid, 64 * kSmallWaves, 0, stream>>>(p, n_per);
+  else lora_small_kernel<kMost, false><<<grid, 64 * kSmallWaves, 0, stream>>>(p, n_per);
 }
 
 template <bool kMany>
@@ -462,9 +550,15 @@ void launch_up_wide(const LoraArgs& p, int64_t tiles, int n_per, hipStream_t str
 
 }  // namespace
 
-LoraPlan plan_lora(int M, int segments, int N, int K, int max_rank, int num_cus) {
+LoraPlan plan_lora(int M, int segments, int adapters, int N, int K, int max_rank, int num_cus) {
   LoraPlan c;
   c.tiles = most_tiles(M, segments, 1, 16);
+  // Few rows in more segments than there are adapters: the rows of an adapter together, which
+  // reads it once.  us, 64 requests of a row, by segments / by adapters: 24 adapters of ranks up
+  // to 64, K = 9728 17.0 / 14.2; of ranks up to 16, K = 2560, N = 4096 8.8 / 8.9, 8 of those
+  // 7.8 / 6.4.
+  const int64_t groups = std::min<int64_t>(M, int64_t{adapters} + 1 + M / 16);
+  c.grouped = M <= 64 && groups < std::min(M, segments);
   // One launch while what every slice forms again, all of its rows' t, costs less than a
   // launch: us, one / two launches, rank 16, K = 2560, N = 4096: 1 row 6.2 / 6.9, 64 requests
   // of a row 8.0 / 11.4, 3000 rows 25.7 / 32.3; N = 9728: 2000 rows 45 / 51, 3000 rows 79 / 60;
@@ -473,6 +567,7 @@ LoraPlan plan_lora(int M, int segments, int N, int K, int max_rank, int num_cus)
       (N <= 4096 || 2 * c.tiles <= num_cus)) {
     c.small = true;
     const int cols = 32 * kSmallWaves;
+    if (c.grouped) c.tiles = groups;
     const int64_t slices = std::max<int64_t>(1, num_cus / c.tiles);
     c.n_per = static_cast<int>(((N + slices - 1) / slices + cols - 1) / cols * cols);
     return c;
@@ -488,6 +583,7 @@ LoraPlan plan_lora(int M, int segments, int N, int K, int max_rank, int num_cus)
   const int64_t want = (4 * static_cast<int64_t>(num_cus) + c.tiles - 1) / c.tiles;
   const int64_t most = std::min(std::max(1, steps / (2 * kWaves)), kMaxRanges);
   const int splits = static_cast<int>(std::max<int64_t>(1, std::min(want, most)));
+  if (c.grouped) c.tiles = c.up_tiles = groups;        // (the workspace is the same either way)
   c.k_per = (steps + splits - 1) / splits * 64;
   c.splits = (K + c.k_per - 1) / c.k_per;
   // Short slices: many workgroups a CU hide each other's start (8192 rows x 9728 columns,
@@ -509,29 +605,28 @@ hipError_t launch_lora(const LoraPlan& c, const uint16_t* x, int64_t ld_x, int M
   const LoraArgs p{x, ld_x, A, B, rank_offsets, scales, offsets, of, Y, out, ld_y, ld_out,
                    static_cast<float*>(workspace), adapters, rank_rows, segments, M, N, K, max_rank, c.splits, c.k_per};
   if (c.small) {
-    const dim3 grid((N + c.n_per - 1) / c.n_per, static_cast<unsigned>(c.tiles));
-    if (max_rank <= 16) lora_small_kernel<1><<<grid, 64 * kSmallWaves, 0, stream>>>(p, c.n_per);
-    else if (max_rank <= 32) lora_small_kernel<2><<<grid, 64 * kSmallWaves, 0, stream>>>(p, c.n_per);
-    else lora_small_kernel<4><<<grid, 64 * kSmallWaves, 0, stream>>>(p, c.n_per);
+    if (max_rank <= 16) launch_small<1>(p, c.tiles, c.n_per, c.grouped, stream);
+    else if (max_rank <= 32) launch_small<2>(p, c.tiles, c.n_per, c.grouped, stream);
+    else launch_small<4>(p, c.tiles, c.n_per, c.grouped, stream);
     return hipGetLastError();
   }
   if (c.row_tiles == 2) {
-    if (max_rank <= 16) launch_down<2, 1>(p, c.tiles, stream);
-    else if (max_rank <= 32) launch_down<2, 2>(p, c.tiles, stream);
-    else launch_down<2, 4>(p, c.tiles, stream);
+    if (max_rank <= 16) launch_down<2, 1>(p, c.tiles, false, stream);
+    else if (max_rank <= 32) launch_down<2, 2>(p, c.tiles, false, stream);
+    else launch_down<2, 4>(p, c.tiles, false, stream);
   } else {
-    if (max_rank <= 16) launch_down<1, 1>(p, c.tiles, stream);
-    else if (max_rank <= 32) launch_down<1, 2>(p, c.tiles, stream);
-    else launch_down<1, 4>(p, c.tiles, stream);
+    if (max_rank <= 16) launch_down<1, 1>(p, c.tiles, c.grouped, stream);
+    else if (max_rank <= 32) launch_down<1, 2>(p, c.tiles, c.grouped, stream);
+    else launch_down<1, 4>(p, c.tiles, c.grouped, stream);
   }
   if (c.row_waves == kWaves) {
     if (max_rank <= 64) launch_up_wide<false>(p, c.up_tiles, c.n_per, stream);
     else launch_up_wide<true>(p, c.up_tiles, c.n_per, stream);
   } else {
-    if (max_rank <= 32) launch_up<1>(p, c.up_tiles, c.n_per, stream);
-    else if (max_rank <= 64) launch_up<2>(p, c.up_tiles, c.n_per, stream);
-    else if (max_rank <= 128) launch_up<4>(p, c.up_tiles, c.n_per, stream);
-    else launch_up<8>(p, c.up_tiles, c.n_per, stream);
+    if (max_rank <= 32) launch_up<1>(p, c.up_tiles, c.n_per, c.grouped, stream);
+    else if (max_rank <= 64) launch_up<2>(p, c.up_tiles, c.n_per, c.grouped, stream);
+    else if (max_rank <= 128) launch_up<4>(p, c.up_tiles, c.n_per, c.grouped, stream);
+    else launch_up<8>(p, c.up_tiles, c.n_per, c.grouped, stream);
   }
   return hipGetLastError();
 }

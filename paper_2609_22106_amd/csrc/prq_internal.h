@@ -232,13 +232,14 @@ hipError_t launch_tree_attention(const TreePlan& c, const uint16_t* q, int64_t l
 
 // lora.hip.  Tiles of 16 * row_tiles rows and ranges of K a tile of the first product;
 // tiles of 16 * row_waves rows and columns a workgroup of the second; small: one launch of
-// both, `tiles` of 16 rows by slices of n_per columns.
+// both, `tiles` of 16 rows by slices of n_per columns; grouped: tiles of an adapter's rows,
+// wherever they are, not of a segment's.
 struct LoraPlan {
-  bool small = false;
+  bool small = false, grouped = false;
   int64_t tiles = 0, up_tiles = 0;
   int splits = 1, k_per = 0, row_tiles = 1, row_waves = 1, n_per = 0;
 };
-LoraPlan plan_lora(int M, int segments, int N, int K, int max_rank, int num_cus);
+LoraPlan plan_lora(int M, int segments, int adapters, int N, int K, int max_rank, int num_cus);
 size_t lora_workspace_bytes(const LoraPlan& c, int M, int max_rank);
 hipError_t launch_lora(const LoraPlan& c, const uint16_t* x, int64_t ld_x, int M, int K, const uint16_t* A,
                        const uint16_t* B, const int32_t* rank_offsets, const float* scales, int adapters,

@@ -167,17 +167,6 @@ struct Part {
   int splits, first_slot, tiles;         // parts of this request's keys; the tile's slots are
 };                                       // first_slot + tiles s
 
-// Every lane's sum over itself and the lanes before it.
-__device__ __forceinline__ int prefix_sum(int x) {
-  x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xF, 0xF, false);    // row_shr 1, 2, 4, 8
-  x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xF, 0xF, false);
-  x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xF, 0xF, false);
-  x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xF, 0xF, false);
-  x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xA, 0xF, false);    // row_bcast 15, 31
-  x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xC, 0xF, false);
-  return x;
-}
-
 // One request as a lane holds it; offsets and lengths that no table should hold are
 // clamped, so that nothing outside the buffers is reached.
 struct Request {
@@ -223,7 +212,7 @@ __device__ __forceinline__ bool find_part(const TreeArgs& p, int per_tile, Part*
     float total = 0.f;
     for (int base = 0; base < p.B; base += 64) {
       const Request y = base ? load_request(p, base + lane, per_tile) : r;
-      tiles += __builtin_amdgcn_readlane(prefix_sum(y.tiles), 63);
+      tiles += __builtin_amdgcn_readlane(dev::prefix_sum(y.tiles), 63);
       float units = static_cast<float>(y.tiles) * static_cast<float>(y.units);
       int top = y.units;
 #pragma unroll
@@ -246,7 +235,7 @@ __device__ __forceinline__ bool find_part(const TreeArgs& p, int per_tile, Part*
       for (int i = 0; i < 4; ++i) {
         const float mid = 0.5f * (low + high);
         const bool fits =
-            __builtin_amdgcn_readlane(prefix_sum(r.tiles * parts_of(r.units, 1.f / mid)), 63) <= p.slots;
+            __builtin_amdgcn_readlane(dev::prefix_sum(r.tiles * parts_of(r.units, 1.f / mid)), 63) <= p.slots;
         low = fits ? low : mid;
         high = fits ? mid : high;
       }
@@ -256,10 +245,10 @@ __device__ __forceinline__ bool find_part(const TreeArgs& p, int per_tile, Part*
   for (; base < p.B; base += 64) {
     if (base) r = load_request(p, base + lane, per_tile);
     splits = p.split ? parts_of(r.units, per) : 1;
-    sum = prefix_sum(r.tiles * splits);
+    sum = dev::prefix_sum(r.tiles * splits);
     if (p.B <= 64 && __builtin_amdgcn_readlane(sum, 63) > p.slots) {   // (not by the bounds above)
       splits = 1;
-      sum = prefix_sum(r.tiles);
+      sum = dev::prefix_sum(r.tiles);
     }
     const uint64_t past = __ballot(before + sum > x);
     if (past) {

@@ -157,3 +157,39 @@ def test_no_rows_and_refused_shapes():
         prq.prq_lora(c.x, c.adapters, c.offsets, c.of, torch.zeros(4, 4096, device="cuda"))   # B too small
     with pytest.raises(ValueError):
         prq.prq_lora(c.x, c.adapters, c.offsets, c.of, c.Y.cpu())
+
+
+@pytest.mark.parametrize("rows,of,ranks,N,K", [
+    ([1] * 64, [i * 7 % 3 for i in range(64)], [16, 8, 64], 272, 2560),            # more than 16 rows of one
+    ([1] * 64, [0] * 64, [32], 64, 6000), ([1] * 9, [1, 0, -1, 1, 5, 1, 0, -3, 1 << 30], [8, 200], 96, 264),
+    ([0, 2, 0, 3, 1, 0, 5, 1, 1, 7], [0, 1, 1, 0, 2, 0, 1, -1, 0, 2], [48, 8, 24], 512, 4104),
+    ([i % 2 for i in range(100)], [i // 2 % 4 for i in range(100)], [16, 16, 8, 40], 1040, 520),
+    ([1] * 37, [36 - i if i % 5 else -1 for i in range(37)], [8 + 8 * (i % 3) for i in range(35)], 128, 9728)])
+def test_rows_of_an_adapter_in_many_segments(rows, of, ranks, N, K):
+    say("adapters of many segments", len(rows), ranks[:4], N, K)
+    c = Case(rows, of, ranks, N, K, seed=N)
+    out = c.run()
+    c.check(out)
+    Y = c.Y.clone()
+    _prq().prq_lora(c.x, c.adapters, c.offsets, c.of, Y)
+    assert torch.equal(Y, out)
+    # a row's result does not depend on the rows beside it
+    order = torch.from_numpy(np.random.default_rng(0).permutation(out.shape[0])).cuda()
+    by_row = torch.repeat_interleave(c.of.long(), torch.tensor(rows, device="cuda"))
+    d = Case([1] * out.shape[0], [0] * out.shape[0], [8], N, K)
+    d.x, d.Y, d.adapters = c.x[order].contiguous(), c.Y[order].contiguous(), c.adapters
+    d.of = by_row[order].int().contiguous()
+    c.check(d.run()[torch.argsort(order)])
+
+
+def test_rows_in_no_segment_are_left_alone_among_many_segments():
+    c = Case([1] * 20, [0, 1] * 10, [16, 8], 64, 128)
+    want = c.run()
+    off = torch.arange(21, dtype=torch.int32, device="cuda")
+    off[:3] = 2                                                    # rows 0 and 1: nobody's
+    off[20] = 400
+    c.offsets = off
+    got = c.run()
+    assert torch.equal(got[2:], want[2:]) and bool(torch.isnan(got[:2]).all())
+    c.offsets = torch.flip(torch.arange(21, dtype=torch.int32, device="cuda"), [0]).contiguous()       # descending
+    assert bool(torch.isnan(c.run()).all())
