@@ -295,7 +295,8 @@ __device__ __forceinline__ void join_ranges(const LoraArgs& p, const Adapter& ad
     const float* tp = p.t + row_at(row) * p.max_rank + 4 * quad;
     f32x4 in[kMaxRanges];
 #pragma unroll
-    for (int s = 0; s < kMaxRanges; ++s) in[s] = *reinterpret_cast<const f32x4*>(tp + min(s, p.splits - 1) * next_range);
+    for (int s = 0; s < kMaxRanges; ++s)
+      in[s] = *reinterpret_cast<const f32x4*>(tp + min(s, p.splits - 1) * next_range);
     f32x4 sum = in[0];
 #pragma unroll
     for (int s = 1; s < kMaxRanges; ++s)
@@ -600,10 +601,12 @@ size_t lora_workspace_bytes(const LoraPlan& c, int M, int max_rank) {
 
 hipError_t launch_lora(const LoraPlan& c, const uint16_t* x, int64_t ld_x, int M, int K, const uint16_t* A,
                        const uint16_t* B, const int32_t* rank_offsets, const float* scales, int adapters,
-                       int rank_rows, int max_rank, const int32_t* offsets, const int32_t* of, int segments, int N, const float* Y,
-                       int64_t ld_y, float* out, int64_t ld_out, void* workspace, hipStream_t stream) {
+                       int rank_rows, int max_rank, const int32_t* offsets, const int32_t* of, int segments, int N,
+                       const float* Y, int64_t ld_y, float* out, int64_t ld_out, void* workspace,
+                       hipStream_t stream) {
   const LoraArgs p{x, ld_x, A, B, rank_offsets, scales, offsets, of, Y, out, ld_y, ld_out,
-                   static_cast<float*>(workspace), adapters, rank_rows, segments, M, N, K, max_rank, c.splits, c.k_per};
+                   static_cast<float*>(workspace), adapters, rank_rows, segments, M, N, K, max_rank, c.splits,
+                   c.k_per};
   if (c.small) {
     if (max_rank <= 16) launch_small<1>(p, c.tiles, c.n_per, c.grouped, stream);
     else if (max_rank <= 32) launch_small<2>(p, c.tiles, c.n_per, c.grouped, stream);
