@@ -45,6 +45,31 @@ __device__ __forceinline__ int prefix_sum(int x) {
   return x;
 }
 
+// The wave's largest value, and its sum (lane 63's, in the same order for every wave).
+template <int kCtrl, int kRows>
+__device__ __forceinline__ float moved(float old, float x) {
+  return __int_as_float(
+      __builtin_amdgcn_update_dpp(__float_as_int(old), __float_as_int(x), kCtrl, kRows, 0xF, false));
+}
+__device__ __forceinline__ float wave_max(float x) {
+  x = fmaxf(x, moved<0x111, 0xF>(x, x));
+  x = fmaxf(x, moved<0x112, 0xF>(x, x));
+  x = fmaxf(x, moved<0x114, 0xF>(x, x));
+  x = fmaxf(x, moved<0x118, 0xF>(x, x));
+  x = fmaxf(x, moved<0x142, 0xA>(x, x));
+  x = fmaxf(x, moved<0x143, 0xC>(x, x));
+  return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(x), 63));
+}
+__device__ __forceinline__ float wave_sum(float x) {
+  x += moved<0x111, 0xF>(0.f, x);
+  x += moved<0x112, 0xF>(0.f, x);
+  x += moved<0x114, 0xF>(0.f, x);
+  x += moved<0x118, 0xF>(0.f, x);
+  x += moved<0x142, 0xA>(0.f, x);
+  x += moved<0x143, 0xC>(0.f, x);
+  return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(x), 63));
+}
+
 // Segment tables on the device: segment s holds rows [offsets[s], offsets[s + 1]),
 // per_row units each, cut into tiles of per_tile units.  find_tile: the segment that
 // holds tile `t` (counted over all segments), the tile's number in it, and the

@@ -206,29 +206,23 @@ __device__ __forceinline__ bool find_part(const TreeArgs& p, int per_tile, Part*
   float per = 0.f;                       // parts a unit
   if (p.split && !p.spread && p.B == 1) {
     per = static_cast<float>(p.slots / max(r.tiles, 1)) / static_cast<float>(max(r.units, 1));
-    per = __shfl(per, 0) * 0.999f;       // rounded up by parts_of, and never past the slots
+    per = __int_as_float(__builtin_amdgcn_readfirstlane(__float_as_int(per))) * 0.999f;
+    // (rounded up by parts_of, and never past the slots)
   } else if (p.split) {
-    int tiles = 0, longest = 1;
-    float total = 0.f;
+    int tiles = 0;
+    float total = 0.f, longest = 1.f;
     for (int base = 0; base < p.B; base += 64) {
       const Request y = base ? load_request(p, base + lane, per_tile) : r;
+      const float units = static_cast<float>(y.units);
       tiles += __builtin_amdgcn_readlane(dev::prefix_sum(y.tiles), 63);
-      float units = static_cast<float>(y.tiles) * static_cast<float>(y.units);
-      int top = y.units;
-#pragma unroll
-      for (int d = 32; d > 0; d >>= 1) {
-        units += __shfl_xor(units, d);
-        top = max(top, __shfl_xor(top, d));
-      }
-      total += __shfl(units, 0);
-      longest = max(longest, __shfl(top, 0));
+      total += dev::wave_sum(static_cast<float>(y.tiles) * units);
+      longest = fmaxf(longest, dev::wave_max(units));
     }
     // total / most + tiles parts at most: `high` suffices, nothing below `low` does.  Where
     // there are tiles enough to fill the chip only what is half as long again as the mean
     // is cut.
     float low = max(total / p.slots, 1.f);
-    float high = p.slots > tiles ? max(min(total / (p.slots - tiles), static_cast<float>(longest)), low)
-                                 : static_cast<float>(longest);
+    float high = p.slots > tiles ? max(min(total / (p.slots - tiles), longest), low) : longest;
     if (p.spread)
       high = 1.5f * max(total, 1.f) / max(tiles, 1);
     else if (p.B <= 64)
@@ -559,13 +553,8 @@ __device__ __forceinline__ void join_parts(const TreeArgs& p, const Part& w, flo
   for (int c = tid >> 6; c < w.cols; c += kNarrowWaves<D>) {    // a wave a column
     const int s = tid & 63;
     const float m = s < w.splits ? weight[c * kMaxSplits + s] : kNone;
-    float top = m;
-#pragma unroll
-    for (int d = 32; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor(top, d));
-    const float a = exp2_from(m, top, 1.0f);
-    float sum = s < w.splits ? a * l[c * kMaxSplits + s] : 0.f;
-#pragma unroll
-    for (int d = 32; d > 0; d >>= 1) sum += __shfl_xor(sum, d);
+    const float top = dev::wave_max(m), a = exp2_from(m, top, 1.0f);
+    const float sum = dev::wave_sum(s < w.splits ? a * l[c * kMaxSplits + s] : 0.f);
     weight[c * kMaxSplits + s] = a;
     if (s == 0) {
       inv[c] = sum == 0.f ? 0.f : 1.0f / sum;
@@ -1005,13 +994,7 @@ __global__ __launch_bounds__(64 * kJoinWaves) void tree_join_kernel(const float*
             part_o + at(min(s0 + x * kAtOnce + lane / kPer, splits - 1)) * D + 4 * (lane % kPer));
   };
   load(0);
-  float top = ml.x;
-#pragma unroll
-  for (int d = 32; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor(top, d));
-  const float a = exp2_from(ml.x, top, 1.0f);
-  float sum = a * ml.y;
-#pragma unroll
-  for (int d = 32; d > 0; d >>= 1) sum += __shfl_xor(sum, d);
+  const float top = dev::wave_max(ml.x), a = exp2_from(ml.x, top, 1.0f), sum = dev::wave_sum(a * ml.y);
   f32x4 o = {0.f, 0.f, 0.f, 0.f};
   for (int s0 = 0; s0 < splits; s0 += kBatch * kAtOnce) {
     if (s0 > 0) load(s0);
