@@ -218,7 +218,8 @@ hipError_t launch_qk_norm_rope(const void* q, int64_t ld_q, const void* k, int64
 // tile of one request's columns and a part of its keys; whether keys are split, and if so
 // whether the tiles fill the chip as it is; the blocks of the launch.
 struct TreePlan {
-  int tile_cols = 16, step = 128;    // parts are multiples of `step` keys
+  int tile_cols = 16, waves = 8;     // of a workgroup of 16 columns
+  int step = 128;                    // parts are multiples of `step` keys
   bool split = false, spread = false;
   int64_t slots = 0, blocks = 0;
 };

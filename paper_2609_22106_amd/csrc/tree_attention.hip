@@ -57,8 +57,6 @@ namespace {
 using dev::f32x4;
 using dev::u32x4v;
 
-template <int D>
-constexpr int kNarrowWaves = D <= 128 ? 8 : 4;                       // of the narrow one (by its registers)
 constexpr int kMaxSplits = 64;
 constexpr float kSlack = 8.0f;           // log2 a score may pass the maximum by before it is renewed
 constexpr float kNone = -INFINITY;
@@ -506,12 +504,12 @@ __device__ __forceinline__ float2 get(const void* at) {
 template <int D>
 constexpr int kJoinCols = D <= 128 ? 4 : 1;                  // columns at a time
 constexpr int kJoinWeights = 16 * (2 * kMaxSplits + 1);
-template <int D>
-constexpr int kJoinFloats = kJoinWeights + 2 * kJoinCols<D> * 64 * kNarrowWaves<D>;
+template <int D, int kN>
+constexpr int kJoinFloats = kJoinWeights + 2 * kJoinCols<D> * 64 * kN;
 
-template <int D>
+template <int D, int kN>
 __device__ __forceinline__ void join_parts(const TreeArgs& p, const Part& w, float* sh) {
-  constexpr int kThreads = 64 * kNarrowWaves<D>, kCols = kJoinCols<D>;
+  constexpr int kThreads = 64 * kN, kCols = kJoinCols<D>;
   __shared__ int sh_last;
   const int tid = static_cast<int>(threadIdx.x);
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");           // what this wave has put is there
@@ -550,7 +548,7 @@ __device__ __forceinline__ void join_parts(const TreeArgs& p, const Part& w, flo
     l[c * kMaxSplits + s] = ml.y;
   }
   __syncthreads();
-  for (int c = tid >> 6; c < w.cols; c += kNarrowWaves<D>) {    // a wave a column
+  for (int c = tid >> 6; c < w.cols; c += kN) {         // a wave a column
     const int s = tid & 63;
     const float m = s < w.splits ? weight[c * kMaxSplits + s] : kNone;
     const float top = dev::wave_max(m), a = exp2_from(m, top, 1.0f);
@@ -599,11 +597,11 @@ __device__ __forceinline__ void join_parts(const TreeArgs& p, const Part& w, flo
 
 // Up to 16 query columns: the waves take every kN-th 32 keys each, straight into
 // registers, the next ones under way, and join through LDS at the end.
-template <int D>
-__global__ __launch_bounds__(64 * kNarrowWaves<D>, D <= 128 ? 2 : 1) void tree_attention_kernel(const TreeArgs p) {
-  constexpr int kV = D / 16, kPitch = D + 4, kN = kNarrowWaves<D>, kThreads = 64 * kN, kStride = 32 * kN;
+template <int D, int kN>
+__global__ __launch_bounds__(64 * kN, D <= 128 ? 2 : 1) void tree_attention_kernel(const TreeArgs p) {
+  constexpr int kV = D / 16, kPitch = D + 4, kThreads = 64 * kN, kStride = 32 * kN;
   __shared__ __align__(16) float sh_o[kN][16][kPitch];
-  static_assert(kN * 16 * kPitch >= kJoinFloats<D>, "the join's LDS");
+  static_assert(kN * 16 * kPitch >= (kJoinFloats<D, kN>), "the join's LDS");
   __shared__ float sh_m[kN][16], sh_l[kN][16];
   Part w;
   if (!find_part(p, 16, &w)) return;
@@ -692,7 +690,7 @@ __global__ __launch_bounds__(64 * kNarrowWaves<D>, D <= 128 ? 2 : 1) void tree_a
       if (d == 0) put(p.part_ml + part, top * p.scale, sum);
     }
   }
-  if (w.splits > 1) join_parts<D>(p, w, &sh_o[0][0][0]);
+  if (w.splits > 1) join_parts<D, kN>(p, w, &sh_o[0][0][0]);
 }
 
 // Copies 16 bytes a lane straight to LDS: from src (the same for the wave) + the lane's
@@ -1019,10 +1017,13 @@ __global__ __launch_bounds__(64 * kJoinWaves) void tree_join_kernel(const float*
 }
 
 template <int D>
-void launch(const TreeArgs& p, int tile_cols, int64_t blocks, hipStream_t stream) {
+void launch(const TreeArgs& p, int tile_cols, int waves, int64_t blocks, hipStream_t stream) {
   const dim3 grid(static_cast<unsigned>(blocks));
-  if (tile_cols == 16)
-    tree_attention_kernel<D><<<grid, 64 * kNarrowWaves<D>, 0, stream>>>(p);
+  if (tile_cols == 16 && waves == 4)
+    tree_attention_kernel<D, 4><<<grid, 256, 0, stream>>>(p);
+  else if (tile_cols == 16) {
+    if constexpr (D <= 128) tree_attention_kernel<D, 8><<<grid, 512, 0, stream>>>(p);
+  }
   else if (tile_cols == 64)
     tree_attention_wide_kernel<D, 1, 4><<<grid, 256, 0, stream>>>(p);
   else if constexpr (D <= 128) {
@@ -1048,7 +1049,6 @@ TreePlan plan_tree_attention(int M, int B, int Hq, int Hk, int D, int max_kv_len
   const int64_t per = (M * G + used - 1) / used;        // query columns of a mean request
   // (188 columns a request over 32 k tokens, heads of 128: 256 / 128 columns a workgroup 247 / 258 us)
   c.tile_cols = per <= 16 ? 16 : per <= 64 || D > 128 ? 64 : per <= 128 ? 128 : 256;
-  c.step = c.tile_cols == 16 ? 32 * (D <= 128 ? kNarrowWaves<128> : kNarrowWaves<256>) : 128;
   const int64_t tiles = most_tiles(M, B, G, c.tile_cols);
   // Slots a kv head: as many as the chip holds workgroups at once (by their registers and
   // LDS), but no more than there are parts; where the tiles alone are that many, some for
@@ -1057,8 +1057,16 @@ TreePlan plan_tree_attention(int M, int B, int Hq, int Hk, int D, int max_kv_len
   // trees of up to 13 nodes over 6 x 8 k tokens)
   const int per_cu = c.tile_cols == 16 || c.tile_cols == 256 || D > 128 ? 1 : 2;
   const int64_t at_once = std::max<int64_t>(static_cast<int64_t>(per_cu) * num_cus / Hk, 1);
-  const int64_t parts = tiles * std::min<int64_t>(kMaxSplits, std::max((max_kv_len + c.step - 1) / c.step, 1));
   c.spread = tiles >= at_once;
+  // Waves of a narrow workgroup: eight while a request has several of them, or is long; four,
+  // two workgroups a CU, where short requests alone fill the chip and one's start and end hide
+  // behind another's loads.  us, eight / four, 8 kv heads of 128, requests of up to as many tokens:
+  // 1 x 4097 13.6 / 15.7, 16 x 1000 18.5 / 19.7, 32 x 300 19.7 / 12.1, 128 x 500 56.7 / 45.8,
+  // 64 x 2000 83 / 80, 40 x 4000 112 / 121; 12 heads of 64: 50 x 1000 30.7 / 26.3, 50 x 2000
+  // 55 / 54, 50 x 3000 74 / 77.  (Heads of 256 leave registers for four.)
+  c.waves = D > 128 || (c.spread && max_kv_len <= 2048) ? 4 : 8;
+  c.step = c.tile_cols == 16 ? 32 * c.waves : 128;
+  const int64_t parts = tiles * std::min<int64_t>(kMaxSplits, std::max((max_kv_len + c.step - 1) / c.step, 1));
   c.slots = c.spread ? tiles + (2 * tiles + 2) / 3 : std::max(tiles, std::min(at_once, parts));
   c.split = c.slots > tiles && tiles < 4 * at_once &&
             c.slots * Hk * static_cast<int64_t>(sizeof(uint32_t)) <= static_cast<int64_t>(kWorkspaceStateBytes);
@@ -1091,9 +1099,9 @@ hipError_t launch_tree_attention(const TreePlan& c, const uint16_t* q, int64_t l
                    max_keys, cached, offsets, mask, ld_mask, mask ? mask_wide : 0, size, kSlack / size,
                    std::signbit(scale) ? 0x80008000u : 0u, out, lse, part_o, part_ml, arrived, joins, M, B, Hq, Hk,
                    Hq / Hk, static_cast<int>(c.slots), c.step, c.split, c.spread};
-  if (D == 64) launch<64>(p, c.tile_cols, c.blocks, stream);
-  else if (D == 128) launch<128>(p, c.tile_cols, c.blocks, stream);
-  else launch<256>(p, c.tile_cols, c.blocks, stream);
+  if (D == 64) launch<64>(p, c.tile_cols, c.waves, c.blocks, stream);
+  else if (D == 128) launch<128>(p, c.tile_cols, c.waves, c.blocks, stream);
+  else launch<256>(p, c.tile_cols, c.waves, c.blocks, stream);
   return hipGetLastError();
 }
 
