@@ -99,6 +99,11 @@ __device__ __forceinline__ float max_of(float a, float b, float c) { return max_
 
 __device__ __forceinline__ bool finite_bf16(uint32_t b) { return (b & 0x7F80u) != 0x7F80u; }
 
+// The sign bits of the halves that are infinite or NaN.
+__device__ __forceinline__ uint32_t odd_halves(uint32_t two) {
+  return ((two & 0x7F807F80u) + 0x00800080u) & 0x80008000u;
+}
+
 // K and V of two 16-key blocks, as a lane (g = l / 16, r = l % 16) holds them.
 template <int D>
 struct Tile {
@@ -118,6 +123,18 @@ struct Tile {
     for (int e = 0; e < 4; ++e)
       out[e] = __builtin_amdgcn_perm(values[2 * e + 1][x >> 1], values[2 * e][x >> 1],
                                      x & 1 ? 0x07060302u : 0x05040100u);
+    return out;
+  }
+  // Whether a V among the keys `ok` is infinite or NaN.
+  __device__ __forceinline__ uint32_t odd(uint32_t ok, const u32x4v&) const {
+    uint32_t out = 0;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      uint32_t row = 0;
+#pragma unroll
+      for (int x = 0; x < kWords; ++x) row |= odd_halves(values[e][x]);
+      out |= ok >> e & 1 ? row : 0u;
+    }
     return out;
   }
   static __device__ __forceinline__ int dim(int x, int m) { return D / 16 * m + x; }
@@ -285,6 +302,12 @@ __device__ __forceinline__ int64_t block_base(const TreeArgs& p, int h, int page
          ((static_cast<int64_t>(h) << p.page_shift) + (key & ((1 << p.page_shift) - 1))) * D;
 }
 
+// The page of the block at `key`, -1 where there is none.
+__device__ __forceinline__ int page_entry(const TreeArgs& p, const Part& w, int key) {
+  const int page = key < w.hi ? p.pages[w.segment * p.ld_pages + (key >> p.page_shift)] : -1;
+  return page < p.num_pages ? page : -1;
+}
+
 // A wave's T tiles of 16 query columns: operands, running maximum (of q . k, the same
 // in the four lanes of a column), sum (a lane's own keys) and output.
 template <int D, int T>
@@ -312,10 +335,11 @@ struct Wave {
     }
   }
 
-  // A step: 32 keys from k0 on, blocks 0 and 1 of them on pages page[] of the pool (-1: none).
+  // A step: 32 keys from k0 on, blocks 0 and 1 of them on pages of the pool (page[]; -1: on none).
   // kPlain: every row sees all of them.
   // `src`: where the operands are, k(b, ..) block b's keys, v(x) V^T's for both blocks and the
-  // dims dim(x, 0 .. 15).  A lane's keys: e is 16 (e / 4) + 4 g + e % 4.
+  // dims dim(x, 0 .. 15), odd(ok, keep) whether V holds an infinity or a NaN in the keys that
+  // `ok` names (`keep`: the same as masks of v's words).  A lane's keys: e is 16 (e / 4) + 4 g + e % 4.
   struct Scores {
     float s[T][8];
     uint32_t seen[T];                    // (not plain) bit e
@@ -415,31 +439,40 @@ struct Wave {
   __device__ __forceinline__ void absorb(const TreeArgs& p, const Part& w, const Source& src, int k0,
                                          const int (&page)[2], const Scores* in, const u32x4v (&pw)[T]) {
     const int lane = static_cast<int>(threadIdx.x) & 63, r = lane & 15, g = lane >> 4;
-    bool odd_v = false;                  // some key's V holds an infinity or a NaN
+    // What no row may see must not reach the product either (0 x NaN): V past the keys becomes
+    // 0, and if there are infinities and NaN, those are taken out and added below for the rows
+    // that do see them.
+    u32x4v keep;
+    bool odd_v = false;
+    if constexpr (!kPlain) {
+      uint32_t ok = 0;
+#pragma unroll
+      for (int e = 0; e < 8; ++e)
+        ok |= static_cast<uint32_t>(k0 + 16 * (e >> 2) + 4 * g + (e & 3) < w.hi && page[e >> 2] >= 0) << e;
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        keep[e] = (ok >> 2 * e & 1 ? 0xFFFFu : 0u) | (ok >> (2 * e + 1) & 1 ? 0xFFFF0000u : 0u);
+      odd_v = __any(src.odd(ok, keep) != 0);
+    }
 #pragma unroll
     for (int x = 0; x < kV; ++x) {
       u32x4v a = src.v(x);
-      // What no row may see must not reach the product either (0 x NaN): V past the
-      // keys becomes 0, and infinities and NaN are taken out and added below for the
-      // rows that do see them.
       if constexpr (!kPlain) {
+        a &= keep;
+        if (odd_v)
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          const bool ok = k0 + 16 * (e >> 2) + 4 * g + (e & 3) < w.hi && page[e >> 2] >= 0;
-          const bool odd = ok && !finite_bf16(a[e >> 1] >> (16 * (e & 1)));
-          if (!ok || odd) a[e >> 1] &= e & 1 ? 0xFFFFu : 0xFFFF0000u;
-          odd_v |= odd;
-        }
+          for (int e = 0; e < 4; ++e) a[e] &= ~((odd_halves(a[e]) >> 15) * 0xFFFFu);
       }
 #pragma unroll
       for (int t = 0; t < T; ++t) o[t][x] = dev::mfma_bf16(a, pw[t], o[t][x]);
     }
-    if (!kPlain && __any(odd_v)) {            // rare: the words taken out above, row by row
+    if (!kPlain && odd_v) {                   // rare: the values taken out above, row by row
 #pragma unroll
       for (int b = 0; b < 2; ++b) {
-        const int64_t base = block_base<D>(p, w.h, page[b], k0 + 16 * b);
+        const int at = page_entry(p, w, k0 + 16 * b);
+        const int64_t base = block_base<D>(p, w.h, at, k0 + 16 * b);
         for (int kk = 0; kk < 16; ++kk) {
-          if (k0 + 16 * b + kk >= w.hi || page[b] < 0) break;
+          if (k0 + 16 * b + kk >= w.hi || at < 0) break;
           const uint16_t* vp = p.V + base + kk * D;
           const int from = 16 * (kk >> 2) + r;
 #pragma unroll
@@ -475,12 +508,6 @@ struct Wave {
     absorb<kPlain>(p, w, src, k0, page, &s, pw);
   }
 };
-
-// The page of the block at `key`, -1 where there is none.
-__device__ __forceinline__ int page_entry(const TreeArgs& p, const Part& w, int key) {
-  const int page = key < w.hi ? p.pages[w.segment * p.ld_pages + (key >> p.page_shift)] : -1;
-  return page < p.num_pages ? page : -1;
-}
 
 // Values that another workgroup reads in this launch, perhaps on another XCD with an L2 of its
 // own: device-scope accesses, 8 bytes each.
@@ -741,6 +768,16 @@ struct Staged {
     }
     return out;
   }
+  __device__ __forceinline__ uint32_t odd(uint32_t, const u32x4v& keep) const {
+    uint32_t out = 0;
+#pragma unroll
+    for (int x = 0; x < D / 16; ++x) {
+      const u32x4v a = v(x) & keep;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) out |= odd_halves(a[e]);
+    }
+    return out;
+  }
   static __device__ __forceinline__ int dim(int x, int m) { return 16 * x + m; }
 };
 
@@ -802,11 +839,16 @@ __global__ __launch_bounds__(64 * kN, D <= 128 ? 2 : 1) void tree_attention_wide
   // (Stages past the last are copied from the pool's first page, so that as many are always
   // under way.)
   int64_t entry = 0;                     // lane b: byte offset of block b (of 64)
+  uint64_t there = 0, before = 0;        // which of them are on a page, and of the 64 before them
+  int looked_up = 0;                     // the stage of the first
   uint32_t load_k = 0, load_v = kKeyBuffers * 2 * kStage;    // of the next stage to load
   auto look_up = [&](int stage) {        // before the load of a stage that starts 64 blocks
     if (stage % 32) return;
     const int key = w.lo + kKeys * stage + 16 * lane, page = page_entry(p, w, key);
     entry = 2 * block_base<D>(p, w.h, page, key);
+    before = there;
+    there = __ballot(page >= 0);
+    looked_up = stage;
     if (__any(key < w.hi && page < 0)) plain = min(plain, stage);
   };
   uint32_t of[kCopies];                  // a lane's place in its block
@@ -903,7 +945,8 @@ __global__ __launch_bounds__(64 * kN, D <= 128 ? 2 : 1) void tree_attention_wide
     for (int stage = plain; stage < stages; ++stage) {
       if (stage > plain + 1 - (plain & 1) || plain == 0) enter(stage);
       const int k0 = w.lo + kKeys * stage;
-      const int page[2] = {page_entry(p, w, k0), page_entry(p, w, k0 + 16)};
+      const uint64_t on = (stage >= looked_up ? there : before) >> (2 * stage & 63);
+      const int page[2] = {on & 1 ? 0 : -1, on & 2 ? 0 : -1};
       q.template step<false>(p, w, Staged<D>{read_k + k_lane, read_v + v_lane}, k0, page);
       read_k = keys_after(read_k);
       read_v = values_after(read_v);
