@@ -367,3 +367,35 @@ def test_long_parts(rows, D, page):
         assert bool((err <= 2.0 ** -8 * want.abs() + (2.0 ** -8 + 2.0 ** -18 * S) * spread).all()), (b, float(err.max()))
         err = (rows_of(lse[r])[..., 0] - want_l).abs()
         assert bool((err <= 2.0 ** -18 * S[..., 0] + 2.0 ** -22 * want_l.abs()).all()), (b, float(err.max()))
+
+
+@pytest.mark.parametrize("rows,D", [(3, 128), (10, 64), (20, 64), (20, 128), (24, 256), (40, 64), (40, 128)])
+def test_infinities_and_nan_among_many_columns(rows, D):
+    """NaN and infinities in an own token that few rows see, in a cached one that all see, and on a
+    page that is missing."""
+    Hq, Hk = 8, 2
+    c = Case([(75, rows), (200, rows)], Hq, Hk, D, 16, mask="any", seed=rows)
+    c.mask[:, 2] = False
+    c.mask[1, 2] = c.mask[rows - 1, 2] = True
+    c.check(*c.run())
+    clean = c.run()
+    V, slot = c.cache.V, 75 + 2
+    page, at_ = c.table[0, slot // 16].item(), slot % 16
+    V[page, :, at_, 3], V[page, :, at_, D - 1] = float("-inf"), float("nan")
+    out, lse = c.run()
+    sees = torch.zeros(2 * rows, dtype=torch.bool, device="cuda")
+    sees[[1, rows - 1]] = True
+    assert bool((out[sees][..., 3] == float("-inf")).all()) and bool(torch.isnan(out[sees][..., D - 1]).all())
+    assert torch.equal(out[~sees], clean[0][~sees]) and torch.equal(lse, clean[1])
+    between = torch.ones(D, dtype=torch.bool, device="cuda")
+    between[[3, D - 1]] = False
+    assert bool((out[sees][..., between].float() - clean[0][sees][..., between].float()).abs().max() < 2.0 ** -5)
+    # an infinity that every row sees, among the cached tokens: all of the request's rows have it
+    V[c.table[1, 100 // 16].item(), :, 100 % 16, 5] = float("inf")
+    out, _ = c.run()
+    assert bool((out[rows:, :, 5] == float("inf")).all())
+    assert torch.equal(out[:rows][~sees[:rows]], clean[0][:rows][~sees[:rows]])
+    # on a page that is missing from the table, nothing of it is left
+    c.table[1, 100 // 16] = -1
+    out, _ = c.run()
+    assert bool(torch.isfinite(out[rows:]).all())
