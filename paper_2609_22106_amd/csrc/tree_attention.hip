@@ -18,7 +18,7 @@
 // the next ones under way, and join through LDS.  V's operand needs 8 keys of one column: a
 // lane group loads whole rows of its 8 keys, 16 lanes a row, and pairs up halves of registers
 // (32 v_perm per 32 x 128 tile).  32 sequences of up to 2176 tokens, 8 kv heads of 128:
-// 46 us, 206 MB of K and V at 4.5 TB/s; one token over 4097: 14 us, the latency of the
+// 45 us, 206 MB of K and V at 4.6 TB/s; one token over 4097: 13.3 us, the latency of the
 // loads, the arrival and the join one after another.
 //
 // More columns (wide): they are dealt to the waves, one or two tiles of 16 each, and 32 keys
@@ -26,7 +26,7 @@
 // back transposed.  Trees of up to 64 nodes over 8 x 32 k tokens (377 rows, 204 k keys): straight
 // from memory 714 us, through LDS with v_perm 272, transposed reads 258; a stage's scores
 // beside the exponentials of the one before and LDS read ahead, 8 waves for more than 128
-// columns, those dealt evenly to the SIMDs, a barrier every two stages, 227: 700 TFLOP/s, the
+// columns, those dealt evenly to the SIMDs, a barrier every two stages, 230: 690 TFLOP/s, the
 // matrix units 40% of the time, 9 us of it the join's.  What is left: the parts, unequal by 17%,
 // and a SIMD's two waves, in step more often than in turn.
 //
@@ -40,7 +40,7 @@
 // parts as the chip holds at once, dealt to the requests by their lengths, and the partial
 // (m, l, O) joined in a fixed order: by the last part of a tile to arrive where there are few
 // columns, by a second kernel where they are many (trees of up to 13 nodes over 6 x 8 k tokens
-// 50 us the first way, 24.5 the second, 22.7 by now: one workgroup is then slow to read all parts
+// 50 us the first way, 24.5 the second, 22.5 by now: one workgroup is then slow to read all parts
 // of a tile).
 #include <hip/hip_runtime.h>
 
