@@ -579,9 +579,12 @@ LoraPlan plan_lora(int M, int segments, int adapters, int N, int K, int max_rank
   c.row_waves = mean >= 32 ? kWaves : 1;
   c.tiles = most_tiles(M, segments, 1, 16 * c.row_tiles);
   c.up_tiles = most_tiles(M, segments, 1, 16 * c.row_waves);
-  // Ranges of K until there are four workgroups a CU, two steps a wave at least.
+  // Ranges of K until there are four workgroups a CU, or the two that its registers hold of 32 rows
+  // and more than 32 ranks (4 / 2 a CU: 8192 rows, K = 2560, N = 9728, rank 64 138.5 / 135.3 us, 4096
+  // rows, K = 9728, N = 2560, rank 64 59.0 / 57.5, rank 32 50.7 / 53.5), two steps a wave at least.
   const int steps = (K + 63) / 64;
-  const int64_t want = (4 * static_cast<int64_t>(num_cus) + c.tiles - 1) / c.tiles;
+  const int64_t at_once = (c.row_tiles == 2 && max_rank > 32 ? 2 : 4) * static_cast<int64_t>(num_cus);
+  const int64_t want = (at_once + c.tiles - 1) / c.tiles;
   const int64_t most = std::min(std::max(1, steps / (2 * kWaves)), kMaxRanges);
   const int splits = static_cast<int>(std::max<int64_t>(1, std::min(want, most)));
   if (c.grouped) c.tiles = c.up_tiles = groups;        // (the workspace is the same either way)
