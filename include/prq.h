@@ -498,7 +498,8 @@ int prq_qk_norm_rope(const void* q, int64_t ld_q, const void* k, int64_t ld_k, c
  *   page_table [B] rows of pages_wide int32, ld_pages apart; tokens beyond
  *              pages_wide * page_size, and tokens on a page outside the pool, are
  *              not seen
- *   cached_lens [B], q_offsets [B + 1] int32; rows of no request are not computed
+ *   cached_lens [B], q_offsets [B + 1] int32; rows of no request are not computed,
+ *              and their out and lse are left alone
  *   max_kv_len the most tokens (cached and own) a request is expected to have: it
  *              sizes the split over workgroups.  A longer request is computed too,
  *              more slowly

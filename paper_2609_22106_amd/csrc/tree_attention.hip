@@ -80,7 +80,8 @@ struct TreeArgs {
   float *lse, *part_o;
   float2* part_ml;
   uint32_t* arrived;                     // narrow: parts done, of every tile that has several (0 between calls)
-  int4* joins;                           // wide, of every row: its request's first row, first slot, tiles, parts
+  int4* joins;                           // wide, of every row: its request's first row, first slot, tiles, and
+                                         // parts (8 bits) beside its number
   int M, B, Hq, Hk, G, slots, step;      // a part of the keys is a multiple of `step`
   bool split, spread;                    // keys may be split; there are enough tiles as it is
 };
@@ -814,7 +815,7 @@ __global__ __launch_bounds__(64 * kN, D <= 128 ? 2 : 1) void tree_attention_wide
   if (!find_part(p, 16 * T * kN, &w)) return;
   if (p.split && w.h == 0 && static_cast<int>(blockIdx.x) / p.Hk == w.first_slot)      // for the join
     for (int row = w.c0 / p.G + static_cast<int>(threadIdx.x); row * p.G < w.c0 + w.cols; row += kThreads)
-      p.joins[w.first + row] = {w.first, w.first_slot - w.c0 / (16 * T * kN), w.tiles, w.splits};
+      p.joins[w.first + row] = {w.first, w.first_slot - w.c0 / (16 * T * kN), w.tiles, w.segment << 8 | w.splits};
   const int lane = static_cast<int>(threadIdx.x) & 63, r = lane & 15, g = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x) >> 6);
   const uint32_t sh_at = static_cast<uint32_t>(
@@ -999,14 +1000,17 @@ __global__ __launch_bounds__(64 * kN, D <= 128 ? 2 : 1) void tree_attention_wide
 }
 
 // After the wide kernel: the parts' (m, l, O) of one row and head, a wave each; nothing
-// where a workgroup had all of the row's keys.  (What `joins` holds for a row of no request
-// may be anything: it is clamped to the workspace.)
+// where a workgroup had all of the row's keys.  What `joins` holds for a row of no request is
+// an earlier call's, or anything: an entry counts if the request that it names has the row
+// (of such a row it is this call's); the parts' places are clamped to the workspace, so
+// that their loads need not wait to know.
 constexpr int kJoinWaves = 4;
 template <int D>
 __global__ __launch_bounds__(64 * kJoinWaves) void tree_join_kernel(const float* __restrict__ part_o,
                                                              const float2* __restrict__ part_ml,
-                                                             const int4* __restrict__ joins, int64_t heads, int Hq,
-                                                             int Hk, int tile_cols, int slots,
+                                                             const int4* __restrict__ joins,
+                                                             const int32_t* __restrict__ offsets, int B,
+                                                             int64_t heads, int Hq, int Hk, int tile_cols, int slots,
                                                              uint16_t* __restrict__ out, float* __restrict__ lse) {
   constexpr int kPer = D / 4, kAtOnce = 64 / kPer;     // lanes a part, parts a load
   constexpr int kBatch = 8;                            // loads under way
@@ -1015,8 +1019,9 @@ __global__ __launch_bounds__(64 * kJoinWaves) void tree_join_kernel(const float*
   if (head >= heads) return;
   const int64_t row = head / Hq;
   const int4 j = joins[row];
-  const int splits = __builtin_amdgcn_readfirstlane(min(j.w, kMaxSplits));
-  if (splits <= 1) return;
+  const int splits = __builtin_amdgcn_readfirstlane(j.w & 255), segment = __builtin_amdgcn_readfirstlane(j.w >> 8);
+  if (splits <= 1 || splits > kMaxSplits || segment < 0 || segment >= B) return;
+  const int first = offsets[segment], end = offsets[segment + 1];
   const int G = Hq / Hk, q = static_cast<int>(head - row * Hq);
   const uint32_t c = static_cast<uint32_t>((row - j.x) * G + q % G);
   const int col = static_cast<int>(c % tile_cols), tile = static_cast<int>(c / tile_cols);
@@ -1035,6 +1040,7 @@ __global__ __launch_bounds__(64 * kJoinWaves) void tree_join_kernel(const float*
             part_o + at(min(s0 + x * kAtOnce + lane / kPer, splits - 1)) * D + 4 * (lane % kPer));
   };
   load(0);
+  if (row < first || row >= end) return;
   const float top = dev::wave_max(ml.x), a = exp2_from(ml.x, top, 1.0f), sum = dev::wave_sum(a * ml.y);
   f32x4 o = {0.f, 0.f, 0.f, 0.f};
   for (int s0 = 0; s0 < splits; s0 += kBatch * kAtOnce) {
@@ -1078,8 +1084,8 @@ void launch(const TreeArgs& p, int tile_cols, int waves, int64_t blocks, hipStre
   if (p.split && tile_cols > 16) {
     const int64_t heads = static_cast<int64_t>(p.M) * p.Hq;
     tree_join_kernel<D><<<dim3(static_cast<unsigned>((heads + kJoinWaves - 1) / kJoinWaves)), 64 * kJoinWaves, 0,
-                          stream>>>(p.part_o, p.part_ml, p.joins, heads, p.Hq, p.Hk, tile_cols, p.slots, p.out,
-                                    p.lse);
+                          stream>>>(p.part_o, p.part_ml, p.joins, p.offsets, p.B, heads, p.Hq, p.Hk, tile_cols,
+                                    p.slots, p.out, p.lse);
   }
 }
 

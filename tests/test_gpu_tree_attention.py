@@ -399,3 +399,35 @@ def test_infinities_and_nan_among_many_columns(rows, D):
     c.table[1, 100 // 16] = -1
     out, _ = c.run()
     assert bool(torch.isfinite(out[rows:]).all())
+
+
+@pytest.mark.parametrize("rows,D", [(1, 64), (4, 128), (5, 64), (9, 256), (10, 64), (10, 128), (20, 64), (40, 128)])
+def test_rows_of_no_request_are_left_alone(rows, D):
+    """16, 64, 128 and 256 columns a workgroup, the keys split: rows before the first offset and from
+    the last one on keep what out and lse held, whatever an earlier call or a program left in the
+    workspace behind its head."""
+    prq = _prq()
+    c = Case([(600, rows), (900, rows), (700, rows)], 8, 2, D, 16, seed=rows)
+    M = 3 * rows
+    ws = torch.zeros(64 << 20, dtype=torch.uint8, device="cuda")
+    assert prq.prq_tree_attention_workspace_bytes(M, 1, 8, 2, D, 940) > 16384
+    outs = [torch.full(s, 7.0, dtype=t, device="cuda") for s, t in (((M, 8, D), BF16), ((M, 8), torch.float32))]
+
+    def one(b, out, lse):                                            # request b's rows alone
+        return prq.prq_tree_attention(c.q, c.cache, c.table[b:b + 1], c.cached[b:b + 1],
+                                      c.offsets[b:b + 2].contiguous(), c.scale, tree_mask=c.mask, max_kv_len=940,
+                                      out=out, lse=lse, workspace=ws)
+    for fill in (0, 1, 255):
+        say("rows of no request", rows, D, fill)
+        ws[16384:] = fill
+        for t in outs:
+            t.fill_(7.0)
+        one(1, *outs)
+        assert bool((outs[0][:rows] == 7).all()) and bool((outs[0][2 * rows:] == 7).all())
+        assert bool((outs[1][:rows] == 7).all()) and bool((outs[1][2 * rows:] == 7).all())
+        mine = [t[rows:2 * rows].clone() for t in outs]
+        one(2, *outs)                                                # (in the parts that the call before has left)
+        one(0, *outs)
+        assert torch.equal(outs[0][rows:2 * rows], mine[0]) and torch.equal(outs[1][rows:2 * rows], mine[1])
+        c.check(*outs)
+        assert not ws[:16384].any()
