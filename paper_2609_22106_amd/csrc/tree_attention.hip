@@ -236,11 +236,11 @@ __device__ __forceinline__ bool find_part(const TreeArgs& p, int per_tile, Part*
     }
     // total / most + tiles parts at most: `high` suffices, nothing below `low` does.  Where
     // there are tiles enough to fill the chip only what is half as long again as the mean
-    // is cut.
+    // is cut (and no more than there are slots for: offsets that rise and fall count rows twice).
     float low = max(total / p.slots, 1.f);
     float high = p.slots > tiles ? max(min(total / (p.slots - tiles), longest), low) : longest;
     if (p.spread)
-      high = 1.5f * max(total, 1.f) / max(tiles, 1);
+      high = max(1.5f * max(total, 1.f) / max(tiles, 1), total / max(p.slots - tiles, 1));
     else if (p.B <= 64)
       for (int i = 0; i < 4; ++i) {
         const float mid = 0.5f * (low + high);

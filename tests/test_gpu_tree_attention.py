@@ -431,3 +431,34 @@ def test_rows_of_no_request_are_left_alone(rows, D):
         assert torch.equal(outs[0][rows:2 * rows], mine[0]) and torch.equal(outs[1][rows:2 * rows], mine[1])
         c.check(*outs)
         assert not ws[:16384].any()
+
+
+def test_offsets_that_rise_and_fall_leave_the_workspace_ready():
+    """More than 64 requests, rows counted twice: more tiles and parts than the launch was planned for.
+    Every part of a tile that is begun has its workgroup all the same, so the state head is zero again,
+    and a call with a table in order is as on a workspace of its own."""
+    prq = _prq()
+    M, Hq, Hk, D, page, L = 70, 32, 8, 64, 256, 3840
+    g = torch.Generator(device="cuda").manual_seed(1)
+    K, V = (torch.randn(L // page + 1, Hk, page, D, generator=g, device="cuda").to(BF16) for _ in range(2))
+    q = torch.randn(M, Hq, D, generator=g, device="cuda").to(BF16)
+    offsets = torch.tensor([0, M] + list(range(M - 1)), dtype=torch.int32, device="cuda")
+    B = len(offsets) - 1
+    pages = torch.arange(L // page + 1, dtype=torch.int32, device="cuda").repeat(B, 1)
+    # the first request has all rows and no cached tokens, 54 of those with a row have many
+    cached = torch.tensor([0, 0] + [L - 1] * 54 + [0] * (B - 56), dtype=torch.int32, device="cuda")
+    need = prq.prq_tree_attention_workspace_bytes(M, B, Hq, Hk, D, L)
+    assert need > 16384
+
+    def call(offsets, ws):
+        return prq.prq_tree_attention(q, prq.PagedKV(K, V), pages, cached, offsets, D ** -0.5, max_kv_len=L,
+                                      workspace=ws)
+    ws = torch.zeros(need, dtype=torch.uint8, device="cuda")
+    say("offsets that rise and fall")
+    out, lse = call(offsets, ws)
+    assert bool(torch.isfinite(out).all()) and bool(torch.isfinite(lse).all())
+    assert not ws[:16384].any()
+    in_order = torch.arange(B + 1, dtype=torch.int32, device="cuda")
+    got, want = call(in_order, ws), call(in_order, torch.zeros(need, dtype=torch.uint8, device="cuda"))
+    assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+    assert not ws[:16384].any()
