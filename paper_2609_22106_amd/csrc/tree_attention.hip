@@ -1115,7 +1115,8 @@ TreePlan plan_tree_attention(int M, int B, int Hq, int Hk, int D, int max_kv_len
   // 55 / 54, 50 x 3000 74 / 77.  (Heads of 256 leave registers for four.)
   c.waves = D > 128 || (c.spread && max_kv_len <= 2048) ? 4 : 8;
   c.step = c.tile_cols == 16 ? 32 * c.waves : 128;
-  const int64_t parts = tiles * std::min<int64_t>(kMaxSplits, std::max((max_kv_len + c.step - 1) / c.step, 1));
+  const int64_t steps = (static_cast<int64_t>(max_kv_len) + c.step - 1) / c.step;
+  const int64_t parts = tiles * std::min<int64_t>(kMaxSplits, std::max<int64_t>(steps, 1));
   c.slots = c.spread ? tiles + (2 * tiles + 2) / 3 : std::max(tiles, std::min(at_once, parts));
   c.split = c.slots > tiles && tiles < 4 * at_once &&
             c.slots * Hk * static_cast<int64_t>(sizeof(uint32_t)) <= static_cast<int64_t>(kWorkspaceStateBytes);

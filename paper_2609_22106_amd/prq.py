@@ -626,6 +626,7 @@ def prq_grouped_gemm(Aq, Asc, group_offsets, W, Y=None, workspace=None, variant=
 # --------------------------------------------------------- attention block ---
 _BF16, _I64, _BOOL = torch.bfloat16, torch.int64, torch.bool
 _ROPE_IN = (_F32, _BF16)
+_I32_MAX = (1 << 31) - 1
 
 
 class PagedKV:
@@ -781,7 +782,7 @@ def prq_qk_norm_rope(q, k, v, positions, table, cache, slots, q_weight=None, k_w
 
 
 def prq_tree_attention_workspace_bytes(M, B, Hq, Hk, D, max_kv_len):
-    return int(_tree_ws(M, B, Hq, Hk, D, max_kv_len))
+    return int(_tree_ws(M, B, Hq, Hk, D, min(max_kv_len, _I32_MAX)))
 
 
 def prq_tree_attention(q, cache, page_table, cached_lens, q_offsets, scale, tree_mask=None, max_kv_len=None,
@@ -811,6 +812,7 @@ def prq_tree_attention(q, cache, page_table, cached_lens, q_offsets, scale, tree
         mask = tree_mask.data_ptr() if mask_wide else q_offsets.data_ptr()
     if max_kv_len is None:
         max_kv_len = wide * cache.page_size
+    max_kv_len = min(max_kv_len, _I32_MAX)        # (ctypes would take its low 32 bits)
     out = _output(out, "out", (M, Hq, D), _BF16, q, stream)
     lse = _output(lse, "lse", (M, Hq), _F32, q, stream)
     if workspace is None:

@@ -199,3 +199,12 @@ def test_adapters_are_laid_out_padded():
         assert torch.equal(a.A[lo:lo + r], A.bfloat16()) and not a.A[lo + r:hi].any()
         got = a.B[16 * lo:16 * hi].view(16, -1)
         assert torch.equal(got[:, :r], B.bfloat16()) and not got[:, r:].any()
+
+
+@pytest.mark.parametrize("M,B,Hq,Hk,D", [(1, 1, 32, 8, 128), (377, 8, 32, 8, 128), (3, 2, 4, 2, 256), (40, 40, 12, 12, 64)])
+def test_workspace_does_not_shrink_as_requests_may_be_longer(M, B, Hq, Hk, D):
+    """Up to the largest length, which says that none is known."""
+    top = (1 << 31) - 1
+    sizes = [prq.prq_tree_attention_workspace_bytes(M, B, Hq, Hk, D, kv)
+             for kv in (0, 1, 100, 1 << 12, 10 ** 6, 1 << 30, top - 255, top - 127, top - 1, top, top + 1, 1 << 32, 1 << 40)]
+    assert sizes == sorted(sizes) and sizes[-1] > 0

@@ -462,3 +462,12 @@ def test_offsets_that_rise_and_fall_leave_the_workspace_ready():
     got, want = call(in_order, ws), call(in_order, torch.zeros(need, dtype=torch.uint8, device="cuda"))
     assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
     assert not ws[:16384].any()
+
+
+@pytest.mark.parametrize("max_kv", [(1 << 31) - 1, 1 << 40])
+def test_no_bound_on_the_lengths(max_kv):
+    """The plan of the longest requests there may be: the bits of one that is long enough."""
+    c = Case([(900, 4), (2, 1)], 8, 2, 64, 16)
+    want, got = c.run(max_kv_len=1 << 20), c.run(max_kv_len=max_kv)
+    c.check(*got)
+    assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
