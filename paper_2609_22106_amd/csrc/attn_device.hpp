@@ -34,6 +34,15 @@ __device__ __forceinline__ f32x4 mfma_bf16(u32x4v a, u32x4v b, f32x4 c) {
                                                  0, 0, 0);
 }
 
+// Between LDS accesses by which the lanes of one wave hand values to each other.  The wave's
+// LDS operations are done in order, so nothing waits; but the barrier builtin orders no memory
+// for the compiler, and the places that a lane writes and reads itself may be different ones.
+__device__ __forceinline__ void wave_lds_barrier() {
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront", "local");
+  __builtin_amdgcn_wave_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront", "local");
+}
+
 // Every lane's sum over itself and the lanes before it.
 __device__ __forceinline__ int prefix_sum(int x) {
   x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xF, 0xF, false);    // row_shr 1, 2, 4, 8

@@ -85,7 +85,7 @@ __device__ __forceinline__ bool find_rows(const LoraArgs& p, int* owner, Tile* o
   }
   constexpr int kNobody = -2;
   owner[lane] = kNobody;
-  __builtin_amdgcn_wave_barrier();
+  dev::wave_lds_barrier();
   for (int base = 0; base < p.segments; base += 64) {
     const int s = base + lane;
     if (s < p.segments) {
@@ -93,7 +93,7 @@ __device__ __forceinline__ bool find_rows(const LoraArgs& p, int* owner, Tile* o
       for (int row = first; row < end; ++row) owner[row] = with >= 0 && with < p.adapters ? with : -1;
     }
   }
-  __builtin_amdgcn_wave_barrier();
+  dev::wave_lds_barrier();
   const int own = lane < p.M ? owner[lane] : kNobody;
   // The rows with the lane's adapter, bit by bit of its index; the first of them counts their tiles.
   uint64_t same = __ballot(own != kNobody);
@@ -165,7 +165,7 @@ __device__ __forceinline__ void down_rows(const LoraArgs& p, const Adapter& ad, 
 #pragma unroll
       for (int i = 0; i < kLoads; ++i)
         mine[(8 * i + lr) * 8 + (unit ^ ((8 * i + lr) >> 1 & 7))] = here ? in[s][i] : none;
-      __builtin_amdgcn_wave_barrier();
+      dev::wave_lds_barrier();
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
         u32x4v x[kRowTiles];
@@ -178,7 +178,7 @@ __device__ __forceinline__ void down_rows(const LoraArgs& p, const Adapter& ad, 
           for (int a = 0; a < kRowTiles; ++a) acc[a][j] = dev::mfma_bf16(x[a], w, acc[a][j]);
         }
       }
-      __builtin_amdgcn_wave_barrier();
+      dev::wave_lds_barrier();
     }
   }
   // Join the waves, 16 rows at a time: sum[w][j][16 g + c][i] is row 4 g + i, rank 16 j + c.

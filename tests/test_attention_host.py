@@ -1,6 +1,7 @@
 """The attention block's calls on the host (no GPU): the oracle's pins, the rotation
 tables, argument checks of the C calls and of the binding."""
 import ctypes
+import os
 
 import numpy as np
 import pytest
@@ -208,3 +209,19 @@ def test_workspace_does_not_shrink_as_requests_may_be_longer(M, B, Hq, Hk, D):
     sizes = [prq.prq_tree_attention_workspace_bytes(M, B, Hq, Hk, D, kv)
              for kv in (0, 1, 100, 1 << 12, 10 ** 6, 1 << 30, top - 255, top - 127, top - 1, top, top + 1, 1 << 32, 1 << 40)]
     assert sizes == sorted(sizes) and sizes[-1] > 0
+
+
+def test_a_wave_barrier_stands_between_fences():
+    """The barrier builtin orders no memory for the compiler: wherever lanes of a wave hand values to
+    each other through LDS, a release comes before it and an acquire behind it."""
+    found = 0
+    for root, _, files in os.walk(os.path.dirname(prq.__file__)):
+        for name in files:
+            if name.endswith((".hip", ".hpp", ".h", ".cpp")):
+                lines = [s.strip() for s in open(os.path.join(root, name))]
+                for i, line in enumerate(lines):
+                    if line.startswith("__builtin_amdgcn_wave_barrier"):
+                        found += 1
+                        assert lines[i - 1].startswith("__builtin_amdgcn_fence(__ATOMIC_RELEASE"), (name, i + 1)
+                        assert lines[i + 1].startswith("__builtin_amdgcn_fence(__ATOMIC_ACQUIRE"), (name, i + 1)
+    assert found
