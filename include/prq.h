@@ -537,8 +537,10 @@ int prq_tree_attention(const void* q, int64_t ld_q, int32_t M, int32_t Hq, int32
  *   A          [rank_rows][K] bf16: adapter a's [rank, K] from row rank_offsets[a]
  *   B          bf16: adapter a's [N, rank] from element N * rank_offsets[a]
  *   rank_offsets [adapters + 1] int32, multiples of 8 (pad a rank with zero rows
- *              of A and columns of B); an adapter whose offsets are not, or reach
- *              beyond rank_rows, or hold more than max_rank, counts as none
+ *              of A and columns of B: they take part like any others, so that an
+ *              infinity in x meets their zeros unless prq_lora_ex is told of them);
+ *              an adapter whose offsets are not, or reach beyond rank_rows, or hold
+ *              more than max_rank, counts as none
  *   max_rank   multiple of 8, at most 256
  *   scales     [adapters] float32
  *   Y, out     [M] rows of N float32, ld_y / ld_out apart (multiples of 4); out
@@ -556,6 +558,14 @@ int prq_lora(const void* x_bf16, int64_t ld_x, int32_t M, int32_t K, const void*
              int32_t max_rank, const int32_t* segment_offsets, const int32_t* segment_adapter, int32_t segments,
              int32_t N, const float* Y, int64_t ld_y, float* out, int64_t ld_out, void* workspace,
              size_t workspace_bytes, hipStream_t stream);
+/* As prq_lora with the adapters' own ranks, [adapters] int32 (NULL: prq_lora): an
+ * adapter's first ranks[a] rank rows are its own (all of them where it names more, none
+ * below 1), and A x of the others, which pad it, is 0 whatever x holds. */
+int prq_lora_ex(const void* x_bf16, int64_t ld_x, int32_t M, int32_t K, const void* A, const void* B,
+                const int32_t* rank_offsets, const int32_t* ranks, const float* scales, int32_t adapters,
+                int32_t rank_rows, int32_t max_rank, const int32_t* segment_offsets,
+                const int32_t* segment_adapter, int32_t segments, int32_t N, const float* Y, int64_t ld_y,
+                float* out, int64_t ld_out, void* workspace, size_t workspace_bytes, hipStream_t stream);
 
 #ifdef __cplusplus
 }

@@ -145,11 +145,11 @@ size_t prq_lora_workspace_bytes(int32_t M, int32_t segments, int32_t N, int32_t 
   return prq::lora_workspace_bytes(prq::plan_lora(M, segments, M, N, K, max_rank, device_cus()), M, max_rank);
 }
 
-int prq_lora(const void* x_bf16, int64_t ld_x, int32_t M, int32_t K, const void* A, const void* B,
-             const int32_t* rank_offsets, const float* scales, int32_t adapters, int32_t rank_rows,
-             int32_t max_rank, const int32_t* segment_offsets, const int32_t* segment_adapter, int32_t segments,
-             int32_t N, const float* Y, int64_t ld_y, float* out, int64_t ld_out, void* workspace,
-             size_t workspace_bytes, hipStream_t stream) {
+int prq_lora_ex(const void* x_bf16, int64_t ld_x, int32_t M, int32_t K, const void* A, const void* B,
+                const int32_t* rank_offsets, const int32_t* ranks, const float* scales, int32_t adapters,
+                int32_t rank_rows, int32_t max_rank, const int32_t* segment_offsets,
+                const int32_t* segment_adapter, int32_t segments, int32_t N, const float* Y, int64_t ld_y,
+                float* out, int64_t ld_out, void* workspace, size_t workspace_bytes, hipStream_t stream) {
   if (adapters < 0 || rank_rows < 0) return PRQ_EINVAL;
   int st = check_lora_sizes(M, segments, N, K, max_rank);
   if (st != PRQ_OK) return st;
@@ -171,8 +171,18 @@ int prq_lora(const void* x_bf16, int64_t ld_x, int32_t M, int32_t K, const void*
   if (need && !aligned(workspace, 16)) return PRQ_EALIGN;
   return launch_status(prq::launch_lora(
       plan, static_cast<const uint16_t*>(x_bf16), ld_x, M, K, static_cast<const uint16_t*>(A),
-      static_cast<const uint16_t*>(B), rank_offsets, scales, adapters, rank_rows, max_rank, segment_offsets,
+      static_cast<const uint16_t*>(B), rank_offsets, ranks, scales, adapters, rank_rows, max_rank, segment_offsets,
       segment_adapter, segments, N, Y, ld_y, out, ld_out, workspace, stream));
+}
+
+int prq_lora(const void* x_bf16, int64_t ld_x, int32_t M, int32_t K, const void* A, const void* B,
+             const int32_t* rank_offsets, const float* scales, int32_t adapters, int32_t rank_rows,
+             int32_t max_rank, const int32_t* segment_offsets, const int32_t* segment_adapter, int32_t segments,
+             int32_t N, const float* Y, int64_t ld_y, float* out, int64_t ld_out, void* workspace,
+             size_t workspace_bytes, hipStream_t stream) {
+  return prq_lora_ex(x_bf16, ld_x, M, K, A, B, rank_offsets, nullptr, scales, adapters, rank_rows, max_rank,
+                     segment_offsets, segment_adapter, segments, N, Y, ld_y, out, ld_out, workspace,
+                     workspace_bytes, stream);
 }
 
 }  // extern "C"

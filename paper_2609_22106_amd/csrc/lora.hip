@@ -38,7 +38,7 @@ struct LoraArgs {
   const uint16_t* x;
   int64_t ld_x;
   const uint16_t *A, *B;
-  const int32_t* rank_offsets;
+  const int32_t *rank_offsets, *ranks;
   const float* scales;
   const int32_t *offsets, *of;
   const float* Y;
@@ -48,17 +48,20 @@ struct LoraArgs {
   int adapters, rank_rows, segments, M, N, K, max_rank, splits, k_per;
 };
 
-// An adapter: its first rank row and its rank, 0 where it has none (or
-// where the tables name one that A and B do not hold).
+// An adapter: its first rank row and its rank as A and B hold it, 0 where it has none (or
+// where the tables name one that they do not hold), and how many of those ranks are its own.
+// The others pad it: their t is 0 whatever x holds (0 x infinity is not).
 struct Adapter {
-  int index, first, rank;
+  int index, first, rank, own;
 };
 
 __device__ __forceinline__ Adapter adapter_of(const LoraArgs& p, int index) {
-  Adapter a{index, 0, 0};
+  Adapter a{index, 0, 0, 0};
   if (a.index < 0 || a.index >= p.adapters) return a;
   const int first = p.rank_offsets[a.index], end = p.rank_offsets[a.index + 1];
   if (first < 0 || end > p.rank_rows || end - first > p.max_rank || ((first | end) & 7)) return a;
+  a.own = p.ranks ? min(p.ranks[a.index], end - first) : end - first;
+  if (a.own <= 0) return a;
   a.first = first;
   a.rank = end - first;
   return a;
@@ -197,7 +200,7 @@ __device__ __forceinline__ void down_rows(const LoraArgs& p, const Adapter& ad, 
 #pragma unroll
         for (int w = 0; w < kN; ++w)
           x += sum[(w * kTiles + (rank >> 4)) * 64 + 16 * (row >> 2) + (rank & 15)][row & 3];
-        emit(16 * a + row, rank0 + rank, x);
+        emit(16 * a + row, rank0 + rank, rank0 + rank < ad.own ? x : 0.f);
       }
     }
   }
@@ -603,11 +606,11 @@ size_t lora_workspace_bytes(const LoraPlan& c, int M, int max_rank) {
 }
 
 hipError_t launch_lora(const LoraPlan& c, const uint16_t* x, int64_t ld_x, int M, int K, const uint16_t* A,
-                       const uint16_t* B, const int32_t* rank_offsets, const float* scales, int adapters,
-                       int rank_rows, int max_rank, const int32_t* offsets, const int32_t* of, int segments, int N,
-                       const float* Y, int64_t ld_y, float* out, int64_t ld_out, void* workspace,
-                       hipStream_t stream) {
-  const LoraArgs p{x, ld_x, A, B, rank_offsets, scales, offsets, of, Y, out, ld_y, ld_out,
+                       const uint16_t* B, const int32_t* rank_offsets, const int32_t* ranks, const float* scales,
+                       int adapters, int rank_rows, int max_rank, const int32_t* offsets, const int32_t* of,
+                       int segments, int N, const float* Y, int64_t ld_y, float* out, int64_t ld_out,
+                       void* workspace, hipStream_t stream) {
+  const LoraArgs p{x, ld_x, A, B, rank_offsets, ranks, scales, offsets, of, Y, out, ld_y, ld_out,
                    static_cast<float*>(workspace), adapters, rank_rows, segments, M, N, K, max_rank, c.splits,
                    c.k_per};
   if (c.small) {

@@ -243,9 +243,9 @@ struct LoraPlan {
 LoraPlan plan_lora(int M, int segments, int adapters, int N, int K, int max_rank, int num_cus);
 size_t lora_workspace_bytes(const LoraPlan& c, int M, int max_rank);
 hipError_t launch_lora(const LoraPlan& c, const uint16_t* x, int64_t ld_x, int M, int K, const uint16_t* A,
-                       const uint16_t* B, const int32_t* rank_offsets, const float* scales, int adapters,
-                       int rank_rows, int max_rank, const int32_t* offsets, const int32_t* of, int segments, int N,
-                       const float* Y, int64_t ld_y, float* out, int64_t ld_out, void* workspace,
-                       hipStream_t stream);
+                       const uint16_t* B, const int32_t* rank_offsets, const int32_t* ranks, const float* scales,
+                       int adapters, int rank_rows, int max_rank, const int32_t* offsets, const int32_t* of,
+                       int segments, int N, const float* Y, int64_t ld_y, float* out, int64_t ld_out,
+                       void* workspace, hipStream_t stream);
 
 }  // namespace prq

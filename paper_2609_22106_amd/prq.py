@@ -96,6 +96,9 @@ _lora_ws = _decl("prq_lora_workspace_bytes", _sz, [_i32, _i32, _i32, _i32, _i32]
 _lora = _decl("prq_lora", ctypes.c_int,
               [_p, _i64, _i32, _i32, _p, _p, _p, _p, _i32, _i32, _i32, _p, _p, _i32, _i32, _p, _i64, _p, _i64, _p,
                _sz, _p])
+_lora_ex = _decl("prq_lora_ex", ctypes.c_int,
+                 [_p, _i64, _i32, _i32, _p, _p, _p, _p, _p, _i32, _i32, _i32, _p, _p, _i32, _i32, _p, _i64, _p, _i64,
+                  _p, _sz, _p])
 
 
 class PRQError(RuntimeError):
@@ -831,12 +834,14 @@ def prq_tree_attention(q, cache, page_table, cached_lens, q_offsets, scale, tree
 class LoraAdapters:
     """Device buffers of a set of adapters: A [sum of ranks, K] bf16, B bf16 flat (adapter a's [N, rank]
     from element N * rank_offsets[a]), rank_offsets int32 [adapters + 1] in multiples of 8, scales float32
-    [adapters], and the largest rank."""
+    [adapters], the largest rank, and where ranks are padded to those multiples the ranks themselves,
+    int32 [adapters] (None: what lies between the offsets)."""
 
-    __slots__ = ("A", "B", "rank_offsets", "scales", "max_rank", "rank_rows", "count")
+    __slots__ = ("A", "B", "rank_offsets", "scales", "max_rank", "ranks", "rank_rows", "count")
 
-    def __init__(self, A, B, rank_offsets, scales, max_rank):
+    def __init__(self, A, B, rank_offsets, scales, max_rank, ranks=None):
         self.A, self.B, self.rank_offsets, self.scales, self.max_rank = A, B, rank_offsets, scales, max_rank
+        self.ranks = ranks
         self.rank_rows, self.count = A.shape[0], scales.shape[0]
 
 
@@ -846,7 +851,7 @@ def prq_lora_adapters(pairs, scales, device="cuda"):
     if not pairs or len(pairs) != len(scales):
         raise ValueError("as many scales as adapters are needed, and one adapter at least")
     K, N = pairs[0][0].shape[1], pairs[0][1].shape[0]
-    ranks, As, Bs = [], [], []
+    own, ranks, As, Bs = [], [], [], []
     for A, B in pairs:
         r = A.shape[0]
         if A.shape != (r, K) or B.shape != (N, r):
@@ -855,10 +860,12 @@ def prq_lora_adapters(pairs, scales, device="cuda"):
         A, B = A.to(device, _BF16), B.to(device, _BF16)
         As.append(torch.nn.functional.pad(A, (0, 0, 0, pad)))
         Bs.append(torch.nn.functional.pad(B, (0, pad)).reshape(-1))
+        own.append(r)
         ranks.append(r + pad)
     return LoraAdapters(torch.cat(As).contiguous(), torch.cat(Bs).contiguous(),
                         torch.tensor(np.concatenate([[0], np.cumsum(ranks)]), dtype=_I32, device=device),
-                        torch.tensor([float(s) for s in scales], dtype=_F32, device=device), max(ranks))
+                        torch.tensor([float(s) for s in scales], dtype=_F32, device=device), max(ranks),
+                        torch.tensor(own, dtype=_I32, device=device) if own != ranks else None)
 
 
 def prq_lora_workspace_bytes(M, segments, N, K, max_rank):
@@ -878,6 +885,8 @@ def prq_lora(x, adapters, segment_offsets, segment_adapter, Y, out=None, workspa
     ld_out = _rows(out, "out", (_F32,), M, N)
     a = adapters
     n, R = a.count, a.rank_rows
+    if a.ranks is not None:
+        _vector(a.ranks, "adapters.ranks", _I32, n)
     if not (_is(a.A, _BF16, (R, K)) and _holds(a.B, _BF16, N * R) and _is(a.rank_offsets, _I32, (n + 1,))
             and _is(a.scales, _F32, (n,))):
         _need(a.A, "adapters.A", _BF16, (R, K))
@@ -898,9 +907,9 @@ def prq_lora(x, adapters, segment_offsets, segment_adapter, Y, out=None, workspa
             ws = workspace.data_ptr()
     else:
         ws, ws_bytes = _workspace_arg(workspace)
-    st = _lora(x.data_ptr(), ld_x, M, K, a.A.data_ptr(), a.B.data_ptr(), a.rank_offsets.data_ptr(),
-               a.scales.data_ptr(), n, R, a.max_rank, segment_offsets.data_ptr(),
-               segment_adapter.data_ptr(), segments, N, Y.data_ptr(), ld_y, out.data_ptr(), ld_out, ws, ws_bytes,
-               _stream_of_call(stream))
+    st = _lora_ex(x.data_ptr(), ld_x, M, K, a.A.data_ptr(), a.B.data_ptr(), a.rank_offsets.data_ptr(),
+                  None if a.ranks is None else a.ranks.data_ptr(), a.scales.data_ptr(), n, R, a.max_rank,
+                  segment_offsets.data_ptr(), segment_adapter.data_ptr(), segments, N, Y.data_ptr(), ld_y,
+                  out.data_ptr(), ld_out, ws, ws_bytes, _stream_of_call(stream))
     _check(st, "prq_lora")
     return out

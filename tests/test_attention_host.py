@@ -225,3 +225,18 @@ def test_a_wave_barrier_stands_between_fences():
                         assert lines[i - 1].startswith("__builtin_amdgcn_fence(__ATOMIC_RELEASE"), (name, i + 1)
                         assert lines[i + 1].startswith("__builtin_amdgcn_fence(__ATOMIC_ACQUIRE"), (name, i + 1)
     assert found
+
+
+def test_adapters_carry_the_ranks_that_are_their_own():
+    pairs = [(torch.ones(r, 32), torch.ones(16, r)) for r in (3, 8, 16)]
+    assert prq.prq_lora_adapters(pairs, [1.0] * 3, device="cpu").ranks.tolist() == [3, 8, 16]
+    assert prq.prq_lora_adapters(pairs[1:], [1.0] * 2, device="cpu").ranks is None          # nothing is padded
+
+
+@pytest.mark.parametrize("ranks", [None, FAKE])
+@pytest.mark.parametrize("change,status", [
+    (dict(M=-1), EINVAL), (dict(x=None), EINVAL), (dict(scales=None), EINVAL), (dict(N=56), EALIGN),
+    (dict(max_rank=264), EUNSUP), (dict(M=0, x=None, Y=None, out=None), 0), (dict(segments=0, offsets=None, of=None), 0)])
+def test_lora_with_ranks_refuses_as_without(change, status, ranks):
+    args = list({**LORA, **change}.values())
+    assert prq._lora_ex(*args[:7], ranks, *args[7:]) == status

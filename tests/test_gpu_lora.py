@@ -193,3 +193,52 @@ def test_rows_in_no_segment_are_left_alone_among_many_segments():
     assert torch.equal(got[2:], want[2:]) and bool(torch.isnan(got[:2]).all())
     c.offsets = torch.flip(torch.arange(21, dtype=torch.int32, device="cuda"), [0]).contiguous()       # descending
     assert bool(torch.isnan(c.run()).all())
+
+
+@pytest.mark.parametrize("rows,of,ranks,N,K", [
+    ([1], [0], [1], 64, 128), ([3, 20], [1, 0], [5, 17], 64, 2560), ([100], [0], [33], 256, 264),
+    ([2, 40], [0, 1], [3, 63], 128, 9728), ([300, 70], [1, 0], [100, 129], 64, 96), ([1] * 20, [0, 1] * 10, [12, 2], 64, 128),
+    ([1] * 20, [0, 1] * 10, [200, 1], 64, 520)])
+def test_an_infinity_meets_the_ranks_there_are(rows, of, ranks, N, K):
+    """A is positive and a column of B has one sign, so that a row of x with an infinity becomes one of
+    that sign everywhere: what pads a rank to a multiple of 8 does not make it 0 x inf."""
+    say("infinity and padded ranks", len(rows), ranks, N, K)
+    prq = _prq()
+    c = Case(rows, of, ranks, N, K, seed=K)
+    sign = torch.where(torch.arange(N, device="cuda") % 3 == 0, -1.0, 1.0)
+    c.pairs = [(A.abs() + 2.0 ** -6, ((B.float().abs() + 0.5) * sign[:, None]).to(BF16)) for A, B in c.pairs]
+    c.adapters = prq.prq_lora_adapters(c.pairs, c.scales)
+    want = c.run()
+    c.check(want)
+    M = sum(rows)
+    for r in {0, M // 2, M - 1}:
+        c.x[r, (7 * r) % K] = float("inf")
+    got = c.run()
+    for r in range(M):
+        if r in (0, M // 2, M - 1):
+            assert torch.equal(got[r], sign * float("inf")), r
+        else:
+            assert torch.equal(got[r], want[r]), r
+
+
+def test_ranks_that_do_not_fit_the_offsets():
+    """A rank beyond what the offsets hold is what they hold, one below 1 is none; what the others pad
+    a rank with is not read as one of its own, whatever it is."""
+    prq = _prq()
+    for rows, K in ([5, 6, 7], 128), ([1] * 3, 5000), ([100, 64, 40], 264):
+        c = Case(rows, [0, 1, 2], [16, 16, 24], 64, K, seed=K)
+        want = c.run()
+        a = c.adapters
+        ranks = torch.tensor([99, 16, 1 << 30], dtype=torch.int32, device="cuda")
+        c.adapters = prq.LoraAdapters(a.A, a.B, a.rank_offsets, a.scales, a.max_rank, ranks)
+        assert torch.equal(c.run(), want)
+        ranks[:] = torch.tensor([0, 11, -(1 << 31)], dtype=torch.int32, device="cuda")
+        got, n = c.run(), rows[0] + rows[1]
+        assert torch.equal(got[:rows[0]], c.Y[:rows[0]]) and torch.equal(got[n:], c.Y[n:])
+        c.of_host, c.pairs[1] = [-1, 1, -1], (c.pairs[1][0][:11], c.pairs[1][1][:, :11])
+        c.check(got)
+        a.A[a.rank_offsets[1] + 11:a.rank_offsets[1] + 16] = float("nan")
+        assert torch.equal(c.run(), got)
+        with pytest.raises(ValueError):
+            c.adapters = prq.LoraAdapters(a.A, a.B, a.rank_offsets, a.scales, a.max_rank, ranks[:2])
+            c.run()
