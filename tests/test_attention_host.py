@@ -240,3 +240,12 @@ def test_adapters_carry_the_ranks_that_are_their_own():
 def test_lora_with_ranks_refuses_as_without(change, status, ranks):
     args = list({**LORA, **change}.values())
     assert prq._lora_ex(*args[:7], ranks, *args[7:]) == status
+
+
+@pytest.mark.parametrize("dtype,kind", [(torch.float32, prq.PRQ_F32), (torch.bfloat16, prq.PRQ_BF16)])
+@pytest.mark.parametrize("own", [lambda t: t, lambda t: torch.nn.Parameter(t)])
+def test_a_norm_weight_has_its_own_type(monkeypatch, dtype, kind, own):
+    """A module's Parameter too, which takes the checks' other way: its bf16 values are not float32."""
+    monkeypatch.setattr(prq, "_on_gpu", lambda **t: None)
+    w = own(torch.ones(64, dtype=dtype))
+    assert prq._head_weight(w, "q_weight", 64) == (w.data_ptr(), kind)
