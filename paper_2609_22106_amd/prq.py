@@ -640,8 +640,8 @@ class PagedKV:
 
     def __init__(self, K, V):
         self.K, self.V = K, V
-        if not (type(K) is type(V) is torch.Tensor and K.dtype is V.dtype is _BF16 and K.dim() == 4 and K.is_cuda
-                and V.is_cuda and K.shape == V.shape):
+        if not (isinstance(K, torch.Tensor) and isinstance(V, torch.Tensor) and K.dtype is V.dtype is _BF16
+                and K.dim() == 4 and K.is_cuda and V.is_cuda and K.shape == V.shape):
             raise ValueError("K and V must be bfloat16 GPU tensors [pages, kv heads, page size, D] of one shape")
         self.pages, self.heads, self.page_size, self.D = K.shape
         page = self.heads * self.page_size * self.D
@@ -701,7 +701,7 @@ def prq_rope_table(positions, rotary_dim, theta=10000.0, scaling="none", factor=
 
 def _rows(t, name, dtypes, M, wide):
     """A GPU tensor [M, wide] whose rows are contiguous -> its row stride."""
-    if type(t) is torch.Tensor and t.dtype in dtypes and t.is_cuda and t.shape == (M, wide):
+    if isinstance(t, torch.Tensor) and t.dtype in dtypes and t.is_cuda and t.shape == (M, wide):
         if t.is_contiguous():
             return wide
         if t.stride(1) == 1 or wide == 1:
@@ -755,7 +755,7 @@ def prq_qk_norm_rope(q, k, v, positions, table, cache, slots, q_weight=None, k_w
     rot = rows = 0
     table_at = positions_at = None
     if table is not None:
-        if not (type(table) is torch.Tensor and table.dtype is _F32 and table.is_cuda and table.is_contiguous()
+        if not (isinstance(table, torch.Tensor) and table.dtype is _F32 and table.is_cuda and table.is_contiguous()
                 and table.dim() == 3 and table.shape[2] == 2):
             raise ValueError("table must be a contiguous float32 GPU tensor [positions, rotary_dim / 2, 2]")
         rows, half, _ = table.shape
@@ -794,12 +794,12 @@ def prq_tree_attention(q, cache, page_table, cached_lens, q_offsets, scale, tree
     a row sees (None: itself and those before it).  max_kv_len: the most tokens a request has (default:
     what the page table holds).  workspace: uint8, prq_tree_attention_workspace_bytes, zeroed before its
     first use and left ready by every call (else allocated, zeroed by another launch)."""
-    if not (type(q) is torch.Tensor and q.dtype is _BF16 and q.is_cuda and q.dim() == 3 and q.shape[2] == cache.D
+    if not (isinstance(q, torch.Tensor) and q.dtype is _BF16 and q.is_cuda and q.dim() == 3 and q.shape[2] == cache.D
             and (q.is_contiguous() or (q.stride(2) == 1 and (q.shape[1] <= 1 or q.stride(1) == cache.D)))):
         raise ValueError(f"q must be a bfloat16 GPU tensor [M, heads, {cache.D}] with contiguous rows")
     M, Hq, D = q.shape
     ld_q = q.stride(0) if M > 1 else Hq * D
-    if not (type(page_table) is torch.Tensor and page_table.dim() == 2):
+    if not (isinstance(page_table, torch.Tensor) and page_table.dim() == 2):
         raise ValueError("page_table must be a GPU tensor [requests, pages]")
     B, wide = page_table.shape
     ld_pages = _rows(page_table, "page_table", (_I32,), B, wide)
@@ -892,7 +892,7 @@ def prq_lora(x, adapters, segment_offsets, segment_adapter, Y, out=None, workspa
         _need(a.rank_offsets, "adapters.rank_offsets", _I32, (n + 1,))
         _need(a.scales, "adapters.scales", _F32, (n,))
         _on_gpu(A=a.A, B=a.B, rank_offsets=a.rank_offsets, scales=a.scales)
-    if not (type(segment_adapter) is torch.Tensor and segment_adapter.dim() == 1):
+    if not (isinstance(segment_adapter, torch.Tensor) and segment_adapter.dim() == 1):
         raise ValueError("segment_adapter must be an int32 GPU tensor [segments]")
     segments = segment_adapter.shape[0]
     _vector(segment_adapter, "segment_adapter", _I32, segments)

@@ -269,3 +269,32 @@ def test_another_stream():
     got = prq.prq_lora(late, ad, off, of, Y, out=torch.empty_like(Y), stream=side)
     torch.cuda.synchronize()
     assert torch.equal(got, want)
+
+
+def test_parameters_are_taken_as_tensors_are():
+    """A module's Parameters in the place of inputs, tables and the cache: the bits of plain tensors."""
+    from paper_2609_22106_amd import prq
+    own = lambda t: torch.nn.Parameter(t.clone(), requires_grad=False)       # noqa: E731
+    g = torch.Generator("cuda").manual_seed(31)
+    rnd = lambda *s: torch.randn(s, generator=g, device="cuda")       # noqa: E731
+    M = 6
+    pos, slots = torch.arange(M, dtype=torch.int32, device="cuda"), torch.arange(M, device="cuda")
+    table, w = prq.prq_rope_table(64, 64), rnd(64).to(BF16)
+    got = []
+    for wrap in (lambda t: t.clone(), own):
+        g.manual_seed(32)
+        K, V = wrap(torch.zeros(4, KV, 16, 64, dtype=BF16, device="cuda")), wrap(torch.zeros(4, KV, 16, 64, dtype=BF16,
+                                                                                        device="cuda"))
+        cache = prq.PagedKV(K, V)
+        q = prq.prq_qk_norm_rope(wrap(rnd(M, 8 * 64)), wrap(rnd(M, KV * 64)), wrap(rnd(M, KV * 64)), wrap(pos),
+                                 wrap(table), cache, wrap(slots), wrap(w), wrap(w))
+        pages = wrap(torch.arange(4, dtype=torch.int32, device="cuda")[None])
+        one = torch.tensor([0, M], dtype=torch.int32, device="cuda")
+        out, lse = prq.prq_tree_attention(wrap(q), cache, pages, wrap(one[:1]), wrap(one), 0.1,
+                                          wrap(torch.ones(M, M, dtype=torch.bool, device="cuda")))
+        ad = prq.prq_lora_adapters([(rnd(8, 128), rnd(64, 8))], [1.0])
+        ad = prq.LoraAdapters(wrap(ad.A), wrap(ad.B), wrap(ad.rank_offsets), wrap(ad.scales), 8)
+        y = prq.prq_lora(wrap(rnd(M, 128).to(BF16)), ad, wrap(one), wrap(one[:1]), wrap(rnd(M, 64)))
+        got.append([t.detach().clone() for t in (q, K, V, out, lse, y)])
+    for a, b in zip(*got):
+        assert torch.equal(a, b)
