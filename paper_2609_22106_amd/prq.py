@@ -720,7 +720,9 @@ def _vector(t, name, dtype, n):
 
 def _head_weight(w, name, D):
     """(address, type) of a norm's weight [D]."""
-    if not (_is(w, _F32, (D,)) or _is(w, _BF16, (D,))):
+    if _is(w, _BF16, (D,)):
+        return w.data_ptr(), PRQ_BF16
+    if not _is(w, _F32, (D,)):
         _need(w, name, (_F32, _BF16), (D,))
         _on_gpu(**{name: w})
     return w.data_ptr(), PRQ_BF16 if w.dtype is _BF16 else PRQ_F32
