@@ -298,3 +298,152 @@ def test_parameters_are_taken_as_tensors_are():
         got.append([t.detach().clone() for t in (q, K, V, out, lse, y)])
     for a, b in zip(*got):
         assert torch.equal(a, b)
+
+
+def test_a_captured_step_serves_other_tables():
+    """One graph, replayed with other rows a request, lengths, pages, slots, positions, masks and
+    adapters in its tables: each replay has an eager call's bits, and that call's stages match the
+    oracle."""
+    from paper_2609_22106_amd import prq
+    layer = Layer(seed=2, longest=1024)
+    rng = np.random.default_rng(12)
+    g = torch.Generator("cuda").manual_seed(11)
+    for t in (layer.cache.K, layer.cache.V):
+        t.copy_(torch.randn(t.shape, generator=g, device="cuda"))
+
+    def step(M):
+        """Tables of M rows of four requests; the mask M wide."""
+        rows = np.diff(np.concatenate([[0], np.sort(rng.integers(0, M + 1, 3)), [M]]))
+        requests = [(int(rng.integers(0, 1024 - M)), [int(rng.integers(-1, i)) if i else -1 for i in range(n)])
+                    for n in rows]
+        layer.pages = rng.permutation(layer.pages.size).astype(np.int32).reshape(layer.pages.shape)
+        adapter = [int(a) for a in rng.integers(-1, len(RANKS), 4)]
+        now = layer.batch(requests, adapter)
+        see = torch.zeros((M, M), dtype=torch.bool, device="cuda")
+        if now.mask is None:                                          # chains all of them
+            row = 0
+            for n in rows:
+                see[row:row + n, :n] = torch.ones(n, n, dtype=torch.bool, device="cuda").tril()
+                row += n
+        else:
+            see[:, :now.mask.shape[1]] = now.mask
+        now.mask = see
+        return now, requests, adapter
+
+    for M in (4, 24, 70):                                             # 16, 64 and 64 columns a workgroup
+        assert prq.prq_tree_attention_workspace_bytes(M, 4, HEADS, KV, D, 1024) > 16384       # keys are split
+        static = step(M)[0]
+        x = _x(M, M)
+        layer.block(x, static)
+        torch.cuda.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            y = layer.block(x, static)
+        for replay in range(5):
+            say("captured step", M, "rows, replay", replay)
+            now, requests, adapter = step(M)
+            for name in ("position", "slot", "mask", "pages", "cached", "offsets", "adapter"):
+                getattr(static, name).copy_(getattr(now, name))
+            x.copy_(_x(M, 100 * M + replay))
+            for t in (y, layer.block.q, layer.block.attended, layer.block.lse):
+                t.fill_(float("nan"))
+            graph.replay()
+            got = [t.clone() for t in (y, layer.block.attended[:M], layer.block.lse[:M])]
+            layer.check(x, now, requests, adapter)
+            for a, b in zip(got, (y, layer.block.attended[:M], layer.block.lse[:M])):
+                assert torch.equal(a, b)
+
+
+def _calls(seed):
+    """{name: (call(inputs, stream), inputs, the cache that it writes)} of the three operators' plans,
+    with outputs and workspaces made by the call itself."""
+    from paper_2609_22106_amd import prq
+    g = torch.Generator("cuda").manual_seed(seed)
+    rnd = lambda *s: torch.randn(s, generator=g, device="cuda")       # noqa: E731
+    ints = lambda a: torch.tensor(a, dtype=torch.int32, device="cuda")       # noqa: E731
+    pages = torch.arange(30, dtype=torch.int32, device="cuda").reshape(3, 10)
+    K, V = rnd(30, KV, 64, 128).to(BF16), rnd(30, KV, 64, 128).to(BF16)
+    calls = {}
+    for n in (1, 5, 40):                                              # 16, 64 and 256 columns a workgroup
+        M, off, cached, mask = 3 * n, ints([0, n, 2 * n, 3 * n]), ints([600 - n, 300, 17]), rnd(3 * n, n) > 0
+        assert prq.prq_tree_attention_workspace_bytes(M, 3, 8, KV, 128, 640) > 16384
+        calls[f"attention, {n} rows a request"] = (
+            lambda a, st, c=cached, o=off, m=mask: prq.prq_tree_attention(a[0], prq.PagedKV(a[1], a[2]), pages, c, o,
+                                                                          0.1, m, max_kv_len=640, stream=st),
+            (rnd(M, 8, 128).to(BF16), K, V), ())
+    table = prq.prq_rope_table(512, 128)
+    for M in (1, 300):
+        pos, slots = torch.arange(M, dtype=torch.int32, device="cuda"), torch.arange(M, device="cuda")
+        pool = prq.prq_paged_kv(8, KV, 64, 128)
+        calls[f"norm and rotation, {M} rows"] = (
+            lambda a, st, p=pos, s=slots, pool=pool: (prq.prq_qk_norm_rope(*a, p, table, pool, s, stream=st),
+                                                      pool.K, pool.V),
+            (rnd(M, 8 * 128), rnd(M, KV * 128), rnd(M, KV * 128)), (pool.K, pool.V))
+    for rows, N, K_ in (([1, 2], 512, 256), ([30, 33], 512, 5000), ([400, 0, 600], 1024, 256)):
+        M = sum(rows)
+        ad = prq.prq_lora_adapters([(rnd(r, K_), rnd(N, r)) for r in (16, 64)], [0.5, 1.5])
+        off, of = ints(np.concatenate([[0], np.cumsum(rows)])), ints([i % 2 for i in range(len(rows))])
+        calls[f"adapters, {M} rows of {K_}"] = (
+            lambda a, st, ad=ad, off=off, of=of: prq.prq_lora(a[0], ad, off, of, a[1], out=a[2], stream=st),
+            (rnd(M, K_).to(BF16), rnd(M, N), torch.zeros((M, N), device="cuda")), ())
+    return calls
+
+
+def _outputs(result):
+    return [t.clone() for t in (result if isinstance(result, tuple) else (result,))]
+
+
+def _keep_busy(stream):
+    with torch.cuda.stream(stream):
+        busy = torch.randn((2048, 2048), device="cuda")
+        for _ in range(40):
+            busy = busy @ busy * 0.01
+
+
+def test_inputs_made_late_on_the_calls_stream():
+    """NaN until a stream that is not the current one, busy at first, writes them: a call on that
+    stream waits for them, one on any other would read the NaN."""
+    for name, (call, inputs, cache) in _calls(21).items():
+        say("late inputs", name)
+        want = _outputs(call([t.clone() for t in inputs], None))
+        assert all(bool(torch.isfinite(t).all()) for t in want)
+        late = [torch.full_like(t, float("nan")) for t in inputs]
+        for t in cache:
+            t.zero_()
+        side = torch.cuda.Stream()
+        torch.cuda.synchronize()
+        _keep_busy(side)
+        with torch.cuda.stream(side):
+            for t, u in zip(late, inputs):
+                t.copy_(u)
+        got = call(late, side)
+        torch.cuda.synchronize()
+        for a, b in zip(_outputs(got), want):
+            assert torch.equal(a, b), name
+
+
+def test_a_call_on_another_stream_does_not_wait_for_the_current_one():
+    """The current stream is busy while the call runs on its own: what the call makes for itself, a
+    workspace that starts at zero among it, is ready there, also where both streams' memory was left
+    full of ones."""
+    for name, (call, inputs, cache) in _calls(22).items():
+        say("busy current stream", name)
+        want = _outputs(call([t.clone() for t in inputs], None))
+        side = torch.cuda.Stream()
+        torch.cuda.synchronize()
+        for stream in (side, torch.cuda.current_stream()):
+            with torch.cuda.stream(stream):
+                dirty = [torch.full((n,), 255, dtype=torch.uint8, device="cuda") for n in (1 << 14, 1 << 19, 1 << 21, 1 << 23)]
+                del dirty
+        args = [t.clone() for t in inputs]
+        for t in cache:
+            t.zero_()
+        torch.cuda.synchronize()
+        _keep_busy(torch.cuda.current_stream())
+        got = call(args, side)
+        side.synchronize()
+        with torch.cuda.stream(side):
+            got = _outputs(got)
+        torch.cuda.synchronize()
+        for a, b in zip(got, want):
+            assert torch.equal(a, b), name

@@ -471,3 +471,22 @@ def test_no_bound_on_the_lengths(max_kv):
     want, got = c.run(max_kv_len=1 << 20), c.run(max_kv_len=max_kv)
     c.check(*got)
     assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+
+
+@pytest.mark.parametrize("rows", [1, 9, 30])
+@pytest.mark.parametrize("scale", [-0.07, 0.0, -0.0, 1e-35, -2.5])
+def test_scales_of_either_sign_and_zero(rows, scale):
+    """Scores of either sign; with a scale of 0 every seen key weighs alike.  (Bars as above, the size
+    of the scores with the scale's magnitude.)"""
+    say("scale", scale, rows)
+    c = Case([(200, rows), (0, rows)], 8, 2, 64, 16, seed=rows)
+    c.scale = scale
+    out, lse = c.run()
+    out, lse = out.double().cpu().numpy(), lse.double().cpu().numpy()
+    q, mask = c.q.double().cpu().numpy(), c.mask.cpu().numpy()
+    for b, at_ in enumerate((slice(0, rows), slice(rows, 2 * rows))):
+        k, v = c.keys[b].double().cpu().numpy(), c.values[b].double().cpu().numpy()
+        want, wl, spread, size = at.tree_attention(q[at_], k, v, c.requests[b][0], float(np.float32(scale)), mask[at_])
+        S = (abs(scale) * size + 16)[..., None]
+        assert np.all(np.abs(out[at_] - want) <= 2.0 ** -8 * np.abs(want) + (2.0 ** -8 + 2.0 ** -18 * S) * spread)
+        assert np.all(np.abs(lse[at_] - wl) <= 2.0 ** -18 * S[..., 0] + 2.0 ** -22 * np.abs(wl))
