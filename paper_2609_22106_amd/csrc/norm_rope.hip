@@ -15,8 +15,8 @@
 // rot / 2 + 4i.., or 8 consecutive elements of interleaved pairs), so that the
 // rotation needs no other lane and loads and stores stay 16 and 8 bytes wide.  A
 // workgroup takes heads of one row, the loads of all of its kHeads heads a lane
-// group in flight at once.  8192 rows of 32 + 8 + 8 float32 heads of 128: 61 us, 306 MB at
-// 5.0 TB/s (a plain copy here 5.5); one row: 2.9 us, a launch and two dependent loads.
+// group in flight at once.  8192 rows of 32 + 8 + 8 float32 heads of 128: 59 us, 306 MB at
+// 5.2 TB/s (a plain copy here 5.5); one row: 2.9 us, a launch and two dependent loads.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>

@@ -26,9 +26,9 @@
 // back transposed.  Trees of up to 64 nodes over 8 x 32 k tokens (377 rows, 204 k keys): straight
 // from memory 714 us, through LDS with v_perm 272, transposed reads 258; a stage's scores
 // beside the exponentials of the one before and LDS read ahead, 8 waves for more than 128
-// columns, those dealt evenly to the SIMDs, a barrier every two stages, 230: 690 TFLOP/s, the
-// matrix units 40% of the time, 9 us of it the join's.  What is left: the parts, unequal by 17%,
-// and a SIMD's two waves, in step more often than in turn.
+// columns, those dealt evenly to the SIMDs, a barrier every two stages, 230 (224 to 232 from card
+// to card): 690 TFLOP/s, the matrix units 41% of the time, 9 us of it the join's.  What is left:
+// the parts, unequal by 17%, and a SIMD's two waves, in step more often than in turn.
 //
 // The maximum is kept per lane group and only joined across the groups when a score
 // passes it by 8 (powers of two): until then the stale maximum serves, P up to 2^8.
