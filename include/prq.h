@@ -567,6 +567,104 @@ int prq_lora_ex(const void* x_bf16, int64_t ld_x, int32_t M, int32_t K, const vo
                 const int32_t* segment_adapter, int32_t segments, int32_t N, const float* Y, int64_t ld_y,
                 float* out, int64_t ld_out, void* workspace, size_t workspace_bytes, hipStream_t stream);
 
+/*
+ * The mixture-of-experts half of a layer: what stands around its blocks (prq_block_norm), the
+ * router (prq_moe_route), and all experts of a decoding step's few tokens (prq_moe_layer; more
+ * tokens take prq_grouped_gemm with rows sorted by expert).  Activations are bf16, sums float32.
+ */
+
+/*
+ * prq_block_norm -- the norm behind a block, its gate, the scaled sum with the residual and the norm
+ * before the next block, in one pass over M rows of H:
+ *   u  = y                                      without post_weight
+ *      = y / sqrt(mean(y^2) + eps) * (weight_offset + post_weight)
+ *   r' = residual_scale * r + block_scale * g * u      (g = 1 for rows without a gate)
+ *   h  = r' / sqrt(mean(r'^2) + eps) * (weight_offset + pre_weight)
+ * in float32; r' is rounded once, as it is stored, and h, which takes the unrounded r', once, to
+ * bf16.
+ *
+ *   y            device [M, ld_y] PRQ_F32 (a GEMM's output) or PRQ_BF16; NULL: no block, r' is the
+ *                scaled residual (post_weight and gate must be NULL)
+ *   residual     device [M, ld_r] r of type r_type; NULL: none, r' is the block's part
+ *   post_weight, pre_weight  device [H] of one type; NULL: no such norm
+ *   gate         device [gate_rows, ld_gate] of gate_type, or NULL.  gate_index (device int32 [M])
+ *                names each row's gate; an entry outside [0, gate_rows) names none.  Without
+ *                gate_index gate_rows is 1 (every row's) or M (row m's).
+ *   residual_out device [M, ld_ro] r' of type r_type, or NULL; may be residual itself (with its
+ *                stride)
+ *   h_out        device [M, ld_h] bf16; given exactly when pre_weight is
+ * Outputs overlap no other operand.  Rows and pointers 16-byte aligned.
+ * Limits: H % 8 == 0, H <= 16384, M < 2^24.  M == 0 is a no-op.
+ * Errors: PRQ_EINVAL also for neither y nor residual, neither output, a NaN or infinite scale, a
+ * negative eps.
+ */
+int prq_block_norm(const void* y, int64_t ld_y, int32_t y_type, const void* residual, int64_t ld_r, int32_t r_type,
+                   int32_t M, int32_t H, const void* post_weight, const void* pre_weight, int32_t weight_type,
+                   float weight_offset, const void* gate, int64_t ld_gate, int32_t gate_type, int32_t gate_rows,
+                   const int32_t* gate_index, float eps, float residual_scale, float block_scale,
+                   void* residual_out, int64_t ld_ro, void* h_out, int64_t ld_h, hipStream_t stream);
+
+/* How prq_moe_route scores an expert's logit. */
+enum {
+  PRQ_ROUTE_SOFTMAX = 0,  /* softmax over all experts                            */
+  PRQ_ROUTE_SIGMOID = 1   /* 1 / (1 + exp(-l)), each by itself                   */
+};
+
+/*
+ * prq_moe_route -- M tokens to k of E experts each:
+ *   l = x W^T (float32 sums), s = softmax(l) or sigmoid(l);
+ *   ids: the k experts with the largest s (+ bias, with the sigmoid; scores and keys are then
+ *        float64), in descending order, the lower index first among equals, NaN last;
+ *   weights: their s, with `renormalize` divided by the sum of the k, times `scale`.
+ *
+ *   x       device [M, ld_x] bf16
+ *   W       device [E, ld_w] bf16
+ *   bias    device [E] float or NULL: a correction of the choice, not of the weights
+ *           (PRQ_ROUTE_SIGMOID only)
+ *   ids     device [M, k] int32, weights device [M, k] float
+ *   logits  device [M, ld_logits] float output (E used), or NULL
+ *   workspace  device buffer of prq_moe_route_workspace_bytes, 16-byte aligned (may be NULL
+ *           where that is 0): the 16 KiB state head of prq_gemm's workspaces (zero before the
+ *           first use, left zero by every call), then scratch.  One buffer serves all calls
+ *           that take such a head, in turn; calls that share it must be ordered.
+ * x and W rows and pointers 16-byte aligned.
+ * Limits: H % 8 == 0, H <= 65536, E <= 1024, k <= 32, k <= E, M < 2^24.  M == 0 is a no-op.
+ */
+size_t prq_moe_route_workspace_bytes(int32_t M, int32_t E, int32_t H);
+int prq_moe_route(const void* x_bf16, int64_t ld_x, int32_t M, int32_t H, const void* W_bf16, int64_t ld_w, int32_t E,
+                  int32_t k, int32_t scoring, const float* bias, int32_t renormalize, float scale, int32_t* ids,
+                  float* weights, float* logits, int64_t ld_logits, void* workspace, size_t workspace_bytes,
+                  hipStream_t stream);
+
+/*
+ * prq_moe_layer -- all experts of up to 64 tokens, from the layer's input to the weighted sum:
+ *   h_e = SiLU(Wgate_e x) * (Wup_e x)
+ *   out[m] = sum_j weights[m, j] * Wdown_e [h_e ; last k_tail of h_e],   e = ids[m, j]
+ * MXFP4 weights against bf16 activations: at so few rows the weights are the bytes, so the
+ * activations are not quantized.  Sums are float32; weights[m, j] h is rounded to bf16 once, and
+ * out once.
+ *
+ *   x        device [M, ld_x] bf16
+ *   ids      device [M, k] int32; an entry outside [0, E) adds nothing (padding, an expert held
+ *            elsewhere); an expert named twice counts with both weights.  A row without experts is 0.
+ *   weights  device [M, k] float
+ *   up_Wp, up_Wps      E weights [2 I, H], the gate's I rows before the up-projection's, in the
+ *            packed layout (prq_pack_weight with E, N = 2 I, K_aug = H): prq_prepare's with
+ *            PRQ_SCALE_NONE and k_tail = 0, whose channels are in their own order
+ *   down_Wp, down_Wps  E weights [N, I + k_tail] in the packed layout.  With a permutation and
+ *            scales from prq_prepare the gate and up rows are prq_expand_producer's first I.
+ *   out      device [M, ld_out] bf16, ld_out % 8 == 0
+ *   workspace  device buffer of prq_moe_layer_workspace_bytes, 16-byte aligned: the state head as
+ *            for prq_moe_route, then scratch
+ * Limits: M <= 64, k <= 32, E <= 4096, H % 32 == 0, I % 32 == 0, k_tail % 32 == 0, k_tail <= I,
+ * N % 16 == 0 (else PRQ_EALIGN), H, N <= 65536, I <= 32768.  M == 0 is a no-op.
+ */
+size_t prq_moe_layer_workspace_bytes(int32_t M, int32_t k, int32_t E, int32_t H, int32_t I, int32_t k_tail, int32_t N);
+int prq_moe_layer(const void* x_bf16, int64_t ld_x, int32_t M, const int32_t* ids, const float* weights, int32_t k,
+                  const uint8_t* up_Wp, const uint8_t* up_Wps, const uint8_t* down_Wp, const uint8_t* down_Wps,
+                  int32_t E, int32_t H, int32_t I, int32_t k_tail, int32_t N, void* out, int64_t ld_out,
+                  void* workspace, size_t workspace_bytes, hipStream_t stream);
+
 #ifdef __cplusplus
 }
 #endif

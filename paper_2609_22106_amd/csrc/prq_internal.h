@@ -248,4 +248,71 @@ hipError_t launch_lora(const LoraPlan& c, const uint16_t* x, int64_t ld_x, int M
                        int segments, int N, const float* Y, int64_t ld_y, float* out, int64_t ld_out,
                        void* workspace, hipStream_t stream);
 
+// The mixture-of-experts half of a layer.
+// block_norm.hip.  Rows of H (a multiple of 8, up to kMaxNormWidth); y, residual and the outputs
+// may be null (include/prq.h); gate_index null: row m of the gate, or its only one.
+constexpr int kMaxNormWidth = 16384;
+struct BlockNormArgs {
+  const void *y, *residual;
+  int64_t ld_y, ld_r;
+  const void *post, *pre, *gate;
+  int64_t ld_gate;
+  const int32_t* gate_index;
+  void* residual_out;
+  int64_t ld_ro;
+  uint16_t* h;
+  int64_t ld_h, M;
+  int H, gate_rows;
+  bool w_bf16, gate_bf16;
+  float offset, eps, a, b;
+};
+hipError_t launch_block_norm(const BlockNormArgs& p, bool y_bf16, bool r_bf16, int num_cus, hipStream_t stream);
+
+// moe_route.hip.  Tokens in blocks of `rows`; with `split` the experts' tiles of a block are in
+// workgroups of their own and the last of them to arrive chooses (workspace: the state head, then
+// the logits).
+struct RoutePlan {
+  bool split = false;
+  int rows = 16;
+  int64_t blocks = 0;
+};
+struct RouteArgs {
+  const uint16_t *x, *w;
+  int64_t ld_x, ld_w;
+  const float* bias;
+  int32_t* ids;
+  float* weights;
+  float* logits;                     // [M][E], or null
+  int64_t ld_logits;
+  int M, E, H, k;
+  bool sigmoid, renormalize;
+  float scale;
+};
+constexpr int kMaxRouteExperts = 1024;
+constexpr int kMaxRouteTop = 32;
+RoutePlan plan_moe_route(int M, int E, int H, int num_cus);
+size_t route_workspace_bytes(const RoutePlan& c, int M, int E);
+hipError_t launch_moe_route(const RoutePlan& c, const RouteArgs& p, void* workspace, hipStream_t stream);
+
+// moe_layer.hip.  Workgroups along the experts of an output tile of the second product.
+constexpr int kMaxLayerTokens = 64;
+constexpr int kMaxLayerTop = 32;
+struct MoePlan {
+  int slots = 0;                     // experts that the tokens can reach
+  int splits = 1;
+};
+struct MoeArgs {
+  const uint16_t* x;
+  int64_t ld_x;
+  const int32_t* ids;
+  const float* weights;
+  const uint8_t *up_codes, *up_scales, *down_codes, *down_scales;
+  uint16_t* out;
+  int64_t ld_out;
+  int M, k, E, H, I, k_tail, N;
+};
+MoePlan plan_moe_layer(const MoeArgs& p, int num_cus);
+size_t moe_workspace_bytes(const MoePlan& c, const MoeArgs& p);
+hipError_t launch_moe_layer(const MoePlan& c, const MoeArgs& p, void* workspace, hipStream_t stream);
+
 }  // namespace prq

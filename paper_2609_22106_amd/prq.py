@@ -100,6 +100,17 @@ _lora_ex = _decl("prq_lora_ex", ctypes.c_int,
                  [_p, _i64, _i32, _i32, _p, _p, _p, _p, _p, _i32, _i32, _i32, _p, _p, _i32, _i32, _p, _i64, _p, _i64,
                   _p, _sz, _p])
 
+ROUTE_SCORINGS = {"softmax": 0, "sigmoid": 1}
+_block_norm = _decl("prq_block_norm", ctypes.c_int,
+                    [_p, _i64, _i32, _p, _i64, _i32, _i32, _i32, _p, _p, _i32, _f32, _p, _i64, _i32, _i32, _p, _f32,
+                     _f32, _f32, _p, _i64, _p, _i64, _p])
+_route_ws = _decl("prq_moe_route_workspace_bytes", _sz, [_i32, _i32, _i32])
+_route = _decl("prq_moe_route", ctypes.c_int,
+               [_p, _i64, _i32, _i32, _p, _i64, _i32, _i32, _i32, _p, _i32, _f32, _p, _p, _p, _i64, _p, _sz, _p])
+_moe_ws = _decl("prq_moe_layer_workspace_bytes", _sz, [_i32, _i32, _i32, _i32, _i32, _i32, _i32])
+_moe = _decl("prq_moe_layer", ctypes.c_int,
+             [_p, _i64, _i32, _p, _p, _i32, _p, _p, _p, _p, _i32, _i32, _i32, _i32, _i32, _p, _i64, _p, _sz, _p])
+
 
 class PRQError(RuntimeError):
     def __init__(self, status, where):
@@ -912,4 +923,162 @@ def prq_lora(x, adapters, segment_offsets, segment_adapter, Y, out=None, workspa
                   segment_offsets.data_ptr(), segment_adapter.data_ptr(), segments, N, Y.data_ptr(), ld_y,
                   out.data_ptr(), ld_out, ws, ws_bytes, _stream_of_call(stream))
     _check(st, "prq_lora")
+    return out
+
+
+# ---------------------------------------------------- mixture-of-experts half ---
+def _on_current_device(x, *others):
+    """The launch goes to the current device: `x` and the tensors beside it must be there."""
+    d = x.get_device()
+    for t in others:
+        if t is not None and t.get_device() != d:
+            raise ValueError(f"tensors on different devices: {x.device}, {t.device}")
+    if d != (torch.cuda.current_device() if _cur_device is None else _cur_device()):
+        raise ValueError(f"the tensors are on {x.device}, which is not the current device")
+
+
+def prq_block_norm(y, residual, pre_weight=None, post_weight=None, gate=None, gate_index=None, eps=1e-6,
+                   weight_offset=0.0, residual_scale=1.0, block_scale=1.0, out=None, residual_out=None, stream=None):
+    """A block's output y and the residual, [M, H] float32 or bf16 -> (h, r') with
+    u = y, or y / rms(y) * (weight_offset + post_weight); r' = residual_scale * residual +
+    block_scale * gate * u; h [M, H] bf16 = r' / rms(r') * (weight_offset + pre_weight).
+
+    y None: no block.  residual None: none, and r' (then y's type) is stored only with residual_out.
+    Else residual_out=None writes r' over residual.  gate: [rows, H] float32 or bf16, one row for
+    all, one for each, or gate_index int32 [M] names each row's (outside: none).  pre_weight None:
+    h is None."""
+    lead = residual if y is None else y
+    if not isinstance(lead, torch.Tensor) or lead.dim() != 2:
+        raise ValueError("y or residual must be [M, H]")
+    M, H = lead.shape
+    ld_y = _rows(y, "y", _ROPE_IN, M, H) if y is not None else 0
+    ld_r, r_type = 0, lead.dtype
+    if residual is not None:
+        ld_r, r_type = _rows(residual, "residual", _ROPE_IN, M, H), residual.dtype
+        if residual_out is None and (y is not None or residual_scale != 1.0):
+            residual_out = residual
+    ld_ro = 0
+    if residual_out is residual:
+        ld_ro = ld_r
+    elif residual_out is not None:
+        ld_ro = _rows(residual_out, "residual_out", (r_type,), M, H)
+    post = pre = None
+    w_kind = 0
+    if pre_weight is not None:
+        pre, w_kind = _head_weight(pre_weight, "pre_weight", H)
+    if post_weight is not None:
+        post, kind = _head_weight(post_weight, "post_weight", H)
+        if pre is not None and kind != w_kind:
+            raise ValueError("post_weight and pre_weight must have one type")
+        w_kind = kind
+    ld_gate = gate_rows = gate_kind = 0
+    gate_at = index_at = None
+    if gate is not None:
+        if not isinstance(gate, torch.Tensor) or gate.dim() != 2:
+            raise ValueError(f"gate must be [rows, {H}]")
+        gate_rows = gate.shape[0]
+        ld_gate, gate_kind, gate_at = _rows(gate, "gate", _ROPE_IN, gate_rows, H), int(gate.dtype is _BF16), gate.data_ptr()
+        if gate_index is not None:
+            _vector(gate_index, "gate_index", _I32, M)
+            index_at = gate_index.data_ptr()
+    elif gate_index is not None:
+        raise ValueError("gate_index needs a gate")
+    h_at, ld_h = None, 0
+    if pre is not None:
+        if out is None:
+            out = _output(None, "out", (M, H), _BF16, lead, stream)
+        ld_h = _rows(out, "out", (_BF16,), M, H)
+        h_at = out.data_ptr()
+    elif out is not None:
+        raise ValueError("out needs pre_weight")
+    _on_current_device(lead, residual, residual_out, pre_weight, post_weight, gate, gate_index, out)
+    if h_at is not None or residual_out is not None:
+        st = _block_norm(None if y is None else y.data_ptr(), ld_y, int(lead.dtype is _BF16),
+                         None if residual is None else residual.data_ptr(), ld_r, int(r_type is _BF16), M, H, post, pre,
+                         w_kind, weight_offset, gate_at, ld_gate, gate_kind, gate_rows, index_at, eps, residual_scale,
+                         block_scale, None if residual_out is None else residual_out.data_ptr(), ld_ro, h_at, ld_h,
+                         _stream_of_call(stream))
+        _check(st, "prq_block_norm")
+    return out, residual if residual_out is None else residual_out
+
+
+def prq_moe_route_workspace_bytes(M, E, H):
+    return int(_route_ws(M, E, H))
+
+
+def _state_workspace(workspace, need, like, stream):
+    """(address, bytes) of a workspace with a state head, made (zeroed) where none is given."""
+    if workspace is None and need:
+        workspace = _alloc(torch.zeros, need, _U8, like.device, stream, kept=False)
+    elif workspace is not None and not _holds(workspace, _U8, 0):
+        _need(workspace, "workspace", _U8)
+        _on_gpu(workspace=workspace)
+    return (None, 0, None) if workspace is None else (workspace.data_ptr(), workspace.numel(), workspace)
+
+
+def prq_moe_route(x, W, k, scoring="softmax", bias=None, renormalize=True, scale=1.0, ids=None, weights=None,
+                  logits=None, workspace=None, stream=None):
+    """x [M, H] bf16, router weight W [E, H] bf16 -> (ids int32 [M, k], weights float32 [M, k]): the k
+    experts with the largest softmax or sigmoid of x W^T (+ bias float32 [E], with the sigmoid),
+    descending, the lower index first among equals, and their scores (renormalize: divided by their
+    sum) times scale.  logits: float32 [M, E] to write x W^T into.  workspace: uint8,
+    prq_moe_route_workspace_bytes, zeroed before its first use and left ready by every call (else
+    allocated, zeroed by another launch)."""
+    if not isinstance(x, torch.Tensor) or x.dim() != 2 or not isinstance(W, torch.Tensor) or W.dim() != 2:
+        raise ValueError("x must be [M, H] and W [E, H]")
+    M, H = x.shape
+    E = W.shape[0]
+    if scoring not in ROUTE_SCORINGS:
+        raise ValueError(f"unknown scoring {scoring!r}")
+    ld_x, ld_w = _rows(x, "x", (_BF16,), M, H), _rows(W, "W", (_BF16,), E, H)
+    if bias is not None:
+        _vector(bias, "bias", _F32, E)
+    if not 1 <= k <= E:
+        raise ValueError(f"k {k} must lie between 1 and the {E} experts")
+    ids = _output(ids, "ids", (M, k), _I32, x, stream)
+    weights = _output(weights, "weights", (M, k), _F32, x, stream)
+    ld_l = _rows(logits, "logits", (_F32,), M, E) if logits is not None else 0
+    ws, ws_bytes, workspace = _state_workspace(workspace, 0 if workspace is not None else _route_ws(M, E, H), x, stream)
+    _on_current_device(x, W, bias, ids, weights, logits, workspace)
+    st = _route(x.data_ptr(), ld_x, M, H, W.data_ptr(), ld_w, E, k, ROUTE_SCORINGS[scoring], _ptr(bias),
+                1 if renormalize else 0, scale, ids.data_ptr(), weights.data_ptr(), _ptr(logits), ld_l, ws, ws_bytes,
+                _stream_of_call(stream))
+    _check(st, "prq_moe_route")
+    return ids, weights
+
+
+def prq_moe_layer_workspace_bytes(M, k, E, H, I, k_tail, N):
+    return int(_moe_ws(M, k, E, H, I, k_tail, N))
+
+
+def prq_moe_layer(x, ids, weights, gate_up, down, k_tail=0, out=None, workspace=None, stream=None):
+    """All experts of up to 64 tokens: x [M, H] bf16, ids int32 and weights float32 [M, k] (prq_moe_route's;
+    an id outside [0, E) adds nothing) -> out [M, N] bf16 = sum_j weights[:, j] * down_e [h; last k_tail of
+    h], h = SiLU(gate_e x) * (up_e x).  gate_up: PackedWeight of E weights [2 I, H], gate rows first;
+    down: of E weights [N, I + k_tail].  workspace: as prq_moe_route's, prq_moe_layer_workspace_bytes."""
+    if not isinstance(x, torch.Tensor) or x.dim() != 2 or not isinstance(ids, torch.Tensor) or ids.dim() != 2:
+        raise ValueError("x must be [M, H] and ids [M, k]")
+    (M, H), k = x.shape, ids.shape[1]
+    E, N, I = gate_up.E, down.N, down.K_aug - k_tail
+    if gate_up.K_aug != H or gate_up.N != 2 * I or down.E != E:
+        raise ValueError(f"gate_up ({gate_up.E} x [{gate_up.N}, {gate_up.K_aug}]) and down ({down.E} x [{down.N}, "
+                         f"{down.K_aug}]) do not fit [2 I, {H}] and [N, I + {k_tail}]")
+    ld_x = _rows(x, "x", (_BF16,), M, H)
+    if not (_is(ids, _I32, (M, k)) and _is(weights, _F32, (M, k)) and _weight_fits(gate_up) and _weight_fits(down)):
+        _need(ids, "ids", _I32, (M, k))
+        _need(weights, "weights", _F32, (M, k))
+        gate_up.check_sizes()
+        down.check_sizes()
+        _on_gpu(ids=ids, weights=weights, gate_up=gate_up.Wp, gate_up_scales=gate_up.Wps, down=down.Wp,
+                down_scales=down.Wps)
+    if out is None:
+        out = _output(None, "out", (M, N), _BF16, x, stream)
+    ld_out = _rows(out, "out", (_BF16,), M, N)
+    ws, ws_bytes, workspace = _state_workspace(workspace, 0 if workspace is not None else
+                                               _moe_ws(M, k, E, H, I, k_tail, N), x, stream)
+    _on_current_device(x, ids, weights, gate_up.Wp, gate_up.Wps, down.Wp, down.Wps, out, workspace)
+    st = _moe(x.data_ptr(), ld_x, M, ids.data_ptr(), weights.data_ptr(), k, gate_up.Wp.data_ptr(), gate_up.Wps.data_ptr(),
+              down.Wp.data_ptr(), down.Wps.data_ptr(), E, H, I, k_tail, N, out.data_ptr(), ld_out, ws, ws_bytes,
+              _stream_of_call(stream))
+    _check(st, "prq_moe_layer")
     return out

@@ -1,0 +1,187 @@
+"""prq_moe_layer against the float64 oracle.
+
+Bar, per output: its rounding (bf16, 2^-8 of the value); the roundings of w h to bf16, each at most
+2^-8 of its value and independent of each other, uniform within their step: a standard deviation of
+at most 2^-8 / sqrt(3) of the root of the squares' sum, six of which cover the outputs checked here;
+and float32 sums: 2^-24 times the number of terms times the magnitudes that are added, in the first
+product (whose errors reach y through h) and the second, with 8 more for SiLU and the products."""
+import numpy as np
+import pytest
+
+torch = pytest.importorskip("torch")
+
+from oracle import moe                                  # noqa: E402
+from paper_2609_22106_amd import inputs                 # noqa: E402
+from tests.gpu_util import dev, say                     # noqa: E402
+
+pytestmark = pytest.mark.gpu
+BF16 = torch.bfloat16
+
+
+def _prq():
+    from paper_2609_22106_amd import prq
+    return prq
+
+
+def _np(t):
+    return t.double().cpu().numpy()
+
+
+class Layer:
+    def __init__(self, E, H, I, tail, N, seed, scale_lo=118, scale_hi=124):
+        rng = np.random.default_rng(seed)
+        up, down = (inputs.random_mxfp4(rng, (E, n), K, scale_lo, scale_hi) for n, K in ((2 * I, H), (N, I + tail)))
+        self.up, self.down = moe.dequantized(*up), moe.dequantized(*down)
+        self.gate_up, self.down_w = (_prq().prq_pack_weight(dev(q), dev(s)) for q, s in (up, down))
+        self.E, self.H, self.I, self.tail, self.N = E, H, I, tail, N
+
+    def __call__(self, x, ids, weights, **kw):
+        return _prq().prq_moe_layer(x, ids, weights, self.gate_up, self.down_w, k_tail=self.tail, **kw)
+
+    def check(self, got, x, ids, weights):
+        y, size, root, reach = moe.layer(_np(x), ids.cpu().numpy(), _np(weights), self.up, self.down, self.tail)
+        k = ids.shape[1]
+        tol = (2.0 ** -8 * np.abs(y) + 6 * 2.0 ** -8 / np.sqrt(3) * root
+               + 2.0 ** -24 * ((self.H + 8) * reach + (k * (self.I + self.tail) + 8) * size))
+        err = np.abs(_np(got) - y)
+        assert np.all(err <= tol), (float(np.max(err / np.maximum(tol, 1e-300))), np.argwhere(err > tol)[:4])
+
+
+def _routed(M, E, k, seed, H):
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    ids = torch.argsort(torch.rand(M, E, generator=g, device="cuda"), dim=1)[:, :k].to(torch.int32).contiguous()
+    return ((torch.randn(M, H, generator=g, device="cuda") / 4).to(BF16), ids,
+            torch.rand(M, k, generator=g, device="cuda") + 0.1)
+
+
+@pytest.mark.parametrize("M,E,k,H,I,tail,N", [
+    (1, 1, 1, 32, 32, 0, 16), (1, 128, 8, 2048, 96, 32, 64), (2, 3, 2, 160, 64, 64, 48), (7, 16, 2, 1056, 352, 32, 1056),
+    (16, 4, 3, 128, 128, 0, 256), (17, 9, 5, 384, 160, 32, 112), (31, 2, 1, 96, 32, 0, 32), (33, 64, 6, 256, 192, 64, 320),
+    (48, 8, 8, 64, 32, 32, 16), (64, 128, 8, 512, 96, 32, 128), (64, 1, 1, 288, 64, 0, 64), (64, 5, 4, 2080, 416, 96, 80),
+    (64, 300, 32, 64, 32, 0, 32), (3, 4096, 4, 64, 32, 0, 16), (40, 40, 20, 1120, 32, 0, 48), (64, 16, 2, 128, 1408, 0, 1040)])
+def test_matches_oracle(M, E, k, H, I, tail, N):
+    say("experts", M, E, k, H, I, tail, N)
+    layer = Layer(E, H, I, tail, N, seed=M + E)
+    x, ids, w = _routed(M, E, k, M + H, H)
+    out = torch.full((M, N), float("nan"), dtype=BF16, device="cuda")
+    got = layer(x, ids, w, out=out)
+    assert got is out
+    layer.check(got, x, ids, w)
+
+
+@pytest.mark.parametrize("M", [1, 20, 64])
+def test_ids_that_name_nothing_rows_without_experts_and_an_expert_named_twice(M):
+    layer = Layer(6, 128, 64, 32, 96, seed=3)
+    x, ids, w = _routed(M, 6, 4, 5, 128)
+    full = layer(x, ids, w).clone()
+    ids[0, 1], ids[0, 2] = -1, 6
+    ids[0, 3] = ids[0, 0]
+    if M > 8:
+        ids[3] = torch.tensor([1 << 30, -(1 << 31), 7, -5], dtype=torch.int32)
+        ids[8] = 2
+    got = layer(x, ids, w, out=torch.full((M, 96), float("nan"), dtype=BF16, device="cuda"))
+    layer.check(got, x, ids, w)
+    if M > 8:
+        assert not got[3].any()
+        keep = [i for i in range(M) if i not in (0, 3, 8)]
+        layer.check(full, *(_routed(M, 6, 4, 5, 128)))
+        # sums over other numbers of experts may be split elsewhere: equal to rounding, which check has shown
+        assert torch.allclose(got[keep].float(), full[keep].float(), rtol=2 ** -6, atol=1e-3)
+    ids.fill_(-1)
+    assert not layer(x, ids, w, out=torch.full((M, 96), float("nan"), dtype=BF16, device="cuda")).any()
+
+
+def test_all_tokens_at_one_expert():
+    layer = Layer(32, 256, 96, 32, 64, seed=4)
+    x, ids, w = _routed(64, 32, 2, 6, 256)
+    ids[:, 0], ids[:, 1] = 31, -1
+    layer.check(layer(x, ids, w), x, ids, w)
+
+
+def test_nan_and_infinity_stay_in_their_token():
+    layer = Layer(8, 96, 64, 0, 48, seed=5)
+    x, ids, w = _routed(40, 8, 3, 7, 96)
+    want = layer(x, ids, w).clone()
+    x[3, 5], x[17, 95], w[20, 1] = float("nan"), float("inf"), float("nan")
+    got = layer(x, ids, w)
+    keep = torch.ones(40, dtype=torch.bool, device="cuda")
+    keep[[3, 17, 20]] = False
+    assert torch.equal(got[keep], want[keep])
+    assert bool(torch.isnan(got[3]).all()) and bool(torch.isnan(got[20]).all()) and not bool(torch.isfinite(got[17]).all())
+
+
+@pytest.mark.parametrize("lo,hi", [(1, 20), (60, 70), (127, 127), (150, 180)])
+def test_scale_codes_far_from_one(lo, hi):
+    """Each E8M0 code as the power of two that it is: one weight of ones in either product."""
+    prq = _prq()
+    H = I = 32
+    N = 16
+    for code in range(lo, hi + 1):
+        up_q, up_s = np.zeros((1, 2 * I, H // 2), np.uint8), np.full((1, 2 * I, 1), 127, np.uint8)
+        for r in range(2 * I):                                       # row r: 1 at column r % 32
+            up_q[0, r, (r % 32) // 2] = 2 << (4 * (r % 2))
+        up_s[0, I:] = code                                           # the up-projection's rows: 2^(code - 127)
+        down_q, down_s = np.zeros((1, N, I // 2), np.uint8), np.full((1, N, 1), 127, np.uint8)
+        for r in range(N):
+            down_q[0, r, r // 2] = 2 << (4 * (r % 2))
+        x = torch.full((1, H), 64.0, dtype=BF16, device="cuda")       # SiLU(64) is 64 in bf16
+        ids, w = torch.zeros(1, 1, dtype=torch.int32, device="cuda"), torch.ones(1, 1, device="cuda")
+        pack = lambda q, s: prq.prq_pack_weight(dev(q), dev(s))       # noqa: E731
+        got = prq.prq_moe_layer(x, ids, w, pack(up_q, up_s), pack(down_q, down_s))
+        assert bool((got.double() == 4096.0 * 2.0 ** (code - 127)).all()), code
+        down_s[:] = code
+        up_s[:] = 127
+        got = prq.prq_moe_layer(x, ids, w, pack(up_q, up_s), pack(down_q, down_s))
+        assert bool((got.double() == 4096.0 * 2.0 ** (code - 127)).all()), code
+
+
+def test_strides_and_a_shared_workspace():
+    """Rows of wider tensors; one workspace for layers of several sizes in turn, left ready by each."""
+    prq = _prq()
+    a, b = Layer(64, 256, 224, 32, 512, seed=8), Layer(3, 64, 32, 0, 16, seed=9)
+    ws = torch.zeros(8 << 20, dtype=torch.uint8, device="cuda")
+    for M, layer in ((64, a), (1, b), (33, a), (64, b), (64, a)):
+        x, ids, w = _routed(M, layer.E, 3, M, layer.H)
+        wide = torch.full((M, layer.H + 8), float("nan"), dtype=BF16, device="cuda")
+        wide[:, :layer.H] = x
+        buf = torch.full((M + 1, layer.N + 24), 7.0, dtype=BF16, device="cuda")
+        got = layer(wide[:, :layer.H], ids, w, out=buf[:M, :layer.N], workspace=ws)
+        layer.check(got, x, ids, w)
+        assert bool((buf[:, layer.N:] == 7).all()) and bool((buf[M:] == 7).all())
+        assert not ws[:16384].any()
+        assert torch.equal(layer(x, ids, w, workspace=ws), got)      # the same bits again
+        ws[16384:] = 255                                             # (NaN) nothing is read that was not written
+    assert prq.prq_moe_layer_workspace_bytes(64, 3, 64, 256, 224, 32, 512) <= ws.numel()
+
+
+def test_zero_tokens():
+    layer = Layer(2, 32, 32, 0, 16, seed=1)
+    x, ids, w = (torch.empty(0, 32, dtype=BF16, device="cuda"), torch.empty(0, 2, dtype=torch.int32, device="cuda"),
+                 torch.empty(0, 2, device="cuda"))
+    assert layer(x, ids, w).shape == (0, 16)
+
+
+def test_tail_of_a_prepared_weight():
+    """Gate and up rows from prq_expand_producer (its first I), the down-projection from prq_prepare: the
+    layer computes the augmented product on unquantized activations."""
+    from oracle import prquant as pq
+    prq = _prq()
+    rng = np.random.default_rng(12)
+    H, I, N, tail = 128, 96, 64, 32
+    bits = lambda *s: inputs.f32_to_bf16_bits((0.1 * rng.standard_normal(s)).astype(np.float32))   # noqa: E731
+    down, xcal, up, gate = bits(N, I), bits(16, I), bits(I, H), bits(I, H)
+    art = prq.prq_prepare(down, xcal, 0.5, tail)
+    up_aug, gate_aug = prq.prq_expand_producer(up, gate, art["inv_scale"], art["perm"], tail)
+    both = np.concatenate([gate_aug[:I], up_aug[:I]])
+    first = prq.prq_prepare(both, both[:1], 0.0, 0, "none")
+    layer = object.__new__(Layer)
+    layer.E, layer.H, layer.I, layer.tail, layer.N = 1, H, I, tail, N
+    layer.up = moe.dequantized(first["Wq"], first["Wsc"])[None]
+    layer.down = moe.dequantized(art["Wq"], art["Wsc"])[None]
+    layer.gate_up = prq.prq_pack_weight(dev(first["Wq"]), dev(first["Wsc"]))
+    layer.down_w = prq.prq_pack_weight(dev(art["Wq"]), dev(art["Wsc"]))
+    x, ids, w = _routed(5, 1, 1, 13, H)
+    layer.check(layer(x, ids, w), x, ids, w)
+    np.testing.assert_array_equal(first["perm"], np.arange(H))       # own order
+    assert np.all(first["scale"] == 1)
+    assert pq.prepare(both, both[:1], 0.0, 0, "none")["Wq"].shape == first["Wq"].shape

@@ -1,0 +1,147 @@
+"""prq_moe_route against the float64 oracle.
+
+Logits whose sums are exact in float32 (x and W on a grid of few bits) make the choice exact too: ids
+are compared for equality, ties among them.  Weights: expf and the sums behind them, at most 32
+terms of the chosen or E / 64 + 6 of all, a quotient and a product: 2^-20 of the value.  Before that the
+logit's distance d to the largest one is rounded to float32, which is d 2^-24 of the exponent and so
+of the weight (d is below 8 for the logits on the grid; logits of deviation 45 reach 150, and 150 * 2^-24
+alone is 9 * 2^-20); a weight below float32's normal numbers may be anything down to 0, 2^-126.  The
+sigmoid's are float64 rounded once (2^-24, with 2^-40 for its own chain).  Logits of other inputs: sums of H
+products in float32, 2^-24 H of the magnitudes that are added."""
+import numpy as np
+import pytest
+
+torch = pytest.importorskip("torch")
+
+from oracle import moe                        # noqa: E402
+from tests.gpu_util import say                # noqa: E402
+
+pytestmark = pytest.mark.gpu
+
+
+def _prq():
+    from paper_2609_22106_amd import prq
+    return prq
+
+
+def _np(t):
+    return None if t is None else t.double().cpu().numpy()
+
+
+def _grid(M, E, H, seed):
+    """Products are multiples of 2^-13 and sums stay below 2^11: 24 bits hold them in any order."""
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    x = (torch.round(torch.randn(M, H, generator=g, device="cuda") * 16) / 16).clamp(-7, 7)
+    w = torch.round(torch.randn(E, H, generator=g, device="cuda") * (512 / H ** 0.5)).clamp(-255, 255) / 512
+    bias = 0.1 * torch.randn(E, generator=g, device="cuda")
+    assert float((x.abs() @ w.abs().t()).max()) < 2 ** 11 if M else True
+    return x.bfloat16(), w.bfloat16(), bias
+
+
+def _check(got, logits, k, sigmoid=False, bias=None, renormalize=True, scale=1.0):
+    ids, weights = got
+    want_ids, want = moe.route(logits, k, sigmoid, _np(bias), renormalize, scale)
+    np.testing.assert_array_equal(ids.cpu().numpy(), want_ids)
+    tol = 2.0 ** -23
+    if not sigmoid:
+        chosen = np.take_along_axis(logits, want_ids, 1)
+        tol = 2.0 ** -20 + 2.0 ** -24 * (chosen[:, :1] - chosen)
+    assert np.all(np.abs(_np(weights) - want) <= tol * np.abs(want) + 2.0 ** -126)
+
+
+SIZES = [(1, 128, 8, 2048), (1, 1, 1, 8), (3, 5, 5, 40), (17, 16, 2, 1056), (16, 17, 3, 136), (64, 64, 6, 2560),
+         (33, 1024, 32, 256), (1000, 250, 8, 512), (1025, 128, 8, 256), (1100, 16, 4, 1056), (1030, 32, 32, 64),
+         (1027, 40, 1, 328), (1033, 1000, 10, 128), (1029, 512, 8, 64), (4100, 128, 8, 128), (2048, 60, 4, 24)]
+
+
+@pytest.mark.parametrize("M,E,k,H", SIZES)
+@pytest.mark.parametrize("sigmoid,renormalize", [(False, True), (False, False), (True, True), (True, False)])
+def test_matches_oracle(M, E, k, H, sigmoid, renormalize):
+    say("route", M, E, k, H, sigmoid, renormalize)
+    x, w, bias = _grid(M, E, H, M + E + H)
+    logits = torch.full((M, E), float("nan"), device="cuda")
+    got = _prq().prq_moe_route(x, w, k, scoring="sigmoid" if sigmoid else "softmax", bias=bias if sigmoid else None,
+                               renormalize=renormalize, scale=2.5, logits=logits)
+    want = _np(x) @ _np(w).T
+    np.testing.assert_array_equal(_np(logits), want)
+    _check(got, want, k, sigmoid, bias if sigmoid else None, renormalize, 2.5)
+
+
+@pytest.mark.parametrize("M", [5, 1200])
+def test_sums_of_any_values(M):
+    g = torch.Generator(device="cuda").manual_seed(M)
+    x, w = torch.randn(M, 2048, generator=g, device="cuda").bfloat16(), torch.randn(128, 2048, generator=g, device="cuda").bfloat16()
+    logits = torch.empty(M, 128, device="cuda")
+    got = _prq().prq_moe_route(x, w, 8, logits=logits)
+    far = 2.0 ** -24 * 2048 * (np.abs(_np(x)) @ np.abs(_np(w)).T)
+    assert np.all(np.abs(_np(logits) - _np(x) @ _np(w).T) <= far)
+    _check(got, _np(logits), 8)                                     # the choice from what the sums came to
+
+
+@pytest.mark.parametrize("M", [4, 1400])
+def test_ties_go_to_the_lowest_index(M):
+    x = torch.zeros(M, 64, dtype=torch.bfloat16, device="cuda")
+    w = torch.randn(130, 64, device="cuda").bfloat16()
+    for kw in (dict(), dict(scoring="sigmoid")):
+        ids, weights = _prq().prq_moe_route(x, w, 7, **kw)
+        assert bool((ids == torch.arange(7, device="cuda")).all()) and bool((weights == weights[0, 0]).all())
+    # a logit of -0 is 0
+    x[:, 0] = 1
+    w.zero_()
+    w[::2, 0] = -0.0
+    assert bool((_prq().prq_moe_route(x, w, 7)[0] == torch.arange(7, device="cuda")).all())
+    # scores that are 1 in 32 bits differ in 64
+    w[:, 0] = 20 + torch.arange(130, device="cuda") % 64 / 8
+    ids, _ = _prq().prq_moe_route(x, w, 4, scoring="sigmoid")
+    assert ids[0].tolist() == [63, 127, 62, 126]
+
+
+@pytest.mark.parametrize("M", [6, 1300])
+@pytest.mark.parametrize("sigmoid", [False, True])
+def test_nan_and_infinite_logits(M, sigmoid):
+    """NaN behind everything, infinities in their place; other rows are as they were."""
+    x = torch.zeros(M, 8, dtype=torch.bfloat16, device="cuda")
+    x[:, 0] = 1
+    w = torch.zeros(70, 8, dtype=torch.bfloat16, device="cuda")
+    w[:, 0] = torch.arange(70, device="cuda") / 8
+    run = lambda **kw: _prq().prq_moe_route(x, w, 5, scoring="sigmoid" if sigmoid else "softmax", **kw)   # noqa: E731
+    want = [t.clone() for t in run()]
+    x[2, 1] = float("nan")
+    x[3, 1] = 1                                  # row 3 alone meets these
+    w[69, 1], w[3, 1], w[68, 1] = float("nan"), float("inf"), -float("inf")
+    # 0 * inf and 0 * nan are NaN for the other rows: give them their own column
+    ids, weights = run()
+    assert ids[2].tolist() == [0, 1, 2, 3, 4]    # all NaN
+    assert bool(torch.isnan(weights[2]).all())
+    assert ids[3].tolist() == [3, 67, 66, 65, 64]
+    if sigmoid:
+        assert bool(torch.isfinite(weights[3]).all())
+    # experts 3, 68 and 69 are NaN for everybody else
+    assert ids[0].tolist() == [67, 66, 65, 64, 63] and torch.equal(ids[0], ids[-1])
+    w[:, 1] = 0
+    x[2, 1] = 0
+    for g, t in zip(run(), want):
+        assert torch.equal(g, t)
+
+
+@pytest.mark.parametrize("M", [20, 1280])
+def test_strides_and_a_shared_workspace(M):
+    """Rows of wider tensors; one workspace for calls of several sizes in turn, left ready by each."""
+    prq = _prq()
+    x, w, _ = _grid(M, 96, 128, 11)
+    wide, w_wide = torch.full((M, 200), float("nan"), dtype=torch.bfloat16, device="cuda"), torch.cat([w, w], 1)
+    wide[:, :128] = x
+    ws = torch.zeros(4 << 20, dtype=torch.uint8, device="cuda")
+    logits = torch.full((M, 100), 7.0, device="cuda")
+    ids = torch.full((M + 1, 4), -7, dtype=torch.int32, device="cuda")
+    for m in (M, 1, M, 3):
+        got = prq.prq_moe_route(wide[:m, :128], w_wide[:, :128], 4, logits=logits[:m, :96], workspace=ws, ids=ids[:m])
+        _check(got, _np(x[:m]) @ _np(w).T, 4)
+        assert bool((logits[:, 96:] == 7).all()) and bool((ids[M:] == -7).all())
+        assert not ws[:16384].any()
+
+
+def test_zero_tokens():
+    x, w, _ = _grid(0, 8, 64, 1)
+    ids, weights = _prq().prq_moe_route(x, w, 2)
+    assert ids.shape == weights.shape == (0, 2)
