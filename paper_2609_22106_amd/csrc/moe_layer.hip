@@ -12,7 +12,13 @@
 // The weights of the experts that are reached are most of the bytes, and what bounds both
 // launches; a CU has 80 cycles of matrix work free for every kilobyte of them, so the
 // activations stay in bf16 at no cost and the weights are brought to bf16 in registers (a 4-bit
-// value times a power of two is exact there).
+// value times a power of two is exact there).  A wave asks for four K steps of its weights and
+// the activations that meet them at once; enough waves a CU keep the memory busy meanwhile.
+//
+// A slot is an expert (its number), or where there are fewer pairs of a token and an expert than
+// experts a pair (its first occurrence), so that a launch of `slots` workgroups in y reaches every
+// expert that is named.  An expert's tokens are gathered into columns in ascending order, 16 to a
+// block.  The first launch finds them with a lane a token, and leaves the second a table.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -27,41 +33,16 @@ using dev::f32x4;
 using dev::u32x4v;
 
 constexpr int kWaves = 8, kThreads = 64 * kWaves;
-constexpr int kMaxExperts = 4096;
-constexpr int kMaxPairs = kMaxLayerTokens * kMaxLayerTop;
+constexpr int kSteps = 2;                            // K steps of 128 in a wave's unit
 
-// What a workgroup knows about the routing: every pair's expert, and the experts that some token
-// goes to in ascending order.
-struct Routing {
-  int ids[kMaxPairs];
-  uint32_t reached[kMaxExperts / 32];
-  int experts[kMaxPairs];
+// What the first launch leaves: of every slot the number of its tokens (0: none, or the expert is
+// another slot's), its expert, and for column i the row of `hidden` times 64 plus the token, -1 past
+// the last.
+struct Table {
+  int32_t* counts;
+  int32_t* experts;
+  int32_t* columns;                                  // [slots][64]
 };
-
-// Fills `r` and returns the number of experts.  All threads of the workgroup.
-__device__ __forceinline__ int read_routing(const MoeArgs& p, Routing& r) {
-  const int tid = static_cast<int>(threadIdx.x), lane = tid & 63;
-  const int pairs = p.M * p.k;
-  for (int i = tid; i < kMaxExperts / 32; i += kThreads) r.reached[i] = 0;
-  __syncthreads();
-  for (int i = tid; i < pairs; i += kThreads) {
-    const int e = p.ids[i];
-    r.ids[i] = e;
-    if (e >= 0 && e < p.E) atomicOr(&r.reached[e >> 5], 1u << (e & 31));
-  }
-  __syncthreads();
-  // Lane i: experts 64 i .. 64 i + 63, and how many are reached before them.
-  const int n = __popc(r.reached[2 * lane]) + __popc(r.reached[2 * lane + 1]);
-  const int upto = dev::prefix_sum(n);
-  for (int e = tid; e < ((p.E + 63) & ~63); e += kThreads) {     // a wave's lanes: the 64 experts of one such group
-    const int group = __builtin_amdgcn_readfirstlane(e >> 6);
-    const int before = __builtin_amdgcn_readlane(upto, group) - __builtin_amdgcn_readlane(n, group);
-    const uint64_t mask = static_cast<uint64_t>(r.reached[2 * group + 1]) << 32 | r.reached[2 * group];
-    if (mask >> lane & 1) r.experts[before + __popcll(mask & ((uint64_t{1} << lane) - 1))] = e;
-  }
-  __syncthreads();
-  return __builtin_amdgcn_readlane(upto, 63);
-}
 
 // A lane's 32 weights of a K step (the 16 bytes of an MXFP4 block, its E8M0 code) as the four
 // bf16 operands of the matrix instruction.
@@ -76,192 +57,235 @@ __device__ __forceinline__ void to_bf16(u32x4v w, uint32_t code, u32x4v (&out)[4
   }
 }
 
-// A tile of 16 rows of a packed weight: kilobyte s and the dwords that hold its scales.
-struct Tile {
-  const uint8_t* codes;
-  const uint32_t* scales;
-  __device__ __forceinline__ Tile(const uint8_t* Wp, const uint8_t* Wps, int64_t tile, int steps) {
+// kSteps steps of a packed weight's tile of 16 rows, from a multiple of kSteps on: their kilobytes
+// (the last one's again past the end, for which the activations are zeros) and the dword of their
+// scales.
+struct Unit {
+  u32x4v codes[kSteps];
+  uint32_t scales;
+  __device__ __forceinline__ void load(const uint8_t* Wp, const uint8_t* Wps, int64_t tile, int steps, int unit) {
     const int lane = static_cast<int>(threadIdx.x) & 63;
-    codes = Wp + (tile * steps * 64 + lane) * 16;
-    scales = reinterpret_cast<const uint32_t*>(Wps) + tile * ((steps + 3) >> 2) * 64 + lane;
+    const u32x4v* from = reinterpret_cast<const u32x4v*>(Wp) + tile * steps * 64 + lane;
+    scales = reinterpret_cast<const uint32_t*>(Wps)[(tile * ((steps + 3) >> 2) + (kSteps * unit >> 2)) * 64 + lane] >>
+             (8 * (kSteps * unit & 3));
+#pragma unroll
+    for (int i = 0; i < kSteps; ++i)
+      codes[i] = __builtin_nontemporal_load(from + min(kSteps * unit + i, steps - 1) * 64);
   }
-  __device__ __forceinline__ u32x4v code(int s) const {
-    return *reinterpret_cast<const u32x4v*>(codes + static_cast<int64_t>(s) * 1024);
-  }
-  __device__ __forceinline__ uint32_t scale(int s) const { return scales[(s >> 2) * 64] >> (8 * (s & 3)) & 255u; }
 };
 
-// First launch: one expert's 16 intermediate features (a gate tile and an up tile) for all of its
-// tokens; the waves share the steps of H.  kG: blocks of 16 tokens that an expert can have.
-template <int kG>
-__global__ __launch_bounds__(kThreads) void moe_up_kernel(const MoeArgs p, uint16_t* __restrict__ hidden) {
-  extern __shared__ __align__(16) float red[];       // [kWaves][2][kG][64][4]
-  __shared__ Routing routing;
-  __shared__ int token_of[64], row_of[64];
-  __shared__ float weight_of[64];
-  const int tid = static_cast<int>(threadIdx.x), lane = tid & 63, wave = tid >> 6;
-  const int c = lane & 15, q = lane >> 4;
-  const int n = read_routing(p, routing);
-  if (static_cast<int>(blockIdx.y) >= n) return;
-  const int e = routing.experts[blockIdx.y], tile = static_cast<int>(blockIdx.x);
-
-  if (wave == 0) {                                   // lane t: token t's share of the expert
-    int slot = -1;
-    float w = 0.f;
-    if (lane < p.M)
-      for (int j = 0; j < p.k; ++j)
-        if (routing.ids[lane * p.k + j] == e) {
-          w += p.weights[lane * p.k + j];
-          if (slot < 0) slot = j;
-        }
-    const uint64_t mine = __ballot(slot >= 0);
-    const int at = __popcll(mine & ((uint64_t{1} << lane) - 1));
-    token_of[lane] = -1;
-    dev::wave_lds_barrier();
-    if (slot >= 0) {
-      token_of[at] = lane;
-      row_of[at] = lane * p.k + slot;
-      weight_of[at] = w;
-    }
-  }
-  __syncthreads();
-
-  const int steps = (p.H + 127) >> 7, tiles = p.I >> 4;
-  const int64_t first = static_cast<int64_t>(e) * 2 * tiles + tile;
-  const Tile gate(p.up_codes, p.up_scales, first, steps), up(p.up_codes, p.up_scales, first + tiles, steps);
-  const uint16_t* x[kG];
-  int groups = 0;
+// The columns' activations of a unit: lane (c, q) gets elements 32 q .. 32 q + 31 of each step, zeros
+// for a column without a token (row null).  whole: a row's elements; K: the weight's, of which those
+// past `whole` meet the row's last ones again, and zeros are behind.
+__device__ __forceinline__ void load_columns(const uint16_t* row, int unit, int whole, int K, u32x4v (&b)[kSteps][4]) {
+  const int q = (static_cast<int>(threadIdx.x) >> 4) & 3;
 #pragma unroll
-  for (int g = 0; g < kG; ++g) {
-    const int t = token_of[16 * g + c];
-    x[g] = t < 0 ? nullptr : p.x + t * p.ld_x;
-    if (token_of[16 * g] >= 0) groups = g + 1;
-  }
-  f32x4 acc[2][kG] = {};
-  for (int s = wave; s < steps; s += kWaves) {
-    u32x4v a[2][4];
-    to_bf16(gate.code(s), gate.scale(s), a[0]);
-    to_bf16(up.code(s), up.scale(s), a[1]);
-    const int at = 128 * s + 32 * q;
+  for (int i = 0; i < kSteps; ++i) {
+    const int k = 128 * (kSteps * unit + i) + 32 * q;
+    const bool in = row && k < K;
+    const u32x4v* from = reinterpret_cast<const u32x4v*>(row + (k < whole ? k : k - (K - whole)));
 #pragma unroll
-    for (int g = 0; g < kG; ++g) {
-      if (g >= groups) break;
-      u32x4v b[4] = {};
-      if (x[g] && at < p.H) {
-        const u32x4v* from = reinterpret_cast<const u32x4v*>(x[g] + at);
-#pragma unroll
-        for (int j = 0; j < 4; ++j) b[j] = from[j];
-      }
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        acc[0][g] = dev::mfma_bf16(a[0][j], b[j], acc[0][g]);
-        acc[1][g] = dev::mfma_bf16(a[1][j], b[j], acc[1][g]);
-      }
-    }
-  }
-  f32x4* sums = reinterpret_cast<f32x4*>(red);
-#pragma unroll
-  for (int g = 0; g < kG; ++g)
-    if (g < groups) {
-      sums[((wave * 2 + 0) * kG + g) * 64 + lane] = acc[0][g];
-      sums[((wave * 2 + 1) * kG + g) * 64 + lane] = acc[1][g];
-    }
-  __syncthreads();
-  for (int g = wave; g < groups; g += kWaves) {
-    f32x4 a = 0.f, b = 0.f;
-#pragma unroll
-    for (int w = 0; w < kWaves; ++w) {
-      a += sums[((w * 2 + 0) * kG + g) * 64 + lane];
-      b += sums[((w * 2 + 1) * kG + g) * 64 + lane];
-    }
-    if (token_of[16 * g + c] >= 0) {                 // column c's features 4 q .. 4 q + 3 of the tile
-      const float w = weight_of[16 * g + c];
-      float h[4];
-#pragma unroll
-      for (int i = 0; i < 4; ++i) h[i] = a[i] / (1.f + expf(-a[i])) * b[i] * w;
-      const dev::u32x2 v = {dev::pack_bf16(h[0], h[1]), dev::pack_bf16(h[2], h[3])};
-      *reinterpret_cast<dev::u32x2*>(hidden + static_cast<int64_t>(row_of[16 * g + c]) * p.I + 16 * tile + 4 * q) = v;
+    for (int j = 0; j < 4; ++j) {
+      b[i][j] = 0u;
+      if (in) b[i][j] = from[j];
     }
   }
 }
 
-// Second launch: 16 output features of all tokens, over the experts that are reached.  Column c of
-// block g is token 16 g + c, so that all experts add into the same registers; the units (an
-// expert's kilobyte of the tile) are dealt evenly to the waves of the tile's workgroups, in
-// order.  The workgroups' sums are added in their order by the one that arrives last.
-template <int kG>
-__global__ __launch_bounds__(kThreads) void moe_down_kernel(const MoeArgs p, const uint16_t* __restrict__ hidden,
-                                                             float* parts, uint32_t* arrived) {
-  __shared__ Routing routing;
-  __shared__ __align__(16) float red[kWaves * kG * 64 * 4];
-  __shared__ int sh_last;
-  const int tid = static_cast<int>(threadIdx.x), lane = tid & 63, wave = tid >> 6;
-  const int c = lane & 15, q = lane >> 4;
-  const int n = read_routing(p, routing);
-  const int tile = static_cast<int>(blockIdx.x), splits = static_cast<int>(gridDim.y), part = static_cast<int>(blockIdx.y);
-  const int K = p.I + p.k_tail, steps = (K + 127) >> 7;
-  const int units = n * steps, shares = splits * kWaves, share = part * kWaves + wave;
-  int u = static_cast<int>(static_cast<int64_t>(units) * share / shares);
-  const int end = static_cast<int>(static_cast<int64_t>(units) * (share + 1) / shares);
-
-  f32x4 acc[kG] = {};
-  while (u < end) {
-    const int e = routing.experts[u / steps];
-    int s = u % steps;
-    const int stop = min(steps, s + end - u);
-    u += stop - s;
-    const Tile down(p.down_codes, p.down_scales, static_cast<int64_t>(e) * (p.N >> 4) + tile, steps);
-    int row = -1;                                    // lane t: where token t's share of the expert is
-    if (lane < p.M)
-      for (int j = p.k - 1; j >= 0; --j)
-        if (routing.ids[lane * p.k + j] == e) row = lane * p.k + j;
-    const uint64_t mine = __ballot(row >= 0);
-    const uint16_t* h[kG];
+// A lane's token's share of expert e: whether it has one, the first of its k ids that names it, and
+// the sum of the weights that do.
+struct Share {
+  bool has = false;
+  int first = 0;
+  float weight = 0.f;
+  __device__ __forceinline__ Share(const MoeArgs& p, int e) {
+    const int lane = static_cast<int>(threadIdx.x) & 63;
+    if (lane >= p.M) return;
+    const int32_t* ids = p.ids + lane * p.k;
+    for (int j0 = 0; j0 < p.k; j0 += 8) {
+      int id[8];
 #pragma unroll
-    for (int g = 0; g < kG; ++g) {
-      const int at = __shfl(row, 16 * g + c, 64);
-      h[g] = at < 0 ? nullptr : hidden + static_cast<int64_t>(at) * p.I;
-    }
-    for (; s < stop; ++s) {
-      u32x4v a[4];
-      to_bf16(down.code(s), down.scale(s), a);
-      int at = 128 * s + 32 * q;
-      const bool in = at < K;
-      if (at >= p.I) at -= p.k_tail;                 // the tail meets the last values again
+      for (int j = 0; j < 8; ++j) id[j] = j0 + j < p.k ? ids[j0 + j] : -1;
 #pragma unroll
-      for (int g = 0; g < kG; ++g) {
-        if (!(mine >> (16 * g) & 0xFFFF)) continue;
-        u32x4v b[4] = {};
-        if (h[g] && in) {
-          const u32x4v* from = reinterpret_cast<const u32x4v*>(h[g] + at);
-#pragma unroll
-          for (int j = 0; j < 4; ++j) b[j] = from[j];
+      for (int j = 0; j < 8; ++j)
+        if (id[j] == e) {                            // (e >= 0)
+          weight += p.weights[lane * p.k + j0 + j];
+          if (!has) first = j0 + j;
+          has = true;
         }
+    }
+  }
+};
+
+// First launch: a wave has 16 intermediate features of one expert (a gate tile and an up tile) for
+// all of its tokens, and of the steps of H every kS-th unit.
+template <int kS>
+__global__ __launch_bounds__(kThreads, 4) void moe_up_kernel(const MoeArgs p, bool by_expert,
+                                                              uint16_t* __restrict__ hidden, const Table table) {
+  constexpr int kTiles = kWaves / kS;
+  __shared__ f32x4 sums[kS > 1 ? kWaves * 2 * 64 : 1];
+  const int lane = static_cast<int>(threadIdx.x) & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x) >> 6);
+  const int c = lane & 15, q = lane >> 4;
+  const int slot = static_cast<int>(blockIdx.y);
+  const int tile = static_cast<int>(blockIdx.x) * kTiles + wave / kS, part = wave % kS;
+  const int steps = (p.H + 127) >> 7, tiles = p.I >> 4, units = (steps + kSteps - 1) / kSteps;
+
+  const int e = by_expert ? slot : p.ids[slot];
+  const bool reached = e >= 0 && e < p.E;
+  const Share share(p, reached ? e : -2);
+  const uint64_t mine = __ballot(share.has);
+  int n = __popcll(mine);
+  if (!by_expert) {                                  // an earlier pair of the same expert has it
+    const int token = slot / p.k;
+    if (__ballot(share.has && (lane < token || (lane == token && lane * p.k + share.first < slot)))) n = 0;
+  }
+  // Column i: the i-th token.  Lanes without a share go behind the others.
+  const uint64_t below = (uint64_t{1} << lane) - 1;
+  const int at = share.has ? __popcll(mine & below) : __popcll(mine) + __popcll(~mine & below);
+  const int row = share.has ? lane * p.k + share.first : -1;
+  const int entry = share.has ? row * 64 + lane : -1;
+  const int column = __builtin_amdgcn_ds_permute(4 * at, entry);
+  if (blockIdx.x == 0 && wave == 0) {
+    if (lane == 0) {
+      table.counts[slot] = n;
+      table.experts[slot] = e;
+    }
+    table.columns[slot * 64 + lane] = column;
+  }
+  if (n == 0) return;                                // the whole workgroup
+  const float weight = __int_as_float(__builtin_amdgcn_ds_permute(4 * at, __float_as_int(share.weight)));
+
+  const int64_t first = static_cast<int64_t>(e) * 2 * tiles + tile;
+  for (int g = 0; 16 * g < n; ++g) {                 // (more than 16 tokens: the weights come from L2 again)
+    const int col = __shfl(column, 16 * g + c, 64);
+    f32x4 z = 0.f, y = 0.f;
+    if (tile < tiles) {
+      const uint16_t* x = col < 0 ? nullptr : p.x + (col & 63) * p.ld_x;
+      for (int u = part; u < units; u += kS) {
+        Unit gate, up;
+        gate.load(p.up_codes, p.up_scales, first, steps, u);
+        up.load(p.up_codes, p.up_scales, first + tiles, steps, u);
+        u32x4v b[kSteps][4];
+        load_columns(x, u, p.H, p.H, b);
 #pragma unroll
-        for (int j = 0; j < 4; ++j) acc[g] = dev::mfma_bf16(a[j], b[j], acc[g]);
+        for (int i = 0; i < kSteps; ++i) {
+          u32x4v a[4];
+          to_bf16(gate.codes[i], gate.scales >> (8 * i) & 255u, a);
+#pragma unroll
+          for (int j = 0; j < 4; ++j) z = dev::mfma_bf16(a[j], b[i][j], z);
+          to_bf16(up.codes[i], up.scales >> (8 * i) & 255u, a);
+#pragma unroll
+          for (int j = 0; j < 4; ++j) y = dev::mfma_bf16(a[j], b[i][j], y);
+        }
       }
     }
-  }
-  f32x4* sums = reinterpret_cast<f32x4*>(red);
+    if constexpr (kS > 1) {
+      if (g) __syncthreads();
+      sums[(wave * 2) * 64 + lane] = z;
+      sums[(wave * 2 + 1) * 64 + lane] = y;
+      __syncthreads();
+      if (part) continue;
 #pragma unroll
-  for (int g = 0; g < kG; ++g) sums[(wave * kG + g) * 64 + lane] = acc[g];
+      for (int w = 1; w < kS; ++w) {
+        z += sums[((wave + w) * 2) * 64 + lane];
+        y += sums[((wave + w) * 2 + 1) * 64 + lane];
+      }
+    }
+    // column c's features 4 q .. 4 q + 3 of the tile
+    const float w = __shfl(weight, 16 * g + c, 64);
+    if (col >= 0 && tile < tiles) {
+      float h[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) h[i] = z[i] / (1.f + expf(-z[i])) * y[i] * w;
+      const dev::u32x2 v = {dev::pack_bf16(h[0], h[1]), dev::pack_bf16(h[2], h[3])};
+      *reinterpret_cast<dev::u32x2*>(hidden + static_cast<int64_t>(col >> 6) * p.I + 16 * tile + 4 * q) = v;
+    }
+  }
+}
+
+// Second launch: 16 output features of all tokens.  The units of the experts that are reached are
+// dealt evenly, in order, to the waves of the tile's workgroups.  A unit's columns are its expert's
+// tokens; their sums are added to the tokens' in LDS, of which each wave has its own.  The waves'
+// sums are added in their order, the workgroups' in theirs, by the one that arrives last.
+__global__ __launch_bounds__(kThreads, 4) void moe_down_kernel(const MoeArgs p, const uint16_t* __restrict__ hidden,
+                                                                const Table table, int slots, float* parts,
+                                                                uint32_t* arrived) {
+  extern __shared__ __align__(16) float own[];       // [kWaves][M][16]
+  __shared__ int sh_last;
+  const int tid = static_cast<int>(threadIdx.x), lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int c = lane & 15, q = lane >> 4;
+  const int tile = static_cast<int>(blockIdx.x), splits = static_cast<int>(gridDim.y), part = static_cast<int>(blockIdx.y);
+  const int K = p.I + p.k_tail, steps = (K + 127) >> 7, units = (steps + kSteps - 1) / kSteps;
+  f32x4* mine = reinterpret_cast<f32x4*>(own) + wave * p.M * 4;
+  for (int i = lane; i < p.M * 4; i += 64) mine[i] = 0.f;
+  dev::wave_lds_barrier();
+
+  // The slots with tokens, 64 at a time.
+  auto there = [&](int base) { return __ballot(base + lane < slots && table.counts[min(base + lane, slots - 1)] > 0); };
+  int n = 0;
+  for (int base = 0; base < slots; base += 64) n += __popcll(there(base));
+  const int64_t all = static_cast<int64_t>(n) * units;
+  const int shares = splits * kWaves, share = part * kWaves + wave;
+  int u = static_cast<int>(all * share / shares);
+  const int end = static_cast<int>(all * (share + 1) / shares);
+
+  if (u < end) {
+    int skip = u / units, base = 0;
+    uint64_t left = there(0);
+    for (; __popcll(left) <= skip; left = there(base)) skip -= __popcll(left), base += 64;
+    for (; skip; --skip) left &= left - 1;
+    while (true) {
+      const int slot = base + __builtin_ctzll(left);
+      const int e = table.experts[slot];
+      const int64_t first = static_cast<int64_t>(e) * (p.N >> 4) + tile;
+      const int column = table.columns[slot * 64 + lane];
+      const int blocks = (table.counts[slot] + 15) >> 4;
+      const int stop = min(u / units * units + units, end);
+      for (; u < stop; ++u) {
+        Unit down;
+        down.load(p.down_codes, p.down_scales, first, steps, u % units);
+        for (int g = 0; g < blocks; ++g) {
+          const int col = __shfl(column, 16 * g + c, 64);
+          u32x4v b[kSteps][4];
+          load_columns(col < 0 ? nullptr : hidden + static_cast<int64_t>(col >> 6) * p.I, u % units, p.I, K, b);
+          f32x4 acc = 0.f;
+#pragma unroll
+          for (int i = 0; i < kSteps; ++i) {
+            u32x4v a[4];
+            to_bf16(down.codes[i], down.scales >> (8 * i) & 255u, a);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) acc = dev::mfma_bf16(a[j], b[i][j], acc);
+          }
+          if (col >= 0) mine[(col & 63) * 4 + q] += acc;
+          dev::wave_lds_barrier();
+        }
+      }
+      if (u >= end) break;
+      left &= left - 1;
+      while (!left) base += 64, left = there(base);
+    }
+  }
   __syncthreads();
-  const int g = wave;                                // wave g: block g
-  const int t = 16 * g + c;
+  // Thread (t, i): token t's features 4 i .. 4 i + 3.
+  const int t = tid >> 2, i = tid & 3;
+  const bool here = t < p.M;
+  const f32x4* sums = reinterpret_cast<const f32x4*>(own);
   f32x4 y = 0.f;
-  if (g < kG) {
+  if (here) {
 #pragma unroll
-    for (int w = 0; w < kWaves; ++w) y += sums[(w * kG + g) * 64 + lane];
+    for (int w = 0; w < kWaves; ++w) y += sums[(w * p.M + t) * 4 + i];
   }
-  const bool here = g < kG && t < p.M;
-  const int64_t at = static_cast<int64_t>(t) * p.N + 16 * tile + 4 * q;
+  const int64_t at = static_cast<int64_t>(t) * p.N + 16 * tile + 4 * i;
   if (splits > 1) {
-    const int64_t all = static_cast<int64_t>(p.M) * p.N;
+    const int64_t stride = static_cast<int64_t>(p.M) * p.N;
     if (here) {
       // device scope: the last workgroup may be on another XCD with an L2 of its own
-      for (int i = 0; i < 4; i += 2)
-        __hip_atomic_store(reinterpret_cast<uint64_t*>(parts + part * all + at + i),
-                           static_cast<uint64_t>(__float_as_uint(y[i + 1])) << 32 | __float_as_uint(y[i]),
+#pragma unroll
+      for (int j = 0; j < 4; j += 2)
+        __hip_atomic_store(reinterpret_cast<uint64_t*>(parts + part * stride + at + j),
+                           static_cast<uint64_t>(__float_as_uint(y[j + 1])) << 32 | __float_as_uint(y[j]),
                            __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     }
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");       // what this wave has stored is there
@@ -274,61 +298,69 @@ __global__ __launch_bounds__(kThreads) void moe_down_kernel(const MoeArgs p, con
     if (tid == 0) __hip_atomic_store(arrived + tile, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     if (here) {
       y = 0.f;
-      for (int w = 0; w < splits; ++w)
-        for (int i = 0; i < 4; i += 2) {
-          const uint64_t v = __hip_atomic_load(reinterpret_cast<const uint64_t*>(parts + w * all + at + i),
+      for (int w = 0; w < splits; ++w) {
+#pragma unroll
+        for (int j = 0; j < 4; j += 2) {
+          const uint64_t v = __hip_atomic_load(reinterpret_cast<const uint64_t*>(parts + w * stride + at + j),
                                                __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-          y[i] += __uint_as_float(static_cast<uint32_t>(v));
-          y[i + 1] += __uint_as_float(static_cast<uint32_t>(v >> 32));
+          y[j] += __uint_as_float(static_cast<uint32_t>(v));
+          y[j + 1] += __uint_as_float(static_cast<uint32_t>(v >> 32));
         }
+      }
     }
   }
   if (here) {
     const dev::u32x2 v = {dev::pack_bf16(y[0], y[1]), dev::pack_bf16(y[2], y[3])};
-    *reinterpret_cast<dev::u32x2*>(p.out + t * p.ld_out + 16 * tile + 4 * q) = v;
+    *reinterpret_cast<dev::u32x2*>(p.out + t * p.ld_out + 16 * tile + 4 * i) = v;
   }
 }
 
-size_t hidden_bytes(const MoeArgs& p) { return (static_cast<size_t>(p.M) * p.k * p.I * 2 + 255) & ~size_t{255}; }
+size_t up16(size_t n) { return (n + 15) & ~size_t{15}; }
+size_t hidden_bytes(const MoeArgs& p) { return up16(static_cast<size_t>(p.M) * p.k * p.I * 2); }
+size_t table_bytes(const MoePlan& c) { return up16(static_cast<size_t>(c.slots) * 4 * (2 + 64)); }
 
 }  // namespace
 
 MoePlan plan_moe_layer(const MoeArgs& p, int num_cus) {
   MoePlan c;
   c.slots = std::min(p.E, p.M * p.k);
-  const int64_t units = static_cast<int64_t>(c.slots) * ((p.I + p.k_tail + 127) / 128);
-  while (c.splits < 8 && static_cast<int64_t>(p.N / 16) * c.splits < 2 * num_cus && units >= 2 * c.splits * kWaves * 4)
+  c.by_expert = c.slots == p.E;
+  // The first launch: 16 waves a CU, by parts of H where the tiles are fewer.
+  const int64_t tiles = static_cast<int64_t>(p.I / 16) * c.slots;
+  const int up_units = (p.H + 128 * kSteps - 1) / (128 * kSteps);
+  while (c.parts < kWaves && c.parts < up_units && tiles * c.parts < 16 * num_cus) c.parts *= 2;
+  const int64_t units = static_cast<int64_t>(c.slots) * ((p.I + p.k_tail + 128 * kSteps - 1) / (128 * kSteps));
+  while (c.splits < 8 && static_cast<int64_t>(p.N / 16) * c.splits < 2 * num_cus && units >= 4 * c.splits * kWaves)
     c.splits *= 2;
   return c;
 }
 
 size_t moe_workspace_bytes(const MoePlan& c, const MoeArgs& p) {
-  return kWorkspaceStateBytes + hidden_bytes(p) +
+  return kWorkspaceStateBytes + hidden_bytes(p) + table_bytes(c) +
          (c.splits > 1 ? static_cast<size_t>(c.splits) * p.M * p.N * 4 : 0);
 }
 
 hipError_t launch_moe_layer(const MoePlan& c, const MoeArgs& p, void* workspace, hipStream_t stream) {
   char* at = static_cast<char*>(workspace);
   uint32_t* arrived = reinterpret_cast<uint32_t*>(at);
-  uint16_t* hidden = reinterpret_cast<uint16_t*>(at + kWorkspaceStateBytes);
-  float* parts = reinterpret_cast<float*>(at + kWorkspaceStateBytes + hidden_bytes(p));
-  auto go = [&](auto blocks) {
-    constexpr int kG = decltype(blocks)::value;
-    const int lds = kWaves * 2 * kG * 64 * 16;
-    if (lds > 32 * 1024) {
-      const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(&moe_up_kernel<kG>),
-                                               hipFuncAttributeMaxDynamicSharedMemorySize, lds);
-      if (e != hipSuccess) return e;
-    }
-    moe_up_kernel<kG><<<dim3(p.I / 16, c.slots), kThreads, lds, stream>>>(p, hidden);
-    const hipError_t e = hipGetLastError();
-    if (e != hipSuccess) return e;
-    moe_down_kernel<kG><<<dim3(p.N / 16, c.splits), kThreads, 0, stream>>>(p, hidden, parts, arrived);
-    return hipGetLastError();
+  uint16_t* hidden = reinterpret_cast<uint16_t*>(at += kWorkspaceStateBytes);
+  int32_t* const ints = reinterpret_cast<int32_t*>(at += hidden_bytes(p));
+  const Table table{ints, ints + c.slots, ints + 2 * c.slots};
+  float* parts = reinterpret_cast<float*>(at += table_bytes(c));
+  auto up = [&](auto shared) {
+    constexpr int kS = decltype(shared)::value, kTiles = kWaves / kS;
+    moe_up_kernel<kS><<<dim3((p.I / 16 + kTiles - 1) / kTiles, c.slots), kThreads, 0, stream>>>(p, c.by_expert, hidden,
+                                                                                                 table);
   };
-  if (p.M <= 16) return go(std::integral_constant<int, 1>{});
-  if (p.M <= 32) return go(std::integral_constant<int, 2>{});
-  return go(std::integral_constant<int, 4>{});
+  if (c.parts == 1) up(std::integral_constant<int, 1>{});
+  else if (c.parts == 2) up(std::integral_constant<int, 2>{});
+  else if (c.parts == 4) up(std::integral_constant<int, 4>{});
+  else up(std::integral_constant<int, 8>{});
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  moe_down_kernel<<<dim3(p.N / 16, c.splits), kThreads, kWaves * p.M * 16 * 4, stream>>>(p, hidden, table, c.slots,
+                                                                                         parts, arrived);
+  return hipGetLastError();
 }
 
 }  // namespace prq

@@ -294,12 +294,15 @@ RoutePlan plan_moe_route(int M, int E, int H, int num_cus);
 size_t route_workspace_bytes(const RoutePlan& c, int M, int E);
 hipError_t launch_moe_route(const RoutePlan& c, const RouteArgs& p, void* workspace, hipStream_t stream);
 
-// moe_layer.hip.  Workgroups along the experts of an output tile of the second product.
+// moe_layer.hip.  Slots: workgroups along the experts, one for each, or for each pair of a token and
+// an expert where those are fewer; waves along H of a tile of the first product; workgroups along
+// the experts of a tile of the second.
 constexpr int kMaxLayerTokens = 64;
 constexpr int kMaxLayerTop = 32;
 struct MoePlan {
-  int slots = 0;                     // experts that the tokens can reach
-  int splits = 1;
+  int slots = 0;
+  bool by_expert = true;
+  int parts = 1, splits = 1;
 };
 struct MoeArgs {
   const uint16_t* x;
