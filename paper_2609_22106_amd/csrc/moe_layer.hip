@@ -33,6 +33,7 @@ using dev::f32x4;
 using dev::u32x4v;
 
 constexpr int kWaves = 8, kThreads = 64 * kWaves;
+constexpr int kMaxSplits = 8;                       // workgroups that share output tiles
 constexpr int kSteps = 2;                            // K steps of 128 in a wave's unit
 
 // What the first launch leaves: of every slot the number of its tokens (0: none, or the expert is
@@ -74,24 +75,6 @@ struct Unit {
   }
 };
 
-// The columns' activations of a unit: lane (c, q) gets elements 32 q .. 32 q + 31 of each step, zeros
-// for a column without a token (row null).  whole: a row's elements; K: the weight's, of which those
-// past `whole` meet the row's last ones again, and zeros are behind.
-__device__ __forceinline__ void load_columns(const uint16_t* row, int unit, int whole, int K, u32x4v (&b)[kSteps][4]) {
-  const int q = (static_cast<int>(threadIdx.x) >> 4) & 3;
-#pragma unroll
-  for (int i = 0; i < kSteps; ++i) {
-    const int k = 128 * (kSteps * unit + i) + 32 * q;
-    const bool in = row && k < K;
-    const u32x4v* from = reinterpret_cast<const u32x4v*>(row + (k < whole ? k : k - (K - whole)));
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      b[i][j] = 0u;
-      if (in) b[i][j] = from[j];
-    }
-  }
-}
-
 // A lane's token's share of expert e: whether it has one, the first of its k ids that names it, and
 // the sum of the weights that do.
 struct Share {
@@ -117,15 +100,23 @@ struct Share {
   }
 };
 
+// Rows of x in LDS: kPiece / kG elements of 16 kG tokens at a time, rows 16 bytes past a multiple of
+// 128, at which the lanes of an operand's read meet different banks.
+constexpr int kPiece = 2048;
+constexpr int kPieceUnits = kPiece / (128 * kSteps);
+__host__ __device__ constexpr int pitch_of(int blocks) { return kPiece / blocks * 2 + 16; }   // bytes
+
 // First launch: a wave has 16 intermediate features of one expert (a gate tile and an up tile) for
-// all of its tokens, and of the steps of H every kS-th unit.
+// all of its tokens, and of the steps of H every kS-th unit.  The workgroup's waves share the
+// expert's rows of x in LDS.
 template <int kS>
 __global__ __launch_bounds__(kThreads, 4) void moe_up_kernel(const MoeArgs p, bool by_expert,
                                                               uint16_t* __restrict__ hidden, const Table table) {
   constexpr int kTiles = kWaves / kS;
-  __shared__ f32x4 sums[kS > 1 ? kWaves * 2 * 64 : 1];
-  const int lane = static_cast<int>(threadIdx.x) & 63;
-  const int wave = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x) >> 6);
+  extern __shared__ __align__(16) unsigned char smem[];
+  f32x4* const sums = reinterpret_cast<f32x4*>(smem);       // [kWaves][2][64], behind the rows of x
+  const int tid = static_cast<int>(threadIdx.x), lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int c = lane & 15, q = lane >> 4;
   const int slot = static_cast<int>(blockIdx.y);
   const int tile = static_cast<int>(blockIdx.x) * kTiles + wave / kS, part = wave % kS;
@@ -156,126 +147,263 @@ __global__ __launch_bounds__(kThreads, 4) void moe_up_kernel(const MoeArgs p, bo
   if (n == 0) return;                                // the whole workgroup
   const float weight = __int_as_float(__builtin_amdgcn_ds_permute(4 * at, __float_as_int(share.weight)));
 
-  const int64_t first = static_cast<int64_t>(e) * 2 * tiles + tile;
-  for (int g = 0; 16 * g < n; ++g) {                 // (more than 16 tokens: the weights come from L2 again)
-    const int col = __shfl(column, 16 * g + c, 64);
-    f32x4 z = 0.f, y = 0.f;
-    if (tile < tiles) {
-      const uint16_t* x = col < 0 ? nullptr : p.x + (col & 63) * p.ld_x;
-      for (int u = part; u < units; u += kS) {
-        Unit gate, up;
-        gate.load(p.up_codes, p.up_scales, first, steps, u);
-        up.load(p.up_codes, p.up_scales, first + tiles, steps, u);
-        u32x4v b[kSteps][4];
-        load_columns(x, u, p.H, p.H, b);
+  const bool work = tile < tiles;
+  const int64_t first = static_cast<int64_t>(e) * 2 * tiles + (work ? tile : 0);
+  // Tokens 16 block0 .. 16 (block0 + kG) - 1 of the expert.
+  auto pass = [&](int block0, auto blocks) {
+    constexpr int kG = decltype(blocks)::value, kUnits = kPieceUnits / kG, kPitch = pitch_of(kG);
+    constexpr int kStride = kS < kUnits ? kS : kUnits;     // (parts past a piece's units have none)
+    const int rows = min(n - 16 * block0, 16 * kG);
+    f32x4 acc[kG][2] = {};
+    Unit gate, up;
+    gate.load(p.up_codes, p.up_scales, first, steps, min(part, units - 1));
+    up.load(p.up_codes, p.up_scales, first + tiles, steps, min(part, units - 1));
+    for (int u0 = 0; u0 < units; u0 += kUnits) {
+      if (u0 || block0) __syncthreads();             // what is there has been read
+      constexpr int kRow = kPiece / kG / 8;          // 16-byte parts of a row
+      for (int i = tid; i < rows * kRow; i += kThreads) {
+        const int r = i / kRow, k = u0 * 128 * kSteps + i % kRow * 8;
+        const int token = __builtin_amdgcn_readfirstlane(__shfl(column, 16 * block0 + r, 64)) & 63;
+        u32x4v v = 0u;
+        if (k < p.H) v = *reinterpret_cast<const u32x4v*>(p.x + token * p.ld_x + k);
+        *reinterpret_cast<u32x4v*>(smem + r * kPitch + i % kRow * 16) = v;
+      }
+      __syncthreads();
+      for (int u = u0 + part; u < min(u0 + kUnits, units); u += kStride) {
+        const Unit g0 = gate, up0 = up;
+        const int next = min(u + kStride, units - 1);
+        gate.load(p.up_codes, p.up_scales, first, steps, next);
+        up.load(p.up_codes, p.up_scales, first + tiles, steps, next);
 #pragma unroll
         for (int i = 0; i < kSteps; ++i) {
-          u32x4v a[4];
-          to_bf16(gate.codes[i], gate.scales >> (8 * i) & 255u, a);
+          u32x4v a[4], b[4];
+          to_bf16(g0.codes[i], g0.scales >> (8 * i) & 255u, a);
+          u32x4v a2[4];
+          to_bf16(up0.codes[i], up0.scales >> (8 * i) & 255u, a2);
 #pragma unroll
-          for (int j = 0; j < 4; ++j) z = dev::mfma_bf16(a[j], b[i][j], z);
-          to_bf16(up.codes[i], up.scales >> (8 * i) & 255u, a);
+          for (int g = 0; g < kG; ++g) {
+            // columns without a token read the first one's row: their sums are nobody's
+            const unsigned char* from = smem + (16 * g + c < rows ? 16 * g + c : 0) * kPitch +
+                                        ((u - u0) * kSteps + i) * 256 + q * 64;
 #pragma unroll
-          for (int j = 0; j < 4; ++j) y = dev::mfma_bf16(a[j], b[i][j], y);
+            for (int j = 0; j < 4; ++j) b[j] = *reinterpret_cast<const u32x4v*>(from + 16 * j);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+              acc[g][0] = dev::mfma_bf16(a[j], b[j], acc[g][0]);
+              acc[g][1] = dev::mfma_bf16(a2[j], b[j], acc[g][1]);
+            }
+          }
         }
       }
     }
-    if constexpr (kS > 1) {
-      if (g) __syncthreads();
-      sums[(wave * 2) * 64 + lane] = z;
-      sums[(wave * 2 + 1) * 64 + lane] = y;
-      __syncthreads();
-      if (part) continue;
 #pragma unroll
-      for (int w = 1; w < kS; ++w) {
-        z += sums[((wave + w) * 2) * 64 + lane];
-        y += sums[((wave + w) * 2 + 1) * 64 + lane];
+    for (int g = 0; g < kG; ++g) {
+      f32x4 z = acc[g][0], y = acc[g][1];
+      if constexpr (kS > 1) {
+        __syncthreads();
+        sums[(wave * 2) * 64 + lane] = z;
+        sums[(wave * 2 + 1) * 64 + lane] = y;
+        __syncthreads();
+        if (part) continue;
+#pragma unroll
+        for (int w = 1; w < kS; ++w) {
+          z += sums[((wave + w) * 2) * 64 + lane];
+          y += sums[((wave + w) * 2 + 1) * 64 + lane];
+        }
+      }
+      // column c's features 4 q .. 4 q + 3 of the tile
+      const int col = __shfl(column, 16 * (block0 + g) + c, 64);
+      const float w = __shfl(weight, 16 * (block0 + g) + c, 64);
+      if (16 * g + c < rows && work) {
+        float h[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) h[i] = z[i] / (1.f + expf(-z[i])) * y[i] * w;
+        const dev::u32x2 v = {dev::pack_bf16(h[0], h[1]), dev::pack_bf16(h[2], h[3])};
+        *reinterpret_cast<dev::u32x2*>(hidden + static_cast<int64_t>(col >> 6) * p.I + 16 * tile + 4 * q) = v;
       }
     }
-    // column c's features 4 q .. 4 q + 3 of the tile
-    const float w = __shfl(weight, 16 * g + c, 64);
-    if (col >= 0 && tile < tiles) {
-      float h[4];
-#pragma unroll
-      for (int i = 0; i < 4; ++i) h[i] = z[i] / (1.f + expf(-z[i])) * y[i] * w;
-      const dev::u32x2 v = {dev::pack_bf16(h[0], h[1]), dev::pack_bf16(h[2], h[3])};
-      *reinterpret_cast<dev::u32x2*>(hidden + static_cast<int64_t>(col >> 6) * p.I + 16 * tile + 4 * q) = v;
-    }
+  };
+  if (n <= 16) {
+    pass(0, std::integral_constant<int, 1>{});
+  } else {                                           // past 32 tokens the weights come from L2 again
+    for (int block = 0; 16 * block < n; block += 2) pass(block, std::integral_constant<int, 2>{});
   }
 }
 
-// Second launch: 16 output features of all tokens.  The units of the experts that are reached are
-// dealt evenly, in order, to the waves of the tile's workgroups.  A unit's columns are its expert's
-// tokens; their sums are added to the tokens' in LDS, of which each wave has its own.  The waves'
-// sums are added in their order, the workgroups' in theirs, by the one that arrives last.
+// The second launch's order of work: items, an expert's tokens 16 at a time, of all slots in
+// ascending order, each of `steps` K steps.  Every lane of a wave has the same position.
+class Items {
+ public:
+  __device__ __forceinline__ Items(const Table& table, int slots) : counts_(table.counts), slots_(slots) {
+    for (int base = 0; base < slots; base += 64)
+      total_ += __builtin_amdgcn_readlane(dev::prefix_sum(items(base)), 63);
+  }
+  __device__ __forceinline__ int total() const { return total_; }
+  __device__ __forceinline__ void seek(int item) {             // item < total()
+    base_ = 0;
+    while (true) {
+      const int mine = items(base_), upto = dev::prefix_sum(mine), all = __builtin_amdgcn_readlane(upto, 63);
+      if (item < all) {
+        const int at = __builtin_ctzll(__ballot(item < upto));
+        here_ = mine;
+        slot_ = base_ + at;
+        block_ = item - (__builtin_amdgcn_readlane(upto, at) - __builtin_amdgcn_readlane(mine, at));
+        return;
+      }
+      item -= all;
+      base_ += 64;
+    }
+  }
+  __device__ __forceinline__ void next() {                     // there is one
+    if (++block_ < __builtin_amdgcn_readlane(here_, slot_ - base_)) return;
+    block_ = 0;
+    uint64_t left = __ballot(here_ > 0) & ~((uint64_t{2} << (slot_ - base_)) - 1);
+    while (!left) {
+      base_ += 64;
+      here_ = items(base_);
+      left = __ballot(here_ > 0);
+    }
+    slot_ = base_ + __builtin_ctzll(left);
+  }
+  __device__ __forceinline__ int slot() const { return slot_; }
+  __device__ __forceinline__ int block() const { return block_; }
+
+ private:
+  __device__ __forceinline__ int items(int base) const {
+    const int i = base + (static_cast<int>(threadIdx.x) & 63);
+    return i < slots_ ? (counts_[i] + 15) >> 4 : 0;
+  }
+  const int32_t* counts_;
+  int slots_, total_ = 0, base_ = 0, here_ = 0, slot_ = 0, block_ = 0;
+};
+
+// Floats between two tokens' sums of kT tiles in LDS: the 16 columns of a store meet different banks.
+constexpr int sums_pitch(int tiles) { return 16 * tiles + 4; }
+
+// Second launch: kT tiles of 16 output features of all tokens.  The steps of all items are dealt
+// evenly, in order, to the waves of the tiles' workgroups.  An item's sums are added to its tokens' in
+// LDS, of which each wave has its own.  The waves' sums are added in their order, the workgroups' in
+// theirs, by the one that arrives last.
+//
+// A wave asks for the activations of a step one step ahead and for its weights two ahead.
+template <int kT>
 __global__ __launch_bounds__(kThreads, 4) void moe_down_kernel(const MoeArgs p, const uint16_t* __restrict__ hidden,
                                                                 const Table table, int slots, float* parts,
                                                                 uint32_t* arrived) {
-  extern __shared__ __align__(16) float own[];       // [kWaves][M][16]
+  constexpr int kPitch = sums_pitch(kT);
+  extern __shared__ __align__(16) float own[];       // [kWaves][M][kPitch]
   __shared__ int sh_last;
   const int tid = static_cast<int>(threadIdx.x), lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int c = lane & 15, q = lane >> 4;
-  const int tile = static_cast<int>(blockIdx.x), splits = static_cast<int>(gridDim.y), part = static_cast<int>(blockIdx.y);
-  const int K = p.I + p.k_tail, steps = (K + 127) >> 7, units = (steps + kSteps - 1) / kSteps;
-  f32x4* mine = reinterpret_cast<f32x4*>(own) + wave * p.M * 4;
-  for (int i = lane; i < p.M * 4; i += 64) mine[i] = 0.f;
+  const int tile = static_cast<int>(blockIdx.x) * kT, splits = static_cast<int>(gridDim.y), part = static_cast<int>(blockIdx.y);
+  const int K = p.I + p.k_tail, steps = (K + 127) >> 7, groups = (steps + 3) >> 2, tiles = p.N >> 4;
+  float* const mine = own + wave * p.M * kPitch;
+  for (int i = lane; i < p.M * kPitch / 4; i += 64) reinterpret_cast<f32x4*>(mine)[i] = 0.f;
   dev::wave_lds_barrier();
 
-  // The slots with tokens, 64 at a time.
-  auto there = [&](int base) { return __ballot(base + lane < slots && table.counts[min(base + lane, slots - 1)] > 0); };
-  int n = 0;
-  for (int base = 0; base < slots; base += 64) n += __popcll(there(base));
-  const int64_t all = static_cast<int64_t>(n) * units;
+  Items front(table, slots);
+  const int64_t all = static_cast<int64_t>(front.total()) * steps;
   const int shares = splits * kWaves, share = part * kWaves + wave;
-  int u = static_cast<int>(all * share / shares);
-  const int end = static_cast<int>(all * (share + 1) / shares);
+  const int begin = static_cast<int>(all * share / shares), end = static_cast<int>(all * (share + 1) / shares);
 
-  if (u < end) {
-    int skip = u / units, base = 0;
-    uint64_t left = there(0);
-    for (; __popcll(left) <= skip; left = there(base)) skip -= __popcll(left), base += 64;
-    for (; skip; --skip) left &= left - 1;
-    while (true) {
-      const int slot = base + __builtin_ctzll(left);
-      const int e = table.experts[slot];
-      const int64_t first = static_cast<int64_t>(e) * (p.N >> 4) + tile;
-      const int column = table.columns[slot * 64 + lane];
-      const int blocks = (table.counts[slot] + 15) >> 4;
-      const int stop = min(u / units * units + units, end);
-      for (; u < stop; ++u) {
-        Unit down;
-        down.load(p.down_codes, p.down_scales, first, steps, u % units);
-        for (int g = 0; g < blocks; ++g) {
-          const int col = __shfl(column, 16 * g + c, 64);
-          u32x4v b[kSteps][4];
-          load_columns(col < 0 ? nullptr : hidden + static_cast<int64_t>(col >> 6) * p.I, u % units, p.I, K, b);
-          f32x4 acc = 0.f;
+  struct Weights {
+    u32x4v codes[kT];
+    uint32_t scales[kT];
+  };
+  // Where the weights that are asked for next are: an item and a step of it, its expert's tiles, and
+  // this lane's column of it (the row of its token, or null).
+  int front_step = 0;
+  const u32x4v* codes = nullptr;
+  const uint32_t* scales = nullptr;
+  int column = -1;
+  auto enter = [&] {                                 // the front's item
+    const int64_t first = static_cast<int64_t>(table.experts[front.slot()]) * tiles + tile;
+    codes = reinterpret_cast<const u32x4v*>(p.down_codes) + first * steps * 64 + lane;
+    scales = reinterpret_cast<const uint32_t*>(p.down_scales) + first * groups * 64 + lane;
+    column = table.columns[front.slot() * 64 + 16 * front.block() + c];
+  };
+  auto ask = [&](Weights& w) {
 #pragma unroll
-          for (int i = 0; i < kSteps; ++i) {
-            u32x4v a[4];
-            to_bf16(down.codes[i], down.scales >> (8 * i) & 255u, a);
+    for (int t = 0; t < kT; ++t) {
+      w.codes[t] = __builtin_nontemporal_load(codes + (t * steps + front_step) * 64);
+      w.scales[t] = scales[(t * groups + (front_step >> 2)) * 64] >> (8 * (front_step & 3));
+    }
+  };
+  // The activations of the front's step, zeros for columns without a token and behind K; the tail meets
+  // the last values again.
+  auto columns = [&](u32x4v (&b)[4]) {
+    const int k = 128 * front_step + 32 * q;
+    const uint16_t* from = hidden + static_cast<int64_t>(column >> 6) * p.I + (k < p.I ? k : k - p.k_tail);
+    const bool in = column >= 0 && k < K;
 #pragma unroll
-            for (int j = 0; j < 4; ++j) acc = dev::mfma_bf16(a[j], b[i][j], acc);
-          }
-          if (col >= 0) mine[(col & 63) * 4 + q] += acc;
-          dev::wave_lds_barrier();
-        }
+    for (int j = 0; j < 4; ++j) {
+      b[j] = 0u;
+      if (in) b[j] = reinterpret_cast<const u32x4v*>(from)[j];
+    }
+  };
+
+  if (begin < end) {
+    front.seek(begin / steps);
+    front_step = begin % steps;
+    enter();
+    Weights w[2];
+    u32x4v b[2][4];
+    int token[2];
+    bool ends[2];                                    // the item's sums are complete behind this step
+    int u = begin;                                   // the step whose weights are asked for next
+    auto advance = [&] {
+      if (++u >= end) return;
+      if (++front_step == steps) {
+        front_step = 0;
+        front.next();
+        enter();
       }
-      if (u >= end) break;
-      left &= left - 1;
-      while (!left) base += 64, left = there(base);
+    };
+    f32x4 acc[kT] = {};
+    auto compute = [&](const Weights& w, const u32x4v (&b)[4], int token, bool ends) {
+#pragma unroll
+      for (int t = 0; t < kT; ++t) {
+        u32x4v a[4];
+        to_bf16(w.codes[t], w.scales[t] & 255u, a);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) acc[t] = dev::mfma_bf16(a[j], b[j], acc[t]);
+      }
+      if (ends) {
+#pragma unroll
+        for (int t = 0; t < kT; ++t) {
+          if (token >= 0) *reinterpret_cast<f32x4*>(mine + token * kPitch + 16 * t + 4 * q) += acc[t];
+          acc[t] = 0.f;
+        }
+        dev::wave_lds_barrier();
+      }
+    };
+    // Step i's weights and columns are in slot i % 2.
+    auto request = [&](int i) {
+      columns(b[i]);
+      ask(w[i]);
+      token[i] = column < 0 ? -1 : column & 63;
+      ends[i] = front_step + 1 == steps || u + 1 >= end;
+    };
+    request(0);
+    for (int i = begin; i < end; i += 2) {
+      advance();
+      if (i + 1 < end) request(1);
+      compute(w[0], b[0], token[0], ends[0]);
+      if (i + 1 >= end) break;
+      advance();
+      if (i + 2 < end) request(0);
+      compute(w[1], b[1], token[1], ends[1]);
     }
   }
   __syncthreads();
   // Thread (t, i): token t's features 4 i .. 4 i + 3.
-  const int t = tid >> 2, i = tid & 3;
+  const int t = tid / (4 * kT), i = tid % (4 * kT);
   const bool here = t < p.M;
-  const f32x4* sums = reinterpret_cast<const f32x4*>(own);
   f32x4 y = 0.f;
   if (here) {
 #pragma unroll
-    for (int w = 0; w < kWaves; ++w) y += sums[(w * p.M + t) * 4 + i];
+    for (int w = 0; w < kWaves; ++w) y += *reinterpret_cast<const f32x4*>(own + (w * p.M + t) * kPitch + 4 * i);
   }
   const int64_t at = static_cast<int64_t>(t) * p.N + 16 * tile + 4 * i;
   if (splits > 1) {
@@ -291,22 +419,28 @@ __global__ __launch_bounds__(kThreads, 4) void moe_down_kernel(const MoeArgs p, 
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");       // what this wave has stored is there
     __syncthreads();
     if (tid == 0)
-      sh_last = __hip_atomic_fetch_add(arrived + tile, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) ==
+      sh_last = __hip_atomic_fetch_add(arrived + blockIdx.x, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) ==
                 static_cast<uint32_t>(splits - 1);
     __syncthreads();
     if (!sh_last) return;
-    if (tid == 0) __hip_atomic_store(arrived + tile, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    if (tid == 0) __hip_atomic_store(arrived + blockIdx.x, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     if (here) {
-      y = 0.f;
-      for (int w = 0; w < splits; ++w) {
+      uint64_t v[kMaxSplits][2];                     // all loads under way together
 #pragma unroll
-        for (int j = 0; j < 4; j += 2) {
-          const uint64_t v = __hip_atomic_load(reinterpret_cast<const uint64_t*>(parts + w * stride + at + j),
-                                               __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-          y[j] += __uint_as_float(static_cast<uint32_t>(v));
-          y[j + 1] += __uint_as_float(static_cast<uint32_t>(v >> 32));
+      for (int w = 0; w < kMaxSplits; ++w)
+#pragma unroll
+        for (int j = 0; j < 2; ++j)
+          v[w][j] = w < splits ? __hip_atomic_load(reinterpret_cast<const uint64_t*>(parts + w * stride + at) + j,
+                                                   __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT)
+                               : 0;
+      y = 0.f;
+#pragma unroll
+      for (int w = 0; w < kMaxSplits; ++w)
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+          y[2 * j] += __uint_as_float(static_cast<uint32_t>(v[w][j]));
+          y[2 * j + 1] += __uint_as_float(static_cast<uint32_t>(v[w][j] >> 32));
         }
-      }
     }
   }
   if (here) {
@@ -329,8 +463,12 @@ MoePlan plan_moe_layer(const MoeArgs& p, int num_cus) {
   const int64_t tiles = static_cast<int64_t>(p.I / 16) * c.slots;
   const int up_units = (p.H + 128 * kSteps - 1) / (128 * kSteps);
   while (c.parts < kWaves && c.parts < up_units && tiles * c.parts < 16 * num_cus) c.parts *= 2;
-  const int64_t units = static_cast<int64_t>(c.slots) * ((p.I + p.k_tail + 128 * kSteps - 1) / (128 * kSteps));
-  while (c.splits < 8 && static_cast<int64_t>(p.N / 16) * c.splits < 2 * num_cus && units >= 4 * c.splits * kWaves)
+  // The second: two workgroups a CU, of a tile, or of two where the waves have steps enough, so that the
+  // activations are loaded for two.
+  const int64_t steps = static_cast<int64_t>(c.slots) * ((p.I + p.k_tail + 127) / 128);
+  c.tiles = p.N % 32 == 0 && p.N / 32 * steps >= static_cast<int64_t>(2) * num_cus * kWaves * 4 ? 2 : 1;
+  while (c.splits < kMaxSplits && static_cast<int64_t>(p.N / 16 / c.tiles) * c.splits < 2 * num_cus &&
+         steps >= 8 * c.splits * kWaves)
     c.splits *= 2;
   return c;
 }
@@ -347,20 +485,37 @@ hipError_t launch_moe_layer(const MoePlan& c, const MoeArgs& p, void* workspace,
   int32_t* const ints = reinterpret_cast<int32_t*>(at += hidden_bytes(p));
   const Table table{ints, ints + c.slots, ints + 2 * c.slots};
   float* parts = reinterpret_cast<float*>(at += table_bytes(c));
+  const int rows = p.M <= 16 ? p.M * pitch_of(1) : std::max(16 * pitch_of(1), 32 * pitch_of(2));
+  const int lds = c.parts > 1 ? std::max(rows, kWaves * 2 * 64 * 16) : rows;
   auto up = [&](auto shared) {
     constexpr int kS = decltype(shared)::value, kTiles = kWaves / kS;
-    moe_up_kernel<kS><<<dim3((p.I / 16 + kTiles - 1) / kTiles, c.slots), kThreads, 0, stream>>>(p, c.by_expert, hidden,
-                                                                                                 table);
+    if (lds > 64 * 1024) {
+      const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(&moe_up_kernel<kS>),
+                                               hipFuncAttributeMaxDynamicSharedMemorySize, lds);
+      if (e != hipSuccess) return e;
+    }
+    moe_up_kernel<kS><<<dim3((p.I / 16 + kTiles - 1) / kTiles, c.slots), kThreads, lds, stream>>>(p, c.by_expert,
+                                                                                                   hidden, table);
+    return hipGetLastError();
   };
-  if (c.parts == 1) up(std::integral_constant<int, 1>{});
-  else if (c.parts == 2) up(std::integral_constant<int, 2>{});
-  else if (c.parts == 4) up(std::integral_constant<int, 4>{});
-  else up(std::integral_constant<int, 8>{});
-  const hipError_t e = hipGetLastError();
+  const hipError_t e = c.parts == 1   ? up(std::integral_constant<int, 1>{})
+                       : c.parts == 2 ? up(std::integral_constant<int, 2>{})
+                       : c.parts == 4 ? up(std::integral_constant<int, 4>{})
+                                      : up(std::integral_constant<int, 8>{});
   if (e != hipSuccess) return e;
-  moe_down_kernel<<<dim3(p.N / 16, c.splits), kThreads, kWaves * p.M * 16 * 4, stream>>>(p, hidden, table, c.slots,
-                                                                                         parts, arrived);
-  return hipGetLastError();
+  auto down = [&](auto together) {
+    constexpr int kT = decltype(together)::value;
+    const int sums = kWaves * p.M * sums_pitch(kT) * 4;
+    if (sums > 64 * 1024) {
+      const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(&moe_down_kernel<kT>),
+                                               hipFuncAttributeMaxDynamicSharedMemorySize, sums);
+      if (e != hipSuccess) return e;
+    }
+    moe_down_kernel<kT><<<dim3(p.N / 16 / kT, c.splits), kThreads, sums, stream>>>(p, hidden, table, c.slots, parts,
+                                                                                  arrived);
+    return hipGetLastError();
+  };
+  return c.tiles == 2 ? down(std::integral_constant<int, 2>{}) : down(std::integral_constant<int, 1>{});
 }
 
 }  // namespace prq
