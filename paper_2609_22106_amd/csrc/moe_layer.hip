@@ -36,12 +36,11 @@ constexpr int kWaves = 8, kThreads = 64 * kWaves;
 constexpr int kMaxSplits = 8;                       // workgroups that share output tiles
 constexpr int kSteps = 2;                            // K steps of 128 in a wave's unit
 
-// What the first launch leaves: of every slot the number of its tokens (0: none, or the expert is
-// another slot's), its expert, and for column i the row of `hidden` times 64 plus the token, -1 past
-// the last.
+// What the first launch leaves of every slot: its expert and 2^16 times the number of its tokens (0:
+// none, or the expert is another slot's), and for column i the row of `hidden` times 64 plus the
+// token, -1 past the last.
 struct Table {
-  int32_t* counts;
-  int32_t* experts;
+  int32_t* slots;
   int32_t* columns;                                  // [slots][64]
 };
 
@@ -138,10 +137,7 @@ __global__ __launch_bounds__(kThreads, 4) void moe_up_kernel(const MoeArgs p, bo
   const int entry = share.has ? row * 64 + lane : -1;
   const int column = __builtin_amdgcn_ds_permute(4 * at, entry);
   if (blockIdx.x == 0 && wave == 0) {
-    if (lane == 0) {
-      table.counts[slot] = n;
-      table.experts[slot] = e;
-    }
+    if (lane == 0) table.slots[slot] = n ? n << 16 | e : 0;
     table.columns[slot * 64 + lane] = column;
   }
   if (n == 0) return;                                // the whole workgroup
@@ -230,170 +226,139 @@ __global__ __launch_bounds__(kThreads, 4) void moe_up_kernel(const MoeArgs p, bo
   }
 }
 
-// The second launch's order of work: items, an expert's tokens 16 at a time, of all slots in
-// ascending order, each of `steps` K steps.  Every lane of a wave has the same position.
-class Items {
- public:
-  __device__ __forceinline__ Items(const Table& table, int slots) : counts_(table.counts), slots_(slots) {
-    for (int base = 0; base < slots; base += 64)
-      total_ += __builtin_amdgcn_readlane(dev::prefix_sum(items(base)), 63);
-  }
-  __device__ __forceinline__ int total() const { return total_; }
-  __device__ __forceinline__ void seek(int item) {             // item < total()
-    base_ = 0;
-    while (true) {
-      const int mine = items(base_), upto = dev::prefix_sum(mine), all = __builtin_amdgcn_readlane(upto, 63);
-      if (item < all) {
-        const int at = __builtin_ctzll(__ballot(item < upto));
-        here_ = mine;
-        slot_ = base_ + at;
-        block_ = item - (__builtin_amdgcn_readlane(upto, at) - __builtin_amdgcn_readlane(mine, at));
-        return;
-      }
-      item -= all;
-      base_ += 64;
-    }
-  }
-  __device__ __forceinline__ void next() {                     // there is one
-    if (++block_ < __builtin_amdgcn_readlane(here_, slot_ - base_)) return;
-    block_ = 0;
-    uint64_t left = __ballot(here_ > 0) & ~((uint64_t{2} << (slot_ - base_)) - 1);
-    while (!left) {
-      base_ += 64;
-      here_ = items(base_);
-      left = __ballot(here_ > 0);
-    }
-    slot_ = base_ + __builtin_ctzll(left);
-  }
-  __device__ __forceinline__ int slot() const { return slot_; }
-  __device__ __forceinline__ int block() const { return block_; }
-
- private:
-  __device__ __forceinline__ int items(int base) const {
-    const int i = base + (static_cast<int>(threadIdx.x) & 63);
-    return i < slots_ ? (counts_[i] + 15) >> 4 : 0;
-  }
-  const int32_t* counts_;
-  int slots_, total_ = 0, base_ = 0, here_ = 0, slot_ = 0, block_ = 0;
-};
-
 // Floats between two tokens' sums of kT tiles in LDS: the 16 columns of a store meet different banks.
 constexpr int sums_pitch(int tiles) { return 16 * tiles + 4; }
 
-// Second launch: kT tiles of 16 output features of all tokens.  The steps of all items are dealt
-// evenly, in order, to the waves of the tiles' workgroups.  An item's sums are added to its tokens' in
-// LDS, of which each wave has its own.  The waves' sums are added in their order, the workgroups' in
-// theirs, by the one that arrives last.
+// Second launch: kT tiles of 16 output features of all tokens.  Its items are an expert's tokens, 16 at
+// a time; they are dealt to the tiles' workgroups, up to kWindow at a time, and the K steps of a
+// window's items evenly, in order, to the waves.  An item's sums are added to its tokens' in LDS, of
+// which each wave has its own.  The waves' sums are added in their order, the workgroups' in theirs, by
+// the one that arrives last.
 //
-// A wave asks for the activations of a step one step ahead and for its weights two ahead.
-template <int kT>
-__global__ __launch_bounds__(kThreads, 4) void moe_down_kernel(const MoeArgs p, const uint16_t* __restrict__ hidden,
-                                                                const Table table, int slots, float* parts,
-                                                                uint32_t* arrived) {
-  constexpr int kPitch = sums_pitch(kT);
-  extern __shared__ __align__(16) float own[];       // [kWaves][M][kPitch]
+// A wave asks for the weights and activations of a step kAhead steps ahead.  The loop has loads
+// without conditions only (past the end the last step's again, columns without a token outside the
+// buffer, which reads as zeros), so that every wait counts exactly the loads behind it.
+constexpr int kWindow = 64;
+
+template <int kT, int kN, int kAhead>
+__global__ __launch_bounds__(64 * kN, 4) void moe_down_kernel(const MoeArgs p, const uint16_t* __restrict__ hidden,
+                                                               const Table table, int slots, float* parts,
+                                                               uint32_t* arrived) {
+  constexpr int kPitch = sums_pitch(kT), kRing = kAhead + 1;
+  extern __shared__ __align__(16) float own[];       // [kN][M][kPitch]
+  __shared__ int sh_items[kWindow];                  // slot, 2^13 times the block, 2^16 times the expert
+  __shared__ int sh_columns[kWindow][16];
   __shared__ int sh_last;
   const int tid = static_cast<int>(threadIdx.x), lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int c = lane & 15, q = lane >> 4;
   const int tile = static_cast<int>(blockIdx.x) * kT, splits = static_cast<int>(gridDim.y), part = static_cast<int>(blockIdx.y);
   const int K = p.I + p.k_tail, steps = (K + 127) >> 7, groups = (steps + 3) >> 2, tiles = p.N >> 4;
+  const auto rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint16_t*>(hidden), 0, p.M * p.k * p.I * 2, 0x00020000);
+
+  // Lane i: slot base + i, and the number of its items.
+  auto slot_at = [&](int base) { return base + lane < slots ? table.slots[base + lane] : 0; };
+  auto items_of = [](int slot) { return (slot + (15 << 16)) >> 20; };
+  int total = 0;
+  for (int base = 0; base < slots; base += 64)
+    total += __builtin_amdgcn_readlane(dev::prefix_sum(items_of(slot_at(base))), 63);
   float* const mine = own + wave * p.M * kPitch;
   for (int i = lane; i < p.M * kPitch / 4; i += 64) reinterpret_cast<f32x4*>(mine)[i] = 0.f;
-  dev::wave_lds_barrier();
 
-  Items front(table, slots);
-  const int64_t all = static_cast<int64_t>(front.total()) * steps;
-  const int shares = splits * kWaves, share = part * kWaves + wave;
-  const int begin = static_cast<int>(all * share / shares), end = static_cast<int>(all * (share + 1) / shares);
-
-  struct Weights {
-    u32x4v codes[kT];
-    uint32_t scales[kT];
-  };
-  // Where the weights that are asked for next are: an item and a step of it, its expert's tiles, and
-  // this lane's column of it (the row of its token, or null).
-  int front_step = 0;
-  const u32x4v* codes = nullptr;
-  const uint32_t* scales = nullptr;
-  int column = -1;
-  auto enter = [&] {                                 // the front's item
-    const int64_t first = static_cast<int64_t>(table.experts[front.slot()]) * tiles + tile;
-    codes = reinterpret_cast<const u32x4v*>(p.down_codes) + first * steps * 64 + lane;
-    scales = reinterpret_cast<const uint32_t*>(p.down_scales) + first * groups * 64 + lane;
-    column = table.columns[front.slot() * 64 + 16 * front.block() + c];
-  };
-  auto ask = [&](Weights& w) {
-#pragma unroll
-    for (int t = 0; t < kT; ++t) {
-      w.codes[t] = __builtin_nontemporal_load(codes + (t * steps + front_step) * 64);
-      w.scales[t] = scales[(t * groups + (front_step >> 2)) * 64] >> (8 * (front_step & 3));
-    }
-  };
-  // The activations of the front's step, zeros for columns without a token and behind K; the tail meets
-  // the last values again.
-  auto columns = [&](u32x4v (&b)[4]) {
-    const int k = 128 * front_step + 32 * q;
-    const uint16_t* from = hidden + static_cast<int64_t>(column >> 6) * p.I + (k < p.I ? k : k - p.k_tail);
-    const bool in = column >= 0 && k < K;
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      b[j] = 0u;
-      if (in) b[j] = reinterpret_cast<const u32x4v*>(from)[j];
-    }
-  };
-
-  if (begin < end) {
-    front.seek(begin / steps);
-    front_step = begin % steps;
-    enter();
-    Weights w[2];
-    u32x4v b[2][4];
-    int token[2];
-    bool ends[2];                                    // the item's sums are complete behind this step
-    int u = begin;                                   // the step whose weights are asked for next
-    auto advance = [&] {
-      if (++u >= end) return;
-      if (++front_step == steps) {
-        front_step = 0;
-        front.next();
-        enter();
+  const int last_item = static_cast<int>(static_cast<int64_t>(total) * (part + 1) / splits);
+  for (int item0 = static_cast<int>(static_cast<int64_t>(total) * part / splits); item0 < last_item; item0 += kWindow) {
+    const int items = min(last_item - item0, kWindow);
+    __syncthreads();                                 // the window before has been read
+    if (wave == 0) {
+      int before = 0;
+      for (int base = 0; base < slots && before < item0 + items; base += 64) {
+        const int slot = slot_at(base), n = items_of(slot), upto = dev::prefix_sum(n);
+        for (int g = 0; g < n; ++g) {
+          const int at = before + upto - n + g - item0;
+          if (at >= 0 && at < items) sh_items[at] = (slot & 0xFFFF) << 16 | g << 13 | (base + lane);
+        }
+        before += __builtin_amdgcn_readlane(upto, 63);
       }
-    };
-    f32x4 acc[kT] = {};
-    auto compute = [&](const Weights& w, const u32x4v (&b)[4], int token, bool ends) {
-#pragma unroll
-      for (int t = 0; t < kT; ++t) {
-        u32x4v a[4];
-        to_bf16(w.codes[t], w.scales[t] & 255u, a);
-#pragma unroll
-        for (int j = 0; j < 4; ++j) acc[t] = dev::mfma_bf16(a[j], b[j], acc[t]);
-      }
-      if (ends) {
+    }
+    __syncthreads();
+    for (int i = tid; i < items * 16; i += 64 * kN) {
+      const int item = sh_items[i >> 4];
+      sh_columns[i >> 4][i & 15] = table.columns[(item & 0x1FFF) * 64 + 16 * (item >> 13 & 3) + (i & 15)];
+    }
+    __syncthreads();
+
+    const int begin = items * steps * wave / kN, n = items * steps * (wave + 1) / kN - begin;
+    if (n > 0) {
+      // The step that is asked for next: its item, the expert's tiles, and where this lane's column
+      // is in `hidden` (past its end: no token).
+      int item = begin / steps, step = begin % steps, u = 0, column;
+      const u32x4v* codes;
+      const uint32_t* scales;
+      uint32_t row;
+      auto enter = [&] {
+        const int64_t first = static_cast<int64_t>(__builtin_amdgcn_readfirstlane(sh_items[item]) >> 16) * tiles + tile;
+        codes = reinterpret_cast<const u32x4v*>(p.down_codes) + first * steps * 64;
+        scales = reinterpret_cast<const uint32_t*>(p.down_scales) + first * groups * 64;
+        column = sh_columns[item][c];
+        row = column < 0 ? 0x80000000u : static_cast<uint32_t>(column >> 6) * static_cast<uint32_t>(2 * p.I);
+      };
+      enter();
+      struct Step {
+        u32x4v codes[kT];
+        uint32_t scales[kT];
+        u32x4v b[4];
+      } ring[kRing];
+      auto ask = [&](Step& s) {
+        const int k = 128 * step + 32 * q;           // the tail meets the last values again, zeros behind it
+        const uint32_t at = k < K ? row + 2 * static_cast<uint32_t>(k < p.I ? k : k - p.k_tail) : 0x80000000u;
 #pragma unroll
         for (int t = 0; t < kT; ++t) {
-          if (token >= 0) *reinterpret_cast<f32x4*>(mine + token * kPitch + 16 * t + 4 * q) += acc[t];
-          acc[t] = 0.f;
+          s.codes[t] = __builtin_nontemporal_load(codes + (t * steps + step) * 64 + lane);
+          s.scales[t] = scales[(t * groups + (step >> 2)) * 64 + lane];
         }
-        dev::wave_lds_barrier();
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+          s.b[j] = __builtin_bit_cast(u32x4v, __builtin_amdgcn_raw_buffer_load_b128(rsrc, at, 16 * j, 0));
+        if (u + 1 < n) {
+          ++u;
+          if (++step == steps) {
+            step = 0;
+            ++item;
+            enter();
+          }
+        }
+      };
+      f32x4 acc[kT] = {};
+      int now = step, now_item = item, now_column = column;    // of the step that is computed
+      auto compute = [&](const Step& s, bool last) {
+#pragma unroll
+        for (int t = 0; t < kT; ++t) {
+          u32x4v a[4];
+          to_bf16(s.codes[t], s.scales[t] >> (8 * (now & 3)) & 255u, a);
+#pragma unroll
+          for (int j = 0; j < 4; ++j) acc[t] = dev::mfma_bf16(a[j], s.b[j], acc[t]);
+        }
+        if (++now == steps || last) {                // the item's sums are complete here
+          now = 0;
+#pragma unroll
+          for (int t = 0; t < kT; ++t) {
+            if (now_column >= 0)
+              *reinterpret_cast<f32x4*>(mine + (now_column & 63) * kPitch + 16 * t + 4 * q) += acc[t];
+            acc[t] = 0.f;
+          }
+          dev::wave_lds_barrier();
+          if (!last) now_column = sh_columns[++now_item][c];
+        }
+      };
+#pragma unroll
+      for (int i = 0; i < kAhead; ++i) ask(ring[i]);
+      for (int i0 = 0; i0 < n; i0 += kRing) {
+#pragma unroll
+        for (int r = 0; r < kRing; ++r) {
+          ask(ring[(r + kAhead) % kRing]);
+          if (i0 + r < n) compute(ring[r], i0 + r + 1 == n);
+        }
       }
-    };
-    // Step i's weights and columns are in slot i % 2.
-    auto request = [&](int i) {
-      columns(b[i]);
-      ask(w[i]);
-      token[i] = column < 0 ? -1 : column & 63;
-      ends[i] = front_step + 1 == steps || u + 1 >= end;
-    };
-    request(0);
-    for (int i = begin; i < end; i += 2) {
-      advance();
-      if (i + 1 < end) request(1);
-      compute(w[0], b[0], token[0], ends[0]);
-      if (i + 1 >= end) break;
-      advance();
-      if (i + 2 < end) request(0);
-      compute(w[1], b[1], token[1], ends[1]);
     }
   }
   __syncthreads();
@@ -403,7 +368,7 @@ __global__ __launch_bounds__(kThreads, 4) void moe_down_kernel(const MoeArgs p, 
   f32x4 y = 0.f;
   if (here) {
 #pragma unroll
-    for (int w = 0; w < kWaves; ++w) y += *reinterpret_cast<const f32x4*>(own + (w * p.M + t) * kPitch + 4 * i);
+    for (int w = 0; w < kN; ++w) y += *reinterpret_cast<const f32x4*>(own + (w * p.M + t) * kPitch + 4 * i);
   }
   const int64_t at = static_cast<int64_t>(t) * p.N + 16 * tile + 4 * i;
   if (splits > 1) {
@@ -451,7 +416,7 @@ __global__ __launch_bounds__(kThreads, 4) void moe_down_kernel(const MoeArgs p, 
 
 size_t up16(size_t n) { return (n + 15) & ~size_t{15}; }
 size_t hidden_bytes(const MoeArgs& p) { return up16(static_cast<size_t>(p.M) * p.k * p.I * 2); }
-size_t table_bytes(const MoePlan& c) { return up16(static_cast<size_t>(c.slots) * 4 * (2 + 64)); }
+size_t table_bytes(const MoePlan& c) { return up16(static_cast<size_t>(c.slots) * 4 * (1 + 64)); }
 
 }  // namespace
 
@@ -468,7 +433,7 @@ MoePlan plan_moe_layer(const MoeArgs& p, int num_cus) {
   const int64_t steps = static_cast<int64_t>(c.slots) * ((p.I + p.k_tail + 127) / 128);
   c.tiles = p.N % 32 == 0 && p.N / 32 * steps >= static_cast<int64_t>(2) * num_cus * kWaves * 4 ? 2 : 1;
   while (c.splits < kMaxSplits && static_cast<int64_t>(p.N / 16 / c.tiles) * c.splits < 2 * num_cus &&
-         steps >= 8 * c.splits * kWaves)
+         steps >= 8 * c.splits * (c.tiles == 2 ? 8 : 16))
     c.splits *= 2;
   return c;
 }
@@ -483,7 +448,7 @@ hipError_t launch_moe_layer(const MoePlan& c, const MoeArgs& p, void* workspace,
   uint32_t* arrived = reinterpret_cast<uint32_t*>(at);
   uint16_t* hidden = reinterpret_cast<uint16_t*>(at += kWorkspaceStateBytes);
   int32_t* const ints = reinterpret_cast<int32_t*>(at += hidden_bytes(p));
-  const Table table{ints, ints + c.slots, ints + 2 * c.slots};
+  const Table table{ints, ints + c.slots};
   float* parts = reinterpret_cast<float*>(at += table_bytes(c));
   const int rows = p.M <= 16 ? p.M * pitch_of(1) : std::max(16 * pitch_of(1), 32 * pitch_of(2));
   const int lds = c.parts > 1 ? std::max(rows, kWaves * 2 * 64 * 16) : rows;
@@ -503,19 +468,17 @@ hipError_t launch_moe_layer(const MoePlan& c, const MoeArgs& p, void* workspace,
                        : c.parts == 4 ? up(std::integral_constant<int, 4>{})
                                       : up(std::integral_constant<int, 8>{});
   if (e != hipSuccess) return e;
-  auto down = [&](auto together) {
-    constexpr int kT = decltype(together)::value;
-    const int sums = kWaves * p.M * sums_pitch(kT) * 4;
+  auto down = [&](auto kernel, int kT, int kN) {
+    const int sums = kN * p.M * sums_pitch(kT) * 4;
     if (sums > 64 * 1024) {
-      const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(&moe_down_kernel<kT>),
+      const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel),
                                                hipFuncAttributeMaxDynamicSharedMemorySize, sums);
       if (e != hipSuccess) return e;
     }
-    moe_down_kernel<kT><<<dim3(p.N / 16 / kT, c.splits), kThreads, sums, stream>>>(p, hidden, table, c.slots, parts,
-                                                                                  arrived);
+    kernel<<<dim3(p.N / 16 / kT, c.splits), 64 * kN, sums, stream>>>(p, hidden, table, c.slots, parts, arrived);
     return hipGetLastError();
   };
-  return c.tiles == 2 ? down(std::integral_constant<int, 2>{}) : down(std::integral_constant<int, 1>{});
+  return c.tiles == 2 ? down(&moe_down_kernel<2, 8, 2>, 2, 8) : down(&moe_down_kernel<1, 16, 3>, 1, 16);
 }
 
 }  // namespace prq
