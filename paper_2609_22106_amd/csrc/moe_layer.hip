@@ -32,16 +32,16 @@ namespace {
 using dev::f32x4;
 using dev::u32x4v;
 
-constexpr int kWaves = 8, kThreads = 64 * kWaves;
 constexpr int kMaxSplits = 8;                       // workgroups that share output tiles
 constexpr int kSteps = 2;                            // K steps of 128 in a wave's unit
 
-// What the first launch leaves of every slot: its expert and 2^16 times the number of its tokens (0:
-// none, or the expert is another slot's), and for column i the row of `hidden` times 64 plus the
-// token, -1 past the last.
+// What the first launch leaves: the second's items, an expert's tokens 16 at a time, experts in
+// ascending order; of each the expert and for column i the row of `hidden` times 64 plus the token, -1
+// past the last.  An expert that a token names twice may have an empty item.
 struct Table {
-  int32_t* slots;
-  int32_t* columns;                                  // [slots][64]
+  int32_t* total;                                    // the number of items
+  int32_t* experts;
+  int32_t* columns;                                  // [items][16]
 };
 
 // A lane's 32 weights of a K step (the 16 bytes of an MXFP4 block, its E8M0 code) as the four
@@ -74,30 +74,87 @@ struct Unit {
   }
 };
 
-// A lane's token's share of expert e: whether it has one, the first of its k ids that names it, and
-// the sum of the weights that do.
+// The tokens' experts and weights in LDS, a token's k entries apart by an odd number, at which 64 tokens'
+// j-th ones lie in different banks.
+struct Routing {
+  int* ids;
+  float* weights;
+  int pitch;
+  __device__ __forceinline__ Routing(const MoeArgs& p, unsigned char* lds) {
+    pitch = p.k | 1;
+    ids = reinterpret_cast<int*>(lds);
+    weights = reinterpret_cast<float*>(lds) + p.M * pitch;
+    const float inv = 1.0f / static_cast<float>(p.k);
+    for (int i = static_cast<int>(threadIdx.x); i < p.M * p.k; i += static_cast<int>(blockDim.x)) {
+      // i / k: i + 1/2 is at least 1 / 64 of a token from a whole one, the product off by 2^-23 of it
+      const int t = static_cast<int>((static_cast<float>(i) + 0.5f) * inv), at = t * pitch + i - t * p.k;
+      ids[at] = p.ids[i];
+      weights[at] = p.weights[i];
+    }
+    __syncthreads();
+  }
+};
+__host__ __device__ constexpr int routing_bytes(int M, int k) { return 8 * M * (k | 1); }
+
+// A lane's token's share of expert e (>= 0): whether it has one, the first of its k ids that names it,
+// and the sum of the weights that do.
 struct Share {
   bool has = false;
   int first = 0;
   float weight = 0.f;
-  __device__ __forceinline__ Share(const MoeArgs& p, int e) {
+  __device__ __forceinline__ Share(const MoeArgs& p, const Routing& r, int e) {
     const int lane = static_cast<int>(threadIdx.x) & 63;
     if (lane >= p.M) return;
-    const int32_t* ids = p.ids + lane * p.k;
-    for (int j0 = 0; j0 < p.k; j0 += 8) {
-      int id[8];
-#pragma unroll
-      for (int j = 0; j < 8; ++j) id[j] = j0 + j < p.k ? ids[j0 + j] : -1;
-#pragma unroll
-      for (int j = 0; j < 8; ++j)
-        if (id[j] == e) {                            // (e >= 0)
-          weight += p.weights[lane * p.k + j0 + j];
-          if (!has) first = j0 + j;
-          has = true;
-        }
-    }
+    for (int j = p.k - 1; j >= 0; --j)
+      if (r.ids[lane * r.pitch + j] == e) {
+        weight += r.weights[lane * r.pitch + j];
+        first = j;
+        has = true;
+      }
   }
 };
+
+// The table's entries of expert e's n tokens (lane i: token i's column), and with the first slot the
+// number of all.  The whole workgroup; bins: LDS for an int an expert.
+template <int kN>
+__device__ __forceinline__ void write_items(const MoeArgs& p, int slot, int e, int n, int column, const Table& table,
+                                            int* bins) {
+  __shared__ int sums[2][kN];
+  const int tid = static_cast<int>(threadIdx.x), lane = tid & 63, wave = tid >> 6;
+  __syncthreads();                                   // the routing has been read
+  for (int i = tid; i < p.E; i += 64 * kN) bins[i] = 0;
+  __syncthreads();
+  for (int i = tid; i < p.M * p.k; i += 64 * kN) {
+    const int id = p.ids[i];
+    if (id >= 0 && id < p.E) atomicAdd(&bins[id], 1);
+  }
+  __syncthreads();
+  int before = 0, all = 0;
+  for (int i = tid; i < p.E; i += 64 * kN) {
+    const int items = (bins[i] + 15) >> 4;
+    all += items;
+    if (i < e) before += items;
+  }
+  before = __builtin_amdgcn_readlane(dev::prefix_sum(before), 63);
+  all = __builtin_amdgcn_readlane(dev::prefix_sum(all), 63);
+  if (lane == 0) {
+    sums[0][wave] = before;
+    sums[1][wave] = all;
+  }
+  __syncthreads();
+  before = all = 0;
+  for (int w = 0; w < kN; ++w) {
+    before += sums[0][w];
+    all += sums[1][w];
+  }
+  if (slot == 0 && tid == 0) *table.total = all;
+  if (wave || n == 0) return;
+  const int items = (bins[e] + 15) >> 4;
+  for (int i = lane; i < items * 16; i += 64) {
+    if (i % 16 == 0) table.experts[before + i / 16] = e;
+    table.columns[before * 16 + i] = i < 64 ? column : -1;
+  }
+}
 
 // Rows of x in LDS: kPiece / kG elements of 16 kG tokens at a time, rows 16 bytes past a multiple of
 // 128, at which the lanes of an operand's read meet different banks.
@@ -107,13 +164,13 @@ __host__ __device__ constexpr int pitch_of(int blocks) { return kPiece / blocks 
 
 // First launch: a wave has 16 intermediate features of one expert (a gate tile and an up tile) for
 // all of its tokens, and of the steps of H every kS-th unit.  The workgroup's waves share the
-// expert's rows of x in LDS.
-template <int kS>
-__global__ __launch_bounds__(kThreads, 4) void moe_up_kernel(const MoeArgs p, bool by_expert,
+// expert's rows of x in LDS.  The last workgroup of a slot writes the table.
+template <int kN, int kS>
+__global__ __launch_bounds__(64 * kN, 4) void moe_up_kernel(const MoeArgs p, bool by_expert, int rows_bytes,
                                                               uint16_t* __restrict__ hidden, const Table table) {
-  constexpr int kTiles = kWaves / kS;
+  constexpr int kTiles = kN / kS;
   extern __shared__ __align__(16) unsigned char smem[];
-  f32x4* const sums = reinterpret_cast<f32x4*>(smem);       // [kWaves][2][64], behind the rows of x
+  f32x4* const sums = reinterpret_cast<f32x4*>(smem + rows_bytes);       // [kN][2][64]
   const int tid = static_cast<int>(threadIdx.x), lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int c = lane & 15, q = lane >> 4;
@@ -121,43 +178,78 @@ __global__ __launch_bounds__(kThreads, 4) void moe_up_kernel(const MoeArgs p, bo
   const int tile = static_cast<int>(blockIdx.x) * kTiles + wave / kS, part = wave % kS;
   const int steps = (p.H + 127) >> 7, tiles = p.I >> 4, units = (steps + kSteps - 1) / kSteps;
 
-  const int e = by_expert ? slot : p.ids[slot];
-  const bool reached = e >= 0 && e < p.E;
-  const Share share(p, reached ? e : -2);
-  const uint64_t mine = __ballot(share.has);
+  const Routing routing(p, smem);
+  int e = slot;
+  if (!by_expert) {
+    e = __builtin_amdgcn_readfirstlane(routing.ids[slot / p.k * routing.pitch + slot % p.k]);
+    if (e >= p.E) e = -1;
+  }
+  const Share share(p, routing, e);
+  const uint64_t mine = e < 0 ? 0 : __ballot(share.has);
   int n = __popcll(mine);
   if (!by_expert) {                                  // an earlier pair of the same expert has it
     const int token = slot / p.k;
-    if (__ballot(share.has && (lane < token || (lane == token && lane * p.k + share.first < slot)))) n = 0;
+    if (__ballot(e >= 0 && share.has && (lane < token || (lane == token && lane * p.k + share.first < slot)))) n = 0;
   }
   // Column i: the i-th token.  Lanes without a share go behind the others.
   const uint64_t below = (uint64_t{1} << lane) - 1;
-  const int at = share.has ? __popcll(mine & below) : __popcll(mine) + __popcll(~mine & below);
-  const int row = share.has ? lane * p.k + share.first : -1;
-  const int entry = share.has ? row * 64 + lane : -1;
+  const bool has = mine >> lane & 1;
+  const int at = has ? __popcll(mine & below) : __popcll(mine) + __popcll(~mine & below);
+  const int entry = has ? (lane * p.k + share.first) * 64 + lane : -1;
   const int column = __builtin_amdgcn_ds_permute(4 * at, entry);
-  if (blockIdx.x == 0 && wave == 0) {
-    if (lane == 0) table.slots[slot] = n ? n << 16 | e : 0;
-    table.columns[slot * 64 + lane] = column;
-  }
+  if (blockIdx.x + 1 == gridDim.x) return write_items<kN>(p, slot, e, n, column, table, reinterpret_cast<int*>(smem));
   if (n == 0) return;                                // the whole workgroup
   const float weight = __int_as_float(__builtin_amdgcn_ds_permute(4 * at, __float_as_int(share.weight)));
 
-  const bool work = tile < tiles;
-  const int64_t first = static_cast<int64_t>(e) * 2 * tiles + (work ? tile : 0);
+  const int64_t first = static_cast<int64_t>(e) * 2 * tiles + min(tile, tiles - 1);
   // Tokens 16 block0 .. 16 (block0 + kG) - 1 of the expert.
   auto pass = [&](int block0, auto blocks) {
     constexpr int kG = decltype(blocks)::value, kUnits = kPieceUnits / kG, kPitch = pitch_of(kG);
-    constexpr int kStride = kS < kUnits ? kS : kUnits;     // (parts past a piece's units have none)
     const int rows = min(n - 16 * block0, 16 * kG);
+    // A piece's units of a wave, of which there is an even number (past the end the last one's again, and
+    // unused), so that the two that are under way have registers of their own.
+    auto turns = [&](int u0) { return ((min(units - u0, kUnits) + kS - 1) / kS + 1) & ~1; };
+    struct Both {
+      Unit gate, up;
+    } ring[2];
+    int next_u0 = 0, next_turn = 0;                  // what is asked for next
+    auto ask = [&](Both& w) {
+      const int u = min(next_u0 + next_turn * kS + part, units - 1);
+      w.gate.load(p.up_codes, p.up_scales, first, steps, u);
+      w.up.load(p.up_codes, p.up_scales, first + tiles, steps, u);
+      if (++next_turn == turns(next_u0)) {
+        next_turn = 0;
+        next_u0 = min(next_u0 + kUnits, (units - 1) / kUnits * kUnits);
+      }
+    };
     f32x4 acc[kG][2] = {};
-    Unit gate, up;
-    gate.load(p.up_codes, p.up_scales, first, steps, min(part, units - 1));
-    up.load(p.up_codes, p.up_scales, first + tiles, steps, min(part, units - 1));
+    auto compute = [&](const Both& w, int u0, int turn) {
+      const int u = turn * kS + part;                // of the piece
+      if (u >= min(units - u0, kUnits)) return;
+#pragma unroll
+      for (int i = 0; i < kSteps; ++i) {
+        u32x4v a[4], a2[4], b[4];
+        to_bf16(w.gate.codes[i], w.gate.scales >> (8 * i) & 255u, a);
+        to_bf16(w.up.codes[i], w.up.scales >> (8 * i) & 255u, a2);
+#pragma unroll
+        for (int g = 0; g < kG; ++g) {
+          // columns without a token read the first one's row: their sums are nobody's
+          const unsigned char* from = smem + (16 * g + c < rows ? 16 * g + c : 0) * kPitch + (u * kSteps + i) * 256 + q * 64;
+#pragma unroll
+          for (int j = 0; j < 4; ++j) b[j] = *reinterpret_cast<const u32x4v*>(from + 16 * j);
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            acc[g][0] = dev::mfma_bf16(a[j], b[j], acc[g][0]);
+            acc[g][1] = dev::mfma_bf16(a2[j], b[j], acc[g][1]);
+          }
+        }
+      }
+    };
+    ask(ring[0]);
     for (int u0 = 0; u0 < units; u0 += kUnits) {
-      if (u0 || block0) __syncthreads();             // what is there has been read
+      __syncthreads();                               // what is there has been read
       constexpr int kRow = kPiece / kG / 8;          // 16-byte parts of a row
-      for (int i = tid; i < rows * kRow; i += kThreads) {
+      for (int i = tid; i < rows * kRow; i += 64 * kN) {
         const int r = i / kRow, k = u0 * 128 * kSteps + i % kRow * 8;
         const int token = __builtin_amdgcn_readfirstlane(__shfl(column, 16 * block0 + r, 64)) & 63;
         u32x4v v = 0u;
@@ -165,38 +257,19 @@ __global__ __launch_bounds__(kThreads, 4) void moe_up_kernel(const MoeArgs p, bo
         *reinterpret_cast<u32x4v*>(smem + r * kPitch + i % kRow * 16) = v;
       }
       __syncthreads();
-      for (int u = u0 + part; u < min(u0 + kUnits, units); u += kStride) {
-        const Unit g0 = gate, up0 = up;
-        const int next = min(u + kStride, units - 1);
-        gate.load(p.up_codes, p.up_scales, first, steps, next);
-        up.load(p.up_codes, p.up_scales, first + tiles, steps, next);
-#pragma unroll
-        for (int i = 0; i < kSteps; ++i) {
-          u32x4v a[4], b[4];
-          to_bf16(g0.codes[i], g0.scales >> (8 * i) & 255u, a);
-          u32x4v a2[4];
-          to_bf16(up0.codes[i], up0.scales >> (8 * i) & 255u, a2);
-#pragma unroll
-          for (int g = 0; g < kG; ++g) {
-            // columns without a token read the first one's row: their sums are nobody's
-            const unsigned char* from = smem + (16 * g + c < rows ? 16 * g + c : 0) * kPitch +
-                                        ((u - u0) * kSteps + i) * 256 + q * 64;
-#pragma unroll
-            for (int j = 0; j < 4; ++j) b[j] = *reinterpret_cast<const u32x4v*>(from + 16 * j);
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-              acc[g][0] = dev::mfma_bf16(a[j], b[j], acc[g][0]);
-              acc[g][1] = dev::mfma_bf16(a2[j], b[j], acc[g][1]);
-            }
-          }
-        }
+#pragma unroll 1
+      for (int turn = 0; turn < turns(u0); turn += 2) {
+        ask(ring[1]);
+        compute(ring[0], u0, turn);
+        ask(ring[0]);
+        compute(ring[1], u0, turn + 1);
       }
     }
 #pragma unroll
     for (int g = 0; g < kG; ++g) {
       f32x4 z = acc[g][0], y = acc[g][1];
       if constexpr (kS > 1) {
-        __syncthreads();
+        if (g || block0) __syncthreads();
         sums[(wave * 2) * 64 + lane] = z;
         sums[(wave * 2 + 1) * 64 + lane] = y;
         __syncthreads();
@@ -210,7 +283,7 @@ __global__ __launch_bounds__(kThreads, 4) void moe_up_kernel(const MoeArgs p, bo
       // column c's features 4 q .. 4 q + 3 of the tile
       const int col = __shfl(column, 16 * (block0 + g) + c, 64);
       const float w = __shfl(weight, 16 * (block0 + g) + c, 64);
-      if (16 * g + c < rows && work) {
+      if (16 * g + c < rows && tile < tiles) {
         float h[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) h[i] = z[i] / (1.f + expf(-z[i])) * y[i] * w;
@@ -229,11 +302,10 @@ __global__ __launch_bounds__(kThreads, 4) void moe_up_kernel(const MoeArgs p, bo
 // Floats between two tokens' sums of kT tiles in LDS: the 16 columns of a store meet different banks.
 constexpr int sums_pitch(int tiles) { return 16 * tiles + 4; }
 
-// Second launch: kT tiles of 16 output features of all tokens.  Its items are an expert's tokens, 16 at
-// a time; they are dealt to the tiles' workgroups, up to kWindow at a time, and the K steps of a
-// window's items evenly, in order, to the waves.  An item's sums are added to its tokens' in LDS, of
-// which each wave has its own.  The waves' sums are added in their order, the workgroups' in theirs, by
-// the one that arrives last.
+// Second launch: kT tiles of 16 output features of all tokens.  The items are dealt in turn to the
+// tiles' workgroups, and the K steps of up to kWindow of a workgroup's evenly, in order, to its waves.
+// An item's sums are added to its tokens' in LDS, of which each wave has its own.  The waves' sums are
+// added in their order, the workgroups' in theirs, by the one that arrives last.
 //
 // A wave asks for the weights and activations of a step kAhead steps ahead.  The loop has loads
 // without conditions only (past the end the last step's again, columns without a token outside the
@@ -242,11 +314,11 @@ constexpr int kWindow = 64;
 
 template <int kT, int kN, int kAhead>
 __global__ __launch_bounds__(64 * kN, 4) void moe_down_kernel(const MoeArgs p, const uint16_t* __restrict__ hidden,
-                                                               const Table table, int slots, float* parts,
+                                                               const Table table, int most, float* parts,
                                                                uint32_t* arrived) {
   constexpr int kPitch = sums_pitch(kT), kRing = kAhead + 1;
   extern __shared__ __align__(16) float own[];       // [kN][M][kPitch]
-  __shared__ int sh_items[kWindow];                  // slot, 2^13 times the block, 2^16 times the expert
+  __shared__ int sh_experts[kWindow];
   __shared__ int sh_columns[kWindow][16];
   __shared__ int sh_last;
   const int tid = static_cast<int>(threadIdx.x), lane = tid & 63;
@@ -255,35 +327,32 @@ __global__ __launch_bounds__(64 * kN, 4) void moe_down_kernel(const MoeArgs p, c
   const int tile = static_cast<int>(blockIdx.x) * kT, splits = static_cast<int>(gridDim.y), part = static_cast<int>(blockIdx.y);
   const int K = p.I + p.k_tail, steps = (K + 127) >> 7, groups = (steps + 3) >> 2, tiles = p.N >> 4;
   const auto rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint16_t*>(hidden), 0, p.M * p.k * p.I * 2, 0x00020000);
-
-  // Lane i: slot base + i, and the number of its items.
-  auto slot_at = [&](int base) { return base + lane < slots ? table.slots[base + lane] : 0; };
-  auto items_of = [](int slot) { return (slot + (15 << 16)) >> 20; };
-  int total = 0;
-  for (int base = 0; base < slots; base += 64)
-    total += __builtin_amdgcn_readlane(dev::prefix_sum(items_of(slot_at(base))), 63);
   float* const mine = own + wave * p.M * kPitch;
-  for (int i = lane; i < p.M * kPitch / 4; i += 64) reinterpret_cast<f32x4*>(mine)[i] = 0.f;
 
-  const int last_item = static_cast<int>(static_cast<int64_t>(total) * (part + 1) / splits);
-  for (int item0 = static_cast<int>(static_cast<int64_t>(total) * part / splits); item0 < last_item; item0 += kWindow) {
-    const int items = min(last_item - item0, kWindow);
-    __syncthreads();                                 // the window before has been read
-    if (wave == 0) {
-      int before = 0;
-      for (int base = 0; base < slots && before < item0 + items; base += 64) {
-        const int slot = slot_at(base), n = items_of(slot), upto = dev::prefix_sum(n);
-        for (int g = 0; g < n; ++g) {
-          const int at = before + upto - n + g - item0;
-          if (at >= 0 && at < items) sh_items[at] = (slot & 0xFFFF) << 16 | g << 13 | (base + lane);
-        }
-        before += __builtin_amdgcn_readlane(upto, 63);
-      }
+  // Item i of this workgroup is item part + splits i of all; the first window's are loaded before their
+  // number is known.
+  for (int item0 = 0;; item0 += kWindow) {
+    int expert = 0, column[kWindow * 16 / (64 * kN)];
+    const int at = part + splits * item0;
+    if (tid < kWindow) expert = table.experts[min(at + splits * tid, most - 1)];
+#pragma unroll
+    for (int i = 0; i < kWindow * 16 / (64 * kN); ++i) {
+      const int entry = tid + i * 64 * kN;
+      column[i] = table.columns[min(at + splits * (entry >> 4), most - 1) * 16 + (entry & 15)];
     }
-    __syncthreads();
-    for (int i = tid; i < items * 16; i += 64 * kN) {
-      const int item = sh_items[i >> 4];
-      sh_columns[i >> 4][i & 15] = table.columns[(item & 0x1FFF) * 64 + 16 * (item >> 13 & 3) + (i & 15)];
+    const int total = *table.total;
+    if (item0 == 0) {
+      for (int i = lane; i < p.M * kPitch / 4; i += 64) reinterpret_cast<f32x4*>(mine)[i] = 0.f;
+    } else {
+      __syncthreads();                               // the window before has been read
+    }
+    const int items = min((total - at + splits - 1) / splits, kWindow);
+    if (at >= total) break;                          // the whole workgroup
+    if (tid < kWindow) sh_experts[tid] = expert;
+#pragma unroll
+    for (int i = 0; i < kWindow * 16 / (64 * kN); ++i) {
+      const int entry = tid + i * 64 * kN;
+      sh_columns[entry >> 4][entry & 15] = column[i];
     }
     __syncthreads();
 
@@ -296,7 +365,7 @@ __global__ __launch_bounds__(64 * kN, 4) void moe_down_kernel(const MoeArgs p, c
       const uint32_t* scales;
       uint32_t row;
       auto enter = [&] {
-        const int64_t first = static_cast<int64_t>(__builtin_amdgcn_readfirstlane(sh_items[item]) >> 16) * tiles + tile;
+        const int64_t first = static_cast<int64_t>(__builtin_amdgcn_readfirstlane(sh_experts[item])) * tiles + tile;
         codes = reinterpret_cast<const u32x4v*>(p.down_codes) + first * steps * 64;
         scales = reinterpret_cast<const uint32_t*>(p.down_scales) + first * groups * 64;
         column = sh_columns[item][c];
@@ -416,7 +485,11 @@ __global__ __launch_bounds__(64 * kN, 4) void moe_down_kernel(const MoeArgs p, c
 
 size_t up16(size_t n) { return (n + 15) & ~size_t{15}; }
 size_t hidden_bytes(const MoeArgs& p) { return up16(static_cast<size_t>(p.M) * p.k * p.I * 2); }
-size_t table_bytes(const MoePlan& c) { return up16(static_cast<size_t>(c.slots) * 4 * (1 + 64)); }
+// An expert has as many items as 16 go into the pairs that name it, rounded up.
+int most_items(const MoePlan& c, const MoeArgs& p) { return std::min(p.M * p.k, c.slots + p.M * p.k / 16); }
+size_t table_bytes(const MoePlan& c, const MoeArgs& p) {
+  return up16(4 * (4 + static_cast<size_t>(most_items(c, p)) * (1 + 16)));
+}
 
 }  // namespace
 
@@ -424,22 +497,19 @@ MoePlan plan_moe_layer(const MoeArgs& p, int num_cus) {
   MoePlan c;
   c.slots = std::min(p.E, p.M * p.k);
   c.by_expert = c.slots == p.E;
-  // The first launch: 16 waves a CU, by parts of H where the tiles are fewer.
-  const int64_t tiles = static_cast<int64_t>(p.I / 16) * c.slots;
-  const int up_units = (p.H + 128 * kSteps - 1) / (128 * kSteps);
-  while (c.parts < kWaves && c.parts < up_units && tiles * c.parts < 16 * num_cus) c.parts *= 2;
-  // The second: two workgroups a CU, of a tile, or of two where the waves have steps enough, so that the
+  // The first launch: a wave a tile, or four where those would be few.
+  c.parts = static_cast<int64_t>(p.I / 16) * c.slots <= 3 * num_cus ? 4 : 1;
+  // The second: a workgroup a CU, of a tile, or of two where the waves have steps enough, so that the
   // activations are loaded for two.
   const int64_t steps = static_cast<int64_t>(c.slots) * ((p.I + p.k_tail + 127) / 128);
-  c.tiles = p.N % 32 == 0 && p.N / 32 * steps >= static_cast<int64_t>(2) * num_cus * kWaves * 4 ? 2 : 1;
-  while (c.splits < kMaxSplits && static_cast<int64_t>(p.N / 16 / c.tiles) * c.splits < 2 * num_cus &&
-         steps >= 8 * c.splits * (c.tiles == 2 ? 8 : 16))
-    c.splits *= 2;
+  c.tiles = p.N % 32 == 0 && p.N / 32 * steps >= static_cast<int64_t>(2) * num_cus * 32 ? 2 : 1;
+  c.splits = static_cast<int>(std::min<int64_t>(num_cus / (p.N / 16 / c.tiles), steps / 32));
+  c.splits = std::max(1, std::min(c.splits, kMaxSplits));
   return c;
 }
 
 size_t moe_workspace_bytes(const MoePlan& c, const MoeArgs& p) {
-  return kWorkspaceStateBytes + hidden_bytes(p) + table_bytes(c) +
+  return kWorkspaceStateBytes + hidden_bytes(p) + table_bytes(c, p) +
          (c.splits > 1 ? static_cast<size_t>(c.splits) * p.M * p.N * 4 : 0);
 }
 
@@ -448,25 +518,23 @@ hipError_t launch_moe_layer(const MoePlan& c, const MoeArgs& p, void* workspace,
   uint32_t* arrived = reinterpret_cast<uint32_t*>(at);
   uint16_t* hidden = reinterpret_cast<uint16_t*>(at += kWorkspaceStateBytes);
   int32_t* const ints = reinterpret_cast<int32_t*>(at += hidden_bytes(p));
-  const Table table{ints, ints + c.slots};
-  float* parts = reinterpret_cast<float*>(at += table_bytes(c));
+  const int most = most_items(c, p);
+  const Table table{ints, ints + 4 + 16 * most, ints + 4};
+  float* parts = reinterpret_cast<float*>(at += table_bytes(c, p));
   const int rows = p.M <= 16 ? p.M * pitch_of(1) : std::max(16 * pitch_of(1), 32 * pitch_of(2));
-  const int lds = c.parts > 1 ? std::max(rows, kWaves * 2 * 64 * 16) : rows;
-  auto up = [&](auto shared) {
-    constexpr int kS = decltype(shared)::value, kTiles = kWaves / kS;
+  auto up = [&](auto kernel, int kN, int kS) {
+    const int lds = std::max(rows + (kS > 1 ? kN * 2 * 64 * 16 : 0), std::max(routing_bytes(p.M, p.k), 4 * p.E));
     if (lds > 64 * 1024) {
-      const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(&moe_up_kernel<kS>),
+      const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel),
                                                hipFuncAttributeMaxDynamicSharedMemorySize, lds);
       if (e != hipSuccess) return e;
     }
-    moe_up_kernel<kS><<<dim3((p.I / 16 + kTiles - 1) / kTiles, c.slots), kThreads, lds, stream>>>(p, c.by_expert,
-                                                                                                   hidden, table);
+    const int tiles = kN / kS;
+    kernel<<<dim3((p.I / 16 + tiles - 1) / tiles + 1, c.slots), 64 * kN, lds, stream>>>(
+        p, c.by_expert, rows, hidden, table);
     return hipGetLastError();
   };
-  const hipError_t e = c.parts == 1   ? up(std::integral_constant<int, 1>{})
-                       : c.parts == 2 ? up(std::integral_constant<int, 2>{})
-                       : c.parts == 4 ? up(std::integral_constant<int, 4>{})
-                                      : up(std::integral_constant<int, 8>{});
+  const hipError_t e = c.parts == 1 ? up(&moe_up_kernel<8, 1>, 8, 1) : up(&moe_up_kernel<4, 4>, 4, 4);
   if (e != hipSuccess) return e;
   auto down = [&](auto kernel, int kT, int kN) {
     const int sums = kN * p.M * sums_pitch(kT) * 4;
@@ -475,10 +543,10 @@ hipError_t launch_moe_layer(const MoePlan& c, const MoeArgs& p, void* workspace,
                                                hipFuncAttributeMaxDynamicSharedMemorySize, sums);
       if (e != hipSuccess) return e;
     }
-    kernel<<<dim3(p.N / 16 / kT, c.splits), 64 * kN, sums, stream>>>(p, hidden, table, c.slots, parts, arrived);
+    kernel<<<dim3(p.N / 16 / kT, c.splits), 64 * kN, sums, stream>>>(p, hidden, table, most, parts, arrived);
     return hipGetLastError();
   };
-  return c.tiles == 2 ? down(&moe_down_kernel<2, 8, 2>, 2, 8) : down(&moe_down_kernel<1, 16, 3>, 1, 16);
+  return c.tiles == 2 ? down(&moe_down_kernel<2, 4, 2>, 2, 4) : down(&moe_down_kernel<1, 4, 3>, 1, 4);
 }
 
 }  // namespace prq
