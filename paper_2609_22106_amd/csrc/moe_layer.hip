@@ -35,14 +35,23 @@ using dev::u32x4v;
 constexpr int kMaxSplits = 8;                       // workgroups that share output tiles
 constexpr int kSteps = 2;                            // K steps of 128 in a wave's unit
 
-// What the first launch leaves: the second's items, an expert's tokens 16 at a time, experts in
-// ascending order; of each the expert and for column i the row of `hidden` times 64 plus the token, -1
-// past the last.  An expert that a token names twice may have an empty item.
+// What the first launch leaves.  `hidden`: w h of the pairs, an expert's behind those of the lower
+// ones, its tokens 16 at a time: of n of them [octets][n][8] elements, the 16 octets of a K step in the
+// order in which a lane group's operands are loaded (octet_at), so that one load's lanes read one
+// stretch.  The table: the second launch's items, an expert's tokens 16 at a time, experts in
+// ascending order; of each the expert, its tokens in `hidden` (first 2^5 n), and the token of column i,
+// -1 past the last.  An expert that a token names twice may have an empty item.
 struct Table {
   int32_t* total;                                    // the number of items
   int32_t* experts;
+  int32_t* rows;
   int32_t* columns;                                  // [items][16]
 };
+
+// Elements of a row of `hidden`: whole K steps.
+__host__ __device__ constexpr int64_t hidden_pitch(int I) { return (I + 127) & ~127; }
+// Where octet o of a row stands: lane group q's j-th of a K step, which is octet 4 q + j of it, at 4 j + q.
+__device__ __forceinline__ int octet_at(int o) { return (o & ~15) | (o & 3) << 2 | (o >> 2 & 3); }
 
 // A lane's 32 weights of a K step (the 16 bytes of an MXFP4 block, its E8M0 code) as the four
 // bf16 operands of the matrix instruction.
@@ -84,14 +93,16 @@ struct Routing {
     pitch = p.k | 1;
     ids = reinterpret_cast<int*>(lds);
     weights = reinterpret_cast<float*>(lds) + p.M * pitch;
-    const float inv = 1.0f / static_cast<float>(p.k);
     for (int i = static_cast<int>(threadIdx.x); i < p.M * p.k; i += static_cast<int>(blockDim.x)) {
-      // i / k: i + 1/2 is at least 1 / 64 of a token from a whole one, the product off by 2^-23 of it
-      const int t = static_cast<int>((static_cast<float>(i) + 0.5f) * inv), at = t * pitch + i - t * p.k;
+      const int t = token(p, i), at = t * pitch + i - t * p.k;
       ids[at] = p.ids[i];
       weights[at] = p.weights[i];
     }
     __syncthreads();
+  }
+  // Pair i's: i + 1/2 is at least 1 / 64 of a token from a whole one, the product off by 2^-22 of it.
+  __device__ __forceinline__ int token(const MoeArgs& p, int i) const {
+    return static_cast<int>((static_cast<float>(i) + 0.5f) * (1.0f / static_cast<float>(p.k)));
   }
 };
 __host__ __device__ constexpr int routing_bytes(int M, int k) { return 8 * M * (k | 1); }
@@ -114,11 +125,11 @@ struct Share {
   }
 };
 
-// The table's entries of expert e's n tokens (lane i: token i's column), and with the first slot the
-// number of all.  The whole workgroup; bins: LDS for an int an expert.
+// The table's entries of expert e's n tokens (lane i: the i-th), whose pairs are behind `pairs` others, and
+// with the first slot the number of all.  The whole workgroup; bins: LDS for an int an expert.
 template <int kN>
-__device__ __forceinline__ void write_items(const MoeArgs& p, int slot, int e, int n, int column, const Table& table,
-                                            int* bins) {
+__device__ __forceinline__ void write_items(const MoeArgs& p, int slot, int e, int n, int token, int pairs,
+                                            const Table& table, int* bins) {
   __shared__ int sums[2][kN];
   const int tid = static_cast<int>(threadIdx.x), lane = tid & 63, wave = tid >> 6;
   __syncthreads();                                   // the routing has been read
@@ -151,8 +162,11 @@ __device__ __forceinline__ void write_items(const MoeArgs& p, int slot, int e, i
   if (wave || n == 0) return;
   const int items = (bins[e] + 15) >> 4;
   for (int i = lane; i < items * 16; i += 64) {
-    if (i % 16 == 0) table.experts[before + i / 16] = e;
-    table.columns[before * 16 + i] = i < 64 ? column : -1;
+    if (i % 16 == 0) {
+      table.experts[before + i / 16] = e;
+      table.rows[before + i / 16] = (pairs + i) << 5 | max(0, min(n - i, 16));
+    }
+    table.columns[before * 16 + i] = i < 64 ? token : -1;
   }
 }
 
@@ -195,9 +209,13 @@ __global__ __launch_bounds__(64 * kN, 4) void moe_up_kernel(const MoeArgs p, boo
   const uint64_t below = (uint64_t{1} << lane) - 1;
   const bool has = mine >> lane & 1;
   const int at = has ? __popcll(mine & below) : __popcll(mine) + __popcll(~mine & below);
-  const int entry = has ? (lane * p.k + share.first) * 64 + lane : -1;
-  const int column = __builtin_amdgcn_ds_permute(4 * at, entry);
-  if (blockIdx.x + 1 == gridDim.x) return write_items<kN>(p, slot, e, n, column, table, reinterpret_cast<int*>(smem));
+  const int column = __builtin_amdgcn_ds_permute(4 * at, has ? lane : -1);
+  int pairs = 0;                                     // of lower experts
+  for (int i = lane; i < ((p.M * p.k + 63) & ~63); i += 64) {
+    const int t = routing.token(p, i), id = i < p.M * p.k ? routing.ids[t * routing.pitch + i - t * p.k] : -1;
+    pairs += __popcll(__ballot(id >= 0 && id < e));
+  }
+  if (blockIdx.x + 1 == gridDim.x) return write_items<kN>(p, slot, e, n, column, pairs, table, reinterpret_cast<int*>(smem));
   if (n == 0) return;                                // the whole workgroup
   const float weight = __int_as_float(__builtin_amdgcn_ds_permute(4 * at, __float_as_int(share.weight)));
 
@@ -281,14 +299,16 @@ __global__ __launch_bounds__(64 * kN, 4) void moe_up_kernel(const MoeArgs p, boo
         }
       }
       // column c's features 4 q .. 4 q + 3 of the tile
-      const int col = __shfl(column, 16 * (block0 + g) + c, 64);
       const float w = __shfl(weight, 16 * (block0 + g) + c, 64);
-      if (16 * g + c < rows && tile < tiles) {
+      const int columns = min(n - 16 * (block0 + g), 16);
+      if (c < columns && tile < tiles) {
         float h[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) h[i] = z[i] / (1.f + expf(-z[i])) * y[i] * w;
         const dev::u32x2 v = {dev::pack_bf16(h[0], h[1]), dev::pack_bf16(h[2], h[3])};
-        *reinterpret_cast<dev::u32x2*>(hidden + static_cast<int64_t>(col >> 6) * p.I + 16 * tile + 4 * q) = v;
+        uint16_t* to = hidden + (pairs + 16 * (block0 + g)) * hidden_pitch(p.I) +
+                       (octet_at(2 * tile + (q >> 1)) * columns + c) * 8 + 4 * (q & 1);
+        *reinterpret_cast<dev::u32x2*>(to) = v;
       }
     }
   };
@@ -318,7 +338,7 @@ __global__ __launch_bounds__(64 * kN, 4) void moe_down_kernel(const MoeArgs p, c
                                                                uint32_t* arrived) {
   constexpr int kPitch = sums_pitch(kT), kRing = kAhead + 1;
   extern __shared__ __align__(16) float own[];       // [kN][M][kPitch]
-  __shared__ int sh_experts[kWindow];
+  __shared__ int sh_experts[kWindow], sh_rows[kWindow];
   __shared__ int sh_columns[kWindow][16];
   __shared__ int sh_last;
   const int tid = static_cast<int>(threadIdx.x), lane = tid & 63;
@@ -326,15 +346,19 @@ __global__ __launch_bounds__(64 * kN, 4) void moe_down_kernel(const MoeArgs p, c
   const int c = lane & 15, q = lane >> 4;
   const int tile = static_cast<int>(blockIdx.x) * kT, splits = static_cast<int>(gridDim.y), part = static_cast<int>(blockIdx.y);
   const int K = p.I + p.k_tail, steps = (K + 127) >> 7, groups = (steps + 3) >> 2, tiles = p.N >> 4;
-  const auto rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint16_t*>(hidden), 0, p.M * p.k * p.I * 2, 0x00020000);
+  const auto rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint16_t*>(hidden), 0,
+                                                      static_cast<int>(p.M * p.k * hidden_pitch(p.I) * 2), 0x00020000);
   float* const mine = own + wave * p.M * kPitch;
 
   // Item i of this workgroup is item part + splits i of all; the first window's are loaded before their
   // number is known.
   for (int item0 = 0;; item0 += kWindow) {
-    int expert = 0, column[kWindow * 16 / (64 * kN)];
+    int expert = 0, rows = 0, column[kWindow * 16 / (64 * kN)];
     const int at = part + splits * item0;
-    if (tid < kWindow) expert = table.experts[min(at + splits * tid, most - 1)];
+    if (tid < kWindow) {
+      expert = table.experts[min(at + splits * tid, most - 1)];
+      rows = table.rows[min(at + splits * tid, most - 1)];
+    }
 #pragma unroll
     for (int i = 0; i < kWindow * 16 / (64 * kN); ++i) {
       const int entry = tid + i * 64 * kN;
@@ -348,7 +372,10 @@ __global__ __launch_bounds__(64 * kN, 4) void moe_down_kernel(const MoeArgs p, c
     }
     const int items = min((total - at + splits - 1) / splits, kWindow);
     if (at >= total) break;                          // the whole workgroup
-    if (tid < kWindow) sh_experts[tid] = expert;
+    if (tid < kWindow) {
+      sh_experts[tid] = expert;
+      sh_rows[tid] = rows;
+    }
 #pragma unroll
     for (int i = 0; i < kWindow * 16 / (64 * kN); ++i) {
       const int entry = tid + i * 64 * kN;
@@ -358,18 +385,19 @@ __global__ __launch_bounds__(64 * kN, 4) void moe_down_kernel(const MoeArgs p, c
 
     const int begin = items * steps * wave / kN, n = items * steps * (wave + 1) / kN - begin;
     if (n > 0) {
-      // The step that is asked for next: its item, the expert's tiles, and where this lane's column
-      // is in `hidden` (past its end: no token).
-      int item = begin / steps, step = begin % steps, u = 0, column;
+      // The step that is asked for next: its item, the expert's tiles, and where the item's tokens are
+      // in `hidden`, in bytes, and how many.
+      int item = begin / steps, step = begin % steps, u = 0, columns;
       const u32x4v* codes;
       const uint32_t* scales;
-      uint32_t row;
+      uint32_t base;
       auto enter = [&] {
         const int64_t first = static_cast<int64_t>(__builtin_amdgcn_readfirstlane(sh_experts[item])) * tiles + tile;
         codes = reinterpret_cast<const u32x4v*>(p.down_codes) + first * steps * 64;
         scales = reinterpret_cast<const uint32_t*>(p.down_scales) + first * groups * 64;
-        column = sh_columns[item][c];
-        row = column < 0 ? 0x80000000u : static_cast<uint32_t>(column >> 6) * static_cast<uint32_t>(2 * p.I);
+        const int rows = __builtin_amdgcn_readfirstlane(sh_rows[item]);
+        base = static_cast<uint32_t>((rows >> 5) * hidden_pitch(p.I) * 2);
+        columns = rows & 31;
       };
       enter();
       struct Step {
@@ -378,8 +406,10 @@ __global__ __launch_bounds__(64 * kN, 4) void moe_down_kernel(const MoeArgs p, c
         u32x4v b[4];
       } ring[kRing];
       auto ask = [&](Step& s) {
-        const int k = 128 * step + 32 * q;           // the tail meets the last values again, zeros behind it
-        const uint32_t at = k < K ? row + 2 * static_cast<uint32_t>(k < p.I ? k : k - p.k_tail) : 0x80000000u;
+        int k = 128 * step + 32 * q;                 // the tail meets the last values again, zeros behind it
+        const bool in = k < K && c < columns;
+        if (k >= p.I) k -= p.k_tail;
+        const uint32_t at = in ? base + static_cast<uint32_t>((((k >> 7) * 16 + (k >> 5 & 3)) * columns + c) * 16) : 0x80000000u;
 #pragma unroll
         for (int t = 0; t < kT; ++t) {
           s.codes[t] = __builtin_nontemporal_load(codes + (t * steps + step) * 64 + lane);
@@ -387,7 +417,7 @@ __global__ __launch_bounds__(64 * kN, 4) void moe_down_kernel(const MoeArgs p, c
         }
 #pragma unroll
         for (int j = 0; j < 4; ++j)
-          s.b[j] = __builtin_bit_cast(u32x4v, __builtin_amdgcn_raw_buffer_load_b128(rsrc, at, 16 * j, 0));
+          s.b[j] = __builtin_bit_cast(u32x4v, __builtin_amdgcn_raw_buffer_load_b128(rsrc, at, 64 * j * columns, 0));
         if (u + 1 < n) {
           ++u;
           if (++step == steps) {
@@ -398,7 +428,7 @@ __global__ __launch_bounds__(64 * kN, 4) void moe_down_kernel(const MoeArgs p, c
         }
       };
       f32x4 acc[kT] = {};
-      int now = step, now_item = item, now_column = column;    // of the step that is computed
+      int now = step, now_item = item, now_column = sh_columns[item][c];    // of the step that is computed
       auto compute = [&](const Step& s, bool last) {
 #pragma unroll
         for (int t = 0; t < kT; ++t) {
@@ -412,7 +442,7 @@ __global__ __launch_bounds__(64 * kN, 4) void moe_down_kernel(const MoeArgs p, c
 #pragma unroll
           for (int t = 0; t < kT; ++t) {
             if (now_column >= 0)
-              *reinterpret_cast<f32x4*>(mine + (now_column & 63) * kPitch + 16 * t + 4 * q) += acc[t];
+              *reinterpret_cast<f32x4*>(mine + now_column * kPitch + 16 * t + 4 * q) += acc[t];
             acc[t] = 0.f;
           }
           dev::wave_lds_barrier();
@@ -431,25 +461,33 @@ __global__ __launch_bounds__(64 * kN, 4) void moe_down_kernel(const MoeArgs p, c
     }
   }
   __syncthreads();
-  // Thread (t, i): token t's features 4 i .. 4 i + 3.
-  const int t = tid / (4 * kT), i = tid % (4 * kT);
-  const bool here = t < p.M;
-  f32x4 y = 0.f;
-  if (here) {
+  // Thread (t, i): features 4 i .. 4 i + 3 of tokens t, t + kTogether, ...
+  constexpr int kTogether = 16 * kN / kT, kPasses = (kMaxLayerTokens + kTogether - 1) / kTogether;
+  const int t0 = tid / (4 * kT), i = tid % (4 * kT);
+  f32x4 y[kPasses];
+  auto here = [&](int s) { return t0 + s * kTogether < p.M; };
+  auto place = [&](int s) { return static_cast<int64_t>(t0 + s * kTogether) * p.N + 16 * tile + 4 * i; };
 #pragma unroll
-    for (int w = 0; w < kN; ++w) y += *reinterpret_cast<const f32x4*>(own + (w * p.M + t) * kPitch + 4 * i);
+  for (int s = 0; s < kPasses; ++s) {
+    y[s] = 0.f;
+    if (here(s)) {
+#pragma unroll
+      for (int w = 0; w < kN; ++w)
+        y[s] += *reinterpret_cast<const f32x4*>(own + (w * p.M + t0 + s * kTogether) * kPitch + 4 * i);
+    }
   }
-  const int64_t at = static_cast<int64_t>(t) * p.N + 16 * tile + 4 * i;
   if (splits > 1) {
     const int64_t stride = static_cast<int64_t>(p.M) * p.N;
-    if (here) {
-      // device scope: the last workgroup may be on another XCD with an L2 of its own
 #pragma unroll
-      for (int j = 0; j < 4; j += 2)
-        __hip_atomic_store(reinterpret_cast<uint64_t*>(parts + part * stride + at + j),
-                           static_cast<uint64_t>(__float_as_uint(y[j + 1])) << 32 | __float_as_uint(y[j]),
-                           __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    }
+    for (int s = 0; s < kPasses; ++s)
+      if (here(s)) {
+        // device scope: the last workgroup may be on another XCD with an L2 of its own
+#pragma unroll
+        for (int j = 0; j < 4; j += 2)
+          __hip_atomic_store(reinterpret_cast<uint64_t*>(parts + part * stride + place(s) + j),
+                             static_cast<uint64_t>(__float_as_uint(y[s][j + 1])) << 32 | __float_as_uint(y[s][j]),
+                             __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+      }
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");       // what this wave has stored is there
     __syncthreads();
     if (tid == 0)
@@ -458,37 +496,43 @@ __global__ __launch_bounds__(64 * kN, 4) void moe_down_kernel(const MoeArgs p, c
     __syncthreads();
     if (!sh_last) return;
     if (tid == 0) __hip_atomic_store(arrived + blockIdx.x, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    if (here) {
-      uint64_t v[kMaxSplits][2];                     // all loads under way together
+    uint64_t v[kPasses][kMaxSplits][2];              // all loads under way together
+#pragma unroll
+    for (int s = 0; s < kPasses; ++s)
 #pragma unroll
       for (int w = 0; w < kMaxSplits; ++w)
 #pragma unroll
         for (int j = 0; j < 2; ++j)
-          v[w][j] = w < splits ? __hip_atomic_load(reinterpret_cast<const uint64_t*>(parts + w * stride + at) + j,
-                                                   __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT)
-                               : 0;
-      y = 0.f;
+          v[s][w][j] = w < splits && here(s)
+                           ? __hip_atomic_load(reinterpret_cast<const uint64_t*>(parts + w * stride + place(s)) + j,
+                                               __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT)
+                           : 0;
+#pragma unroll
+    for (int s = 0; s < kPasses; ++s) {
+      y[s] = 0.f;
 #pragma unroll
       for (int w = 0; w < kMaxSplits; ++w)
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
-          y[2 * j] += __uint_as_float(static_cast<uint32_t>(v[w][j]));
-          y[2 * j + 1] += __uint_as_float(static_cast<uint32_t>(v[w][j] >> 32));
+          y[s][2 * j] += __uint_as_float(static_cast<uint32_t>(v[s][w][j]));
+          y[s][2 * j + 1] += __uint_as_float(static_cast<uint32_t>(v[s][w][j] >> 32));
         }
     }
   }
-  if (here) {
-    const dev::u32x2 v = {dev::pack_bf16(y[0], y[1]), dev::pack_bf16(y[2], y[3])};
-    *reinterpret_cast<dev::u32x2*>(p.out + t * p.ld_out + 16 * tile + 4 * i) = v;
-  }
+#pragma unroll
+  for (int s = 0; s < kPasses; ++s)
+    if (here(s)) {
+      const dev::u32x2 v = {dev::pack_bf16(y[s][0], y[s][1]), dev::pack_bf16(y[s][2], y[s][3])};
+      *reinterpret_cast<dev::u32x2*>(p.out + (t0 + s * kTogether) * p.ld_out + 16 * tile + 4 * i) = v;
+    }
 }
 
 size_t up16(size_t n) { return (n + 15) & ~size_t{15}; }
-size_t hidden_bytes(const MoeArgs& p) { return up16(static_cast<size_t>(p.M) * p.k * p.I * 2); }
+size_t hidden_bytes(const MoeArgs& p) { return up16(static_cast<size_t>(p.M) * p.k * hidden_pitch(p.I) * 2); }
 // An expert has as many items as 16 go into the pairs that name it, rounded up.
 int most_items(const MoePlan& c, const MoeArgs& p) { return std::min(p.M * p.k, c.slots + p.M * p.k / 16); }
 size_t table_bytes(const MoePlan& c, const MoeArgs& p) {
-  return up16(4 * (4 + static_cast<size_t>(most_items(c, p)) * (1 + 16)));
+  return up16(4 * (4 + static_cast<size_t>(most_items(c, p)) * (2 + 16)));
 }
 
 }  // namespace
@@ -499,11 +543,14 @@ MoePlan plan_moe_layer(const MoeArgs& p, int num_cus) {
   c.by_expert = c.slots == p.E;
   // The first launch: a wave a tile, or four where those would be few.
   c.parts = static_cast<int64_t>(p.I / 16) * c.slots <= 3 * num_cus ? 4 : 1;
-  // The second: a workgroup a CU, of a tile, or of two where the waves have steps enough, so that the
-  // activations are loaded for two.
+  // The second: two tiles a workgroup where their number is even, so that the activations are loaded for
+  // two, and a workgroup a CU, of which a wave has three steps at least.  us, two tiles and four
+  // workgroups along the experts / two / one, then one tile and two workgroups (128 experts of 768 + 64,
+  // N = 2048): one token 7.5 / 8.0 / 8.3 / 7.4, 4 tokens 10.1 / 13.0 / 18.7 / 11.7, 8 tokens
+  // 13.3 / 18.8 / 29.0 / 16.3.
   const int64_t steps = static_cast<int64_t>(c.slots) * ((p.I + p.k_tail + 127) / 128);
-  c.tiles = p.N % 32 == 0 && p.N / 32 * steps >= static_cast<int64_t>(2) * num_cus * 32 ? 2 : 1;
-  c.splits = static_cast<int>(std::min<int64_t>(num_cus / (p.N / 16 / c.tiles), steps / 32));
+  c.tiles = p.N % 32 == 0 ? 2 : 1;
+  c.splits = static_cast<int>(std::min<int64_t>(num_cus / (p.N / 16 / c.tiles), steps / 12));
   c.splits = std::max(1, std::min(c.splits, kMaxSplits));
   return c;
 }
@@ -519,7 +566,7 @@ hipError_t launch_moe_layer(const MoePlan& c, const MoeArgs& p, void* workspace,
   uint16_t* hidden = reinterpret_cast<uint16_t*>(at += kWorkspaceStateBytes);
   int32_t* const ints = reinterpret_cast<int32_t*>(at += hidden_bytes(p));
   const int most = most_items(c, p);
-  const Table table{ints, ints + 4 + 16 * most, ints + 4};
+  const Table table{ints, ints + 4 + 16 * most, ints + 4 + 17 * most, ints + 4};
   float* parts = reinterpret_cast<float*>(at += table_bytes(c, p));
   const int rows = p.M <= 16 ? p.M * pitch_of(1) : std::max(16 * pitch_of(1), 32 * pitch_of(2));
   auto up = [&](auto kernel, int kN, int kS) {
