@@ -3,21 +3,23 @@
 //
 //   l = x W^T                                     x [M, H], W [E, H] bf16, float32 sums
 //   s = softmax(l)  or  1 / (1 + exp(-l))
-//   the k experts with the largest s (+ bias, with the sigmoid), descending, the lower index
-//   first among equals, NaN behind everything
+//   the k experts with the largest s (or s + bias), descending, the lower index first among
+//   equals, NaN behind everything
 //   w = s (or s divided by the sum of the chosen) times `scale`
-// softmax keeps the order of l, so l itself is compared; the sigmoid does not in 32 bits (scores
-// near 1 meet) and a bias moves borders, so that key, like the sigmoid's weights, is computed
-// in 64 bits.
+// Both scores keep the order of l, so without a bias l itself is compared.  A bias moves borders: its
+// key, and the sigmoid's weights, are computed in 64 bits.
 //
-// The product is MFMA work with 16 experts as rows and 16 tokens as columns.  A wave owns a tile of
-// experts, or a part of H where there are fewer tiles than waves.  Many tokens: a workgroup takes
-// 32 of them and all experts, and its waves choose from the logits in LDS.  Few tokens: a
-// workgroup a tile of experts, so that W is read by as many CUs as there are tiles; the last one
-// to arrive of a block of 16 tokens reads the block's logits back and chooses.
+// The product is MFMA work with experts as rows and tokens as columns; the operands' rows are loaded
+// whole and brought into operand order through LDS (loaded in operand order, 16 rows at once, a load
+// takes four times as long: 8192 tokens of 128 experts 53 us).  Few tokens: a workgroup has 16 of them
+// and 16 experts, and its waves share H, so that W is read by as many CUs as possible.  The last
+// one of a block of tokens to arrive reads the block's logits back.  Many: a workgroup has 32 tokens and
+// all experts, in two stages of LDS.  Choosing, a
+// token has 16 lanes (a wave past 256 experts).
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
+#include <type_traits>
 
 #include "attn_device.hpp"
 #include "prq_internal.h"
@@ -30,247 +32,408 @@ using dev::u32x4v;
 
 constexpr int kWaves = 8, kThreads = 64 * kWaves;
 
-// Unsigned integers in the order of the numbers, 0 for none, NaN below everything.
+// Unsigned integers in the order of the numbers, above 0, NaN below everything; and back.
 __device__ __forceinline__ uint32_t ordered(float x) {
   const uint32_t u = __float_as_uint(x + 0.0f);           // -0 is 0
   return x != x ? 1u : u ^ (u >> 31 ? 0xFFFFFFFFu : 0x80000000u);
+}
+__device__ __forceinline__ float number(uint32_t u) {
+  return u == 1u ? __builtin_nanf("") : __uint_as_float(u ^ (u >> 31 ? 0x80000000u : 0xFFFFFFFFu));
 }
 __device__ __forceinline__ uint64_t ordered(double x) {
   const uint64_t u = __double_as_longlong(x + 0.0);
   return x != x ? 1u : u ^ (u >> 63 ? ~uint64_t{0} : uint64_t{1} << 63);
 }
 
-// A lane's value at other lanes of its wave by a row shift or broadcast, 0 from outside.
-template <int kCtrl, int kRows>
-__device__ __forceinline__ uint32_t shifted(uint32_t x) {
-  return static_cast<uint32_t>(__builtin_amdgcn_update_dpp(0, static_cast<int>(x), kCtrl, kRows, 0xF, false));
-}
-template <int kCtrl, int kRows>
-__device__ __forceinline__ uint64_t shifted(uint64_t x) {
-  return static_cast<uint64_t>(shifted<kCtrl, kRows>(static_cast<uint32_t>(x >> 32))) << 32 |
-         shifted<kCtrl, kRows>(static_cast<uint32_t>(x));
-}
-__device__ __forceinline__ uint32_t at_lane(uint32_t x, int lane) {
-  return static_cast<uint32_t>(__builtin_amdgcn_readlane(static_cast<int>(x), lane));
-}
-__device__ __forceinline__ uint64_t at_lane(uint64_t x, int lane) {
-  return static_cast<uint64_t>(at_lane(static_cast<uint32_t>(x >> 32), lane)) << 32 |
-         at_lane(static_cast<uint32_t>(x), lane);
-}
-template <typename T>
-__device__ __forceinline__ T wave_most(T x) {
-  x = max(x, shifted<0x111, 0xF>(x));
-  x = max(x, shifted<0x112, 0xF>(x));
-  x = max(x, shifted<0x114, 0xF>(x));
-  x = max(x, shifted<0x118, 0xF>(x));
-  x = max(x, shifted<0x142, 0xA>(x));
-  x = max(x, shifted<0x143, 0xC>(x));
-  return at_lane(x, 63);
-}
+__device__ __forceinline__ double sigmoid64(float l) { return 1.0 / (1.0 + exp(-static_cast<double>(l))); }
 
-__device__ __forceinline__ double wave_sum64(double x) {
-#pragma unroll
-  for (int d = 32; d > 0; d >>= 1) x += __shfl_xor(x, d, 64);
+// fold(move) for the exchanges after which every lane of a group of kLanes has met every other: each
+// neighbour, pair, quad and octet, then each 16 and 32.
+template <int kLanes, typename Fold>
+__device__ __forceinline__ void over_group(Fold fold) {
+  auto by = [](auto ctrl) {
+    return [](uint32_t x) {
+      return static_cast<uint32_t>(
+          __builtin_amdgcn_update_dpp(0, static_cast<int>(x), decltype(ctrl)::value, 0xF, 0xF, false));
+    };
+  };
+  fold(by(std::integral_constant<int, 0xB1>{}));         // quad_perm 1 0 3 2
+  fold(by(std::integral_constant<int, 0x4E>{}));         // quad_perm 2 3 0 1
+  fold(by(std::integral_constant<int, 0x141>{}));        // row_half_mirror
+  fold(by(std::integral_constant<int, 0x140>{}));        // row_mirror
+  if constexpr (kLanes == 64) {
+    fold([](uint32_t x) { return static_cast<uint32_t>(__shfl_xor(static_cast<int>(x), 16, 64)); });
+    fold([](uint32_t x) { return static_cast<uint32_t>(__shfl_xor(static_cast<int>(x), 32, 64)); });
+  }
+}
+template <int kLanes>
+__device__ __forceinline__ float group_sum(float x) {
+  over_group<kLanes>([&](auto move) { x += __uint_as_float(move(__float_as_uint(x))); });
+  return x;
+}
+template <int kLanes>
+__device__ __forceinline__ double group_sum(double x) {
+  over_group<kLanes>([&](auto move) {
+    const uint64_t u = __double_as_longlong(x);
+    x += __longlong_as_double(static_cast<uint64_t>(move(static_cast<uint32_t>(u >> 32))) << 32 | move(static_cast<uint32_t>(u)));
+  });
   return x;
 }
 
-__device__ __forceinline__ double sigmoid64(float l) { return 1.0 / (1.0 + exp(-static_cast<double>(l))); }
+template <int kLanes>
+__device__ __forceinline__ uint32_t group_max(uint32_t x) {
+  over_group<kLanes>([&](auto move) { x = max(x, move(x)); });
+  return x;
+}
 
-// One token by a wave.  Lane i holds experts kR i .. kR i + kR - 1, so that the first lane with
-// the largest key has the lowest index of equal ones.  logit(e): expert e's.
-template <int kR, bool kSigmoid, typename Logit>
-__device__ __forceinline__ void choose(const RouteArgs& p, int token, Logit logit) {
-  using Key = std::conditional_t<kSigmoid, uint64_t, uint32_t>;
-  const int lane = static_cast<int>(threadIdx.x) & 63;
+// A token by a group of kLanes lanes, of which lane i has experts kR i .. kR i + kR - 1 and keeps choices
+// i, kLanes + i, ...  live: the group has a token.  logit(e): expert e's.  A choice is the largest key
+// (of two words, with a bias) and the lowest index that has it: steps of 32 bits, since a
+// comparison of 64 takes four times as long.
+template <int kLanes, int kR, bool kBias, typename Logit>
+__device__ __forceinline__ void choose(const RouteArgs& p, int token, bool live, Logit logit) {
+  constexpr int kKept = (kMaxRouteTop + kLanes - 1) / kLanes;
+  const int mine = static_cast<int>(threadIdx.x) % kLanes;
   float l[kR];
-  Key key[kR];
+#pragma unroll
+  for (int i = 0; i < kR; ++i) l[i] = live && mine * kR + i < p.E ? logit(mine * kR + i) : -__builtin_inff();
+  uint32_t key[kR], low[kBias ? kR : 1];         // 0: no expert
 #pragma unroll
   for (int i = 0; i < kR; ++i) {
-    const int e = lane * kR + i;
-    l[i] = e < p.E ? logit(e) : -__builtin_inff();
-    key[i] = 0;
-    if (e < p.E) {
-      if constexpr (kSigmoid) key[i] = ordered(sigmoid64(l[i]) + static_cast<double>(p.bias ? p.bias[e] : 0.f));
-      else key[i] = ordered(l[i]);
-      if (p.logits) p.logits[token * p.ld_logits + e] = l[i];
+    const int e = mine * kR + i;
+    const bool in = live && e < p.E;
+    if (in && p.logits) p.logits[token * p.ld_logits + e] = l[i];
+    if constexpr (kBias) {
+      const uint64_t both = in ? ordered(sigmoid64(l[i]) + static_cast<double>(p.bias[e])) : 0;
+      key[i] = static_cast<uint32_t>(both >> 32);
+      low[i] = static_cast<uint32_t>(both);
+    } else {
+      key[i] = in ? ordered(l[i]) : 0;
     }
   }
-  int id = 0;                                   // lane j: the j-th expert
-  float mine = 0.f, first = 0.f;
+  int ids[kKept];
+  float chosen[kKept], first = 0.f;
   for (int j = 0; j < p.k; ++j) {
-    Key best = key[0];
-    int at = 0;
-    float best_l = l[0];
+    uint32_t most = key[0];
 #pragma unroll
-    for (int i = 1; i < kR; ++i)
-      if (key[i] > best) best = key[i], at = i, best_l = l[i];
-    const Key most = wave_most(best);
-    const int from = __builtin_ctzll(__ballot(best == most));
-    const int e = __builtin_amdgcn_readlane(lane * kR + at, from);
-    const float chosen = __uint_as_float(at_lane(__float_as_uint(best_l), from));
+    for (int i = 1; i < kR; ++i) most = max(most, key[i]);
+    most = group_max<kLanes>(most);
+    uint32_t most_low = 0;
+    if constexpr (kBias) {
+#pragma unroll
+      for (int i = 0; i < kR; ++i) most_low = max(most_low, key[i] == most ? low[i] : 0u);
+      most_low = group_max<kLanes>(most_low);
+    }
+    uint32_t above = 0;                          // ~ the lowest index
+#pragma unroll
+    for (int i = kR - 1; i >= 0; --i)
+      if (key[i] == most && (!kBias || low[i] == most_low)) above = ~static_cast<uint32_t>(mine * kR + i);
+    const int e = static_cast<int>(~group_max<kLanes>(above));
+    float of_e = 0.f;
+    if constexpr (kBias) {
+      uint32_t u = 0;
+#pragma unroll
+      for (int i = 0; i < kR; ++i)
+        if (e == mine * kR + i) u = ordered(l[i]);
+      of_e = number(group_max<kLanes>(u));
+    } else {
+      of_e = number(most);
+    }
 #pragma unroll
     for (int i = 0; i < kR; ++i)
-      if (lane == from && at == i) key[i] = 0;
-    if (lane == j) id = e, mine = chosen;
-    if (j == 0) first = chosen;
+      if (e == mine * kR + i) {
+        key[i] = 0;
+        if constexpr (kBias) low[i] = 0;
+      }
+    if (j == 0) first = of_e;
+#pragma unroll
+    for (int i = 0; i < kKept; ++i)
+      if (j == mine + i * kLanes) ids[i] = e, chosen[i] = of_e;
   }
-  float w = 0.f;
-  if constexpr (kSigmoid) {
-    double s = lane < p.k ? sigmoid64(mine) : 0.0;
-    if (p.renormalize) s /= wave_sum64(s);
-    w = static_cast<float>(s * p.scale);
+  auto kept = [&](int i) { return mine + i * kLanes < p.k; };
+  float w[kKept];
+  if (p.sigmoid) {
+    double s[kKept], total = 0.0;
+#pragma unroll
+    for (int i = 0; i < kKept; ++i) total += s[i] = kept(i) ? sigmoid64(chosen[i]) : 0.0;
+    total = p.renormalize ? group_sum<kLanes>(total) : 1.0;
+#pragma unroll
+    for (int i = 0; i < kKept; ++i) w[i] = static_cast<float>(s[i] / total * p.scale);
   } else {
-    const float s = lane < p.k ? expf(mine - first) : 0.f;
-    float total = s;
+    float total = 0.f;
+#pragma unroll
+    for (int i = 0; i < kKept; ++i) total += w[i] = kept(i) ? expf(chosen[i] - first) : 0.f;
     if (!p.renormalize) {
       total = 0.f;
 #pragma unroll
       for (int i = 0; i < kR; ++i)
-        if (lane * kR + i < p.E) total += expf(l[i] - first);
+        if (mine * kR + i < p.E) total += expf(l[i] - first);
     }
-    w = s / dev::wave_sum(total) * p.scale;
+    total = group_sum<kLanes>(total);
+#pragma unroll
+    for (int i = 0; i < kKept; ++i) w[i] = w[i] / total * p.scale;
   }
-  if (lane < p.k) {
-    p.ids[static_cast<int64_t>(token) * p.k + lane] = id;
-    p.weights[static_cast<int64_t>(token) * p.k + lane] = w;
+#pragma unroll
+  for (int i = 0; i < kKept; ++i)
+    if (live && kept(i)) {
+      const int64_t at = static_cast<int64_t>(token) * p.k + mine + i * kLanes;
+      p.ids[at] = ids[i];
+      p.weights[at] = w[i];
+    }
+}
+
+// Tokens token0 .. token0 + rows - 1 by the workgroup: 16 lanes each, or 64 where there are no more tokens
+// than waves or the experts are many.  logit(row, e).
+template <bool kBias, typename Logit>
+__device__ __forceinline__ void choose_rows(const RouteArgs& p, int token0, int rows, Logit logit) {
+  const int wave = static_cast<int>(threadIdx.x) >> 6;
+  if (p.E > 256 || rows <= kWaves) {
+    for (int r = wave; r < rows; r += kWaves) {
+      auto of = [&](int e) { return logit(r, e); };
+      if (p.E <= 128) choose<64, 2, kBias>(p, token0 + r, true, of);
+      else if (p.E <= 256) choose<64, 4, kBias>(p, token0 + r, true, of);
+      else choose<64, kMaxRouteExperts / 64, kBias>(p, token0 + r, true, of);
+    }
+  } else {
+    for (int r0 = 4 * wave; r0 < rows; r0 += 4 * kWaves) {
+      const int r = r0 + (static_cast<int>(threadIdx.x) >> 4 & 3);
+      auto of = [&](int e) { return logit(r, e); };
+      if (p.E <= 64) choose<16, 4, kBias>(p, token0 + r, r < rows, of);
+      else if (p.E <= 128) choose<16, 8, kBias>(p, token0 + r, r < rows, of);
+      else choose<16, 16, kBias>(p, token0 + r, r < rows, of);
+    }
   }
 }
 
-template <typename Logit>
-__device__ __forceinline__ void choose_any(const RouteArgs& p, int token, Logit logit) {
-  auto go = [&](auto sigmoid) {
-    constexpr bool kS = decltype(sigmoid)::value;
-    if (p.E <= 64) choose<1, kS>(p, token, logit);
-    else if (p.E <= 128) choose<2, kS>(p, token, logit);
-    else if (p.E <= 256) choose<4, kS>(p, token, logit);
-    else if (p.E <= 512) choose<8, kS>(p, token, logit);
-    else choose<16, kS>(p, token, logit);
-  };
-  if (p.sigmoid) go(std::true_type{});
-  else go(std::false_type{});
-}
-
-// Floats between two tokens' logits in LDS: 4 past a multiple of 32, so that the 16 tokens of a
-// tile's float4 stores lie in different banks.
-__host__ __device__ inline int pitch_of(int experts) { return ((experts + 31) & ~31) + 4; }
-
-// kG blocks of 16 tokens and kTw tiles of 16 experts a workgroup at a time, kWaves / kTw parts of H.
-template <int kG, int kTw, bool kSplit>
-__global__ __launch_bounds__(kThreads) void moe_route_kernel(const RouteArgs p, float* parts, uint32_t* arrived) {
-  constexpr int kKs = kWaves / kTw, kRows = 16 * kG;
-  extern __shared__ __align__(16) float sh[];   // [kKs][kRows][pitch]
+// A workgroup's logits (value(row, e) of its experts e0 .. e0 + experts - 1) to where the last one to
+// arrive of a block finds them, and whether this is it: device-scope accesses, since that may be
+// another XCD with an L2 of its own.
+template <typename Value>
+__device__ __forceinline__ bool arrive(const RouteArgs& p, float* parts, uint32_t* arrived, int row0, int rows, int e0,
+                                       int experts, int groups, Value value) {
   __shared__ int sh_last;
+  const int tid = static_cast<int>(threadIdx.x);
+  for (int i = tid; i < rows * experts; i += kThreads) {
+    const int r = i / experts, e = i % experts;
+    if (e0 + e < p.E)
+      __hip_atomic_store(parts + static_cast<int64_t>(row0 + r) * p.E + e0 + e, value(r, e), __ATOMIC_RELAXED,
+                         __HIP_MEMORY_SCOPE_AGENT);
+  }
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");         // what this wave has stored is there
+  __syncthreads();
+  if (tid == 0)
+    sh_last = __hip_atomic_fetch_add(arrived, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) ==
+              static_cast<uint32_t>(groups - 1);
+  __syncthreads();
+  if (!sh_last) return false;
+  if (tid == 0) __hip_atomic_store(arrived, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  return true;
+}
+__device__ __forceinline__ float arrived_logit(const RouteArgs& p, const float* parts, int row, int e) {
+  return __hip_atomic_load(parts + static_cast<int64_t>(row) * p.E + e, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+
+// Rows in LDS: 16 bytes past a multiple of 128, at which 16 rows' octets at one place meet different
+// banks.
+__host__ __device__ constexpr int pitch_of(int elements) { return 2 * elements + 16; }
+// The two stages, or the parts' sums, of 32 tokens and 32 kE experts.
+__host__ __device__ constexpr int stages_bytes(int kE) {
+  const int rows = 2 * (32 + 32 * kE) * pitch_of(64 * kWaves / kE), sums = kWaves / kE * 32 * (32 * kE + 4) * 4;
+  return rows > sums ? rows : sums;
+}
+
+// 16 tokens and 16 experts; the waves share H by steps of 128, each with LDS of its own.
+template <bool kBias>
+__global__ __launch_bounds__(kThreads) void route_few_kernel(const RouteArgs p, int first, float* parts, uint32_t* arrived) {
+  constexpr int kPitch = pitch_of(128);
+  __shared__ __align__(16) unsigned char rows[kWaves][32 * kPitch];
+  __shared__ f32x4 sums[kWaves][64];
   const int tid = static_cast<int>(threadIdx.x), lane = tid & 63, wave = tid >> 6;
   const int c = lane & 15, q = lane >> 4;
-  const int token0 = static_cast<int>(blockIdx.x) * kRows;
-  const int tiles = (p.E + 15) >> 4;
-  const int first = kSplit ? static_cast<int>(blockIdx.y) : 0, last = kSplit ? first + 1 : tiles;
-  const int pitch = pitch_of(kSplit ? 16 : p.E);
-  const int part = wave / kTw;
-  const int steps = (p.H + 127) >> 7;           // of 128: lane group q has elements 32 q .. 32 q + 31 of each
+  const int token0 = first + static_cast<int>(blockIdx.x) * 16, e0 = static_cast<int>(blockIdx.y) * 16;
+  const int steps = (p.H + 127) >> 7, count = min(p.M - token0, 16);
 
-  const uint16_t* x[kG];
+  f32x4 acc = 0.f;
+  u32x4v x[4], w[4];                             // rows 4 j + q, octet c
+  auto ask = [&](int s) {
+    const int k = 128 * s + 8 * c;
 #pragma unroll
-  for (int g = 0; g < kG; ++g)                  // columns past M: the last token's again, not stored
-    x[g] = p.x + static_cast<int64_t>(min(token0 + 16 * g + c, p.M - 1)) * p.ld_x;
-  for (int t = first + wave % kTw; t < last; t += kTw) {
-    const uint16_t* w = p.w + static_cast<int64_t>(min(16 * t + c, p.E - 1)) * p.ld_w;
-    f32x4 acc[kG] = {};
-#pragma unroll 2
-    for (int s = part; s < steps; s += kKs) {
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const int at = 128 * s + 32 * q + 8 * j;
-        u32x4v a = 0u;
-        if (at < p.H) a = *reinterpret_cast<const u32x4v*>(w + at);
-#pragma unroll
-        for (int g = 0; g < kG; ++g) {
-          u32x4v b = 0u;
-          if (at < p.H) b = *reinterpret_cast<const u32x4v*>(x[g] + at);
-          acc[g] = dev::mfma_bf16(a, b, acc[g]);
-        }
+    for (int j = 0; j < 4; ++j) {
+      x[j] = w[j] = 0u;
+      const int r = 4 * j + q;
+      if (k < p.H) {
+        if (r < count) x[j] = *reinterpret_cast<const u32x4v*>(p.x + (token0 + r) * p.ld_x + k);
+        if (e0 + r < p.E) w[j] = *reinterpret_cast<const u32x4v*>(p.w + (e0 + r) * p.ld_w + k);
       }
     }
+  };
+  ask(wave);
+  unsigned char* const mine = rows[wave];
+  for (int s = wave; s < steps; s += kWaves) {
 #pragma unroll
-    for (int g = 0; g < kG; ++g)
-      *reinterpret_cast<f32x4*>(sh + (part * kRows + 16 * g + c) * pitch + 16 * (t - first) + 4 * q) = acc[g];
+    for (int j = 0; j < 4; ++j) {
+      *reinterpret_cast<u32x4v*>(mine + (4 * j + q) * kPitch + 16 * c) = x[j];
+      *reinterpret_cast<u32x4v*>(mine + (16 + 4 * j + q) * kPitch + 16 * c) = w[j];
+    }
+    dev::wave_lds_barrier();
+    if (s + kWaves < steps) ask(s + kWaves);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const u32x4v b = *reinterpret_cast<const u32x4v*>(mine + c * kPitch + (4 * j + q) * 16);
+      const u32x4v a = *reinterpret_cast<const u32x4v*>(mine + (16 + c) * kPitch + (4 * j + q) * 16);
+      acc = dev::mfma_bf16(a, b, acc);
+    }
+    dev::wave_lds_barrier();
+  }
+  sums[wave][lane] = acc;
+  __syncthreads();
+  auto sum = [&](int r, int e) {                 // token r's, of expert e0 + e
+    float l = 0.f;
+#pragma unroll
+    for (int v = 0; v < kWaves; ++v) l += sums[v][(e >> 2) * 16 + r][e & 3];
+    return l;
+  };
+  if (gridDim.y == 1) return choose_rows<kBias>(p, token0, count, sum);
+  if (arrive(p, parts, arrived + blockIdx.x, token0 - first, count, e0, 16, static_cast<int>(gridDim.y), sum))
+    choose_rows<kBias>(p, token0, count, [&](int r, int e) { return arrived_logit(p, parts, token0 - first + r, e); });
+}
+
+// 32 tokens and all experts, 32 kE at a time; wave (g, part) has 32 of those, all tokens and 64 elements
+// of every chunk of H.  Chunks come by way of registers, kAhead of them under way, into two stages of
+// LDS.
+__host__ __device__ inline int logits_pitch(int E, int kE) { return (E + 32 * kE - 1) / (32 * kE) * 32 * kE + 4; }
+
+template <int kE, bool kBias>
+__global__ __launch_bounds__(kThreads, 2) void route_many_kernel(const RouteArgs p) {
+  constexpr int kParts = kWaves / kE, kChunk = 64 * kParts, kPitch = pitch_of(kChunk);
+  constexpr int kRows = 32 + 32 * kE, kOctets = kChunk / 8, kEach = kThreads / kOctets;      // rows a pass
+  constexpr int kLoads = kRows / kEach, kAhead = kE == 4 ? 4 : kE == 2 ? 3 : 2;
+  constexpr int kSums = 32 * kE + 4;             // floats between two tokens' sums
+  extern __shared__ __align__(16) unsigned char smem[];      // [2][kRows][kPitch] or [kParts][32][kSums], and the logits
+  const int tid = static_cast<int>(threadIdx.x), lane = tid & 63, wave = tid >> 6;
+  const int c = lane & 15, q = lane >> 4;
+  const int token0 = static_cast<int>(blockIdx.x) * 32;
+  const int count = min(p.M - token0, 32);
+  float* const sums = reinterpret_cast<float*>(smem);
+  float* const logits = reinterpret_cast<float*>(smem + stages_bytes(kE));
+  const int pitch = logits_pitch(p.E, kE);
+
+  const int octet = tid % kOctets, row = tid / kOctets;
+  const int part = wave / kE, g = wave % kE;
+  for (int e0 = 0; e0 < p.E; e0 += 32 * kE) {
+    const uint16_t* from[kLoads];                // rows past the end: the last one's again, not stored
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) {
+      const int r = row + i * kEach;
+      from[i] = (r < 32 ? p.x + min(token0 + r, p.M - 1) * p.ld_x : p.w + min(e0 + r - 32, p.E - 1) * p.ld_w) + 8 * octet;
+    }
+    u32x4v ring[kAhead][kLoads];
+    // (loads without conditions, so that every wait counts exactly the loads behind it)
+    auto ask = [&](int chunk, u32x4v (&to)[kLoads]) {      // chunk: its first element
+      const int k = min(chunk, p.H - 8 - 8 * octet);
+#pragma unroll
+      for (int i = 0; i < kLoads; ++i) to[i] = *reinterpret_cast<const u32x4v*>(from[i] + k);
+    };
+    auto put = [&](const u32x4v (&v)[kLoads], int chunk, int stage) {
+      unsigned char* to = smem + stage * kRows * kPitch + row * kPitch + 16 * octet;
+      const bool in = chunk + 8 * octet < p.H;
+#pragma unroll
+      for (int i = 0; i < kLoads; ++i) *reinterpret_cast<u32x4v*>(to + i * kEach * kPitch) = in ? v[i] : u32x4v{};
+    };
+    f32x4 acc[2][2] = {};
+    auto compute = [&](int stage) {
+      const unsigned char* at = smem + stage * kRows * kPitch + c * kPitch + (part * 8 + q) * 16;
+#pragma unroll
+      for (int s = 0; s < 2; ++s) {
+        u32x4v a[2], b[2];
+#pragma unroll
+        for (int m = 0; m < 2; ++m) {
+          b[m] = *reinterpret_cast<const u32x4v*>(at + 16 * m * kPitch + 64 * s);
+          a[m] = *reinterpret_cast<const u32x4v*>(at + (32 + 32 * g + 16 * m) * kPitch + 64 * s);
+        }
+#pragma unroll
+        for (int m = 0; m < 2; ++m)
+#pragma unroll
+          for (int t = 0; t < 2; ++t) acc[m][t] = dev::mfma_bf16(a[m], b[t], acc[m][t]);
+      }
+    };
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) ask(i * kChunk, ring[i]);
+    __syncthreads();                             // the sums before have been read
+    constexpr int kRound = kAhead % 2 ? 2 * kAhead : kAhead;
+    for (int i0 = 0; i0 < p.H; i0 += kRound * kChunk) {      // (chunks past the end are zeros)
+#pragma unroll
+      for (int r = 0; r < kRound; ++r) {
+        const int k = i0 + r * kChunk;
+        put(ring[r % kAhead], k, r % 2);
+        ask(k + kAhead * kChunk, ring[r % kAhead]);
+        __syncthreads();                         // of a stage: written before this one, read before the next but one
+        compute(r % 2);
+      }
+    }
+    __syncthreads();
+#pragma unroll
+    for (int m = 0; m < 2; ++m)
+#pragma unroll
+      for (int t = 0; t < 2; ++t)
+        *reinterpret_cast<f32x4*>(sums + (part * 32 + 16 * t + c) * kSums + 32 * g + 16 * m + 4 * q) = acc[m][t];
+    __syncthreads();
+    for (int i = tid; i < 32 * 8 * kE; i += kThreads) {
+      const int r = i / (8 * kE), e = i % (8 * kE) * 4;
+      f32x4 l = *reinterpret_cast<const f32x4*>(sums + r * kSums + e);
+#pragma unroll
+      for (int v = 1; v < kParts; ++v) l += *reinterpret_cast<const f32x4*>(sums + (v * 32 + r) * kSums + e);
+      *reinterpret_cast<f32x4*>(logits + r * pitch + e0 + e) = l;
+    }
   }
   __syncthreads();
-  if constexpr (!kSplit) {
-    for (int i = wave; i < kRows && token0 + i < p.M; i += kWaves)
-      choose_any(p, token0 + i, [&](int e) {
-        float l = sh[i * pitch + e];
-#pragma unroll
-        for (int ks = 1; ks < kKs; ++ks) l += sh[(ks * kRows + i) * pitch + e];
-        return l;
-      });
-  } else {
-    // The tile's logits for whoever arrives last: device-scope accesses, since that may be another
-    // XCD with an L2 of its own.
-    if (tid < 256) {
-      const int i = tid >> 4, e = tid & 15;
-      float l = 0.f;
-#pragma unroll
-      for (int ks = 0; ks < kKs; ++ks) l += sh[(ks * kRows + i) * pitch + e];
-      if (token0 + i < p.M && 16 * first + e < p.E)
-        __hip_atomic_store(parts + static_cast<int64_t>(token0 + i) * p.E + 16 * first + e, l, __ATOMIC_RELAXED,
-                           __HIP_MEMORY_SCOPE_AGENT);
-    }
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");       // what this wave has stored is there
-    __syncthreads();
-    if (tid == 0)
-      sh_last = __hip_atomic_fetch_add(arrived + blockIdx.x, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) ==
-                static_cast<uint32_t>(tiles - 1);
-    __syncthreads();
-    if (!sh_last) return;
-    if (tid == 0) __hip_atomic_store(arrived + blockIdx.x, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    for (int i = wave; i < kRows && token0 + i < p.M; i += kWaves)
-      choose_any(p, token0 + i, [&](int e) {
-        return __hip_atomic_load(parts + static_cast<int64_t>(token0 + i) * p.E + e, __ATOMIC_RELAXED,
-                                 __HIP_MEMORY_SCOPE_AGENT);
-      });
-  }
+  choose_rows<kBias>(p, token0, count, [&](int r, int e) { return logits[r * pitch + e]; });
 }
+
+// Experts past which a block's logits do not fit beside the stages, and tokens in a launch of the
+// other kernel: what the state's counters and a modest workspace hold.
+constexpr int kMaxManyExperts = 512;
+constexpr int kMaxFewTokens = 8192;
+static_assert(kMaxFewTokens / 16 <= static_cast<int>(kWorkspaceStateBytes / 4), "a counter a block");
 
 }  // namespace
 
 RoutePlan plan_moe_route(int M, int E, int H, int num_cus) {
   RoutePlan c;
-  const int tiles = (E + 15) / 16;
-  c.split = tiles > 1 && M <= 16 * num_cus / 4;
-  c.rows = c.split ? 16 : 32;
-  c.blocks = (static_cast<int64_t>(M) + c.rows - 1) / c.rows;
+  const int64_t few = (static_cast<int64_t>(M) + 15) / 16 * ((E + 15) / 16);
+  if (E <= kMaxManyExperts && few > 2 * num_cus) c.groups = E > 64 ? 4 : E > 32 ? 2 : 1;
   return c;
 }
 
 size_t route_workspace_bytes(const RoutePlan& c, int M, int E) {
-  return c.split ? kWorkspaceStateBytes + static_cast<size_t>(M) * E * 4 : 0;
+  return c.groups || E <= 16 ? 0 : kWorkspaceStateBytes + static_cast<size_t>(std::min(M, kMaxFewTokens)) * E * 4;
 }
 
 hipError_t launch_moe_route(const RoutePlan& c, const RouteArgs& p, void* workspace, hipStream_t stream) {
-  const int tiles = (p.E + 15) / 16, grid = static_cast<int>(c.blocks);
-  if (c.split) {
-    static_assert(kWaves * 16 * (32 + 4) * 4 <= 64 * 1024, "LDS");
-    float* parts = reinterpret_cast<float*>(static_cast<char*>(workspace) + kWorkspaceStateBytes);
-    moe_route_kernel<1, 1, true><<<dim3(grid, tiles), kThreads, kWaves * 16 * pitch_of(16) * 4, stream>>>(
-        p, parts, static_cast<uint32_t*>(workspace));
-    return hipGetLastError();
-  }
-  auto go = [&](auto tw) {
-    constexpr int kTw = decltype(tw)::value;
-    const void* fn = reinterpret_cast<const void*>(&moe_route_kernel<2, kTw, false>);
-    const int lds = kWaves / kTw * 32 * pitch_of(p.E) * 4;
-    if (lds > 64 * 1024) {
-      const hipError_t e = hipFuncSetAttribute(fn, hipFuncAttributeMaxDynamicSharedMemorySize, lds);
-      if (e != hipSuccess) return e;
-    }
-    moe_route_kernel<2, kTw, false><<<grid, kThreads, lds, stream>>>(p, nullptr, nullptr);
+  auto many = [&](auto kernel, int kE) {
+    const int lds = stages_bytes(kE) + 32 * logits_pitch(p.E, kE) * 4;
+    const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel),
+                                             hipFuncAttributeMaxDynamicSharedMemorySize, lds);
+    if (e != hipSuccess) return e;
+    kernel<<<(p.M + 31) / 32, kThreads, lds, stream>>>(p);
     return hipGetLastError();
   };
-  if (tiles > 4) return go(std::integral_constant<int, 8>{});
-  if (tiles > 2) return go(std::integral_constant<int, 4>{});
-  if (tiles > 1) return go(std::integral_constant<int, 2>{});
-  return go(std::integral_constant<int, 1>{});
+  auto go = [&](auto bias) {
+    constexpr bool kBias = decltype(bias)::value;
+    if (c.groups == 4) return many(&route_many_kernel<4, kBias>, 4);
+    if (c.groups == 2) return many(&route_many_kernel<2, kBias>, 2);
+    if (c.groups == 1) return many(&route_many_kernel<1, kBias>, 1);
+    const int tiles = (p.E + 15) / 16, most = tiles > 1 ? kMaxFewTokens : p.M;
+    float* const parts = tiles > 1 ? reinterpret_cast<float*>(static_cast<char*>(workspace) + kWorkspaceStateBytes) : nullptr;
+    for (int first = 0; first < p.M; first += most) {
+      route_few_kernel<kBias><<<dim3((std::min(p.M - first, most) + 15) / 16, tiles), kThreads, 0, stream>>>(
+          p, first, parts, static_cast<uint32_t*>(workspace));
+      const hipError_t e = hipGetLastError();
+      if (e != hipSuccess) return e;
+    }
+    return hipSuccess;
+  };
+  return p.bias ? go(std::true_type{}) : go(std::false_type{});
 }
 
 }  // namespace prq

@@ -268,13 +268,11 @@ struct BlockNormArgs {
 };
 hipError_t launch_block_norm(const BlockNormArgs& p, bool y_bf16, bool r_bf16, int num_cus, hipStream_t stream);
 
-// moe_route.hip.  Tokens in blocks of `rows`; with `split` the experts' tiles of a block are in
-// workgroups of their own and the last of them to arrive chooses (workspace: the state head, then
-// the logits).
+// moe_route.hip.  Groups of 32 experts at a time of a workgroup with 32 tokens, or 0: a workgroup 16
+// tokens and 16 experts, of which the last one of a block of tokens chooses (workspace: the state head,
+// then the logits).
 struct RoutePlan {
-  bool split = false;
-  int rows = 16;
-  int64_t blocks = 0;
+  int groups = 0;
 };
 struct RouteArgs {
   const uint16_t *x, *w;
