@@ -90,7 +90,7 @@ int prq_block_norm(const void* y, int64_t ld_y, int32_t y_type, const void* resi
                              residual_out, ld_ro, static_cast<uint16_t*>(h_out), ld_h, M, H, gate_rows,
                              weight_type == PRQ_BF16, gate_type == PRQ_BF16, weight_offset, eps, residual_scale,
                              block_scale};
-  return launch_status(prq::launch_block_norm(p, y_type == PRQ_BF16, r_type == PRQ_BF16, cus, stream));
+  return launch_status(prq::launch_block_norm(p, y_type == PRQ_BF16, r_type == PRQ_BF16, stream));
 }
 
 size_t prq_moe_route_workspace_bytes(int32_t M, int32_t E, int32_t H) {

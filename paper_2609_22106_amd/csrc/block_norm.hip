@@ -11,7 +11,8 @@
 //
 // Bytes: y, r, r' and h once each; HBM bounds many rows, the launch and two dependent
 // reductions a few.  A row's elements stay in the registers of its lanes between the
-// reductions, so that nothing is read twice.
+// reductions, so that nothing is read twice.  8192 rows of 2560, float32: 48.6 us, 293 MB at
+// 6.0 TB/s (a large copy here 5.4, a sum of two tensors 5.9); one row of 2048: 2.3 us.
 #include <hip/hip_runtime.h>
 
 #include <type_traits>
@@ -26,20 +27,45 @@ using dev::f32x4;
 
 constexpr int kThreads = 256;
 
-__device__ __forceinline__ f32x4 load4(const float* p, int64_t at) { return *reinterpret_cast<const f32x4*>(p + at); }
-__device__ __forceinline__ f32x4 load4(const uint16_t* p, int64_t at) {
-  const dev::u32x2 w = *reinterpret_cast<const dev::u32x2*>(p + at);
+// Four elements as they lie in memory; their values are made where they are used, so that no load is
+// waited for among the others.
+template <typename T>
+using Raw = std::conditional_t<std::is_same_v<T, float>, f32x4, dev::u32x2>;
+template <bool kOnce, typename T>
+__device__ __forceinline__ Raw<T> load4(const T* p, int64_t at) {
+  const Raw<T>* from = reinterpret_cast<const Raw<T>*>(p + at);
+  if constexpr (kOnce) return __builtin_nontemporal_load(from);
+  else return *from;
+}
+__device__ __forceinline__ f32x4 values(f32x4 x) { return x; }
+__device__ __forceinline__ f32x4 values(dev::u32x2 w) {
   return {dev::bf16_lo(w.x), dev::bf16_hi(w.x), dev::bf16_lo(w.y), dev::bf16_hi(w.y)};
 }
-__device__ __forceinline__ void store4(float* p, int64_t at, f32x4 x) { *reinterpret_cast<f32x4*>(p + at) = x; }
-__device__ __forceinline__ void store4(uint16_t* p, int64_t at, f32x4 x) {
-  const dev::u32x2 w = {dev::pack_bf16(x[0], x[1]), dev::pack_bf16(x[2], x[3])};
-  *reinterpret_cast<dev::u32x2*>(p + at) = w;
+template <bool kOnce, typename T>
+__device__ __forceinline__ void store4(T* p, int64_t at, f32x4 x) {
+  Raw<T> v;
+  if constexpr (std::is_same_v<T, float>) v = x;
+  else v = Raw<T>{dev::pack_bf16(x[0], x[1]), dev::pack_bf16(x[2], x[3])};
+  Raw<T>* to = reinterpret_cast<Raw<T>*>(p + at);
+  if constexpr (kOnce) __builtin_nontemporal_store(v, to);
+  else *to = v;
 }
-// A weight or gate, float32 or bf16.
-__device__ __forceinline__ f32x4 load4(const void* p, bool bf16, int64_t at) {
-  return bf16 ? load4(static_cast<const uint16_t*>(p), at) : load4(static_cast<const float*>(p), at);
-}
+// The same of a weight or a gate, whose type the call says.
+struct Weight {
+  dev::u32x4v raw;
+  __device__ __forceinline__ void load(const void* p, bool bf16, int64_t at) {
+    if (bf16) {
+      const dev::u32x2 w = *reinterpret_cast<const dev::u32x2*>(static_cast<const uint16_t*>(p) + at);
+      raw[0] = w.x;
+      raw[1] = w.y;
+    } else {
+      raw = *reinterpret_cast<const dev::u32x4v*>(static_cast<const float*>(p) + at);
+    }
+  }
+  __device__ __forceinline__ f32x4 get(bool bf16) const {
+    return bf16 ? values(dev::u32x2{raw[0], raw[1]}) : __builtin_bit_cast(f32x4, raw);
+  }
+};
 
 // The sum over a row's lanes, in every one of them.  sh: 4 floats that nothing else uses
 // between two calls.
@@ -57,10 +83,12 @@ __device__ __forceinline__ float row_sum(float x, float* sh) {
 
 __device__ __forceinline__ float dot4(f32x4 x) { return (x[0] * x[0] + x[1] * x[1]) + (x[2] * x[2] + x[3] * x[3]); }
 
-// kLanes lanes a row (a wave or the workgroup), kU quadruples a lane.
-template <typename Y, typename R, int kLanes, int kU>
+// kLanes lanes a row (a wave or the workgroup), kU quadruples a lane.  kOnce: what is more than the
+// caches keep is loaded and stored past them.
+template <typename Y, typename R, int kLanes, int kU, bool kOnce>
 __global__ __launch_bounds__(kThreads) void block_norm_kernel(const BlockNormArgs p) {
   constexpr int kRows = kThreads / kLanes;
+  constexpr bool kEarly = kU <= 4;              // weights and gate in registers from the start
   __shared__ float sh[2][4];
   const int lane = static_cast<int>(threadIdx.x) % kLanes;
   const int64_t row = static_cast<int64_t>(blockIdx.x) * kRows + static_cast<int>(threadIdx.x) / kLanes;
@@ -68,79 +96,103 @@ __global__ __launch_bounds__(kThreads) void block_norm_kernel(const BlockNormArg
   const Y* y = static_cast<const Y*>(p.y);
   const R* r = static_cast<const R*>(p.residual);
   R* r_out = static_cast<R*>(p.residual_out);
+  // A lane's i-th quadruple; past the end the row's last one, whose values are made zeros.
+  auto place = [&](int i) { return min(4 * (lane + i * kLanes), p.H - 4); };
+  auto in = [&](int i) { return 4 * (lane + i * kLanes) < p.H; };
 
-  f32x4 u[kU], x[kU];
+  Raw<Y> y_raw[kU];
+  Raw<R> r_raw[kU];
+  if (y) {
 #pragma unroll
-  for (int i = 0; i < kU; ++i) {
-    const int at = 4 * (lane + i * kLanes);
-    u[i] = x[i] = 0.f;
-    if (at < p.H) {
-      if (y) u[i] = load4(y, row * p.ld_y + at);
-      if (r) x[i] = load4(r, row * p.ld_r + at);
-    }
+    for (int i = 0; i < kU; ++i) y_raw[i] = load4<kOnce>(y, row * p.ld_y + place(i));
+  }
+  if (r) {
+#pragma unroll
+    for (int i = 0; i < kU; ++i) r_raw[i] = load4<kOnce>(r, row * p.ld_r + place(i));
   }
   int64_t gate_row = p.gate ? 0 : -1;
   if (p.gate) gate_row = p.gate_index ? p.gate_index[row] : p.gate_rows > 1 ? row : 0;
   const bool gated = gate_row >= 0 && gate_row < p.gate_rows;     // a row that names none has none
+  Weight post[kU], gate[kU], pre[kU];
+  auto weights = [&](Weight (&w)[kU], const void* from, bool bf16, int64_t at) {
+#pragma unroll
+    for (int i = 0; i < kU; ++i) w[i].load(from, bf16, at + place(i));
+  };
+  if constexpr (kEarly) {
+    if (p.post) weights(post, p.post, p.w_bf16, 0);
+    if (p.pre) weights(pre, p.pre, p.w_bf16, 0);
+    if (gated) weights(gate, p.gate, p.gate_bf16, gate_row * p.ld_gate);
+  }
+  f32x4 u[kU], x[kU];
+#pragma unroll
+  for (int i = 0; i < kU; ++i) u[i] = y && in(i) ? values(y_raw[i]) : f32x4{};
+#pragma unroll
+  for (int i = 0; i < kU; ++i) x[i] = r && in(i) ? values(r_raw[i]) : f32x4{};
 
   if (p.post) {
+    if constexpr (!kEarly) weights(post, p.post, p.w_bf16, 0);
     float s = 0.f;
 #pragma unroll
     for (int i = 0; i < kU; ++i) s += dot4(u[i]);
     const float inv = 1.0f / sqrtf(row_sum<kLanes>(s, sh[0]) / static_cast<float>(p.H) + p.eps);
 #pragma unroll
-    for (int i = 0; i < kU; ++i) {
-      const int at = 4 * (lane + i * kLanes);
-      if (at < p.H) u[i] *= inv * (load4(p.post, p.w_bf16, at) + p.offset);
-    }
+    for (int i = 0; i < kU; ++i) u[i] *= inv * (post[i].get(p.w_bf16) + p.offset);
   }
+  if (gated) {
+    if constexpr (!kEarly) weights(gate, p.gate, p.gate_bf16, gate_row * p.ld_gate);
+#pragma unroll
+    for (int i = 0; i < kU; ++i) u[i] *= gate[i].get(p.gate_bf16);
+  }
+  if constexpr (!kEarly)
+    if (p.pre) weights(pre, p.pre, p.w_bf16, 0);
   float s = 0.f;
 #pragma unroll
   for (int i = 0; i < kU; ++i) {
-    const int at = 4 * (lane + i * kLanes);
-    if (at < p.H) {
-      if (gated) u[i] *= load4(p.gate, p.gate_bf16, gate_row * p.ld_gate + at);
-      x[i] = p.a * x[i] + p.b * u[i];
-      if (r_out) store4(r_out, row * p.ld_ro + at, x[i]);
-    }
-    s += dot4(x[i]);
+    x[i] = p.a * x[i] + p.b * u[i];
+    if (r_out && in(i)) store4<kOnce>(r_out, row * p.ld_ro + place(i), x[i]);
+    if (in(i)) s += dot4(x[i]);
   }
   if (!p.pre) return;
   const float inv = 1.0f / sqrtf(row_sum<kLanes>(s, sh[1]) / static_cast<float>(p.H) + p.eps);
 #pragma unroll
-  for (int i = 0; i < kU; ++i) {
-    const int at = 4 * (lane + i * kLanes);
-    if (at < p.H) store4(p.h, row * p.ld_h + at, x[i] * inv * (load4(p.pre, p.w_bf16, at) + p.offset));
-  }
+  for (int i = 0; i < kU; ++i)
+    if (in(i)) store4<kOnce>(p.h, row * p.ld_h + place(i), x[i] * inv * (pre[i].get(p.w_bf16) + p.offset));
 }
 
-template <typename Y, typename R, int kLanes>
+template <typename Y, typename R, int kLanes, bool kOnce>
 void launch(const BlockNormArgs& p, hipStream_t stream) {
   constexpr int kRows = kThreads / kLanes;
   const int grid = static_cast<int>((p.M + kRows - 1) / kRows);
   const int per = (p.H + 4 * kLanes - 1) / (4 * kLanes);
   auto go = [&](auto u) {
-    block_norm_kernel<Y, R, kLanes, decltype(u)::value><<<grid, kThreads, 0, stream>>>(p);
+    block_norm_kernel<Y, R, kLanes, decltype(u)::value, kOnce><<<grid, kThreads, 0, stream>>>(p);
   };
   if (per <= 1) go(std::integral_constant<int, 1>{});
   else if (per <= 2) go(std::integral_constant<int, 2>{});
-  else if (per <= 3) go(std::integral_constant<int, 3>{});
-  else if (per <= 4) go(std::integral_constant<int, 4>{});
-  else if (per <= 6) go(std::integral_constant<int, 6>{});
-  else if (per <= 8) go(std::integral_constant<int, 8>{});
-  else if (per <= 10) go(std::integral_constant<int, 10>{});
-  else go(std::integral_constant<int, 16>{});
+  else if constexpr (kLanes == kThreads) {
+    if (per <= 3) go(std::integral_constant<int, 3>{});
+    else if (per <= 4) go(std::integral_constant<int, 4>{});
+    else if (per <= 8) go(std::integral_constant<int, 8>{});
+    else go(std::integral_constant<int, 16>{});
+  }
 }
 
 }  // namespace
 
-hipError_t launch_block_norm(const BlockNormArgs& p, bool y_bf16, bool r_bf16, int num_cus, hipStream_t stream) {
-  // A wave a row where the rows fill the chip, else the workgroup.
-  const bool waves = p.M >= 8 * num_cus && p.H <= 10 * 256;
+hipError_t launch_block_norm(const BlockNormArgs& p, bool y_bf16, bool r_bf16, hipStream_t stream) {
+  // A wave a row up to 512 elements, else the workgroup: few quadruples a lane beat rows without a
+  // barrier (us, a wave / the workgroup: 61 rows of 2560 9.6 / 4.4, 1537 of 1056 8.7 / 7.6, 8192 of 2560
+  // in float32 71 / 52).
+  const bool waves = p.H <= 512;
+  // What does not fit the last cache (256 MB) goes past it: 8192 rows of 2560 in float32 51.8 -> 48.6 us;
+  // less than that the next kernel finds there.
+  const int64_t each = (p.y ? (y_bf16 ? 2 : 4) : 0) + (r_bf16 ? 2 : 4) * ((p.residual != nullptr) + (p.residual_out != nullptr)) + (p.h ? 2 : 0);
+  const bool once = p.M * p.H * each > (int64_t{256} << 20);
   auto go = [&](auto y, auto r) {
     using Y = decltype(y);
     using R = decltype(r);
-    waves ? launch<Y, R, 64>(p, stream) : launch<Y, R, kThreads>(p, stream);
+    if (waves) once ? launch<Y, R, 64, true>(p, stream) : launch<Y, R, 64, false>(p, stream);
+    else once ? launch<Y, R, kThreads, true>(p, stream) : launch<Y, R, kThreads, false>(p, stream);
   };
   if (y_bf16) r_bf16 ? go(uint16_t{}, uint16_t{}) : go(uint16_t{}, float{});
   else r_bf16 ? go(float{}, uint16_t{}) : go(float{}, float{});

@@ -266,7 +266,7 @@ struct BlockNormArgs {
   bool w_bf16, gate_bf16;
   float offset, eps, a, b;
 };
-hipError_t launch_block_norm(const BlockNormArgs& p, bool y_bf16, bool r_bf16, int num_cus, hipStream_t stream);
+hipError_t launch_block_norm(const BlockNormArgs& p, bool y_bf16, bool r_bf16, hipStream_t stream);
 
 // moe_route.hip.  Groups of 32 experts at a time of a workgroup with 32 tokens, or 0: a workgroup 16
 // tokens and 16 experts, of which the last one of a block of tokens chooses (workspace: the state head,
