@@ -170,11 +170,11 @@ __device__ __forceinline__ void write_items(const MoeArgs& p, int slot, int e, i
   }
 }
 
-// Rows of x in LDS: kPiece / kG elements of 16 kG tokens at a time, rows 16 bytes past a multiple of
+// Rows of x in LDS: kPiece / kG elements of 16 kG tokens at a time, rows 32 bytes past a multiple of
 // 128, at which the lanes of an operand's read meet different banks.
 constexpr int kPiece = 2048;
 constexpr int kPieceUnits = kPiece / (128 * kSteps);
-__host__ __device__ constexpr int pitch_of(int blocks) { return kPiece / blocks * 2 + 16; }   // bytes
+__host__ __device__ constexpr int pitch_of(int blocks) { return kPiece / blocks * 2 + 32; }   // bytes
 
 // First launch: a wave has 16 intermediate features of one expert (a gate tile and an up tile) for
 // all of its tokens, and of the steps of H every kS-th unit.  The workgroup's waves share the

@@ -233,9 +233,9 @@ __device__ __forceinline__ float arrived_logit(const RouteArgs& p, const float* 
   return __hip_atomic_load(parts + static_cast<int64_t>(row) * p.E + e, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
 }
 
-// Rows in LDS: 16 bytes past a multiple of 128, at which 16 rows' octets at one place meet different
-// banks.
-__host__ __device__ constexpr int pitch_of(int elements) { return 2 * elements + 16; }
+// Rows in LDS: 32 bytes past a multiple of 128, at which 16 rows' octets at one place meet different
+// banks (16, 48 or 64 past it: twelve times the conflicts, 16.8 -> 17.6 us).
+__host__ __device__ constexpr int pitch_of(int elements) { return 2 * elements + 32; }
 // The two stages, or the parts' sums, of 32 tokens and 32 kE experts.
 __host__ __device__ constexpr int stages_bytes(int kE) {
   const int rows = 2 * (32 + 32 * kE) * pitch_of(64 * kWaves / kE), sums = kWaves / kE * 32 * (32 * kE + 4) * 4;
@@ -341,34 +341,38 @@ __global__ __launch_bounds__(kThreads, 2) void route_many_kernel(const RouteArgs
       for (int i = 0; i < kLoads; ++i) *reinterpret_cast<u32x4v*>(to + i * kEach * kPitch) = in ? v[i] : u32x4v{};
     };
     f32x4 acc[2][2] = {};
-    auto compute = [&](int stage) {
+    u32x4v a[2][2], b[2][2];
+    auto read = [&](int stage) {
       const unsigned char* at = smem + stage * kRows * kPitch + c * kPitch + (part * 8 + q) * 16;
 #pragma unroll
-      for (int s = 0; s < 2; ++s) {
-        u32x4v a[2], b[2];
+      for (int s = 0; s < 2; ++s)
 #pragma unroll
         for (int m = 0; m < 2; ++m) {
-          b[m] = *reinterpret_cast<const u32x4v*>(at + 16 * m * kPitch + 64 * s);
-          a[m] = *reinterpret_cast<const u32x4v*>(at + (32 + 32 * g + 16 * m) * kPitch + 64 * s);
+          b[s][m] = *reinterpret_cast<const u32x4v*>(at + 16 * m * kPitch + 64 * s);
+          a[s][m] = *reinterpret_cast<const u32x4v*>(at + (32 + 32 * g + 16 * m) * kPitch + 64 * s);
         }
-#pragma unroll
-        for (int m = 0; m < 2; ++m)
-#pragma unroll
-          for (int t = 0; t < 2; ++t) acc[m][t] = dev::mfma_bf16(a[m], b[t], acc[m][t]);
-      }
     };
 #pragma unroll
     for (int i = 0; i < kAhead; ++i) ask(i * kChunk, ring[i]);
     __syncthreads();                             // the sums before have been read
+    put(ring[0], 0, 0);
+    ask(kAhead * kChunk, ring[0]);
     constexpr int kRound = kAhead % 2 ? 2 * kAhead : kAhead;
     for (int i0 = 0; i0 < p.H; i0 += kRound * kChunk) {      // (chunks past the end are zeros)
 #pragma unroll
       for (int r = 0; r < kRound; ++r) {
-        const int k = i0 + r * kChunk;
-        put(ring[r % kAhead], k, r % 2);
-        ask(k + kAhead * kChunk, ring[r % kAhead]);
-        __syncthreads();                         // of a stage: written before this one, read before the next but one
-        compute(r % 2);
+        // A stage is written while the other is read: the next chunk's LDS writes overlap this one's reads.
+        const int next = i0 + (r + 1) * kChunk;
+        __syncthreads();
+        read(r % 2);
+        put(ring[(r + 1) % kAhead], next, (r + 1) % 2);
+        ask(next + kAhead * kChunk, ring[(r + 1) % kAhead]);
+#pragma unroll
+        for (int s = 0; s < 2; ++s)
+#pragma unroll
+          for (int m = 0; m < 2; ++m)
+#pragma unroll
+            for (int t = 0; t < 2; ++t) acc[m][t] = dev::mfma_bf16(a[s][m], b[s][t], acc[m][t]);
       }
     }
     __syncthreads();
