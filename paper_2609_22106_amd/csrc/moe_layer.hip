@@ -571,26 +571,16 @@ hipError_t launch_moe_layer(const MoePlan& c, const MoeArgs& p, void* workspace,
   const int rows = p.M <= 16 ? p.M * pitch_of(1) : std::max(16 * pitch_of(1), 32 * pitch_of(2));
   auto up = [&](auto kernel, int kN, int kS) {
     const int lds = std::max(rows + (kS > 1 ? kN * 2 * 64 * 16 : 0), std::max(routing_bytes(p.M, p.k), 4 * p.E));
-    if (lds > 64 * 1024) {
-      const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel),
-                                               hipFuncAttributeMaxDynamicSharedMemorySize, lds);
-      if (e != hipSuccess) return e;
-    }
     const int tiles = kN / kS;
-    kernel<<<dim3((p.I / 16 + tiles - 1) / tiles + 1, c.slots), 64 * kN, lds, stream>>>(
-        p, c.by_expert, rows, hidden, table);
+    kernel<<<dim3((p.I / 16 + tiles - 1) / tiles + 1, c.slots), 64 * kN, lds, stream>>>(p, c.by_expert, rows, hidden, table);
     return hipGetLastError();
   };
-  const hipError_t e = c.parts == 1 ? up(&moe_up_kernel<8, 1>, 8, 1) : up(&moe_up_kernel<4, 4>, 4, 4);
+  const hipError_t e = c.parts == 1 ? up(LargeLds<&moe_up_kernel<8, 1>>::kernel(), 8, 1)
+                                    : up(LargeLds<&moe_up_kernel<4, 4>>::kernel(), 4, 4);
   if (e != hipSuccess) return e;
   auto down = [&](auto kernel, int kT, int kN) {
-    const int sums = kN * p.M * sums_pitch(kT) * 4;
-    if (sums > 64 * 1024) {
-      const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel),
-                                               hipFuncAttributeMaxDynamicSharedMemorySize, sums);
-      if (e != hipSuccess) return e;
-    }
-    kernel<<<dim3(p.N / 16 / kT, c.splits), 64 * kN, sums, stream>>>(p, hidden, table, most, parts, arrived);
+    kernel<<<dim3(p.N / 16 / kT, c.splits), 64 * kN, kN * p.M * sums_pitch(kT) * 4, stream>>>(p, hidden, table, most, parts,
+                                                                                             arrived);
     return hipGetLastError();
   };
   return c.tiles == 2 ? down(&moe_down_kernel<2, 4, 2>, 2, 4) : down(&moe_down_kernel<1, 4, 3>, 1, 4);

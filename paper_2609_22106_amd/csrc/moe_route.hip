@@ -416,17 +416,14 @@ size_t route_workspace_bytes(const RoutePlan& c, int M, int E) {
 hipError_t launch_moe_route(const RoutePlan& c, const RouteArgs& p, void* workspace, hipStream_t stream) {
   auto many = [&](auto kernel, int kE) {
     const int lds = stages_bytes(kE) + 32 * logits_pitch(p.E, kE) * 4;
-    const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel),
-                                             hipFuncAttributeMaxDynamicSharedMemorySize, lds);
-    if (e != hipSuccess) return e;
     kernel<<<(p.M + 31) / 32, kThreads, lds, stream>>>(p);
     return hipGetLastError();
   };
   auto go = [&](auto bias) {
     constexpr bool kBias = decltype(bias)::value;
-    if (c.groups == 4) return many(&route_many_kernel<4, kBias>, 4);
-    if (c.groups == 2) return many(&route_many_kernel<2, kBias>, 2);
-    if (c.groups == 1) return many(&route_many_kernel<1, kBias>, 1);
+    if (c.groups == 4) return many(LargeLds<&route_many_kernel<4, kBias>>::kernel(), 4);
+    if (c.groups == 2) return many(LargeLds<&route_many_kernel<2, kBias>>::kernel(), 2);
+    if (c.groups == 1) return many(LargeLds<&route_many_kernel<1, kBias>>::kernel(), 1);
     const int tiles = (p.E + 15) / 16, most = tiles > 1 ? kMaxFewTokens : p.M;
     float* const parts = tiles > 1 ? reinterpret_cast<float*>(static_cast<char*>(workspace) + kWorkspaceStateBytes) : nullptr;
     for (int first = 0; first < p.M; first += most) {

@@ -5,6 +5,8 @@
 #include <cstddef>
 #include <cstdint>
 
+#include <mutex>
+
 #include <hip/hip_runtime_api.h>
 
 namespace prq {
@@ -247,6 +249,20 @@ hipError_t launch_lora(const LoraPlan& c, const uint16_t* x, int64_t ld_x, int M
                        int adapters, int rank_rows, int max_rank, const int32_t* offsets, const int32_t* of,
                        int segments, int N, const float* Y, int64_t ld_y, float* out, int64_t ld_out,
                        void* workspace, hipStream_t stream);
+
+// A kernel that is launched with more dynamic LDS than the 64 KiB default, which it is allowed once.
+template <auto kKernel>
+struct LargeLds {
+  static auto kernel() {
+    static std::once_flag once;
+    std::call_once(once, [] {
+      (void)hipFuncSetAttribute(reinterpret_cast<const void*>(kKernel), hipFuncAttributeMaxDynamicSharedMemorySize,
+                                160 * 1024);
+      (void)hipGetLastError();
+    });
+    return kKernel;
+  }
+};
 
 // The mixture-of-experts half of a layer.
 // block_norm.hip.  Rows of H (a multiple of 8, up to kMaxNormWidth); y, residual and the outputs

@@ -927,14 +927,48 @@ def prq_lora(x, adapters, segment_offsets, segment_adapter, Y, out=None, workspa
 
 
 # ---------------------------------------------------- mixture-of-experts half ---
-def _on_current_device(x, *others):
-    """The launch goes to the current device: `x` and the tensors beside it must be there."""
-    d = x.get_device()
-    for t in others:
-        if t is not None and t.get_device() != d:
-            raise ValueError(f"tensors on different devices: {x.device}, {t.device}")
+def _device_of(t, name):
+    """The device of a call's leading tensor, which must be the current one: the launch goes there."""
+    d = t.get_device()
+    if d < 0:
+        raise ValueError(f"{name} must be a GPU tensor")
     if d != (torch.cuda.current_device() if _cur_device is None else _cur_device()):
-        raise ValueError(f"the tensors are on {x.device}, which is not the current device")
+        raise ValueError(f"{name} is on {t.device}, which is not the current device")
+    return d
+
+
+# The checks of these calls: one expression a tensor, on one device d; whatever does not pass goes
+# through the functions behind, which say why.
+def _here(t, dtype, shape, d):
+    return (isinstance(t, torch.Tensor) and t.dtype is dtype and t.shape == shape and t.get_device() == d
+            and t.is_contiguous())
+
+
+def _on_device(t, name, d):
+    if t.get_device() != d:
+        raise ValueError(f"{name} is on {t.device}, which is not the current device")
+
+
+def _matrix(t, name, dtypes, M, wide, d):
+    """_rows on the current device."""
+    ld = _rows(t, name, dtypes, M, wide)
+    _on_device(t, name, d)
+    return ld
+
+
+def _exact(t, name, dtype, shape, d):
+    """A contiguous tensor of a shape on the current device."""
+    if not _here(t, dtype, shape, d):
+        _need(t, name, dtype, shape)
+        _on_gpu(**{name: t})
+        _on_device(t, name, d)
+
+
+def _norm_weight(w, name, H, d):
+    """(address, type) of a norm's weight [H] on the current device."""
+    if not _here(w, _BF16, (H,), d):
+        _exact(w, name, (_F32, _BF16), (H,), d)
+    return w.data_ptr(), PRQ_BF16 if w.dtype is _BF16 else PRQ_F32
 
 
 def prq_block_norm(y, residual, pre_weight=None, post_weight=None, gate=None, gate_index=None, eps=1e-6,
@@ -950,55 +984,57 @@ def prq_block_norm(y, residual, pre_weight=None, post_weight=None, gate=None, ga
     lead = residual if y is None else y
     if not isinstance(lead, torch.Tensor) or lead.dim() != 2:
         raise ValueError("y or residual must be [M, H]")
-    M, H = lead.shape
-    ld_y = _rows(y, "y", _ROPE_IN, M, H) if y is not None else 0
-    ld_r, r_type = 0, lead.dtype
+    M, H = shape = lead.shape
+    d = _device_of(lead, "residual" if y is None else "y")
+    y_at = r_at = ro_at = h_at = post = pre = gate_at = index_at = None
+    ld_y = ld_r = ld_ro = ld_h = ld_gate = w_kind = gate_rows = gate_kind = 0
+    y_kind = r_kind = lead.dtype
+    if y is not None:
+        ld_y = H if _here(y, _F32, shape, d) else _matrix(y, "y", _ROPE_IN, M, H, d)
+        y_at = y.data_ptr()
     if residual is not None:
-        ld_r, r_type = _rows(residual, "residual", _ROPE_IN, M, H), residual.dtype
+        ld_r = H if _here(residual, _BF16, shape, d) else _matrix(residual, "residual", _ROPE_IN, M, H, d)
+        r_at, r_kind = residual.data_ptr(), residual.dtype
         if residual_out is None and (y is not None or residual_scale != 1.0):
             residual_out = residual
-    ld_ro = 0
     if residual_out is residual:
-        ld_ro = ld_r
+        ro_at, ld_ro = r_at, ld_r
+        if y is None and residual_scale == 1.0:      # (nothing to change)
+            ro_at = None
     elif residual_out is not None:
-        ld_ro = _rows(residual_out, "residual_out", (r_type,), M, H)
-    post = pre = None
-    w_kind = 0
+        ld_ro = H if _here(residual_out, r_kind, shape, d) else _matrix(residual_out, "residual_out", (r_kind,), M, H, d)
+        ro_at = residual_out.data_ptr()
     if pre_weight is not None:
-        pre, w_kind = _head_weight(pre_weight, "pre_weight", H)
+        pre, w_kind = _norm_weight(pre_weight, "pre_weight", H, d)
     if post_weight is not None:
-        post, kind = _head_weight(post_weight, "post_weight", H)
+        post, kind = _norm_weight(post_weight, "post_weight", H, d)
         if pre is not None and kind != w_kind:
             raise ValueError("post_weight and pre_weight must have one type")
         w_kind = kind
-    ld_gate = gate_rows = gate_kind = 0
-    gate_at = index_at = None
     if gate is not None:
         if not isinstance(gate, torch.Tensor) or gate.dim() != 2:
             raise ValueError(f"gate must be [rows, {H}]")
         gate_rows = gate.shape[0]
-        ld_gate, gate_kind, gate_at = _rows(gate, "gate", _ROPE_IN, gate_rows, H), int(gate.dtype is _BF16), gate.data_ptr()
+        ld_gate, gate_kind = _matrix(gate, "gate", _ROPE_IN, gate_rows, H, d), int(gate.dtype is _BF16)
+        gate_at = gate.data_ptr()
         if gate_index is not None:
-            _vector(gate_index, "gate_index", _I32, M)
+            _exact(gate_index, "gate_index", _I32, (M,), d)
             index_at = gate_index.data_ptr()
     elif gate_index is not None:
         raise ValueError("gate_index needs a gate")
-    h_at, ld_h = None, 0
     if pre is not None:
         if out is None:
             out = _output(None, "out", (M, H), _BF16, lead, stream)
-        ld_h = _rows(out, "out", (_BF16,), M, H)
+        ld_h = H if _here(out, _BF16, shape, d) else _matrix(out, "out", (_BF16,), M, H, d)
         h_at = out.data_ptr()
     elif out is not None:
         raise ValueError("out needs pre_weight")
-    _on_current_device(lead, residual, residual_out, pre_weight, post_weight, gate, gate_index, out)
-    if h_at is not None or residual_out is not None:
-        st = _block_norm(None if y is None else y.data_ptr(), ld_y, int(lead.dtype is _BF16),
-                         None if residual is None else residual.data_ptr(), ld_r, int(r_type is _BF16), M, H, post, pre,
+    if h_at is not None or ro_at is not None:
+        st = _block_norm(y_at, ld_y, 1 if y_kind is _BF16 else 0, r_at, ld_r, 1 if r_kind is _BF16 else 0, M, H, post, pre,
                          w_kind, weight_offset, gate_at, ld_gate, gate_kind, gate_rows, index_at, eps, residual_scale,
-                         block_scale, None if residual_out is None else residual_out.data_ptr(), ld_ro, h_at, ld_h,
-                         _stream_of_call(stream))
-        _check(st, "prq_block_norm")
+                         block_scale, ro_at, ld_ro, h_at, ld_h, _stream_of_call(stream))
+        if st:
+            _check(st, "prq_block_norm")
     return out, residual if residual_out is None else residual_out
 
 
@@ -1006,14 +1042,16 @@ def prq_moe_route_workspace_bytes(M, E, H):
     return int(_route_ws(M, E, H))
 
 
-def _state_workspace(workspace, need, like, stream):
-    """(address, bytes) of a workspace with a state head, made (zeroed) where none is given."""
-    if workspace is None and need:
-        workspace = _alloc(torch.zeros, need, _U8, like.device, stream, kept=False)
-    elif workspace is not None and not _holds(workspace, _U8, 0):
+def _state_workspace(workspace, need, like, stream, d):
+    """A workspace with a state head (need() bytes, zeroed, where none is given), or None."""
+    if workspace is None:
+        n = need()
+        return _alloc(torch.zeros, n, _U8, like.device, stream, kept=False) if n else None
+    if not _holds(workspace, _U8, 0):
         _need(workspace, "workspace", _U8)
         _on_gpu(workspace=workspace)
-    return (None, 0, None) if workspace is None else (workspace.data_ptr(), workspace.numel(), workspace)
+    _on_device(workspace, "workspace", d)
+    return workspace
 
 
 def prq_moe_route(x, W, k, scoring="softmax", bias=None, renormalize=True, scale=1.0, ids=None, weights=None,
@@ -1026,29 +1064,48 @@ def prq_moe_route(x, W, k, scoring="softmax", bias=None, renormalize=True, scale
     allocated, zeroed by another launch)."""
     if not isinstance(x, torch.Tensor) or x.dim() != 2 or not isinstance(W, torch.Tensor) or W.dim() != 2:
         raise ValueError("x must be [M, H] and W [E, H]")
-    M, H = x.shape
-    E = W.shape[0]
+    (M, H), E = x.shape, W.shape[0]
     if scoring not in ROUTE_SCORINGS:
         raise ValueError(f"unknown scoring {scoring!r}")
-    ld_x, ld_w = _rows(x, "x", (_BF16,), M, H), _rows(W, "W", (_BF16,), E, H)
-    if bias is not None:
-        _vector(bias, "bias", _F32, E)
     if not 1 <= k <= E:
         raise ValueError(f"k {k} must lie between 1 and the {E} experts")
-    ids = _output(ids, "ids", (M, k), _I32, x, stream)
-    weights = _output(weights, "weights", (M, k), _F32, x, stream)
-    ld_l = _rows(logits, "logits", (_F32,), M, E) if logits is not None else 0
-    ws, ws_bytes, workspace = _state_workspace(workspace, 0 if workspace is not None else _route_ws(M, E, H), x, stream)
-    _on_current_device(x, W, bias, ids, weights, logits, workspace)
+    d = _device_of(x, "x")
+    ld_x = H if _here(x, _BF16, (M, H), d) else _matrix(x, "x", (_BF16,), M, H, d)
+    ld_w = H if _here(W, _BF16, (E, H), d) else _matrix(W, "W", (_BF16,), E, H, d)
+    if bias is not None:
+        _exact(bias, "bias", _F32, (E,), d)
+    if ids is None:
+        ids = _output(None, "ids", (M, k), _I32, x, stream)
+    if weights is None:
+        weights = _output(None, "weights", (M, k), _F32, x, stream)
+    _exact(ids, "ids", _I32, (M, k), d)
+    _exact(weights, "weights", _F32, (M, k), d)
+    ld_l = _matrix(logits, "logits", (_F32,), M, E, d) if logits is not None else 0
+    workspace = _state_workspace(workspace, lambda: _route_ws(M, E, H), x, stream, d)
     st = _route(x.data_ptr(), ld_x, M, H, W.data_ptr(), ld_w, E, k, ROUTE_SCORINGS[scoring], _ptr(bias),
-                1 if renormalize else 0, scale, ids.data_ptr(), weights.data_ptr(), _ptr(logits), ld_l, ws, ws_bytes,
-                _stream_of_call(stream))
-    _check(st, "prq_moe_route")
+                1 if renormalize else 0, scale, ids.data_ptr(), weights.data_ptr(), _ptr(logits), ld_l, _ptr(workspace),
+                0 if workspace is None else workspace.numel(), _stream_of_call(stream))
+    if st:
+        _check(st, "prq_moe_route")
     return ids, weights
 
 
 def prq_moe_layer_workspace_bytes(M, k, E, H, I, k_tail, N):
     return int(_moe_ws(M, k, E, H, I, k_tail, N))
+
+
+def _weight_here(W, name, d):
+    """(codes, scales) addresses of a PackedWeight on the current device."""
+    Wp, Wps = W.Wp, W.Wps
+    steps = (W.K_aug + 127) // 128
+    blocks = W.E * (W.N // 16)
+    if not (W.N % 16 == 0 and W.K_aug % 32 == 0 and _here(Wp, _U8, (blocks * steps * 1024,), d)
+            and _here(Wps, _U8, (blocks * ((steps + 3) // 4) * 256,), d)):
+        W.check_sizes()
+        _on_gpu(**{name + ".Wp": Wp, name + ".Wps": Wps})
+        _on_device(Wp, name + ".Wp", d)
+        _on_device(Wps, name + ".Wps", d)
+    return Wp.data_ptr(), Wps.data_ptr()
 
 
 def prq_moe_layer(x, ids, weights, gate_up, down, k_tail=0, out=None, workspace=None, stream=None):
@@ -1063,22 +1120,19 @@ def prq_moe_layer(x, ids, weights, gate_up, down, k_tail=0, out=None, workspace=
     if gate_up.K_aug != H or gate_up.N != 2 * I or down.E != E:
         raise ValueError(f"gate_up ({gate_up.E} x [{gate_up.N}, {gate_up.K_aug}]) and down ({down.E} x [{down.N}, "
                          f"{down.K_aug}]) do not fit [2 I, {H}] and [N, I + {k_tail}]")
-    ld_x = _rows(x, "x", (_BF16,), M, H)
-    if not (_is(ids, _I32, (M, k)) and _is(weights, _F32, (M, k)) and _weight_fits(gate_up) and _weight_fits(down)):
-        _need(ids, "ids", _I32, (M, k))
-        _need(weights, "weights", _F32, (M, k))
-        gate_up.check_sizes()
-        down.check_sizes()
-        _on_gpu(ids=ids, weights=weights, gate_up=gate_up.Wp, gate_up_scales=gate_up.Wps, down=down.Wp,
-                down_scales=down.Wps)
+    d = _device_of(x, "x")
+    ld_x = H if _here(x, _BF16, (M, H), d) else _matrix(x, "x", (_BF16,), M, H, d)
+    _exact(ids, "ids", _I32, (M, k), d)
+    _exact(weights, "weights", _F32, (M, k), d)
+    up_at, up_scales_at = _weight_here(gate_up, "gate_up", d)
+    down_at, down_scales_at = _weight_here(down, "down", d)
     if out is None:
         out = _output(None, "out", (M, N), _BF16, x, stream)
-    ld_out = _rows(out, "out", (_BF16,), M, N)
-    ws, ws_bytes, workspace = _state_workspace(workspace, 0 if workspace is not None else
-                                               _moe_ws(M, k, E, H, I, k_tail, N), x, stream)
-    _on_current_device(x, ids, weights, gate_up.Wp, gate_up.Wps, down.Wp, down.Wps, out, workspace)
-    st = _moe(x.data_ptr(), ld_x, M, ids.data_ptr(), weights.data_ptr(), k, gate_up.Wp.data_ptr(), gate_up.Wps.data_ptr(),
-              down.Wp.data_ptr(), down.Wps.data_ptr(), E, H, I, k_tail, N, out.data_ptr(), ld_out, ws, ws_bytes,
+    ld_out = N if _here(out, _BF16, (M, N), d) else _matrix(out, "out", (_BF16,), M, N, d)
+    workspace = _state_workspace(workspace, lambda: _moe_ws(M, k, E, H, I, k_tail, N), x, stream, d)
+    st = _moe(x.data_ptr(), ld_x, M, ids.data_ptr(), weights.data_ptr(), k, up_at, up_scales_at, down_at, down_scales_at, E,
+              H, I, k_tail, N, out.data_ptr(), ld_out, _ptr(workspace), 0 if workspace is None else workspace.numel(),
               _stream_of_call(stream))
-    _check(st, "prq_moe_layer")
+    if st:
+        _check(st, "prq_moe_layer")
     return out

@@ -149,18 +149,34 @@ def test_binding_refuses_host_tensors_and_wrong_shapes():
         prq.prq_moe_layer(r, ids, torch.zeros(3, 2), up, prq.PackedWeight(w, w, 9, 48, 96), k_tail=32)
 
 
-class _At:
-    """What a tensor says of its place."""
+class _At(torch.Tensor):
+    """A tensor that says it is elsewhere."""
 
-    def __init__(self, index):
-        self.device = f"cuda:{index}"
-        self.get_device = lambda: index
+    def get_device(self):
+        return self.index
 
 
 def test_tensors_of_another_device_are_refused(monkeypatch):
     monkeypatch.setattr(prq, "_cur_device", lambda: 1)
-    prq._on_current_device(_At(1), None, _At(1))
-    with pytest.raises(ValueError, match="different devices"):
-        prq._on_current_device(_At(1), _At(0))
-    with pytest.raises(ValueError, match="not the current"):
-        prq._on_current_device(_At(0), _At(0))
+    monkeypatch.setattr(prq, "_rows", lambda t, *a: t.shape[1])
+    monkeypatch.setattr(prq, "_on_gpu", lambda **t: None)
+
+    def at(index, *shape, dtype=BF16):
+        t = torch.zeros(shape, dtype=dtype).as_subclass(_At)
+        t.index = index
+        return t
+    w = at(1, 64, dtype=torch.float32)
+    for y, r, g in ((at(0, 3, 64), at(1, 3, 64), None), (at(1, 3, 64), at(0, 3, 64), None),
+                    (at(1, 3, 64), at(1, 3, 64), at(0, 1, 64))):
+        with pytest.raises(ValueError, match="not the current device"):
+            prq.prq_block_norm(y, r, w, gate=g)
+    with pytest.raises(ValueError, match="W is on"):
+        prq.prq_moe_route(at(1, 3, 64), at(0, 8, 64), 2)
+    up, down = (prq.PackedWeight(at(1, n, dtype=torch.uint8), at(1, s, dtype=torch.uint8), 8, *size)
+                for n, s, size in ((8 * 8 * 1024, 8 * 8 * 256, (128, 64)), (8 * 3 * 1024, 8 * 3 * 256, (48, 96))))
+    ids = at(1, 3, 2, dtype=torch.int32)
+    with pytest.raises(ValueError, match="weights is on"):
+        prq.prq_moe_layer(at(1, 3, 64), ids, at(0, 3, 2, dtype=torch.float32), up, down, k_tail=32)
+    down.Wps.index = 0
+    with pytest.raises(ValueError, match="down.Wps is on"):
+        prq.prq_moe_layer(at(1, 3, 64), ids, at(1, 3, 2, dtype=torch.float32), up, down, k_tail=32)
