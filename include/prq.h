@@ -613,9 +613,12 @@ enum {
 /*
  * prq_moe_route -- M tokens to k of E experts each:
  *   l = x W^T (float32 sums), s = softmax(l) or sigmoid(l);
- *   ids: the k experts with the largest s (+ bias, with the sigmoid; scores and keys are then
- *        float64), in descending order, the lower index first among equals, NaN last;
- *   weights: their s, with `renormalize` divided by the sum of the k, times `scale`.
+ *   ids: the k experts with the largest s, or s + bias (in float64; without a bias l itself is
+ *        compared, whose order is that of either score), in descending order, the lower index
+ *        first among equals, NaN last;
+ *   weights: their s, with `renormalize` divided by the sum of the k, times `scale`; the sigmoid in
+ *        float64, rounded at the end.  Infinite logits give what the formulas give (NaN weights where
+ *        a softmax has one).
  *
  *   x       device [M, ld_x] bf16
  *   W       device [E, ld_w] bf16
@@ -624,9 +627,10 @@ enum {
  *   ids     device [M, k] int32, weights device [M, k] float
  *   logits  device [M, ld_logits] float output (E used), or NULL
  *   workspace  device buffer of prq_moe_route_workspace_bytes, 16-byte aligned (may be NULL
- *           where that is 0): the 16 KiB state head of prq_gemm's workspaces (zero before the
- *           first use, left zero by every call), then scratch.  One buffer serves all calls
- *           that take such a head, in turn; calls that share it must be ordered.
+ *           where that is 0, which it may be for more tokens than another count needs one for): the
+ *           16 KiB state head of prq_gemm's workspaces (zero before the first use, left zero by
+ *           every call), then scratch.  One buffer serves all calls that take such a head, in
+ *           turn; calls that share it must be ordered.
  * x and W rows and pointers 16-byte aligned.
  * Limits: H % 8 == 0, H <= 65536, E <= 1024, k <= 32, k <= E, M < 2^24.  M == 0 is a no-op.
  */
@@ -641,8 +645,8 @@ int prq_moe_route(const void* x_bf16, int64_t ld_x, int32_t M, int32_t H, const 
  *   h_e = SiLU(Wgate_e x) * (Wup_e x)
  *   out[m] = sum_j weights[m, j] * Wdown_e [h_e ; last k_tail of h_e],   e = ids[m, j]
  * MXFP4 weights against bf16 activations: at so few rows the weights are the bytes, so the
- * activations are not quantized.  Sums are float32; weights[m, j] h is rounded to bf16 once, and
- * out once.
+ * activations are not quantized.  Sums are float32, in a fixed order (calls repeat bit for bit);
+ * weights[m, j] h is rounded to bf16 once, and out once.  Two launches.
  *
  *   x        device [M, ld_x] bf16
  *   ids      device [M, k] int32; an entry outside [0, E) adds nothing (padding, an expert held
