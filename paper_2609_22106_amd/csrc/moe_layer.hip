@@ -66,20 +66,43 @@ __device__ __forceinline__ void to_bf16(u32x4v w, uint32_t code, u32x4v (&out)[4
   }
 }
 
-// kSteps steps of a packed weight's tile of 16 rows, from a multiple of kSteps on: their kilobytes
-// (the last one's again past the end, for which the activations are zeros) and the dword of their
-// scales.
+// A buffer of `bytes` from p on, both the same for the wave: a load from outside it reads zeros and goes
+// nowhere, so that loops may ask for what is past their end.
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t buffer(const void* p, int bytes) {
+  return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(p), 0, bytes, 0x00020000);
+}
+constexpr uint32_t kOutside = 0x80000000u;
+constexpr int kStreamed = 2;                         // non-temporal
+
+// Consecutive tiles of 16 rows of a packed weight.
+struct Tiles {
+  __amdgpu_buffer_rsrc_t codes, scales;
+  int groups, steps;
+  __device__ __forceinline__ Tiles() = default;
+  __device__ __forceinline__ Tiles(const uint8_t* Wp, const uint8_t* Wps, int64_t first, int count, int steps)
+      : codes(buffer(Wp + first * steps * 1024, count * steps * 1024)),
+        scales(buffer(Wps + first * ((steps + 3) >> 2) * 256, count * ((steps + 3) >> 2) * 256)),
+        groups((steps + 3) >> 2), steps(steps) {}
+  // A lane's 16 code bytes of step s of tile t, and the dword that has its scale. The whole offset is the
+  // lane's, as only that is held against the buffer's size.
+  __device__ __forceinline__ u32x4v code(int t, int s, uint32_t past = 0) const {
+    const uint32_t at = (threadIdx.x & 63) * 16 + static_cast<uint32_t>(t * steps + s) * 1024 | past;
+    return __builtin_bit_cast(u32x4v, __builtin_amdgcn_raw_buffer_load_b128(codes, at, 0, kStreamed));
+  }
+  __device__ __forceinline__ uint32_t scale(int t, int s, uint32_t past = 0) const {
+    const uint32_t at = (threadIdx.x & 63) * 4 + static_cast<uint32_t>(t * groups + (s >> 2)) * 256 | past;
+    return __builtin_amdgcn_raw_buffer_load_b32(scales, at, 0, 0);
+  }
+};
+
+// kSteps steps of a tile, from a multiple of kSteps on (zeros past its end), and their scales.
 struct Unit {
   u32x4v codes[kSteps];
   uint32_t scales;
-  __device__ __forceinline__ void load(const uint8_t* Wp, const uint8_t* Wps, int64_t tile, int steps, int unit) {
-    const int lane = static_cast<int>(threadIdx.x) & 63;
-    const u32x4v* from = reinterpret_cast<const u32x4v*>(Wp) + tile * steps * 64 + lane;
-    scales = reinterpret_cast<const uint32_t*>(Wps)[(tile * ((steps + 3) >> 2) + (kSteps * unit >> 2)) * 64 + lane] >>
-             (8 * (kSteps * unit & 3));
+  __device__ __forceinline__ void load(const Tiles& w, int unit) {
+    scales = w.scale(0, kSteps * unit) >> (8 * (kSteps * unit & 3));
 #pragma unroll
-    for (int i = 0; i < kSteps; ++i)
-      codes[i] = __builtin_nontemporal_load(from + min(kSteps * unit + i, steps - 1) * 64);
+    for (int i = 0; i < kSteps; ++i) codes[i] = w.code(0, kSteps * unit + i);
   }
 };
 
@@ -220,24 +243,25 @@ __global__ __launch_bounds__(64 * kN, 4) void moe_up_kernel(const MoeArgs p, boo
   const float weight = __int_as_float(__builtin_amdgcn_ds_permute(4 * at, __float_as_int(share.weight)));
 
   const int64_t first = static_cast<int64_t>(e) * 2 * tiles + min(tile, tiles - 1);
+  const Tiles gate(p.up_codes, p.up_scales, first, 1, steps), up(p.up_codes, p.up_scales, first + tiles, 1, steps);
   // Tokens 16 block0 .. 16 (block0 + kG) - 1 of the expert.
   auto pass = [&](int block0, auto blocks) {
     constexpr int kG = decltype(blocks)::value, kUnits = kPieceUnits / kG, kPitch = pitch_of(kG);
     const int rows = min(n - 16 * block0, 16 * kG);
-    // A piece's units of a wave, of which there is an even number (past the end the last one's again, and
-    // unused), so that the two that are under way have registers of their own.
-    auto turns = [&](int u0) { return ((min(units - u0, kUnits) + kS - 1) / kS + 1) & ~1; };
+    // A piece's units of a wave, of which there is an even number (zeros past the end), so that the two that
+    // are under way have registers of their own.
+    auto turns = [&](int u0) { return max(((min(units - u0, kUnits) + kS - 1) / kS + 1) & ~1, 2); };
     struct Both {
       Unit gate, up;
     } ring[2];
     int next_u0 = 0, next_turn = 0;                  // what is asked for next
     auto ask = [&](Both& w) {
-      const int u = min(next_u0 + next_turn * kS + part, units - 1);
-      w.gate.load(p.up_codes, p.up_scales, first, steps, u);
-      w.up.load(p.up_codes, p.up_scales, first + tiles, steps, u);
+      const int u = next_u0 + next_turn * kS + part;
+      w.gate.load(gate, u);
+      w.up.load(up, u);
       if (++next_turn == turns(next_u0)) {
         next_turn = 0;
-        next_u0 = min(next_u0 + kUnits, (units - 1) / kUnits * kUnits);
+        next_u0 += kUnits;
       }
     };
     f32x4 acc[kG][2] = {};
@@ -328,8 +352,8 @@ constexpr int sums_pitch(int tiles) { return 16 * tiles + 4; }
 // added in their order, the workgroups' in theirs, by the one that arrives last.
 //
 // A wave asks for the weights and activations of a step kAhead steps ahead.  The loop has loads
-// without conditions only (past the end the last step's again, columns without a token outside the
-// buffer, which reads as zeros), so that every wait counts exactly the loads behind it.
+// without conditions only (past the end, and of columns without a token, outside their buffers), so
+// that every wait counts exactly the loads behind it.
 constexpr int kWindow = 64;
 
 template <int kT, int kN, int kAhead>
@@ -345,9 +369,8 @@ __global__ __launch_bounds__(64 * kN, 4) void moe_down_kernel(const MoeArgs p, c
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int c = lane & 15, q = lane >> 4;
   const int tile = static_cast<int>(blockIdx.x) * kT, splits = static_cast<int>(gridDim.y), part = static_cast<int>(blockIdx.y);
-  const int K = p.I + p.k_tail, steps = (K + 127) >> 7, groups = (steps + 3) >> 2, tiles = p.N >> 4;
-  const auto rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint16_t*>(hidden), 0,
-                                                      static_cast<int>(p.M * p.k * hidden_pitch(p.I) * 2), 0x00020000);
+  const int K = p.I + p.k_tail, steps = (K + 127) >> 7, tiles = p.N >> 4;
+  const auto rsrc = buffer(hidden, static_cast<int>(p.M * p.k * hidden_pitch(p.I) * 2));
   float* const mine = own + wave * p.M * kPitch;
 
   // Item i of this workgroup is item part + splits i of all; the first window's are loaded before their
@@ -388,13 +411,11 @@ __global__ __launch_bounds__(64 * kN, 4) void moe_down_kernel(const MoeArgs p, c
       // The step that is asked for next: its item, the expert's tiles, and where the item's tokens are
       // in `hidden`, in bytes, and how many.
       int item = begin / steps, step = begin % steps, u = 0, columns;
-      const u32x4v* codes;
-      const uint32_t* scales;
+      Tiles down;
       uint32_t base;
       auto enter = [&] {
         const int64_t first = static_cast<int64_t>(__builtin_amdgcn_readfirstlane(sh_experts[item])) * tiles + tile;
-        codes = reinterpret_cast<const u32x4v*>(p.down_codes) + first * steps * 64;
-        scales = reinterpret_cast<const uint32_t*>(p.down_scales) + first * groups * 64;
+        down = Tiles(p.down_codes, p.down_scales, first, kT, steps);
         const int rows = __builtin_amdgcn_readfirstlane(sh_rows[item]);
         base = static_cast<uint32_t>((rows >> 5) * hidden_pitch(p.I) * 2);
         columns = rows & 31;
@@ -407,24 +428,22 @@ __global__ __launch_bounds__(64 * kN, 4) void moe_down_kernel(const MoeArgs p, c
       } ring[kRing];
       auto ask = [&](Step& s) {
         int k = 128 * step + 32 * q;                 // the tail meets the last values again, zeros behind it
-        const bool in = k < K && c < columns;
+        const uint32_t past = u < n ? 0 : kOutside;
+        const bool in = k < K && c < columns && u < n;
         if (k >= p.I) k -= p.k_tail;
-        const uint32_t at = in ? base + static_cast<uint32_t>((((k >> 7) * 16 + (k >> 5 & 3)) * columns + c) * 16) : 0x80000000u;
+        const uint32_t at = in ? base + static_cast<uint32_t>((((k >> 7) * 16 + (k >> 5 & 3)) * columns + c) * 16) : kOutside;
 #pragma unroll
         for (int t = 0; t < kT; ++t) {
-          s.codes[t] = __builtin_nontemporal_load(codes + (t * steps + step) * 64 + lane);
-          s.scales[t] = scales[(t * groups + (step >> 2)) * 64 + lane];
+          s.codes[t] = down.code(t, step, past);
+          s.scales[t] = down.scale(t, step, past);
         }
 #pragma unroll
         for (int j = 0; j < 4; ++j)
           s.b[j] = __builtin_bit_cast(u32x4v, __builtin_amdgcn_raw_buffer_load_b128(rsrc, at, 64 * j * columns, 0));
-        if (u + 1 < n) {
-          ++u;
-          if (++step == steps) {
-            step = 0;
-            ++item;
-            enter();
-          }
+        if (++u < n && ++step == steps) {
+          step = 0;
+          ++item;
+          enter();
         }
       };
       f32x4 acc[kT] = {};
