@@ -14,8 +14,13 @@
 // takes four times as long: 8192 tokens of 128 experts 53 us).  Few tokens: a workgroup has 16 of them
 // and 16 experts, and its waves share H, so that W is read by as many CUs as possible.  The last
 // one of a block of tokens to arrive reads the block's logits back.  Many: a workgroup has 32 tokens and
-// all experts, in two stages of LDS.  Choosing, a
-// token has 16 lanes (a wave past 256 experts).
+// all experts, in two stages of LDS.  Choosing, a token has 16 lanes (or a wave).
+//
+// Bounds.  One token of 128 experts, H = 2048, 6.6 us: launch 2, one trip to memory and the product 2,
+// arrival 1, choosing 1.5.  8192 of them 16.8 us: their bytes are 6.4, but one workgroup a CU passes 640 KB
+// through its LDS in 16 chunks at 0.45 us (20 TB/s over the card, most of it W from L2), behind a launch of
+// 3 and in front of 3 of choosing.  1537 tokens of 250 experts, H = 1024, 18.8 us: the same on 49 CUs with
+// two groups of experts.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -47,42 +52,60 @@ __device__ __forceinline__ uint64_t ordered(double x) {
 
 __device__ __forceinline__ double sigmoid64(float l) { return 1.0 / (1.0 + exp(-static_cast<double>(l))); }
 
-// fold(move) for the exchanges after which every lane of a group of kLanes has met every other: each
-// neighbour, pair, quad and octet, then each 16 and 32.
+// fold(both) for the exchanges after which every lane of a group of kLanes has met every other: each
+// neighbour, pair, quad and octet, then each 16 and 32.  both(x): x of the two lanes that meet, in one
+// order or the other.
 template <int kLanes, typename Fold>
 __device__ __forceinline__ void over_group(Fold fold) {
+  struct Both {
+    uint32_t a, b;
+  };
   auto by = [](auto ctrl) {
     return [](uint32_t x) {
-      return static_cast<uint32_t>(
-          __builtin_amdgcn_update_dpp(0, static_cast<int>(x), decltype(ctrl)::value, 0xF, 0xF, false));
+      return Both{x, static_cast<uint32_t>(
+                         __builtin_amdgcn_update_dpp(0, static_cast<int>(x), decltype(ctrl)::value, 0xF, 0xF, false))};
     };
   };
   fold(by(std::integral_constant<int, 0xB1>{}));         // quad_perm 1 0 3 2
   fold(by(std::integral_constant<int, 0x4E>{}));         // quad_perm 2 3 0 1
   fold(by(std::integral_constant<int, 0x141>{}));        // row_half_mirror
   fold(by(std::integral_constant<int, 0x140>{}));        // row_mirror
-  if constexpr (kLanes == 64) {
-    fold([](uint32_t x) { return static_cast<uint32_t>(__shfl_xor(static_cast<int>(x), 16, 64)); });
-    fold([](uint32_t x) { return static_cast<uint32_t>(__shfl_xor(static_cast<int>(x), 32, 64)); });
+  if constexpr (kLanes == 64) {                          // (an exchange through LDS takes a hundred cycles)
+    fold([](uint32_t x) {
+      const auto r = __builtin_amdgcn_permlane16_swap(x, x, false, false);
+      return Both{r[0], r[1]};
+    });
+    fold([](uint32_t x) {
+      const auto r = __builtin_amdgcn_permlane32_swap(x, x, false, false);
+      return Both{r[0], r[1]};
+    });
   }
 }
 template <int kLanes>
 __device__ __forceinline__ float group_sum(float x) {
-  over_group<kLanes>([&](auto move) { x += __uint_as_float(move(__float_as_uint(x))); });
+  over_group<kLanes>([&](auto both) {
+    const auto v = both(__float_as_uint(x));
+    x = __uint_as_float(v.a) + __uint_as_float(v.b);
+  });
   return x;
 }
 template <int kLanes>
 __device__ __forceinline__ double group_sum(double x) {
-  over_group<kLanes>([&](auto move) {
+  over_group<kLanes>([&](auto both) {
     const uint64_t u = __double_as_longlong(x);
-    x += __longlong_as_double(static_cast<uint64_t>(move(static_cast<uint32_t>(u >> 32))) << 32 | move(static_cast<uint32_t>(u)));
+    const auto high = both(static_cast<uint32_t>(u >> 32)), low = both(static_cast<uint32_t>(u));
+    x = __longlong_as_double(static_cast<uint64_t>(high.a) << 32 | low.a) +
+        __longlong_as_double(static_cast<uint64_t>(high.b) << 32 | low.b);
   });
   return x;
 }
 
 template <int kLanes>
 __device__ __forceinline__ uint32_t group_max(uint32_t x) {
-  over_group<kLanes>([&](auto move) { x = max(x, move(x)); });
+  over_group<kLanes>([&](auto both) {
+    const auto v = both(x);
+    x = max(v.a, v.b);
+  });
   return x;
 }
 
@@ -164,10 +187,14 @@ __device__ __forceinline__ void choose(const RouteArgs& p, int token, bool live,
 #pragma unroll
     for (int i = 0; i < kKept; ++i) total += w[i] = kept(i) ? expf(chosen[i] - first) : 0.f;
     if (!p.renormalize) {
-      total = 0.f;
+      float each[kR];
 #pragma unroll
-      for (int i = 0; i < kR; ++i)
-        if (mine * kR + i < p.E) total += expf(l[i] - first);
+      for (int i = 0; i < kR; ++i) each[i] = mine * kR + i < p.E ? expf(l[i] - first) : 0.f;
+#pragma unroll
+      for (int n = kR / 2; n; n /= 2)            // in pairs: five roundings of a lane's 32
+#pragma unroll
+        for (int i = 0; i < n; ++i) each[i] += each[i + n];
+      total = each[0];
     }
     total = group_sum<kLanes>(total);
 #pragma unroll
@@ -183,15 +210,17 @@ __device__ __forceinline__ void choose(const RouteArgs& p, int token, bool live,
 }
 
 // Tokens token0 .. token0 + rows - 1 by the workgroup: 16 lanes each, or 64 where there are no more tokens
-// than waves or the experts are many.  logit(row, e).
+// than waves or the experts are many (300 tokens of 512 experts: 25 us with 16, 26 with 64; 2000 tokens 84
+// and 93).  logit(row, e).
 template <bool kBias, typename Logit>
 __device__ __forceinline__ void choose_rows(const RouteArgs& p, int token0, int rows, Logit logit) {
   const int wave = static_cast<int>(threadIdx.x) >> 6;
-  if (p.E > 256 || rows <= kWaves) {
+  if (p.E > 512 || rows <= kWaves) {
     for (int r = wave; r < rows; r += kWaves) {
       auto of = [&](int e) { return logit(r, e); };
       if (p.E <= 128) choose<64, 2, kBias>(p, token0 + r, true, of);
       else if (p.E <= 256) choose<64, 4, kBias>(p, token0 + r, true, of);
+      else if (p.E <= 512) choose<64, 8, kBias>(p, token0 + r, true, of);
       else choose<64, kMaxRouteExperts / 64, kBias>(p, token0 + r, true, of);
     }
   } else {
@@ -200,7 +229,8 @@ __device__ __forceinline__ void choose_rows(const RouteArgs& p, int token0, int 
       auto of = [&](int e) { return logit(r, e); };
       if (p.E <= 64) choose<16, 4, kBias>(p, token0 + r, r < rows, of);
       else if (p.E <= 128) choose<16, 8, kBias>(p, token0 + r, r < rows, of);
-      else choose<16, 16, kBias>(p, token0 + r, r < rows, of);
+      else if (p.E <= 256) choose<16, 16, kBias>(p, token0 + r, r < rows, of);
+      else choose<16, 32, kBias>(p, token0 + r, r < rows, of);
     }
   }
 }
@@ -394,8 +424,8 @@ __global__ __launch_bounds__(kThreads, 2) void route_many_kernel(const RouteArgs
   choose_rows<kBias>(p, token0, count, [&](int r, int e) { return logits[r * pitch + e]; });
 }
 
-// Experts past which a block's logits do not fit beside the stages, and tokens in a launch of the
-// other kernel: what the state's counters and a modest workspace hold.
+// Experts past which a block's logits do not fit beside the stages (512: 158 of 160 KB), and tokens in a
+// launch of the other kernel: what the state's counters and a modest workspace hold.
 constexpr int kMaxManyExperts = 512;
 constexpr int kMaxFewTokens = 8192;
 static_assert(kMaxFewTokens / 16 <= static_cast<int>(kWorkspaceStateBytes / 4), "a counter a block");
@@ -404,8 +434,13 @@ static_assert(kMaxFewTokens / 16 <= static_cast<int>(kWorkspaceStateBytes / 4), 
 
 RoutePlan plan_moe_route(int M, int E, int H, int num_cus) {
   RoutePlan c;
+  // A workgroup for 16 experts while there are no more than two a CU; the other kernel's time grows with
+  // the groups of 128 experts that its workgroups take in turn.  us, this one / the other: 128 experts
+  // (H = 2048) 600 tokens 12.1 / 15.1, 1024 12.9 / 15.1, 2000 23.3 / 15.2; 64 (2560) 1000 tokens 10.4 / 14.0,
+  // 2048 13.0 / 14.4, 4000 22.9 / 13.2; 250 (1024) 700 tokens 16.3 / 18.6, 1000 20.4 / 18.9, 1537 27.6 / 18.9;
+  // 512 (2048) 800 tokens 38.0 / 51.9, 1100 50.5 / 51.9, 2000 80.8 / 51.8.
   const int64_t few = (static_cast<int64_t>(M) + 15) / 16 * ((E + 15) / 16);
-  if (E <= kMaxManyExperts && few > 2 * num_cus) c.groups = E > 64 ? 4 : E > 32 ? 2 : 1;
+  if (E <= kMaxManyExperts && few > 2 * num_cus * ((E + 127) / 128)) c.groups = E > 64 ? 4 : E > 32 ? 2 : 1;
   return c;
 }
 

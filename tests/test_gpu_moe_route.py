@@ -1,8 +1,8 @@
 """prq_moe_route against the float64 oracle.
 
 Logits whose sums are exact in float32 (x and W on a grid of few bits) make the choice exact too: ids
-are compared for equality, ties among them.  Weights: expf and the sums behind them, at most 32
-terms of the chosen or E / 64 + 6 of all, a quotient and a product: 2^-20 of the value.  Before that the
+are compared for equality, ties among them.  Weights: expf (2^-23) and the sum of its values, two and six
+roundings of the chosen, ten of all, a quotient and a product: below 2^-20 of the value.  Before that the
 logit's distance d to the largest one is rounded to float32, which is d 2^-24 of the exponent and so
 of the weight (d is below 8 for the logits on the grid; logits of deviation 45 reach 150, and 150 * 2^-24
 alone is 9 * 2^-20); a weight below float32's normal numbers may be anything down to 0, 2^-126.  The
@@ -65,6 +65,18 @@ def test_matches_oracle(M, E, k, H, sigmoid, renormalize):
     want = _np(x) @ _np(w).T
     np.testing.assert_array_equal(_np(logits), want)
     _check(got, want, k, sigmoid, bias if sigmoid else None, renormalize, 2.5)
+
+
+@pytest.mark.parametrize("M,E,k,H", [(2, 257, 8, 64), (9, 300, 31, 64), (40, 512, 8, 72), (1300, 300, 32, 16),
+                                     (1150, 257, 3, 136), (8200, 520, 8, 8)])
+@pytest.mark.parametrize("sigmoid", [False, True])
+def test_more_experts_than_a_group(M, E, k, H, sigmoid):
+    """Past 256 experts a token has 32 keys a lane, past 512 a wave; past 8192 tokens of those, two launches."""
+    say("route", M, E, k, H, sigmoid)
+    x, w, bias = _grid(M, E, H, M + E + H)
+    got = _prq().prq_moe_route(x, w, k, scoring="sigmoid" if sigmoid else "softmax", bias=bias if sigmoid else None,
+                               renormalize=False)
+    _check(got, _np(x) @ _np(w).T, k, sigmoid, bias if sigmoid else None, False)
 
 
 @pytest.mark.parametrize("M", [5, 1200])
