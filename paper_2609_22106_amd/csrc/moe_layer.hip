@@ -9,11 +9,15 @@
 // of them the output's own.  A token that names an expert twice gets it with both weights; an id
 // outside [0, E) names none.
 //
-// The weights of the experts that are reached are most of the bytes, and what bounds both
-// launches; a CU has 80 cycles of matrix work free for every kilobyte of them, so the
-// activations stay in bf16 at no cost and the weights are brought to bf16 in registers (a 4-bit
-// value times a power of two is exact there).  A wave asks for four K steps of its weights and
-// the activations that meet them at once; enough waves a CU keep the memory busy meanwhile.
+// The weights of the experts that are reached are most of the bytes, and what bounds both launches
+// where they are many: 64 tokens of 128 experts, eight a token, of 2048 -> 768 + 64 -> 2048, 292 MB in
+// 65 us, 39 and 26 (4.8 and 4.0 TB/s, of 5.4 that a copy reaches); 19 tokens of 64, six a token, of
+// 2560 -> 1408, 282 MB in 59, 38.5 and 20.4.  A CU has 80 cycles of matrix work free for every kilobyte of
+// weights, so the activations stay in bf16 at no cost and the weights are brought to bf16 in registers
+// (a 4-bit value times a power of two is exact there).  A wave has two units of weights under way; enough
+// waves a CU keep the memory busy meanwhile.  One token (21 MB, 3.8 us of them) takes 14.6 us, since its trips
+// to memory follow each other: in the first launch (7.4) the launch itself 1.5, routing 2.2, x 0.4, weights
+// 1.9, the rest of them and the sums 1.5; in the second the table, weights, and the join of workgroups.
 //
 // A slot is an expert (its number), or where there are fewer pairs of a token and an expert than
 // experts a pair (its first occurrence), so that a launch of `slots` workgroups in y reaches every
@@ -560,8 +564,12 @@ MoePlan plan_moe_layer(const MoeArgs& p, int num_cus) {
   MoePlan c;
   c.slots = std::min(p.E, p.M * p.k);
   c.by_expert = c.slots == p.E;
-  // The first launch: a wave a tile, or four where those would be few.
-  c.parts = static_cast<int64_t>(p.I / 16) * c.slots <= 3 * num_cus ? 4 : 1;
+  // The first launch: a wave a tile, or two or four where those would be few.  us of the whole call, four /
+  // two / one (128 experts, eight a token, of 2048 -> 768): one token 14.6 / 15.1 / 18.0, 2 18.3 / 18.4 / 20.8,
+  // 4 26.4 / 25.3 / 25.4, 8 40.5 / 37.0 / 37.1, 16 64.0 / 52.6 / 48.6, 64 104 / 82 / 69; 64 experts, six a token,
+  // of 2560 -> 1408: one 17.3 / 18.5 / 21.2, 3 31.1 / 28.8 / 29.3, 19 84.5 / 69.0 / 66.4.
+  const int64_t waves = static_cast<int64_t>(p.I / 16) * c.slots;
+  c.parts = waves <= 4 * num_cus ? 4 : waves <= 12 * num_cus ? 2 : 1;
   // The second: two tiles a workgroup where their number is even, so that the activations are loaded for
   // two, and a workgroup a CU, of which a wave has three steps at least.  us, two tiles and four
   // workgroups along the experts / two / one, then one tile and two workgroups (128 experts of 768 + 64,
@@ -594,8 +602,9 @@ hipError_t launch_moe_layer(const MoePlan& c, const MoeArgs& p, void* workspace,
     kernel<<<dim3((p.I / 16 + tiles - 1) / tiles + 1, c.slots), 64 * kN, lds, stream>>>(p, c.by_expert, rows, hidden, table);
     return hipGetLastError();
   };
-  const hipError_t e = c.parts == 1 ? up(LargeLds<&moe_up_kernel<8, 1>>::kernel(), 8, 1)
-                                    : up(LargeLds<&moe_up_kernel<4, 4>>::kernel(), 4, 4);
+  const hipError_t e = c.parts == 1   ? up(LargeLds<&moe_up_kernel<8, 1>>::kernel(), 8, 1)
+                       : c.parts == 2 ? up(LargeLds<&moe_up_kernel<4, 2>>::kernel(), 4, 2)
+                                      : up(LargeLds<&moe_up_kernel<4, 4>>::kernel(), 4, 4);
   if (e != hipSuccess) return e;
   auto down = [&](auto kernel, int kT, int kN) {
     kernel<<<dim3(p.N / 16 / kT, c.splits), 64 * kN, kN * p.M * sums_pitch(kT) * 4, stream>>>(p, hidden, table, most, parts,

@@ -69,6 +69,17 @@ def test_matches_oracle(M, E, k, H, I, tail, N):
     layer.check(got, x, ids, w)
 
 
+@pytest.mark.parametrize("M,E,k,H,I,tail,N", [
+    (20, 64, 6, 160, 352, 32, 48), (50, 64, 6, 2144, 288, 0, 32), (64, 60, 9, 96, 448, 64, 80),      # two waves a tile
+    (12, 128, 9, 288, 480, 32, 32), (40, 128, 8, 1184, 416, 0, 48), (64, 130, 8, 64, 544, 96, 16)])   # one
+def test_many_tiles(M, E, k, H, I, tail, N):
+    """More intermediate features of all experts: fewer waves of the first launch share a tile."""
+    say("experts", M, E, k, H, I, tail, N)
+    layer = Layer(E, H, I, tail, N, seed=M + E + H)
+    x, ids, w = _routed(M, E, k, M + 1, H)
+    layer.check(layer(x, ids, w), x, ids, w)
+
+
 @pytest.mark.parametrize("M", [1, 20, 64])
 def test_ids_that_name_nothing_rows_without_experts_and_an_expert_named_twice(M):
     layer = Layer(6, 128, 64, 32, 96, seed=3)
