@@ -250,12 +250,15 @@ hipError_t launch_lora(const LoraPlan& c, const uint16_t* x, int64_t ld_x, int M
                        int segments, int N, const float* Y, int64_t ld_y, float* out, int64_t ld_out,
                        void* workspace, hipStream_t stream);
 
-// A kernel that is launched with more dynamic LDS than the 64 KiB default, which it is allowed once.
+// A kernel that is launched with more dynamic LDS than the 64 KiB default, which it is allowed once on
+// each device.
 template <auto kKernel>
 struct LargeLds {
   static auto kernel() {
-    static std::once_flag once;
-    std::call_once(once, [] {
+    static std::once_flag once[64];
+    int device = 0;
+    (void)hipGetDevice(&device);
+    std::call_once(once[device & 63], [] {
       (void)hipFuncSetAttribute(reinterpret_cast<const void*>(kKernel), hipFuncAttributeMaxDynamicSharedMemorySize,
                                 160 * 1024);
       (void)hipGetLastError();

@@ -984,6 +984,8 @@ def prq_block_norm(y, residual, pre_weight=None, post_weight=None, gate=None, ga
     lead = residual if y is None else y
     if not isinstance(lead, torch.Tensor) or lead.dim() != 2:
         raise ValueError("y or residual must be [M, H]")
+    if y is None and (post_weight is not None or gate is not None):
+        raise ValueError("post_weight and gate need y")
     M, H = shape = lead.shape
     d = _device_of(lead, "residual" if y is None else "y")
     y_at = r_at = ro_at = h_at = post = pre = gate_at = index_at = None

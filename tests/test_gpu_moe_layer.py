@@ -121,7 +121,7 @@ def test_nan_and_infinity_stay_in_their_token():
     assert bool(torch.isnan(got[3]).all()) and bool(torch.isnan(got[20]).all()) and not bool(torch.isfinite(got[17]).all())
 
 
-@pytest.mark.parametrize("lo,hi", [(1, 20), (60, 70), (127, 127), (150, 180)])
+@pytest.mark.parametrize("lo,hi", [(0, 0), (1, 20), (60, 70), (127, 127), (150, 180), (230, 242)])
 def test_scale_codes_far_from_one(lo, hi):
     """Each E8M0 code as the power of two that it is: one weight of ones in either product."""
     prq = _prq()
@@ -163,6 +163,28 @@ def test_strides_and_a_shared_workspace():
         assert torch.equal(layer(x, ids, w, workspace=ws), got)      # the same bits again
         ws[16384:] = 255                                             # (NaN) nothing is read that was not written
     assert prq.prq_moe_layer_workspace_bytes(64, 3, 64, 256, 224, 32, 512) <= ws.numel()
+
+
+@pytest.mark.parametrize("M,E,k,H,I,tail,N", [(2, 1, 1, 65536, 32, 0, 16), (64, 2, 2, 32, 32768, 32, 16),
+                                              (35, 2, 1, 32, 32, 0, 65536)])
+def test_largest_widths(M, E, k, H, I, tail, N):
+    say("experts", M, E, k, H, I, tail, N)
+    layer = Layer(E, H, I, tail, N, seed=M + E)
+    x, ids, w = _routed(M, E, k, M, H)
+    layer.check(layer(x, ids, w), x, ids, w)
+
+
+def test_rows_past_32_bits():
+    """Rows of x and out more than 2^31 elements apart, first to last."""
+    M, ld = 20, 1 << 27
+    layer = Layer(8, 64, 32, 0, 48, seed=4)
+    x, ids, w = _routed(M, 8, 2, 6, 64)
+    far = torch.empty((M - 1) * ld + 16384, dtype=BF16, device="cuda")
+    rows, out = far.as_strided((M, 64), (ld, 1)), far[8192:].as_strided((M, 48), (ld, 1))
+    rows.copy_(x)
+    layer(rows, ids, w, out=out)
+    layer.check(out, x, ids, w)
+    assert torch.equal(rows, x)
 
 
 def test_zero_tokens():

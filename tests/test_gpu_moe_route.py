@@ -153,6 +153,20 @@ def test_strides_and_a_shared_workspace(M):
         assert not ws[:16384].any()
 
 
+@pytest.mark.parametrize("M,ld", [(20, 1 << 27), (1100, 1 << 21)])
+def test_rows_past_32_bits(M, ld):
+    """Rows of x, and of the logits, more than 2^31 elements apart, first to last."""
+    x, w, _ = _grid(M, 40, 64, 7)
+    far = torch.empty((M - 1) * ld + 16384, dtype=torch.bfloat16, device="cuda")
+    rows = far.as_strided((M, 64), (ld, 1))
+    rows.copy_(x)
+    logits = far.view(torch.float32)[4096:].as_strided((M, 40), (ld // 2, 1))
+    got = _prq().prq_moe_route(rows, w, 4, logits=logits)
+    _check(got, _np(x) @ _np(w).T, 4)
+    np.testing.assert_array_equal(_np(logits), _np(x) @ _np(w).T)
+    assert torch.equal(rows, x)
+
+
 def test_zero_tokens():
     x, w, _ = _grid(0, 8, 64, 1)
     ids, weights = _prq().prq_moe_route(x, w, 2)

@@ -133,6 +133,9 @@ def test_binding_refuses_host_tensors_and_wrong_shapes():
     for args, kw in (((y, r, w), {}), ((None, r, w), {}), ((y, None, w), {}), ((None, None, w), {}), ((y[0], r, w), {})):
         with pytest.raises(ValueError):
             prq.prq_block_norm(*args, **kw)
+    for kw in (dict(post_weight=w), dict(gate=torch.zeros(1, 64))):      # also where nothing would be launched
+        with pytest.raises(ValueError, match="need y"):
+            prq.prq_block_norm(None, r, **kw)
     W = torch.zeros(8, 64, dtype=BF16)
     with pytest.raises(ValueError, match="x must be"):
         prq.prq_moe_route(r, W, 2)                                       # not on a GPU
