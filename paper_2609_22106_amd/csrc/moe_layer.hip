@@ -11,13 +11,15 @@
 //
 // The weights of the experts that are reached are most of the bytes, and what bounds both launches
 // where they are many: 64 tokens of 128 experts, eight a token, of 2048 -> 768 + 64 -> 2048, 292 MB in
-// 65 us, 39 and 26 (4.8 and 4.0 TB/s, of 5.4 that a copy reaches); 19 tokens of 64, six a token, of
-// 2560 -> 1408, 282 MB in 59, 38.5 and 20.4.  A CU has 80 cycles of matrix work free for every kilobyte of
-// weights, so the activations stay in bf16 at no cost and the weights are brought to bf16 in registers
-// (a 4-bit value times a power of two is exact there).  A wave has two units of weights under way; enough
-// waves a CU keep the memory busy meanwhile.  One token (21 MB, 3.8 us of them) takes 14.6 us, since its trips
-// to memory follow each other: in the first launch (7.4) the launch itself 1.5, routing 2.2, x 0.4, weights
-// 1.9, the rest of them and the sums 1.5; in the second the table, weights, and the join of workgroups.
+// 65 us, 39 and 26; 19 tokens of 64, six a token, of 2560 -> 1408, 282 MB in 55, 34 and 20.5 (a copy reaches
+// 5.4 TB/s, the first launch 5.0 and 5.5).  The second loses 5 us to its start and 2.5 to the join of
+// workgroups; twice the waves or workgroups change nothing there (65.2 and 65 us).  A CU has 80 cycles of
+// matrix work free for every kilobyte of weights, so the activations stay in bf16 at no cost and the
+// weights are brought to bf16 in registers (a 4-bit value times a power of two is exact there).  A wave
+// has two units of weights under way; enough waves a CU keep the memory busy meanwhile.  One token (21 MB,
+// 3.8 us of them) takes 14.6 us, since its trips to memory follow each other: in the first launch (7.3) the
+// launch itself 1.5, routing 2.2, x 0.4, weights 1.9, the rest of them and the sums 1.5; in the second the
+// table, weights, and the join.
 //
 // A slot is an expert (its number), or where there are fewer pairs of a token and an expert than
 // experts a pair (its first occurrence), so that a launch of `slots` workgroups in y reaches every
@@ -197,11 +199,17 @@ __device__ __forceinline__ void write_items(const MoeArgs& p, int slot, int e, i
   }
 }
 
-// Rows of x in LDS: kPiece / kG elements of 16 kG tokens at a time, rows 32 bytes past a multiple of
-// 128, at which the lanes of an operand's read meet different banks.
-constexpr int kPiece = 2048;
-constexpr int kPieceUnits = kPiece / (128 * kSteps);
-__host__ __device__ constexpr int pitch_of(int blocks) { return kPiece / blocks * 2 + 32; }   // bytes
+// Rows of x in LDS: piece_of() / kG elements of 16 kG tokens at a time, rows 32 bytes past a multiple of
+// 128, at which the lanes of an operand's read meet different banks.  Pieces of 1024 where a wave has more
+// than a piece's two turns anyway: a CU then holds four workgroups, not two (19 tokens of 64 experts
+// 66.4 -> 62.4 us with workgroups of four waves, which in turn leave fewer CUs idle at the end than eight);
+// 512 is no faster (63.1).
+__host__ __device__ constexpr int piece_of(int parts, int blocks) {       // elements, of one block's rows
+  return parts == 1 || parts * blocks == 2 ? 1024 : 2048;
+}
+__host__ __device__ constexpr int pitch_of(int parts, int blocks) {       // bytes
+  return piece_of(parts, blocks) / blocks * 2 + 32;
+}
 
 // First launch: a wave has 16 intermediate features of one expert (a gate tile and an up tile) for
 // all of its tokens, and of the steps of H every kS-th unit.  The workgroup's waves share the
@@ -250,7 +258,7 @@ __global__ __launch_bounds__(64 * kN, 4) void moe_up_kernel(const MoeArgs p, boo
   const Tiles gate(p.up_codes, p.up_scales, first, 1, steps), up(p.up_codes, p.up_scales, first + tiles, 1, steps);
   // Tokens 16 block0 .. 16 (block0 + kG) - 1 of the expert.
   auto pass = [&](int block0, auto blocks) {
-    constexpr int kG = decltype(blocks)::value, kUnits = kPieceUnits / kG, kPitch = pitch_of(kG);
+    constexpr int kG = decltype(blocks)::value, kPiece = piece_of(kS, kG), kUnits = kPiece / (128 * kSteps) / kG, kPitch = pitch_of(kS, kG);
     const int rows = min(n - 16 * block0, 16 * kG);
     // A piece's units of a wave, of which there is an even number (zeros past the end), so that the two that
     // are under way have registers of their own.
@@ -260,7 +268,7 @@ __global__ __launch_bounds__(64 * kN, 4) void moe_up_kernel(const MoeArgs p, boo
     } ring[2];
     int next_u0 = 0, next_turn = 0;                  // what is asked for next
     auto ask = [&](Both& w) {
-      const int u = next_u0 + next_turn * kS + part;
+      const int turn = next_turn * kS + part, u = turn < kUnits ? next_u0 + turn : units;
       w.gate.load(gate, u);
       w.up.load(up, u);
       if (++next_turn == turns(next_u0)) {
@@ -564,11 +572,12 @@ MoePlan plan_moe_layer(const MoeArgs& p, int num_cus) {
   MoePlan c;
   c.slots = std::min(p.E, p.M * p.k);
   c.by_expert = c.slots == p.E;
-  // The first launch: a wave a tile, or two or four where those would be few.  us of the whole call, four /
-  // two / one (128 experts, eight a token, of 2048 -> 768): one token 14.6 / 15.1 / 18.0, 2 18.3 / 18.4 / 20.8,
-  // 4 26.4 / 25.3 / 25.4, 8 40.5 / 37.0 / 37.1, 16 64.0 / 52.6 / 48.6, 64 104 / 82 / 69; 64 experts, six a token,
-  // of 2560 -> 1408: one 17.3 / 18.5 / 21.2, 3 31.1 / 28.8 / 29.3, 19 84.5 / 69.0 / 66.4.
-  const int64_t waves = static_cast<int64_t>(p.I / 16) * c.slots;
+  // The first launch: a wave a tile, or two or four where those would be few, fewer where a wave has
+  // more to compute.  us of the whole call, four / two / one (128 experts, eight a token, of 2048 -> 768):
+  // one token 14.6 / 15.3 / 16.6, 3 22.5 / 22.0 / 23.1, 8 40.6 / 37.6 / 37.4, 16 64.2 / 49.2 / 45.5, 64 104 / 84 / 70;
+  // 64 experts, six a token, of 2560 -> 1408: 2 24.0 / 24.1 / 26.4, 5 38.3 / 35.9 / 36.9, 19 85.1 / 70.2 / 62.4;
+  // 64 tokens of 2048 -> 1408: two of 8 experts 33.0 / 30.6 / 33.5, four of 16 51.0 / 42.9 / 39.0.
+  const int64_t waves = static_cast<int64_t>(p.I / 16) * c.slots * (p.M <= 16 ? 1 : 3);
   c.parts = waves <= 4 * num_cus ? 4 : waves <= 12 * num_cus ? 2 : 1;
   // The second: two tiles a workgroup where their number is even, so that the activations are loaded for
   // two, and a workgroup a CU, of which a wave has three steps at least.  us, two tiles and four
@@ -595,14 +604,14 @@ hipError_t launch_moe_layer(const MoePlan& c, const MoeArgs& p, void* workspace,
   const int most = most_items(c, p);
   const Table table{ints, ints + 4 + 16 * most, ints + 4 + 17 * most, ints + 4};
   float* parts = reinterpret_cast<float*>(at += table_bytes(c, p));
-  const int rows = p.M <= 16 ? p.M * pitch_of(1) : std::max(16 * pitch_of(1), 32 * pitch_of(2));
   auto up = [&](auto kernel, int kN, int kS) {
+    const int rows = p.M <= 16 ? p.M * pitch_of(kS, 1) : std::max(16 * pitch_of(kS, 1), 32 * pitch_of(kS, 2));
     const int lds = std::max(rows + (kS > 1 ? kN * 2 * 64 * 16 : 0), std::max(routing_bytes(p.M, p.k), 4 * p.E));
     const int tiles = kN / kS;
     kernel<<<dim3((p.I / 16 + tiles - 1) / tiles + 1, c.slots), 64 * kN, lds, stream>>>(p, c.by_expert, rows, hidden, table);
     return hipGetLastError();
   };
-  const hipError_t e = c.parts == 1   ? up(LargeLds<&moe_up_kernel<8, 1>>::kernel(), 8, 1)
+  const hipError_t e = c.parts == 1   ? up(LargeLds<&moe_up_kernel<4, 1>>::kernel(), 4, 1)
                        : c.parts == 2 ? up(LargeLds<&moe_up_kernel<4, 2>>::kernel(), 4, 2)
                                       : up(LargeLds<&moe_up_kernel<4, 4>>::kernel(), 4, 4);
   if (e != hipSuccess) return e;
