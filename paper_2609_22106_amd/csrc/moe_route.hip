@@ -14,7 +14,8 @@
 // takes four times as long: 8192 tokens of 128 experts 53 us).  Few tokens: a workgroup has 16 of them
 // and 16 experts, and its waves share H, so that W is read by as many CUs as possible.  The last
 // one of a block of tokens to arrive reads the block's logits back.  Many: a workgroup has 32 tokens and
-// all experts, in two stages of LDS.  Choosing, a token has 16 lanes (or a wave).
+// all experts, in two stages of LDS, or of many experts a group of 128.  Choosing, a token has 16 lanes (or a
+// wave).
 //
 // Bounds.  One token of 128 experts, H = 2048, 6.6 us: launch 2, one trip to memory and the product 2,
 // arrival 1, choosing 1.5.  8192 of them 16.8 us: their bytes are 6.4, but one workgroup a CU passes 640 KB
@@ -328,13 +329,13 @@ __global__ __launch_bounds__(kThreads) void route_few_kernel(const RouteArgs p, 
     choose_rows<kBias>(p, token0, count, [&](int r, int e) { return arrived_logit(p, parts, token0 - first + r, e); });
 }
 
-// 32 tokens and all experts, 32 kE at a time; wave (g, part) has 32 of those, all tokens and 64 elements
-// of every chunk of H.  Chunks come by way of registers, kAhead of them under way, into two stages of
-// LDS.
+// 32 tokens and all experts, 32 kE at a time (kSplit: the grid's 32 kE); wave (g, part) has 32 of those, all
+// tokens and 64 elements of every chunk of H.  Chunks come by way of registers, kAhead of them under way,
+// into two stages of LDS.
 __host__ __device__ inline int logits_pitch(int E, int kE) { return (E + 32 * kE - 1) / (32 * kE) * 32 * kE + 4; }
 
-template <int kE, bool kBias>
-__global__ __launch_bounds__(kThreads, 2) void route_many_kernel(const RouteArgs p) {
+template <int kE, bool kBias, bool kSplit>
+__global__ __launch_bounds__(kThreads, 2) void route_many_kernel(const RouteArgs p, float* parts, uint32_t* arrived) {
   constexpr int kParts = kWaves / kE, kChunk = 64 * kParts, kPitch = pitch_of(kChunk);
   constexpr int kRows = 32 + 32 * kE, kOctets = kChunk / 8, kEach = kThreads / kOctets;      // rows a pass
   constexpr int kLoads = kRows / kEach, kAhead = kE == 4 ? 4 : kE == 2 ? 3 : 2;
@@ -350,7 +351,7 @@ __global__ __launch_bounds__(kThreads, 2) void route_many_kernel(const RouteArgs
 
   const int octet = tid % kOctets, row = tid / kOctets;
   const int part = wave / kE, g = wave % kE;
-  for (int e0 = 0; e0 < p.E; e0 += 32 * kE) {
+  for (int e0 = kSplit ? static_cast<int>(blockIdx.y) * 32 * kE : 0; e0 < p.E; e0 += 32 * kE) {
     const uint16_t* from[kLoads];                // rows past the end: the last one's again, not stored
 #pragma unroll
     for (int i = 0; i < kLoads; ++i) {
@@ -412,6 +413,16 @@ __global__ __launch_bounds__(kThreads, 2) void route_many_kernel(const RouteArgs
       for (int t = 0; t < 2; ++t)
         *reinterpret_cast<f32x4*>(sums + (part * 32 + 16 * t + c) * kSums + 32 * g + 16 * m + 4 * q) = acc[m][t];
     __syncthreads();
+    if constexpr (kSplit) {
+      auto sum = [&](int r, int e) {
+        float l = sums[r * kSums + e];
+#pragma unroll
+        for (int v = 1; v < kParts; ++v) l += sums[(v * 32 + r) * kSums + e];
+        return l;
+      };
+      if (!arrive(p, parts, arrived + blockIdx.x, token0, count, e0, 32 * kE, static_cast<int>(gridDim.y), sum)) return;
+      break;
+    }
     for (int i = tid; i < 32 * 8 * kE; i += kThreads) {
       const int r = i / (8 * kE), e = i % (8 * kE) * 4;
       f32x4 l = *reinterpret_cast<const f32x4*>(sums + r * kSums + e);
@@ -421,7 +432,9 @@ __global__ __launch_bounds__(kThreads, 2) void route_many_kernel(const RouteArgs
     }
   }
   __syncthreads();
-  choose_rows<kBias>(p, token0, count, [&](int r, int e) { return logits[r * pitch + e]; });
+  choose_rows<kBias>(p, token0, count, [&](int r, int e) {
+    return kSplit ? arrived_logit(p, parts, token0 + r, e) : logits[r * pitch + e];
+  });
 }
 
 // Experts past which a block's logits do not fit beside the stages (512: 158 of 160 KB), and tokens in a
@@ -434,36 +447,47 @@ static_assert(kMaxFewTokens / 16 <= static_cast<int>(kWorkspaceStateBytes / 4), 
 
 RoutePlan plan_moe_route(int M, int E, int H, int num_cus) {
   RoutePlan c;
-  // A workgroup for 16 experts while there are no more than two a CU; the other kernel's time grows with
-  // the groups of 128 experts that its workgroups take in turn.  us, this one / the other: 128 experts
+  // A workgroup for 16 experts while there are no more than two a CU, or four past 128 experts, where the
+  // other kernel's workgroups take two groups of them in turn.  us, this one / the other: 128 experts
   // (H = 2048) 600 tokens 12.1 / 15.1, 1024 12.9 / 15.1, 2000 23.3 / 15.2; 64 (2560) 1000 tokens 10.4 / 14.0,
-  // 2048 13.0 / 14.4, 4000 22.9 / 13.2; 250 (1024) 700 tokens 16.3 / 18.6, 1000 20.4 / 18.9, 1537 27.6 / 18.9;
-  // 512 (2048) 800 tokens 38.0 / 51.9, 1100 50.5 / 51.9, 2000 80.8 / 51.8.
+  // 2048 13.0 / 14.4, 4000 22.9 / 13.2; 250 (1024) 700 tokens 16.3 / 18.6, 1000 20.4 / 18.9, 1537 27.6 / 18.9.
   const int64_t few = (static_cast<int64_t>(M) + 15) / 16 * ((E + 15) / 16);
-  if (E <= kMaxManyExperts && few > 2 * num_cus * ((E + 127) / 128)) c.groups = E > 64 ? 4 : E > 32 ? 2 : 1;
+  if (E > kMaxManyExperts || few <= (E > 128 ? 4 : 2) * num_cus) return c;
+  c.groups = E > 64 ? 4 : E > 32 ? 2 : 1;
+  // Three and four groups of a block go to workgroups of their own while those are at most two a CU, and
+  // meet in the workspace.  us, 16 experts / groups apart / groups in turn (H = 2048): 512 experts 400 tokens
+  // 27.4 / 27.9 / 51.9, 1100 50.7 / 30.2 / 52.0, 4096 130 / 44.7 / 52.2, 8192 257 / 72.5 / 54.4; 384 and a bias 600
+  // tokens 38.9 / 41.2 / 54.9, 1000 50.7 / 40.6 / 55.2.  Two groups gain less than the room for all logits
+  // is worth (250 experts, 4096 tokens 70.6 / 29.7 / 33.5).
+  const int64_t apart = (static_cast<int64_t>(M) + 31) / 32 * ((E + 127) / 128);
+  c.split = E > 256 && apart <= 2 * num_cus;
   return c;
 }
 
 size_t route_workspace_bytes(const RoutePlan& c, int M, int E) {
-  return c.groups || E <= 16 ? 0 : kWorkspaceStateBytes + static_cast<size_t>(std::min(M, kMaxFewTokens)) * E * 4;
+  if (c.groups ? !c.split : E <= 16) return 0;
+  return kWorkspaceStateBytes + static_cast<size_t>(c.split ? M : std::min(M, kMaxFewTokens)) * E * 4;
 }
 
 hipError_t launch_moe_route(const RoutePlan& c, const RouteArgs& p, void* workspace, hipStream_t stream) {
+  uint32_t* const arrived = static_cast<uint32_t*>(workspace);
+  float* const parts = workspace ? reinterpret_cast<float*>(arrived + kWorkspaceStateBytes / 4) : nullptr;
   auto many = [&](auto kernel, int kE) {
-    const int lds = stages_bytes(kE) + 32 * logits_pitch(p.E, kE) * 4;
-    kernel<<<(p.M + 31) / 32, kThreads, lds, stream>>>(p);
+    const int lds = stages_bytes(kE) + (c.split ? 0 : 32 * logits_pitch(p.E, kE) * 4);
+    const int apart = c.split ? (p.E + 32 * kE - 1) / (32 * kE) : 1;
+    kernel<<<dim3((p.M + 31) / 32, apart), kThreads, lds, stream>>>(p, parts, arrived);
     return hipGetLastError();
   };
   auto go = [&](auto bias) {
     constexpr bool kBias = decltype(bias)::value;
-    if (c.groups == 4) return many(LargeLds<&route_many_kernel<4, kBias>>::kernel(), 4);
-    if (c.groups == 2) return many(LargeLds<&route_many_kernel<2, kBias>>::kernel(), 2);
-    if (c.groups == 1) return many(LargeLds<&route_many_kernel<1, kBias>>::kernel(), 1);
+    if (c.split) return many(LargeLds<&route_many_kernel<4, kBias, true>>::kernel(), 4);
+    if (c.groups == 4) return many(LargeLds<&route_many_kernel<4, kBias, false>>::kernel(), 4);
+    if (c.groups == 2) return many(LargeLds<&route_many_kernel<2, kBias, false>>::kernel(), 2);
+    if (c.groups == 1) return many(LargeLds<&route_many_kernel<1, kBias, false>>::kernel(), 1);
     const int tiles = (p.E + 15) / 16, most = tiles > 1 ? kMaxFewTokens : p.M;
-    float* const parts = tiles > 1 ? reinterpret_cast<float*>(static_cast<char*>(workspace) + kWorkspaceStateBytes) : nullptr;
     for (int first = 0; first < p.M; first += most) {
       route_few_kernel<kBias><<<dim3((std::min(p.M - first, most) + 15) / 16, tiles), kThreads, 0, stream>>>(
-          p, first, parts, static_cast<uint32_t*>(workspace));
+          p, first, parts, arrived);
       const hipError_t e = hipGetLastError();
       if (e != hipSuccess) return e;
     }

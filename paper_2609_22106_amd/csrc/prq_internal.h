@@ -288,10 +288,11 @@ struct BlockNormArgs {
 hipError_t launch_block_norm(const BlockNormArgs& p, bool y_bf16, bool r_bf16, hipStream_t stream);
 
 // moe_route.hip.  Groups of 32 experts at a time of a workgroup with 32 tokens, or 0: a workgroup 16
-// tokens and 16 experts, of which the last one of a block of tokens chooses (workspace: the state head,
-// then the logits).
+// tokens and 16 experts.  There and where `split` is set the last workgroup of a block of tokens chooses
+// (workspace: the state head, then the logits).
 struct RoutePlan {
   int groups = 0;
+  bool split = false;                                // no workgroup takes all experts
 };
 struct RouteArgs {
   const uint16_t *x, *w;

@@ -68,7 +68,8 @@ def test_matches_oracle(M, E, k, H, sigmoid, renormalize):
 
 
 @pytest.mark.parametrize("M,E,k,H", [(2, 257, 8, 64), (9, 300, 31, 64), (40, 512, 8, 72), (1300, 300, 32, 16),
-                                     (1150, 257, 3, 136), (8200, 520, 8, 8)])
+                                     (1150, 257, 3, 136), (8200, 520, 8, 8), (4096, 512, 2, 8), (4099, 500, 8, 24),
+                                     (5470, 300, 4, 16)])
 @pytest.mark.parametrize("sigmoid", [False, True])
 def test_more_experts_than_a_group(M, E, k, H, sigmoid):
     """Past 256 experts a token has 32 keys a lane, past 512 a wave; past 8192 tokens of those, two launches."""
