@@ -76,14 +76,14 @@ __device__ __forceinline__ float row_sum(float x, float* sh) {
     const int wave = static_cast<int>(threadIdx.x) >> 6;
     if ((threadIdx.x & 63) == 0) sh[wave] = x;
     __syncthreads();
-    x = (sh[0] + sh[1]) + (sh[2] + sh[3]);
+    x = kLanes == kThreads ? (sh[0] + sh[1]) + (sh[2] + sh[3]) : sh[wave & 2] + sh[wave | 1];
   }
   return x;
 }
 
 __device__ __forceinline__ float dot4(f32x4 x) { return (x[0] * x[0] + x[1] * x[1]) + (x[2] * x[2] + x[3] * x[3]); }
 
-// kLanes lanes a row (a wave or the workgroup), kU quadruples a lane.  kOnce: what is more than the
+// kLanes lanes a row (a wave, two or the workgroup), kU quadruples a lane.  kOnce: what is more than the
 // caches keep is loaded and stored past them.
 template <typename Y, typename R, int kLanes, int kU, bool kOnce>
 __global__ __launch_bounds__(kThreads) void block_norm_kernel(const BlockNormArgs p) {
@@ -91,8 +91,11 @@ __global__ __launch_bounds__(kThreads) void block_norm_kernel(const BlockNormArg
   constexpr bool kEarly = kU <= 4;              // weights and gate in registers from the start
   __shared__ float sh[2][4];
   const int lane = static_cast<int>(threadIdx.x) % kLanes;
-  const int64_t row = static_cast<int64_t>(blockIdx.x) * kRows + static_cast<int>(threadIdx.x) / kLanes;
-  if (row >= p.M) return;                       // a whole wave, and only where a wave is a row
+  // Past the last row: nothing to wait for where a wave is a row, else that row again, not stored.
+  const int64_t own = static_cast<int64_t>(blockIdx.x) * kRows + static_cast<int>(threadIdx.x) / kLanes;
+  if (kLanes == 64 && own >= p.M) return;
+  const int64_t row = min(own, p.M - 1);
+  const bool live = own < p.M;
   const Y* y = static_cast<const Y*>(p.y);
   const R* r = static_cast<const R*>(p.residual);
   R* r_out = static_cast<R*>(p.residual_out);
@@ -149,14 +152,14 @@ __global__ __launch_bounds__(kThreads) void block_norm_kernel(const BlockNormArg
 #pragma unroll
   for (int i = 0; i < kU; ++i) {
     x[i] = p.a * x[i] + p.b * u[i];
-    if (r_out && in(i)) store4<kOnce>(r_out, row * p.ld_ro + place(i), x[i]);
+    if (r_out && live && in(i)) store4<kOnce>(r_out, row * p.ld_ro + place(i), x[i]);
     if (in(i)) s += dot4(x[i]);
   }
   if (!p.pre) return;
   const float inv = 1.0f / sqrtf(row_sum<kLanes>(s, sh[1]) / static_cast<float>(p.H) + p.eps);
 #pragma unroll
   for (int i = 0; i < kU; ++i)
-    if (in(i)) store4<kOnce>(p.h, row * p.ld_h + place(i), x[i] * inv * (pre[i].get(p.w_bf16) + p.offset));
+    if (live && in(i)) store4<kOnce>(p.h, row * p.ld_h + place(i), x[i] * inv * (pre[i].get(p.w_bf16) + p.offset));
 }
 
 template <typename Y, typename R, int kLanes, bool kOnce>
@@ -169,8 +172,8 @@ void launch(const BlockNormArgs& p, hipStream_t stream) {
   };
   if (per <= 1) go(std::integral_constant<int, 1>{});
   else if (per <= 2) go(std::integral_constant<int, 2>{});
-  else if constexpr (kLanes == kThreads) {
-    if (per <= 3) go(std::integral_constant<int, 3>{});
+  else if constexpr (kLanes > 64) {
+    if (per <= 3 || kLanes < kThreads) go(std::integral_constant<int, 3>{});
     else if (per <= 4) go(std::integral_constant<int, 4>{});
     else if (per <= 8) go(std::integral_constant<int, 8>{});
     else go(std::integral_constant<int, 16>{});
@@ -182,8 +185,10 @@ void launch(const BlockNormArgs& p, hipStream_t stream) {
 hipError_t launch_block_norm(const BlockNormArgs& p, bool y_bf16, bool r_bf16, hipStream_t stream) {
   // A wave a row up to 512 elements, else the workgroup: few quadruples a lane beat rows without a
   // barrier (us, a wave / the workgroup: 61 rows of 2560 9.6 / 4.4, 1537 of 1056 8.7 / 7.6, 8192 of 2560
-  // in float32 71 / 52).
-  const bool waves = p.H <= 512;
+  // in float32 71 / 52).  Many rows of up to 1536, three quadruples a lane, by half a workgroup each (the
+  // workgroup / half: 512 rows of 1024 2.9 / 3.0, 1537 of 1056 6.9 / 6.35, 4096 of 1024 9.7 / 8.5, 20000 38 / 31,
+  // 4096 of 1536 13.2 / 12.7; but of 2048 14.2 / 14.5).
+  const int lanes = p.H <= 512 ? 64 : p.H <= 1536 && p.M >= 1024 ? 128 : kThreads;
   // What does not fit the last cache (256 MB) goes past it: 8192 rows of 2560 in float32 51.8 -> 48.6 us;
   // less than that the next kernel finds there.
   const int64_t each = (p.y ? (y_bf16 ? 2 : 4) : 0) + (r_bf16 ? 2 : 4) * ((p.residual != nullptr) + (p.residual_out != nullptr)) + (p.h ? 2 : 0);
@@ -191,7 +196,8 @@ hipError_t launch_block_norm(const BlockNormArgs& p, bool y_bf16, bool r_bf16, h
   auto go = [&](auto y, auto r) {
     using Y = decltype(y);
     using R = decltype(r);
-    if (waves) once ? launch<Y, R, 64, true>(p, stream) : launch<Y, R, 64, false>(p, stream);
+    if (lanes == 64) once ? launch<Y, R, 64, true>(p, stream) : launch<Y, R, 64, false>(p, stream);
+    else if (lanes == 128) once ? launch<Y, R, 128, true>(p, stream) : launch<Y, R, 128, false>(p, stream);
     else once ? launch<Y, R, kThreads, true>(p, stream) : launch<Y, R, kThreads, false>(p, stream);
   };
   if (y_bf16) r_bf16 ? go(uint16_t{}, uint16_t{}) : go(uint16_t{}, float{});

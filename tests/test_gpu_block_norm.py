@@ -73,6 +73,19 @@ def test_matches_oracle(M, H, y_type, r_type, post, gates, index, w_type):
     _check(c, got, a=0.75, b=-0.5)
 
 
+@pytest.mark.parametrize("M,H,y_type,r_type,post,gates", [
+    (1024, 520, F32, BF16, True, 1), (1025, 1056, BF16, BF16, True, 7), (1601, 1536, F32, F32, True, 0),
+    (1023, 1536, BF16, F32, False, 0), (1027, 1544, F32, F32, True, 3), (3333, 1024, F32, F32, False, 0)])
+def test_rows_by_half_a_workgroup(M, H, y_type, r_type, post, gates):
+    """1024 rows and more of 513 to 1536 elements, and their neighbours, in place: the last row alone."""
+    say("block norm", M, H, y_type, r_type, post, gates)
+    c = _make(M, H, y_type, r_type, post, gates, M + H, index=gates > 1)
+    r0 = c["r"].clone()
+    got = _prq().prq_block_norm(c["y"], c["r"], c["pre"], post_weight=c["post"], gate=c["gate"], gate_index=c["index"])
+    assert got[1] is c["r"]
+    _check(c, got, r0=r0)
+
+
 def test_in_place_and_offset_weights():
     c = _make(9, 264, F32, BF16, True, 0, 1)
     r0 = c["r"].clone()
