@@ -2,6 +2,10 @@
 // check, plans and workspace sizes.
 #include <cmath>
 #include <cstdint>
+#include <cstring>
+#include <tuple>
+#include <type_traits>
+#include <utility>
 
 #include <hip/hip_runtime_api.h>
 
@@ -53,6 +57,34 @@ prq::MoeArgs layer_sizes(int32_t M, int32_t k, int32_t E, int32_t H, int32_t I, 
   prq::MoeArgs p{};
   p.M = M, p.k = k, p.E = E, p.H = H, p.I = I, p.k_tail = k_tail, p.N = N;
   return p;
+}
+
+// One argument of a record as its parameter's type; fits: an integer lies in that type's range.
+template <typename T>
+T argument(uint64_t raw, bool& fits) {
+  if constexpr (std::is_pointer_v<T>) {
+    return reinterpret_cast<T>(static_cast<uintptr_t>(raw));
+  } else if constexpr (std::is_floating_point_v<T>) {
+    double v;
+    std::memcpy(&v, &raw, sizeof(v));
+    return static_cast<T>(v);
+  } else {
+    if (sizeof(T) < 8 && static_cast<int64_t>(raw) != static_cast<int64_t>(static_cast<T>(raw))) fits = false;
+    return static_cast<T>(raw);
+  }
+}
+template <typename... T, size_t... kAt>
+int call_record(int (*call)(T...), const void* record, std::index_sequence<kAt...>) {
+  uint64_t raw[sizeof...(T)];
+  if (!record) return PRQ_EINVAL;
+  std::memcpy(raw, record, sizeof(raw));
+  bool fits = true;
+  const std::tuple<T...> arguments{argument<T>(raw[kAt], fits)...};
+  return fits ? call(std::get<kAt>(arguments)...) : PRQ_EINVAL;
+}
+template <typename... T>
+int call_record(int (*call)(T...), const void* record) {
+  return call_record(call, record, std::index_sequence_for<T...>{});
 }
 
 }  // namespace
@@ -164,5 +196,9 @@ int prq_moe_layer(const void* x_bf16, int64_t ld_x, int32_t M, const int32_t* id
   p.ld_out = ld_out;
   return launch_status(prq::launch_moe_layer(plan, p, workspace, stream));
 }
+
+int prq_block_norm_record(const void* record) { return call_record(prq_block_norm, record); }
+int prq_moe_route_record(const void* record) { return call_record(prq_moe_route, record); }
+int prq_moe_layer_record(const void* record) { return call_record(prq_moe_layer, record); }
 
 }  // extern "C"

@@ -12,6 +12,7 @@ from __future__ import annotations
 import ctypes
 import os
 import re
+import struct
 
 import numpy as np
 import torch  # noqa: F401  (loads the HIP runtime the library binds to)
@@ -101,15 +102,27 @@ _lora_ex = _decl("prq_lora_ex", ctypes.c_int,
                   _p, _sz, _p])
 
 ROUTE_SCORINGS = {"softmax": 0, "sigmoid": 1}
-_block_norm = _decl("prq_block_norm", ctypes.c_int,
-                    [_p, _i64, _i32, _p, _i64, _i32, _i32, _i32, _p, _p, _i32, _f32, _p, _i64, _i32, _i32, _p, _f32,
-                     _f32, _f32, _p, _i64, _p, _i64, _p])
+
+
+def _record(name, argtypes):
+    """(pack, call) of prq_<name>_record: call(pack(*arguments)), with 0 for no pointer."""
+    kinds = {_p: "Q", _sz: "Q", _i32: "q", _i64: "q", _f32: "d"}
+    return (struct.Struct("=" + "".join(kinds[t] for t in argtypes)).pack,
+            _decl(name + "_record", ctypes.c_int, [ctypes.c_char_p]))
+
+
+_block_norm_types = [_p, _i64, _i32, _p, _i64, _i32, _i32, _i32, _p, _p, _i32, _f32, _p, _i64, _i32, _i32, _p, _f32,
+                     _f32, _f32, _p, _i64, _p, _i64, _p]
+_block_norm = _decl("prq_block_norm", ctypes.c_int, _block_norm_types)
+_block_norm_pack, _block_norm_call = _record("prq_block_norm", _block_norm_types)
 _route_ws = _decl("prq_moe_route_workspace_bytes", _sz, [_i32, _i32, _i32])
-_route = _decl("prq_moe_route", ctypes.c_int,
-               [_p, _i64, _i32, _i32, _p, _i64, _i32, _i32, _i32, _p, _i32, _f32, _p, _p, _p, _i64, _p, _sz, _p])
+_route_types = [_p, _i64, _i32, _i32, _p, _i64, _i32, _i32, _i32, _p, _i32, _f32, _p, _p, _p, _i64, _p, _sz, _p]
+_route = _decl("prq_moe_route", ctypes.c_int, _route_types)
+_route_pack, _route_call = _record("prq_moe_route", _route_types)
 _moe_ws = _decl("prq_moe_layer_workspace_bytes", _sz, [_i32, _i32, _i32, _i32, _i32, _i32, _i32])
-_moe = _decl("prq_moe_layer", ctypes.c_int,
-             [_p, _i64, _i32, _p, _p, _i32, _p, _p, _p, _p, _i32, _i32, _i32, _i32, _i32, _p, _i64, _p, _sz, _p])
+_moe_types = [_p, _i64, _i32, _p, _p, _i32, _p, _p, _p, _p, _i32, _i32, _i32, _i32, _i32, _p, _i64, _p, _sz, _p]
+_moe = _decl("prq_moe_layer", ctypes.c_int, _moe_types)
+_moe_pack, _moe_call = _record("prq_moe_layer", _moe_types)
 
 
 class PRQError(RuntimeError):
@@ -162,6 +175,13 @@ def _stream_of_call(stream):
     if stream is None and _raw_stream is not None and _cur_device is not None:
         return _raw_stream(_cur_device())
     return _stream(stream)
+
+
+def _stream_at(stream):
+    """_stream_of_call as a number."""
+    if stream is not None:
+        return stream.cuda_stream
+    return _raw_stream(_cur_device()) if _raw_stream is not None and _cur_device is not None else _stream(None).value or 0
 
 
 def _alloc(make, shape, dtype, device, stream, kept=True):
@@ -988,7 +1008,7 @@ def prq_block_norm(y, residual, pre_weight=None, post_weight=None, gate=None, ga
         raise ValueError("post_weight and gate need y")
     M, H = shape = lead.shape
     d = _device_of(lead, "residual" if y is None else "y")
-    y_at = r_at = ro_at = h_at = post = pre = gate_at = index_at = None
+    y_at = r_at = ro_at = h_at = post = pre = gate_at = index_at = 0          # (no pointer)
     ld_y = ld_r = ld_ro = ld_h = ld_gate = w_kind = gate_rows = gate_kind = 0
     y_kind = r_kind = lead.dtype
     if y is not None:
@@ -999,10 +1019,11 @@ def prq_block_norm(y, residual, pre_weight=None, post_weight=None, gate=None, ga
         r_at, r_kind = residual.data_ptr(), residual.dtype
         if residual_out is None and (y is not None or residual_scale != 1.0):
             residual_out = residual
+    stores = residual_out is not None
     if residual_out is residual:
         ro_at, ld_ro = r_at, ld_r
         if y is None and residual_scale == 1.0:      # (nothing to change)
-            ro_at = None
+            ro_at, stores = 0, False
     elif residual_out is not None:
         ld_ro = H if _here(residual_out, r_kind, shape, d) else _matrix(residual_out, "residual_out", (r_kind,), M, H, d)
         ro_at = residual_out.data_ptr()
@@ -1010,7 +1031,7 @@ def prq_block_norm(y, residual, pre_weight=None, post_weight=None, gate=None, ga
         pre, w_kind = _norm_weight(pre_weight, "pre_weight", H, d)
     if post_weight is not None:
         post, kind = _norm_weight(post_weight, "post_weight", H, d)
-        if pre is not None and kind != w_kind:
+        if pre_weight is not None and kind != w_kind:
             raise ValueError("post_weight and pre_weight must have one type")
         w_kind = kind
     if gate is not None:
@@ -1024,17 +1045,18 @@ def prq_block_norm(y, residual, pre_weight=None, post_weight=None, gate=None, ga
             index_at = gate_index.data_ptr()
     elif gate_index is not None:
         raise ValueError("gate_index needs a gate")
-    if pre is not None:
+    if pre_weight is not None:
         if out is None:
             out = _output(None, "out", (M, H), _BF16, lead, stream)
         ld_h = H if _here(out, _BF16, shape, d) else _matrix(out, "out", (_BF16,), M, H, d)
         h_at = out.data_ptr()
     elif out is not None:
         raise ValueError("out needs pre_weight")
-    if h_at is not None or ro_at is not None:
-        st = _block_norm(y_at, ld_y, 1 if y_kind is _BF16 else 0, r_at, ld_r, 1 if r_kind is _BF16 else 0, M, H, post, pre,
-                         w_kind, weight_offset, gate_at, ld_gate, gate_kind, gate_rows, index_at, eps, residual_scale,
-                         block_scale, ro_at, ld_ro, h_at, ld_h, _stream_of_call(stream))
+    if stores or pre_weight is not None:
+        st = _block_norm_call(_block_norm_pack(
+            y_at, ld_y, 1 if y_kind is _BF16 else 0, r_at, ld_r, 1 if r_kind is _BF16 else 0, M, H, post, pre, w_kind,
+            weight_offset, gate_at, ld_gate, gate_kind, gate_rows, index_at, eps, residual_scale, block_scale, ro_at, ld_ro,
+            h_at, ld_h, _stream_at(stream)))
         if st:
             _check(st, "prq_block_norm")
     return out, residual if residual_out is None else residual_out
@@ -1054,6 +1076,10 @@ def _state_workspace(workspace, need, like, stream, d):
         _on_gpu(workspace=workspace)
     _on_device(workspace, "workspace", d)
     return workspace
+
+
+def _extent(workspace):
+    return (0, 0) if workspace is None else (workspace.data_ptr(), workspace.numel())
 
 
 def prq_moe_route(x, W, k, scoring="softmax", bias=None, renormalize=True, scale=1.0, ids=None, weights=None,
@@ -1084,9 +1110,10 @@ def prq_moe_route(x, W, k, scoring="softmax", bias=None, renormalize=True, scale
     _exact(weights, "weights", _F32, (M, k), d)
     ld_l = _matrix(logits, "logits", (_F32,), M, E, d) if logits is not None else 0
     workspace = _state_workspace(workspace, lambda: _route_ws(M, E, H), x, stream, d)
-    st = _route(x.data_ptr(), ld_x, M, H, W.data_ptr(), ld_w, E, k, ROUTE_SCORINGS[scoring], _ptr(bias),
-                1 if renormalize else 0, scale, ids.data_ptr(), weights.data_ptr(), _ptr(logits), ld_l, _ptr(workspace),
-                0 if workspace is None else workspace.numel(), _stream_of_call(stream))
+    st = _route_call(_route_pack(
+        x.data_ptr(), ld_x, M, H, W.data_ptr(), ld_w, E, k, ROUTE_SCORINGS[scoring], 0 if bias is None else bias.data_ptr(),
+        1 if renormalize else 0, scale, ids.data_ptr(), weights.data_ptr(), 0 if logits is None else logits.data_ptr(), ld_l,
+        *_extent(workspace), _stream_at(stream)))
     if st:
         _check(st, "prq_moe_route")
     return ids, weights
@@ -1132,9 +1159,9 @@ def prq_moe_layer(x, ids, weights, gate_up, down, k_tail=0, out=None, workspace=
         out = _output(None, "out", (M, N), _BF16, x, stream)
     ld_out = N if _here(out, _BF16, (M, N), d) else _matrix(out, "out", (_BF16,), M, N, d)
     workspace = _state_workspace(workspace, lambda: _moe_ws(M, k, E, H, I, k_tail, N), x, stream, d)
-    st = _moe(x.data_ptr(), ld_x, M, ids.data_ptr(), weights.data_ptr(), k, up_at, up_scales_at, down_at, down_scales_at, E,
-              H, I, k_tail, N, out.data_ptr(), ld_out, _ptr(workspace), 0 if workspace is None else workspace.numel(),
-              _stream_of_call(stream))
+    st = _moe_call(_moe_pack(
+        x.data_ptr(), ld_x, M, ids.data_ptr(), weights.data_ptr(), k, up_at, up_scales_at, down_at, down_scales_at, E, H, I,
+        k_tail, N, out.data_ptr(), ld_out, *_extent(workspace), _stream_at(stream)))
     if st:
         _check(st, "prq_moe_layer")
     return out

@@ -113,6 +113,24 @@ def test_layer_refuses_before_touching_the_gpu(change, status):
     assert prq._moe(*{**LAYER, **change}.values()) == status
 
 
+@pytest.mark.parametrize("call,pack,arguments,changes", [
+    (prq._block_norm_call, prq._block_norm_pack, NORM,
+     [(dict(M=-1), EINVAL), (dict(eps=NAN), EINVAL), (dict(a=1e300), EINVAL), (dict(H=252), EALIGN), (dict(M=1 << 24), EUNSUP),
+      (dict(M=1 << 32), EINVAL), (dict(H=256 - (1 << 32)), EINVAL), (dict(M=0, y=None, r=None, h=None, r_out=None), 0)]),
+    (prq._route_call, prq._route_pack, ROUTE,
+     [(dict(k=0), EINVAL), (dict(scale=NAN), EINVAL), (dict(ld_x=260), EALIGN), (dict(E=1025), EUNSUP),
+      (dict(E=(1 << 32) + 32), EINVAL), (dict(M=0, x=None, ids=None, weights=None), 0)]),
+    (prq._moe_call, prq._moe_pack, LAYER,
+     [(dict(tail=-32), EINVAL), (dict(out=ODD), EALIGN), (dict(M=65), EUNSUP), (dict(M=1 << 33), EINVAL),
+      (dict(M=0, x=None, ids=None, out=None, ws=None), 0)])])
+def test_records_are_the_calls(call, pack, arguments, changes):
+    """The arguments in a record of 8 bytes each; integers past their parameter's range are refused, not cut."""
+    for change, status in changes:
+        values = [getattr(v, "value", v) or 0 for v in {**arguments, **change}.values()]      # (pointers as numbers)
+        assert call(pack(*values)) == status, change
+    assert call(None) == EINVAL
+
+
 def test_workspace_sizes():
     assert prq.prq_moe_route_workspace_bytes(-1, 8, 64) == prq.prq_moe_route_workspace_bytes(4, 8, 60) == 0
     assert prq.prq_moe_route_workspace_bytes(0, 128, 2048) == prq.prq_moe_route_workspace_bytes(4, 2000, 64) == 0
