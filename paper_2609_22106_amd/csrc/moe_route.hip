@@ -18,10 +18,10 @@
 // wave).
 //
 // Bounds.  One token of 128 experts, H = 2048, 6.6 us: launch 2, one trip to memory and the product 2,
-// arrival 1, choosing 1.5.  8192 of them 16.8 us: their bytes are 6.4, but one workgroup a CU passes 640 KB
-// through its LDS in 16 chunks at 0.45 us (20 TB/s over the card, most of it W from L2), behind a launch of
-// 3 and in front of 3 of choosing.  1537 tokens of 250 experts, H = 1024, 18.8 us: the same on 49 CUs with
-// two groups of experts.
+// arrival 1, choosing 1.5.  8192 of them 16.5 us: their bytes are 6.4, but one workgroup a CU loads 640 KB in
+// 16 chunks at 0.5 to 0.6 us (16 to 20 TB/s over the card, most of it W from L2; LDS is active a third of
+// the time, deeper rings change nothing), behind a launch of 3 and in front of 3 of choosing.  1537 tokens of
+// 250 experts, H = 1024, 19.6 us: the same on 49 CUs with two groups of experts.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
