@@ -646,7 +646,8 @@ int prq_moe_route(const void* x_bf16, int64_t ld_x, int32_t M, int32_t H, const 
  *   out[m] = sum_j weights[m, j] * Wdown_e [h_e ; last k_tail of h_e],   e = ids[m, j]
  * MXFP4 weights against bf16 activations: at so few rows the weights are the bytes, so the
  * activations are not quantized.  Sums are float32, in a fixed order (calls repeat bit for bit);
- * weights[m, j] h is rounded to bf16 once, and out once.  Two launches.
+ * weights[m, j] h is held to 2^-15 of it between the two launches (the sum of two bf16), and out is
+ * rounded once.
  *
  *   x        device [M, ld_x] bf16
  *   ids      device [M, k] int32; an entry outside [0, E) adds nothing (padding, an expert held

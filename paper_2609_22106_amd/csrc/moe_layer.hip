@@ -4,10 +4,10 @@
 // D (N x (I + k_tail)):
 //   h_e = SiLU(G_e x) * (U_e x),  SiLU(z) = z / (1 + exp(-z))
 //   y   = sum_j w_j D_{e_j} [h; the last k_tail of h again]
-// Sums are float32.  w h is rounded to bf16 between the launches (the operand of the second
-// product's matrix instructions), y to bf16 at the end: two roundings of 2^-9 relative, the second
-// of them the output's own.  A token that names an expert twice gets it with both weights; an id
-// outside [0, E) names none.
+// Sums are float32.  Between the launches w h is held in two bf16, its upper bits and the rest (the
+// operands of the second product's matrix instructions), which is off by less than 2^-15 of it; y is
+// rounded to bf16, by up to 2^-8, at the end.  A token that names an expert twice gets it with both
+// weights; an id outside [0, E) names none.
 //
 // The weights of the experts that are reached are most of the bytes, and what bounds both launches
 // where they are many: 64 tokens of 128 experts, eight a token, of 2048 -> 768 + 64 -> 2048, 292 MB in
@@ -24,7 +24,8 @@
 // A slot is an expert (its number), or where there are fewer pairs of a token and an expert than
 // experts a pair (its first occurrence), so that a launch of `slots` workgroups in y reaches every
 // expert that is named.  An expert's tokens are gathered into columns in ascending order, 16 to a
-// block.  The first launch finds them with a lane a token, and leaves the second a table.
+// block of the first launch and 8 or 16 to an item of the second.  The first launch finds them with a
+// lane a token, and leaves the second a table.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -42,22 +43,30 @@ constexpr int kMaxSplits = 8;                       // workgroups that share out
 constexpr int kSteps = 2;                            // K steps of 128 in a wave's unit
 
 // What the first launch leaves.  `hidden`: w h of the pairs, an expert's behind those of the lower
-// ones, its tokens 16 at a time: of n of them [octets][n][8] elements, the 16 octets of a K step in the
-// order in which a lane group's operands are loaded (octet_at), so that one load's lanes read one
-// stretch.  The table: the second launch's items, an expert's tokens 16 at a time, experts in
-// ascending order; of each the expert, its tokens in `hidden` (first 2^5 n), and the token of column i,
-// -1 past the last.  An expert that a token names twice may have an empty item.
+// ones, its tokens an item (8 or 16) at a time: of n of them [K steps][2][16][n][8] elements, the upper
+// bits of a K step's octets and then what is left (low_part), the octets in the order in which a lane
+// group's operands are loaded (octet_at), so that one load's lanes read one or two stretches.  The
+// table: the second launch's items, experts in ascending order; of each the expert, its tokens in
+// `hidden` (first 2^5 n), and the token of column i, -1 past the last.  An expert that a token names twice
+// may have an empty item.
 struct Table {
   int32_t* total;                                    // the number of items
   int32_t* experts;
   int32_t* rows;
-  int32_t* columns;                                  // [items][16]
+  int32_t* columns;                                  // [items][tokens of an item]
+  int shift;                                         // an item's tokens: 2^shift
 };
 
-// Elements of a row of `hidden`: whole K steps.
-__host__ __device__ constexpr int64_t hidden_pitch(int I) { return (I + 127) & ~127; }
-// Where octet o of a row stands: lane group q's j-th of a K step, which is octet 4 q + j of it, at 4 j + q.
-__device__ __forceinline__ int octet_at(int o) { return (o & ~15) | (o & 3) << 2 | (o >> 2 & 3); }
+// Elements of a pair's row of `hidden`: whole K steps, twice.
+__host__ __device__ constexpr int64_t hidden_pitch(int I) { return 2 * ((I + 127) & ~127); }
+// What is left of x without its lower 16 bits: 16 bits, of which bf16 keeps 8.  (A finite x has a finite upper
+// part; nothing is left of an infinity, where inf - inf would make it a NaN.)
+__device__ __forceinline__ float low_part(float x) {
+  return __builtin_isinf(x) ? 0.f : x - dev::bf16_hi(__float_as_uint(x));
+}
+// Where octet o of a row's upper bits stands: lane group q's j-th of a K step, which is octet 4 q + j of it, at
+// 4 j + q; the rest of it 16 further.
+__device__ __forceinline__ int octet_at(int o) { return (o & ~15) << 1 | (o & 3) << 2 | (o >> 2 & 3); }
 
 // A lane's 32 weights of a K step (the 16 bytes of an MXFP4 block, its E8M0 code) as the four
 // bf16 operands of the matrix instruction.
@@ -161,6 +170,7 @@ __device__ __forceinline__ void write_items(const MoeArgs& p, int slot, int e, i
                                             const Table& table, int* bins) {
   __shared__ int sums[2][kN];
   const int tid = static_cast<int>(threadIdx.x), lane = tid & 63, wave = tid >> 6;
+  const int whole = (1 << table.shift) - 1;
   __syncthreads();                                   // the routing has been read
   for (int i = tid; i < p.E; i += 64 * kN) bins[i] = 0;
   __syncthreads();
@@ -171,7 +181,7 @@ __device__ __forceinline__ void write_items(const MoeArgs& p, int slot, int e, i
   __syncthreads();
   int before = 0, all = 0;
   for (int i = tid; i < p.E; i += 64 * kN) {
-    const int items = (bins[i] + 15) >> 4;
+    const int items = (bins[i] + whole) >> table.shift;
     all += items;
     if (i < e) before += items;
   }
@@ -189,13 +199,13 @@ __device__ __forceinline__ void write_items(const MoeArgs& p, int slot, int e, i
   }
   if (slot == 0 && tid == 0) *table.total = all;
   if (wave || n == 0) return;
-  const int items = (bins[e] + 15) >> 4;
-  for (int i = lane; i < items * 16; i += 64) {
-    if (i % 16 == 0) {
-      table.experts[before + i / 16] = e;
-      table.rows[before + i / 16] = (pairs + i) << 5 | max(0, min(n - i, 16));
+  const int items = (bins[e] + whole) >> table.shift;
+  for (int i = lane; i < items << table.shift; i += 64) {
+    if ((i & whole) == 0) {
+      table.experts[before + (i >> table.shift)] = e;
+      table.rows[before + (i >> table.shift)] = (pairs + i) << 5 | max(0, min(n - i, whole + 1));
     }
-    table.columns[before * 16 + i] = i < 64 ? token : -1;
+    table.columns[(before << table.shift) + i] = i < 64 ? token : -1;
   }
 }
 
@@ -336,15 +346,18 @@ __global__ __launch_bounds__(64 * kN, 4) void moe_up_kernel(const MoeArgs p, boo
       }
       // column c's features 4 q .. 4 q + 3 of the tile
       const float w = __shfl(weight, 16 * (block0 + g) + c, 64);
-      const int columns = min(n - 16 * (block0 + g), 16);
-      if (c < columns && tile < tiles) {
+      const int row = 16 * (block0 + g) + c;
+      if (row < n && tile < tiles) {
         float h[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) h[i] = z[i] / (1.f + expf(-z[i])) * y[i] * w;
-        const dev::u32x2 v = {dev::pack_bf16(h[0], h[1]), dev::pack_bf16(h[2], h[3])};
-        uint16_t* to = hidden + (pairs + 16 * (block0 + g)) * hidden_pitch(p.I) +
-                       (octet_at(2 * tile + (q >> 1)) * columns + c) * 8 + 4 * (q & 1);
-        *reinterpret_cast<dev::u32x2*>(to) = v;
+        auto upper = [](float x, float y) { return __float_as_uint(x) >> 16 | (__float_as_uint(y) & 0xFFFF0000u); };
+        auto rest = [](float x, float y) { return dev::pack_bf16(low_part(x), low_part(y)); };
+        const int first = row >> table.shift << table.shift, columns = min(n - first, 1 << table.shift);
+        uint16_t* to = hidden + (pairs + first) * hidden_pitch(p.I) +
+                       (octet_at(2 * tile + (q >> 1)) * columns + row - first) * 8 + 4 * (q & 1);
+        *reinterpret_cast<dev::u32x2*>(to) = dev::u32x2{upper(h[0], h[1]), upper(h[2], h[3])};
+        *reinterpret_cast<dev::u32x2*>(to + 16 * 8 * columns) = dev::u32x2{rest(h[0], h[1]), rest(h[2], h[3])};
       }
     }
   };
@@ -363,23 +376,28 @@ constexpr int sums_pitch(int tiles) { return 16 * tiles + 4; }
 // An item's sums are added to its tokens' in LDS, of which each wave has its own.  The waves' sums are
 // added in their order, the workgroups' in theirs, by the one that arrives last.
 //
+// kBoth: an item has 8 tokens, whose upper bits are columns 0 to 7 of the operand and the rest columns 8
+// to 15, so that one load and one product serve both (16 tokens take two of each).
+//
 // A wave asks for the weights and activations of a step kAhead steps ahead.  The loop has loads
 // without conditions only (past the end, and of columns without a token, outside their buffers), so
 // that every wait counts exactly the loads behind it.
 constexpr int kWindow = 64;
 
-template <int kT, int kN, int kAhead>
-__global__ __launch_bounds__(64 * kN, 4) void moe_down_kernel(const MoeArgs p, const uint16_t* __restrict__ hidden,
-                                                               const Table table, int most, float* parts,
-                                                               uint32_t* arrived) {
+template <int kT, int kN, int kAhead, bool kBoth>
+__global__ __launch_bounds__(64 * kN, kBoth ? 4 : 2) void moe_down_kernel(const MoeArgs p,
+                                                                          const uint16_t* __restrict__ hidden,
+                                                                          const Table table, int most, float* parts,
+                                                                          uint32_t* arrived) {
   constexpr int kPitch = sums_pitch(kT), kRing = kAhead + 1;
+  constexpr int kItem = kBoth ? 8 : 16, kOperands = kBoth ? 1 : 2;
   extern __shared__ __align__(16) float own[];       // [kN][M][kPitch]
   __shared__ int sh_experts[kWindow], sh_rows[kWindow];
-  __shared__ int sh_columns[kWindow][16];
+  __shared__ int sh_columns[kWindow][kItem];
   __shared__ int sh_last;
   const int tid = static_cast<int>(threadIdx.x), lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int c = lane & 15, q = lane >> 4;
+  const int c = lane & 15, q = lane >> 4, token = c % kItem;           // of the item
   const int tile = static_cast<int>(blockIdx.x) * kT, splits = static_cast<int>(gridDim.y), part = static_cast<int>(blockIdx.y);
   const int K = p.I + p.k_tail, steps = (K + 127) >> 7, tiles = p.N >> 4;
   const auto rsrc = buffer(hidden, static_cast<int>(p.M * p.k * hidden_pitch(p.I) * 2));
@@ -388,16 +406,16 @@ __global__ __launch_bounds__(64 * kN, 4) void moe_down_kernel(const MoeArgs p, c
   // Item i of this workgroup is item part + splits i of all; the first window's are loaded before their
   // number is known.
   for (int item0 = 0;; item0 += kWindow) {
-    int expert = 0, rows = 0, column[kWindow * 16 / (64 * kN)];
+    int expert = 0, rows = 0, column[kWindow * kItem / (64 * kN)];
     const int at = part + splits * item0;
     if (tid < kWindow) {
       expert = table.experts[min(at + splits * tid, most - 1)];
       rows = table.rows[min(at + splits * tid, most - 1)];
     }
 #pragma unroll
-    for (int i = 0; i < kWindow * 16 / (64 * kN); ++i) {
+    for (int i = 0; i < kWindow * kItem / (64 * kN); ++i) {
       const int entry = tid + i * 64 * kN;
-      column[i] = table.columns[min(at + splits * (entry >> 4), most - 1) * 16 + (entry & 15)];
+      column[i] = table.columns[min(at + splits * (entry / kItem), most - 1) * kItem + entry % kItem];
     }
     const int total = *table.total;
     if (item0 == 0) {
@@ -412,9 +430,9 @@ __global__ __launch_bounds__(64 * kN, 4) void moe_down_kernel(const MoeArgs p, c
       sh_rows[tid] = rows;
     }
 #pragma unroll
-    for (int i = 0; i < kWindow * 16 / (64 * kN); ++i) {
+    for (int i = 0; i < kWindow * kItem / (64 * kN); ++i) {
       const int entry = tid + i * 64 * kN;
-      sh_columns[entry >> 4][entry & 15] = column[i];
+      sh_columns[entry / kItem][entry % kItem] = column[i];
     }
     __syncthreads();
 
@@ -436,22 +454,26 @@ __global__ __launch_bounds__(64 * kN, 4) void moe_down_kernel(const MoeArgs p, c
       struct Step {
         u32x4v codes[kT];
         uint32_t scales[kT];
-        u32x4v b[4];
+        u32x4v b[kOperands][4];
       } ring[kRing];
       auto ask = [&](Step& s) {
         int k = 128 * step + 32 * q;                 // the tail meets the last values again, zeros behind it
         const uint32_t past = u < n ? 0 : kOutside;
-        const bool in = k < K && c < columns && u < n;
+        const bool in = k < K && token < columns && u < n;
         if (k >= p.I) k -= p.k_tail;
-        const uint32_t at = in ? base + static_cast<uint32_t>((((k >> 7) * 16 + (k >> 5 & 3)) * columns + c) * 16) : kOutside;
+        const int slot = (k >> 7) * 32 + (k >> 5 & 3) + (kBoth && c >= kItem ? 16 : 0);
+        const uint32_t at = in ? base + static_cast<uint32_t>((slot * columns + token) * 16) : kOutside;
 #pragma unroll
         for (int t = 0; t < kT; ++t) {
           s.codes[t] = down.code(t, step, past);
           s.scales[t] = down.scale(t, step, past);
         }
 #pragma unroll
-        for (int j = 0; j < 4; ++j)
-          s.b[j] = __builtin_bit_cast(u32x4v, __builtin_amdgcn_raw_buffer_load_b128(rsrc, at, 64 * j * columns, 0));
+        for (int h = 0; h < kOperands; ++h)
+#pragma unroll
+          for (int j = 0; j < 4; ++j)
+            s.b[h][j] = __builtin_bit_cast(
+                u32x4v, __builtin_amdgcn_raw_buffer_load_b128(rsrc, at, (256 * h + 64 * j) * columns, 0));
         if (++u < n && ++step == steps) {
           step = 0;
           ++item;
@@ -459,25 +481,30 @@ __global__ __launch_bounds__(64 * kN, 4) void moe_down_kernel(const MoeArgs p, c
         }
       };
       f32x4 acc[kT] = {};
-      int now = step, now_item = item, now_column = sh_columns[item][c];    // of the step that is computed
+      int now = step, now_item = item, now_column = sh_columns[item][token];    // of the step that is computed
       auto compute = [&](const Step& s, bool last) {
 #pragma unroll
         for (int t = 0; t < kT; ++t) {
           u32x4v a[4];
           to_bf16(s.codes[t], s.scales[t] >> (8 * (now & 3)) & 255u, a);
 #pragma unroll
-          for (int j = 0; j < 4; ++j) acc[t] = dev::mfma_bf16(a[j], s.b[j], acc[t]);
+          for (int h = 0; h < kOperands; ++h)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) acc[t] = dev::mfma_bf16(a[j], s.b[h][j], acc[t]);
         }
         if (++now == steps || last) {                // the item's sums are complete here
           now = 0;
 #pragma unroll
           for (int t = 0; t < kT; ++t) {
-            if (now_column >= 0)
+            if constexpr (kBoth)                     // the upper bits' sums and the rest's
+#pragma unroll
+              for (int i = 0; i < 4; ++i) acc[t][i] += dev::moved<0x128, 0xF>(0.f, acc[t][i]);        // row_ror 8
+            if (now_column >= 0 && c < kItem)
               *reinterpret_cast<f32x4*>(mine + now_column * kPitch + 16 * t + 4 * q) += acc[t];
             acc[t] = 0.f;
           }
           dev::wave_lds_barrier();
-          if (!last) now_column = sh_columns[++now_item][c];
+          if (!last) now_column = sh_columns[++now_item][token];
         }
       };
 #pragma unroll
@@ -560,10 +587,10 @@ __global__ __launch_bounds__(64 * kN, 4) void moe_down_kernel(const MoeArgs p, c
 
 size_t up16(size_t n) { return (n + 15) & ~size_t{15}; }
 size_t hidden_bytes(const MoeArgs& p) { return up16(static_cast<size_t>(p.M) * p.k * hidden_pitch(p.I) * 2); }
-// An expert has as many items as 16 go into the pairs that name it, rounded up.
-int most_items(const MoePlan& c, const MoeArgs& p) { return std::min(p.M * p.k, c.slots + p.M * p.k / 16); }
+// An expert has as many items as their size goes into the pairs that name it, rounded up.
+int most_items(const MoePlan& c, const MoeArgs& p) { return std::min(p.M * p.k, c.slots + p.M * p.k / c.item); }
 size_t table_bytes(const MoePlan& c, const MoeArgs& p) {
-  return up16(4 * (4 + static_cast<size_t>(most_items(c, p)) * (2 + 16)));
+  return up16(4 * (4 + static_cast<size_t>(most_items(c, p)) * (2 + c.item)));
 }
 
 }  // namespace
@@ -588,6 +615,11 @@ MoePlan plan_moe_layer(const MoeArgs& p, int num_cus) {
   c.tiles = p.N % 32 == 0 ? 2 : 1;
   c.splits = static_cast<int>(std::min<int64_t>(num_cus / (p.N / 16 / c.tiles), steps / 12));
   c.splits = std::max(1, std::min(c.splits, kMaxSplits));
+  // Its items: 8 tokens, whose w h fill an operand's columns with both parts, while an expert has no more than
+  // four on average; else 16, which need twice the loads and products but the weights less often.  us of the
+  // whole call, 8 / 16: one token of 128 experts 14.0 / 14.3, 16 45.9 / 49.7, 64 74.0 / 75.3; 24 of 64 experts 68.6 / 73.1;
+  // 16 of 8 experts of 2816, two a token 25.4 / 26.4, 32 30.5 / 29.7, 64 42.0 / 40.9, four a token 60.4 / 55.9.
+  c.item = p.M <= 8 || p.M * p.k <= 4 * p.E ? 8 : 16;
   return c;
 }
 
@@ -602,7 +634,8 @@ hipError_t launch_moe_layer(const MoePlan& c, const MoeArgs& p, void* workspace,
   uint16_t* hidden = reinterpret_cast<uint16_t*>(at += kWorkspaceStateBytes);
   int32_t* const ints = reinterpret_cast<int32_t*>(at += hidden_bytes(p));
   const int most = most_items(c, p);
-  const Table table{ints, ints + 4 + 16 * most, ints + 4 + 17 * most, ints + 4};
+  int32_t* const experts = ints + 4 + c.item * most;
+  const Table table{ints, experts, experts + most, ints + 4, c.item == 8 ? 3 : 4};
   float* parts = reinterpret_cast<float*>(at += table_bytes(c, p));
   auto up = [&](auto kernel, int kN, int kS) {
     const int rows = p.M <= 16 ? p.M * pitch_of(kS, 1) : std::max(16 * pitch_of(kS, 1), 32 * pitch_of(kS, 2));
@@ -620,7 +653,9 @@ hipError_t launch_moe_layer(const MoePlan& c, const MoeArgs& p, void* workspace,
                                                                                              arrived);
     return hipGetLastError();
   };
-  return c.tiles == 2 ? down(&moe_down_kernel<2, 4, 2>, 2, 4) : down(&moe_down_kernel<1, 4, 3>, 1, 4);
+  if (c.item == 8)
+    return c.tiles == 2 ? down(&moe_down_kernel<2, 4, 2, true>, 2, 4) : down(&moe_down_kernel<1, 4, 3, true>, 1, 4);
+  return c.tiles == 2 ? down(&moe_down_kernel<2, 4, 1, false>, 2, 4) : down(&moe_down_kernel<1, 4, 2, false>, 1, 4);
 }
 
 }  // namespace prq

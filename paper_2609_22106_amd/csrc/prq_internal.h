@@ -314,13 +314,13 @@ hipError_t launch_moe_route(const RoutePlan& c, const RouteArgs& p, void* worksp
 
 // moe_layer.hip.  Slots: workgroups along the experts, one for each, or for each pair of a token and
 // an expert where those are fewer; waves along H of a tile of the first product; tiles a
-// workgroup of the second, and workgroups along the experts of those.
+// workgroup of the second, workgroups along the experts of those, and tokens of an expert at a time.
 constexpr int kMaxLayerTokens = 64;
 constexpr int kMaxLayerTop = 32;
 struct MoePlan {
   int slots = 0;
   bool by_expert = true;
-  int parts = 1, tiles = 1, splits = 1;
+  int parts = 1, tiles = 1, splits = 1, item = 8;
 };
 struct MoeArgs {
   const uint16_t* x;

@@ -218,3 +218,47 @@ def test_tail_of_a_prepared_weight():
     np.testing.assert_array_equal(first["perm"], np.arange(H))       # own order
     assert np.all(first["scale"] == 1)
     assert pq.prepare(both, both[:1], 0.0, 0, "none")["Wq"].shape == first["Wq"].shape
+
+
+def _check_between(layer, got, x, ids, weights):
+    """Without the roundings to 8 bits of the bar above: w h between the launches is off by less than 2^-15 of
+    it, and is summed as two operands.  An output's own rounding, and 2^-7 of the errors for their products."""
+    y, size, _, reach = moe.layer(_np(x), ids.cpu().numpy(), _np(weights), layer.up, layer.down, layer.tail)
+    terms = 2 * ids.shape[1] * (layer.I + layer.tail)
+    far = 2.0 ** -15 * size + 2.0 ** -24 * ((layer.H + 8) * reach + (terms + 16) * size)
+    tol = 2.0 ** -8 * np.abs(y) + (1 + 2.0 ** -7) * far
+    err = np.abs(_np(got) - y)
+    assert np.all(err <= tol), (float(np.max(err / np.maximum(tol, 1e-300))), np.mean(err > tol))
+
+
+@pytest.mark.parametrize("M,E,k,H,I,tail,N", [
+    (1, 1, 1, 32, 32, 0, 64), (64, 4, 1, 32, 32, 32, 64), (40, 3, 2, 64, 64, 32, 80), (5, 128, 4, 96, 32, 0, 256),
+    (64, 16, 2, 32, 96, 96, 48), (17, 1, 1, 160, 256, 64, 32)])
+def test_little_is_lost_between_the_launches(M, E, k, H, I, tail, N):
+    say("experts", M, E, k, H, I, tail, N)
+    layer = Layer(E, H, I, tail, N, seed=M + N)
+    x, ids, w = _routed(M, E, k, M + H, H)
+    _check_between(layer, layer(x, ids, w), x, ids, w)
+
+
+def _one_feature(up_code, down_code, weight):
+    """One token, H = I = 32, N = 16: SiLU(64) * (64 2^(up_code - 127)) * weight as feature 0, and that times
+    2^(down_code - 127) as output 0; all else is 0."""
+    prq = _prq()
+    up_q, up_s = np.zeros((1, 64, 16), np.uint8), np.full((1, 64, 1), 127, np.uint8)
+    up_q[0, 0, 0] = up_q[0, 32, 0] = 2                               # a weight of 1 in column 0
+    up_s[0, 32] = up_code
+    down_q, down_s = np.zeros((1, 16, 16), np.uint8), np.full((1, 16, 1), 127, np.uint8)
+    down_q[0, 0, 0], down_s[0, 0] = 2, down_code
+    x = torch.zeros(1, 32, dtype=BF16, device="cuda")
+    x[0, 0] = 64
+    ids, w = torch.zeros(1, 1, dtype=torch.int32, device="cuda"), torch.full((1, 1), weight, device="cuda")
+    return prq.prq_moe_layer(x, ids, w, prq.prq_pack_weight(dev(up_q), dev(up_s)), prq.prq_pack_weight(dev(down_q), dev(down_s)))[0]
+
+
+def test_the_largest_values_between_the_launches():
+    """The largest float32 stays finite, an infinity infinite."""
+    below_two = float(np.nextafter(np.float32(2), np.float32(0)))
+    assert float(_one_feature(242, 125, below_two)[0]) == 2.0 ** 126       # 2^127 of those, a quarter of it
+    assert float(_one_feature(243, 125, 1.0)[0]) == float("inf")
+    assert float(_one_feature(243, 125, -1.0)[0]) == -float("inf")
