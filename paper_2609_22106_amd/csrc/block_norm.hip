@@ -26,6 +26,8 @@ namespace {
 using dev::f32x4;
 
 constexpr int kThreads = 256;
+template <int kValue>
+using Int = std::integral_constant<int, kValue>;
 
 // Four elements as they lie in memory; their values are made where they are used, so that no load is
 // waited for among the others.
@@ -162,47 +164,59 @@ __global__ __launch_bounds__(kThreads) void block_norm_kernel(const BlockNormArg
     if (live && in(i)) store4<kOnce>(p.h, row * p.ld_h + place(i), x[i] * inv * (pre[i].get(p.w_bf16) + p.offset));
 }
 
-template <typename Y, typename R, int kLanes, bool kOnce>
-void launch(const BlockNormArgs& p, hipStream_t stream) {
-  constexpr int kRows = kThreads / kLanes;
-  const int grid = static_cast<int>((p.M + kRows - 1) / kRows);
-  const int per = (p.H + 4 * kLanes - 1) / (4 * kLanes);
-  auto go = [&](auto u) {
-    block_norm_kernel<Y, R, kLanes, decltype(u)::value, kOnce><<<grid, kThreads, 0, stream>>>(p);
-  };
-  if (per <= 1) go(std::integral_constant<int, 1>{});
-  else if (per <= 2) go(std::integral_constant<int, 2>{});
-  else if constexpr (kLanes > 64) {
-    if (per <= 3 || kLanes < kThreads) go(std::integral_constant<int, 3>{});
-    else if (per <= 4) go(std::integral_constant<int, 4>{});
-    else if (per <= 8) go(std::integral_constant<int, 8>{});
-    else go(std::integral_constant<int, 16>{});
-  }
-}
-
 }  // namespace
 
-hipError_t launch_block_norm(const BlockNormArgs& p, bool y_bf16, bool r_bf16, hipStream_t stream) {
+NormPlan plan_block_norm(const BlockNormArgs& p, bool y_bf16, bool r_bf16) {
+  NormPlan c;
   // A wave a row up to 512 elements, else the workgroup: few quadruples a lane beat rows without a
   // barrier (us, a wave / the workgroup: 61 rows of 2560 9.6 / 4.4, 1537 of 1056 8.7 / 7.6, 8192 of 2560
   // in float32 71 / 52).  Many rows of up to 1536, three quadruples a lane, by half a workgroup each (the
   // workgroup / half: 512 rows of 1024 2.9 / 3.0, 1537 of 1056 6.9 / 6.35, 4096 of 1024 9.7 / 8.5, 20000 38 / 31,
   // 4096 of 1536 13.2 / 12.7; but of 2048 14.2 / 14.5).
-  const int lanes = p.H <= 512 ? 64 : p.H <= 1536 && p.M >= 1024 ? 128 : kThreads;
+  c.lanes = p.H <= 512 ? 64 : p.H <= 1536 && p.M >= 1024 ? 128 : kThreads;
+  const int per = (p.H + 4 * c.lanes - 1) / (4 * c.lanes);
+  c.quads = per <= 4 ? per : per <= 8 ? 8 : 16;
   // What does not fit the last cache (256 MB) goes past it: 8192 rows of 2560 in float32 51.8 -> 48.6 us;
   // less than that the next kernel finds there.
-  const int64_t each = (p.y ? (y_bf16 ? 2 : 4) : 0) + (r_bf16 ? 2 : 4) * ((p.residual != nullptr) + (p.residual_out != nullptr)) + (p.h ? 2 : 0);
-  const bool once = p.M * p.H * each > (int64_t{256} << 20);
-  auto go = [&](auto y, auto r) {
+  const int64_t each = (p.y ? (y_bf16 ? 2 : 4) : 0) +
+                       (r_bf16 ? 2 : 4) * ((p.residual != nullptr) + (p.residual_out != nullptr)) + (p.h ? 2 : 0);
+  c.once = p.M * p.H * each > (int64_t{256} << 20);
+  return c;
+}
+
+hipError_t launch_block_norm(const BlockNormArgs& p, bool y_bf16, bool r_bf16, hipStream_t stream) {
+  const NormPlan c = plan_block_norm(p, y_bf16, r_bf16);
+  auto of_types = [&](auto y, auto r) {
     using Y = decltype(y);
     using R = decltype(r);
-    if (lanes == 64) once ? launch<Y, R, 64, true>(p, stream) : launch<Y, R, 64, false>(p, stream);
-    else if (lanes == 128) once ? launch<Y, R, 128, true>(p, stream) : launch<Y, R, 128, false>(p, stream);
-    else once ? launch<Y, R, kThreads, true>(p, stream) : launch<Y, R, kThreads, false>(p, stream);
+    auto go = [&](auto kernel) {
+      const int rows = kThreads / c.lanes;
+      kernel<<<static_cast<int>((p.M + rows - 1) / rows), kThreads, 0, stream>>>(p);
+      return hipGetLastError();
+    };
+    auto with = [&](auto lanes, auto quads) {
+      constexpr int kLanes = decltype(lanes)::value, kU = decltype(quads)::value;
+      if constexpr (kLanes == kThreads && kU == 1)             // (fewer than 1024 rows of 1024)
+        return go(&block_norm_kernel<Y, R, kLanes, kU, false>);
+      else
+        return go(c.once ? &block_norm_kernel<Y, R, kLanes, kU, true> : &block_norm_kernel<Y, R, kLanes, kU, false>);
+    };
+    const Int<64> wave{};
+    const Int<128> half{};
+    const Int<kThreads> whole{};
+    if (c.lanes == 64) return c.quads == 1 ? with(wave, Int<1>{}) : with(wave, Int<2>{});
+    if (c.lanes == 128) return c.quads == 2 ? with(half, Int<2>{}) : with(half, Int<3>{});
+    switch (c.quads) {
+      case 1: return with(whole, Int<1>{});
+      case 2: return with(whole, Int<2>{});
+      case 3: return with(whole, Int<3>{});
+      case 4: return with(whole, Int<4>{});
+      case 8: return with(whole, Int<8>{});
+      default: return with(whole, Int<16>{});
+    }
   };
-  if (y_bf16) r_bf16 ? go(uint16_t{}, uint16_t{}) : go(uint16_t{}, float{});
-  else r_bf16 ? go(float{}, uint16_t{}) : go(float{}, float{});
-  return hipGetLastError();
+  if (y_bf16) return r_bf16 ? of_types(uint16_t{}, uint16_t{}) : of_types(uint16_t{}, float{});
+  return r_bf16 ? of_types(float{}, uint16_t{}) : of_types(float{}, float{});
 }
 
 }  // namespace prq

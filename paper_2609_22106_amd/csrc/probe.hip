@@ -240,6 +240,34 @@ int prq_tune_gemm_stream(const uint8_t* Aq, const uint8_t* Asc, int M, const int
              : -3;
 }
 
+// The kernels that calls of these sizes take (host only): plan[] is what a test of a kernel expects.
+// Norm with y and residual_out, with or without residual and h: lanes, quadruples a lane, past the cache.
+int prq_probe_norm_plan(int M, int H, int y_bf16, int r_bf16, int residual, int h, int32_t* plan) {
+  prq::BlockNormArgs p{};
+  p.M = M;
+  p.H = H;
+  p.y = p.residual_out = plan;                   // not read
+  if (residual) p.residual = plan;
+  if (h) p.h = reinterpret_cast<uint16_t*>(plan);
+  const prq::NormPlan c = prq::plan_block_norm(p, y_bf16 != 0, r_bf16 != 0);
+  plan[0] = c.lanes, plan[1] = c.quads, plan[2] = c.once;
+  return 0;
+}
+// Router: groups of 32 experts a workgroup (0: 16 tokens and 16 experts), groups of a block apart.
+int prq_probe_route_plan(int M, int E, int H, int cus, int32_t* plan) {
+  const prq::RoutePlan c = prq::plan_moe_route(M, E, H, cus);
+  plan[0] = c.groups, plan[1] = c.split;
+  return 0;
+}
+// Experts: slots, by expert, waves a tile, tiles a workgroup, workgroups along the experts, tokens an item.
+int prq_probe_layer_plan(int M, int k, int E, int H, int I, int k_tail, int N, int cus, int32_t* plan) {
+  prq::MoeArgs p{};
+  p.M = M, p.k = k, p.E = E, p.H = H, p.I = I, p.k_tail = k_tail, p.N = N;
+  const prq::MoePlan c = prq::plan_moe_layer(p, cus);
+  plan[0] = c.slots, plan[1] = c.by_expert, plan[2] = c.parts, plan[3] = c.tiles, plan[4] = c.splits, plan[5] = c.item;
+  return 0;
+}
+
 typedef float v16f_t __attribute__((ext_vector_type(16)));
 
 // One 32x32x64 block-scaled FP4 MFMA on lane-supplied operands: a, b are

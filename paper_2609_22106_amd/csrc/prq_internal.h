@@ -285,6 +285,12 @@ struct BlockNormArgs {
   bool w_bf16, gate_bf16;
   float offset, eps, a, b;
 };
+// Lanes a row, quadruples of elements a lane, and whether the bytes go past the last cache.
+struct NormPlan {
+  int lanes = 64, quads = 1;
+  bool once = false;
+};
+NormPlan plan_block_norm(const BlockNormArgs& p, bool y_bf16, bool r_bf16);
 hipError_t launch_block_norm(const BlockNormArgs& p, bool y_bf16, bool r_bf16, hipStream_t stream);
 
 // moe_route.hip.  Groups of 32 experts at a time of a workgroup with 32 tokens, or 0: a workgroup 16

@@ -1,0 +1,38 @@
+"""The kernels that the calls of a mixture-of-experts half layer take, by size (no GPU): every kernel that
+is built is one that a call takes."""
+import re
+import shutil
+import subprocess
+
+import pytest
+
+from tests import moe_plans
+
+
+def _built(kernel):
+    """Template arguments of every instance of a kernel in the library."""
+    from paper_2609_22106_amd import build
+    if not shutil.which("nm"):
+        pytest.skip("no nm")
+    names = subprocess.run(["nm", "-C", build.LIB], capture_output=True, text=True, check=True).stdout
+    found = re.findall(r"__device_stub__" + kernel + r"<([^>]*)>\(", names)
+    assert found and len(found) == len(set(found))
+    return {tuple(s.strip() for s in f.split(",")) for f in found}
+
+
+def _text(*values):
+    return tuple(str(v).lower() if isinstance(v, bool) else str(v) for v in values)
+
+
+def test_every_norm_kernel_is_taken():
+    taken = set()
+    rows = [1, 7, 1023, 1024, 1 << 14, 1 << 17, 1 << 20, (1 << 24) - 1]
+    for H in [8, 256, 264, 512, 520, 1024, 1032, 1536, 1544, 2048, 2056, 2560, 3080, 4096, 4104, 8192, 8200, 16384]:
+        for M in rows:
+            for y in (False, True):
+                for r in (False, True):
+                    lanes, quads, once = moe_plans.norm(M, H, y, r)
+                    assert lanes * quads * 4 >= H and (quads == 1 or quads > 4 or lanes * (quads - 1) * 4 < H)
+                    kind = ("float", "unsigned short")
+                    taken.add(_text(kind[y], kind[r], lanes, quads, bool(once)))
+    assert _built("block_norm_kernel") == taken
