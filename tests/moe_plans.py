@@ -25,3 +25,17 @@ def route(M, E, H):
 def layer(M, k, E, H, I, k_tail, N):
     """Slots, by expert, waves a tile, tiles a workgroup, workgroups along the experts, tokens an item."""
     return _plan("prq_probe_layer_plan", 6, M, k, E, H, I, k_tail, N, CUS)
+
+
+# (rows, width, y in bf16, residual in bf16) and the plan: every form, at the ends of its range.
+NORM_FORMS = [
+    (61, 1024, 0, 1, (256, 1, 0)), (5, 520, 1, 0, (256, 1, 0)), (1023, 1016, 0, 0, (256, 1, 0)), (2, 1000, 1, 1, (256, 1, 0)),
+    (7, 4096, 1, 1, (256, 4, 0)), (900, 3080, 0, 0, (256, 4, 0)), (3, 3584, 1, 0, (256, 4, 0)), (1100, 4088, 0, 1, (256, 4, 0)),
+    (9, 1032, 0, 0, (256, 2, 0)), (1030, 2048, 1, 0, (256, 2, 0)), (4, 8192, 0, 1, (256, 8, 0)), (3, 8200, 1, 1, (256, 16, 0)),
+    (1024, 1032, 0, 0, (128, 3, 0)), (1025, 1024, 1, 1, (128, 2, 0)), (6, 512, 1, 0, (64, 2, 0)), (4097, 264, 0, 1, (64, 2, 0)),
+    (3, 256, 0, 1, (64, 1, 0)), (4099, 8, 1, 0, (64, 1, 0)), (5, 2056, 1, 1, (256, 3, 0)), (1027, 2560, 0, 0, (256, 3, 0))]
+# The same of what is more than the last cache holds.
+NORM_PAST_THE_CACHE = [
+    (80001, 256, 0, 0, (64, 1, 1)), (60003, 504, 0, 1, (64, 2, 1)), (30001, 1024, 0, 0, (128, 2, 1)),
+    (20003, 1056, 0, 0, (128, 3, 1)), (18001, 2048, 1, 1, (256, 2, 1)), (8192, 2560, 0, 0, (256, 3, 1)),
+    (5003, 4096, 1, 0, (256, 4, 1)), (2801, 8192, 0, 0, (256, 8, 1)), (2003, 16384, 0, 1, (256, 16, 1))]

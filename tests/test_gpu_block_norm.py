@@ -13,6 +13,7 @@ import pytest
 torch = pytest.importorskip("torch")
 
 from oracle import moe                        # noqa: E402
+from tests import moe_plans                   # noqa: E402
 from tests.gpu_util import say                # noqa: E402
 
 pytestmark = pytest.mark.gpu
@@ -174,3 +175,52 @@ def test_rows_past_32_bits():
     prq.prq_block_norm(y, r, c["pre"], post_weight=c["post"], out=h)
     want = prq.prq_block_norm(c["y"], c["r"], c["pre"], post_weight=c["post"])
     assert torch.equal(h[-3:], want[0]) and torch.equal(r[-3:], want[1])
+
+
+# A lane adds at most 64 squares in 16 sums of 4; a wave's lanes meet in 6 steps and the waves in 2, so a sum of
+# squares is off by at most 1 + 2 + 16 + 6 + 2 = 27 roundings of it, the root of the mean by half of those and of
+# the quotient's and eps's, and its own, 1 / it one more: 17.  u takes 3 more, the gate 1, the scaled sum 3: 24
+# roundings of b u at most and 2 of a r.  Without a norm behind the block 4 are left.
+STEP = 2.0 ** -24
+
+
+def _check_rows(rows, c, got, a, b, eps=1e-6):
+    """Rows against the oracle, with the roundings that there are."""
+    pick = lambda t: None if t is None else _np(t[rows])                      # noqa: E731
+    post, pre, gate = _np(c["post"]), _np(c["pre"]), _np(c["gate"])
+    index = None if c["index"] is None else pick(c["index"])
+    want_r, want_h = moe.block_norm(pick(c["y"]), pick(c["r"]), post, pre, gate, index, eps, 0.0, a, b)
+    part, _ = moe.block_norm(pick(c["y"]), None, post, None, gate, index, eps, 0.0, a, b)
+    far = STEP * ((24 if post is not None else 4) * np.abs(part) + 2 * np.abs(a * pick(c["r"])))
+    far = (1 + 2.0 ** -7) * far                                                # second order, and of what is rounded
+    half = 2.0 ** -8 if got[1].dtype is BF16 else STEP
+    assert np.all(np.abs(pick(got[1]) - want_r) <= half * np.abs(want_r) + far)
+    rms = np.sqrt(np.mean(want_r ** 2, 1, keepdims=True) + eps)
+    moved = far / rms * np.abs(pre) + np.abs(want_h) * np.sqrt(np.mean(far ** 2, 1, keepdims=True)) / rms
+    assert np.all(np.abs(pick(got[0]) - want_h) <= 2.0 ** -8 * np.abs(want_h) + (1 + 2.0 ** -7) * (moved + 20 * STEP * np.abs(want_h)))
+
+
+def _form(M, H, y_bf16, r_bf16, post, gates, index):
+    say("block norm", M, H, y_bf16, r_bf16, post, gates, index)
+    c = _make(M, H, BF16 if y_bf16 else F32, BF16 if r_bf16 else F32, post, gates, M + H, index=index)
+    out = torch.full((M, H), float("nan"), dtype=BF16, device="cuda")
+    r = torch.full((M, H), float("nan"), dtype=c["r"].dtype, device="cuda")
+    return c, _prq().prq_block_norm(c["y"], c["r"], c["pre"], post_weight=c["post"], gate=c["gate"], gate_index=c["index"],
+                                    out=out, residual_out=r, residual_scale=0.75, block_scale=-0.5)
+
+
+@pytest.mark.parametrize("M,H,y_bf16,r_bf16,plan", moe_plans.NORM_FORMS)
+@pytest.mark.parametrize("post,gates,index", [(True, 3, True), (False, 1, False)])
+def test_every_form(M, H, y_bf16, r_bf16, plan, post, gates, index):
+    c, got = _form(M, H, y_bf16, r_bf16, post, gates, index)
+    _check_rows(slice(None), c, got, 0.75, -0.5)
+
+
+@pytest.mark.parametrize("M,H,y_bf16,r_bf16,plan", moe_plans.NORM_PAST_THE_CACHE)
+@pytest.mark.parametrize("post", [True, False])
+def test_past_the_last_cache(M, H, y_bf16, r_bf16, plan, post):
+    c, got = _form(M, H, y_bf16, r_bf16, post, 2, True)
+    g = torch.Generator().manual_seed(M)
+    rows = torch.unique(torch.cat([torch.randint(0, M, (30,), generator=g), torch.tensor([0, 1, M - 2, M - 1])])).cuda()
+    _check_rows(rows, c, got, 0.75, -0.5)
+    assert not bool(torch.isnan(got[0]).any()) and not bool(torch.isnan(got[1]).any())      # all rows are written

@@ -36,3 +36,13 @@ def test_every_norm_kernel_is_taken():
                     kind = ("float", "unsigned short")
                     taken.add(_text(kind[y], kind[r], lanes, quads, bool(once)))
     assert _built("block_norm_kernel") == taken
+
+
+def test_norm_sizes_reach_the_forms_that_they_name():
+    cases = moe_plans.NORM_FORMS + moe_plans.NORM_PAST_THE_CACHE
+    for M, H, y, r, plan in cases:
+        assert moe_plans.norm(M, H, y, r) == plan, (M, H)
+    reached = {plan for *_, plan in cases}
+    for H in range(8, 16385, 40):
+        for M in (1, 1023, 1024, 1 << 20):
+            assert moe_plans.norm(M, H, 0, 0) in reached, (M, H)
