@@ -38,4 +38,4 @@ NORM_FORMS = [
 NORM_PAST_THE_CACHE = [
     (80001, 256, 0, 0, (64, 1, 1)), (60003, 504, 0, 1, (64, 2, 1)), (30001, 1024, 0, 0, (128, 2, 1)),
     (20003, 1056, 0, 0, (128, 3, 1)), (18001, 2048, 1, 1, (256, 2, 1)), (8192, 2560, 0, 0, (256, 3, 1)),
-    (5003, 4096, 1, 0, (256, 4, 1)), (2801, 8192, 0, 0, (256, 8, 1)), (2003, 16384, 0, 1, (256, 16, 1))]
+    (6003, 4096, 1, 0, (256, 4, 1)), (2801, 8192, 0, 0, (256, 8, 1)), (2003, 16384, 0, 1, (256, 16, 1))]
