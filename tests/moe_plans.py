@@ -39,3 +39,15 @@ NORM_PAST_THE_CACHE = [
     (80001, 256, 0, 0, (64, 1, 1)), (60003, 504, 0, 1, (64, 2, 1)), (30001, 1024, 0, 0, (128, 2, 1)),
     (20003, 1056, 0, 0, (128, 3, 1)), (18001, 2048, 1, 1, (256, 2, 1)), (8192, 2560, 0, 0, (256, 3, 1)),
     (6003, 4096, 1, 0, (256, 4, 1)), (2801, 8192, 0, 0, (256, 8, 1)), (2003, 16384, 0, 1, (256, 16, 1))]
+
+# (tokens, experts, chosen, width) of the router and the plan: last blocks of 32 with few tokens and with many, widths
+# within a chunk of H, at its end and past it.
+ROUTE_FORMS = [
+    (8200, 16, 4, 40, (1, 0)), (4200, 32, 32, 24, (1, 0)), (4129, 20, 3, 1056, (1, 0)), (8193, 1, 1, 520, (1, 0)),
+    (2800, 40, 5, 328, (2, 0)), (2053, 60, 4, 136, (2, 0)), (2080, 64, 6, 1032, (2, 0)), (2753, 33, 32, 256, (2, 0)),
+    (1700, 70, 5, 72, (4, 0)), (1400, 96, 8, 264, (4, 0)), (1029, 128, 8, 520, (4, 0)), (1900, 130, 7, 64, (4, 0)),
+    (1029, 250, 8, 1024, (4, 0)), (1100, 256, 32, 40, (4, 0)), (5470, 300, 4, 16, (4, 0)), (4100, 512, 3, 24, (4, 0)),
+    (1000, 300, 8, 136, (4, 1)), (1033, 512, 16, 2056, (4, 1)), (900, 400, 4, 8, (4, 1)), (1025, 257, 2, 640, (4, 1)),
+    (1, 128, 8, 2048, (0, 0)), (61, 64, 6, 264, (0, 0)), (1100, 16, 4, 72, (0, 0)), (1100, 1000, 9, 72, (0, 0))]
+# One of each for the inputs that are the same in all of them.
+ROUTE_KINDS = [(8200, 16), (2800, 40), (1400, 96), (1029, 250), (4100, 512), (1000, 300), (40, 300)]

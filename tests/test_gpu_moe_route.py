@@ -14,6 +14,7 @@ import pytest
 torch = pytest.importorskip("torch")
 
 from oracle import moe                        # noqa: E402
+from tests import moe_plans                   # noqa: E402
 from tests.gpu_util import say                # noqa: E402
 
 pytestmark = pytest.mark.gpu
@@ -172,3 +173,118 @@ def test_zero_tokens():
     x, w, _ = _grid(0, 8, 64, 1)
     ids, weights = _prq().prq_moe_route(x, w, 2)
     assert ids.shape == weights.shape == (0, 2)
+
+
+def _same(got, logits, k, sigmoid=False, bias=None, renormalize=True, scale=1.0):
+    """_check, where weights may be NaN: in the same places."""
+    ids, weights = got
+    with np.errstate(invalid="ignore"):
+        want_ids, want = moe.route(logits, k, sigmoid, _np(bias), renormalize, scale)
+        np.testing.assert_array_equal(ids.cpu().numpy(), want_ids)
+        nan = np.isnan(want)
+        np.testing.assert_array_equal(np.isnan(_np(weights)), nan)
+        tol = 2.0 ** -23
+        if not sigmoid:
+            chosen = np.take_along_axis(logits, want_ids, 1)
+            tol = 2.0 ** -20 + 2.0 ** -24 * np.where(want > 0, chosen[:, :1] - chosen, 0)
+        assert np.all((np.abs(_np(weights) - want) <= tol * np.abs(want) + 2.0 ** -126)[~nan])
+
+
+@pytest.mark.parametrize("M,E,k,H,plan", moe_plans.ROUTE_FORMS)
+@pytest.mark.parametrize("sigmoid,renormalize", [(False, False), (True, True)])
+def test_every_form(M, E, k, H, plan, sigmoid, renormalize):
+    say("route", M, E, k, H, sigmoid, renormalize)
+    x, w, bias = _grid(M, E, H, M + E + H)
+    bias = bias if sigmoid else None
+    kw = dict(scoring="sigmoid" if sigmoid else "softmax", bias=bias, renormalize=renormalize, scale=0.5)
+    logits = torch.full((M, E), float("nan"), device="cuda")
+    got = _prq().prq_moe_route(x, w, k, logits=logits, **kw)
+    want = _np(x) @ _np(w).T
+    np.testing.assert_array_equal(_np(logits), want)
+    _check(got, want, k, sigmoid, bias, renormalize, 0.5)
+    for again, t in zip(_prq().prq_moe_route(x, w, k, **kw), got):                 # without logits
+        assert torch.equal(again, t)
+
+
+@pytest.mark.parametrize("M,E", moe_plans.ROUTE_KINDS)
+def test_ties_of_every_form(M, E):
+    x = torch.zeros(M, 64, dtype=torch.bfloat16, device="cuda")
+    w = torch.randn(E, 64, device="cuda").bfloat16()
+    k = min(E, 9)
+    for kw in (dict(), dict(scoring="sigmoid"), dict(scoring="sigmoid", bias=torch.full((E,), 0.25, device="cuda"))):
+        ids, weights = _prq().prq_moe_route(x, w, k, **kw)
+        assert bool((ids == torch.arange(k, device="cuda")).all()) and bool((weights == weights[0, 0]).all())
+    # two values in turn: the experts of the larger one first, each in order
+    x[:, 0] = 1
+    w.zero_()
+    w[1::2, 0] = 1
+    want = torch.cat([torch.arange(1, E, 2), torch.arange(0, E, 2)])[:k].cuda()
+    assert bool((_prq().prq_moe_route(x, w, k)[0] == want).all())
+
+
+@pytest.mark.parametrize("M,E", moe_plans.ROUTE_KINDS)
+@pytest.mark.parametrize("kw", [dict(renormalize=True), dict(renormalize=False), dict(scoring="sigmoid", renormalize=False)])
+def test_nan_and_infinite_logits_of_every_form(M, E, kw):
+    """Rows with a logit of +inf, of -inf and of NaN, among the chosen and not, and rows of nothing else; the
+    weights too: a softmax over all is NaN wherever a logit is, the chosen alone are not where that is not chosen."""
+    g = torch.Generator(device="cuda").manual_seed(M)
+    x = torch.zeros(M, 8, dtype=torch.bfloat16, device="cuda")
+    x[:, 0] = 1
+    w = torch.zeros(E, 8, dtype=torch.bfloat16, device="cuda")
+    w[:, 0] = torch.randperm(E, generator=g, device="cuda") / 32                     # (8 bits at most)
+    inf, nan = float("inf"), float("nan")
+    at = [m for m in (0, 3, M // 2, M - 1)]
+    for m, v in zip(at, (inf, nan, -inf, inf)):
+        x[m, 1] = v                                                                # times column 1
+    w[0, 1], w[E // 2, 1], w[E - 1, 1] = 1, -1, 0.5                                 # 0 times inf and NaN: NaN for the others
+    with np.errstate(invalid="ignore"):
+        logits = _np(x) @ _np(w).T
+    k, rows = min(E, 5), sorted({*at, *range(1, M, 37)})
+
+    def check():
+        got = _prq().prq_moe_route(x, w, k, **kw)
+        _same([t[rows] for t in got], logits[rows], k, "scoring" in kw, renormalize=kw["renormalize"])
+    check()
+    x[:, 1] = 0
+    x[at, 2] = 1
+    w[E // 3, 2], w[2 * E // 3, 2] = nan, -inf                                      # NaN for every row: 0 times those
+    w[:, 1] = 0
+    with np.errstate(invalid="ignore"):
+        logits = _np(x) @ _np(w).T
+    check()
+
+
+@pytest.mark.parametrize("M,E", moe_plans.ROUTE_KINDS)
+def test_strides_and_a_poisoned_workspace_of_every_form(M, E):
+    """Rows of wider tensors; one workspace for calls of several sizes in turn, whose scratch holds NaN."""
+    prq = _prq()
+    k = min(E, 6)
+    x, w, _ = _grid(M, E, 136, M + E)
+    wide, w_wide = torch.full((M, 200), float("nan"), dtype=torch.bfloat16, device="cuda"), torch.cat([w, w + 1], 1)
+    wide[:, 8:144] = x
+    ws = torch.zeros(max(prq.prq_moe_route_workspace_bytes(m, E, 136) for m in (1, 3, M)) + 16384, dtype=torch.uint8, device="cuda")
+    logits = torch.full((M + 1, E + 4), 7.0, device="cuda")[:, :(E + 3) // 4 * 4]
+    ids, weights = torch.full((M + 1, k), -7, dtype=torch.int32, device="cuda"), torch.full((M + 1, k), -7.0, device="cuda")
+    for m in (M, 1, M, 3):
+        ws[16384:] = 255
+        got = prq.prq_moe_route(wide[:m, 8:144], w_wide[:, :136], k, workspace=ws, ids=ids[:m], weights=weights[:m],
+                                logits=logits[:m, :E] if E % 4 == 0 else None)
+        _check(got, _np(x[:m]) @ _np(w).T, k)
+        assert not ws[:16384].any() and bool((logits[M:] == 7).all())
+        assert bool((ids[M:] == -7).all()) and bool((weights[M:] == -7).all())
+
+
+@pytest.mark.parametrize("M,E,ld", [(8200, 16, 1 << 18), (2800, 40, 1 << 20), (1400, 96, 1 << 21), (1029, 250, 1 << 21),
+                                    (1000, 300, 1 << 22)])
+def test_rows_past_32_bits_of_every_form(M, E, ld):
+    """Rows of x, and of the logits, more than 2^31 elements apart, first to last."""
+    x, w, _ = _grid(M, E, 64, 7)
+    far = torch.empty((M - 1) * ld + 16384, dtype=torch.bfloat16, device="cuda")
+    rows = far.as_strided((M, 64), (ld, 1))
+    rows.copy_(x)
+    logits = far.view(torch.float32)[4096:].as_strided((M, E), (ld // 2, 1))
+    got = _prq().prq_moe_route(rows, w, 4, logits=logits)
+    want = _np(x) @ _np(w).T
+    _check(got, want, 4)
+    np.testing.assert_array_equal(_np(logits), want)
+    assert torch.equal(rows, x)

@@ -46,3 +46,17 @@ def test_norm_sizes_reach_the_forms_that_they_name():
     for H in range(8, 16385, 40):
         for M in (1, 1023, 1024, 1 << 20):
             assert moe_plans.norm(M, H, 0, 0) in reached, (M, H)
+
+
+def test_every_router_kernel_is_taken_and_the_sizes_reach_them():
+    reached = set()
+    for M, E, k, H, plan in moe_plans.ROUTE_FORMS:
+        assert moe_plans.route(M, E, H) == plan, (M, E)
+        reached.add(plan)
+    assert reached == {moe_plans.route(M, E, H) for M, E in moe_plans.ROUTE_KINDS for H in (8, 64)}
+    assert reached == {moe_plans.route(M, E, 64) for E in range(1, 1025, 3)
+                       for M in (1, 100, 1000, 2000, 3000, 5000, 10000, 1 << 20)}
+    for bias in (False, True):
+        assert {f for f in _built("route_many_kernel") if f[1] == _text(bias)[0]} == \
+            {_text(groups, bias, bool(split)) for groups, split in reached if groups}
+    assert _built("route_few_kernel") == {("false",), ("true",)}
