@@ -617,8 +617,10 @@ enum {
  *        compared, whose order is that of either score), in descending order, the lower index
  *        first among equals, NaN last;
  *   weights: their s, with `renormalize` divided by the sum of the k, times `scale`; the sigmoid in
- *        float64, rounded at the end.  Infinite logits give what the formulas give (NaN weights where
- *        a softmax has one).
+ *        float64, rounded at the end.  A softmax that is renormalized is computed of the k chosen
+ *        logits alone, where the sum over all cancels: a NaN of an expert that is not chosen, which
+ *        makes every weight of its row NaN without `renormalize`, does not count with it.  Infinite
+ *        logits give what the formulas give (a chosen +infinity NaN weights of a softmax).
  *
  *   x       device [M, ld_x] bf16
  *   W       device [E, ld_w] bf16

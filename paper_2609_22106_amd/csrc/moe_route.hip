@@ -5,7 +5,8 @@
 //   s = softmax(l)  or  1 / (1 + exp(-l))
 //   the k experts with the largest s (or s + bias), descending, the lower index first among
 //   equals, NaN behind everything
-//   w = s (or s divided by the sum of the chosen) times `scale`
+//   w = s (or s divided by the sum of the chosen, for which a softmax needs the chosen logits only)
+//     times `scale`
 // Both scores keep the order of l, so without a bias l itself is compared.  A bias moves borders: its
 // key, and the sigmoid's weights, are computed in 64 bits.
 //

@@ -1087,7 +1087,7 @@ def prq_moe_route(x, W, k, scoring="softmax", bias=None, renormalize=True, scale
     """x [M, H] bf16, router weight W [E, H] bf16 -> (ids int32 [M, k], weights float32 [M, k]): the k
     experts with the largest softmax or sigmoid of x W^T (+ bias float32 [E], with the sigmoid),
     descending, the lower index first among equals, and their scores (renormalize: divided by their
-    sum) times scale.  logits: float32 [M, E] to write x W^T into.  workspace: uint8,
+    sum; a softmax of the k alone, so a NaN that is not chosen does not count) times scale.  logits: float32 [M, E] to write x W^T into.  workspace: uint8,
     prq_moe_route_workspace_bytes, zeroed before its first use and left ready by every call (else
     allocated, zeroed by another launch)."""
     if not isinstance(x, torch.Tensor) or x.dim() != 2 or not isinstance(W, torch.Tensor) or W.dim() != 2:

@@ -201,3 +201,14 @@ def test_tensors_of_another_device_are_refused(monkeypatch):
     down.Wps.index = 0
     with pytest.raises(ValueError, match="down.Wps is on"):
         prq.prq_moe_layer(at(1, 3, 64), ids, at(1, 3, 2, dtype=torch.float32), up, down, k_tail=32)
+
+
+def test_oracle_route_with_a_nan_that_is_not_chosen():
+    """What the header says: the chosen logits alone with renormalize, NaN without; a chosen infinity either way."""
+    l = np.array([[2.0, np.nan, 3, 1], [np.inf, 0, 1, 2]])
+    with np.errstate(invalid="ignore"):
+        ids, w = moe.route(l, 2)
+        of_all = moe.route(l, 2, renormalize=False)[1]
+    assert ids.tolist() == [[2, 0], [0, 3]]
+    np.testing.assert_allclose(w[0], np.exp([0, -1]) / (1 + np.exp(-1)))
+    assert np.isnan(of_all).all() and np.isnan(w[1]).all()
