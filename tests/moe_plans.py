@@ -51,3 +51,24 @@ ROUTE_FORMS = [
     (1, 128, 8, 2048, (0, 0)), (61, 64, 6, 264, (0, 0)), (1100, 16, 4, 72, (0, 0)), (1100, 1000, 9, 72, (0, 0))]
 # One of each for the inputs that are the same in all of them.
 ROUTE_KINDS = [(8200, 16), (2800, 40), (1400, 96), (1029, 250), (4100, 512), (1000, 300), (40, 300)]
+
+# (tokens, experts, experts a token, hidden, intermediate, tail, output width) of the experts' call and of the plan: by
+# expert, waves a tile, tiles a workgroup, workgroups along the experts, tokens an item.
+LAYER_FORMS = [
+    # two waves a tile: up to 16 tokens, more than 16 of an expert over several pieces of H, wide
+    (12, 128, 8, 1184, 256, 32, 32, (0, 2, 2, 8, 8)), (64, 8, 4, 2144, 1024, 0, 64, (1, 2, 2, 5, 16)),
+    (20, 2, 2, 1056, 4096, 0, 32, (1, 2, 2, 5, 16)), (64, 8, 4, 1056, 1024, 32, 48, (1, 2, 1, 6, 16)),
+    # one: the same
+    (16, 64, 6, 1056, 1408, 0, 48, (1, 1, 1, 8, 8)), (64, 12, 4, 544, 1408, 64, 48, (1, 1, 1, 8, 16)),
+    (64, 8, 4, 1184, 2816, 0, 32, (1, 1, 2, 8, 16)), (33, 512, 2, 160, 352, 64, 64, (0, 1, 2, 8, 8)),
+    (64, 130, 2, 96, 544, 32, 48, (0, 1, 1, 8, 8)),
+    # four: the same
+    (9, 16, 4, 2080, 96, 32, 64, (1, 4, 2, 1, 8)), (20, 16, 4, 2080, 96, 32, 48, (1, 4, 1, 1, 16)),
+    (64, 3, 2, 2112, 64, 0, 96, (1, 4, 2, 1, 16)), (8, 3, 2, 1056, 1408, 0, 64, (1, 4, 2, 2, 8)),
+    # more workgroups than CUs of the second launch, an output of odd tiles
+    (64, 4, 1, 32, 96, 96, 8224, (1, 4, 2, 1, 16)), (40, 16, 5, 544, 160, 0, 8208, (1, 4, 1, 1, 16))]
+# More than 64 items to a workgroup of the second launch.
+LAYER_WINDOWS = [
+    (64, 256, 8, 64, 32, 0, 7168, (1, 2, 2, 1, 8)), (64, 300, 8, 32, 32, 32, 4112, (1, 2, 1, 1, 8)),
+    (64, 400, 32, 32, 32, 0, 4112, (1, 2, 1, 1, 16)), (64, 200, 30, 64, 32, 0, 7200, (1, 2, 2, 1, 16)),
+    (64, 4096, 32, 64, 32, 0, 16, (0, 1, 1, 8, 8))]

@@ -12,6 +12,7 @@ torch = pytest.importorskip("torch")
 
 from oracle import moe                                  # noqa: E402
 from paper_2609_22106_amd import inputs                 # noqa: E402
+from tests import moe_plans                             # noqa: E402
 from tests.gpu_util import dev, say                     # noqa: E402
 
 pytestmark = pytest.mark.gpu
@@ -262,3 +263,38 @@ def test_the_largest_values_between_the_launches():
     assert float(_one_feature(242, 125, below_two)[0]) == 2.0 ** 126       # 2^127 of those, a quarter of it
     assert float(_one_feature(243, 125, 1.0)[0]) == float("inf")
     assert float(_one_feature(243, 125, -1.0)[0]) == -float("inf")
+
+
+def _check_some(layer, got, x, ids, w, seed):
+    """Twelve rows (the oracle takes a row at a time); all are written."""
+    g = torch.Generator().manual_seed(seed)
+    rows = torch.unique(torch.cat([torch.randint(0, len(x), (10,), generator=g), torch.tensor([0, len(x) - 1])])).cuda()
+    layer.check(got[rows], x[rows], ids[rows], w[rows])
+    assert not bool(torch.isnan(got).any())
+
+
+@pytest.mark.parametrize("M,E,k,H,I,tail,N,plan", moe_plans.LAYER_FORMS + moe_plans.LAYER_WINDOWS)
+def test_every_form(M, E, k, H, I, tail, N, plan):
+    """As many experts as tokens ask for, then one of them asked for by all, with a workspace of NaN."""
+    say("experts", M, E, k, H, I, tail, N)
+    layer = Layer(E, H, I, tail, N, seed=M + E + H)
+    x, ids, w = _routed(M, E, k, M + N, H)
+    ws = torch.zeros(_prq().prq_moe_layer_workspace_bytes(M, k, E, H, I, tail, N), dtype=torch.uint8, device="cuda")
+    for _ in range(2):
+        ws[16384:] = 255
+        out = torch.full((M, N), float("nan"), dtype=BF16, device="cuda")
+        layer(x, ids, w, out=out, workspace=ws)
+        _check_some(layer, out, x, ids, w, M)
+        assert not ws[:16384].any()
+        ids[:, 0] = E // 2
+
+
+@pytest.mark.parametrize("M,E,k,H,I,tail,N", [(64, 64, 32, 32, 32, 32, 48), (64, 1024, 32, 64, 32, 0, 48), (50, 600, 20, 64, 64, 32, 64)])
+def test_an_expert_named_by_every_choice(M, E, k, H, I, tail, N):
+    """Room for as many tokens as choices, most of it empty: behind an expert of lower number and before others."""
+    layer = Layer(E, H, I, tail, N, seed=M + E)
+    x, ids, w = _routed(M, E, k, M + H, H)
+    ids[:] = E // 2
+    _check_some(layer, layer(x, ids, w, out=torch.full((M, N), float("nan"), dtype=BF16, device="cuda")), x, ids, w, 1)
+    ids[::3, 1], ids[1::5, 2], ids[:, k - 1] = 3, E - 1, -1
+    _check_some(layer, layer(x, ids, w, out=torch.full((M, N), float("nan"), dtype=BF16, device="cuda")), x, ids, w, 2)

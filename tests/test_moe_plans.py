@@ -60,3 +60,20 @@ def test_every_router_kernel_is_taken_and_the_sizes_reach_them():
         assert {f for f in _built("route_many_kernel") if f[1] == _text(bias)[0]} == \
             {_text(groups, bias, bool(split)) for groups, split in reached if groups}
     assert _built("route_few_kernel") == {("false",), ("true",)}
+
+
+def test_every_kernel_of_the_experts_is_taken_and_the_sizes_reach_them():
+    up, down = set(), set()
+    for M, E, k, H, I, tail, N, plan in moe_plans.LAYER_FORMS + moe_plans.LAYER_WINDOWS:
+        slots, by_expert, parts, tiles, splits, item = moe_plans.layer(M, k, E, H, I, tail, N)
+        assert (by_expert, parts, tiles, splits, item) == plan, (M, E)
+        assert slots == min(E, M * k) and by_expert == (slots == E)
+        up.add((parts, M > 16, H > 1024))
+        down.add((tiles, item, splits > 1))
+    assert up >= {(parts, many, True) for parts in (1, 2, 4) for many in (False, True)}
+    assert down >= {(tiles, item, True) for tiles in (1, 2) for item in (8, 16)}
+    assert {int(f[1]) for f in _built("moe_up_kernel")} == {parts for parts, *_ in up}
+    assert {(int(f[0]), 8 if f[3] == "true" else 16) for f in _built("moe_down_kernel")} == {d[:2] for d in down}
+    # the experts that random choices name, an item each at least, over the workgroups along them
+    for M, E, k, H, I, tail, N, (*_, splits, _) in moe_plans.LAYER_WINDOWS:
+        assert 0.8 * E * (1 - (1 - k / E) ** M) / splits > 64, (M, E)
