@@ -649,7 +649,8 @@ int prq_moe_route(const void* x_bf16, int64_t ld_x, int32_t M, int32_t H, const 
  * MXFP4 weights against bf16 activations: at so few rows the weights are the bytes, so the
  * activations are not quantized.  Sums are float32, in a fixed order (calls repeat bit for bit);
  * weights[m, j] h is held to 2^-15 of it between the two launches (the sum of two bf16), and out is
- * rounded once.
+ * rounded once.  Weights of 2^128 and more (scale codes 253 and 254) are beyond float32: an output that
+ * meets one is infinite or NaN.
  *
  *   x        device [M, ld_x] bf16
  *   ids      device [M, k] int32; an entry outside [0, E) adds nothing (padding, an expert held

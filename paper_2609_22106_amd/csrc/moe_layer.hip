@@ -15,7 +15,8 @@
 // 5.4 TB/s, the first launch 5.0 and 5.5).  The second loses 5 us to its start and 2.5 to the join of
 // workgroups; twice the waves or workgroups change nothing there (65.2 and 65 us).  A CU has 80 cycles of
 // matrix work free for every kilobyte of weights, so the activations stay in bf16 at no cost and the
-// weights are brought to bf16 in registers (a 4-bit value times a power of two is exact there).  A wave
+// weights are brought to bf16 in registers (a 4-bit value times a power of two is exact there below
+// 2^128, where float32 ends too; scale codes 253 and 254 reach beyond).  A wave
 // has two units of weights under way; enough waves a CU keep the memory busy meanwhile.  One token (21 MB,
 // 3.8 us of them) takes 14.6 us, since its trips to memory follow each other: in the first launch (7.3) the
 // launch itself 1.5, routing 2.2, x 0.4, weights 1.9, the rest of them and the sums 1.5; in the second the

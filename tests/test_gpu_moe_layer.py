@@ -298,3 +298,34 @@ def test_an_expert_named_by_every_choice(M, E, k, H, I, tail, N):
     _check_some(layer, layer(x, ids, w, out=torch.full((M, N), float("nan"), dtype=BF16, device="cuda")), x, ids, w, 1)
     ids[::3, 1], ids[1::5, 2], ids[:, k - 1] = 3, E - 1, -1
     _check_some(layer, layer(x, ids, w, out=torch.full((M, N), float("nan"), dtype=BF16, device="cuda")), x, ids, w, 2)
+
+
+@pytest.mark.parametrize("code", [0, 1, 127, 242, 243, 250, 251, 252, 253, 254])
+def test_every_weight_of_a_scale_code(code):
+    """In either product a weight is its value times the power of two; of 2^128 and more, which codes of 253 and
+    254 have and float32 has not, it is infinite.  An output that meets one is not finite: infinity times the
+    part 0 of a w h that fits 8 bits, as here, is NaN."""
+    prq = _prq()
+    values = np.array([0, .5, 1, 1.5, 2, 3, 4, 6, -0., -.5, -1, -1.5, -2, -3, -4, -6])
+    small = 2.0 ** -100 if code > 127 else 2.0 ** 60                  # with which 64 times it stays within bf16
+    want = values * 2.0 ** (code - 127)
+    finite = np.abs(want) < 2.0 ** 128
+    want = want * 64 * small
+    pack = lambda q, s: prq.prq_pack_weight(dev(q), dev(s))           # noqa: E731
+    x = torch.zeros(1, 32, dtype=BF16, device="cuda")
+    x[0, 0], x[0, 1] = 64, small                                      # gate and up columns
+    ids, w = torch.zeros(1, 1, dtype=torch.int32, device="cuda"), torch.ones(1, 1, device="cuda")
+
+    def run(up_row, up_code, down_q, down_code):
+        up_q, up_s = np.zeros((1, 64, 16), np.uint8), np.full((1, 64, 1), 127, np.uint8)
+        up_q[0, 0, 0] = 2                                             # SiLU(64), feature 0
+        up_q[0, 32, 0], up_s[0, 32] = up_row << 4, up_code
+        return prq.prq_moe_layer(x, ids, w, pack(up_q, up_s), pack(down_q, np.full((1, 16, 1), down_code, np.uint8)))[0]
+
+    ones, codes = np.zeros((1, 16, 16), np.uint8), np.zeros((1, 16, 16), np.uint8)
+    ones[0, :, 0], codes[0, :, 0] = 2, np.arange(16)                  # column 0
+    got = _np(run(2, 127, codes, code))
+    assert np.array_equal(got[finite], want[finite]) and not np.isfinite(got[~finite]).any()
+    for v in range(16):
+        got = _np(run(v, code, ones, 127))
+        assert (got == want[v]).all() if finite[v] else not np.isfinite(got).any()
