@@ -33,7 +33,7 @@
 // The maximum is kept per lane group and only joined across the groups when a score
 // passes it by 8 (powers of two): until then the stale maximum serves, P up to 2^8.
 // Scores, statistics and O are float32; P is rounded to bf16 for its product (relative
-// error 2^-9 each, as large as the rounding of the output; the sum that divides takes
+// error 2^-8 each at most, as large as the rounding of the output; the sum that divides takes
 // the unrounded P).
 //
 // Few rows leave most CUs idle, so a request's keys are split over workgroups: as many
