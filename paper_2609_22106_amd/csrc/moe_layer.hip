@@ -11,16 +11,15 @@
 //
 // The weights of the experts that are reached are most of the bytes, and what bounds both launches
 // where they are many: 64 tokens of 128 experts, eight a token, of 2048 -> 768 + 64 -> 2048, 292 MB in
-// 65 us, 39 and 26; 19 tokens of 64, six a token, of 2560 -> 1408, 282 MB in 55, 34 and 20.5 (a copy reaches
-// 5.4 TB/s, the first launch 5.0 and 5.5).  The second loses 5 us to its start and 2.5 to the join of
-// workgroups; twice the waves or workgroups change nothing there (65.2 and 65 us).  A CU has 80 cycles of
-// matrix work free for every kilobyte of weights, so the activations stay in bf16 at no cost and the
-// weights are brought to bf16 in registers (a 4-bit value times a power of two is exact there below
-// 2^128, where float32 ends too; scale codes 253 and 254 reach beyond).  A wave
-// has two units of weights under way; enough waves a CU keep the memory busy meanwhile.  One token (21 MB,
-// 3.8 us of them) takes 14.6 us, since its trips to memory follow each other: in the first launch (7.3) the
-// launch itself 1.5, routing 2.2, x 0.4, weights 1.9, the rest of them and the sums 1.5; in the second the
-// table, weights, and the join.
+// 67 us, 38.5 and 29; 19 tokens of 64, six a token, of 2560 -> 1408, 282 MB in 54.5, 34 and 20.5 (a copy
+// reaches 5.4 TB/s, the first launch 5.0 and 5.5).  The second loses 5 us to its start and 2.5 to the join of
+// workgroups; twice the waves or workgroups changed nothing there.  A CU has 80 cycles of matrix work
+// free for every kilobyte of weights, so the activations are not quantized and the weights are brought
+// to bf16 in registers (a 4-bit value times a power of two is exact there below 2^128, where float32 ends
+// too; scale codes 253 and 254 reach beyond).  A wave has two units of weights under way; enough waves a
+// CU keep the memory busy meanwhile.  One token (21 MB, 3.8 us of them) takes 14.0 us, since its trips to
+// memory follow each other: in the first launch (7.4) the launch itself 1.5, routing 2.2, x 0.4, weights
+// 1.9, the rest of them and the sums 1.5; in the second the table, weights, and the join.
 //
 // A slot is an expert (its number), or where there are fewer pairs of a token and an expert than
 // experts a pair (its first occurrence), so that a launch of `slots` workgroups in y reaches every
@@ -378,7 +377,8 @@ constexpr int sums_pitch(int tiles) { return 16 * tiles + 4; }
 // added in their order, the workgroups' in theirs, by the one that arrives last.
 //
 // kBoth: an item has 8 tokens, whose upper bits are columns 0 to 7 of the operand and the rest columns 8
-// to 15, so that one load and one product serve both (16 tokens take two of each).
+// to 15, so that one load and one product serve both.  (16 tokens take two of each, and a load's time in
+// the address unit goes by its lanes, also those that get nothing.)
 //
 // A wave asks for the weights and activations of a step kAhead steps ahead.  The loop has loads
 // without conditions only (past the end, and of columns without a token, outside their buffers), so

@@ -212,8 +212,8 @@ __device__ __forceinline__ void choose(const RouteArgs& p, int token, bool live,
 }
 
 // Tokens token0 .. token0 + rows - 1 by the workgroup: 16 lanes each, or 64 where there are no more tokens
-// than waves or the experts are many (300 tokens of 512 experts: 25 us with 16, 26 with 64; 2000 tokens 84
-// and 93).  logit(row, e).
+// than waves or more experts than 32 a lane.  us, 16 / 64 lanes (H = 2048): 512 experts 300 tokens 25.1 / 23.9, 1100
+// 30.0 / 30.5, 2000 34.6 / 31.5, 8192 54.3 / 56.4; 300 experts (H = 1024) 8192 29.4 / 32.8.  logit(row, e).
 template <bool kBias, typename Logit>
 __device__ __forceinline__ void choose_rows(const RouteArgs& p, int token0, int rows, Logit logit) {
   const int wave = static_cast<int>(threadIdx.x) >> 6;
