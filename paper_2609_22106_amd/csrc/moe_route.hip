@@ -38,6 +38,8 @@ using dev::f32x4;
 using dev::u32x4v;
 
 constexpr int kWaves = 8, kThreads = 64 * kWaves;
+// Experts past which a block's logits do not fit beside the stages of route_many_kernel (512: 158 of 160 KB).
+constexpr int kMaxManyExperts = 512;
 
 // Unsigned integers in the order of the numbers, above 0, NaN below everything; and back.
 __device__ __forceinline__ uint32_t ordered(float x) {
@@ -211,28 +213,32 @@ __device__ __forceinline__ void choose(const RouteArgs& p, int token, bool live,
     }
 }
 
+// choose with as many keys a lane as E takes, of a kernel that takes kMost experts at most.
+template <int kLanes, int kR, int kMost, bool kBias, typename Logit>
+__device__ __forceinline__ void choose_of(const RouteArgs& p, int token, bool live, Logit logit) {
+  if constexpr (kLanes * kR >= kMost) {
+    choose<kLanes, kR, kBias>(p, token, live, logit);
+  } else {
+    if (p.E <= kLanes * kR) choose<kLanes, kR, kBias>(p, token, live, logit);
+    else choose_of<kLanes, 2 * kR, kMost, kBias>(p, token, live, logit);
+  }
+}
+
 // Tokens token0 .. token0 + rows - 1 by the workgroup: 16 lanes each, or 64 where there are no more tokens
 // than waves or more experts than 32 a lane.  us, 16 / 64 lanes (H = 2048): 512 experts 300 tokens 25.1 / 23.9, 1100
 // 30.0 / 30.5, 2000 34.6 / 31.5, 8192 54.3 / 56.4; 300 experts (H = 1024) 8192 29.4 / 32.8.  logit(row, e).
-template <bool kBias, typename Logit>
+template <bool kBias, int kMost, typename Logit>
 __device__ __forceinline__ void choose_rows(const RouteArgs& p, int token0, int rows, Logit logit) {
+  constexpr int kMostOf16 = 512;
   const int wave = static_cast<int>(threadIdx.x) >> 6;
-  if (p.E > 512 || rows <= kWaves) {
-    for (int r = wave; r < rows; r += kWaves) {
-      auto of = [&](int e) { return logit(r, e); };
-      if (p.E <= 128) choose<64, 2, kBias>(p, token0 + r, true, of);
-      else if (p.E <= 256) choose<64, 4, kBias>(p, token0 + r, true, of);
-      else if (p.E <= 512) choose<64, 8, kBias>(p, token0 + r, true, of);
-      else choose<64, kMaxRouteExperts / 64, kBias>(p, token0 + r, true, of);
-    }
+  if ((kMost > kMostOf16 && p.E > kMostOf16) || rows <= kWaves) {
+    for (int r = wave; r < rows; r += kWaves)
+      choose_of<64, 2, kMost, kBias>(p, token0 + r, true, [&](int e) { return logit(r, e); });
   } else {
     for (int r0 = 4 * wave; r0 < rows; r0 += 4 * kWaves) {
       const int r = r0 + (static_cast<int>(threadIdx.x) >> 4 & 3);
-      auto of = [&](int e) { return logit(r, e); };
-      if (p.E <= 64) choose<16, 4, kBias>(p, token0 + r, r < rows, of);
-      else if (p.E <= 128) choose<16, 8, kBias>(p, token0 + r, r < rows, of);
-      else if (p.E <= 256) choose<16, 16, kBias>(p, token0 + r, r < rows, of);
-      else choose<16, 32, kBias>(p, token0 + r, r < rows, of);
+      choose_of<16, 4, (kMost < kMostOf16 ? kMost : kMostOf16), kBias>(p, token0 + r, r < rows,
+                                                                       [&](int e) { return logit(r, e); });
     }
   }
 }
@@ -325,9 +331,11 @@ __global__ __launch_bounds__(kThreads) void route_few_kernel(const RouteArgs p, 
     for (int v = 0; v < kWaves; ++v) l += sums[v][(e >> 2) * 16 + r][e & 3];
     return l;
   };
-  if (gridDim.y == 1) return choose_rows<kBias>(p, token0, count, sum);
+  if (gridDim.y == 1) return choose_rows<kBias, 16>(p, token0, count, sum);
   if (arrive(p, parts, arrived + blockIdx.x, token0 - first, count, e0, 16, static_cast<int>(gridDim.y), sum))
-    choose_rows<kBias>(p, token0, count, [&](int r, int e) { return arrived_logit(p, parts, token0 - first + r, e); });
+    choose_rows<kBias, kMaxRouteExperts>(p, token0, count, [&](int r, int e) {
+      return arrived_logit(p, parts, token0 - first + r, e);
+    });
 }
 
 // 32 tokens and all experts, 32 kE at a time (kSplit: the grid's 32 kE); wave (g, part) has 32 of those, all
@@ -433,14 +441,12 @@ __global__ __launch_bounds__(kThreads, 2) void route_many_kernel(const RouteArgs
     }
   }
   __syncthreads();
-  choose_rows<kBias>(p, token0, count, [&](int r, int e) {
+  choose_rows<kBias, kE == 4 ? kMaxManyExperts : 32 * kE>(p, token0, count, [&](int r, int e) {
     return kSplit ? arrived_logit(p, parts, token0 + r, e) : logits[r * pitch + e];
   });
 }
 
-// Experts past which a block's logits do not fit beside the stages (512: 158 of 160 KB), and tokens in a
-// launch of the other kernel: what the state's counters and a modest workspace hold.
-constexpr int kMaxManyExperts = 512;
+// Tokens in a launch of the other kernel: what the state's counters and a modest workspace hold.
 constexpr int kMaxFewTokens = 8192;
 static_assert(kMaxFewTokens / 16 <= static_cast<int>(kWorkspaceStateBytes / 4), "a counter a block");
 
