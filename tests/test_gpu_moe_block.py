@@ -203,3 +203,40 @@ def test_the_command_runs(capsys):
     assert moe_block.main([]) == 0
     lines = [json.loads(s) for s in capsys.readouterr().out.splitlines() if s.startswith("{")]
     assert [s["sequences"] for s in lines] == [1, 64] and all(s["us"] > 0 for s in lines)
+
+
+def test_workspaces_of_the_calls_own_in_a_graph():
+    """Calls without a workspace inside a capture: made and cleared there, on every replay."""
+    from paper_2609_22106_amd import prq
+    block, _ = _block(11, E=300)
+    y, residual = _inputs(40, 256, 4)
+
+    def step(r):
+        h, _ = prq.prq_block_norm(y, r, block.norm_weight)
+        ids, weights = prq.prq_moe_route(h, block.router, block.k)
+        return prq.prq_moe_layer(h, ids, weights, block.gate_up, block.down, k_tail=block.k_tail)
+    want = step(residual.clone()).clone()
+    torch.cuda.synchronize()
+    live = residual.clone()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = step(live)
+    for _ in range(4):
+        live.copy_(residual)
+        graph.replay()
+        assert torch.equal(step(residual.clone()), want)           # eager work between the replays
+        torch.cuda.synchronize()
+        assert torch.equal(got, want)
+
+
+@pytest.mark.parametrize("M", [0, 1])
+def test_no_token_and_one(M):
+    block, layer = _block(12, max_rows=4)
+    y, residual = _inputs(M, 256, 5)
+    r0 = residual.clone()
+    out = block(y, residual)
+    assert out.shape == (M, 256)
+    if M:
+        _check(block, layer, y, r0, residual, out)
+    with pytest.raises(ValueError):
+        block(*_inputs(5, 256, 6))                                 # more rows than the block has room for
